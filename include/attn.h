@@ -311,6 +311,108 @@ int attn_gemm(const void* a, const void* b, void* c, int M, int N, int K, int fl
 int attn_gemm_plan(const attn_device_desc* desc, int M, int N, int K, int flags, char* buf,
                    int buflen);
 
+/*
+ * The gradients of attn_fwd_ex (of attn_fwd: Hq = Hkv = H).  With S = q k^T,
+ * P = exp(scale S - lse) over the allowed pairs and d_o the gradient of o,
+ *     dv = P^T d_o,  dS = P o (d_o v^T - delta),  delta_i = sum_c d_o_ic o_ic - dlse_i,
+ *     dq = scale dS k,  dk = scale dS^T q,
+ * dk and dv summed over the query heads of a key/value head.
+ *   q, k, v, scale, causal, dims: as the forward call got them.
+ *   o, lse: its results; o fp32, or bf16 with ATTN_O_BF16.
+ *   d_o: bf16 [B][Hq][Sq][d].
+ *   dlse: NULL, or fp32 [B][Hq][Sq]: the gradient of lse, where a caller uses it
+ *   (merging partial attention results).
+ *   dq: [B][Hq][Sq][d], dk, dv: [B][Hkv][Skv][d], fp32, or bf16 with ATTN_OUT_BF16;
+ *   fully overwritten; they must not overlap each other or the inputs.
+ *   workspace: NULL (the library's per-stream workspace, which grows as described
+ *   under attn_decode, also under stream capture), or a 16-byte aligned device
+ *   buffer of at least attn_bwd_workspace_bytes(...) bytes that the caller keeps
+ *   alive until the stream has passed this call; calls that share it must be ordered
+ *   on one stream.  With a caller workspace the call allocates nothing.
+ * Work: seven products on bf16 MFMA with fp32 accumulation; P and dS are rounded
+ * to bf16 as operands; every call gives the same bits (no atomics).
+ * Errors as attn_fwd_ex; EINVAL also for a misaligned workspace or one smaller
+ * than needed; EUNSUPPORTED also for one head's q, k or v over 2 GiB; ENOMEM if
+ * there is no memory for the library's workspace.
+ */
+#define ATTN_O_BF16 4          /* attn_bwd flag: o is bf16 */
+int attn_bwd(const void* q, const void* k, const void* v, const void* o, const float* lse,
+             const void* d_o, const float* dlse, void* dq, void* dk, void* dv, int B, int Hq,
+             int Hkv, int Sq, int Skv, int d, float scale, int causal, int flags, void* workspace,
+             size_t workspace_bytes);
+
+/* Bytes of workspace attn_bwd needs for this problem (needs the device), or a
+ * negative ATTN_E* code. */
+long long attn_bwd_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Skv, int d, int causal);
+
+/*
+ * Rows of d values of a 4-dimensional tensor: head h of token s of batch b starts at
+ * element b * batch_stride + s * row_stride + h * head_stride of ptr.  ptr is 16-byte
+ * aligned, and the strides (not negative) are multiples of 8 elements.  An input's may
+ * be 0 (broadcast); the rows of an output must not overlap.
+ */
+typedef struct attn_heads {
+    void* ptr;
+    long long batch_stride, row_stride, head_stride;
+} attn_heads;
+
+/*
+ * What a projection passes through before attention: every query and key head is
+ * normalised by its root mean square and rotated by its position, and values are moved
+ * along.  For a row x of d values at position p, with w its weight:
+ *     y = w x / sqrt(mean(x^2) + eps)
+ *     (a, b) -> (a cos t - b sin t, b cos t + a sin t),  t = p * inv_freq[i],
+ * for the pairs (y_i, y_{i+rot/2}), i < rot/2, or with ATTN_ROPE_INTERLEAVED
+ * (y_2i, y_{2i+1}); the values from rot on are not rotated.
+ *   q, k, v: bf16 projections, Hq, Hkv and Hkv heads (parts of one fused projection, or
+ *   tensors of their own); v may be NULL, and then v_out too.
+ *   q_out, k_out, v_out: bf16 results, of any layout: contiguous [B][H][S][d] for
+ *   attn_fwd, or rows of a longer cache.  They must not overlap the inputs or each other.
+ *   q_weight, k_weight: [d], bf16, or fp32 with ATTN_WEIGHT_F32; 16-byte aligned.
+ *   inv_freq: fp32 [rot / 2].
+ *   positions: NULL (row s is at position s), or int32, with ATTN_POSITIONS_I64 int64,
+ *   the position of token s of batch b at b * positions_batch_stride + s.  Any value is
+ *   taken; the angle is exact to 1e-7 turns up to |p| = 2^24 and to 1e-5 up to 2^31.
+ * Supported: d in {64, 128}, rot a multiple of 16 up to d, dims >= 1, eps >= 0.
+ * All arithmetic is fp32 (angles fp64), rounded once.  Asynchronous on the thread's
+ * stream; uses no workspace.
+ * Errors: EINVAL for null or misaligned pointers, bad strides or overlapping output
+ * rows, dims <= 0, unknown flags or eps; EUNSUPPORTED for d or rot.
+ */
+#define ATTN_ROPE_INTERLEAVED 8
+#define ATTN_WEIGHT_F32 16
+#define ATTN_POSITIONS_I64 32
+int attn_qk_norm_rope(const attn_heads* q, const attn_heads* k, const attn_heads* v,
+                      const attn_heads* q_out, const attn_heads* k_out, const attn_heads* v_out,
+                      const void* q_weight, const void* k_weight, const float* inv_freq,
+                      const void* positions, long long positions_batch_stride, int B, int S,
+                      int Hq, int Hkv, int d, int rot, float eps, int flags);
+
+/*
+ * Its gradients.
+ *   dq, dk, dv: those of the results, bf16, or fp32 with ATTN_GRAD_F32; dv may be
+ *   NULL, and then dv_out too.
+ *   q, k: the forward call's inputs (as are the weights, positions and dims).
+ *   dq_out, dk_out, dv_out: bf16, the gradients of the projections.  They must not
+ *   overlap the inputs or each other.
+ *   dq_weight, dk_weight: fp32 [d], the gradients of the weights, both or (both NULL)
+ *   neither.
+ *   workspace: with weight gradients, as for attn_bwd
+ *   (attn_qk_norm_rope_bwd_workspace_bytes(...) bytes); otherwise not used.
+ * The weight gradients are summed in a fixed order: every call gives the same bits.
+ * Errors as attn_qk_norm_rope, and for the workspace as attn_bwd.
+ */
+#define ATTN_GRAD_F32 64
+int attn_qk_norm_rope_bwd(const attn_heads* dq, const attn_heads* dk, const attn_heads* dv,
+                          const attn_heads* q, const attn_heads* k, const attn_heads* dq_out,
+                          const attn_heads* dk_out, const attn_heads* dv_out,
+                          const void* q_weight, const void* k_weight, const float* inv_freq,
+                          const void* positions, long long positions_batch_stride,
+                          float* dq_weight, float* dk_weight, int B, int S, int Hq, int Hkv,
+                          int d, int rot, float eps, int flags, void* workspace,
+                          size_t workspace_bytes);
+long long attn_qk_norm_rope_bwd_workspace_bytes(int B, int S, int Hq, int Hkv, int d);
+
 #ifdef __cplusplus
 }
 #endif

@@ -9,9 +9,12 @@ device.
 
     o = attn_fwd(q, k, v, scale=None, causal=False)  # q [B,H,Sq,d], k/v [B,H,Skv,d] bf16
     o = attn_decode(q, k, v, n_splits=0)             # q [B,H,d], k/v [B,H,Skv,d] bf16
+    dq, dk, dv = attn_bwd(do, q, k, v, o, lse)       # the gradients of attn_fwd
+    q, k, v = qk_norm_rope(q, k, v, wq, wk, freq)    # [B,S,H,d] projections to [B,H,S,d]
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -28,12 +31,19 @@ KIND_FWD = 0
 KIND_DECODE = 1
 ATTN_OUT_BF16 = 1
 ATTN_GEMM_B_NK = 2
+ATTN_O_BF16 = 4
+ATTN_ROPE_INTERLEAVED = 8
+ATTN_WEIGHT_F32 = 16
+ATTN_POSITIONS_I64 = 32
+ATTN_GRAD_F32 = 64
 
 # Entry points declared in include/attn.h.
 EXPORTED = ("attn_fwd", "attn_decode", "attn_fwd_ex", "attn_decode_ex",
             "attn_decode_workspace_bytes", "attn_set_stream", "attn_get_stream",
             "attn_last_error", "attn_query_device", "attn_measure_device", "attn_get_plan",
-            "attn_get_plan_for", "attn_get_plan_ex", "attn_gemm", "attn_gemm_plan", "attn_decode_noalloc")
+            "attn_get_plan_for", "attn_get_plan_ex", "attn_gemm", "attn_gemm_plan", "attn_decode_noalloc",
+            "attn_bwd", "attn_bwd_workspace_bytes", "attn_qk_norm_rope",
+            "attn_qk_norm_rope_bwd", "attn_qk_norm_rope_bwd_workspace_bytes")
 NOALLOC_SCRATCH_BYTES = 16 << 20  # ATTN_NOALLOC_SCRATCH_BYTES
 
 
@@ -41,6 +51,12 @@ class AttnError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"attn error {code}: {msg}")
         self.code = code
+
+
+class Heads(ctypes.Structure):
+    """attn_heads: rows of d values by batch, token and head, strides in elements."""
+    _fields_ = [("ptr", ctypes.c_void_p), ("batch_stride", ctypes.c_longlong),
+                ("row_stride", ctypes.c_longlong), ("head_stride", ctypes.c_longlong)]
 
 
 class DeviceDesc(ctypes.Structure):
@@ -115,7 +131,17 @@ def _load() -> ctypes.CDLL:
                                    ci]
     lib.attn__gemm_candidates.argtypes = [ctypes.POINTER(DeviceDesc), ci, ci, ci, ci, ci,
                                           ctypes.c_char_p, ci]
-    for fn in (lib.attn_fwd, lib.attn_decode, lib.attn_fwd_ex, lib.attn_decode_ex,
+    lib.attn_bwd.argtypes = [vp] * 10 + [ci] * 6 + [cf, ci, ci, vp, ctypes.c_size_t]
+    lib.attn_bwd_workspace_bytes.argtypes = [ci] * 7
+    lib.attn_bwd_workspace_bytes.restype = ctypes.c_longlong
+    hp, ll = ctypes.POINTER(Heads), ctypes.c_longlong
+    lib.attn_qk_norm_rope.argtypes = [hp] * 6 + [vp] * 4 + [ll] + [ci] * 6 + [cf, ci]
+    lib.attn_qk_norm_rope_bwd.argtypes = [hp] * 8 + [vp] * 4 + [ll, vp, vp] + [ci] * 6 + \
+        [cf, ci, vp, ctypes.c_size_t]
+    lib.attn_qk_norm_rope_bwd_workspace_bytes.argtypes = [ci] * 5
+    lib.attn_qk_norm_rope_bwd_workspace_bytes.restype = ctypes.c_longlong
+    for fn in (lib.attn_bwd, lib.attn_qk_norm_rope, lib.attn_qk_norm_rope_bwd,
+               lib.attn_fwd, lib.attn_decode, lib.attn_fwd_ex, lib.attn_decode_ex,
                lib.attn_decode_noalloc,
                lib.attn_set_stream, lib.attn_query_device,
                lib.attn_measure_device, lib.attn_get_plan, lib.attn_get_plan_for,
@@ -279,6 +305,230 @@ def gemm(a, b, c=None, b_nk: bool = False, out_dtype=None):
     _set_stream(a)
     _check(lib.attn_gemm(a.data_ptr(), b.data_ptr(), c.data_ptr(), M, N, K, flags))
     return c
+
+
+def _device_of(tensors):
+    """The one device of these tensors (None among them is skipped), as a context in
+    which it is the current device."""
+    import torch
+    index = None
+    for t in tensors:
+        if t is None:
+            continue
+        if index is None:
+            index = t.get_device()
+        elif t.get_device() != index:
+            raise ValueError("all tensors must be on one device")
+    return contextlib.nullcontext() if torch.cuda.current_device() == index else \
+        torch.cuda.device(index)
+
+
+def _workspace(workspace):
+    """Address and bytes of a caller's workspace (None: the library's)."""
+    import torch
+    if workspace is None:
+        return None, 0
+    if not isinstance(workspace, torch.Tensor) or not workspace.is_cuda or \
+            not workspace.is_contiguous():
+        raise TypeError("workspace must be a contiguous tensor on a HIP device")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def attn_bwd(do, q, k, v, o, lse, scale: float | None = None, causal: bool = False, dlse=None,
+             dq=None, dk=None, dv=None, out_dtype=None, workspace=None):
+    """Gradients of attn_fwd; returns (dq, dk, dv), bf16 (or out_dtype fp32).
+
+    q, k, v, scale, causal: as attn_fwd got them; o (fp32 or bf16) and lse: what it
+    returned (return_lse=True).  do: the gradient of o, bf16 [B,Hq,Sq,d]; dlse: that of
+    lse, fp32 [B,Hq,Sq], or None.  workspace: None (the library's), or a device tensor of
+    at least bwd_workspace_bytes(...) bytes."""
+    import torch
+    B, Hq, Sq, d = q.shape
+    Hkv, Skv = k.shape[1], k.shape[2]
+    bf16, f32 = torch.bfloat16, torch.float32
+    _require(q, bf16, (B, Hq, Sq, d), "q")
+    _require(k, bf16, (B, Hkv, Skv, d), "k")
+    _require(v, bf16, (B, Hkv, Skv, d), "v")
+    _require(do, bf16, (B, Hq, Sq, d), "do")
+    _require(o, bf16 if getattr(o, "dtype", None) is bf16 else f32, (B, Hq, Sq, d), "o")
+    _require(lse, f32, (B, Hq, Sq), "lse")
+    if dlse is not None:
+        _require(dlse, f32, (B, Hq, Sq), "dlse")
+    given = [t for t in (dq, dk, dv) if t is not None]
+    if out_dtype is None:
+        out_dtype = given[0].dtype if given else bf16
+    if out_dtype not in (f32, bf16):
+        raise ValueError("out_dtype must be torch.float32 or torch.bfloat16")
+    outs = []
+    for t, like, name in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")):
+        if t is None:
+            t = torch.empty(like.shape, dtype=out_dtype, device=q.device)
+        else:
+            _require(t, out_dtype, like.shape, name)
+        outs.append(t)
+    ws_ptr, ws_bytes = _workspace(workspace)
+    if scale is None:
+        scale = 1.0 / math.sqrt(d)
+    flags = (ATTN_OUT_BF16 if out_dtype == bf16 else 0) | (ATTN_O_BF16 if o.dtype == bf16 else 0)
+    with _device_of((q, k, v, do, o, lse, dlse, *outs, workspace)):
+        _set_stream(q)
+        _check(lib.attn_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
+                            lse.data_ptr(), do.data_ptr(),
+                            dlse.data_ptr() if dlse is not None else None,
+                            *[t.data_ptr() for t in outs], B, Hq, Hkv, Sq, Skv, d, float(scale),
+                            int(bool(causal)), flags, ws_ptr, ws_bytes))
+    return tuple(outs)
+
+
+def bwd_workspace_bytes(B: int, Hq: int, Hkv: int, Sq: int, Skv: int, d: int,
+                        causal: bool = False) -> int:
+    """Bytes of workspace attn_bwd needs with a caller-provided buffer."""
+    n = lib.attn_bwd_workspace_bytes(B, Hq, Hkv, Sq, Skv, d, int(bool(causal)))
+    if n < 0:
+        raise AttnError(int(n), last_error())
+    return int(n)
+
+
+def _rows(t, dtype, shape, dims, name):
+    """attn_heads of a 4-dimensional tensor whose batch, token and head dimensions are
+    dims, its last one contiguous (None for None)."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or not t.is_cuda:
+        raise TypeError(f"{name} must be a {dtype} tensor on a HIP device")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    strides = t.stride()
+    if strides[3] != 1:
+        raise ValueError(f"{name} must be contiguous in its last dimension")
+    # (a dimension of one element has any stride)
+    return Heads(t.data_ptr(), *[strides[i] if shape[i] > 1 else 0 for i in dims])
+
+
+def _rope_common(q, k, q_weight, k_weight, inv_freq, positions, interleaved):
+    """Dimensions, checked small operands and flags of the two rotation calls."""
+    import torch
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q and k must be [B,S,H,d]")
+    B, S, Hq, d = q.shape
+    Hkv = k.shape[2]
+    wdtype = torch.float32 if getattr(q_weight, "dtype", None) is torch.float32 else torch.bfloat16
+    _require(q_weight, wdtype, (d,), "q_weight")
+    _require(k_weight, wdtype, (d,), "k_weight")
+    if not isinstance(inv_freq, torch.Tensor) or inv_freq.dim() != 1:
+        raise TypeError("inv_freq must be a one-dimensional tensor")
+    _require(inv_freq, torch.float32, (inv_freq.shape[0],), "inv_freq")
+    flags = (ATTN_ROPE_INTERLEAVED if interleaved else 0) | \
+        (ATTN_WEIGHT_F32 if wdtype is torch.float32 else 0)
+    pos_ptr, pos_stride = None, 0
+    if positions is not None:
+        if not isinstance(positions, torch.Tensor) or not positions.is_cuda or \
+                positions.dtype not in (torch.int32, torch.int64):
+            raise TypeError("positions must be an int32 or int64 tensor on a HIP device")
+        if positions.shape not in ((S,), (B, S)):
+            raise ValueError(f"positions has shape {tuple(positions.shape)}, expected "
+                             f"{(S,)} or {(B, S)}")
+        if S > 1 and positions.stride(-1) != 1:
+            raise ValueError("positions must be contiguous in its last dimension")
+        if positions.dim() == 2 and B > 1:
+            pos_stride = positions.stride(0)
+        pos_ptr = positions.data_ptr()
+        flags |= ATTN_POSITIONS_I64 if positions.dtype is torch.int64 else 0
+    return (B, S, Hq, Hkv, d), 2 * inv_freq.shape[0], pos_ptr, pos_stride, flags
+
+
+def _ref(heads):
+    return None if heads is None else ctypes.byref(heads)
+
+
+def qk_norm_rope(q, k, v, q_weight, k_weight, inv_freq, positions=None, eps: float = 1e-6,
+                 interleaved: bool = False, q_out=None, k_out=None, v_out=None):
+    """RMS norm of every query and key head and rotation by position, from token-major
+    projections to what attn_fwd and attn_decode read; returns (q, k, v), bf16 [B,H,S,d].
+
+    q: bf16 [B,S,Hq,d], k, v: bf16 [B,S,Hkv,d], any strides with contiguous rows (views
+    of one fused projection); v may be None (None is returned for it).  q_weight, k_weight:
+    [d], bf16 or fp32.  inv_freq: fp32 [rot/2]; pair i is (i, i + rot/2), or interleaved
+    (2i, 2i+1), and turns by position * inv_freq[i].  positions: int32 or int64 [S] or
+    [B,S]; None: 0..S-1.  q_out, k_out, v_out: [B,H,S,d], any strides with contiguous rows
+    (for a step of decoding, the cache's rows: k_out=cache[:, :, pos:pos + S])."""
+    import torch
+    (B, S, Hq, Hkv, d), rot, pos_ptr, pos_stride, flags = _rope_common(
+        q, k, q_weight, k_weight, inv_freq, positions, interleaved)
+    if v is None and v_out is not None:
+        raise ValueError("v_out without v")
+    ins, outs, results = [], [], []
+    for t, out, H, name in ((q, q_out, Hq, "q"), (k, k_out, Hkv, "k"), (v, v_out, Hkv, "v")):
+        if t is None:
+            ins.append(None), outs.append(None), results.append(None)
+            continue
+        ins.append(_rows(t, torch.bfloat16, (B, S, H, d), (0, 1, 2), name))
+        if out is None:
+            out = torch.empty((B, H, S, d), dtype=torch.bfloat16, device=q.device)
+        outs.append(_rows(out, torch.bfloat16, (B, H, S, d), (0, 2, 1), name + "_out"))
+        results.append(out)
+    with _device_of((q, k, v, *results, q_weight, k_weight, inv_freq, positions)):
+        _set_stream(q)
+        _check(lib.attn_qk_norm_rope(*[_ref(h) for h in ins + outs], q_weight.data_ptr(),
+                                     k_weight.data_ptr(), inv_freq.data_ptr(), pos_ptr,
+                                     pos_stride, B, S, Hq, Hkv, d, rot, float(eps), flags))
+    return tuple(results)
+
+
+def qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, inv_freq, positions=None,
+                     eps: float = 1e-6, interleaved: bool = False, dq_out=None, dk_out=None,
+                     dv_out=None, weight_grads: bool = True, workspace=None):
+    """Gradients of qk_norm_rope; returns those of q, k and v (bf16 [B,S,H,d]) and of
+    q_weight and k_weight (fp32 [d]; None without weight_grads).
+
+    dq, dk, dv: gradients of its results, bf16 or fp32 [B,H,S,d] (dv may be None); the
+    rest as qk_norm_rope got it.  dq_out, dk_out, dv_out: any strides with contiguous
+    rows; without them, they are the heads of one fused [B,S,Hq+2*Hkv,d] tensor in this
+    order.  workspace: None (the library's), or a device tensor of at least
+    qk_norm_rope_bwd_workspace_bytes(...) bytes."""
+    import torch
+    (B, S, Hq, Hkv, d), rot, pos_ptr, pos_stride, flags = _rope_common(
+        q, k, q_weight, k_weight, inv_freq, positions, interleaved)
+    if dv is None and dv_out is not None:
+        raise ValueError("dv_out without dv")
+    gdtype = torch.float32 if getattr(dq, "dtype", None) is torch.float32 else torch.bfloat16
+    flags |= ATTN_GRAD_F32 if gdtype is torch.float32 else 0
+    xs = [_rows(q, torch.bfloat16, (B, S, Hq, d), (0, 1, 2), "q"),
+          _rows(k, torch.bfloat16, (B, S, Hkv, d), (0, 1, 2), "k")]
+    if dq_out is None or dk_out is None or (dv_out is None and dv is not None):
+        fused = torch.empty((B, S, Hq + 2 * Hkv, d), dtype=torch.bfloat16, device=q.device)
+        parts = fused.split((Hq, Hkv, Hkv), dim=2)
+    ins, outs, results = [], [], []
+    for i, (g, out, H, name) in enumerate(((dq, dq_out, Hq, "dq"), (dk, dk_out, Hkv, "dk"),
+                                           (dv, dv_out, Hkv, "dv"))):
+        if g is None and name == "dv":
+            ins.append(None), outs.append(None), results.append(None)
+            continue
+        ins.append(_rows(g, gdtype, (B, H, S, d), (0, 2, 1), name))
+        if out is None:
+            out = parts[i]
+        outs.append(_rows(out, torch.bfloat16, (B, S, H, d), (0, 1, 2), name + "_out"))
+        results.append(out)
+    dw = torch.empty((2, d), dtype=torch.float32, device=q.device) if weight_grads else None
+    dqw, dkw = (dw[0], dw[1]) if weight_grads else (None, None)
+    ws_ptr, ws_bytes = _workspace(workspace)
+    with _device_of((dq, dk, dv, q, k, *results, q_weight, k_weight, inv_freq, positions,
+                     workspace)):
+        _set_stream(q)
+        _check(lib.attn_qk_norm_rope_bwd(*[_ref(h) for h in ins + xs + outs],
+                                         q_weight.data_ptr(), k_weight.data_ptr(),
+                                         inv_freq.data_ptr(), pos_ptr, pos_stride,
+                                         dqw.data_ptr() if weight_grads else None,
+                                         dkw.data_ptr() if weight_grads else None, B, S, Hq, Hkv,
+                                         d, rot, float(eps), flags, ws_ptr, ws_bytes))
+    return (*results, dqw, dkw)
+
+
+def qk_norm_rope_bwd_workspace_bytes(B: int, S: int, Hq: int, Hkv: int, d: int) -> int:
+    """Bytes of workspace qk_norm_rope_bwd needs with a caller-provided buffer."""
+    n = lib.attn_qk_norm_rope_bwd_workspace_bytes(B, S, Hq, Hkv, d)
+    if n < 0:
+        raise AttnError(int(n), last_error())
+    return int(n)
 
 
 def gemm_plan(M: int, N: int, K: int, b_nk: bool = False, desc: DeviceDesc | None = None) -> str:

@@ -9,6 +9,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <exception>
 #include <map>
 #include <memory>
 #include <mutex>
@@ -358,6 +359,27 @@ int validate_common(const void* q, const void* k, const void* v, const void* o, 
                     Skv, d);
     if (d != 64 && d != 128) return fail(ATTN_EUNSUPPORTED, "head dim %d not in {64, 128}", d);
     return ATTN_OK;
+}
+
+// The workspace of a call: the caller's, checked, or the stream's.
+int call_workspace(DeviceState* st, size_t need, void* workspace, size_t workspace_bytes,
+                   std::unique_lock<std::mutex>* lk, void** out) {
+    if (!workspace) return stream_workspace(st, need, lk, out);
+    if (!aligned16(workspace)) return fail(ATTN_EINVAL, "workspace must be 16-byte aligned");
+    if (workspace_bytes < need)
+        return fail(ATTN_EINVAL, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+    *out = workspace;
+    return ATTN_OK;
+}
+
+// No C++ exception leaves a C entry.
+template <typename F>
+auto guarded(F&& f) -> decltype(f()) {
+    try {
+        return f();
+    } catch (const std::exception& e) {
+        return fail(ATTN_ENOMEM, "host: %s", e.what());
+    }
 }
 
 }  // namespace
@@ -958,6 +980,283 @@ int attn_gemm(const void* a, const void* b, void* c, int M, int N, int K, int fl
                                      st->desc.num_xcds, static_cast<float*>(ws), t_stream);
     if (e != hipSuccess) return fail_hip(e, "GEMM launch");
     return ATTN_OK;
+}
+
+// ------------------------------------------------- backward, norm and rotation --
+static int validate_bwd_dims(int B, int Hq, int Hkv, int Sq, int Skv, int d, int causal) {
+    if (B <= 0 || Hq <= 0 || Sq <= 0 || Skv <= 0 || d <= 0)
+        return fail(ATTN_EINVAL, "dimensions must be positive (B=%d Hq=%d Sq=%d Skv=%d d=%d)", B,
+                    Hq, Sq, Skv, d);
+    if (Hkv <= 0 || Hq % Hkv != 0)
+        return fail(ATTN_EINVAL, "Hkv (%d) must be positive and divide Hq (%d)", Hkv, Hq);
+    if (d != 64 && d != 128) return fail(ATTN_EUNSUPPORTED, "head dim %d not in {64, 128}", d);
+    if (causal && Sq > Skv)
+        return fail(ATTN_EUNSUPPORTED, "causal attention needs Sq <= Skv (Sq=%d Skv=%d)", Sq, Skv);
+    const long long longest = Sq > Skv ? Sq : Skv;
+    if (longest * d * 2 > 0x7fffffffLL)
+        return fail(ATTN_EUNSUPPORTED, "one head's q, k or v (%lld bytes) exceeds 2 GiB",
+                    longest * d * 2);
+    return ATTN_OK;
+}
+
+static int bwd_plan_of(DeviceState* st, int B, int Hq, int Hkv, int Sq, int Skv, int d,
+                       int causal, BwdPlan* plan, size_t* ws_bytes) {
+    if (!plan_bwd(st->desc.num_cus, B, Hq, Hkv, Sq, Skv, d, causal ? 1 : 0, plan))
+        return fail(ATTN_EUNSUPPORTED, "no feasible backward plan for this shape");
+    *ws_bytes = (size_t)(bwd_rows_floats(B, Hq, Sq) +
+                         bwd_part_floats(*plan, B, Hq, Hkv, Sq, Skv, d)) * sizeof(float);
+    return ATTN_OK;
+}
+
+long long attn_bwd_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Skv, int d, int causal) {
+    return guarded([&]() -> long long {
+        int rc = validate_bwd_dims(B, Hq, Hkv, Sq, Skv, d, causal);
+        if (rc) return rc;
+        DeviceState* st = nullptr;
+        rc = device_state(&st);
+        if (rc) return rc;
+        BwdPlan plan;
+        size_t bytes = 0;
+        rc = bwd_plan_of(st, B, Hq, Hkv, Sq, Skv, d, causal, &plan, &bytes);
+        return rc ? rc : (long long)bytes;
+    });
+}
+
+int attn_bwd(const void* q, const void* k, const void* v, const void* o, const float* lse,
+             const void* d_o, const float* dlse, void* dq, void* dk, void* dv, int B, int Hq,
+             int Hkv, int Sq, int Skv, int d, float scale, int causal, int flags, void* workspace,
+             size_t workspace_bytes) {
+    return guarded([&]() -> int {
+        const void* const tensors[] = {q, k, v, o, d_o, dq, dk, dv};
+        for (const void* t : tensors) {
+            if (!t) return fail(ATTN_EINVAL, "null tensor pointer");
+            if (!aligned16(t))
+                return fail(ATTN_EINVAL, "tensor pointers must be 16-byte aligned");
+        }
+        if (!lse || ((uintptr_t)lse & 3u) || ((uintptr_t)dlse & 3u))
+            return fail(ATTN_EINVAL, "lse must not be null, lse and dlse 4-byte aligned");
+        int rc = validate_bwd_dims(B, Hq, Hkv, Sq, Skv, d, causal);
+        if (rc) return rc;
+        if (flags & ~(ATTN_OUT_BF16 | ATTN_O_BF16))
+            return fail(ATTN_EINVAL, "unknown flags 0x%x", flags);
+        if (!isfinite(scale)) return fail(ATTN_EINVAL, "scale must be finite");
+        DeviceState* st = nullptr;
+        rc = device_state(&st);
+        if (rc) return rc;
+        BwdPlan plan;
+        size_t need = 0;
+        rc = bwd_plan_of(st, B, Hq, Hkv, Sq, Skv, d, causal, &plan, &need);
+        if (rc) return rc;
+        void* ws = nullptr;
+        std::unique_lock<std::mutex> ws_lock;  // held until the kernels are enqueued
+        rc = call_workspace(st, need, workspace, workspace_bytes, &ws_lock, &ws);
+        if (rc) return rc;
+        BwdArgs a{};
+        a.q = static_cast<const uint16_t*>(q);
+        a.k = static_cast<const uint16_t*>(k);
+        a.v = static_cast<const uint16_t*>(v);
+        a.o = o;
+        a.lse = lse;
+        a.d_o = static_cast<const uint16_t*>(d_o);
+        a.dlse = dlse;
+        a.rows = static_cast<float*>(ws);
+        a.Sq = Sq;
+        a.Skv = Skv;
+        a.group = Hq / Hkv;
+        a.q_heads = (long long)B * Hq;
+        a.kv_heads = (long long)B * Hkv;
+        a.num_xcds = st->desc.num_xcds;
+        a.scale = scale;
+        a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+        const hipError_t e =
+            launch_bwd(plan, a, d, causal ? 1 : 0, (flags & ATTN_O_BF16) ? 1 : 0,
+                       (flags & ATTN_OUT_BF16) ? 1 : 0, dq, dk, dv,
+                       a.rows + bwd_rows_floats(B, Hq, Sq), t_stream);
+        return e == hipSuccess ? ATTN_OK : fail_hip(e, "backward launch");
+    });
+}
+
+static int validate_rope_dims(int B, int S, int Hq, int Hkv, int d) {
+    if (B <= 0 || S <= 0 || Hq <= 0 || Hkv <= 0 || d <= 0)
+        return fail(ATTN_EINVAL, "dimensions must be positive (B=%d S=%d Hq=%d Hkv=%d d=%d)", B,
+                    S, Hq, Hkv, d);
+    if (d != 64 && d != 128) return fail(ATTN_EUNSUPPORTED, "head dim %d not in {64, 128}", d);
+    return ATTN_OK;
+}
+
+// One tensor of rows.  written: its rows must not overlap.
+static int validate_heads(const attn_heads* h, const char* name, int B, int S, int H, int d,
+                          bool written) {
+    if (!h || !h->ptr) return fail(ATTN_EINVAL, "%s: null tensor pointer", name);
+    if (!aligned16(h->ptr)) return fail(ATTN_EINVAL, "%s must be 16-byte aligned", name);
+    std::pair<long long, int> dims[3] = {
+        {h->batch_stride, B}, {h->row_stride, S}, {h->head_stride, H}};
+    for (const auto& x : dims)
+        if (x.first < 0 || x.first % 8 != 0 || (x.first > 0 && x.second > (1LL << 60) / x.first))
+            return fail(ATTN_EINVAL, "%s: stride %lld is not a non-negative multiple of 8", name,
+                        x.first);
+    if (!written) return ATTN_OK;
+    std::sort(dims, dims + 3);
+    long long span = d;
+    for (const auto& x : dims) {
+        if (x.second == 1) continue;
+        if (x.first < span) return fail(ATTN_EINVAL, "%s: rows overlap", name);
+        span += x.first * (x.second - 1);
+    }
+    return ATTN_OK;
+}
+
+static int validate_rope(const void* q_weight, const void* k_weight, const float* inv_freq,
+                         const void* positions, long long positions_batch_stride, int rot, int d,
+                         float eps, int flags, int known) {
+    if (!q_weight || !k_weight || !inv_freq) return fail(ATTN_EINVAL, "null weight or inv_freq");
+    if (!aligned16(q_weight) || !aligned16(k_weight))
+        return fail(ATTN_EINVAL, "weights must be 16-byte aligned");
+    if (flags & ~known) return fail(ATTN_EINVAL, "unknown flags 0x%x", flags);
+    if (((uintptr_t)inv_freq & 3u) ||
+        ((uintptr_t)positions & ((flags & ATTN_POSITIONS_I64) ? 7u : 3u)))
+        return fail(ATTN_EINVAL, "inv_freq or positions misaligned");
+    if (positions_batch_stride < 0) return fail(ATTN_EINVAL, "negative positions stride");
+    if (!(eps >= 0.f) || !isfinite(eps))
+        return fail(ATTN_EINVAL, "eps must be finite and not negative");
+    if (rot < 16 || rot > d || rot % 16 != 0)
+        return fail(ATTN_EUNSUPPORTED, "rot (%d) must be a multiple of 16 up to %d", rot, d);
+    return ATTN_OK;
+}
+
+static RopeArgs rope_args(const void* q_weight, const void* k_weight, const float* inv_freq,
+                          const void* positions, long long positions_batch_stride, int B, int S,
+                          int Hq, int Hkv, int rot, float eps, int flags) {
+    RopeArgs a{};
+    a.weight[0] = q_weight;
+    a.weight[1] = k_weight;
+    a.inv_freq = inv_freq;
+    a.positions = positions;
+    a.positions_batch_stride = positions_batch_stride;
+    a.tokens = (long long)B * S;
+    a.S = S;
+    a.Hq = Hq;
+    a.Hkv = Hkv;
+    a.rot = rot;
+    a.interleaved = (flags & ATTN_ROPE_INTERLEAVED) ? 1 : 0;
+    a.weight_f32 = (flags & ATTN_WEIGHT_F32) ? 1 : 0;
+    a.positions_i64 = (flags & ATTN_POSITIONS_I64) ? 1 : 0;
+    a.eps = eps;
+    return a;
+}
+
+int attn_qk_norm_rope(const attn_heads* q, const attn_heads* k, const attn_heads* v,
+                      const attn_heads* q_out, const attn_heads* k_out, const attn_heads* v_out,
+                      const void* q_weight, const void* k_weight, const float* inv_freq,
+                      const void* positions, long long positions_batch_stride, int B, int S,
+                      int Hq, int Hkv, int d, int rot, float eps, int flags) {
+    return guarded([&]() -> int {
+        int rc = validate_rope_dims(B, S, Hq, Hkv, d);
+        if (!rc) rc = validate_heads(q, "q", B, S, Hq, d, false);
+        if (!rc) rc = validate_heads(k, "k", B, S, Hkv, d, false);
+        if (!rc) rc = validate_heads(q_out, "q_out", B, S, Hq, d, true);
+        if (!rc) rc = validate_heads(k_out, "k_out", B, S, Hkv, d, true);
+        if (!rc && !v != !v_out) rc = fail(ATTN_EINVAL, "v and v_out go together");
+        if (!rc && v) rc = validate_heads(v, "v", B, S, Hkv, d, false);
+        if (!rc && v) rc = validate_heads(v_out, "v_out", B, S, Hkv, d, true);
+        if (!rc)
+            rc = validate_rope(q_weight, k_weight, inv_freq, positions, positions_batch_stride,
+                               rot, d, eps, flags,
+                               ATTN_ROPE_INTERLEAVED | ATTN_WEIGHT_F32 | ATTN_POSITIONS_I64);
+        if (rc) return rc;
+        DeviceState* st = nullptr;
+        rc = device_state(&st);
+        if (rc) return rc;
+        RopeArgs a = rope_args(q_weight, k_weight, inv_freq, positions, positions_batch_stride, B,
+                               S, Hq, Hkv, rot, eps, flags);
+        a.in[0] = *q;
+        a.in[1] = *k;
+        a.out[0] = *q_out;
+        a.out[1] = *k_out;
+        if (v) {
+            a.in[2] = *v;
+            a.out[2] = *v_out;
+        }
+        const RopeLaunch l = rope_launch(a.tokens, Hq, Hkv, d, st->desc.num_cus, false);
+        a.tile_log2 = l.tile_log2;
+        const hipError_t e = launch_rope(a, l, d, t_stream);
+        return e == hipSuccess ? ATTN_OK : fail_hip(e, "norm and rotation launch");
+    });
+}
+
+static size_t rope_bwd_bytes(const RopeLaunch& l, int d) {
+    return (size_t)l.grid_x * l.grid_y * 2 * d * sizeof(float);
+}
+
+long long attn_qk_norm_rope_bwd_workspace_bytes(int B, int S, int Hq, int Hkv, int d) {
+    return guarded([&]() -> long long {
+        int rc = validate_rope_dims(B, S, Hq, Hkv, d);
+        if (rc) return rc;
+        DeviceState* st = nullptr;
+        rc = device_state(&st);
+        if (rc) return rc;
+        return (long long)rope_bwd_bytes(
+            rope_launch((long long)B * S, Hq, Hkv, d, st->desc.num_cus, true), d);
+    });
+}
+
+int attn_qk_norm_rope_bwd(const attn_heads* dq, const attn_heads* dk, const attn_heads* dv,
+                          const attn_heads* q, const attn_heads* k, const attn_heads* dq_out,
+                          const attn_heads* dk_out, const attn_heads* dv_out,
+                          const void* q_weight, const void* k_weight, const float* inv_freq,
+                          const void* positions, long long positions_batch_stride,
+                          float* dq_weight, float* dk_weight, int B, int S, int Hq, int Hkv,
+                          int d, int rot, float eps, int flags, void* workspace,
+                          size_t workspace_bytes) {
+    return guarded([&]() -> int {
+        int rc = validate_rope_dims(B, S, Hq, Hkv, d);
+        if (!rc) rc = validate_heads(dq, "dq", B, S, Hq, d, false);
+        if (!rc) rc = validate_heads(dk, "dk", B, S, Hkv, d, false);
+        if (!rc) rc = validate_heads(q, "q", B, S, Hq, d, false);
+        if (!rc) rc = validate_heads(k, "k", B, S, Hkv, d, false);
+        if (!rc) rc = validate_heads(dq_out, "dq_out", B, S, Hq, d, true);
+        if (!rc) rc = validate_heads(dk_out, "dk_out", B, S, Hkv, d, true);
+        if (!rc && !dv != !dv_out) rc = fail(ATTN_EINVAL, "dv and dv_out go together");
+        if (!rc && dv) rc = validate_heads(dv, "dv", B, S, Hkv, d, false);
+        if (!rc && dv) rc = validate_heads(dv_out, "dv_out", B, S, Hkv, d, true);
+        if (!rc)
+            rc = validate_rope(q_weight, k_weight, inv_freq, positions, positions_batch_stride,
+                               rot, d, eps, flags,
+                               ATTN_ROPE_INTERLEAVED | ATTN_WEIGHT_F32 | ATTN_POSITIONS_I64 |
+                                   ATTN_GRAD_F32);
+        if (!rc && (!dq_weight != !dk_weight || ((uintptr_t)dq_weight & 3u) ||
+                    ((uintptr_t)dk_weight & 3u)))
+            rc = fail(ATTN_EINVAL, "weight gradients go together, 4-byte aligned");
+        if (rc) return rc;
+        DeviceState* st = nullptr;
+        rc = device_state(&st);
+        if (rc) return rc;
+        RopeArgs a = rope_args(q_weight, k_weight, inv_freq, positions, positions_batch_stride, B,
+                               S, Hq, Hkv, rot, eps, flags);
+        a.in[0] = *dq;
+        a.in[1] = *dk;
+        a.x[0] = *q;
+        a.x[1] = *k;
+        a.out[0] = *dq_out;
+        a.out[1] = *dk_out;
+        if (dv) {
+            a.in[2] = *dv;
+            a.out[2] = *dv_out;
+        }
+        const RopeLaunch l = rope_launch(a.tokens, Hq, Hkv, d, st->desc.num_cus, true);
+        a.tile_log2 = l.tile_log2;
+        void* ws = nullptr;
+        std::unique_lock<std::mutex> ws_lock;  // held until the kernels are enqueued
+        if (dq_weight) {
+            rc = call_workspace(st, rope_bwd_bytes(l, d), workspace, workspace_bytes, &ws_lock,
+                                &ws);
+            if (rc) return rc;
+        }
+        a.ws = static_cast<float*>(ws);
+        const hipError_t e = launch_rope_bwd(a, l, d, (flags & ATTN_GRAD_F32) ? 1 : 0, dq_weight,
+                                             dk_weight, t_stream);
+        return e == hipSuccess ? ATTN_OK : fail_hip(e, "norm and rotation backward launch");
+    });
 }
 
 }  // extern "C"

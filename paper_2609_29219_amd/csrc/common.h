@@ -282,6 +282,68 @@ hipError_t launch_decode(const DecodePlan& p, const void* q, const void* k, cons
 // and the reduction of the partials follows on the same stream.
 hipError_t launch_gemm(const GemmPlan& p, const void* a, const void* b, void* c, int M, int N,
                        int K, int out_bf16, int num_xcds, float* workspace, hipStream_t stream);
+// ------------------------------------------------------- attention backward --
+// Work split of one backward call: blocks of keys (dK, dV) and of queries (dQ) to a
+// head, and over how many workgroups each block's sum is split.
+struct BwdPlan {
+    int kv_blocks = 0, kv_splits = 1;
+    int q_blocks = 0, q_splits = 1;
+};
+struct BwdArgs {
+    const uint16_t* q;    // bf16 [B][Hq][Sq][D]
+    const uint16_t* k;    // bf16 [B][Hkv][Skv][D]
+    const uint16_t* v;
+    const void* o;        // [B][Hq][Sq][D], fp32 or bf16
+    const float* lse;     // [B][Hq][Sq]
+    const uint16_t* d_o;  // bf16, as o
+    const float* dlse;    // as lse, or null
+    float* rows;          // 64 floats for every 32 query rows (-lse log2 e, -delta)
+    int Sq, Skv, group;
+    long long q_heads, kv_heads;  // over the batch
+    int num_xcds;
+    float scale, scale_log2;      // of either sign, or 0; times log2 e
+    // of the kernel that runs: blocks to a head, splits of each, and its results (fp32
+    // partials part_stride values apart where split)
+    int blocks, splits, out_bf16;
+    long long part_stride;
+    void *out0, *out1;
+};
+// False where a grid would have too many workgroups.
+bool plan_bwd(int num_cus, int B, int Hq, int Hkv, int Sq, int Skv, int d, int causal,
+              BwdPlan* out);
+// Workspace in floats: the row values, then the larger of the two kernels' partials.
+long long bwd_rows_floats(int B, int Hq, int Sq);
+long long bwd_part_floats(const BwdPlan& p, int B, int Hq, int Hkv, int Sq, int Skv, int d);
+hipError_t launch_bwd(const BwdPlan& p, const BwdArgs& a, int d, int causal, int o_bf16,
+                      int out_bf16, void* dq, void* dk, void* dv, float* part,
+                      hipStream_t stream);
+
+// -------------------------------------------------- per-head norm, rotation --
+constexpr int kRopeMaxTile = 16;  // tokens to a tile at most
+// Index 0: queries, 1: keys, 2: values (no norm, no rotation; ptr may be null).
+struct RopeArgs {
+    attn_heads in[3];   // forward: projections; backward: gradients of the results
+    attn_heads x[2];    // backward: the projections
+    attn_heads out[3];
+    const void* weight[2];
+    const float* inv_freq;
+    const void* positions;  // or null: the row's index
+    long long positions_batch_stride;
+    long long tokens;       // B * S
+    int S, Hq, Hkv, rot;
+    int interleaved, weight_f32, positions_i64;
+    int tile_log2;
+    float eps;
+    float* ws;              // backward: weight gradients, [workgroup][2][d], or null
+};
+struct RopeLaunch {
+    int tile_log2 = 0, grid_x = 0, grid_y = 1;
+};
+RopeLaunch rope_launch(long long tokens, int Hq, int Hkv, int d, int num_cus, bool backward);
+hipError_t launch_rope(const RopeArgs& a, const RopeLaunch& l, int d, hipStream_t stream);
+hipError_t launch_rope_bwd(const RopeArgs& a, const RopeLaunch& l, int d, int grad_f32,
+                           float* dq_weight, float* dk_weight, hipStream_t stream);
+
 // Query heads of one key/value group that a decode workgroup serves together.
 int decode_heads_per_wg(int group);
 

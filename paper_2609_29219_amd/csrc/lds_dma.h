@@ -68,6 +68,22 @@ __device__ __forceinline__ void lds_dma16(dma_rsrc_t rsrc, uint32_t lds_base, in
         : "s"(lds_base), "v"(voffset), "s"(rsrc), "s"(soffset)
         : "memory", "m0");
 }
+
+// The same for 4 bytes a lane: lane i loads the word at byte voffset into lds_base + 4*i.
+__device__ __forceinline__ void lds_dma4(dma_rsrc_t rsrc, uint32_t lds_base, int voffset) {
+    rsrc[0] = __builtin_amdgcn_readfirstlane(rsrc[0]);
+    rsrc[1] = __builtin_amdgcn_readfirstlane(rsrc[1]);
+    rsrc[2] = __builtin_amdgcn_readfirstlane(rsrc[2]);
+    rsrc[3] = __builtin_amdgcn_readfirstlane(rsrc[3]);
+    lds_base = __builtin_amdgcn_readfirstlane(lds_base);
+    asm volatile(
+        "s_mov_b32 m0, %0\n\t"
+        "s_nop 0\n\t"
+        "buffer_load_dword %1, %2, 0 offen lds"
+        :
+        : "s"(lds_base), "v"(voffset), "s"(rsrc)
+        : "memory", "m0");
+}
 #pragma clang diagnostic pop
 
 // Wait until at most N of this wave's vector-memory loads are outstanding

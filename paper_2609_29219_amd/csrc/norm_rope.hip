@@ -1,0 +1,353 @@
+// Per-head RMS norm of queries and keys with the position rotation, forward and
+// backward, moving token-major projections [B][S][H][d] (any strides) to and from the
+// head-major tensors [B][H][S][d] that attention reads; values are moved along.
+//
+// Forward, for a row x of d values at position p:
+//     r = 1 / sqrt(mean(x^2) + eps),  y = w x r,
+//     (a, b) -> (a cos t - b sin t, b cos t + a sin t),  t = p inv_freq[i],
+// for each of the rot / 2 pairs of y: (i, i + rot/2), or (2i, 2i + 1) interleaved.
+// Backward, for the gradient g of the rotated row: g' = g turned by -t, then
+//     dw = sum over rows of g' x r,   dx = r (g' w - x r mean(g' w x r)).
+//
+// Bound: HBM.  A row is read and written once, 16 bytes to a lane; everything else is a
+// fraction of that time.  A workgroup takes a tile of tokens and walks all rows of
+// some heads of it, so the angles of a token are evaluated once for all of its heads
+// (into LDS, as cos and sin): in double precision up to the fraction of a turn, since a
+// float product is off by 0.01 rad at position 2^17.  Lane order: the tokens of one head
+// are neighbours, so the head-major side is contiguous over the whole tile.
+// All arithmetic is fp32 with one rounding at the end.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "common.h"
+
+namespace attn {
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kRopeThreads = 256;
+
+__device__ __forceinline__ float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
+
+__device__ __forceinline__ void load8(const uint16_t* p, float (&x)[8]) {
+    const u32x4 u = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[2 * e] = bf16_lo(u[e]);
+        x[2 * e + 1] = bf16_hi(u[e]);
+    }
+}
+
+__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+    const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[e] = a[e];
+        x[4 + e] = b[e];
+    }
+}
+
+__device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8]) {
+    bf16x8 y;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = (__bf16)x[e];  // round to nearest even
+    *reinterpret_cast<bf16x8*>(p) = y;
+}
+
+// 8 weights of a lane's columns
+__device__ __forceinline__ void load_weight(const void* w, int w_f32, int col, float (&x)[8]) {
+    if (w_f32)
+        load8(static_cast<const float*>(w) + col, x);
+    else
+        load8(static_cast<const uint16_t*>(w) + col, x);
+}
+
+// Sum over the L lanes (8 or 16, aligned) that hold one row; every lane gets it.
+template <int L>
+__device__ __forceinline__ float row_sum(float x) {
+    x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0xB1, 0xF, 0xF, false));
+    x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x4E, 0xF, 0xF, false));
+    x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x141, 0xF, 0xF, false));
+    if constexpr (L == 16)
+        x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x140, 0xF, 0xF, false));
+    return x;
+}
+
+// The tokens of a tile: where their rows start, and cos and sin of their angles.
+template <int D>
+struct RopeLds {
+    float cs[2][kRopeMaxTile * (D / 2)];  // [token][pair]
+    int b[kRopeMaxTile], s[kRopeMaxTile];
+};
+
+template <int D>
+__device__ __forceinline__ void load_tile(RopeLds<D>& lds, const RopeArgs& a, long long token0,
+                                          int tile) {
+    const int half = a.rot / 2;
+    for (int t = threadIdx.x; t < tile; t += kRopeThreads) {
+        const long long token = token0 + t < a.tokens ? token0 + t : a.tokens - 1;
+        const int b = (int)(token / a.S);
+        lds.b[t] = b;
+        lds.s[t] = (int)(token - (long long)b * a.S);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < tile * half; i += kRopeThreads) {
+        const int t = i / half, pair = i - t * half;
+        double pos = lds.s[t];
+        if (a.positions) {
+            const long long at = lds.b[t] * a.positions_batch_stride + lds.s[t];
+            pos = a.positions_i64 ? (double)static_cast<const long long*>(a.positions)[at]
+                                  : (double)static_cast<const int*>(a.positions)[at];
+        }
+        // in turns, and of those only the fraction
+        double turn = pos * (double)a.inv_freq[pair] * 0.15915494309189533577;
+        turn -= rint(turn);
+        float sn, cn;
+        sincospif(2.0f * (float)turn, &sn, &cn);
+        lds.cs[0][i] = cn;
+        lds.cs[1][i] = sn;
+    }
+    __syncthreads();
+}
+
+// Turns the lane's 8 columns by the token's angles (sign -1: back).  lane_col: the
+// lane's index in its row; every lane of the wave takes part.
+template <int D>
+__device__ __forceinline__ void rotate8(float (&y)[8], const RopeLds<D>& lds, int t, int lane_col,
+                                        int rot, int interleaved, float sign) {
+    const int half = rot / 2;
+    const bool in = lane_col * 8 < rot;
+    if (interleaved) {
+        const int i0 = t * half + (in ? lane_col * 4 : 0);
+        const f32x4 cn = *reinterpret_cast<const f32x4*>(&lds.cs[0][i0]);
+        const f32x4 sn = *reinterpret_cast<const f32x4*>(&lds.cs[1][i0]) * sign;
+        if (in) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float p = y[2 * e], q = y[2 * e + 1];
+                y[2 * e] = p * cn[e] - q * sn[e];
+                y[2 * e + 1] = q * cn[e] + p * sn[e];
+            }
+        }
+        return;
+    }
+    // the other half of each pair sits half / 8 lanes away
+    const bool second = lane_col * 8 >= half;
+    const int lane = threadIdx.x & 63;
+    const int mate = in ? (second ? lane - half / 8 : lane + half / 8) : lane;
+    const int i0 = t * half + (in ? lane_col * 8 - (second ? half : 0) : 0);
+    float cn[8], sn[8];
+    load8(&lds.cs[0][i0], cn);
+    load8(&lds.cs[1][i0], sn);
+    const float sg = second ? sign : -sign;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float other =
+            __int_as_float(__builtin_amdgcn_ds_bpermute(mate * 4, __float_as_int(y[e])));
+        const float turned = y[e] * cn[e] + other * (sg * sn[e]);
+        y[e] = in ? turned : y[e];
+    }
+}
+
+__device__ __forceinline__ long long row_offset(const attn_heads& h, int b, int s, int head) {
+    return b * h.batch_stride + s * h.row_stride + head * h.head_stride;
+}
+
+// Rows of a tile: row r is token r % tile of head r / tile (tile a power of two), a
+// group of D / 8 lanes to a row.  Workgroup (x, y): tile x, every gridDim.y-th pass.
+template <int D>
+__global__ __launch_bounds__(kRopeThreads) void rope_fwd_kernel(const RopeArgs a) {
+    constexpr int L = D / 8, RPP = kRopeThreads / L;  // lanes to a row, rows to a pass
+    __shared__ RopeLds<D> lds;
+    const int tile = 1 << a.tile_log2;
+    const long long token0 = (long long)blockIdx.x << a.tile_log2;
+    load_tile<D>(lds, a, token0, tile);
+    const int lc = threadIdx.x % L, group = threadIdx.x / L;
+    const int first = blockIdx.y * RPP + group, step = gridDim.y * RPP;
+    auto rows = [&](int which, int heads) __attribute__((always_inline)) {
+        const attn_heads in = a.in[which], out = a.out[which];
+        const uint16_t* src = static_cast<const uint16_t*>(in.ptr) + lc * 8;
+        uint16_t* dst = static_cast<uint16_t*>(out.ptr) + lc * 8;
+        float w[8];
+        if (which < 2) load_weight(a.weight[which], a.weight_f32, lc * 8, w);
+        const int n = heads << a.tile_log2;
+        for (int r0 = first - group; r0 < n; r0 += step) {  // whole waves go round together
+            const int r = r0 + group < n ? r0 + group : n - 1;
+            const int t = r & (tile - 1), head = r >> a.tile_log2;
+            const bool live = r0 + group < n && token0 + t < a.tokens;
+            const uint16_t* p = src + row_offset(in, lds.b[t], lds.s[t], head);
+            uint16_t* q = dst + row_offset(out, lds.b[t], lds.s[t], head);
+            if (which == 2) {
+                const u32x4 u = *reinterpret_cast<const u32x4*>(p);
+                if (live) *reinterpret_cast<u32x4*>(q) = u;
+                continue;
+            }
+            float x[8];
+            load8(p, x);
+            float ss = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
+            ss = row_sum<L>(ss);
+            const float rs = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = x[e] * rs * w[e];
+            rotate8<D>(x, lds, t, lc, a.rot, a.interleaved, 1.0f);
+            if (live) store8(q, x);
+        }
+    };
+    rows(0, a.Hq);
+    rows(1, a.Hkv);
+    if (a.in[2].ptr) rows(2, a.Hkv);
+}
+
+// in: the gradients of the outputs (bf16, or fp32 with G32); x: the forward pass's
+// inputs; out: their gradients.  Workgroups walk the tiles in steps of the grid; each
+// leaves the sums of its rows' weight gradients in ws[workgroup][q, k][D], which
+// rope_weight_kernel adds up in a fixed order.
+template <int D, bool G32>
+__global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(const RopeArgs a) {
+    constexpr int L = D / 8, RPP = kRopeThreads / L;
+    typedef typename std::conditional<G32, float, uint16_t>::type grad_t;
+    __shared__ RopeLds<D> lds;
+    __shared__ float sums[RPP][D];
+    const int tile = 1 << a.tile_log2;
+    const int lc = threadIdx.x % L, group = threadIdx.x / L;
+    const int first = blockIdx.y * RPP, step = gridDim.y * RPP;
+    const long long tiles = (a.tokens + tile - 1) >> a.tile_log2;
+    float dw[2][8] = {};
+    for (long long tl = blockIdx.x; tl < tiles; tl += gridDim.x) {
+        const long long token0 = tl << a.tile_log2;
+        if (tl != blockIdx.x) __syncthreads();  // the last tile's angles are still read
+        load_tile<D>(lds, a, token0, tile);
+        auto rows = [&](auto which_tag, int heads) __attribute__((always_inline)) {
+            constexpr int which = decltype(which_tag)::value;
+            const attn_heads in = a.in[which], out = a.out[which], xin = a.x[which];
+            const grad_t* src = static_cast<const grad_t*>(in.ptr) + lc * 8;
+            const uint16_t* xs = static_cast<const uint16_t*>(xin.ptr) + lc * 8;
+            uint16_t* dst = static_cast<uint16_t*>(out.ptr) + lc * 8;
+            float w[8];
+            if (which < 2) load_weight(a.weight[which], a.weight_f32, lc * 8, w);
+            const int n = heads << a.tile_log2;
+            for (int r0 = first; r0 < n; r0 += step) {
+                const int r = r0 + group < n ? r0 + group : n - 1;
+                const int t = r & (tile - 1), head = r >> a.tile_log2;
+                const bool live = r0 + group < n && token0 + t < a.tokens;
+                float g[8], x[8];
+                load8(src + row_offset(in, lds.b[t], lds.s[t], head), g);
+                uint16_t* q = dst + row_offset(out, lds.b[t], lds.s[t], head);
+                if constexpr (which == 2) {
+                    if (live) store8(q, g);
+                } else {
+                    load8(xs + row_offset(xin, lds.b[t], lds.s[t], head), x);
+                    rotate8<D>(g, lds, t, lc, a.rot, a.interleaved, -1.0f);
+                    float ss = 0.f, sg = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        ss = fmaf(x[e], x[e], ss);
+                        sg = fmaf(g[e] * w[e], x[e], sg);
+                    }
+                    ss = row_sum<L>(ss);
+                    sg = row_sum<L>(sg);
+                    const float rs = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
+                    const float mean = sg * rs * (1.0f / D);  // mean(g' w x r)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float xn = x[e] * rs;
+                        if (live) dw[which][e] = fmaf(g[e], xn, dw[which][e]);
+                        g[e] = rs * (g[e] * w[e] - xn * mean);
+                    }
+                    if (live) store8(q, g);
+                }
+            }
+        };
+        rows(std::integral_constant<int, 0>{}, a.Hq);
+        rows(std::integral_constant<int, 1>{}, a.Hkv);
+        if (a.in[2].ptr) rows(std::integral_constant<int, 2>{}, a.Hkv);
+    }
+    if (!a.ws) return;
+    float* ws = a.ws + ((long long)blockIdx.y * gridDim.x + blockIdx.x) * 2 * D;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sums[group][lc * 8 + e] = dw[which][e];
+        __syncthreads();
+        for (int c = threadIdx.x; c < D; c += kRopeThreads) {
+            float s = 0.f;
+            for (int g = 0; g < RPP; ++g) s += sums[g][c];
+            ws[which * D + c] = s;
+        }
+    }
+}
+
+// dw[c] = sum over n workgroups, in a fixed order and in double precision (long sums of
+// either sign).  Block (x, y): 16 columns of weight y, 64 rows at a time.
+__global__ __launch_bounds__(1024) void rope_weight_kernel(const float* ws, int n, int D,
+                                                           float* dqw, float* dkw) {
+    __shared__ double part[64][16];
+    float* dw = blockIdx.y ? dkw : dqw;
+    const int c = threadIdx.x % 16, row = threadIdx.x / 16;
+    const float* p = ws + (long long)blockIdx.y * D + blockIdx.x * 16 + c;
+    double s = 0.0;
+    for (int i = row; i < n; i += 64) s += (double)p[(long long)i * 2 * D];
+    part[row][c] = s;
+    __syncthreads();
+    for (int m = 32; m > 0; m /= 2) {
+        if (row < m) part[row][c] += part[row + m][c];
+        __syncthreads();
+    }
+    if (row == 0 && dw) dw[blockIdx.x * 16 + c] = (float)part[0][c];
+}
+
+}  // namespace
+
+RopeLaunch rope_launch(long long tokens, int Hq, int Hkv, int d, int num_cus, bool backward) {
+    const int rpp = kRopeThreads / (d / 8);
+    RopeLaunch l;
+    // up to 16 tokens to a tile, fewer where that leaves compute units without a tile
+    while (l.tile_log2 < 4 && (tokens >> (l.tile_log2 + 1)) >= 2 * num_cus) ++l.tile_log2;
+    const long long tiles = (tokens + (1 << l.tile_log2) - 1) >> l.tile_log2;
+    // few tiles: their rows are shared out among workgroups
+    const long long passes = (((long long)(Hq > Hkv ? Hq : Hkv) << l.tile_log2) + rpp - 1) / rpp;
+    long long y = 1;
+    while (y < passes && tiles * y < 2 * num_cus) ++y;
+    l.grid_y = (int)y;
+    const long long cap = backward ? 4LL * num_cus : 0x7fffffffLL;
+    l.grid_x = (int)(tiles < cap ? tiles : cap);
+    return l;
+}
+
+hipError_t launch_rope(const RopeArgs& a, const RopeLaunch& l, int d, hipStream_t stream) {
+    const dim3 grid(l.grid_x, l.grid_y);
+    if (d == 64)
+        rope_fwd_kernel<64><<<grid, kRopeThreads, 0, stream>>>(a);
+    else
+        rope_fwd_kernel<128><<<grid, kRopeThreads, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_rope_bwd(const RopeArgs& a, const RopeLaunch& l, int d, int grad_f32,
+                           float* dq_weight, float* dk_weight, hipStream_t stream) {
+    const dim3 grid(l.grid_x, l.grid_y);
+    if (d == 64 && grad_f32)
+        rope_bwd_kernel<64, true><<<grid, kRopeThreads, 0, stream>>>(a);
+    else if (d == 64)
+        rope_bwd_kernel<64, false><<<grid, kRopeThreads, 0, stream>>>(a);
+    else if (grad_f32)
+        rope_bwd_kernel<128, true><<<grid, kRopeThreads, 0, stream>>>(a);
+    else
+        rope_bwd_kernel<128, false><<<grid, kRopeThreads, 0, stream>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !a.ws) return e;
+    rope_weight_kernel<<<dim3(d / 16, 2), 1024, 0, stream>>>(a.ws, l.grid_x * l.grid_y, d,
+                                                             dq_weight, dk_weight);
+    return hipGetLastError();
+}
+
+}  // namespace attn

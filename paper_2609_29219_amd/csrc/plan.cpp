@@ -1057,4 +1057,42 @@ int format_decode_plan(const DecodePlan& p, char* buf, int buflen) {
                     p.q_blocks, p.grid, p.wg_per_cu, p.modeled_us, p.bound);
 }
 
+// ------------------------------------------------------- attention backward --
+// Workgroups keep 256 keys (dK, dV) or 256 queries (dQ).  Where there are fewer of
+// them than CUs, each one's sum is split among several, as long as a split has at
+// least four tiles of 32 to walk.
+static int bwd_splits(long long workgroups, long long steps, int num_cus) {
+    long long n = num_cus / workgroups;
+    if (n > steps / 4) n = steps / 4;
+    return n < 1 ? 1 : (int)n;
+}
+
+bool plan_bwd(int num_cus, int B, int Hq, int Hkv, int Sq, int Skv, int d, int causal,
+              BwdPlan* out) {
+    (void)d;
+    (void)causal;
+    const long long n_qt = ((long long)Sq + 31) / 32, n_kt = ((long long)Skv + 31) / 32;
+    const long long kv_steps = n_qt * (Hq / Hkv);
+    BwdPlan p;
+    p.kv_blocks = (int)((n_kt + 7) / 8);
+    p.q_blocks = (int)((n_qt + 7) / 8);
+    const long long kv_wg = (long long)B * Hkv * p.kv_blocks;
+    const long long q_wg = (long long)B * Hq * p.q_blocks;
+    if (kv_steps > 0x7fffffffLL || kv_wg > 0x7fffffffLL || q_wg > 0x7fffffffLL) return false;
+    p.kv_splits = bwd_splits(kv_wg, kv_steps, num_cus);
+    p.q_splits = bwd_splits(q_wg, n_kt, num_cus);
+    *out = p;
+    return true;
+}
+
+long long bwd_rows_floats(int B, int Hq, int Sq) {
+    return (long long)B * Hq * (((long long)Sq + 31) / 32) * 64;
+}
+
+long long bwd_part_floats(const BwdPlan& p, int B, int Hq, int Hkv, int Sq, int Skv, int d) {
+    const long long kv = p.kv_splits > 1 ? 2LL * p.kv_splits * B * Hkv * Skv * d : 0;
+    const long long q = p.q_splits > 1 ? (long long)p.q_splits * B * Hq * Sq * d : 0;
+    return kv > q ? kv : q;
+}
+
 }  // namespace attn

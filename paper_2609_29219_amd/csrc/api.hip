@@ -1068,6 +1068,8 @@ int attn_bwd(const void* q, const void* k, const void* v, const void* o, const f
         a.num_xcds = st->desc.num_xcds;
         a.scale = scale;
         a.scale_log2 = (float)((double)scale * 1.4426950408889634);
+        if (fabsf(a.scale_log2) < FLT_MIN) a.scale_log2 = scale < 0.f ? -FLT_MIN : FLT_MIN;
+        a.hidden = scale < 0.f ? INFINITY : -INFINITY;
         const hipError_t e =
             launch_bwd(plan, a, d, causal ? 1 : 0, (flags & ATTN_O_BF16) ? 1 : 0,
                        (flags & ATTN_OUT_BF16) ? 1 : 0, dq, dk, dv,

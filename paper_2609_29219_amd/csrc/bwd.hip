@@ -60,60 +60,123 @@ struct TileLoad {
     static constexpr int PIECES = 32 * D * 2 / 1024;
     static constexpr int NJ = PIECES / kBwdWaves;
     static constexpr int ROWS = 512 / D;  // of one piece
-    int row[NJ], col[NJ];  // this lane's source row and byte within it
+    int off[NJ];  // this lane's source bytes within a tile
 
     __device__ __forceinline__ void init(int wave, int lane) {
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
             const int r = (wave + j * kBwdWaves) * ROWS + lane / (D / 8);
-            row[j] = r;
-            col[j] = ((lane % (D / 8)) ^ tile_swizzle<D>(r)) * 16;
+            off[j] = r * (D * 2) + ((lane % (D / 8)) ^ tile_swizzle<D>(r)) * 16;
         }
     }
     __device__ __forceinline__ void issue(dma_rsrc_t rsrc, uint32_t lds, int row0, int n_rows,
                                           int wave) const {
+        if (row0 + 32 <= n_rows) {
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const uint32_t dst = lds + (wave + j * kBwdWaves) * 1024;
-            const int r = min(row0 + row[j], n_rows - 1);
-            lds_dma16(rsrc, dst, r * (D * 2) + col[j], 0);
+            for (int j = 0; j < NJ; ++j)
+                lds_dma16(rsrc, lds + (wave + j * kBwdWaves) * 1024, off[j], row0 * (D * 2));
+        } else {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                const int r = min(row0 + off[j] / (D * 2), n_rows - 1);
+                lds_dma16(rsrc, lds + (wave + j * kBwdWaves) * 1024,
+                          r * (D * 2) + off[j] % (D * 2), 0);
+            }
         }
     }
 };
 
-// A operand by rows: lane l holds row l%32, values 16*ks + 8*(l/32) ..+7.
+// Operands of one streamed tile at LDS address `tile`.  By rows: lane l holds row l%32,
+// values 16*ks + 8*(l/32) ..+7.  Transposed: column 32*cb + l%32, rows of step t in the
+// order above.  The exchanged piece of an address is an XOR, so each kind has one
+// per-lane base and a compile-time XOR and offset for each operand.
 template <int D>
-__device__ __forceinline__ bf16x8 row_operand(const uint16_t* tile, int ks, int lane) {
-    const int row = lane & 31, c = 2 * ks + (lane >> 5);
-    return *reinterpret_cast<const bf16x8*>(tile + row * D + ((c ^ tile_swizzle<D>(row)) << 3));
-}
+struct TileRead {
+    uint32_t row, col;
 
-// A operand transposed: lane l holds column 32*cb + l%32, rows of step s in the order above.
-template <int D>
-__device__ __forceinline__ bf16x8 col_operand(const uint16_t* tile, int cb, int s, int lane) {
-    const int i = lane & 15, c = 4 * cb + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-    s16x8 x;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int row = 16 * s + 8 * j + 4 * (lane >> 5) + (i >> 2);
-        const s16x4 y =
-            lds_read_tr(tile + row * D + ((c ^ tile_swizzle<D>(row)) << 3) + 4 * (i & 1));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[4 * j + e] = y[e];
+    __device__ __forceinline__ void init(int lane) {
+        const int hh = lane >> 5, i = lane & 15, r = lane & 31;
+        row = r * (D * 2) + ((hh ^ tile_swizzle<D>(r)) << 4);
+        const int rr = 4 * hh + (i >> 2);
+        col = rr * (D * 2) + (((2 * ((lane >> 4) & 1) + ((i & 3) >> 1)) ^ tile_swizzle<D>(rr)) << 4) +
+              8 * (i & 1);
     }
-    return __builtin_bit_cast(bf16x8, x);
+    // of a tile whose bases are row + tile and col + tile
+    template <int KS>
+    static __device__ __forceinline__ bf16x8 by_row(uint32_t base, int offset) {
+        return *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)((base ^ (KS << 5)) +
+                                                                            offset);
+    }
+    template <int CB, int T>
+    static __device__ __forceinline__ bf16x8 by_col(uint32_t base, int offset) {
+        s16x8 x;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const uint32_t at =
+                (base ^ ((4 * CB ^ 2 * j) << 4)) + offset + (16 * T + 8 * j) * (D * 2);
+            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) s16x4*)(uintptr_t)at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[4 * j + e] = y[e];
+        }
+        return __builtin_bit_cast(bf16x8, x);
+    }
+};
+
+__device__ __forceinline__ f32x4 lds_quad(uint32_t at) {
+    return *(const __attribute__((address_space(3))) f32x4*)(uintptr_t)at;
 }
 
+// Two values rounded to bf16, as one register of an operand.
+__device__ __forceinline__ uint32_t round2(float a, float b) {
+    bf16x2 y;
+    y[0] = (__bf16)a;
+    y[1] = (__bf16)b;
+    return __builtin_bit_cast(uint32_t, y);
+}
+
+// A value that is formed at this place and not sunk to where it is used, in a later block.
+template <typename T>
+__device__ __forceinline__ void here(T& x) {
+    asm volatile("" : "+v"(x));
+}
+
+// The loop bodies are written slot by slot (an operand, its products, a share of the
+// other work); nothing moves from one slot to another.
+__device__ __forceinline__ void slot_end() { __builtin_amdgcn_sched_barrier(0); }
+
+constexpr int kRing = 4;  // operands in registers: read three slots ahead
+
+// The gradients' accumulators fill the accumulation registers, and the scores must stay
+// out of them: the VALU cannot read those, and the compiler, left to itself, puts every
+// product's result there and moves accumulators out and back in on every tile (192 moves
+// in the dK/dV kernel).  So the scores' products are written out, with plain registers.
+// The compiler does not see the waits that they need, which the assembly therefore
+// holds itself: two wait states before each (a VALU result read by it), and settle(),
+// twenty, between the last product of a block and its first other use.  (A product that
+// adds to the one before needs none.)
 __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
-
-// Registers 8s..8s+7 of a score block, rounded to bf16: a product's operand of step s.
-__device__ __forceinline__ bf16x8 round8(const f32x16& x, int s) {
-    bf16x8 y;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = (__bf16)x[8 * s + e];
-    return y;
+__device__ __forceinline__ void score_first(f32x16& d, bf16x8 a, bf16x8 b) {
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0"
+                 : "=&v"(d) : "v"(a), "v"(b));
+}
+__device__ __forceinline__ void score_from(f32x16& d, bf16x8 a, bf16x8 b, const f32x16& c) {
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %3"
+                 : "=&v"(d) : "v"(a), "v"(b), "v"(c));
+}
+__device__ __forceinline__ void score_add(f32x16& d, bf16x8 a, bf16x8 b) {
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0"
+                 : "+v"(d) : "v"(a), "v"(b));
+}
+template <int N>
+__device__ __forceinline__ void settle(f32x16 (&d)[N]) {
+    static_assert(N == 1 || N == 2, "");
+    if constexpr (N == 2)
+        asm volatile("s_nop 15\n\ts_nop 3" : "+v"(d[0]), "+v"(d[1]));
+    else
+        asm volatile("s_nop 15\n\ts_nop 3" : "+v"(d[0]));
 }
 
 // Row of accumulator register r in lane half hh.
@@ -240,6 +303,8 @@ __global__ __launch_bounds__(kBwdThreads, 1) void bwd_dkdv_kernel(const BwdArgs 
 
     TileLoad<D> load;
     load.init(wave, lane);
+    TileRead<D> read;
+    read.init(lane);
     const uint32_t lds0 = lds_address(lds), rows0 = lds_address(rows);
     const uint32_t slab = (uint32_t)a.Sq * D * 2;
     auto issue = [&](int step, int slot) __attribute__((always_inline)) {
@@ -253,70 +318,159 @@ __global__ __launch_bounds__(kBwdThreads, 1) void bwd_dkdv_kernel(const BwdArgs 
             lds_dma4(make_dma_rsrc(a.rows + (head * n_qt + qt) * 64, 256), rows0 + slot * 256,
                      lane * 4);
     };
-    if (begin < end) issue(begin, 0);
+
+    // Operand i of a tile, in the order of use: Q by rows (S), dO by rows (dP), dO
+    // transposed (dV), Q transposed (dK); KD of each.
+    constexpr int OPS = 4 * KD;
+    bf16x8 ring[kRing];
+    uint32_t row_base, col_base, nl_base;  // of the tile that is read
+    auto tile_bases = [&](int slot) __attribute__((always_inline)) {
+        row_base = read.row + lds0 + slot * (2 * TILE * 2);
+        col_base = read.col + lds0 + slot * (2 * TILE * 2);
+        nl_base = rows0 + slot * 256 + 16 * hh;
+        // opaque, so that the XORed addresses are formed where they are used instead of
+        // being kept in registers over the whole loop
+        asm volatile("" : "+v"(row_base), "+v"(col_base), "+v"(nl_base));
+    };
+    auto fetch = [&](auto i_tag) __attribute__((always_inline)) {
+        constexpr int i = decltype(i_tag)::value, ph = i / KD, j = i % KD;
+        if constexpr (ph == 0) ring[i % kRing] = TileRead<D>::template by_row<j>(row_base, 0);
+        if constexpr (ph == 1)
+            ring[i % kRing] = TileRead<D>::template by_row<j>(row_base, TILE * 2);
+        if constexpr (ph == 2)
+            ring[i % kRing] = TileRead<D>::template by_col<j % CB, j / CB>(col_base, TILE * 2);
+        if constexpr (ph == 3)
+            ring[i % kRing] = TileRead<D>::template by_col<j % CB, j / CB>(col_base, 0);
+    };
+    struct Scores {
+        f32x16 s[KB], dp[KB];  // S, then P; dP - delta, then dS
+        f32x4 nl[2];           // -lse log2 e of eight rows
+        uint32_t pk[KB][8];    // P as operand
+    };
+    uint32_t dsk[KB][8];  // dS as operand
+    auto product = [&](auto i_tag, auto kb_tag, Scores& x_) __attribute__((always_inline)) {
+        f32x16(&s)[KB] = x_.s;
+        f32x16(&dp)[KB] = x_.dp;
+        uint32_t(&pk)[KB][8] = x_.pk;
+        constexpr int i = decltype(i_tag)::value, kb = decltype(kb_tag)::value;
+        constexpr int ph = i / KD, j = i % KD, t = j / CB, cb = j % CB;
+        const bf16x8 x = ring[i % kRing];
+        if constexpr (ph == 0 && j == 0) score_first(s[kb], x, kf[kb][j]);
+        if constexpr (ph == 0 && j > 0) score_add(s[kb], x, kf[kb][j]);
+        if constexpr (ph == 1) score_add(dp[kb], x, vf[kb][j]);
+        if constexpr (ph >= 2) {
+            const uint32_t* o = ph == 2 ? pk[kb] : dsk[kb];
+            const u32x4 y = {o[4 * t], o[4 * t + 1], o[4 * t + 2], o[4 * t + 3]};
+            f32x16& acc = ph == 2 ? dv[kb][cb] : dk[kb][cb];
+            acc = mfma(x, __builtin_bit_cast(bf16x8, y), acc);
+        }
+    };
+    // The weights (two values of each block) follow S during the products of dP and of the
+    // first half of dV; dS during those of dV.
+    auto weight = [&](auto r_tag, Scores& x_) __attribute__((always_inline)) {
+        f32x16(&s)[KB] = x_.s;
+        f32x4(&nl)[2] = x_.nl;
+        uint32_t(&pk)[KB][8] = x_.pk;
+        constexpr int r = decltype(r_tag)::value;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            s[kb][r] =
+                __builtin_amdgcn_exp2f(fmaf(s[kb][r], a.scale_log2, nl[(r / 4) % 2][r % 4]));
+            if constexpr (r % 2 == 1) pk[kb][r / 2] = round2(s[kb][r - 1], s[kb][r]);
+        }
+        if constexpr (r % 4 == 3 && r + 5 < 16) nl[(r / 4) % 2] = lds_quad(nl_base + 8 * (r + 5));
+    };
+    // Scores of hidden pairs: their weights come out as exactly 0.
+    auto hide = [&](int q0, Scores& x_) __attribute__((always_inline)) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            const int lim = wk0 + kb * 32 + l32 - q0 - diag - 4 * hh;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x_.s[kb][r] = acc_row(r, 0) >= lim ? x_.s[kb][r] : a.hidden;
+        }
+    };
+    auto grad = [&](auto r_tag, Scores& x_) __attribute__((always_inline)) {
+        f32x16(&s)[KB] = x_.s;
+        f32x16(&dp)[KB] = x_.dp;
+        constexpr int r = decltype(r_tag)::value;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            dp[kb][r] *= s[kb][r];
+            if constexpr (r % 2 == 1) dsk[kb][r / 2] = round2(dp[kb][r - 1], dp[kb][r]);
+        }
+    };
+    // -delta, from which the products of dP start
+    auto start_dp = [&](auto r4_tag, Scores& x_) __attribute__((always_inline)) {
+        f32x16(&dp)[KB] = x_.dp;
+        constexpr int r4 = decltype(r4_tag)::value;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            const f32x4 x = lds_quad(nl_base + 128 + 32 * r4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) dp[kb][4 * r4 + e] = x[e];
+        }
+    };
+    constexpr int TAIL = OPS - (kRing - 1);  // the last slots, behind the barrier
+    auto body = [&](int q0) __attribute__((always_inline)) {
+        Scores x;
+        static_for<0, TAIL>([&](auto i_tag) __attribute__((always_inline)) {
+            constexpr int i = decltype(i_tag)::value, ph = i / KD, j = i % KD;
+            fetch(std::integral_constant<int, i + kRing - 1>{});
+            if constexpr (ph == 0 && j >= KD - 4) 
+                start_dp(std::integral_constant<int, j - (KD - 4)>{}, x);
+            if constexpr (ph == 0 && j == KD - 1) {
+                x.nl[0] = lds_quad(nl_base);
+                x.nl[1] = lds_quad(nl_base + 32);
+            }
+            static_for<0, KB>([&](auto kb_tag) __attribute__((always_inline)) {
+                product(i_tag, kb_tag, x);
+                // 12 of the 16 rows' weights in the gaps of dP (but for the first slot's,
+                // when S settles), 4 in the first half of dV's; dS in dV's
+                constexpr int n = KB * KD, gap = j * KB + decltype(kb_tag)::value;
+                auto w = [&](auto r) __attribute__((always_inline)) {
+                    weight(r, x);
+                };
+                if constexpr (ph == 1 && j > 0)
+                    static_for<(gap - KB) * 12 / (n - KB), (gap - KB + 1) * 12 / (n - KB)>(w);
+                if constexpr (ph == 2 && gap < n / 2)
+                    static_for<12 + gap * 4 / (n / 2), 12 + (gap + 1) * 4 / (n / 2)>(w);
+                if constexpr (ph == 2 && j > 0)
+                    static_for<(gap - KB) * 16 / (n - KB), (gap - KB + 1) * 16 / (n - KB)>(
+                        [&](auto r) __attribute__((always_inline)) { grad(r, x); });
+            });
+            if constexpr (ph == 1 && j == 0) {
+                settle(x.s);
+                if (CAUSAL && q0 + diag < wk0 + 32 * KB - 1) hide(q0, x);
+            }
+            if constexpr (ph == 2 && j == 0) settle(x.dp);
+            slot_end();
+        });
+    };
+
+    if (begin < end) {
+        issue(begin, 0);
+        if (begin + 1 < end) issue(begin + 1, 1);
+        publish_barrier<0>();
+        tile_bases(0);
+        static_for<0, kRing - 1>(fetch);
+    }
     for (int step = begin; step < end; ++step) {
         const int slot = (step - begin) & 1;
+        // (a wave whose keys are all hidden computes zeros: it would only wait)
+        body(CAUSAL ? (qt0 + step % per_q) * 32 : 0);
+        // Every operand of this tile has been read: its slot is free behind the barrier,
+        // which also publishes the next tile.
         publish_barrier<0>();
-        if (step + 1 < end) issue(step + 1, slot ^ 1);
-        const int qt = qt0 + step % per_q;
-        const int q0 = qt * 32;
-        if (CAUSAL && q0 + 31 + diag < wk0) continue;  // above the wave's diagonal
-        const uint16_t* qs = lds + slot * (2 * TILE);
-        const uint16_t* gs = qs + TILE;
-        const float* rs = rows[slot];
-        f32x16 s[KB] = {}, dp[KB];
-#pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4) {  // dP - delta: the products start from -delta
-            const f32x4 x = *reinterpret_cast<const f32x4*>(rs + 32 + 8 * r4 + 4 * hh);
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) dp[kb][4 * r4 + e] = x[e];
-        }
-#pragma unroll
-        for (int ks = 0; ks < KD; ++ks) {
-            const bf16x8 x = row_operand<D>(qs, ks, lane);
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb) s[kb] = mfma(x, kf[kb][ks], s[kb]);
-        }
-#pragma unroll
-        for (int ks = 0; ks < KD; ++ks) {
-            const bf16x8 x = row_operand<D>(gs, ks, lane);
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb) dp[kb] = mfma(x, vf[kb][ks], dp[kb]);
-        }
-        const bool masked = CAUSAL && q0 + diag < wk0 + 32 * KB - 1;
-#pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4) {
-            const f32x4 nl = *reinterpret_cast<const f32x4*>(rs + 8 * r4 + 4 * hh);
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int r = 4 * r4 + e;
-                    float p = __builtin_amdgcn_exp2f(fmaf(s[kb][r], a.scale_log2, nl[e]));
-                    if (masked)
-                        p = wk0 + kb * 32 + l32 <= q0 + acc_row(r, hh) + diag ? p : 0.f;
-                    s[kb][r] = p;
-                    dp[kb][r] *= p;
-                }
-        }
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int cb = 0; cb < CB; ++cb) {
-                const bf16x8 x = col_operand<D>(gs, cb, t, lane);
-#pragma unroll
-                for (int kb = 0; kb < KB; ++kb) dv[kb][cb] = mfma(x, round8(s[kb], t), dv[kb][cb]);
-            }
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int cb = 0; cb < CB; ++cb) {
-                const bf16x8 x = col_operand<D>(qs, cb, t, lane);
-#pragma unroll
-                for (int kb = 0; kb < KB; ++kb) dk[kb][cb] = mfma(x, round8(dp[kb], t), dk[kb][cb]);
-            }
+        if (step + 2 < end) issue(step + 2, slot);
+        tile_bases(slot ^ 1);
+        Scores none;  // (dK's products read dsk alone)
+        static_for<TAIL, OPS>([&](auto i_tag) __attribute__((always_inline)) {
+            constexpr int i = decltype(i_tag)::value;
+            static_for<0, KB>(
+                [&](auto kb_tag) __attribute__((always_inline)) { product(i_tag, kb_tag, none); });
+            fetch(std::integral_constant<int, i + kRing - 1 - OPS>{});
+            slot_end();
+        });
     }
 
 #pragma unroll
@@ -338,7 +492,8 @@ template <int D, int QB, bool CAUSAL>
 __global__ __launch_bounds__(kBwdThreads, 1) void bwd_dq_kernel(const BwdArgs a) {
     constexpr int KD = D / 16, CB = D / 32, TILE = 32 * D;
     constexpr int BQ = kBwdWaves * 32 * QB;  // queries of a workgroup
-    __shared__ __attribute__((aligned(1024))) uint16_t lds[2 * 2 * TILE];  // [slot][K, V]
+    constexpr int SLOT = 2 * TILE * 2;  // bytes of a tile of K and one of V
+    __shared__ __attribute__((aligned(1024))) uint16_t lds[3 * 2 * TILE];  // [slot][K, V]
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
@@ -352,7 +507,8 @@ __global__ __launch_bounds__(kBwdThreads, 1) void bwd_dq_kernel(const BwdArgs a)
 
     const int n_qt = (a.Sq + 31) / 32;
     bf16x8 qf[QB][KD], gf[QB][KD];  // B operands: lane l holds query l%32
-    float nl[QB], nd[QB];
+    float nl[QB];
+    f32x16 nd[QB];  // -delta, from which the products of dP start
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
         const int q = wq0 + qb * 32 + l32;
@@ -365,7 +521,9 @@ __global__ __launch_bounds__(kBwdThreads, 1) void bwd_dq_kernel(const BwdArgs a)
         // (queries past Sq: the last tile's padding, or the last row of all)
         const long long tile = (long long)bh * n_qt + min(q, n_qt * 32 - 1) / 32;
         nl[qb] = a.rows[tile * 64 + l32];
-        nd[qb] = a.rows[tile * 64 + 32 + l32];
+        const float x = a.rows[tile * 64 + 32 + l32];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) nd[qb][r] = x;
     }
     f32x16 dq[QB][CB] = {};
 
@@ -377,63 +535,156 @@ __global__ __launch_bounds__(kBwdThreads, 1) void bwd_dq_kernel(const BwdArgs a)
 
     TileLoad<D> load;
     load.init(wave, lane);
+    TileRead<D> read;
+    read.init(lane);
     const uint32_t lds0 = lds_address(lds);
     const uint32_t slab = (uint32_t)a.Skv * D * 2;
     const long long head = bh / a.group;
     const dma_rsrc_t k_rsrc = make_dma_rsrc(a.k + head * a.Skv * D, slab);
     const dma_rsrc_t v_rsrc = make_dma_rsrc(a.v + head * a.Skv * D, slab);
     auto issue = [&](int step, int slot) __attribute__((always_inline)) {
-        const uint32_t dst = lds0 + slot * (2 * TILE * 2);
+        const uint32_t dst = lds0 + slot * SLOT;
         load.issue(k_rsrc, dst, step * 32, a.Skv, wave);
         load.issue(v_rsrc, dst + TILE * 2, step * 32, a.Skv, wave);
     };
-    if (begin < end) issue(begin, 0);
-    for (int step = begin; step < end; ++step) {
-        const int slot = (step - begin) & 1;
+
+    // Operand i of a step: K by rows (S of this tile), K transposed (dQ of the tile before:
+    // its dS is formed during the products of S), V by rows (dP of this tile); KD of each.
+    constexpr int OPS = 3 * KD;
+    bf16x8 ring[kRing];
+    uint32_t row_base, col_base;
+    auto fetch = [&](auto i_tag) __attribute__((always_inline)) {
+        constexpr int i = decltype(i_tag)::value, ph = i / KD, j = i % KD;
+        if constexpr (ph == 0) ring[i % kRing] = TileRead<D>::template by_row<j>(row_base, 0);
+        if constexpr (ph == 1)
+            ring[i % kRing] = TileRead<D>::template by_col<j % CB, j / CB>(col_base, 0);
+        if constexpr (ph == 2)
+            ring[i % kRing] = TileRead<D>::template by_row<j>(row_base, TILE * 2);
+    };
+    f32x16 s[QB], p[QB] = {}, dp[QB] = {};  // (no tile before the first: its dS is 0)
+    uint32_t dsk[QB][8];  // dS as operands
+    auto product = [&](auto i_tag, auto qb_tag) __attribute__((always_inline)) {
+        constexpr int i = decltype(i_tag)::value, qb = decltype(qb_tag)::value;
+        constexpr int ph = i / KD, j = i % KD, t = j / CB, cb = j % CB;
+        const bf16x8 x = ring[i % kRing];
+        if constexpr (ph == 0 && j == 0) score_first(s[qb], x, qf[qb][j]);
+        if constexpr (ph == 0 && j > 0) score_add(s[qb], x, qf[qb][j]);
+        if constexpr (ph == 1) {
+            const u32x4 y = {dsk[qb][4 * t], dsk[qb][4 * t + 1], dsk[qb][4 * t + 2],
+                             dsk[qb][4 * t + 3]};
+            dq[qb][cb] = mfma(x, __builtin_bit_cast(bf16x8, y), dq[qb][cb]);
+        }
+        if constexpr (ph == 2 && j == 0) score_from(dp[qb], x, gf[qb][j], nd[qb]);
+        if constexpr (ph == 2 && j > 0) score_add(dp[qb], x, gf[qb][j]);
+    };
+    auto weight = [&](auto r_tag) __attribute__((always_inline)) {
+        constexpr int r = decltype(r_tag)::value;
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            float x = __builtin_amdgcn_exp2f(fmaf(s[qb][r], a.scale_log2, nl[qb]));
+            here(x);
+            p[qb][r] = x;
+        }
+    };
+    // Scores of hidden pairs and of keys past Skv: their weights come out as exactly 0.
+    auto hide = [&](int k0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            const int last =
+                CAUSAL ? min(a.Skv - 1, wq0 + qb * 32 + l32 + diag) : a.Skv - 1;
+            const int lim = last - k0 - 4 * hh;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[qb][r] = acc_row(r, 0) <= lim ? s[qb][r] : a.hidden;
+        }
+    };
+    auto grad = [&](auto r_tag) __attribute__((always_inline)) {
+        constexpr int r = decltype(r_tag)::value;
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            dp[qb][r] *= p[qb][r];
+            if constexpr (r % 2 == 1) {
+                dsk[qb][r / 2] = round2(dp[qb][r - 1], dp[qb][r]);
+                here(dsk[qb][r / 2]);
+            }
+        }
+    };
+    constexpr int N = QB * KD;  // products, and the gaps behind them, of one kind
+    constexpr int TAIL = OPS - (kRing - 1);  // the last slots, behind the barrier
+    auto body = [&](int k0) __attribute__((always_inline)) {
+        static_for<0, TAIL>([&](auto i_tag) __attribute__((always_inline)) {
+            constexpr int i = decltype(i_tag)::value, ph = i / KD, j = i % KD;
+            fetch(std::integral_constant<int, i + kRing - 1>{});
+            static_for<0, QB>([&](auto qb_tag) __attribute__((always_inline)) {
+                product(i_tag, qb_tag);
+                // dS of the tile before in the gaps of S; 12 of the 16 rows' weights in those
+                // of dQ, 4 in those of dP; the first slots are left to settle
+                constexpr int gap = j * QB + decltype(qb_tag)::value;
+                constexpr int M = N - QB, B = N - QB * (kRing - 1);
+                if constexpr (ph == 0 && j > 0)
+                    static_for<(gap - QB) * 16 / M, (gap - QB + 1) * 16 / M>(grad);
+                if constexpr (ph == 1 && j > 0)
+                    static_for<(gap - QB) * 12 / M, (gap - QB + 1) * 12 / M>(weight);
+                if constexpr (ph == 2) static_for<12 + gap * 4 / B, 12 + (gap + 1) * 4 / B>(weight);
+            });
+            if constexpr (ph == 0 && j == 0) settle(dp);
+            if constexpr (ph == 1 && j == 0) {
+                settle(s);
+                if (k0 + 32 > a.Skv || (CAUSAL && k0 + 31 > wq0 + diag)) hide(k0);
+            }
+            slot_end();
+        });
+    };
+    // dQ of the wave's last tile.
+    auto drain = [&]() __attribute__((always_inline)) {
+        settle(dp);
+        static_for<0, 16>(grad);
+        static_for<KD, KD + kRing - 1>(fetch);
+        static_for<KD, 2 * KD>([&](auto i_tag) __attribute__((always_inline)) {
+            constexpr int i = decltype(i_tag)::value;
+            if constexpr (i + kRing - 1 < 2 * KD)
+                fetch(std::integral_constant<int, i + kRing - 1>{});
+            static_for<0, QB>(
+                [&](auto qb_tag) __attribute__((always_inline)) { product(i_tag, qb_tag); });
+            slot_end();
+        });
+    };
+
+    int slot = 0;
+    if (begin < end) {
+        issue(begin, 0);
+        if (begin + 1 < end) issue(begin + 1, 1);
         publish_barrier<0>();
-        if (step + 1 < end) issue(step + 1, slot ^ 1);
-        const int k0 = step * 32;
-        if (CAUSAL && k0 > wq0 + 32 * QB - 1 + diag) continue;  // past the wave's diagonal
-        const uint16_t* ksl = lds + slot * (2 * TILE);
-        const uint16_t* vsl = ksl + TILE;
-        f32x16 s[QB] = {}, dp[QB];
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) dp[qb][r] = nd[qb];
-#pragma unroll
-        for (int ks = 0; ks < KD; ++ks) {
-            const bf16x8 x = row_operand<D>(ksl, ks, lane);
-#pragma unroll
-            for (int qb = 0; qb < QB; ++qb) s[qb] = mfma(x, qf[qb][ks], s[qb]);
-        }
-#pragma unroll
-        for (int ks = 0; ks < KD; ++ks) {
-            const bf16x8 x = row_operand<D>(vsl, ks, lane);
-#pragma unroll
-            for (int qb = 0; qb < QB; ++qb) dp[qb] = mfma(x, gf[qb][ks], dp[qb]);
-        }
-        const bool masked = k0 + 32 > a.Skv || (CAUSAL && k0 + 31 > wq0 + diag);
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                float p = __builtin_amdgcn_exp2f(fmaf(s[qb][r], a.scale_log2, nl[qb]));
-                if (masked) {
-                    const int key = k0 + acc_row(r, hh);
-                    const bool in = key < a.Skv && (!CAUSAL || key <= wq0 + qb * 32 + l32 + diag);
-                    p = in ? p : 0.f;
-                }
-                dp[qb][r] *= p;
-            }
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int cb = 0; cb < CB; ++cb) {
-                const bf16x8 x = col_operand<D>(ksl, cb, t, lane);
-#pragma unroll
-                for (int qb = 0; qb < QB; ++qb) dq[qb][cb] = mfma(x, round8(dp[qb], t), dq[qb][cb]);
-            }
+        row_base = read.row + lds0;
+        static_for<0, kRing - 1>(fetch);
+    }
+    for (int step = begin; step < end; ++step) {
+        // (before the first tile: itself, with a dS of 0)
+        const int prev = slot == 0 ? 2 : slot - 1, next = slot == 2 ? 0 : slot + 1;
+        // opaque, so that the XORed addresses are formed where they are used instead of
+        // being kept in registers over the whole loop
+        row_base = read.row + lds0 + slot * SLOT;
+        col_base = read.col + lds0 + (step == begin ? slot : prev) * SLOT;
+        asm volatile("" : "+v"(row_base), "+v"(col_base));
+        // (a wave whose pairs are all hidden computes zeros: it would only wait)
+        body(step * 32);
+        // The tile before has been read for good: its slot is free behind the barrier,
+        // which also publishes the next tile.
+        publish_barrier<0>();
+        if (step + 2 < end) issue(step + 2, prev);
+        row_base = read.row + lds0 + next * SLOT;
+        asm volatile("" : "+v"(row_base));
+        static_for<TAIL, OPS>([&](auto i_tag) __attribute__((always_inline)) {
+            constexpr int i = decltype(i_tag)::value;
+            static_for<0, QB>(
+                [&](auto qb_tag) __attribute__((always_inline)) { product(i_tag, qb_tag); });
+            fetch(std::integral_constant<int, i + kRing - 1 - OPS>{});
+            slot_end();
+        });
+        slot = next;
+    }
+    if (begin < end) {
+        col_base = read.col + lds0 + (slot == 0 ? 2 : slot - 1) * SLOT;
+        drain();
     }
 
 #pragma unroll

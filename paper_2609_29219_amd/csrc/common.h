@@ -301,7 +301,10 @@ struct BwdArgs {
     int Sq, Skv, group;
     long long q_heads, kv_heads;  // over the batch
     int num_xcds;
-    float scale, scale_log2;      // of either sign, or 0; times log2 e
+    float scale;       // of either sign, or 0
+    float scale_log2;  // times log2 e; not 0 (hidden * 0 would be NaN): 0 is FLT_MIN,
+    float hidden;      // with which every weight is the same; a hidden pair's score, whose
+                       // product with scale_log2 is -inf
     // of the kernel that runs: blocks to a head, splits of each, and its results (fp32
     // partials part_stride values apart where split)
     int blocks, splits, out_bf16;

@@ -247,6 +247,7 @@ std::map<int, DeviceState> g_devices;  // nodes never move
 std::map<std::tuple<int, int, int, int, int, int, int, int>, FwdPlan> g_fwd_cache;
 std::map<std::tuple<int, int, int, int, int, int, int>, DecodePlan> g_dec_cache;
 std::map<std::tuple<int, int, int, int, int>, GemmPlan> g_gemm_cache;
+std::map<std::tuple<int, int, int, int, int, int, int>, BwdPlan> g_bwd_cache;
 
 // Structural properties from the runtime; performance properties from the
 // built-in gfx950 description.
@@ -1001,10 +1002,21 @@ static int validate_bwd_dims(int B, int Hq, int Hkv, int Sq, int Skv, int d, int
 
 static int bwd_plan_of(DeviceState* st, int B, int Hq, int Hkv, int Sq, int Skv, int d,
                        int causal, BwdPlan* plan, size_t* ws_bytes) {
-    if (!plan_bwd(st->desc.num_cus, B, Hq, Hkv, Sq, Skv, d, causal ? 1 : 0, plan))
-        return fail(ATTN_EUNSUPPORTED, "no feasible backward plan for this shape");
-    *ws_bytes = (size_t)(bwd_rows_floats(B, Hq, Sq) +
-                         bwd_part_floats(*plan, B, Hq, Hkv, Sq, Skv, d)) * sizeof(float);
+    const auto key = std::make_tuple(B, Hq, Hkv, Sq, Skv, d + (causal ? 1 : 0), st->desc.num_cus);
+    bool known = false;
+    {
+        std::lock_guard<std::mutex> lk(g_mu);
+        auto it = g_bwd_cache.find(key);
+        known = it != g_bwd_cache.end();
+        if (known) *plan = it->second;
+    }
+    if (!known) {
+        if (!plan_bwd(st->desc.num_cus, B, Hq, Hkv, Sq, Skv, d, causal ? 1 : 0, plan))
+            return fail(ATTN_EUNSUPPORTED, "no feasible backward plan for this shape");
+        std::lock_guard<std::mutex> lk(g_mu);
+        g_bwd_cache[key] = *plan;
+    }
+    *ws_bytes = (size_t)bwd_workspace_floats(*plan, B, Hq, Hkv, Sq, Skv, d) * sizeof(float);
     return ATTN_OK;
 }
 
@@ -1060,6 +1072,10 @@ int attn_bwd(const void* q, const void* k, const void* v, const void* o, const f
         a.d_o = static_cast<const uint16_t*>(d_o);
         a.dlse = dlse;
         a.rows = static_cast<float*>(ws);
+        a.dq = dq;
+        a.dk = dk;
+        a.dv = dv;
+        a.out_bf16 = (flags & ATTN_OUT_BF16) ? 1 : 0;
         a.Sq = Sq;
         a.Skv = Skv;
         a.group = Hq / Hkv;
@@ -1071,9 +1087,7 @@ int attn_bwd(const void* q, const void* k, const void* v, const void* o, const f
         if (fabsf(a.scale_log2) < FLT_MIN) a.scale_log2 = scale < 0.f ? -FLT_MIN : FLT_MIN;
         a.hidden = scale < 0.f ? INFINITY : -INFINITY;
         const hipError_t e =
-            launch_bwd(plan, a, d, causal ? 1 : 0, (flags & ATTN_O_BF16) ? 1 : 0,
-                       (flags & ATTN_OUT_BF16) ? 1 : 0, dq, dk, dv,
-                       a.rows + bwd_rows_floats(B, Hq, Sq), t_stream);
+            launch_bwd(plan, a, d, causal ? 1 : 0, (flags & ATTN_O_BF16) ? 1 : 0, t_stream);
         return e == hipSuccess ? ATTN_OK : fail_hip(e, "backward launch");
     });
 }

@@ -5,12 +5,13 @@
 //     dV = P^T dO,   dP = dO V^T,   dS = P o (dP - delta),   delta = rowsum(dO o O) - dlse,
 //     dQ = scale dS K,   dK = scale dS^T Q.
 //
-// Three kernels, and no atomics, so that every call gives the same bits:
-//   bwd_rows_kernel   delta and the base-2 log-sum-exp of every row (HBM bound);
-//   bwd_dkdv_kernel   a wave keeps 32*KB keys: K and V as operands and dK, dV as
+// No atomics, so that every call gives the same bits.  bwd_rows_kernel computes delta and
+// the base-2 log-sum-exp of every row (HBM bound); bwd_kernel holds two kinds of
+// workgroups:
+//   dkdv_block        a wave keeps 32*KB keys: K and V as operands and dK, dV as
 //                     accumulators in registers, and walks the query tiles (of all query
 //                     heads of the group): S, dP, dV, dK, four products;
-//   bwd_dq_kernel     a wave keeps 32*QB queries: Q, dO and dQ in registers, and walks the
+//   dq_block          a wave keeps 32*QB queries: Q, dO and dQ in registers, and walks the
 //                     key tiles: S, dP, dQ, three products.
 // Seven products instead of the five of the definition: dQ and dK sum over different
 // axes, and one kernel for both would have to add one of them up across workgroups,
@@ -182,33 +183,66 @@ __device__ __forceinline__ void settle(f32x16 (&d)[N]) {
 // Row of accumulator register r in lane half hh.
 __device__ __forceinline__ int acc_row(int r, int hh) { return 8 * (r >> 2) + 4 * hh + (r & 3); }
 
-// Logical workgroup of this one: the hardware deals workgroups round-robin to the XCDs,
-// so each XCD gets a contiguous range (of few heads, whose tiles stay in its L2).
-__device__ __forceinline__ int logical_wg(int wg, int n_wg, int num_xcds) {
-    const int per = n_wg / num_xcds, rem = n_wg % num_xcds;
-    const int xcd = wg % num_xcds, slot = wg / num_xcds;
-    return (xcd < rem ? xcd * (per + 1) : rem * (per + 1) + (xcd - rem) * per) + slot;
+// 32 result rows of a wave (row l%32 in lane l, columns 32*cb + acc_row) to out, rows from
+// row0 up to n_rows.  Through LDS: stored from the registers, an instruction would write
+// 8 or 16 bytes to each of 32 rows; staged, it writes whole lines (a workgroup's results
+// in 4 us instead of 13, with all workgroups storing at once).  The stage, the wave's
+// own, is 32 rows of half the fp32 values, or of all bf16 ones, padded by 16 bytes.
+template <int D>
+constexpr int stage_bytes() { return 32 * (D * 2 + 16); }
+
+template <int D>
+__device__ __forceinline__ void store_rows(const f32x16 (&x)[D / 32], char* stage, void* out,
+                                           long long row0, long long n_rows, int bf16,
+                                           float factor, int lane) {
+    constexpr int STRIDE = D * 2 + 16, L = D * 2 / 16, RPI = 64 / L;  // lanes to a row, rows at once
+    const int l32 = lane & 31, hh = lane >> 5;
+    auto flush = [&](char* base, long long row_bytes) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 32 / RPI; ++i) {
+            const int r = i * RPI + lane / L;
+            const u32x4 y = *reinterpret_cast<const u32x4*>(stage + r * STRIDE + (lane % L) * 16);
+            if (row0 + r < n_rows)
+                *reinterpret_cast<u32x4*>(base + (row0 + r) * row_bytes + (lane % L) * 16) = y;
+        }
+    };
+    if (bf16) {
+#pragma unroll
+        for (int cb = 0; cb < D / 32; ++cb)
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4) {
+                uint32_t y[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    y[e] = round2(x[cb][4 * r4 + 2 * e] * factor, x[cb][4 * r4 + 2 * e + 1] * factor);
+                *reinterpret_cast<uint64_t*>(stage + l32 * STRIDE +
+                                             (32 * cb + 8 * r4 + 4 * hh) * 2) =
+                    (uint64_t)y[1] << 32 | y[0];
+            }
+        flush(static_cast<char*>(out), D * 2);
+        return;
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4) {
+                f32x4 y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = x[half * (D / 64) + c][4 * r4 + e] * factor;
+                *reinterpret_cast<f32x4*>(stage + l32 * STRIDE + (32 * c + 8 * r4 + 4 * hh) * 4) = y;
+            }
+        flush(static_cast<char*>(out) + half * D * 2, D * 4);
+    }
 }
 
-// A 32 x 32 block of accumulators (one result row per lane, its columns c0 + acc_row) out.
-__device__ __forceinline__ void store_block(const f32x16& x, void* out, long long at, int bf16,
-                                            int hh, float factor) {
-#pragma unroll
-    for (int r4 = 0; r4 < 4; ++r4) {
-        const long long p = at + 8 * r4 + 4 * hh;
-        f32x4 y;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = x[4 * r4 + e] * factor;
-        if (bf16) {
-            typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-            bf16x4 z;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) z[e] = (__bf16)y[e];
-            *reinterpret_cast<bf16x4*>(static_cast<uint16_t*>(out) + p) = z;
-        } else {
-            *reinterpret_cast<f32x4*>(static_cast<float*>(out) + p) = y;
-        }
-    }
+// LDS of a workgroup: two tiles of Q and dO and their row values, or three of K and V;
+// at the end, the waves' stages.
+template <int D>
+constexpr int bwd_lds_bytes() {
+    constexpr int tiles = 3 * 2 * 32 * D * 2, stages = kBwdWaves * stage_bytes<D>();
+    return tiles > stages ? tiles : stages;
 }
 
 // ------------------------------------------------------------- row values --
@@ -263,20 +297,14 @@ __global__ __launch_bounds__(256) void bwd_rows_kernel(const BwdArgs a) {
 }
 
 // ------------------------------------------------------------------ dK, dV --
-template <int D, int KB, bool CAUSAL>
-__global__ __launch_bounds__(kBwdThreads, 1) void bwd_dkdv_kernel(const BwdArgs a) {
-    constexpr int KD = D / 16, CB = D / 32, TILE = 32 * D;
-    constexpr int BK = kBwdWaves * 32 * KB;  // keys of a workgroup
-    __shared__ __attribute__((aligned(1024))) uint16_t lds[2 * 2 * TILE];  // [slot][Q, dO]
-    __shared__ __attribute__((aligned(16))) float rows[2][64];
+// One block of keys (kv head bh, over the batch), part `split` of `splits` of its sum.
+template <int D, bool CAUSAL>
+__device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, int block,
+                                           int split, int splits) {
+    constexpr int KB = 2, KD = D / 16, CB = D / 32, TILE = 32 * D;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-
-    const int logical = logical_wg(blockIdx.x, gridDim.x, a.num_xcds);
-    const int per_head = a.blocks * a.splits;
-    const int bh = logical / per_head;
-    const int split = (logical - bh * per_head) / a.blocks;
-    const int k0 = (logical - bh * per_head - split * a.blocks) * BK;  // heavy blocks first
+    const int k0 = block * kBwdBlock;
     const int wk0 = k0 + wave * 32 * KB;  // first key of the wave
 
     bf16x8 kf[KB][KD], vf[KB][KD];  // B operands: lane l holds key l%32
@@ -292,31 +320,36 @@ __global__ __launch_bounds__(kBwdThreads, 1) void bwd_dkdv_kernel(const BwdArgs 
     }
     f32x16 dk[KB][CB] = {}, dv[KB][CB] = {};
 
-    // steps of this workgroup: query tiles of every head of the group, from the first
-    // that reaches the block's first key
+    // steps: query tiles of every head of the group, from the first that reaches the
+    // block's first key
     const int diag = a.Skv - a.Sq;
     const int n_qt = (a.Sq + 31) / 32;
     const int qt0 = CAUSAL ? max(0, k0 - diag) / 32 : 0;
-    const int per_q = max(0, n_qt - qt0);
-    const long long steps = (long long)per_q * a.group;
-    const int begin = (int)(steps * split / a.splits), end = (int)(steps * (split + 1) / a.splits);
+    const int per_q = n_qt - qt0;
+    const int steps = bwd_kv_steps(block, a.Sq, a.Skv, a.group, CAUSAL);
+    const int begin = (int)((long long)steps * split / splits);
+    const int end = (int)((long long)steps * (split + 1) / splits);
 
     TileLoad<D> load;
     load.init(wave, lane);
     TileRead<D> read;
     read.init(lane);
-    const uint32_t lds0 = lds_address(lds), rows0 = lds_address(rows);
+    const uint32_t lds0 = lds_address(lds), rows0 = lds0 + 2 * 2 * TILE * 2;
     const uint32_t slab = (uint32_t)a.Sq * D * 2;
-    auto issue = [&](int step, int slot) __attribute__((always_inline)) {
-        const int g = step / per_q, qt = qt0 + step - g * per_q;
-        const long long head = (long long)bh * a.group + g;
+    int load_g = begin / per_q, load_qt = qt0 + begin % per_q;  // of the next load
+    auto issue = [&](int slot) __attribute__((always_inline)) {
+        const long long head = (long long)bh * a.group + load_g;
         const uint32_t dst = lds0 + slot * (2 * TILE * 2);
-        load.issue(make_dma_rsrc(a.q + head * a.Sq * D, slab), dst, qt * 32, a.Sq, wave);
-        load.issue(make_dma_rsrc(a.d_o + head * a.Sq * D, slab), dst + TILE * 2, qt * 32, a.Sq,
-                   wave);
+        load.issue(make_dma_rsrc(a.q + head * a.Sq * D, slab), dst, load_qt * 32, a.Sq, wave);
+        load.issue(make_dma_rsrc(a.d_o + head * a.Sq * D, slab), dst + TILE * 2, load_qt * 32,
+                   a.Sq, wave);
         if (wave == 0)
-            lds_dma4(make_dma_rsrc(a.rows + (head * n_qt + qt) * 64, 256), rows0 + slot * 256,
+            lds_dma4(make_dma_rsrc(a.rows + (head * n_qt + load_qt) * 64, 256), rows0 + slot * 256,
                      lane * 4);
+        if (++load_qt == n_qt) {
+            load_qt = qt0;
+            ++load_g;
+        }
     };
 
     // Operand i of a tile, in the order of use: Q by rows (S), dO by rows (dP), dO
@@ -447,21 +480,21 @@ __global__ __launch_bounds__(kBwdThreads, 1) void bwd_dkdv_kernel(const BwdArgs 
         });
     };
 
-    if (begin < end) {
-        issue(begin, 0);
-        if (begin + 1 < end) issue(begin + 1, 1);
-        publish_barrier<0>();
-        tile_bases(0);
-        static_for<0, kRing - 1>(fetch);
-    }
+    int qt = load_qt;
+    issue(0);  // (a part has at least one step)
+    if (begin + 1 < end) issue(1);
+    publish_barrier<0>();
+    tile_bases(0);
+    static_for<0, kRing - 1>(fetch);
     for (int step = begin; step < end; ++step) {
         const int slot = (step - begin) & 1;
         // (a wave whose keys are all hidden computes zeros: it would only wait)
-        body(CAUSAL ? (qt0 + step % per_q) * 32 : 0);
+        body(qt * 32);
+        if (CAUSAL && ++qt == n_qt) qt = qt0;
         // Every operand of this tile has been read: its slot is free behind the barrier,
         // which also publishes the next tile.
         publish_barrier<0>();
-        if (step + 2 < end) issue(step + 2, slot);
+        if (step + 2 < end) issue(slot);
         tile_bases(slot ^ 1);
         Scores none;  // (dK's products read dsk alone)
         static_for<TAIL, OPS>([&](auto i_tag) __attribute__((always_inline)) {
@@ -473,37 +506,31 @@ __global__ __launch_bounds__(kBwdThreads, 1) void bwd_dkdv_kernel(const BwdArgs 
         });
     }
 
+    __syncthreads();  // the stages overlay the tiles
+    const bool part = splits > 1;
+    const long long rows = a.kv_heads * a.Skv, row0 = (long long)bh * a.Skv + wk0;
+    void* dk_out = part ? a.part_k + split * rows * D : a.dk;
+    void* dv_out = part ? a.part_v + split * rows * D : a.dv;
+    const long long last = (long long)(bh + 1) * a.Skv;
+    char* stage = lds + wave * stage_bytes<D>();
+    const int bf16 = part ? 0 : a.out_bf16;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-        const int key = wk0 + kb * 32 + l32;
-        if (key >= a.Skv) continue;
-        long long at = ((long long)bh * a.Skv + key) * D;
-        if (a.splits > 1) at += (long long)split * a.part_stride;
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
-            store_block(dk[kb][cb], a.out0, at + cb * 32, a.out_bf16, hh, a.scale);
-            store_block(dv[kb][cb], a.out1, at + cb * 32, a.out_bf16, hh, 1.f);
-        }
+        store_rows<D>(dk[kb], stage, dk_out, row0 + kb * 32, last, bf16, a.scale, lane);
+        store_rows<D>(dv[kb], stage, dv_out, row0 + kb * 32, last, bf16, 1.f, lane);
     }
 }
 
 // ---------------------------------------------------------------------- dQ --
-template <int D, int QB, bool CAUSAL>
-__global__ __launch_bounds__(kBwdThreads, 1) void bwd_dq_kernel(const BwdArgs a) {
-    constexpr int KD = D / 16, CB = D / 32, TILE = 32 * D;
-    constexpr int BQ = kBwdWaves * 32 * QB;  // queries of a workgroup
+// One block of queries (query head bh, over the batch), part `split` of `splits` of its sum.
+template <int D, bool CAUSAL>
+__device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, int block,
+                                         int split, int splits) {
+    constexpr int QB = 2, KD = D / 16, CB = D / 32, TILE = 32 * D;
     constexpr int SLOT = 2 * TILE * 2;  // bytes of a tile of K and one of V
-    __shared__ __attribute__((aligned(1024))) uint16_t lds[3 * 2 * TILE];  // [slot][K, V]
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-
-    const int logical = logical_wg(blockIdx.x, gridDim.x, a.num_xcds);
-    const int per_head = a.blocks * a.splits;
-    const int bh = logical / per_head;
-    const int split = (logical - bh * per_head) / a.blocks;
-    // heavy blocks first
-    const int q0 = (a.blocks - 1 - (logical - bh * per_head - split * a.blocks)) * BQ;
-    const int wq0 = q0 + wave * 32 * QB;
+    const int wq0 = block * kBwdBlock + wave * 32 * QB;  // first query of the wave
 
     const int n_qt = (a.Sq + 31) / 32;
     bf16x8 qf[QB][KD], gf[QB][KD];  // B operands: lane l holds query l%32
@@ -528,10 +555,9 @@ __global__ __launch_bounds__(kBwdThreads, 1) void bwd_dq_kernel(const BwdArgs a)
     f32x16 dq[QB][CB] = {};
 
     const int diag = a.Skv - a.Sq;
-    const int last_q = min(q0 + BQ, a.Sq) - 1;
-    const int n_keys = CAUSAL ? min(a.Skv, last_q + diag + 1) : a.Skv;
-    const long long steps = (n_keys + 31) / 32;
-    const int begin = (int)(steps * split / a.splits), end = (int)(steps * (split + 1) / a.splits);
+    const int steps = bwd_q_steps(block, a.Sq, a.Skv, CAUSAL);
+    const int begin = (int)((long long)steps * split / splits);
+    const int end = (int)((long long)steps * (split + 1) / splits);
 
     TileLoad<D> load;
     load.init(wave, lane);
@@ -650,13 +676,11 @@ __global__ __launch_bounds__(kBwdThreads, 1) void bwd_dq_kernel(const BwdArgs a)
     };
 
     int slot = 0;
-    if (begin < end) {
-        issue(begin, 0);
-        if (begin + 1 < end) issue(begin + 1, 1);
-        publish_barrier<0>();
-        row_base = read.row + lds0;
-        static_for<0, kRing - 1>(fetch);
-    }
+    issue(begin, 0);  // (a part has at least one step)
+    if (begin + 1 < end) issue(begin + 1, 1);
+    publish_barrier<0>();
+    row_base = read.row + lds0;
+    static_for<0, kRing - 1>(fetch);
     for (int step = begin; step < end; ++step) {
         // (before the first tile: itself, with a dS of 0)
         const int prev = slot == 0 ? 2 : slot - 1, next = slot == 2 ? 0 : slot + 1;
@@ -682,45 +706,85 @@ __global__ __launch_bounds__(kBwdThreads, 1) void bwd_dq_kernel(const BwdArgs a)
         });
         slot = next;
     }
-    if (begin < end) {
-        col_base = read.col + lds0 + (slot == 0 ? 2 : slot - 1) * SLOT;
-        drain();
-    }
+    col_base = read.col + lds0 + (slot == 0 ? 2 : slot - 1) * SLOT;
+    drain();
 
+    __syncthreads();  // the stages overlay the tiles
+    const bool part = splits > 1;
+    const long long rows = a.q_heads * a.Sq, row0 = (long long)bh * a.Sq + wq0;
+    void* out = part ? a.part_q + split * rows * D : a.dq;
+    char* stage = lds + wave * stage_bytes<D>();
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-        const int q = wq0 + qb * 32 + l32;
-        if (q >= a.Sq) continue;
-        long long at = ((long long)bh * a.Sq + q) * D;
-        if (a.splits > 1) at += (long long)split * a.part_stride;
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb)
-            store_block(dq[qb][cb], a.out0, at + cb * 32, a.out_bf16, hh, a.scale);
+    for (int qb = 0; qb < QB; ++qb)
+        store_rows<D>(dq[qb], stage, out, row0 + qb * 32, (long long)(bh + 1) * a.Sq,
+                      part ? 0 : a.out_bf16, a.scale, lane);
+}
+
+// ------------------------------------------------------------------ kernel --
+// Workgroups: for every key/value head, the parts of its blocks of keys and of the blocks
+// of queries of its group, in one launch, so that the one kind fills the other's gaps.
+// The hardware deals workgroups round-robin to the XCDs; each XCD gets whole heads, whose
+// tiles stay in its L2, where they can be dealt evenly.  Under a causal mask blocks differ:
+// the heaviest of both kinds come first, over all heads.
+template <int D, bool CAUSAL>
+__global__ __launch_bounds__(kBwdThreads, 1) void bwd_kernel(const BwdArgs a) {
+    __shared__ __attribute__((aligned(1024))) char lds[bwd_lds_bytes<D>()];
+    const int heads = (int)a.kv_heads, units = a.kv_units + a.group * a.q_units;
+    const bool even = heads % a.num_xcds == 0;
+    const int hx = even ? heads / a.num_xcds : heads;
+    const int first = even ? (int)(blockIdx.x % a.num_xcds) * hx : 0;
+    const int i = even ? (int)(blockIdx.x / a.num_xcds) : (int)blockIdx.x;
+    const int unit = CAUSAL ? i / hx : i % units;
+    const int head = first + (CAUSAL ? i - unit * hx : i / units);
+    // the kinds are interleaved in proportion, each heaviest first
+    const int kv = bwd_kv_before(unit, a.kv_units, units);
+    if (bwd_kv_before(unit + 1, a.kv_units, units) > kv) {
+        int block = kv, split = 0, splits = 1;
+        if (a.kv_chunk) bwd_find_part(kv, a.kv_blocks, [&](int b) {
+            return bwd_parts(bwd_kv_steps(b, a.Sq, a.Skv, a.group, CAUSAL), a.kv_chunk);
+        }, &block, &split, &splits);
+        dkdv_block<D, CAUSAL>(a, lds, head, block, split, splits);
+    } else {
+        const int x = unit - kv;
+        int block = x / a.group, split = 0, splits = 1;
+        const int q_head = head * a.group + x - block * a.group;
+        if (a.q_chunk) bwd_find_part(block, a.q_blocks, [&](int b) {
+            return bwd_parts(bwd_q_steps(a.q_blocks - 1 - b, a.Sq, a.Skv, CAUSAL), a.q_chunk);
+        }, &block, &split, &splits);
+        dq_block<D, CAUSAL>(a, lds, q_head, a.q_blocks - 1 - block, split, splits);
     }
 }
 
-// out[i] = sum of n partials at i, i + stride, ..., in their order; four values to a
-// thread.  HBM bound.
-__global__ __launch_bounds__(256) void bwd_sum_kernel(const float* part, long long stride, int n,
-                                                      void* out, int out_bf16, long long quads) {
+// Adds up the parts of the blocks that have several, in their order, four values to a
+// thread: dK and dV (z = 0, 1), dQ (2).  HBM bound.
+template <int D>
+__global__ __launch_bounds__(256) void bwd_sum_kernel(const BwdArgs a, int causal) {
+    const bool q = blockIdx.z == 2;
+    const int chunk = q ? a.q_chunk : a.kv_chunk, S = q ? a.Sq : a.Skv;
+    const long long rows = (q ? a.q_heads : a.kv_heads) * S;
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (i >= quads) return;
-    f32x4 s = {};
-    for (int j = 0; j < n; ++j) s += *reinterpret_cast<const f32x4*>(part + j * stride + i * 4);
-    if (out_bf16) {
-        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-        bf16x4 z;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) z[e] = (__bf16)s[e];
-        *reinterpret_cast<bf16x4*>(static_cast<uint16_t*>(out) + i * 4) = z;
+    const long long row = i / (D / 4);
+    if (!chunk || row >= rows) return;
+    const int block = (int)(row % S) / kBwdBlock;
+    const int n = bwd_parts(q ? bwd_q_steps(block, a.Sq, a.Skv, causal)
+                              : bwd_kv_steps(block, a.Sq, a.Skv, a.group, causal), chunk);
+    if (n == 1) return;
+    const float* part = (q ? a.part_q : blockIdx.z ? a.part_v : a.part_k) + i * 4;
+    void* out = q ? a.dq : blockIdx.z ? a.dv : a.dk;
+    f32x4 s = *reinterpret_cast<const f32x4*>(part);
+#pragma unroll 4
+    for (int j = 1; j < n; ++j) s += *reinterpret_cast<const f32x4*>(part + j * rows * D);
+    if (a.out_bf16) {
+        const uint64_t y = (uint64_t)round2(s[2], s[3]) << 32 | round2(s[0], s[1]);
+        *reinterpret_cast<uint64_t*>(static_cast<uint16_t*>(out) + i * 4) = y;
     } else {
         *reinterpret_cast<f32x4*>(static_cast<float*>(out) + i * 4) = s;
     }
 }
 
 template <int D>
-hipError_t launch_d(const BwdPlan& p, BwdArgs a, int causal, int o_bf16, int out_bf16, void* dq,
-                    void* dk, void* dv, float* part, hipStream_t stream) {
+hipError_t launch_d(const BwdPlan& p, const BwdArgs& a, int causal, int o_bf16,
+                    hipStream_t stream) {
     const long long slots = a.q_heads * ((a.Sq + 31) / 32) * 32 * (D / 8);
     const dim3 row_grid((unsigned)((slots + 255) / 256));
     if (o_bf16)
@@ -729,52 +793,39 @@ hipError_t launch_d(const BwdPlan& p, BwdArgs a, int causal, int o_bf16, int out
         bwd_rows_kernel<D, false><<<row_grid, 256, 0, stream>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const long long kv_values = a.kv_heads * a.Skv * D, q_values = a.q_heads * a.Sq * D;
-    auto sum = [&](const float* from, void* to, int n, long long values) {
-        bwd_sum_kernel<<<(unsigned)((values / 4 + 255) / 256), 256, 0, stream>>>(
-            from, values, n, to, out_bf16, values / 4);
-        return hipGetLastError();
-    };
-
-    a.blocks = p.kv_blocks;
-    a.splits = p.kv_splits;
-    a.part_stride = kv_values;
-    a.out_bf16 = p.kv_splits > 1 ? 0 : out_bf16;
-    a.out0 = p.kv_splits > 1 ? part : dk;
-    a.out1 = p.kv_splits > 1 ? part + p.kv_splits * kv_values : dv;
-    const dim3 kv_grid((unsigned)(a.kv_heads * a.blocks * a.splits));
+    const dim3 grid((unsigned)p.grid);
     if (causal)
-        bwd_dkdv_kernel<D, 2, true><<<kv_grid, kBwdThreads, 0, stream>>>(a);
+        bwd_kernel<D, true><<<grid, kBwdThreads, 0, stream>>>(a);
     else
-        bwd_dkdv_kernel<D, 2, false><<<kv_grid, kBwdThreads, 0, stream>>>(a);
+        bwd_kernel<D, false><<<grid, kBwdThreads, 0, stream>>>(a);
     e = hipGetLastError();
-    if (e == hipSuccess && p.kv_splits > 1) e = sum(part, dk, p.kv_splits, kv_values);
-    if (e == hipSuccess && p.kv_splits > 1)
-        e = sum(part + p.kv_splits * kv_values, dv, p.kv_splits, kv_values);
-    if (e != hipSuccess) return e;
-
-    a.blocks = p.q_blocks;
-    a.splits = p.q_splits;
-    a.part_stride = q_values;
-    a.out_bf16 = p.q_splits > 1 ? 0 : out_bf16;
-    a.out0 = p.q_splits > 1 ? part : dq;
-    const dim3 q_grid((unsigned)(a.q_heads * a.blocks * a.splits));
-    if (causal)
-        bwd_dq_kernel<D, 2, true><<<q_grid, kBwdThreads, 0, stream>>>(a);
-    else
-        bwd_dq_kernel<D, 2, false><<<q_grid, kBwdThreads, 0, stream>>>(a);
-    e = hipGetLastError();
-    if (e == hipSuccess && p.q_splits > 1) e = sum(part, dq, p.q_splits, q_values);
-    return e;
+    if (e != hipSuccess || (!p.kv_chunk && !p.q_chunk)) return e;
+    const long long kv_rows = p.kv_chunk ? a.kv_heads * a.Skv : 0;
+    const long long q_rows = p.q_chunk ? a.q_heads * a.Sq : 0;
+    const long long quads = (kv_rows > q_rows ? kv_rows : q_rows) * (D / 4);
+    bwd_sum_kernel<D><<<dim3((unsigned)((quads + 255) / 256), 1, p.q_chunk ? 3 : 2), 256, 0,
+                        stream>>>(a, causal);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_bwd(const BwdPlan& p, const BwdArgs& a, int d, int causal, int o_bf16,
-                      int out_bf16, void* dq, void* dk, void* dv, float* part,
+hipError_t launch_bwd(const BwdPlan& p, const BwdArgs& args, int d, int causal, int o_bf16,
                       hipStream_t stream) {
-    return d == 64 ? launch_d<64>(p, a, causal, o_bf16, out_bf16, dq, dk, dv, part, stream)
-                   : launch_d<128>(p, a, causal, o_bf16, out_bf16, dq, dk, dv, part, stream);
+    BwdArgs a = args;
+    a.kv_blocks = p.kv_blocks;
+    a.kv_units = p.kv_units;
+    a.kv_chunk = p.kv_chunk;
+    a.q_blocks = p.q_blocks;
+    a.q_units = p.q_units;
+    a.q_chunk = p.q_chunk;
+    // the parts follow the row values
+    const long long kv_values = a.kv_heads * a.Skv * d;
+    a.part_k = a.rows + a.q_heads * ((a.Sq + 31) / 32) * 64;
+    a.part_v = a.part_k + p.kv_parts * kv_values;
+    a.part_q = a.part_v + p.kv_parts * kv_values;
+    return d == 64 ? launch_d<64>(p, a, causal, o_bf16, stream)
+                   : launch_d<128>(p, a, causal, o_bf16, stream);
 }
 
 }  // namespace attn

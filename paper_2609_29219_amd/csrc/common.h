@@ -283,11 +283,51 @@ hipError_t launch_decode(const DecodePlan& p, const void* q, const void* k, cons
 hipError_t launch_gemm(const GemmPlan& p, const void* a, const void* b, void* c, int M, int N,
                        int K, int out_bf16, int num_xcds, float* workspace, hipStream_t stream);
 // ------------------------------------------------------- attention backward --
-// Work split of one backward call: blocks of keys (dK, dV) and of queries (dQ) to a
-// head, and over how many workgroups each block's sum is split.
+// Workgroups keep a block of kBwdBlock keys (for dK, dV) or queries (for dQ) and walk
+// the tiles of 32 queries (of every head of the group) or keys that it meets: its steps.
+constexpr int kBwdBlock = 256;
+#ifdef __HIP__
+#define ATTN_HD __host__ __device__
+#else
+#define ATTN_HD
+#endif
+ATTN_HD inline int bwd_kv_steps(int block, int Sq, int Skv, int group, int causal) {
+    const int n_qt = (Sq + 31) / 32, reach = block * kBwdBlock - (Skv - Sq);
+    return (n_qt - (causal && reach > 0 ? reach / 32 : 0)) * group;
+}
+ATTN_HD inline int bwd_q_steps(int block, int Sq, int Skv, int causal) {
+    const int q1 = (block + 1) * kBwdBlock < Sq ? (block + 1) * kBwdBlock : Sq;
+    return ((causal ? q1 + Skv - Sq : Skv) + 31) / 32;
+}
+// Parts of a block's sum, of at most chunk steps each (0: one part).
+ATTN_HD inline int bwd_parts(int steps, int chunk) {
+    return chunk ? (steps + chunk - 1) / chunk : 1;
+}
+// Of a head's units (kv of all of them parts of key blocks), how many of the first n are.
+ATTN_HD inline int bwd_kv_before(int n, int kv, int all) {
+    return (int)(((long long)n * kv + all - 1) / all);
+}
+// Block and part of the unit-th part of all (parts(block) to each block).
+template <typename F>
+ATTN_HD inline void bwd_find_part(int unit, int blocks, F parts, int* block, int* split,
+                                  int* splits) {
+    int b = 0, n = parts(0);
+    while (b + 1 < blocks && unit >= n) {
+        unit -= n;
+        n = parts(++b);
+    }
+    *block = b;
+    *split = unit;
+    *splits = n;
+}
+
 struct BwdPlan {
-    int kv_blocks = 0, kv_splits = 1;
-    int q_blocks = 0, q_splits = 1;
+    int kv_blocks = 0, q_blocks = 0;  // of a head
+    int kv_units = 0, q_units = 0;    // their parts
+    int kv_chunk = 0, q_chunk = 0;    // steps of a part at most; 0: no block is split
+    int kv_parts = 0, q_parts = 0;    // most parts of a block (0: no block is split)
+    long long grid = 0;
+    double modeled_us = 0.0;
 };
 struct BwdArgs {
     const uint16_t* q;    // bf16 [B][Hq][Sq][D]
@@ -298,27 +338,24 @@ struct BwdArgs {
     const uint16_t* d_o;  // bf16, as o
     const float* dlse;    // as lse, or null
     float* rows;          // 64 floats for every 32 query rows (-lse log2 e, -delta)
+    void *dq, *dk, *dv;   // fp32 or bf16 (out_bf16)
     int Sq, Skv, group;
     long long q_heads, kv_heads;  // over the batch
-    int num_xcds;
+    int num_xcds, out_bf16;
     float scale;       // of either sign, or 0
     float scale_log2;  // times log2 e; not 0 (hidden * 0 would be NaN): 0 is FLT_MIN,
     float hidden;      // with which every weight is the same; a hidden pair's score, whose
                        // product with scale_log2 is -inf
-    // of the kernel that runs: blocks to a head, splits of each, and its results (fp32
-    // partials part_stride values apart where split)
-    int blocks, splits, out_bf16;
-    long long part_stride;
-    void *out0, *out1;
+    // from the plan
+    int kv_blocks, q_blocks, kv_units, q_units, kv_chunk, q_chunk;
+    float *part_k, *part_v, *part_q;  // fp32 parts, each as long as the whole result
 };
 // False where a grid would have too many workgroups.
 bool plan_bwd(int num_cus, int B, int Hq, int Hkv, int Sq, int Skv, int d, int causal,
               BwdPlan* out);
-// Workspace in floats: the row values, then the larger of the two kernels' partials.
-long long bwd_rows_floats(int B, int Hq, int Sq);
-long long bwd_part_floats(const BwdPlan& p, int B, int Hq, int Hkv, int Sq, int Skv, int d);
+// Workspace in floats: the row values, then the parts.
+long long bwd_workspace_floats(const BwdPlan& p, int B, int Hq, int Hkv, int Sq, int Skv, int d);
 hipError_t launch_bwd(const BwdPlan& p, const BwdArgs& a, int d, int causal, int o_bf16,
-                      int out_bf16, void* dq, void* dk, void* dv, float* part,
                       hipStream_t stream);
 
 // -------------------------------------------------- per-head norm, rotation --

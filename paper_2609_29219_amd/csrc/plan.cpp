@@ -26,6 +26,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <functional>
 
 #include "common.h"
 #include "fwd_primitives.inc"
@@ -1058,41 +1059,97 @@ int format_decode_plan(const DecodePlan& p, char* buf, int buflen) {
 }
 
 // ------------------------------------------------------- attention backward --
-// Workgroups keep 256 keys (dK, dV) or 256 queries (dQ).  Where there are fewer of
-// them than CUs, each one's sum is split among several, as long as a split has at
-// least four tiles of 32 to walk.
-static int bwd_splits(long long workgroups, long long steps, int num_cus) {
-    long long n = num_cus / workgroups;
-    if (n > steps / 4) n = steps / 4;
-    return n < 1 ? 1 : (int)n;
-}
+namespace {
+// Modelled times (us): a step of either kind of block, and what a workgroup takes besides
+// (launch, its own operands in, results out).
+struct BwdCosts {
+    double kv_step, q_step, workgroup;
+};
 
+// Time of the workgroups of `heads` heads on num_cus compute units, in the order in which
+// the kernel starts them, each on the unit that is free first.
+double bwd_makespan(const BwdPlan& p, const BwdCosts& c, int num_cus, int heads, int group, int Sq,
+                    int Skv, int causal) {
+    std::vector<double> kv, q;
+    for (int b = 0; b < p.kv_blocks; ++b) {
+        const int steps = bwd_kv_steps(b, Sq, Skv, group, causal), n = bwd_parts(steps, p.kv_chunk);
+        kv.insert(kv.end(), n, c.workgroup + c.kv_step * steps / n);
+    }
+    for (int b = p.q_blocks - 1; b >= 0; --b) {
+        const int steps = bwd_q_steps(b, Sq, Skv, causal), n = bwd_parts(steps, p.q_chunk);
+        q.insert(q.end(), n, c.workgroup + c.q_step * steps / n);
+    }
+    std::vector<double> free_at(num_cus, 0.0);  // a heap, earliest first
+    const int units = p.kv_units + group * p.q_units;
+    double last = 0.0;
+    for (int u = 0; u < units; ++u) {
+        const int k = bwd_kv_before(u, p.kv_units, units);
+        const double t = bwd_kv_before(u + 1, p.kv_units, units) > k ? kv[k] : q[(u - k) / group];
+        for (int h = 0; h < heads; ++h) {
+            std::pop_heap(free_at.begin(), free_at.end(), std::greater<double>());
+            last = std::max(last, free_at.back() += t);
+            std::push_heap(free_at.begin(), free_at.end(), std::greater<double>());
+        }
+    }
+    return last;
+}
+}  // namespace
+
+// Where workgroups are fewer than the compute units, or so uneven that the largest finish
+// late, the sums of blocks with many steps are split: parts of at most chunk steps go to
+// different workgroups and a last kernel adds them up.  The chunk is the fastest of the
+// model's.
 bool plan_bwd(int num_cus, int B, int Hq, int Hkv, int Sq, int Skv, int d, int causal,
               BwdPlan* out) {
-    (void)d;
-    (void)causal;
-    const long long n_qt = ((long long)Sq + 31) / 32, n_kt = ((long long)Skv + 31) / 32;
-    const long long kv_steps = n_qt * (Hq / Hkv);
+    const int group = Hq / Hkv;
+    const long long n_qt = ((long long)Sq + 31) / 32;
     BwdPlan p;
-    p.kv_blocks = (int)((n_kt + 7) / 8);
-    p.q_blocks = (int)((n_qt + 7) / 8);
-    const long long kv_wg = (long long)B * Hkv * p.kv_blocks;
-    const long long q_wg = (long long)B * Hq * p.q_blocks;
-    if (kv_steps > 0x7fffffffLL || kv_wg > 0x7fffffffLL || q_wg > 0x7fffffffLL) return false;
-    p.kv_splits = bwd_splits(kv_wg, kv_steps, num_cus);
-    p.q_splits = bwd_splits(q_wg, n_kt, num_cus);
+    p.kv_blocks = p.kv_units = (int)(((long long)Skv + kBwdBlock - 1) / kBwdBlock);
+    p.q_blocks = p.q_units = (int)(((long long)Sq + kBwdBlock - 1) / kBwdBlock);
+    const long long heads = (long long)B * Hkv;
+    const long long units = p.kv_units + (long long)group * p.q_units;
+    if (n_qt * group > 0x3fffffffLL || heads > 0x3fffffffLL || units > 0x3fffffffLL ||
+        heads * units > 0x3fffffffLL)
+        return false;
+    p.grid = heads * units;
     *out = p;
+    if (p.grid > 8LL * num_cus) return true;  // many rounds: what a split might save is small
+    const BwdCosts c = d == 64 ? BwdCosts{1.0, 0.8, 8.0} : BwdCosts{1.75, 1.4, 10.0};
+    const int most = std::max(bwd_kv_steps(0, Sq, Skv, group, causal),
+                              bwd_q_steps(p.q_blocks - 1, Sq, Skv, causal));
+    for (int n = 1; n <= 64 && (n == 1 || most / n >= 2); n = n < 8 ? n + 1 : n + n / 4) {
+        BwdPlan t = p;
+        const int chunk = (most + n - 1) / n;
+        double values = 0.0;  // of parts, written and read
+        t.kv_units = t.q_units = 0;
+        for (int b = 0; b < p.kv_blocks; ++b) {
+            const int m = bwd_parts(bwd_kv_steps(b, Sq, Skv, group, causal), chunk);
+            t.kv_units += m;
+            t.kv_parts = std::max(t.kv_parts, m);
+            if (m > 1) values += 2.0 * heads * m * kBwdBlock * d;
+        }
+        for (int b = 0; b < p.q_blocks; ++b) {
+            const int m = bwd_parts(bwd_q_steps(b, Sq, Skv, causal), chunk);
+            t.q_units += m;
+            t.q_parts = std::max(t.q_parts, m);
+            if (m > 1) values += 1.0 * heads * group * m * kBwdBlock * d;
+        }
+        t.kv_chunk = t.kv_parts > 1 ? chunk : 0;
+        t.q_chunk = t.q_parts > 1 ? chunk : 0;
+        if (!t.kv_chunk) t.kv_parts = 0;
+        if (!t.q_chunk) t.q_parts = 0;
+        t.grid = heads * (t.kv_units + (long long)group * t.q_units);
+        if (n > 1 && t.grid > 4LL * num_cus) break;
+        t.modeled_us = bwd_makespan(t, c, num_cus, (int)heads, group, Sq, Skv, causal) +
+                       (values > 0.0 ? 5.0 + values * 8.0 / 4.0e6 : 0.0);
+        if (n == 1 || t.modeled_us < out->modeled_us) *out = t;
+    }
     return true;
 }
 
-long long bwd_rows_floats(int B, int Hq, int Sq) {
-    return (long long)B * Hq * (((long long)Sq + 31) / 32) * 64;
-}
-
-long long bwd_part_floats(const BwdPlan& p, int B, int Hq, int Hkv, int Sq, int Skv, int d) {
-    const long long kv = p.kv_splits > 1 ? 2LL * p.kv_splits * B * Hkv * Skv * d : 0;
-    const long long q = p.q_splits > 1 ? (long long)p.q_splits * B * Hq * Sq * d : 0;
-    return kv > q ? kv : q;
+long long bwd_workspace_floats(const BwdPlan& p, int B, int Hq, int Hkv, int Sq, int Skv, int d) {
+    return (long long)B * Hq * (((long long)Sq + 31) / 32) * 64 +
+           2LL * p.kv_parts * B * Hkv * Skv * d + (long long)p.q_parts * B * Hq * Sq * d;
 }
 
 }  // namespace attn

@@ -159,25 +159,37 @@ constexpr int kRing = 4;  // operands in registers: read three slots ahead
 __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
+// ACC: b lies in accumulation registers, where the kernel has some to spare.
+#define ATTN_SCORE_MFMA(C) "v_mfma_f32_32x32x16_bf16 %0, %1, %2, " C
+template <bool ACC>
 __device__ __forceinline__ void score_first(f32x16& d, bf16x8 a, bf16x8 b) {
-    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0"
-                 : "=&v"(d) : "v"(a), "v"(b));
+    if constexpr (ACC)
+        asm volatile(ATTN_SCORE_MFMA("0") : "=&v"(d) : "v"(a), "a"(b));
+    else
+        asm volatile(ATTN_SCORE_MFMA("0") : "=&v"(d) : "v"(a), "v"(b));
 }
+template <bool ACC>
 __device__ __forceinline__ void score_from(f32x16& d, bf16x8 a, bf16x8 b, const f32x16& c) {
-    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %3"
-                 : "=&v"(d) : "v"(a), "v"(b), "v"(c));
+    if constexpr (ACC)
+        asm volatile(ATTN_SCORE_MFMA("%3") : "=&v"(d) : "v"(a), "a"(b), "v"(c));
+    else
+        asm volatile(ATTN_SCORE_MFMA("%3") : "=&v"(d) : "v"(a), "v"(b), "v"(c));
 }
+template <bool ACC>
 __device__ __forceinline__ void score_add(f32x16& d, bf16x8 a, bf16x8 b) {
-    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0"
-                 : "+v"(d) : "v"(a), "v"(b));
+    if constexpr (ACC)
+        asm volatile(ATTN_SCORE_MFMA("%0") : "+v"(d) : "v"(a), "a"(b));
+    else
+        asm volatile(ATTN_SCORE_MFMA("%0") : "+v"(d) : "v"(a), "v"(b));
 }
+#undef ATTN_SCORE_MFMA
 template <int N>
 __device__ __forceinline__ void settle(f32x16 (&d)[N]) {
     static_assert(N == 1 || N == 2, "");
     if constexpr (N == 2)
-        asm volatile("s_nop 15\n\ts_nop 3" : "+v"(d[0]), "+v"(d[1]));
+        asm volatile("s_nop 9" : "+v"(d[0]), "+v"(d[1]));
     else
-        asm volatile("s_nop 15\n\ts_nop 3" : "+v"(d[0]));
+        asm volatile("s_nop 9" : "+v"(d[0]));
 }
 
 // Row of accumulator register r in lane half hh.
@@ -336,19 +348,25 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
     read.init(lane);
     const uint32_t lds0 = lds_address(lds), rows0 = lds0 + 2 * 2 * TILE * 2;
     const uint32_t slab = (uint32_t)a.Sq * D * 2;
-    int load_g = begin / per_q, load_qt = qt0 + begin % per_q;  // of the next load
-    auto issue = [&](int slot) __attribute__((always_inline)) {
+    // of the next load: its head's slabs, its tile
+    int load_g = begin / per_q, load_qt = qt0 + begin % per_q;
+    dma_rsrc_t q_rsrc, g_rsrc, row_rsrc;
+    auto load_head = [&]() __attribute__((always_inline)) {
         const long long head = (long long)bh * a.group + load_g;
+        q_rsrc = make_dma_rsrc(a.q + head * a.Sq * D, slab);
+        g_rsrc = make_dma_rsrc(a.d_o + head * a.Sq * D, slab);
+        row_rsrc = make_dma_rsrc(a.rows + head * n_qt * 64, n_qt * 256);
+    };
+    load_head();
+    auto issue = [&](int slot) __attribute__((always_inline)) {
         const uint32_t dst = lds0 + slot * (2 * TILE * 2);
-        load.issue(make_dma_rsrc(a.q + head * a.Sq * D, slab), dst, load_qt * 32, a.Sq, wave);
-        load.issue(make_dma_rsrc(a.d_o + head * a.Sq * D, slab), dst + TILE * 2, load_qt * 32,
-                   a.Sq, wave);
-        if (wave == 0)
-            lds_dma4(make_dma_rsrc(a.rows + (head * n_qt + load_qt) * 64, 256), rows0 + slot * 256,
-                     lane * 4);
+        load.issue(q_rsrc, dst, load_qt * 32, a.Sq, wave);
+        load.issue(g_rsrc, dst + TILE * 2, load_qt * 32, a.Sq, wave);
+        if (wave == 0) lds_dma4(row_rsrc, rows0 + slot * 256, lane * 4, load_qt * 256);
         if (++load_qt == n_qt) {
             load_qt = qt0;
             ++load_g;
+            if (load_g < a.group) load_head();
         }
     };
 
@@ -377,6 +395,7 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
     };
     struct Scores {
         f32x16 s[KB], dp[KB];  // S, then P; dP - delta, then dS
+        f32x16 nd;             // -delta, from which the products of dP start
         f32x4 nl[2];           // -lse log2 e of eight rows
         uint32_t pk[KB][8];    // P as operand
     };
@@ -388,9 +407,10 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
         constexpr int i = decltype(i_tag)::value, kb = decltype(kb_tag)::value;
         constexpr int ph = i / KD, j = i % KD, t = j / CB, cb = j % CB;
         const bf16x8 x = ring[i % kRing];
-        if constexpr (ph == 0 && j == 0) score_first(s[kb], x, kf[kb][j]);
-        if constexpr (ph == 0 && j > 0) score_add(s[kb], x, kf[kb][j]);
-        if constexpr (ph == 1) score_add(dp[kb], x, vf[kb][j]);
+        if constexpr (ph == 0 && j == 0) score_first<D == 64>(s[kb], x, kf[kb][j]);
+        if constexpr (ph == 0 && j > 0) score_add<D == 64>(s[kb], x, kf[kb][j]);
+        if constexpr (ph == 1 && j == 0) score_from<D == 64>(dp[kb], x, vf[kb][j], x_.nd);
+        if constexpr (ph == 1 && j > 0) score_add<D == 64>(dp[kb], x, vf[kb][j]);
         if constexpr (ph >= 2) {
             const uint32_t* o = ph == 2 ? pk[kb] : dsk[kb];
             const u32x4 y = {o[4 * t], o[4 * t + 1], o[4 * t + 2], o[4 * t + 3]};
@@ -432,16 +452,11 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
             if constexpr (r % 2 == 1) dsk[kb][r / 2] = round2(dp[kb][r - 1], dp[kb][r]);
         }
     };
-    // -delta, from which the products of dP start
     auto start_dp = [&](auto r4_tag, Scores& x_) __attribute__((always_inline)) {
-        f32x16(&dp)[KB] = x_.dp;
         constexpr int r4 = decltype(r4_tag)::value;
+        const f32x4 x = lds_quad(nl_base + 128 + 32 * r4);
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-            const f32x4 x = lds_quad(nl_base + 128 + 32 * r4);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) dp[kb][4 * r4 + e] = x[e];
-        }
+        for (int e = 0; e < 4; ++e) x_.nd[4 * r4 + e] = x[e];
     };
     constexpr int TAIL = OPS - (kRing - 1);  // the last slots, behind the barrier
     auto body = [&](int q0) __attribute__((always_inline)) {
@@ -593,15 +608,15 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
         constexpr int i = decltype(i_tag)::value, qb = decltype(qb_tag)::value;
         constexpr int ph = i / KD, j = i % KD, t = j / CB, cb = j % CB;
         const bf16x8 x = ring[i % kRing];
-        if constexpr (ph == 0 && j == 0) score_first(s[qb], x, qf[qb][j]);
-        if constexpr (ph == 0 && j > 0) score_add(s[qb], x, qf[qb][j]);
+        if constexpr (ph == 0 && j == 0) score_first<true>(s[qb], x, qf[qb][j]);
+        if constexpr (ph == 0 && j > 0) score_add<true>(s[qb], x, qf[qb][j]);
         if constexpr (ph == 1) {
             const u32x4 y = {dsk[qb][4 * t], dsk[qb][4 * t + 1], dsk[qb][4 * t + 2],
                              dsk[qb][4 * t + 3]};
             dq[qb][cb] = mfma(x, __builtin_bit_cast(bf16x8, y), dq[qb][cb]);
         }
-        if constexpr (ph == 2 && j == 0) score_from(dp[qb], x, gf[qb][j], nd[qb]);
-        if constexpr (ph == 2 && j > 0) score_add(dp[qb], x, gf[qb][j]);
+        if constexpr (ph == 2 && j == 0) score_from<true>(dp[qb], x, gf[qb][j], nd[qb]);
+        if constexpr (ph == 2 && j > 0) score_add<true>(dp[qb], x, gf[qb][j]);
     };
     auto weight = [&](auto r_tag) __attribute__((always_inline)) {
         constexpr int r = decltype(r_tag)::value;
@@ -724,8 +739,9 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
 // Workgroups: for every key/value head, the parts of its blocks of keys and of the blocks
 // of queries of its group, in one launch, so that the one kind fills the other's gaps.
 // The hardware deals workgroups round-robin to the XCDs; each XCD gets whole heads, whose
-// tiles stay in its L2, where they can be dealt evenly.  Under a causal mask blocks differ:
-// the heaviest of both kinds come first, over all heads.
+// tiles stay in its L2, where they can be dealt evenly.  Blocks of keys take longer (four
+// products to three) and come first; under a causal mask blocks of one kind differ too, and
+// the heaviest of both kinds, interleaved in proportion, come first, over all heads.
 template <int D, bool CAUSAL>
 __global__ __launch_bounds__(kBwdThreads, 1) void bwd_kernel(const BwdArgs a) {
     __shared__ __attribute__((aligned(1024))) char lds[bwd_lds_bytes<D>()];
@@ -734,18 +750,29 @@ __global__ __launch_bounds__(kBwdThreads, 1) void bwd_kernel(const BwdArgs a) {
     const int hx = even ? heads / a.num_xcds : heads;
     const int first = even ? (int)(blockIdx.x % a.num_xcds) * hx : 0;
     const int i = even ? (int)(blockIdx.x / a.num_xcds) : (int)blockIdx.x;
-    const int unit = CAUSAL ? i / hx : i % units;
-    const int head = first + (CAUSAL ? i - unit * hx : i / units);
-    // the kinds are interleaved in proportion, each heaviest first
-    const int kv = bwd_kv_before(unit, a.kv_units, units);
-    if (bwd_kv_before(unit + 1, a.kv_units, units) > kv) {
+    int kv, x, head;  // index among the head's parts of key blocks (or -1), or of query blocks
+    if (CAUSAL) {
+        const int unit = i / hx;
+        head = i - unit * hx;
+        kv = bwd_kv_before(unit, a.kv_units, units);
+        x = unit - kv;
+        if (bwd_kv_before(unit + 1, a.kv_units, units) == kv) kv = -1;
+    } else {
+        const bool is_kv = i < hx * a.kv_units;
+        x = is_kv ? i : i - hx * a.kv_units;
+        const int n = is_kv ? a.kv_units : a.group * a.q_units;
+        head = x / n;
+        x -= head * n;
+        kv = is_kv ? x : -1;
+    }
+    head += first;
+    if (kv >= 0) {
         int block = kv, split = 0, splits = 1;
         if (a.kv_chunk) bwd_find_part(kv, a.kv_blocks, [&](int b) {
             return bwd_parts(bwd_kv_steps(b, a.Sq, a.Skv, a.group, CAUSAL), a.kv_chunk);
         }, &block, &split, &splits);
         dkdv_block<D, CAUSAL>(a, lds, head, block, split, splits);
     } else {
-        const int x = unit - kv;
         int block = x / a.group, split = 0, splits = 1;
         const int q_head = head * a.group + x - block * a.group;
         if (a.q_chunk) bwd_find_part(block, a.q_blocks, [&](int b) {

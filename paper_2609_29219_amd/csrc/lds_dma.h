@@ -69,19 +69,22 @@ __device__ __forceinline__ void lds_dma16(dma_rsrc_t rsrc, uint32_t lds_base, in
         : "memory", "m0");
 }
 
-// The same for 4 bytes a lane: lane i loads the word at byte voffset into lds_base + 4*i.
-__device__ __forceinline__ void lds_dma4(dma_rsrc_t rsrc, uint32_t lds_base, int voffset) {
+// The same for 4 bytes a lane: lane i loads the word at byte soffset + voffset into
+// lds_base + 4*i.
+__device__ __forceinline__ void lds_dma4(dma_rsrc_t rsrc, uint32_t lds_base, int voffset,
+                                         int soffset) {
     rsrc[0] = __builtin_amdgcn_readfirstlane(rsrc[0]);
     rsrc[1] = __builtin_amdgcn_readfirstlane(rsrc[1]);
     rsrc[2] = __builtin_amdgcn_readfirstlane(rsrc[2]);
     rsrc[3] = __builtin_amdgcn_readfirstlane(rsrc[3]);
     lds_base = __builtin_amdgcn_readfirstlane(lds_base);
+    soffset = __builtin_amdgcn_readfirstlane(soffset);
     asm volatile(
         "s_mov_b32 m0, %0\n\t"
         "s_nop 0\n\t"
-        "buffer_load_dword %1, %2, 0 offen lds"
+        "buffer_load_dword %1, %2, %3 offen lds"
         :
-        : "s"(lds_base), "v"(voffset), "s"(rsrc)
+        : "s"(lds_base), "v"(voffset), "s"(rsrc), "s"(soffset)
         : "memory", "m0");
 }
 #pragma clang diagnostic pop

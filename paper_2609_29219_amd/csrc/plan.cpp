@@ -1083,8 +1083,13 @@ double bwd_makespan(const BwdPlan& p, const BwdCosts& c, int num_cus, int heads,
     const int units = p.kv_units + group * p.q_units;
     double last = 0.0;
     for (int u = 0; u < units; ++u) {
-        const int k = bwd_kv_before(u, p.kv_units, units);
-        const double t = bwd_kv_before(u + 1, p.kv_units, units) > k ? kv[k] : q[(u - k) / group];
+        int k = u < p.kv_units ? u : -1, x = u - p.kv_units;
+        if (causal) {
+            k = bwd_kv_before(u, p.kv_units, units);
+            x = u - k;
+            if (bwd_kv_before(u + 1, p.kv_units, units) == k) k = -1;
+        }
+        const double t = k >= 0 ? kv[k] : q[x / group];
         for (int h = 0; h < heads; ++h) {
             std::pop_heap(free_at.begin(), free_at.end(), std::greater<double>());
             last = std::max(last, free_at.back() += t);

@@ -146,7 +146,20 @@ __device__ __forceinline__ void here(T& x) {
 // other work); nothing moves from one slot to another.
 __device__ __forceinline__ void slot_end() { __builtin_amdgcn_sched_barrier(0); }
 
-constexpr int kRing = 4;  // operands in registers: read three slots ahead
+// Operands are read into a ring of registers, some slots ahead.  ahead: operands that
+// have been asked for by the end of the reads of slot i.
+template <int D>
+struct KvRing {
+    static constexpr int SIZE = D == 64 ? 8 : 4, OPS = D / 4;
+    static constexpr int ahead(int i) { return i + (D == 64 ? 5 : 4); }
+    static_assert(OPS - ahead(0) + 1 >= 3 * D / 16, "dS is done before the last slots");
+};
+template <int D>
+struct QRing {
+    static constexpr int SIZE = D == 64 ? 4 : 8, OPS = 3 * D / 16;
+    static constexpr int ahead(int i) { return i + (D == 64 ? 4 : 7); }
+    static_assert(OPS - ahead(0) + 1 > 2 * D / 16, "and the weights");
+};
 
 // The gradients' accumulators fill the accumulation registers, and the scores must stay
 // out of them: the VALU cannot read those, and the compiler, left to itself, puts every
@@ -249,12 +262,42 @@ __device__ __forceinline__ void store_rows(const f32x16 (&x)[D / 32], char* stag
     }
 }
 
-// LDS of a workgroup: two tiles of Q and dO and their row values, or three of K and V;
-// at the end, the waves' stages.
+// LDS of a workgroup, in bytes: row values, then slots of a pair of tiles each (Q and dO:
+// 2, K and V: 3).  At the start the waves' own 64 rows of both their operands come through
+// the place from the second slot on; at the end the results through the stages.
 template <int D>
-constexpr int bwd_lds_bytes() {
-    constexpr int tiles = 3 * 2 * 32 * D * 2, stages = kBwdWaves * stage_bytes<D>();
-    return tiles > stages ? tiles : stages;
+struct BwdLds {
+    static constexpr int TILE = 32 * D * 2, SLOT = 2 * TILE;
+    static constexpr int SLOTS = 1024, OWN = SLOTS + SLOT;
+    static constexpr int STAGES = kBwdWaves * stage_bytes<D>();
+    static constexpr int BYTES = OWN + kBwdWaves * 4 * TILE;
+    static_assert(BYTES >= SLOTS + 3 * SLOT && BYTES >= STAGES, "");
+};
+
+// A wave's own 64 rows of a head's slab as operand registers: op[b][ks] holds row l%32 of
+// the b-th 32, values 16*ks + 8*(l/32) ..+7.  Loaded straight into registers, an
+// instruction touches 32 rows, 32 bytes each, and the operands of a workgroup took 5.8 us;
+// through LDS in whole rows they take 3.  own_load issues the loads, own_read reads what
+// has landed.
+template <int D>
+__device__ __forceinline__ void own_load(dma_rsrc_t rsrc, uint32_t lds, int row0, int n_rows,
+                                         int lane) {
+    constexpr int ROWS = 512 / D;
+#pragma unroll
+    for (int p = 0; p < 64 / ROWS; ++p) {
+        const int r = p * ROWS + lane / (D / 8);
+        const int c = (lane % (D / 8)) ^ tile_swizzle<D>(r & 31);
+        lds_dma16(rsrc, lds + p * 1024, min(row0 + r, n_rows - 1) * (D * 2) + c * 16, 0);
+    }
+}
+template <int D>
+__device__ __forceinline__ void own_read(bf16x8 (&op)[2][D / 16], const TileRead<D>& read,
+                                         uint32_t lds) {
+    static_for<0, D / 16>([&](auto ks) __attribute__((always_inline)) {
+        op[0][ks] = TileRead<D>::template by_row<decltype(ks)::value>(read.row + lds, 0);
+        op[1][ks] = TileRead<D>::template by_row<decltype(ks)::value>(read.row + lds,
+                                                                      BwdLds<D>::TILE);
+    });
 }
 
 // ------------------------------------------------------------- row values --
@@ -313,23 +356,14 @@ __global__ __launch_bounds__(256) void bwd_rows_kernel(const BwdArgs a) {
 template <int D, bool CAUSAL>
 __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, int block,
                                            int split, int splits) {
-    constexpr int KB = 2, KD = D / 16, CB = D / 32, TILE = 32 * D;
+    constexpr int KB = 2, KD = D / 16, CB = D / 32;
+    typedef BwdLds<D> L;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int k0 = block * kBwdBlock;
     const int wk0 = k0 + wave * 32 * KB;  // first key of the wave
 
     bf16x8 kf[KB][KD], vf[KB][KD];  // B operands: lane l holds key l%32
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-        const long long at =
-            ((long long)bh * a.Skv + min(wk0 + kb * 32 + l32, a.Skv - 1)) * D + hh * 8;
-#pragma unroll
-        for (int ks = 0; ks < KD; ++ks) {
-            kf[kb][ks] = *reinterpret_cast<const bf16x8*>(a.k + at + ks * 16);
-            vf[kb][ks] = *reinterpret_cast<const bf16x8*>(a.v + at + ks * 16);
-        }
-    }
     f32x16 dk[KB][CB] = {}, dv[KB][CB] = {};
 
     // steps: query tiles of every head of the group, from the first that reaches the
@@ -346,7 +380,7 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
     load.init(wave, lane);
     TileRead<D> read;
     read.init(lane);
-    const uint32_t lds0 = lds_address(lds), rows0 = lds0 + 2 * 2 * TILE * 2;
+    const uint32_t rows0 = lds_address(lds), lds0 = rows0 + L::SLOTS;
     const uint32_t slab = (uint32_t)a.Sq * D * 2;
     // of the next load: its head's slabs, its tile
     int load_g = begin / per_q, load_qt = qt0 + begin % per_q;
@@ -359,9 +393,9 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
     };
     load_head();
     auto issue = [&](int slot) __attribute__((always_inline)) {
-        const uint32_t dst = lds0 + slot * (2 * TILE * 2);
+        const uint32_t dst = lds0 + slot * L::SLOT;
         load.issue(q_rsrc, dst, load_qt * 32, a.Sq, wave);
-        load.issue(g_rsrc, dst + TILE * 2, load_qt * 32, a.Sq, wave);
+        load.issue(g_rsrc, dst + L::TILE, load_qt * 32, a.Sq, wave);
         if (wave == 0) lds_dma4(row_rsrc, rows0 + slot * 256, lane * 4, load_qt * 256);
         if (++load_qt == n_qt) {
             load_qt = qt0;
@@ -372,12 +406,14 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
 
     // Operand i of a tile, in the order of use: Q by rows (S), dO by rows (dP), dO
     // transposed (dV), Q transposed (dK); KD of each.
-    constexpr int OPS = 4 * KD;
-    bf16x8 ring[kRing];
+    typedef KvRing<D> Ring;
+    constexpr int OPS = Ring::OPS, RING = Ring::SIZE;
+    static_assert(OPS == 4 * KD && OPS % RING == 0, "");
+    bf16x8 ring[RING];
     uint32_t row_base, col_base, nl_base;  // of the tile that is read
     auto tile_bases = [&](int slot) __attribute__((always_inline)) {
-        row_base = read.row + lds0 + slot * (2 * TILE * 2);
-        col_base = read.col + lds0 + slot * (2 * TILE * 2);
+        row_base = read.row + lds0 + slot * L::SLOT;
+        col_base = read.col + lds0 + slot * L::SLOT;
         nl_base = rows0 + slot * 256 + 16 * hh;
         // opaque, so that the XORed addresses are formed where they are used instead of
         // being kept in registers over the whole loop
@@ -385,13 +421,13 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
     };
     auto fetch = [&](auto i_tag) __attribute__((always_inline)) {
         constexpr int i = decltype(i_tag)::value, ph = i / KD, j = i % KD;
-        if constexpr (ph == 0) ring[i % kRing] = TileRead<D>::template by_row<j>(row_base, 0);
+        if constexpr (ph == 0) ring[i % RING] = TileRead<D>::template by_row<j>(row_base, 0);
         if constexpr (ph == 1)
-            ring[i % kRing] = TileRead<D>::template by_row<j>(row_base, TILE * 2);
+            ring[i % RING] = TileRead<D>::template by_row<j>(row_base, L::TILE);
         if constexpr (ph == 2)
-            ring[i % kRing] = TileRead<D>::template by_col<j % CB, j / CB>(col_base, TILE * 2);
+            ring[i % RING] = TileRead<D>::template by_col<j % CB, j / CB>(col_base, L::TILE);
         if constexpr (ph == 3)
-            ring[i % kRing] = TileRead<D>::template by_col<j % CB, j / CB>(col_base, 0);
+            ring[i % RING] = TileRead<D>::template by_col<j % CB, j / CB>(col_base, 0);
     };
     struct Scores {
         f32x16 s[KB], dp[KB];  // S, then P; dP - delta, then dS
@@ -406,7 +442,7 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
         uint32_t(&pk)[KB][8] = x_.pk;
         constexpr int i = decltype(i_tag)::value, kb = decltype(kb_tag)::value;
         constexpr int ph = i / KD, j = i % KD, t = j / CB, cb = j % CB;
-        const bf16x8 x = ring[i % kRing];
+        const bf16x8 x = ring[i % RING];
         if constexpr (ph == 0 && j == 0) score_first<D == 64>(s[kb], x, kf[kb][j]);
         if constexpr (ph == 0 && j > 0) score_add<D == 64>(s[kb], x, kf[kb][j]);
         if constexpr (ph == 1 && j == 0) score_from<D == 64>(dp[kb], x, vf[kb][j], x_.nd);
@@ -449,7 +485,10 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
             dp[kb][r] *= s[kb][r];
-            if constexpr (r % 2 == 1) dsk[kb][r / 2] = round2(dp[kb][r - 1], dp[kb][r]);
+            if constexpr (r % 2 == 1) {
+                dsk[kb][r / 2] = round2(dp[kb][r - 1], dp[kb][r]);
+                here(dsk[kb][r / 2]);
+            }
         }
     };
     auto start_dp = [&](auto r4_tag, Scores& x_) __attribute__((always_inline)) {
@@ -458,12 +497,12 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
 #pragma unroll
         for (int e = 0; e < 4; ++e) x_.nd[4 * r4 + e] = x[e];
     };
-    constexpr int TAIL = OPS - (kRing - 1);  // the last slots, behind the barrier
+    constexpr int TAIL = OPS - Ring::ahead(0) + 1;  // the last slots, behind the barrier
     auto body = [&](int q0) __attribute__((always_inline)) {
         Scores x;
         static_for<0, TAIL>([&](auto i_tag) __attribute__((always_inline)) {
             constexpr int i = decltype(i_tag)::value, ph = i / KD, j = i % KD;
-            fetch(std::integral_constant<int, i + kRing - 1>{});
+            static_for<Ring::ahead(i - 1), Ring::ahead(i)>(fetch);
             if constexpr (ph == 0 && j >= KD - 4) 
                 start_dp(std::integral_constant<int, j - (KD - 4)>{}, x);
             if constexpr (ph == 0 && j == KD - 1) {
@@ -485,6 +524,7 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
                 if constexpr (ph == 2 && j > 0)
                     static_for<(gap - KB) * 16 / (n - KB), (gap - KB + 1) * 16 / (n - KB)>(
                         [&](auto r) __attribute__((always_inline)) { grad(r, x); });
+                slot_end();
             });
             if constexpr (ph == 1 && j == 0) {
                 settle(x.s);
@@ -497,10 +537,20 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
 
     int qt = load_qt;
     issue(0);  // (a part has at least one step)
+    {
+        const uint32_t own = rows0 + L::OWN + wave * (4 * L::TILE);
+        const uint32_t slab = (uint32_t)a.Skv * D * 2;
+        const long long at = (long long)bh * a.Skv * D;
+        own_load<D>(make_dma_rsrc(a.k + at, slab), own, wk0, a.Skv, lane);
+        own_load<D>(make_dma_rsrc(a.v + at, slab), own + 2 * L::TILE, wk0, a.Skv, lane);
+        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+        own_read<D>(kf, read, own);
+        own_read<D>(vf, read, own + 2 * L::TILE);
+    }
+    publish_barrier<0>();  // (all have read their own: its place is free)
     if (begin + 1 < end) issue(1);
-    publish_barrier<0>();
     tile_bases(0);
-    static_for<0, kRing - 1>(fetch);
+    static_for<0, Ring::ahead(-1)>(fetch);
     for (int step = begin; step < end; ++step) {
         const int slot = (step - begin) & 1;
         // (a wave whose keys are all hidden computes zeros: it would only wait)
@@ -516,7 +566,7 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
             constexpr int i = decltype(i_tag)::value;
             static_for<0, KB>(
                 [&](auto kb_tag) __attribute__((always_inline)) { product(i_tag, kb_tag, none); });
-            fetch(std::integral_constant<int, i + kRing - 1 - OPS>{});
+            static_for<Ring::ahead(i - 1) - OPS, Ring::ahead(i) - OPS>(fetch);
             slot_end();
         });
     }
@@ -541,8 +591,8 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
 template <int D, bool CAUSAL>
 __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, int block,
                                          int split, int splits) {
-    constexpr int QB = 2, KD = D / 16, CB = D / 32, TILE = 32 * D;
-    constexpr int SLOT = 2 * TILE * 2;  // bytes of a tile of K and one of V
+    constexpr int QB = 2, KD = D / 16, CB = D / 32;
+    typedef BwdLds<D> L;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wq0 = block * kBwdBlock + wave * 32 * QB;  // first query of the wave
@@ -554,12 +604,6 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
         const int q = wq0 + qb * 32 + l32;
-        const long long at = ((long long)bh * a.Sq + min(q, a.Sq - 1)) * D + hh * 8;
-#pragma unroll
-        for (int ks = 0; ks < KD; ++ks) {
-            qf[qb][ks] = *reinterpret_cast<const bf16x8*>(a.q + at + ks * 16);
-            gf[qb][ks] = *reinterpret_cast<const bf16x8*>(a.d_o + at + ks * 16);
-        }
         // (queries past Sq: the last tile's padding, or the last row of all)
         const long long tile = (long long)bh * n_qt + min(q, n_qt * 32 - 1) / 32;
         nl[qb] = a.rows[tile * 64 + l32];
@@ -578,36 +622,38 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
     load.init(wave, lane);
     TileRead<D> read;
     read.init(lane);
-    const uint32_t lds0 = lds_address(lds);
+    const uint32_t lds0 = lds_address(lds) + L::SLOTS;
     const uint32_t slab = (uint32_t)a.Skv * D * 2;
     const long long head = bh / a.group;
     const dma_rsrc_t k_rsrc = make_dma_rsrc(a.k + head * a.Skv * D, slab);
     const dma_rsrc_t v_rsrc = make_dma_rsrc(a.v + head * a.Skv * D, slab);
     auto issue = [&](int step, int slot) __attribute__((always_inline)) {
-        const uint32_t dst = lds0 + slot * SLOT;
+        const uint32_t dst = lds0 + slot * L::SLOT;
         load.issue(k_rsrc, dst, step * 32, a.Skv, wave);
-        load.issue(v_rsrc, dst + TILE * 2, step * 32, a.Skv, wave);
+        load.issue(v_rsrc, dst + L::TILE, step * 32, a.Skv, wave);
     };
 
     // Operand i of a step: K by rows (S of this tile), K transposed (dQ of the tile before:
     // its dS is formed during the products of S), V by rows (dP of this tile); KD of each.
-    constexpr int OPS = 3 * KD;
-    bf16x8 ring[kRing];
+    typedef QRing<D> Ring;
+    constexpr int OPS = Ring::OPS, RING = Ring::SIZE;
+    static_assert(OPS == 3 * KD && OPS % RING == 0, "");
+    bf16x8 ring[RING];
     uint32_t row_base, col_base;
     auto fetch = [&](auto i_tag) __attribute__((always_inline)) {
         constexpr int i = decltype(i_tag)::value, ph = i / KD, j = i % KD;
-        if constexpr (ph == 0) ring[i % kRing] = TileRead<D>::template by_row<j>(row_base, 0);
+        if constexpr (ph == 0) ring[i % RING] = TileRead<D>::template by_row<j>(row_base, 0);
         if constexpr (ph == 1)
-            ring[i % kRing] = TileRead<D>::template by_col<j % CB, j / CB>(col_base, 0);
+            ring[i % RING] = TileRead<D>::template by_col<j % CB, j / CB>(col_base, 0);
         if constexpr (ph == 2)
-            ring[i % kRing] = TileRead<D>::template by_row<j>(row_base, TILE * 2);
+            ring[i % RING] = TileRead<D>::template by_row<j>(row_base, L::TILE);
     };
     f32x16 s[QB], p[QB] = {}, dp[QB] = {};  // (no tile before the first: its dS is 0)
     uint32_t dsk[QB][8];  // dS as operands
     auto product = [&](auto i_tag, auto qb_tag) __attribute__((always_inline)) {
         constexpr int i = decltype(i_tag)::value, qb = decltype(qb_tag)::value;
         constexpr int ph = i / KD, j = i % KD, t = j / CB, cb = j % CB;
-        const bf16x8 x = ring[i % kRing];
+        const bf16x8 x = ring[i % RING];
         if constexpr (ph == 0 && j == 0) score_first<true>(s[qb], x, qf[qb][j]);
         if constexpr (ph == 0 && j > 0) score_add<true>(s[qb], x, qf[qb][j]);
         if constexpr (ph == 1) {
@@ -650,22 +696,23 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
         }
     };
     constexpr int N = QB * KD;  // products, and the gaps behind them, of one kind
-    constexpr int TAIL = OPS - (kRing - 1);  // the last slots, behind the barrier
+    constexpr int TAIL = OPS - Ring::ahead(0) + 1;  // the last slots, behind the barrier
     auto body = [&](int k0) __attribute__((always_inline)) {
         static_for<0, TAIL>([&](auto i_tag) __attribute__((always_inline)) {
             constexpr int i = decltype(i_tag)::value, ph = i / KD, j = i % KD;
-            fetch(std::integral_constant<int, i + kRing - 1>{});
+            static_for<Ring::ahead(i - 1), Ring::ahead(i)>(fetch);
             static_for<0, QB>([&](auto qb_tag) __attribute__((always_inline)) {
                 product(i_tag, qb_tag);
                 // dS of the tile before in the gaps of S; 12 of the 16 rows' weights in those
                 // of dQ, 4 in those of dP; the first slots are left to settle
                 constexpr int gap = j * QB + decltype(qb_tag)::value;
-                constexpr int M = N - QB, B = N - QB * (kRing - 1);
+                constexpr int M = N - QB, B = N - QB * (OPS - TAIL);
                 if constexpr (ph == 0 && j > 0)
                     static_for<(gap - QB) * 16 / M, (gap - QB + 1) * 16 / M>(grad);
                 if constexpr (ph == 1 && j > 0)
                     static_for<(gap - QB) * 12 / M, (gap - QB + 1) * 12 / M>(weight);
                 if constexpr (ph == 2) static_for<12 + gap * 4 / B, 12 + (gap + 1) * 4 / B>(weight);
+                slot_end();
             });
             if constexpr (ph == 0 && j == 0) settle(dp);
             if constexpr (ph == 1 && j == 0) {
@@ -679,11 +726,10 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
     auto drain = [&]() __attribute__((always_inline)) {
         settle(dp);
         static_for<0, 16>(grad);
-        static_for<KD, KD + kRing - 1>(fetch);
+        static_for<KD, KD + 3>(fetch);
         static_for<KD, 2 * KD>([&](auto i_tag) __attribute__((always_inline)) {
             constexpr int i = decltype(i_tag)::value;
-            if constexpr (i + kRing - 1 < 2 * KD)
-                fetch(std::integral_constant<int, i + kRing - 1>{});
+            if constexpr (i + 3 < 2 * KD) fetch(std::integral_constant<int, i + 3>{});
             static_for<0, QB>(
                 [&](auto qb_tag) __attribute__((always_inline)) { product(i_tag, qb_tag); });
             slot_end();
@@ -692,17 +738,27 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
 
     int slot = 0;
     issue(begin, 0);  // (a part has at least one step)
+    {
+        const uint32_t own = lds_address(lds) + L::OWN + wave * (4 * L::TILE);
+        const uint32_t slab = (uint32_t)a.Sq * D * 2;
+        const long long at = (long long)bh * a.Sq * D;
+        own_load<D>(make_dma_rsrc(a.q + at, slab), own, wq0, a.Sq, lane);
+        own_load<D>(make_dma_rsrc(a.d_o + at, slab), own + 2 * L::TILE, wq0, a.Sq, lane);
+        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+        own_read<D>(qf, read, own);
+        own_read<D>(gf, read, own + 2 * L::TILE);
+    }
+    publish_barrier<0>();  // (all have read their own: its place is free)
     if (begin + 1 < end) issue(begin + 1, 1);
-    publish_barrier<0>();
     row_base = read.row + lds0;
-    static_for<0, kRing - 1>(fetch);
+    static_for<0, Ring::ahead(-1)>(fetch);
     for (int step = begin; step < end; ++step) {
         // (before the first tile: itself, with a dS of 0)
         const int prev = slot == 0 ? 2 : slot - 1, next = slot == 2 ? 0 : slot + 1;
         // opaque, so that the XORed addresses are formed where they are used instead of
         // being kept in registers over the whole loop
-        row_base = read.row + lds0 + slot * SLOT;
-        col_base = read.col + lds0 + (step == begin ? slot : prev) * SLOT;
+        row_base = read.row + lds0 + slot * L::SLOT;
+        col_base = read.col + lds0 + (step == begin ? slot : prev) * L::SLOT;
         asm volatile("" : "+v"(row_base), "+v"(col_base));
         // (a wave whose pairs are all hidden computes zeros: it would only wait)
         body(step * 32);
@@ -710,18 +766,18 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
         // which also publishes the next tile.
         publish_barrier<0>();
         if (step + 2 < end) issue(step + 2, prev);
-        row_base = read.row + lds0 + next * SLOT;
+        row_base = read.row + lds0 + next * L::SLOT;
         asm volatile("" : "+v"(row_base));
         static_for<TAIL, OPS>([&](auto i_tag) __attribute__((always_inline)) {
             constexpr int i = decltype(i_tag)::value;
             static_for<0, QB>(
                 [&](auto qb_tag) __attribute__((always_inline)) { product(i_tag, qb_tag); });
-            fetch(std::integral_constant<int, i + kRing - 1 - OPS>{});
+            static_for<Ring::ahead(i - 1) - OPS, Ring::ahead(i) - OPS>(fetch);
             slot_end();
         });
         slot = next;
     }
-    col_base = read.col + lds0 + (slot == 0 ? 2 : slot - 1) * SLOT;
+    col_base = read.col + lds0 + (slot == 0 ? 2 : slot - 1) * L::SLOT;
     drain();
 
     __syncthreads();  // the stages overlay the tiles
@@ -744,7 +800,7 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
 // the heaviest of both kinds, interleaved in proportion, come first, over all heads.
 template <int D, bool CAUSAL>
 __global__ __launch_bounds__(kBwdThreads, 1) void bwd_kernel(const BwdArgs a) {
-    __shared__ __attribute__((aligned(1024))) char lds[bwd_lds_bytes<D>()];
+    __shared__ __attribute__((aligned(1024))) char lds[BwdLds<D>::BYTES];
     const int heads = (int)a.kv_heads, units = a.kv_units + a.group * a.q_units;
     const bool even = heads % a.num_xcds == 0;
     const int hx = even ? heads / a.num_xcds : heads;

@@ -37,6 +37,7 @@
 // Roundings: P and dS to bf16, as operands; everything else is fp32 until the result.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <string.h>
 
 #include <type_traits>
 
@@ -796,8 +797,9 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
 // of queries of its group, in one launch, so that the one kind fills the other's gaps.
 // The hardware deals workgroups round-robin to the XCDs; each XCD gets whole heads, whose
 // tiles stay in its L2, where they can be dealt evenly.  Blocks of keys take longer (four
-// products to three) and come first; under a causal mask blocks of one kind differ too, and
-// the heaviest of both kinds, interleaved in proportion, come first, over all heads.
+// products to three) and come first; under a causal mask, the longest parts of both kinds,
+// over all heads, as the plan names them, or where those would be too many, the blocks of
+// both kinds interleaved in proportion.
 template <int D, bool CAUSAL>
 __global__ __launch_bounds__(kBwdThreads, 1) void bwd_kernel(const BwdArgs a) {
     __shared__ __attribute__((aligned(1024))) char lds[BwdLds<D>::BYTES];
@@ -806,36 +808,51 @@ __global__ __launch_bounds__(kBwdThreads, 1) void bwd_kernel(const BwdArgs a) {
     const int hx = even ? heads / a.num_xcds : heads;
     const int first = even ? (int)(blockIdx.x % a.num_xcds) * hx : 0;
     const int i = even ? (int)(blockIdx.x / a.num_xcds) : (int)blockIdx.x;
-    int kv, x, head;  // index among the head's parts of key blocks (or -1), or of query blocks
-    if (CAUSAL) {
-        const int unit = i / hx;
-        head = i - unit * hx;
-        kv = bwd_kv_before(unit, a.kv_units, units);
-        x = unit - kv;
-        if (bwd_kv_before(unit + 1, a.kv_units, units) == kv) kv = -1;
+    // this workgroup: kind, key/value head, head of its group, block, part of how many
+    bool is_kv;
+    int head, g = 0, block, split = 0, splits = 1;
+    if (CAUSAL && a.ordered) {
+        const BwdUnit u = a.order[i / hx];
+        head = i % hx;
+        is_kv = u.kv;
+        g = u.g;
+        block = u.block;
+        split = u.split;
+        splits = is_kv ? bwd_parts(bwd_kv_steps(block, a.Sq, a.Skv, a.group, true), a.kv_chunk)
+                       : bwd_parts(bwd_q_steps(block, a.Sq, a.Skv, true), a.q_chunk);
     } else {
-        const bool is_kv = i < hx * a.kv_units;
-        x = is_kv ? i : i - hx * a.kv_units;
-        const int n = is_kv ? a.kv_units : a.group * a.q_units;
-        head = x / n;
-        x -= head * n;
-        kv = is_kv ? x : -1;
+        int x;  // among the head's units of the kind
+        if (CAUSAL) {  // many units, none of them split
+            const int unit = i / hx;
+            head = i - unit * hx;
+            x = bwd_kv_before(unit, a.kv_units, units);
+            is_kv = bwd_kv_before(unit + 1, a.kv_units, units) > x;
+            if (!is_kv) x = unit - x;
+        } else {
+            is_kv = i < hx * a.kv_units;
+            x = is_kv ? i : i - hx * a.kv_units;
+            const int n = is_kv ? a.kv_units : a.group * a.q_units;
+            head = x / n;
+            x -= head * n;
+        }
+        block = x;
+        if (!is_kv) {
+            block = x / a.group;
+            g = x - block * a.group;
+        }
+        if (!CAUSAL && (is_kv ? a.kv_chunk : a.q_chunk)) {  // all blocks of a kind alike
+            splits = is_kv ? bwd_parts(bwd_kv_steps(0, a.Sq, a.Skv, a.group, false), a.kv_chunk)
+                           : bwd_parts(bwd_q_steps(0, a.Sq, a.Skv, false), a.q_chunk);
+            split = block % splits;
+            block /= splits;
+        }
+        if (!is_kv) block = a.q_blocks - 1 - block;
     }
     head += first;
-    if (kv >= 0) {
-        int block = kv, split = 0, splits = 1;
-        if (a.kv_chunk) bwd_find_part(kv, a.kv_blocks, [&](int b) {
-            return bwd_parts(bwd_kv_steps(b, a.Sq, a.Skv, a.group, CAUSAL), a.kv_chunk);
-        }, &block, &split, &splits);
+    if (is_kv)
         dkdv_block<D, CAUSAL>(a, lds, head, block, split, splits);
-    } else {
-        int block = x / a.group, split = 0, splits = 1;
-        const int q_head = head * a.group + x - block * a.group;
-        if (a.q_chunk) bwd_find_part(block, a.q_blocks, [&](int b) {
-            return bwd_parts(bwd_q_steps(a.q_blocks - 1 - b, a.Sq, a.Skv, CAUSAL), a.q_chunk);
-        }, &block, &split, &splits);
-        dq_block<D, CAUSAL>(a, lds, q_head, a.q_blocks - 1 - block, split, splits);
-    }
+    else
+        dq_block<D, CAUSAL>(a, lds, head * a.group + g, block, split, splits);
 }
 
 // Adds up the parts of the blocks that have several, in their order, four values to a
@@ -902,6 +919,8 @@ hipError_t launch_bwd(const BwdPlan& p, const BwdArgs& args, int d, int causal, 
     a.q_blocks = p.q_blocks;
     a.q_units = p.q_units;
     a.q_chunk = p.q_chunk;
+    a.ordered = p.ordered;
+    if (p.ordered) memcpy(a.order, p.order, sizeof a.order);
     // the parts follow the row values
     const long long kv_values = a.kv_heads * a.Skv * d;
     a.part_k = a.rows + a.q_heads * ((a.Sq + 31) / 32) * 64;

@@ -307,21 +307,16 @@ ATTN_HD inline int bwd_parts(int steps, int chunk) {
 ATTN_HD inline int bwd_kv_before(int n, int kv, int all) {
     return (int)(((long long)n * kv + all - 1) / all);
 }
-// Block and part of the unit-th part of all (parts(block) to each block).
-template <typename F>
-ATTN_HD inline void bwd_find_part(int unit, int blocks, F parts, int* block, int* split,
-                                  int* splits) {
-    int b = 0, n = parts(0);
-    while (b + 1 < blocks && unit >= n) {
-        unit -= n;
-        n = parts(++b);
-    }
-    *block = b;
-    *split = unit;
-    *splits = n;
-}
-
+// Causal blocks differ in length: the longest parts start first.  Up to kBwdOrder units
+// are named in that order (more need no exact one: interleaved in proportion, heavy blocks
+// first): of a key/value head's, kind (1: keys), head of the group, block, part.
+constexpr int kBwdOrder = 512;
+struct BwdUnit {
+    uint16_t kv : 1, g : 15, block, split;
+};
 struct BwdPlan {
+    BwdUnit order[kBwdOrder];
+    int ordered = 0;
     int kv_blocks = 0, q_blocks = 0;  // of a head
     int kv_units = 0, q_units = 0;    // their parts
     int kv_chunk = 0, q_chunk = 0;    // steps of a part at most; 0: no block is split
@@ -347,7 +342,8 @@ struct BwdArgs {
     float hidden;      // with which every weight is the same; a hidden pair's score, whose
                        // product with scale_log2 is -inf
     // from the plan
-    int kv_blocks, q_blocks, kv_units, q_units, kv_chunk, q_chunk;
+    int kv_blocks, q_blocks, kv_units, q_units, kv_chunk, q_chunk, ordered;
+    BwdUnit order[kBwdOrder];
     float *part_k, *part_v, *part_q;  // fp32 parts, each as long as the whole result
 };
 // False where a grid would have too many workgroups.

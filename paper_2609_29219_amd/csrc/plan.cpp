@@ -1066,44 +1066,69 @@ struct BwdCosts {
     double kv_step, q_step, workgroup;
 };
 
+// Names the plan's units in the order of their lengths, longest first, if they are few.
+void bwd_order(BwdPlan* p, const BwdCosts& c, int group, int Sq, int Skv, int causal) {
+    const long long units = p->kv_units + (long long)group * p->q_units;
+    p->ordered = causal && units <= kBwdOrder && p->kv_blocks < 65536 && group < 32768;
+    if (!p->ordered) return;
+    std::vector<std::pair<double, BwdUnit>> all;
+    for (int b = 0; b < p->kv_blocks; ++b) {
+        const int steps = bwd_kv_steps(b, Sq, Skv, group, causal), n = bwd_parts(steps, p->kv_chunk);
+        for (int i = 0; i < n; ++i)
+            all.push_back({c.kv_step * steps / n, {1, 0, (uint16_t)b, (uint16_t)i}});
+    }
+    for (int b = p->q_blocks - 1; b >= 0; --b) {
+        const int steps = bwd_q_steps(b, Sq, Skv, causal), n = bwd_parts(steps, p->q_chunk);
+        for (int i = 0; i < n; ++i)
+            for (int g = 0; g < group; ++g)
+                all.push_back({c.q_step * steps / n, {0, (uint16_t)g, (uint16_t)b, (uint16_t)i}});
+    }
+    std::stable_sort(all.begin(), all.end(),
+                     [](const auto& x, const auto& y) { return x.first > y.first; });
+    for (size_t i = 0; i < all.size(); ++i) p->order[i] = all[i].second;
+}
+
 // Time of the workgroups of `heads` heads on num_cus compute units, in the order in which
 // the kernel starts them, each on the unit that is free first.
 double bwd_makespan(const BwdPlan& p, const BwdCosts& c, int num_cus, int heads, int group, int Sq,
                     int Skv, int causal) {
-    std::vector<double> kv, q;
-    for (int b = 0; b < p.kv_blocks; ++b) {
-        const int steps = bwd_kv_steps(b, Sq, Skv, group, causal), n = bwd_parts(steps, p.kv_chunk);
-        kv.insert(kv.end(), n, c.workgroup + c.kv_step * steps / n);
-    }
-    for (int b = p.q_blocks - 1; b >= 0; --b) {
-        const int steps = bwd_q_steps(b, Sq, Skv, causal), n = bwd_parts(steps, p.q_chunk);
-        q.insert(q.end(), n, c.workgroup + c.q_step * steps / n);
+    auto kv_time = [&](int b) {
+        const int steps = bwd_kv_steps(b, Sq, Skv, group, causal);
+        return c.workgroup + c.kv_step * steps / bwd_parts(steps, p.kv_chunk);
+    };
+    auto q_time = [&](int b) {
+        const int steps = bwd_q_steps(b, Sq, Skv, causal);
+        return c.workgroup + c.q_step * steps / bwd_parts(steps, p.q_chunk);
+    };
+    std::vector<double> times;  // of a head's units, in order
+    if (p.ordered) {
+        for (int u = 0; u < p.kv_units + group * p.q_units; ++u)
+            times.push_back(p.order[u].kv ? kv_time(p.order[u].block) : q_time(p.order[u].block));
+    } else {
+        for (int b = 0; b < p.kv_blocks; ++b)
+            times.insert(times.end(),
+                         bwd_parts(bwd_kv_steps(b, Sq, Skv, group, causal), p.kv_chunk), kv_time(b));
+        for (int b = p.q_blocks - 1; b >= 0; --b)
+            times.insert(times.end(),
+                         (size_t)group * bwd_parts(bwd_q_steps(b, Sq, Skv, causal), p.q_chunk),
+                         q_time(b));
     }
     std::vector<double> free_at(num_cus, 0.0);  // a heap, earliest first
-    const int units = p.kv_units + group * p.q_units;
     double last = 0.0;
-    for (int u = 0; u < units; ++u) {
-        int k = u < p.kv_units ? u : -1, x = u - p.kv_units;
-        if (causal) {
-            k = bwd_kv_before(u, p.kv_units, units);
-            x = u - k;
-            if (bwd_kv_before(u + 1, p.kv_units, units) == k) k = -1;
-        }
-        const double t = k >= 0 ? kv[k] : q[x / group];
+    for (const double t : times)
         for (int h = 0; h < heads; ++h) {
             std::pop_heap(free_at.begin(), free_at.end(), std::greater<double>());
             last = std::max(last, free_at.back() += t);
             std::push_heap(free_at.begin(), free_at.end(), std::greater<double>());
         }
-    }
     return last;
 }
 }  // namespace
 
-// Where workgroups are fewer than the compute units, or so uneven that the largest finish
-// late, the sums of blocks with many steps are split: parts of at most chunk steps go to
-// different workgroups and a last kernel adds them up.  The chunk is the fastest of the
-// model's.
+// Where workgroups are fewer than the compute units, or so uneven that the longest finish
+// late, the sums of long blocks are split: parts of about equal time go to different
+// workgroups and a last kernel adds them up.  The number of parts of the longest block is
+// the fastest of the model's.
 bool plan_bwd(int num_cus, int B, int Hq, int Hkv, int Sq, int Skv, int d, int causal,
               BwdPlan* out) {
     const int group = Hq / Hkv;
@@ -1116,37 +1141,41 @@ bool plan_bwd(int num_cus, int B, int Hq, int Hkv, int Sq, int Skv, int d, int c
     if (n_qt * group > 0x3fffffffLL || heads > 0x3fffffffLL || units > 0x3fffffffLL ||
         heads * units > 0x3fffffffLL)
         return false;
+    const BwdCosts c = d == 64 ? BwdCosts{0.95, 0.75, 6.0} : BwdCosts{1.7, 1.35, 7.0};
     p.grid = heads * units;
+    bwd_order(&p, c, group, Sq, Skv, causal);
     *out = p;
     if (p.grid > 8LL * num_cus) return true;  // many rounds: what a split might save is small
-    const BwdCosts c = d == 64 ? BwdCosts{1.0, 0.8, 8.0} : BwdCosts{1.75, 1.4, 10.0};
-    const int most = std::max(bwd_kv_steps(0, Sq, Skv, group, causal),
-                              bwd_q_steps(p.q_blocks - 1, Sq, Skv, causal));
-    for (int n = 1; n <= 64 && (n == 1 || most / n >= 2); n = n < 8 ? n + 1 : n + n / 4) {
+    const double longest =
+        std::max(c.kv_step * bwd_kv_steps(0, Sq, Skv, group, causal),
+                 c.q_step * bwd_q_steps(p.q_blocks - 1, Sq, Skv, causal));
+    for (int n = 1; n <= 64 && (n == 1 || longest / n >= 2 * c.kv_step);
+         n = n < 8 ? n + 1 : n + n / 4) {
         BwdPlan t = p;
-        const int chunk = (most + n - 1) / n;
+        t.kv_chunk = (int)ceil(longest / n / c.kv_step);
+        t.q_chunk = (int)ceil(longest / n / c.q_step);
         double values = 0.0;  // of parts, written and read
         t.kv_units = t.q_units = 0;
         for (int b = 0; b < p.kv_blocks; ++b) {
-            const int m = bwd_parts(bwd_kv_steps(b, Sq, Skv, group, causal), chunk);
+            const int m = bwd_parts(bwd_kv_steps(b, Sq, Skv, group, causal), t.kv_chunk);
             t.kv_units += m;
             t.kv_parts = std::max(t.kv_parts, m);
             if (m > 1) values += 2.0 * heads * m * kBwdBlock * d;
         }
         for (int b = 0; b < p.q_blocks; ++b) {
-            const int m = bwd_parts(bwd_q_steps(b, Sq, Skv, causal), chunk);
+            const int m = bwd_parts(bwd_q_steps(b, Sq, Skv, causal), t.q_chunk);
             t.q_units += m;
             t.q_parts = std::max(t.q_parts, m);
             if (m > 1) values += 1.0 * heads * group * m * kBwdBlock * d;
         }
-        t.kv_chunk = t.kv_parts > 1 ? chunk : 0;
-        t.q_chunk = t.q_parts > 1 ? chunk : 0;
-        if (!t.kv_chunk) t.kv_parts = 0;
-        if (!t.q_chunk) t.q_parts = 0;
+        if (t.kv_parts <= 1) t.kv_chunk = t.kv_parts = 0;
+        if (t.q_parts <= 1) t.q_chunk = t.q_parts = 0;
         t.grid = heads * (t.kv_units + (long long)group * t.q_units);
-        if (n > 1 && t.grid > 4LL * num_cus) break;
+        if (n > 1 && t.grid > 6LL * num_cus) break;
+        bwd_order(&t, c, group, Sq, Skv, causal);
+        if (causal && n > 1 && !t.ordered) break;  // the kernel finds no parts without it
         t.modeled_us = bwd_makespan(t, c, num_cus, (int)heads, group, Sq, Skv, causal) +
-                       (values > 0.0 ? 5.0 + values * 8.0 / 4.0e6 : 0.0);
+                       (values > 0.0 ? 4.0 + values * 8.0 / 6.0e6 : 0.0);
         if (n == 1 || t.modeled_us < out->modeled_us) *out = t;
     }
     return true;

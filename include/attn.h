@@ -348,8 +348,9 @@ long long attn_bwd_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Skv, int 
 /*
  * Rows of d values of a 4-dimensional tensor: head h of token s of batch b starts at
  * element b * batch_stride + s * row_stride + h * head_stride of ptr.  ptr is 16-byte
- * aligned, and the strides (not negative) are multiples of 8 elements.  An input's may
- * be 0 (broadcast); the rows of an output must not overlap.
+ * aligned, and the strides (not negative) are multiples of 8 elements, but for those of
+ * dimensions of one.  An input's may be 0 (broadcast); the rows of an output must not
+ * overlap.
  */
 typedef struct attn_heads {
     void* ptr;

@@ -14,7 +14,6 @@ device.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import math
 import os
@@ -134,9 +133,9 @@ def _load() -> ctypes.CDLL:
     lib.attn_bwd.argtypes = [vp] * 10 + [ci] * 6 + [cf, ci, ci, vp, ctypes.c_size_t]
     lib.attn_bwd_workspace_bytes.argtypes = [ci] * 7
     lib.attn_bwd_workspace_bytes.restype = ctypes.c_longlong
-    hp, ll = ctypes.POINTER(Heads), ctypes.c_longlong
-    lib.attn_qk_norm_rope.argtypes = [hp] * 6 + [vp] * 4 + [ll] + [ci] * 6 + [cf, ci]
-    lib.attn_qk_norm_rope_bwd.argtypes = [hp] * 8 + [vp] * 4 + [ll, vp, vp] + [ci] * 6 + \
+    ll = ctypes.c_longlong
+    lib.attn_qk_norm_rope.argtypes = [vp] * 6 + [vp] * 4 + [ll] + [ci] * 6 + [cf, ci]
+    lib.attn_qk_norm_rope_bwd.argtypes = [vp] * 8 + [vp] * 4 + [ll, vp, vp] + [ci] * 6 + \
         [cf, ci, vp, ctypes.c_size_t]
     lib.attn_qk_norm_rope_bwd_workspace_bytes.argtypes = [ci] * 5
     lib.attn_qk_norm_rope_bwd_workspace_bytes.restype = ctypes.c_longlong
@@ -307,23 +306,27 @@ def gemm(a, b, c=None, b_nk: bool = False, out_dtype=None):
     return c
 
 
-def _device_of(tensors):
-    """The one device of these tensors (None among them is skipped), as a context in
-    which it is the current device."""
+def _require_on(t, dtype, shape, name, dev) -> None:
+    """_require, on device dev (one expression for a good tensor)."""
     import torch
-    index = None
-    for t in tensors:
-        if t is None:
-            continue
-        if index is None:
-            index = t.get_device()
-        elif t.get_device() != index:
-            raise ValueError("all tensors must be on one device")
-    return contextlib.nullcontext() if torch.cuda.current_device() == index else \
-        torch.cuda.device(index)
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == dev and \
+            t.shape == shape and t.is_contiguous():
+        return
+    _require(t, dtype, shape, name)
+    raise ValueError(f"{name} is on another device than the first operand")
 
 
-def _workspace(workspace):
+def _call_on(dev, fn, *args) -> None:
+    """A C call on device dev and its current stream."""
+    import torch
+    if torch._C._cuda_getDevice() != dev:
+        with torch.cuda.device(dev):
+            return _call_on(dev, fn, *args)
+    lib.attn_set_stream(_raw_stream(dev))
+    _check(fn(*args))
+
+
+def _workspace(workspace, dev):
     """Address and bytes of a caller's workspace (None: the library's)."""
     import torch
     if workspace is None:
@@ -331,6 +334,8 @@ def _workspace(workspace):
     if not isinstance(workspace, torch.Tensor) or not workspace.is_cuda or \
             not workspace.is_contiguous():
         raise TypeError("workspace must be a contiguous tensor on a HIP device")
+    if workspace.get_device() != dev:
+        raise ValueError("workspace is on another device than the first operand")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
@@ -343,41 +348,47 @@ def attn_bwd(do, q, k, v, o, lse, scale: float | None = None, causal: bool = Fal
     lse, fp32 [B,Hq,Sq], or None.  workspace: None (the library's), or a device tensor of
     at least bwd_workspace_bytes(...) bytes."""
     import torch
-    B, Hq, Sq, d = q.shape
+    B, Hq, Sq, d = qs = q.shape
     Hkv, Skv = k.shape[1], k.shape[2]
+    ks = (B, Hkv, Skv, d)
     bf16, f32 = torch.bfloat16, torch.float32
-    _require(q, bf16, (B, Hq, Sq, d), "q")
-    _require(k, bf16, (B, Hkv, Skv, d), "k")
-    _require(v, bf16, (B, Hkv, Skv, d), "v")
-    _require(do, bf16, (B, Hq, Sq, d), "do")
-    _require(o, bf16 if getattr(o, "dtype", None) is bf16 else f32, (B, Hq, Sq, d), "o")
-    _require(lse, f32, (B, Hq, Sq), "lse")
+    dev = q.get_device()
+    if dev < 0:
+        raise TypeError("q must be on a HIP device")
+    _require_on(q, bf16, qs, "q", dev)
+    _require_on(k, bf16, ks, "k", dev)
+    _require_on(v, bf16, ks, "v", dev)
+    _require_on(do, bf16, qs, "do", dev)
+    o_bf16 = getattr(o, "dtype", None) is bf16
+    _require_on(o, bf16 if o_bf16 else f32, qs, "o", dev)
+    _require_on(lse, f32, (B, Hq, Sq), "lse", dev)
     if dlse is not None:
-        _require(dlse, f32, (B, Hq, Sq), "dlse")
-    given = [t for t in (dq, dk, dv) if t is not None]
+        _require_on(dlse, f32, (B, Hq, Sq), "dlse", dev)
     if out_dtype is None:
-        out_dtype = given[0].dtype if given else bf16
+        given = dq if dq is not None else dk if dk is not None else dv
+        out_dtype = bf16 if given is None else given.dtype
     if out_dtype not in (f32, bf16):
         raise ValueError("out_dtype must be torch.float32 or torch.bfloat16")
-    outs = []
-    for t, like, name in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")):
-        if t is None:
-            t = torch.empty(like.shape, dtype=out_dtype, device=q.device)
-        else:
-            _require(t, out_dtype, like.shape, name)
-        outs.append(t)
-    ws_ptr, ws_bytes = _workspace(workspace)
+    if dq is None:
+        dq = torch.empty(qs, dtype=out_dtype, device=q.device)
+    else:
+        _require_on(dq, out_dtype, qs, "dq", dev)
+    if dk is None:
+        dk = torch.empty(ks, dtype=out_dtype, device=q.device)
+    else:
+        _require_on(dk, out_dtype, ks, "dk", dev)
+    if dv is None:
+        dv = torch.empty(ks, dtype=out_dtype, device=q.device)
+    else:
+        _require_on(dv, out_dtype, ks, "dv", dev)
     if scale is None:
         scale = 1.0 / math.sqrt(d)
-    flags = (ATTN_OUT_BF16 if out_dtype == bf16 else 0) | (ATTN_O_BF16 if o.dtype == bf16 else 0)
-    with _device_of((q, k, v, do, o, lse, dlse, *outs, workspace)):
-        _set_stream(q)
-        _check(lib.attn_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
-                            lse.data_ptr(), do.data_ptr(),
-                            dlse.data_ptr() if dlse is not None else None,
-                            *[t.data_ptr() for t in outs], B, Hq, Hkv, Sq, Skv, d, float(scale),
-                            int(bool(causal)), flags, ws_ptr, ws_bytes))
-    return tuple(outs)
+    flags = (ATTN_OUT_BF16 if out_dtype is bf16 else 0) | (ATTN_O_BF16 if o_bf16 else 0)
+    _call_on(dev, lib.attn_bwd, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
+             lse.data_ptr(), do.data_ptr(), None if dlse is None else dlse.data_ptr(),
+             dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), B, Hq, Hkv, Sq, Skv, d, scale,
+             1 if causal else 0, flags, *_workspace(workspace, dev))
+    return dq, dk, dv
 
 
 def bwd_workspace_bytes(B: int, Hq: int, Hkv: int, Sq: int, Skv: int, d: int,
@@ -389,19 +400,53 @@ def bwd_workspace_bytes(B: int, Hq: int, Hkv: int, Sq: int, Skv: int, d: int,
     return int(n)
 
 
-def _rows(t, dtype, shape, dims, name):
-    """attn_heads of a 4-dimensional tensor whose batch, token and head dimensions are
-    dims, its last one contiguous (None for None)."""
+def _rows(t, dtype, shape, name, dev):
+    """A 4-dimensional tensor whose rows (last dimension) are contiguous, checked; its
+    strides."""
     import torch
-    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or not t.is_cuda:
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() < 0:
         raise TypeError(f"{name} must be a {dtype} tensor on a HIP device")
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on another device than the first operand")
     strides = t.stride()
     if strides[3] != 1:
         raise ValueError(f"{name} must be contiguous in its last dimension")
-    # (a dimension of one element has any stride)
-    return Heads(t.data_ptr(), *[strides[i] if shape[i] > 1 else 0 for i in dims])
+    return strides
+
+
+def _head_major_out(out, B, S, H, d, name, like):
+    """An output [B,H,S,d] (the given one, checked, or a new one) and its fields."""
+    import torch
+    if out is None:
+        out = torch.empty((B, H, S, d), dtype=torch.bfloat16, device=like.device)
+        return out, (out.data_ptr(), H * S * d, d, S * d)
+    return out, _head_major(out, torch.bfloat16, (B, H, S, d), name, like.get_device())
+
+
+def _token_major(t, dtype, shape, name, dev):
+    """The fields of attn_heads for [B,S,H,d]."""
+    b, s, h, _ = _rows(t, dtype, shape, name, dev)
+    return t.data_ptr(), b, s, h
+
+
+def _head_major(t, dtype, shape, name, dev):
+    """The fields of attn_heads for [B,H,S,d]."""
+    b, h, s, _ = _rows(t, dtype, shape, name, dev)
+    return t.data_ptr(), b, s, h
+
+
+_NO_HEADS = (0, 0, 0, 0)
+
+
+def _heads_array(*fields):
+    """An array of attn_heads from their fields, and the address of each (None for
+    _NO_HEADS)."""
+    flat = [x for f in fields for x in f]
+    array = (ctypes.c_longlong * len(flat))(*flat)
+    base = ctypes.addressof(array)
+    return array, [base + 32 * i if f is not _NO_HEADS else None for i, f in enumerate(fields)]
 
 
 def _rope_common(q, k, q_weight, k_weight, inv_freq, positions, interleaved):
@@ -410,15 +455,18 @@ def _rope_common(q, k, q_weight, k_weight, inv_freq, positions, interleaved):
     if q.dim() != 4 or k.dim() != 4:
         raise ValueError("q and k must be [B,S,H,d]")
     B, S, Hq, d = q.shape
-    Hkv = k.shape[2]
-    wdtype = torch.float32 if getattr(q_weight, "dtype", None) is torch.float32 else torch.bfloat16
-    _require(q_weight, wdtype, (d,), "q_weight")
-    _require(k_weight, wdtype, (d,), "k_weight")
+    dev = q.get_device()
+    if dev < 0:
+        raise TypeError("q must be on a HIP device")
+    w_f32 = getattr(q_weight, "dtype", None) is torch.float32
+    wdtype = torch.float32 if w_f32 else torch.bfloat16
+    _require_on(q_weight, wdtype, (d,), "q_weight", dev)
+    _require_on(k_weight, wdtype, (d,), "k_weight", dev)
     if not isinstance(inv_freq, torch.Tensor) or inv_freq.dim() != 1:
         raise TypeError("inv_freq must be a one-dimensional tensor")
-    _require(inv_freq, torch.float32, (inv_freq.shape[0],), "inv_freq")
-    flags = (ATTN_ROPE_INTERLEAVED if interleaved else 0) | \
-        (ATTN_WEIGHT_F32 if wdtype is torch.float32 else 0)
+    half = inv_freq.shape[0]
+    _require_on(inv_freq, torch.float32, (half,), "inv_freq", dev)
+    flags = (ATTN_ROPE_INTERLEAVED if interleaved else 0) | (ATTN_WEIGHT_F32 if w_f32 else 0)
     pos_ptr, pos_stride = None, 0
     if positions is not None:
         if not isinstance(positions, torch.Tensor) or not positions.is_cuda or \
@@ -427,17 +475,17 @@ def _rope_common(q, k, q_weight, k_weight, inv_freq, positions, interleaved):
         if positions.shape not in ((S,), (B, S)):
             raise ValueError(f"positions has shape {tuple(positions.shape)}, expected "
                              f"{(S,)} or {(B, S)}")
+        if positions.get_device() != dev:
+            raise ValueError("positions is on another device than the first operand")
         if S > 1 and positions.stride(-1) != 1:
             raise ValueError("positions must be contiguous in its last dimension")
-        if positions.dim() == 2 and B > 1:
+        if B > 1 and positions.dim() == 2:
             pos_stride = positions.stride(0)
         pos_ptr = positions.data_ptr()
-        flags |= ATTN_POSITIONS_I64 if positions.dtype is torch.int64 else 0
-    return (B, S, Hq, Hkv, d), 2 * inv_freq.shape[0], pos_ptr, pos_stride, flags
-
-
-def _ref(heads):
-    return None if heads is None else ctypes.byref(heads)
+        if positions.dtype is torch.int64:
+            flags |= ATTN_POSITIONS_I64
+    small = (q_weight.data_ptr(), k_weight.data_ptr(), inv_freq.data_ptr(), pos_ptr, pos_stride)
+    return B, S, Hq, k.shape[2], d, 2 * half, dev, flags, small
 
 
 def qk_norm_rope(q, k, v, q_weight, k_weight, inv_freq, positions=None, eps: float = 1e-6,
@@ -452,26 +500,22 @@ def qk_norm_rope(q, k, v, q_weight, k_weight, inv_freq, positions=None, eps: flo
     [B,S]; None: 0..S-1.  q_out, k_out, v_out: [B,H,S,d], any strides with contiguous rows
     (for a step of decoding, the cache's rows: k_out=cache[:, :, pos:pos + S])."""
     import torch
-    (B, S, Hq, Hkv, d), rot, pos_ptr, pos_stride, flags = _rope_common(
-        q, k, q_weight, k_weight, inv_freq, positions, interleaved)
-    if v is None and v_out is not None:
+    B, S, Hq, Hkv, d, rot, dev, flags, small = _rope_common(q, k, q_weight, k_weight, inv_freq,
+                                                            positions, interleaved)
+    bf16 = torch.bfloat16
+    q_in = _token_major(q, bf16, (B, S, Hq, d), "q", dev)
+    k_in = _token_major(k, bf16, (B, S, Hkv, d), "k", dev)
+    q_out, q_to = _head_major_out(q_out, B, S, Hq, d, "q_out", q)
+    k_out, k_to = _head_major_out(k_out, B, S, Hkv, d, "k_out", q)
+    v_in = v_to = _NO_HEADS
+    if v is not None:
+        v_in = _token_major(v, bf16, (B, S, Hkv, d), "v", dev)
+        v_out, v_to = _head_major_out(v_out, B, S, Hkv, d, "v_out", q)
+    elif v_out is not None:
         raise ValueError("v_out without v")
-    ins, outs, results = [], [], []
-    for t, out, H, name in ((q, q_out, Hq, "q"), (k, k_out, Hkv, "k"), (v, v_out, Hkv, "v")):
-        if t is None:
-            ins.append(None), outs.append(None), results.append(None)
-            continue
-        ins.append(_rows(t, torch.bfloat16, (B, S, H, d), (0, 1, 2), name))
-        if out is None:
-            out = torch.empty((B, H, S, d), dtype=torch.bfloat16, device=q.device)
-        outs.append(_rows(out, torch.bfloat16, (B, H, S, d), (0, 2, 1), name + "_out"))
-        results.append(out)
-    with _device_of((q, k, v, *results, q_weight, k_weight, inv_freq, positions)):
-        _set_stream(q)
-        _check(lib.attn_qk_norm_rope(*[_ref(h) for h in ins + outs], q_weight.data_ptr(),
-                                     k_weight.data_ptr(), inv_freq.data_ptr(), pos_ptr,
-                                     pos_stride, B, S, Hq, Hkv, d, rot, float(eps), flags))
-    return tuple(results)
+    heads, at = _heads_array(q_in, k_in, v_in, q_to, k_to, v_to)
+    _call_on(dev, lib.attn_qk_norm_rope, *at, *small, B, S, Hq, Hkv, d, rot, eps, flags)
+    return q_out, k_out, v_out
 
 
 def qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, inv_freq, positions=None,
@@ -480,47 +524,47 @@ def qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, inv_freq, positions=N
     """Gradients of qk_norm_rope; returns those of q, k and v (bf16 [B,S,H,d]) and of
     q_weight and k_weight (fp32 [d]; None without weight_grads).
 
-    dq, dk, dv: gradients of its results, bf16 or fp32 [B,H,S,d] (dv may be None); the
-    rest as qk_norm_rope got it.  dq_out, dk_out, dv_out: any strides with contiguous
-    rows; without them, they are the heads of one fused [B,S,Hq+2*Hkv,d] tensor in this
-    order.  workspace: None (the library's), or a device tensor of at least
-    qk_norm_rope_bwd_workspace_bytes(...) bytes."""
+    dq, dk, dv: gradients of its results, bf16 or fp32 [B,H,S,d], any strides with
+    contiguous rows (dv may be None); the rest as qk_norm_rope got it.  dq_out, dk_out,
+    dv_out: any strides with contiguous rows; without them, they are the heads of one fused
+    [B,S,Hq+2*Hkv,d] tensor in this order.  workspace: None (the library's), or a device
+    tensor of at least qk_norm_rope_bwd_workspace_bytes(...) bytes."""
     import torch
-    (B, S, Hq, Hkv, d), rot, pos_ptr, pos_stride, flags = _rope_common(
-        q, k, q_weight, k_weight, inv_freq, positions, interleaved)
-    if dv is None and dv_out is not None:
-        raise ValueError("dv_out without dv")
-    gdtype = torch.float32 if getattr(dq, "dtype", None) is torch.float32 else torch.bfloat16
-    flags |= ATTN_GRAD_F32 if gdtype is torch.float32 else 0
-    xs = [_rows(q, torch.bfloat16, (B, S, Hq, d), (0, 1, 2), "q"),
-          _rows(k, torch.bfloat16, (B, S, Hkv, d), (0, 1, 2), "k")]
+    B, S, Hq, Hkv, d, rot, dev, flags, small = _rope_common(q, k, q_weight, k_weight, inv_freq,
+                                                            positions, interleaved)
+    bf16, f32 = torch.bfloat16, torch.float32
+    g_type = bf16
+    if getattr(dq, "dtype", None) is f32:
+        g_type = f32
+        flags |= ATTN_GRAD_F32
+    q_shape, k_shape = (B, S, Hq, d), (B, S, Hkv, d)
+    dq_in = _head_major(dq, g_type, (B, Hq, S, d), "dq", dev)
+    dk_in = _head_major(dk, g_type, (B, Hkv, S, d), "dk", dev)
+    q_in = _token_major(q, bf16, q_shape, "q", dev)
+    k_in = _token_major(k, bf16, k_shape, "k", dev)
     if dq_out is None or dk_out is None or (dv_out is None and dv is not None):
-        fused = torch.empty((B, S, Hq + 2 * Hkv, d), dtype=torch.bfloat16, device=q.device)
-        parts = fused.split((Hq, Hkv, Hkv), dim=2)
-    ins, outs, results = [], [], []
-    for i, (g, out, H, name) in enumerate(((dq, dq_out, Hq, "dq"), (dk, dk_out, Hkv, "dk"),
-                                           (dv, dv_out, Hkv, "dv"))):
-        if g is None and name == "dv":
-            ins.append(None), outs.append(None), results.append(None)
-            continue
-        ins.append(_rows(g, gdtype, (B, H, S, d), (0, 2, 1), name))
-        if out is None:
-            out = parts[i]
-        outs.append(_rows(out, torch.bfloat16, (B, S, H, d), (0, 1, 2), name + "_out"))
-        results.append(out)
-    dw = torch.empty((2, d), dtype=torch.float32, device=q.device) if weight_grads else None
-    dqw, dkw = (dw[0], dw[1]) if weight_grads else (None, None)
-    ws_ptr, ws_bytes = _workspace(workspace)
-    with _device_of((dq, dk, dv, q, k, *results, q_weight, k_weight, inv_freq, positions,
-                     workspace)):
-        _set_stream(q)
-        _check(lib.attn_qk_norm_rope_bwd(*[_ref(h) for h in ins + xs + outs],
-                                         q_weight.data_ptr(), k_weight.data_ptr(),
-                                         inv_freq.data_ptr(), pos_ptr, pos_stride,
-                                         dqw.data_ptr() if weight_grads else None,
-                                         dkw.data_ptr() if weight_grads else None, B, S, Hq, Hkv,
-                                         d, rot, float(eps), flags, ws_ptr, ws_bytes))
-    return (*results, dqw, dkw)
+        parts = torch.empty((B, S, Hq + 2 * Hkv, d), dtype=bf16,
+                            device=q.device).split_with_sizes((Hq, Hkv, Hkv), 2)
+        dq_out = parts[0] if dq_out is None else dq_out
+        dk_out = parts[1] if dk_out is None else dk_out
+        if dv is not None and dv_out is None:
+            dv_out = parts[2]
+    dq_to = _token_major(dq_out, bf16, q_shape, "dq_out", dev)
+    dk_to = _token_major(dk_out, bf16, k_shape, "dk_out", dev)
+    dv_in = dv_to = _NO_HEADS
+    if dv is not None:
+        dv_in = _head_major(dv, g_type, (B, Hkv, S, d), "dv", dev)
+        dv_to = _token_major(dv_out, bf16, k_shape, "dv_out", dev)
+    elif dv_out is not None:
+        raise ValueError("dv_out without dv")
+    dqw = dkw = dqw_ptr = dkw_ptr = None
+    if weight_grads:
+        dqw, dkw = torch.empty((2, d), dtype=f32, device=q.device).unbind()
+        dqw_ptr, dkw_ptr = dqw.data_ptr(), dkw.data_ptr()
+    heads, at = _heads_array(dq_in, dk_in, dv_in, q_in, k_in, dq_to, dk_to, dv_to)
+    _call_on(dev, lib.attn_qk_norm_rope_bwd, *at, *small, dqw_ptr, dkw_ptr, B, S, Hq, Hkv, d, rot,
+             eps, flags, *_workspace(workspace, dev))
+    return dq_out, dk_out, dv_out, dqw, dkw
 
 
 def qk_norm_rope_bwd_workspace_bytes(B: int, S: int, Hq: int, Hkv: int, d: int) -> int:

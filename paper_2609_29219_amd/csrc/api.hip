@@ -1107,8 +1107,9 @@ static int validate_heads(const attn_heads* h, const char* name, int B, int S, i
     if (!aligned16(h->ptr)) return fail(ATTN_EINVAL, "%s must be 16-byte aligned", name);
     std::pair<long long, int> dims[3] = {
         {h->batch_stride, B}, {h->row_stride, S}, {h->head_stride, H}};
-    for (const auto& x : dims)
-        if (x.first < 0 || x.first % 8 != 0 || (x.first > 0 && x.second > (1LL << 60) / x.first))
+    for (const auto& x : dims)  // (a dimension of one has any stride)
+        if (x.second > 1 &&
+            (x.first < 0 || x.first % 8 != 0 || (x.first > 0 && x.second > (1LL << 60) / x.first)))
             return fail(ATTN_EINVAL, "%s: stride %lld is not a non-negative multiple of 8", name,
                         x.first);
     if (!written) return ATTN_OK;

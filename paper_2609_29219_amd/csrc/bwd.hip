@@ -37,7 +37,6 @@
 // Roundings: P and dS to bf16, as operands; everything else is fp32 until the result.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
-#include <string.h>
 
 #include <type_traits>
 
@@ -801,7 +800,8 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
 // over all heads, as the plan names them, or where those would be too many, the blocks of
 // both kinds interleaved in proportion.
 template <int D, bool CAUSAL>
-__global__ __launch_bounds__(kBwdThreads, 1) void bwd_kernel(const BwdArgs a) {
+__global__ __launch_bounds__(kBwdThreads, 1) void bwd_kernel(
+    const BwdArgs a, const typename std::conditional<CAUSAL, BwdOrder, int>::type order) {
     __shared__ __attribute__((aligned(1024))) char lds[BwdLds<D>::BYTES];
     const int heads = (int)a.kv_heads, units = a.kv_units + a.group * a.q_units;
     const bool even = heads % a.num_xcds == 0;
@@ -812,7 +812,8 @@ __global__ __launch_bounds__(kBwdThreads, 1) void bwd_kernel(const BwdArgs a) {
     bool is_kv;
     int head, g = 0, block, split = 0, splits = 1;
     if (CAUSAL && a.ordered) {
-        const BwdUnit u = a.order[i / hx];
+        BwdUnit u{};
+        if constexpr (CAUSAL) u = order.unit[i / hx];
         head = i % hx;
         is_kv = u.kv;
         g = u.g;
@@ -895,9 +896,9 @@ hipError_t launch_d(const BwdPlan& p, const BwdArgs& a, int causal, int o_bf16,
     if (e != hipSuccess) return e;
     const dim3 grid((unsigned)p.grid);
     if (causal)
-        bwd_kernel<D, true><<<grid, kBwdThreads, 0, stream>>>(a);
+        bwd_kernel<D, true><<<grid, kBwdThreads, 0, stream>>>(a, p.order);
     else
-        bwd_kernel<D, false><<<grid, kBwdThreads, 0, stream>>>(a);
+        bwd_kernel<D, false><<<grid, kBwdThreads, 0, stream>>>(a, 0);
     e = hipGetLastError();
     if (e != hipSuccess || (!p.kv_chunk && !p.q_chunk)) return e;
     const long long kv_rows = p.kv_chunk ? a.kv_heads * a.Skv : 0;
@@ -920,7 +921,6 @@ hipError_t launch_bwd(const BwdPlan& p, const BwdArgs& args, int d, int causal, 
     a.q_units = p.q_units;
     a.q_chunk = p.q_chunk;
     a.ordered = p.ordered;
-    if (p.ordered) memcpy(a.order, p.order, sizeof a.order);
     // the parts follow the row values
     const long long kv_values = a.kv_heads * a.Skv * d;
     a.part_k = a.rows + a.q_heads * ((a.Sq + 31) / 32) * 64;

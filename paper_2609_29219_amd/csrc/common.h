@@ -314,8 +314,11 @@ constexpr int kBwdOrder = 512;
 struct BwdUnit {
     uint16_t kv : 1, g : 15, block, split;
 };
+struct BwdOrder {
+    BwdUnit unit[kBwdOrder];
+};
 struct BwdPlan {
-    BwdUnit order[kBwdOrder];
+    BwdOrder order;
     int ordered = 0;
     int kv_blocks = 0, q_blocks = 0;  // of a head
     int kv_units = 0, q_units = 0;    // their parts
@@ -343,7 +346,6 @@ struct BwdArgs {
                        // product with scale_log2 is -inf
     // from the plan
     int kv_blocks, q_blocks, kv_units, q_units, kv_chunk, q_chunk, ordered;
-    BwdUnit order[kBwdOrder];
     float *part_k, *part_v, *part_q;  // fp32 parts, each as long as the whole result
 };
 // False where a grid would have too many workgroups.

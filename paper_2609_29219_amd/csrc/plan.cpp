@@ -1085,7 +1085,7 @@ void bwd_order(BwdPlan* p, const BwdCosts& c, int group, int Sq, int Skv, int ca
     }
     std::stable_sort(all.begin(), all.end(),
                      [](const auto& x, const auto& y) { return x.first > y.first; });
-    for (size_t i = 0; i < all.size(); ++i) p->order[i] = all[i].second;
+    for (size_t i = 0; i < all.size(); ++i) p->order.unit[i] = all[i].second;
 }
 
 // Time of the workgroups of `heads` heads on num_cus compute units, in the order in which
@@ -1103,7 +1103,8 @@ double bwd_makespan(const BwdPlan& p, const BwdCosts& c, int num_cus, int heads,
     std::vector<double> times;  // of a head's units, in order
     if (p.ordered) {
         for (int u = 0; u < p.kv_units + group * p.q_units; ++u)
-            times.push_back(p.order[u].kv ? kv_time(p.order[u].block) : q_time(p.order[u].block));
+            times.push_back(p.order.unit[u].kv ? kv_time(p.order.unit[u].block)
+                                              : q_time(p.order.unit[u].block));
     } else {
         for (int b = 0; b < p.kv_blocks; ++b)
             times.insert(times.end(),
@@ -1175,7 +1176,7 @@ bool plan_bwd(int num_cus, int B, int Hq, int Hkv, int Sq, int Skv, int d, int c
         bwd_order(&t, c, group, Sq, Skv, causal);
         if (causal && n > 1 && !t.ordered) break;  // the kernel finds no parts without it
         t.modeled_us = bwd_makespan(t, c, num_cus, (int)heads, group, Sq, Skv, causal) +
-                       (values > 0.0 ? 4.0 + values * 8.0 / 6.0e6 : 0.0);
+                       (values > 0.0 ? 6.0 + values * 8.0 / 6.0e6 : 0.0);
         if (n == 1 || t.modeled_us < out->modeled_us) *out = t;
     }
     return true;

@@ -32,16 +32,16 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kRopeThreads = 256;
 
-__device__ __forceinline__ float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
-__device__ __forceinline__ float bf16_hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
-
-__device__ __forceinline__ void load8(const uint16_t* p, float (&x)[8]) {
-    const u32x4 u = *reinterpret_cast<const u32x4*>(p);
+__device__ __forceinline__ void widen8(u32x4 u, float (&x)[8]) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        x[2 * e] = bf16_lo(u[e]);
-        x[2 * e + 1] = bf16_hi(u[e]);
+        x[2 * e] = __uint_as_float(u[e] << 16);
+        x[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
     }
+}
+
+__device__ __forceinline__ void load8(const uint16_t* p, float (&x)[8]) {
+    widen8(*reinterpret_cast<const u32x4*>(p), x);
 }
 
 __device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
@@ -79,7 +79,7 @@ __device__ __forceinline__ float row_sum(float x) {
     return x;
 }
 
-// The tokens of a tile: where their rows start, and cos and sin of their angles.
+// The tokens of a tile, and cos and sin of their angles.
 template <int D>
 struct RopeLds {
     float cs[2][kRopeMaxTile * (D / 2)];  // [token][pair]
@@ -116,153 +116,196 @@ __device__ __forceinline__ void load_tile(RopeLds<D>& lds, const RopeArgs& a, lo
     __syncthreads();
 }
 
-// Turns the lane's 8 columns by the token's angles (sign -1: back).  lane_col: the
-// lane's index in its row; every lane of the wave takes part.
-template <int D>
-__device__ __forceinline__ void rotate8(float (&y)[8], const RopeLds<D>& lds, int t, int lane_col,
-                                        int rot, int interleaved, float sign) {
-    const int half = rot / 2;
-    const bool in = lane_col * 8 < rot;
-    if (interleaved) {
-        const int i0 = t * half + (in ? lane_col * 4 : 0);
-        const f32x4 cn = *reinterpret_cast<const f32x4*>(&lds.cs[0][i0]);
-        const f32x4 sn = *reinterpret_cast<const f32x4*>(&lds.cs[1][i0]) * sign;
-        if (in) {
+// The rotation of a lane's 8 columns of its token's rows, y cos + mate sin with the mate
+// of each column: of the next or last column (IL, interleaved pairs), or of the same one
+// in the lane half / 8 further or back.  Columns past rot turn by 0.
+template <int D, bool IL>
+struct Rotation {
+    float cn[IL ? 4 : 8], sn[IL ? 4 : 8];
+    int mate;  // lane * 4
+
+    // sign -1: back
+    __device__ __forceinline__ void init(const RopeLds<D>& lds, int t, int lane_col, int rot,
+                                         float sign) {
+        const int half = rot / 2, lane = threadIdx.x & 63;
+        const bool in = lane_col * 8 < rot, second = lane_col * 8 >= half;
+        const int first = !in ? 0 : IL ? lane_col * 4 : lane_col * 8 - (second ? half : 0);
+        mate = (IL || !in ? lane : second ? lane - half / 8 : lane + half / 8) * 4;
+#pragma unroll
+        for (int e = 0; e < (IL ? 4 : 8); ++e) {
+            cn[e] = in ? lds.cs[0][t * half + first + e] : 1.f;
+            sn[e] = in ? lds.cs[1][t * half + first + e] * (IL || second ? sign : -sign) : 0.f;
+        }
+    }
+    // every lane of the wave takes part
+    __device__ __forceinline__ void turn(float (&y)[8]) const {
+        if constexpr (IL) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float p = y[2 * e], q = y[2 * e + 1];
                 y[2 * e] = p * cn[e] - q * sn[e];
                 y[2 * e + 1] = q * cn[e] + p * sn[e];
             }
-        }
-        return;
-    }
-    // the other half of each pair sits half / 8 lanes away
-    const bool second = lane_col * 8 >= half;
-    const int lane = threadIdx.x & 63;
-    const int mate = in ? (second ? lane - half / 8 : lane + half / 8) : lane;
-    const int i0 = t * half + (in ? lane_col * 8 - (second ? half : 0) : 0);
-    float cn[8], sn[8];
-    load8(&lds.cs[0][i0], cn);
-    load8(&lds.cs[1][i0], sn);
-    const float sg = second ? sign : -sign;
+        } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float other =
-            __int_as_float(__builtin_amdgcn_ds_bpermute(mate * 4, __float_as_int(y[e])));
-        const float turned = y[e] * cn[e] + other * (sg * sn[e]);
-        y[e] = in ? turned : y[e];
-    }
-}
-
-__device__ __forceinline__ long long row_offset(const attn_heads& h, int b, int s, int head) {
-    return b * h.batch_stride + s * h.row_stride + head * h.head_stride;
-}
-
-// Rows of a tile: row r is token r % tile of head r / tile (tile a power of two), a
-// group of D / 8 lanes to a row.  Workgroup (x, y): tile x, every gridDim.y-th pass.
-template <int D>
-__global__ __launch_bounds__(kRopeThreads) void rope_fwd_kernel(const RopeArgs a) {
-    constexpr int L = D / 8, RPP = kRopeThreads / L;  // lanes to a row, rows to a pass
-    __shared__ RopeLds<D> lds;
-    const int tile = 1 << a.tile_log2;
-    const long long token0 = (long long)blockIdx.x << a.tile_log2;
-    load_tile<D>(lds, a, token0, tile);
-    const int lc = threadIdx.x % L, group = threadIdx.x / L;
-    const int first = blockIdx.y * RPP + group, step = gridDim.y * RPP;
-    auto rows = [&](int which, int heads) __attribute__((always_inline)) {
-        const attn_heads in = a.in[which], out = a.out[which];
-        const uint16_t* src = static_cast<const uint16_t*>(in.ptr) + lc * 8;
-        uint16_t* dst = static_cast<uint16_t*>(out.ptr) + lc * 8;
-        float w[8];
-        if (which < 2) load_weight(a.weight[which], a.weight_f32, lc * 8, w);
-        const int n = heads << a.tile_log2;
-        for (int r0 = first - group; r0 < n; r0 += step) {  // whole waves go round together
-            const int r = r0 + group < n ? r0 + group : n - 1;
-            const int t = r & (tile - 1), head = r >> a.tile_log2;
-            const bool live = r0 + group < n && token0 + t < a.tokens;
-            const uint16_t* p = src + row_offset(in, lds.b[t], lds.s[t], head);
-            uint16_t* q = dst + row_offset(out, lds.b[t], lds.s[t], head);
-            if (which == 2) {
-                const u32x4 u = *reinterpret_cast<const u32x4*>(p);
-                if (live) *reinterpret_cast<u32x4*>(q) = u;
-                continue;
+            for (int e = 0; e < 8; ++e) {
+                const float other =
+                    __int_as_float(__builtin_amdgcn_ds_bpermute(mate, __float_as_int(y[e])));
+                y[e] = y[e] * cn[e] + other * sn[e];
             }
-            float x[8];
-            load8(p, x);
-            float ss = 0.f;
+        }
+    }
+};
+
+// A group of D / 8 lanes works on the rows of one token t of the tile (a power of two, at
+// most the groups of a workgroup), heads first, first + step, ...; the groups that share
+// a token, and workgroups along y, share its heads out.
+struct GroupRows {
+    int lane_col, t, first, step;
+    template <int D>
+    __device__ __forceinline__ void init(int tile_log2) {
+        constexpr int L = D / 8, GROUPS = kRopeThreads / L;
+        const int group = threadIdx.x / L;
+        lane_col = threadIdx.x % L;
+        t = group & ((1 << tile_log2) - 1);
+        first = blockIdx.y * (GROUPS >> tile_log2) + (group >> tile_log2);
+        step = gridDim.y * (GROUPS >> tile_log2);
+    }
+    // passes over `heads` heads that the workgroup makes together
+    __device__ __forceinline__ int passes(int heads) const { return (heads + step - 1) / step; }
+};
+
+__device__ __forceinline__ long long token_offset(const attn_heads& h, int b, int s) {
+    return b * h.batch_stride + s * h.row_stride;
+}
+
+// Several rows are loaded before the first is worked on, to have enough bytes on their way.
+template <int D, bool IL>
+__global__ __launch_bounds__(kRopeThreads) void rope_fwd_kernel(const RopeArgs a) {
+    constexpr int L = D / 8, U = 4;
+    __shared__ RopeLds<D> lds;
+    const long long token0 = (long long)blockIdx.x << a.tile_log2;
+    load_tile<D>(lds, a, token0, 1 << a.tile_log2);
+    GroupRows g;
+    g.init<D>(a.tile_log2);
+    const int b = lds.b[g.t], s = lds.s[g.t];
+    const bool token = token0 + g.t < a.tokens;
+    Rotation<D, IL> rotation;
+    rotation.init(lds, g.t, g.lane_col, a.rot, 1.0f);
+    auto rows = [&](auto which_tag, int heads) __attribute__((always_inline)) {
+        constexpr int which = decltype(which_tag)::value;
+        const attn_heads in = a.in[which], out = a.out[which];
+        const uint16_t* src =
+            static_cast<const uint16_t*>(in.ptr) + token_offset(in, b, s) + g.lane_col * 8;
+        uint16_t* dst = static_cast<uint16_t*>(out.ptr) + token_offset(out, b, s) + g.lane_col * 8;
+        float w[8];
+        if constexpr (which < 2)
+            load_weight(a.weight[which < 2 ? which : 0], a.weight_f32, g.lane_col * 8, w);
+        const int n = g.passes(heads);
+        for (int i = 0; i < n; i += U) {
+            u32x4 raw[U];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
-            ss = row_sum<L>(ss);
-            const float rs = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
+            for (int u = 0; u < U; ++u) {
+                const int head = min(g.first + (i + u) * g.step, heads - 1);
+                raw[u] = *reinterpret_cast<const u32x4*>(src + head * in.head_stride);
+            }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = x[e] * rs * w[e];
-            rotate8<D>(x, lds, t, lc, a.rot, a.interleaved, 1.0f);
-            if (live) store8(q, x);
+            for (int u = 0; u < U; ++u) {
+                const int head = g.first + (i + u) * g.step;
+                uint16_t* to = dst + head * out.head_stride;
+                if constexpr (which == 2) {
+                    if (token && head < heads) *reinterpret_cast<u32x4*>(to) = raw[u];
+                } else {
+                    float x[8];
+                    widen8(raw[u], x);
+                    float ss = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
+                    const float rs = rsqrtf(row_sum<L>(ss) * (1.0f / D) + a.eps);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = x[e] * rs * w[e];
+                    rotation.turn(x);
+                    if (token && head < heads) store8(to, x);
+                }
+            }
         }
     };
-    rows(0, a.Hq);
-    rows(1, a.Hkv);
-    if (a.in[2].ptr) rows(2, a.Hkv);
+    rows(std::integral_constant<int, 0>{}, a.Hq);
+    rows(std::integral_constant<int, 1>{}, a.Hkv);
+    if (a.in[2].ptr) rows(std::integral_constant<int, 2>{}, a.Hkv);
 }
 
 // in: the gradients of the outputs (bf16, or fp32 with G32); x: the forward pass's
 // inputs; out: their gradients.  Workgroups walk the tiles in steps of the grid; each
 // leaves the sums of its rows' weight gradients in ws[workgroup][q, k][D], which
 // rope_weight_kernel adds up in a fixed order.
-template <int D, bool G32>
+template <int D, bool IL, bool G32>
 __global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(const RopeArgs a) {
-    constexpr int L = D / 8, RPP = kRopeThreads / L;
+    constexpr int L = D / 8, GROUPS = kRopeThreads / L, U = 2;
     typedef typename std::conditional<G32, float, uint16_t>::type grad_t;
     __shared__ RopeLds<D> lds;
-    __shared__ float sums[RPP][D];
+    __shared__ float sums[GROUPS][D];
+    GroupRows g;
+    g.init<D>(a.tile_log2);
     const int tile = 1 << a.tile_log2;
-    const int lc = threadIdx.x % L, group = threadIdx.x / L;
-    const int first = blockIdx.y * RPP, step = gridDim.y * RPP;
     const long long tiles = (a.tokens + tile - 1) >> a.tile_log2;
     float dw[2][8] = {};
     for (long long tl = blockIdx.x; tl < tiles; tl += gridDim.x) {
         const long long token0 = tl << a.tile_log2;
         if (tl != blockIdx.x) __syncthreads();  // the last tile's angles are still read
         load_tile<D>(lds, a, token0, tile);
+        const int b = lds.b[g.t], s = lds.s[g.t];
+        const bool token = token0 + g.t < a.tokens;
+        Rotation<D, IL> rotation;
+        rotation.init(lds, g.t, g.lane_col, a.rot, -1.0f);
         auto rows = [&](auto which_tag, int heads) __attribute__((always_inline)) {
-            constexpr int which = decltype(which_tag)::value;
-            const attn_heads in = a.in[which], out = a.out[which], xin = a.x[which];
-            const grad_t* src = static_cast<const grad_t*>(in.ptr) + lc * 8;
-            const uint16_t* xs = static_cast<const uint16_t*>(xin.ptr) + lc * 8;
-            uint16_t* dst = static_cast<uint16_t*>(out.ptr) + lc * 8;
+            constexpr int which = decltype(which_tag)::value, qk = which < 2 ? which : 0;
+            const attn_heads in = a.in[which], out = a.out[which], xin = a.x[qk];
+            const int c = g.lane_col * 8;
+            const grad_t* src = static_cast<const grad_t*>(in.ptr) + token_offset(in, b, s) + c;
+            const uint16_t* xs =
+                static_cast<const uint16_t*>(xin.ptr) + token_offset(xin, b, s) + c;
+            uint16_t* dst = static_cast<uint16_t*>(out.ptr) + token_offset(out, b, s) + c;
             float w[8];
-            if (which < 2) load_weight(a.weight[which], a.weight_f32, lc * 8, w);
-            const int n = heads << a.tile_log2;
-            for (int r0 = first; r0 < n; r0 += step) {
-                const int r = r0 + group < n ? r0 + group : n - 1;
-                const int t = r & (tile - 1), head = r >> a.tile_log2;
-                const bool live = r0 + group < n && token0 + t < a.tokens;
-                float g[8], x[8];
-                load8(src + row_offset(in, lds.b[t], lds.s[t], head), g);
-                uint16_t* q = dst + row_offset(out, lds.b[t], lds.s[t], head);
-                if constexpr (which == 2) {
-                    if (live) store8(q, g);
-                } else {
-                    load8(xs + row_offset(xin, lds.b[t], lds.s[t], head), x);
-                    rotate8<D>(g, lds, t, lc, a.rot, a.interleaved, -1.0f);
-                    float ss = 0.f, sg = 0.f;
+            if constexpr (which < 2) load_weight(a.weight[qk], a.weight_f32, c, w);
+            const int n = g.passes(heads);
+            for (int i = 0; i < n; i += U) {
+                float gr[U][8];
+                u32x4 raw[U];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        ss = fmaf(x[e], x[e], ss);
-                        sg = fmaf(g[e] * w[e], x[e], sg);
-                    }
-                    ss = row_sum<L>(ss);
-                    sg = row_sum<L>(sg);
-                    const float rs = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
-                    const float mean = sg * rs * (1.0f / D);  // mean(g' w x r)
+                for (int u = 0; u < U; ++u) {
+                    const int head = min(g.first + (i + u) * g.step, heads - 1);
+                    load8(src + head * in.head_stride, gr[u]);
+                    if constexpr (which < 2)
+                        raw[u] = *reinterpret_cast<const u32x4*>(xs + head * xin.head_stride);
+                }
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float xn = x[e] * rs;
-                        if (live) dw[which][e] = fmaf(g[e], xn, dw[which][e]);
-                        g[e] = rs * (g[e] * w[e] - xn * mean);
+                for (int u = 0; u < U; ++u) {
+                    const int head = g.first + (i + u) * g.step;
+                    const bool live = token && head < heads;
+                    uint16_t* to = dst + head * out.head_stride;
+                    if constexpr (which < 2) {
+                        float x[8];
+                        widen8(raw[u], x);
+                        rotation.turn(gr[u]);
+                        float ss = 0.f, sg = 0.f;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            ss = fmaf(x[e], x[e], ss);
+                            sg = fmaf(gr[u][e] * w[e], x[e], sg);
+                        }
+                        ss = row_sum<L>(ss);
+                        sg = row_sum<L>(sg);
+                        const float rs = rsqrtf(ss * (1.0f / D) + a.eps);
+                        const float mean = sg * rs * (1.0f / D);  // mean(g' w x r)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float xn = x[e] * rs;
+                            if (live) dw[qk][e] = fmaf(gr[u][e], xn, dw[qk][e]);
+                            gr[u][e] = rs * (gr[u][e] * w[e] - xn * mean);
+                        }
                     }
-                    if (live) store8(q, g);
+                    if (live) store8(to, gr[u]);
                 }
             }
         };
@@ -276,12 +319,12 @@ __global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(const RopeArgs a
     for (int which = 0; which < 2; ++which) {
         __syncthreads();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sums[group][lc * 8 + e] = dw[which][e];
+        for (int e = 0; e < 8; ++e) sums[threadIdx.x / L][g.lane_col * 8 + e] = dw[which][e];
         __syncthreads();
         for (int c = threadIdx.x; c < D; c += kRopeThreads) {
-            float s = 0.f;
-            for (int g = 0; g < RPP; ++g) s += sums[g][c];
-            ws[which * D + c] = s;
+            float sum = 0.f;
+            for (int i = 0; i < GROUPS; ++i) sum += sums[i][c];
+            ws[which * D + c] = sum;
         }
     }
 }
@@ -325,25 +368,32 @@ RopeLaunch rope_launch(long long tokens, int Hq, int Hkv, int d, int num_cus, bo
 
 hipError_t launch_rope(const RopeArgs& a, const RopeLaunch& l, int d, hipStream_t stream) {
     const dim3 grid(l.grid_x, l.grid_y);
-    if (d == 64)
-        rope_fwd_kernel<64><<<grid, kRopeThreads, 0, stream>>>(a);
-    else
-        rope_fwd_kernel<128><<<grid, kRopeThreads, 0, stream>>>(a);
-    return hipGetLastError();
+    auto go = [&](auto kernel) {
+        kernel<<<grid, kRopeThreads, 0, stream>>>(a);
+        return hipGetLastError();
+    };
+    if (d == 64) return go(a.interleaved ? rope_fwd_kernel<64, true> : rope_fwd_kernel<64, false>);
+    return go(a.interleaved ? rope_fwd_kernel<128, true> : rope_fwd_kernel<128, false>);
 }
 
 hipError_t launch_rope_bwd(const RopeArgs& a, const RopeLaunch& l, int d, int grad_f32,
                            float* dq_weight, float* dk_weight, hipStream_t stream) {
     const dim3 grid(l.grid_x, l.grid_y);
-    if (d == 64 && grad_f32)
-        rope_bwd_kernel<64, true><<<grid, kRopeThreads, 0, stream>>>(a);
-    else if (d == 64)
-        rope_bwd_kernel<64, false><<<grid, kRopeThreads, 0, stream>>>(a);
-    else if (grad_f32)
-        rope_bwd_kernel<128, true><<<grid, kRopeThreads, 0, stream>>>(a);
+    auto go = [&](auto f32, auto bf16) {
+        if (grad_f32)
+            f32<<<grid, kRopeThreads, 0, stream>>>(a);
+        else
+            bf16<<<grid, kRopeThreads, 0, stream>>>(a);
+        return hipGetLastError();
+    };
+    hipError_t e;
+    if (d == 64)
+        e = a.interleaved ? go(rope_bwd_kernel<64, true, true>, rope_bwd_kernel<64, true, false>)
+                          : go(rope_bwd_kernel<64, false, true>, rope_bwd_kernel<64, false, false>);
     else
-        rope_bwd_kernel<128, false><<<grid, kRopeThreads, 0, stream>>>(a);
-    hipError_t e = hipGetLastError();
+        e = a.interleaved
+                ? go(rope_bwd_kernel<128, true, true>, rope_bwd_kernel<128, true, false>)
+                : go(rope_bwd_kernel<128, false, true>, rope_bwd_kernel<128, false, false>);
     if (e != hipSuccess || !a.ws) return e;
     rope_weight_kernel<<<dim3(d / 16, 2), 1024, 0, stream>>>(a.ws, l.grid_x * l.grid_y, d,
                                                              dq_weight, dk_weight);

@@ -53,11 +53,30 @@ __device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
     }
 }
 
+// NT: past the caches.  Where a call moves more than the 256 MB that the memory-side cache
+// holds, keeping the lines only displaces others: B4 S8192 Hq32 Hkv8 d128, 805 MB, 167 us
+// through the caches and 151 past them; S4096 alone, 100 MB, 20 and 25 us.
+template <bool NT>
+__device__ __forceinline__ u32x4 load16(const uint16_t* p) {
+    const u32x4* at = reinterpret_cast<const u32x4*>(p);
+    return NT ? __builtin_nontemporal_load(at) : *at;
+}
+
+template <bool NT>
+__device__ __forceinline__ void store16(uint16_t* p, u32x4 y) {
+    u32x4* at = reinterpret_cast<u32x4*>(p);
+    if constexpr (NT)
+        __builtin_nontemporal_store(y, at);
+    else
+        *at = y;
+}
+
+template <bool NT>
 __device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8]) {
     bf16x8 y;
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] = (__bf16)x[e];  // round to nearest even
-    *reinterpret_cast<bf16x8*>(p) = y;
+    store16<NT>(p, __builtin_bit_cast(u32x4, y));
 }
 
 // 8 weights of a lane's columns
@@ -122,7 +141,8 @@ __device__ __forceinline__ void load_tile(RopeLds<D>& lds, const RopeArgs& a, lo
 template <int D, bool IL>
 struct Rotation {
     float cn[IL ? 4 : 8], sn[IL ? 4 : 8];
-    int mate;  // lane * 4
+    int mate;    // lane * 4
+    bool whole;  // D = 128, all of it rotated: the mate is 8 lanes on, within each 16
 
     // sign -1: back
     __device__ __forceinline__ void init(const RopeLds<D>& lds, int t, int lane_col, int rot,
@@ -130,6 +150,7 @@ struct Rotation {
         const int half = rot / 2, lane = threadIdx.x & 63;
         const bool in = lane_col * 8 < rot, second = lane_col * 8 >= half;
         const int first = !in ? 0 : IL ? lane_col * 4 : lane_col * 8 - (second ? half : 0);
+        whole = D == 128 && rot == D;
         mate = (IL || !in ? lane : second ? lane - half / 8 : lane + half / 8) * 4;
 #pragma unroll
         for (int e = 0; e < (IL ? 4 : 8); ++e) {
@@ -146,6 +167,11 @@ struct Rotation {
                 y[2 * e] = p * cn[e] - q * sn[e];
                 y[2 * e + 1] = q * cn[e] + p * sn[e];
             }
+        } else if (whole) {  // a register exchange (0x128: rows rotated by 8)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                y[e] = y[e] * cn[e] + sn[e] * __int_as_float(__builtin_amdgcn_mov_dpp(
+                                                  __float_as_int(y[e]), 0x128, 0xF, 0xF, false));
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -180,7 +206,7 @@ __device__ __forceinline__ long long token_offset(const attn_heads& h, int b, in
 }
 
 // Several rows are loaded before the first is worked on, to have enough bytes on their way.
-template <int D, bool IL>
+template <int D, bool IL, bool NT>
 __global__ __launch_bounds__(kRopeThreads) void rope_fwd_kernel(const RopeArgs a) {
     constexpr int L = D / 8, U = 4;
     __shared__ RopeLds<D> lds;
@@ -207,14 +233,14 @@ __global__ __launch_bounds__(kRopeThreads) void rope_fwd_kernel(const RopeArgs a
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int head = min(g.first + (i + u) * g.step, heads - 1);
-                raw[u] = *reinterpret_cast<const u32x4*>(src + head * in.head_stride);
+                raw[u] = load16<NT>(src + head * in.head_stride);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int head = g.first + (i + u) * g.step;
                 uint16_t* to = dst + head * out.head_stride;
                 if constexpr (which == 2) {
-                    if (token && head < heads) *reinterpret_cast<u32x4*>(to) = raw[u];
+                    if (token && head < heads) store16<NT>(to, raw[u]);
                 } else {
                     float x[8];
                     widen8(raw[u], x);
@@ -225,7 +251,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_fwd_kernel(const RopeArgs a
 #pragma unroll
                     for (int e = 0; e < 8; ++e) x[e] = x[e] * rs * w[e];
                     rotation.turn(x);
-                    if (token && head < heads) store8(to, x);
+                    if (token && head < heads) store8<NT>(to, x);
                 }
             }
         }
@@ -239,8 +265,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_fwd_kernel(const RopeArgs a
 // inputs; out: their gradients.  Workgroups walk the tiles in steps of the grid; each
 // leaves the sums of its rows' weight gradients in ws[workgroup][q, k][D], which
 // rope_weight_kernel adds up in a fixed order.
-template <int D, bool IL, bool G32>
-__global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(const RopeArgs a) {
+template <int D, bool IL, bool G32, bool NT>
+__global__ __launch_bounds__(kRopeThreads, 3) void rope_bwd_kernel(const RopeArgs a) {
     constexpr int L = D / 8, GROUPS = kRopeThreads / L, U = 2;
     typedef typename std::conditional<G32, float, uint16_t>::type grad_t;
     __shared__ RopeLds<D> lds;
@@ -277,7 +303,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(const RopeArgs a
                     const int head = min(g.first + (i + u) * g.step, heads - 1);
                     load8(src + head * in.head_stride, gr[u]);
                     if constexpr (which < 2)
-                        raw[u] = *reinterpret_cast<const u32x4*>(xs + head * xin.head_stride);
+                        raw[u] = load16<NT>(xs + head * xin.head_stride);
                 }
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
@@ -305,7 +331,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_bwd_kernel(const RopeArgs a
                             gr[u][e] = rs * (gr[u][e] * w[e] - xn * mean);
                         }
                     }
-                    if (live) store8(to, gr[u]);
+                    if (live) store8<NT>(to, gr[u]);
                 }
             }
         };
@@ -366,34 +392,53 @@ RopeLaunch rope_launch(long long tokens, int Hq, int Hkv, int d, int num_cus, bo
     return l;
 }
 
+namespace {
+template <int D, bool IL, bool NT>
+hipError_t launch_fwd(const RopeArgs& a, const dim3& grid, hipStream_t stream) {
+    rope_fwd_kernel<D, IL, NT><<<grid, kRopeThreads, 0, stream>>>(a);
+    return hipGetLastError();
+}
+template <int D, bool IL, bool NT>
+hipError_t launch_bwd(const RopeArgs& a, const dim3& grid, int grad_f32, hipStream_t stream) {
+    if (grad_f32)
+        rope_bwd_kernel<D, IL, true, NT><<<grid, kRopeThreads, 0, stream>>>(a);
+    else
+        rope_bwd_kernel<D, IL, false, NT><<<grid, kRopeThreads, 0, stream>>>(a);
+    return hipGetLastError();
+}
+// f(D, interleaved, past the caches), as compile-time values
+template <typename F>
+hipError_t rope_variant(int d, int interleaved, bool nt, F f) {
+    using T = std::true_type;
+    using N = std::false_type;
+    auto with = [&](auto dim) {
+        if (interleaved) return nt ? f(dim, T{}, T{}) : f(dim, T{}, N{});
+        return nt ? f(dim, N{}, T{}) : f(dim, N{}, N{});
+    };
+    return d == 64 ? with(std::integral_constant<int, 64>{})
+                   : with(std::integral_constant<int, 128>{});
+}
+bool past_caches(const RopeArgs& a, int d, int bytes_per_value) {
+    return a.tokens * (a.Hq + 2LL * a.Hkv) * d * bytes_per_value > 256LL << 20;
+}
+}  // namespace
+
 hipError_t launch_rope(const RopeArgs& a, const RopeLaunch& l, int d, hipStream_t stream) {
     const dim3 grid(l.grid_x, l.grid_y);
-    auto go = [&](auto kernel) {
-        kernel<<<grid, kRopeThreads, 0, stream>>>(a);
-        return hipGetLastError();
-    };
-    if (d == 64) return go(a.interleaved ? rope_fwd_kernel<64, true> : rope_fwd_kernel<64, false>);
-    return go(a.interleaved ? rope_fwd_kernel<128, true> : rope_fwd_kernel<128, false>);
+    return rope_variant(d, a.interleaved, past_caches(a, d, 4), [&](auto D, auto IL, auto NT) {
+        return launch_fwd<decltype(D)::value, decltype(IL)::value, decltype(NT)::value>(a, grid,
+                                                                                      stream);
+    });
 }
 
 hipError_t launch_rope_bwd(const RopeArgs& a, const RopeLaunch& l, int d, int grad_f32,
                            float* dq_weight, float* dk_weight, hipStream_t stream) {
     const dim3 grid(l.grid_x, l.grid_y);
-    auto go = [&](auto f32, auto bf16) {
-        if (grad_f32)
-            f32<<<grid, kRopeThreads, 0, stream>>>(a);
-        else
-            bf16<<<grid, kRopeThreads, 0, stream>>>(a);
-        return hipGetLastError();
-    };
-    hipError_t e;
-    if (d == 64)
-        e = a.interleaved ? go(rope_bwd_kernel<64, true, true>, rope_bwd_kernel<64, true, false>)
-                          : go(rope_bwd_kernel<64, false, true>, rope_bwd_kernel<64, false, false>);
-    else
-        e = a.interleaved
-                ? go(rope_bwd_kernel<128, true, true>, rope_bwd_kernel<128, true, false>)
-                : go(rope_bwd_kernel<128, false, true>, rope_bwd_kernel<128, false, false>);
+    const hipError_t e = rope_variant(
+        d, a.interleaved, past_caches(a, d, grad_f32 ? 8 : 6), [&](auto D, auto IL, auto NT) {
+            return launch_bwd<decltype(D)::value, decltype(IL)::value, decltype(NT)::value>(
+                a, grid, grad_f32, stream);
+        });
     if (e != hipSuccess || !a.ws) return e;
     rope_weight_kernel<<<dim3(d / 16, 2), 1024, 0, stream>>>(a.ws, l.grid_x * l.grid_y, d,
                                                              dq_weight, dk_weight);

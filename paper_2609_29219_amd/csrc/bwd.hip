@@ -45,8 +45,16 @@
 namespace attn {
 namespace {
 
-constexpr int kBwdThreads = 256;
-constexpr int kBwdWaves = kBwdThreads / 64;
+// Waves of a workgroup, and 32-row blocks that each keeps.  With D = 128 one wave to a SIMD
+// and two blocks to a wave: every operand read from LDS serves two products (with one, LDS
+// would be as busy as the matrix cores).  With D = 64 the weights, as many for half the
+// products, take as long as those do, and two waves to a SIMD overlap the two kinds of
+// work better than one does (B4 H16 S2048 290 us against 303).
+template <int D>
+struct BwdShape {
+    static constexpr int BLOCKS = D == 64 ? 1 : 2, WAVES = kBwdBlock / (32 * BLOCKS);
+    static constexpr int THREADS = 64 * WAVES, WAVES_PER_SIMD = WAVES / 4;
+};
 
 // Which 16-byte piece of a row holds piece c: c ^ tile_swizzle(row).
 template <int D>
@@ -54,34 +62,35 @@ __device__ __forceinline__ int tile_swizzle(int row) {
     return D == 128 ? (row & 3) << 2 | ((row >> 2) & 3) : ((row >> 1) & 1) << 2 | ((row >> 2) & 3);
 }
 
-// One operand tile (32 rows of D) from a head's slab into LDS; the four waves share
-// its 1 KiB pieces.  Rows past the slab re-read its last row (finite, and weighted 0).
+// A pair of tiles (32 rows of D each), the same rows of two slabs, into LDS one behind the
+// other; the waves share their 1 KiB pieces.  Rows past the slabs re-read the last row
+// (finite, and weighted 0).
 template <int D>
 struct TileLoad {
-    static constexpr int PIECES = 32 * D * 2 / 1024;
-    static constexpr int NJ = PIECES / kBwdWaves;
+    static constexpr int W = BwdShape<D>::WAVES, PIECES = 32 * D * 2 / 1024;
+    static constexpr int NJ = 2 * PIECES / W, NO = PIECES > W ? PIECES / W : 1;
     static constexpr int ROWS = 512 / D;  // of one piece
-    int off[NJ];  // this lane's source bytes within a tile
+    int off[NO];  // this lane's source bytes within a tile
 
     __device__ __forceinline__ void init(int wave, int lane) {
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const int r = (wave + j * kBwdWaves) * ROWS + lane / (D / 8);
+        for (int j = 0; j < NO; ++j) {
+            const int r = (wave % PIECES + j * W) * ROWS + lane / (D / 8);
             off[j] = r * (D * 2) + ((lane % (D / 8)) ^ tile_swizzle<D>(r)) * 16;
         }
     }
-    __device__ __forceinline__ void issue(dma_rsrc_t rsrc, uint32_t lds, int row0, int n_rows,
-                                          int wave) const {
-        if (row0 + 32 <= n_rows) {
+    __device__ __forceinline__ void issue(dma_rsrc_t slab0, dma_rsrc_t slab1, uint32_t lds,
+                                          int row0, int n_rows, int wave) const {
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)
-                lds_dma16(rsrc, lds + (wave + j * kBwdWaves) * 1024, off[j], row0 * (D * 2));
-        } else {
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                const int r = min(row0 + off[j] / (D * 2), n_rows - 1);
-                lds_dma16(rsrc, lds + (wave + j * kBwdWaves) * 1024,
-                          r * (D * 2) + off[j] % (D * 2), 0);
+        for (int j = 0; j < NJ; ++j) {
+            const int piece = wave + j * W;
+            const dma_rsrc_t slab = NJ > 1 ? (j < NJ / 2 ? slab0 : slab1)
+                                           : (wave < PIECES ? slab0 : slab1);
+            if (row0 + 32 <= n_rows) {
+                lds_dma16(slab, lds + piece * 1024, off[j % NO], row0 * (D * 2));
+            } else {
+                const int r = min(row0 + off[j % NO] / (D * 2), n_rows - 1);
+                lds_dma16(slab, lds + piece * 1024, r * (D * 2) + off[j % NO] % (D * 2), 0);
             }
         }
     }
@@ -263,18 +272,19 @@ __device__ __forceinline__ void store_rows(const f32x16 (&x)[D / 32], char* stag
 }
 
 // LDS of a workgroup, in bytes: row values, then slots of a pair of tiles each (Q and dO:
-// 2, K and V: 3).  At the start the waves' own 64 rows of both their operands come through
+// 2, K and V: 3).  At the start the waves' own rows of both their operands come through
 // the place from the second slot on; at the end the results through the stages.
 template <int D>
 struct BwdLds {
     static constexpr int TILE = 32 * D * 2, SLOT = 2 * TILE;
     static constexpr int SLOTS = 1024, OWN = SLOTS + SLOT;
-    static constexpr int STAGES = kBwdWaves * stage_bytes<D>();
-    static constexpr int BYTES = OWN + kBwdWaves * 4 * TILE;
+    static constexpr int OWN_WAVE = 2 * BwdShape<D>::BLOCKS * TILE;
+    static constexpr int STAGES = BwdShape<D>::WAVES * stage_bytes<D>();
+    static constexpr int BYTES = OWN + BwdShape<D>::WAVES * OWN_WAVE;
     static_assert(BYTES >= SLOTS + 3 * SLOT && BYTES >= STAGES, "");
 };
 
-// A wave's own 64 rows of a head's slab as operand registers: op[b][ks] holds row l%32 of
+// A wave's own rows of a head's slab as operand registers: op[b][ks] holds row l%32 of
 // the b-th 32, values 16*ks + 8*(l/32) ..+7.  Loaded straight into registers, an
 // instruction touches 32 rows, 32 bytes each, and the operands of a workgroup took 5.8 us;
 // through LDS in whole rows they take 3.  own_load issues the loads, own_read reads what
@@ -284,19 +294,20 @@ __device__ __forceinline__ void own_load(dma_rsrc_t rsrc, uint32_t lds, int row0
                                          int lane) {
     constexpr int ROWS = 512 / D;
 #pragma unroll
-    for (int p = 0; p < 64 / ROWS; ++p) {
+    for (int p = 0; p < 32 * BwdShape<D>::BLOCKS / ROWS; ++p) {
         const int r = p * ROWS + lane / (D / 8);
         const int c = (lane % (D / 8)) ^ tile_swizzle<D>(r & 31);
         lds_dma16(rsrc, lds + p * 1024, min(row0 + r, n_rows - 1) * (D * 2) + c * 16, 0);
     }
 }
 template <int D>
-__device__ __forceinline__ void own_read(bf16x8 (&op)[2][D / 16], const TileRead<D>& read,
-                                         uint32_t lds) {
-    static_for<0, D / 16>([&](auto ks) __attribute__((always_inline)) {
-        op[0][ks] = TileRead<D>::template by_row<decltype(ks)::value>(read.row + lds, 0);
-        op[1][ks] = TileRead<D>::template by_row<decltype(ks)::value>(read.row + lds,
-                                                                      BwdLds<D>::TILE);
+__device__ __forceinline__ void own_read(bf16x8 (&op)[BwdShape<D>::BLOCKS][D / 16],
+                                         const TileRead<D>& read, uint32_t lds) {
+    static_for<0, BwdShape<D>::BLOCKS>([&](auto b) __attribute__((always_inline)) {
+        static_for<0, D / 16>([&](auto ks) __attribute__((always_inline)) {
+            op[b][ks] = TileRead<D>::template by_row<decltype(ks)::value>(
+                read.row + lds, decltype(b)::value * BwdLds<D>::TILE);
+        });
     });
 }
 
@@ -356,7 +367,7 @@ __global__ __launch_bounds__(256) void bwd_rows_kernel(const BwdArgs a) {
 template <int D, bool CAUSAL>
 __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, int block,
                                            int split, int splits) {
-    constexpr int KB = 2, KD = D / 16, CB = D / 32;
+    constexpr int KB = BwdShape<D>::BLOCKS, KD = D / 16, CB = D / 32;
     typedef BwdLds<D> L;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -394,8 +405,7 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
     load_head();
     auto issue = [&](int slot) __attribute__((always_inline)) {
         const uint32_t dst = lds0 + slot * L::SLOT;
-        load.issue(q_rsrc, dst, load_qt * 32, a.Sq, wave);
-        load.issue(g_rsrc, dst + L::TILE, load_qt * 32, a.Sq, wave);
+        load.issue(q_rsrc, g_rsrc, dst, load_qt * 32, a.Sq, wave);
         if (wave == 0) lds_dma4(row_rsrc, rows0 + slot * 256, lane * 4, load_qt * 256);
         if (++load_qt == n_qt) {
             load_qt = qt0;
@@ -538,14 +548,14 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
     int qt = load_qt;
     issue(0);  // (a part has at least one step)
     {
-        const uint32_t own = rows0 + L::OWN + wave * (4 * L::TILE);
+        const uint32_t own = rows0 + L::OWN + wave * L::OWN_WAVE;
         const uint32_t slab = (uint32_t)a.Skv * D * 2;
         const long long at = (long long)bh * a.Skv * D;
         own_load<D>(make_dma_rsrc(a.k + at, slab), own, wk0, a.Skv, lane);
-        own_load<D>(make_dma_rsrc(a.v + at, slab), own + 2 * L::TILE, wk0, a.Skv, lane);
+        own_load<D>(make_dma_rsrc(a.v + at, slab), own + L::OWN_WAVE / 2, wk0, a.Skv, lane);
         asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
         own_read<D>(kf, read, own);
-        own_read<D>(vf, read, own + 2 * L::TILE);
+        own_read<D>(vf, read, own + L::OWN_WAVE / 2);
     }
     publish_barrier<0>();  // (all have read their own: its place is free)
     if (begin + 1 < end) issue(1);
@@ -591,7 +601,7 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
 template <int D, bool CAUSAL>
 __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, int block,
                                          int split, int splits) {
-    constexpr int QB = 2, KD = D / 16, CB = D / 32;
+    constexpr int QB = BwdShape<D>::BLOCKS, KD = D / 16, CB = D / 32;
     typedef BwdLds<D> L;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -629,8 +639,7 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
     const dma_rsrc_t v_rsrc = make_dma_rsrc(a.v + head * a.Skv * D, slab);
     auto issue = [&](int step, int slot) __attribute__((always_inline)) {
         const uint32_t dst = lds0 + slot * L::SLOT;
-        load.issue(k_rsrc, dst, step * 32, a.Skv, wave);
-        load.issue(v_rsrc, dst + L::TILE, step * 32, a.Skv, wave);
+        load.issue(k_rsrc, v_rsrc, dst, step * 32, a.Skv, wave);
     };
 
     // Operand i of a step: K by rows (S of this tile), K transposed (dQ of the tile before:
@@ -739,14 +748,14 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
     int slot = 0;
     issue(begin, 0);  // (a part has at least one step)
     {
-        const uint32_t own = lds_address(lds) + L::OWN + wave * (4 * L::TILE);
+        const uint32_t own = lds_address(lds) + L::OWN + wave * L::OWN_WAVE;
         const uint32_t slab = (uint32_t)a.Sq * D * 2;
         const long long at = (long long)bh * a.Sq * D;
         own_load<D>(make_dma_rsrc(a.q + at, slab), own, wq0, a.Sq, lane);
-        own_load<D>(make_dma_rsrc(a.d_o + at, slab), own + 2 * L::TILE, wq0, a.Sq, lane);
+        own_load<D>(make_dma_rsrc(a.d_o + at, slab), own + L::OWN_WAVE / 2, wq0, a.Sq, lane);
         asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
         own_read<D>(qf, read, own);
-        own_read<D>(gf, read, own + 2 * L::TILE);
+        own_read<D>(gf, read, own + L::OWN_WAVE / 2);
     }
     publish_barrier<0>();  // (all have read their own: its place is free)
     if (begin + 1 < end) issue(begin + 1, 1);
@@ -800,7 +809,8 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
 // over all heads, as the plan names them, or where those would be too many, the blocks of
 // both kinds interleaved in proportion.
 template <int D, bool CAUSAL>
-__global__ __launch_bounds__(kBwdThreads, 1) void bwd_kernel(
+__global__ __launch_bounds__(
+    BwdShape<D>::THREADS, BwdShape<D>::WAVES_PER_SIMD) void bwd_kernel(
     const BwdArgs a, const typename std::conditional<CAUSAL, BwdOrder, int>::type order) {
     __shared__ __attribute__((aligned(1024))) char lds[BwdLds<D>::BYTES];
     const int heads = (int)a.kv_heads, units = a.kv_units + a.group * a.q_units;
@@ -896,9 +906,9 @@ hipError_t launch_d(const BwdPlan& p, const BwdArgs& a, int causal, int o_bf16,
     if (e != hipSuccess) return e;
     const dim3 grid((unsigned)p.grid);
     if (causal)
-        bwd_kernel<D, true><<<grid, kBwdThreads, 0, stream>>>(a, p.order);
+        bwd_kernel<D, true><<<grid, BwdShape<D>::THREADS, 0, stream>>>(a, p.order);
     else
-        bwd_kernel<D, false><<<grid, kBwdThreads, 0, stream>>>(a, 0);
+        bwd_kernel<D, false><<<grid, BwdShape<D>::THREADS, 0, stream>>>(a, 0);
     e = hipGetLastError();
     if (e != hipSuccess || (!p.kv_chunk && !p.q_chunk)) return e;
     const long long kv_rows = p.kv_chunk ? a.kv_heads * a.Skv : 0;

@@ -205,13 +205,13 @@ __device__ __forceinline__ void score_add(f32x16& d, bf16x8 a, bf16x8 b) {
         asm volatile(ATTN_SCORE_MFMA("%0") : "+v"(d) : "v"(a), "v"(b));
 }
 #undef ATTN_SCORE_MFMA
-template <int N>
+template <int FROM, int TO, int N>
 __device__ __forceinline__ void settle(f32x16 (&d)[N]) {
-    static_assert(N == 1 || N == 2, "");
-    if constexpr (N == 2)
-        asm volatile("s_nop 9" : "+v"(d[0]), "+v"(d[1]));
+    static_assert(TO <= N && TO - FROM <= 2 && TO > FROM, "");
+    if constexpr (TO - FROM == 2)
+        asm volatile("s_nop 9" : "+v"(d[FROM]), "+v"(d[FROM + 1]));
     else
-        asm volatile("s_nop 9" : "+v"(d[0]));
+        asm volatile("s_nop 9" : "+v"(d[FROM]));
 }
 
 // Row of accumulator register r in lane half hh.
@@ -285,7 +285,7 @@ struct BwdLds {
 };
 
 // A wave's own rows of a head's slab as operand registers: op[b][ks] holds row l%32 of
-// the b-th 32, values 16*ks + 8*(l/32) ..+7.  Loaded straight into registers, an
+// the wave's b-th block, values 16*ks + 8*(l/32) ..+7.  Loaded straight into registers, an
 // instruction touches 32 rows, 32 bytes each, and the operands of a workgroup took 5.8 us;
 // through LDS in whole rows they take 3.  own_load issues the loads, own_read reads what
 // has landed.
@@ -297,7 +297,8 @@ __device__ __forceinline__ void own_load(dma_rsrc_t rsrc, uint32_t lds, int row0
     for (int p = 0; p < 32 * BwdShape<D>::BLOCKS / ROWS; ++p) {
         const int r = p * ROWS + lane / (D / 8);
         const int c = (lane % (D / 8)) ^ tile_swizzle<D>(r & 31);
-        lds_dma16(rsrc, lds + p * 1024, min(row0 + r, n_rows - 1) * (D * 2) + c * 16, 0);
+        const int row = row0 + r / 32 * (32 * BwdShape<D>::WAVES) + r % 32;
+        lds_dma16(rsrc, lds + p * 1024, min(row, n_rows - 1) * (D * 2) + c * 16, 0);
     }
 }
 template <int D>
@@ -372,7 +373,10 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int k0 = block * kBwdBlock;
-    const int wk0 = k0 + wave * 32 * KB;  // first key of the wave
+    // the wave's blocks of 32 keys are KSTEP apart, so that near a causal diagonal all
+    // waves have their second block hidden at the same time
+    constexpr int KSTEP = 32 * BwdShape<D>::WAVES;
+    const int wk0 = k0 + wave * 32;  // first key of the wave's first block
 
     bf16x8 kf[KB][KD], vf[KB][KD];  // B operands: lane l holds key l%32
     f32x16 dk[KB][CB] = {}, dv[KB][CB] = {};
@@ -466,13 +470,15 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
     };
     // The weights (two values of each block) follow S during the products of dP and of the
     // first half of dV; dS during those of dV.
-    auto weight = [&](auto r_tag, Scores& x_) __attribute__((always_inline)) {
+    // (NA: the blocks at work, the first ones)
+    auto weight = [&](auto r_tag, auto na, Scores& x_) __attribute__((always_inline)) {
+        constexpr int NA = decltype(na)::value;
         f32x16(&s)[KB] = x_.s;
         f32x4(&nl)[2] = x_.nl;
         uint32_t(&pk)[KB][8] = x_.pk;
         constexpr int r = decltype(r_tag)::value;
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
+        for (int kb = 0; kb < NA; ++kb) {
             s[kb][r] =
                 __builtin_amdgcn_exp2f(fmaf(s[kb][r], a.scale_log2, nl[(r / 4) % 2][r % 4]));
             if constexpr (r % 2 == 1) pk[kb][r / 2] = round2(s[kb][r - 1], s[kb][r]);
@@ -480,20 +486,20 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
         if constexpr (r % 4 == 3 && r + 5 < 16) nl[(r / 4) % 2] = lds_quad(nl_base + 8 * (r + 5));
     };
     // Scores of hidden pairs: their weights come out as exactly 0.
-    auto hide = [&](int q0, Scores& x_) __attribute__((always_inline)) {
+    auto hide = [&](int q0, auto na, Scores& x_) __attribute__((always_inline)) {
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-            const int lim = wk0 + kb * 32 + l32 - q0 - diag - 4 * hh;
+        for (int kb = 0; kb < decltype(na)::value; ++kb) {
+            const int lim = wk0 + kb * KSTEP + l32 - q0 - diag - 4 * hh;
 #pragma unroll
             for (int r = 0; r < 16; ++r) x_.s[kb][r] = acc_row(r, 0) >= lim ? x_.s[kb][r] : a.hidden;
         }
     };
-    auto grad = [&](auto r_tag, Scores& x_) __attribute__((always_inline)) {
+    auto grad = [&](auto r_tag, auto na, Scores& x_) __attribute__((always_inline)) {
         f32x16(&s)[KB] = x_.s;
         f32x16(&dp)[KB] = x_.dp;
         constexpr int r = decltype(r_tag)::value;
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
+        for (int kb = 0; kb < decltype(na)::value; ++kb) {
             dp[kb][r] *= s[kb][r];
             if constexpr (r % 2 == 1) {
                 dsk[kb][r / 2] = round2(dp[kb][r - 1], dp[kb][r]);
@@ -508,39 +514,38 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
         for (int e = 0; e < 4; ++e) x_.nd[4 * r4 + e] = x[e];
     };
     constexpr int TAIL = OPS - Ring::ahead(0) + 1;  // the last slots, behind the barrier
-    auto body = [&](int q0) __attribute__((always_inline)) {
+    auto body = [&](int q0, auto na) __attribute__((always_inline)) {
+        constexpr int NA = decltype(na)::value;
         Scores x;
         static_for<0, TAIL>([&](auto i_tag) __attribute__((always_inline)) {
             constexpr int i = decltype(i_tag)::value, ph = i / KD, j = i % KD;
             static_for<Ring::ahead(i - 1), Ring::ahead(i)>(fetch);
-            if constexpr (ph == 0 && j >= KD - 4) 
+            if constexpr (ph == 0 && j >= KD - 4)
                 start_dp(std::integral_constant<int, j - (KD - 4)>{}, x);
             if constexpr (ph == 0 && j == KD - 1) {
                 x.nl[0] = lds_quad(nl_base);
                 x.nl[1] = lds_quad(nl_base + 32);
             }
-            static_for<0, KB>([&](auto kb_tag) __attribute__((always_inline)) {
+            static_for<0, NA>([&](auto kb_tag) __attribute__((always_inline)) {
                 product(i_tag, kb_tag, x);
                 // 12 of the 16 rows' weights in the gaps of dP (but for the first slot's,
                 // when S settles), 4 in the first half of dV's; dS in dV's
-                constexpr int n = KB * KD, gap = j * KB + decltype(kb_tag)::value;
-                auto w = [&](auto r) __attribute__((always_inline)) {
-                    weight(r, x);
-                };
+                constexpr int n = NA * KD, gap = j * NA + decltype(kb_tag)::value;
+                auto w = [&](auto r) __attribute__((always_inline)) { weight(r, na, x); };
                 if constexpr (ph == 1 && j > 0)
-                    static_for<(gap - KB) * 12 / (n - KB), (gap - KB + 1) * 12 / (n - KB)>(w);
+                    static_for<(gap - NA) * 12 / (n - NA), (gap - NA + 1) * 12 / (n - NA)>(w);
                 if constexpr (ph == 2 && gap < n / 2)
                     static_for<12 + gap * 4 / (n / 2), 12 + (gap + 1) * 4 / (n / 2)>(w);
                 if constexpr (ph == 2 && j > 0)
-                    static_for<(gap - KB) * 16 / (n - KB), (gap - KB + 1) * 16 / (n - KB)>(
-                        [&](auto r) __attribute__((always_inline)) { grad(r, x); });
+                    static_for<(gap - NA) * 16 / (n - NA), (gap - NA + 1) * 16 / (n - NA)>(
+                        [&](auto r) __attribute__((always_inline)) { grad(r, na, x); });
                 slot_end();
             });
             if constexpr (ph == 1 && j == 0) {
-                settle(x.s);
-                if (CAUSAL && q0 + diag < wk0 + 32 * KB - 1) hide(q0, x);
+                settle<0, NA>(x.s);
+                if (CAUSAL && q0 + diag < wk0 + (NA - 1) * KSTEP + 31) hide(q0, na, x);
             }
-            if constexpr (ph == 2 && j == 0) settle(x.dp);
+            if constexpr (ph == 2 && j == 0) settle<0, NA>(x.dp);
             slot_end();
         });
     };
@@ -561,24 +566,34 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
     if (begin + 1 < end) issue(1);
     tile_bases(0);
     static_for<0, Ring::ahead(-1)>(fetch);
-    for (int step = begin; step < end; ++step) {
-        const int slot = (step - begin) & 1;
+    int slot = 0, step = begin;
+    auto tile = [&](auto na) __attribute__((always_inline)) {
         // (a wave whose keys are all hidden computes zeros: it would only wait)
-        body(qt * 32);
+        body(qt * 32, na);
         if (CAUSAL && ++qt == n_qt) qt = qt0;
         // Every operand of this tile has been read: its slot is free behind the barrier,
         // which also publishes the next tile.
         publish_barrier<0>();
         if (step + 2 < end) issue(slot);
-        tile_bases(slot ^ 1);
+        slot ^= 1;
+        tile_bases(slot);
         Scores none;  // (dK's products read dsk alone)
         static_for<TAIL, OPS>([&](auto i_tag) __attribute__((always_inline)) {
             constexpr int i = decltype(i_tag)::value;
-            static_for<0, KB>(
+            static_for<0, decltype(na)::value>(
                 [&](auto kb_tag) __attribute__((always_inline)) { product(i_tag, kb_tag, none); });
             static_for<Ring::ahead(i - 1) - OPS, Ring::ahead(i) - OPS>(fetch);
             slot_end();
         });
+        ++step;
+    };
+    while (step < end) {
+        // every wave's second block hidden: four of a diagonal's eight tiles
+        if constexpr (CAUSAL && KB == 2)
+            while (step < end && qt * 32 + 31 + diag < k0 + KSTEP)
+                tile(std::integral_constant<int, 1>{});
+        while (step < end && !(CAUSAL && KB == 2 && qt * 32 + 31 + diag < k0 + KSTEP))
+            tile(std::integral_constant<int, KB>{});
     }
 
     __syncthreads();  // the stages overlay the tiles
@@ -591,8 +606,8 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
     const int bf16 = part ? 0 : a.out_bf16;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-        store_rows<D>(dk[kb], stage, dk_out, row0 + kb * 32, last, bf16, a.scale, lane);
-        store_rows<D>(dv[kb], stage, dv_out, row0 + kb * 32, last, bf16, 1.f, lane);
+        store_rows<D>(dk[kb], stage, dk_out, row0 + kb * KSTEP, last, bf16, a.scale, lane);
+        store_rows<D>(dv[kb], stage, dv_out, row0 + kb * KSTEP, last, bf16, 1.f, lane);
     }
 }
 
@@ -605,7 +620,10 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
     typedef BwdLds<D> L;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wq0 = block * kBwdBlock + wave * 32 * QB;  // first query of the wave
+    // the wave's blocks of 32 queries are QSTEP apart, as the keys in dkdv_block
+    constexpr int QSTEP = 32 * BwdShape<D>::WAVES;
+    const int q0 = block * kBwdBlock;
+    const int wq0 = q0 + wave * 32;  // first query of the wave's first block
 
     const int n_qt = (a.Sq + 31) / 32;
     bf16x8 qf[QB][KD], gf[QB][KD];  // B operands: lane l holds query l%32
@@ -613,7 +631,7 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
     f32x16 nd[QB];  // -delta, from which the products of dP start
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-        const int q = wq0 + qb * 32 + l32;
+        const int q = wq0 + qb * QSTEP + l32;
         // (queries past Sq: the last tile's padding, or the last row of all)
         const long long tile = (long long)bh * n_qt + min(q, n_qt * 32 - 1) / 32;
         nl[qb] = a.rows[tile * 64 + l32];
@@ -673,21 +691,24 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
         if constexpr (ph == 2 && j == 0) score_from<true>(dp[qb], x, gf[qb][j], nd[qb]);
         if constexpr (ph == 2 && j > 0) score_add<true>(dp[qb], x, gf[qb][j]);
     };
-    auto weight = [&](auto r_tag) __attribute__((always_inline)) {
-        constexpr int r = decltype(r_tag)::value;
+    // (QF: the first of the blocks at work, the last ones; the others' weights are 0)
+    auto weight = [&](auto r_tag, auto qf_tag) __attribute__((always_inline)) {
+        constexpr int r = decltype(r_tag)::value, QF = decltype(qf_tag)::value;
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) {
+        for (int qb = 0; qb < QF; ++qb) p[qb][r] = 0.f;
+#pragma unroll
+        for (int qb = QF; qb < QB; ++qb) {
             float x = __builtin_amdgcn_exp2f(fmaf(s[qb][r], a.scale_log2, nl[qb]));
             here(x);
             p[qb][r] = x;
         }
     };
     // Scores of hidden pairs and of keys past Skv: their weights come out as exactly 0.
-    auto hide = [&](int k0) __attribute__((always_inline)) {
+    auto hide = [&](int k0, auto qf_tag) __attribute__((always_inline)) {
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb) {
+        for (int qb = decltype(qf_tag)::value; qb < QB; ++qb) {
             const int last =
-                CAUSAL ? min(a.Skv - 1, wq0 + qb * 32 + l32 + diag) : a.Skv - 1;
+                CAUSAL ? min(a.Skv - 1, wq0 + qb * QSTEP + l32 + diag) : a.Skv - 1;
             const int lim = last - k0 - 4 * hh;
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[qb][r] = acc_row(r, 0) <= lim ? s[qb][r] : a.hidden;
@@ -706,34 +727,38 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
     };
     constexpr int N = QB * KD;  // products, and the gaps behind them, of one kind
     constexpr int TAIL = OPS - Ring::ahead(0) + 1;  // the last slots, behind the barrier
-    auto body = [&](int k0) __attribute__((always_inline)) {
+    auto body = [&](int k0, auto qf_tag) __attribute__((always_inline)) {
+        constexpr int QF = decltype(qf_tag)::value;
         static_for<0, TAIL>([&](auto i_tag) __attribute__((always_inline)) {
             constexpr int i = decltype(i_tag)::value, ph = i / KD, j = i % KD;
             static_for<Ring::ahead(i - 1), Ring::ahead(i)>(fetch);
-            static_for<0, QB>([&](auto qb_tag) __attribute__((always_inline)) {
+            // dS of the tile before in the gaps of S; 12 of the 16 rows' weights in those
+            // of dQ, 4 in those of dP; the first slots are left to settle
+            constexpr int Q0 = ph == 1 ? 0 : QF, NQ = QB - Q0;  // (dQ: of all blocks)
+            static_for<Q0, QB>([&](auto qb_tag) __attribute__((always_inline)) {
                 product(i_tag, qb_tag);
-                // dS of the tile before in the gaps of S; 12 of the 16 rows' weights in those
-                // of dQ, 4 in those of dP; the first slots are left to settle
-                constexpr int gap = j * QB + decltype(qb_tag)::value;
-                constexpr int M = N - QB, B = N - QB * (OPS - TAIL);
+                constexpr int gap = j * NQ + decltype(qb_tag)::value - Q0;
+                constexpr int M = NQ * (KD - 1), B = NQ * (KD - (OPS - TAIL));
+                auto w = [&](auto r) __attribute__((always_inline)) { weight(r, qf_tag); };
                 if constexpr (ph == 0 && j > 0)
-                    static_for<(gap - QB) * 16 / M, (gap - QB + 1) * 16 / M>(grad);
+                    static_for<(gap - NQ) * 16 / M, (gap - NQ + 1) * 16 / M>(grad);
                 if constexpr (ph == 1 && j > 0)
-                    static_for<(gap - QB) * 12 / M, (gap - QB + 1) * 12 / M>(weight);
-                if constexpr (ph == 2) static_for<12 + gap * 4 / B, 12 + (gap + 1) * 4 / B>(weight);
+                    static_for<(gap - NQ) * 12 / M, (gap - NQ + 1) * 12 / M>(w);
+                if constexpr (ph == 2) static_for<12 + gap * 4 / B, 12 + (gap + 1) * 4 / B>(w);
                 slot_end();
             });
-            if constexpr (ph == 0 && j == 0) settle(dp);
+            if constexpr (ph == 0 && j == 0) settle<0, QB>(dp);
             if constexpr (ph == 1 && j == 0) {
-                settle(s);
-                if (k0 + 32 > a.Skv || (CAUSAL && k0 + 31 > wq0 + diag)) hide(k0);
+                settle<QF, QB>(s);
+                if (k0 + 32 > a.Skv || (CAUSAL && k0 + 31 > wq0 + QF * QSTEP + diag))
+                    hide(k0, qf_tag);
             }
             slot_end();
         });
     };
     // dQ of the wave's last tile.
     auto drain = [&]() __attribute__((always_inline)) {
-        settle(dp);
+        settle<0, QB>(dp);
         static_for<0, 16>(grad);
         static_for<KD, KD + 3>(fetch);
         static_for<KD, 2 * KD>([&](auto i_tag) __attribute__((always_inline)) {
@@ -761,7 +786,8 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
     if (begin + 1 < end) issue(begin + 1, 1);
     row_base = read.row + lds0;
     static_for<0, Ring::ahead(-1)>(fetch);
-    for (int step = begin; step < end; ++step) {
+    int step = begin;
+    auto tile = [&](auto qf_tag) __attribute__((always_inline)) {
         // (before the first tile: itself, with a dS of 0)
         const int prev = slot == 0 ? 2 : slot - 1, next = slot == 2 ? 0 : slot + 1;
         // opaque, so that the XORed addresses are formed where they are used instead of
@@ -770,7 +796,7 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
         col_base = read.col + lds0 + (step == begin ? slot : prev) * L::SLOT;
         asm volatile("" : "+v"(row_base), "+v"(col_base));
         // (a wave whose pairs are all hidden computes zeros: it would only wait)
-        body(step * 32);
+        body(step * 32, qf_tag);
         // The tile before has been read for good: its slot is free behind the barrier,
         // which also publishes the next tile.
         publish_barrier<0>();
@@ -779,13 +805,19 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
         asm volatile("" : "+v"(row_base));
         static_for<TAIL, OPS>([&](auto i_tag) __attribute__((always_inline)) {
             constexpr int i = decltype(i_tag)::value;
-            static_for<0, QB>(
+            static_for<decltype(qf_tag)::value, QB>(
                 [&](auto qb_tag) __attribute__((always_inline)) { product(i_tag, qb_tag); });
             static_for<Ring::ahead(i - 1) - OPS, Ring::ahead(i) - OPS>(fetch);
             slot_end();
         });
         slot = next;
-    }
+        ++step;
+    };
+    // every wave's first block hidden: four of a diagonal's eight tiles, the last ones
+    const int half = CAUSAL && QB == 2 ? min(end, (q0 + QSTEP - 1 + diag) / 32 + 1) : end;
+    while (step < half) tile(std::integral_constant<int, 0>{});
+    if constexpr (CAUSAL && QB == 2)
+        while (step < end) tile(std::integral_constant<int, 1>{});
     col_base = read.col + lds0 + (slot == 0 ? 2 : slot - 1) * L::SLOT;
     drain();
 
@@ -796,7 +828,7 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
     char* stage = lds + wave * stage_bytes<D>();
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb)
-        store_rows<D>(dq[qb], stage, out, row0 + qb * 32, (long long)(bh + 1) * a.Sq,
+        store_rows<D>(dq[qb], stage, out, row0 + qb * QSTEP, (long long)(bh + 1) * a.Sq,
                       part ? 0 : a.out_bf16, a.scale, lane);
 }
 

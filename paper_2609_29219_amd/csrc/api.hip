@@ -1079,6 +1079,7 @@ int attn_bwd(const void* q, const void* k, const void* v, const void* o, const f
         a.Sq = Sq;
         a.Skv = Skv;
         a.group = Hq / Hkv;
+        a.causal = causal ? 1 : 0;
         a.q_heads = (long long)B * Hq;
         a.kv_heads = (long long)B * Hkv;
         a.num_xcds = st->desc.num_xcds;
@@ -1087,7 +1088,7 @@ int attn_bwd(const void* q, const void* k, const void* v, const void* o, const f
         if (fabsf(a.scale_log2) < FLT_MIN) a.scale_log2 = scale < 0.f ? -FLT_MIN : FLT_MIN;
         a.hidden = scale < 0.f ? INFINITY : -INFINITY;
         const hipError_t e =
-            launch_bwd(plan, a, d, causal ? 1 : 0, (flags & ATTN_O_BF16) ? 1 : 0, t_stream);
+            launch_bwd(plan, a, d, (flags & ATTN_O_BF16) ? 1 : 0, t_stream);
         return e == hipSuccess ? ATTN_OK : fail_hip(e, "backward launch");
     });
 }

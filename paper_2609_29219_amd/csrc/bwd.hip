@@ -173,11 +173,12 @@ struct QRing {
 // The gradients' accumulators fill the accumulation registers, and the scores must stay
 // out of them: the VALU cannot read those, and the compiler, left to itself, puts every
 // product's result there and moves accumulators out and back in on every tile (192 moves
-// in the dK/dV kernel).  So the scores' products are written out, with plain registers.
-// The compiler does not see the waits that they need, which the assembly therefore
-// holds itself: two wait states before each (a VALU result read by it), and settle(),
-// twenty, between the last product of a block and its first other use.  (A product that
-// adds to the one before needs none.)
+// a tile for dK, dV).  So the scores' products are written out, with plain registers.
+// The compiler does not see the wait states that these need.  Between the last product of
+// a block and its first other use (12) settle() holds them; between a VALU result and the
+// product that reads it (2) none are held, because no operand of these products is one:
+// they come from LDS, from registers that the loop does not write, or from the product
+// before.  tests/test_bwd_hazards.py checks both in the generated code.
 __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
@@ -209,9 +210,9 @@ template <int FROM, int TO, int N>
 __device__ __forceinline__ void settle(f32x16 (&d)[N]) {
     static_assert(TO <= N && TO - FROM <= 2 && TO > FROM, "");
     if constexpr (TO - FROM == 2)
-        asm volatile("s_nop 9" : "+v"(d[FROM]), "+v"(d[FROM + 1]));
+        asm volatile("s_nop 11" : "+v"(d[FROM]), "+v"(d[FROM + 1]));
     else
-        asm volatile("s_nop 9" : "+v"(d[FROM]));
+        asm volatile("s_nop 11" : "+v"(d[FROM]));
 }
 
 // Row of accumulator register r in lane half hh.
@@ -836,81 +837,41 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
 // Workgroups: for every key/value head, the parts of its blocks of keys and of the blocks
 // of queries of its group, in one launch, so that the one kind fills the other's gaps.
 // The hardware deals workgroups round-robin to the XCDs; each XCD gets whole heads, whose
-// tiles stay in its L2, where they can be dealt evenly.  Blocks of keys take longer (four
-// products to three) and come first; under a causal mask, the longest parts of both kinds,
-// over all heads, as the plan names them, or where those would be too many, the blocks of
-// both kinds interleaved in proportion.
+// tiles stay in its L2, where they can be dealt evenly.
 template <int D, bool CAUSAL>
 __global__ __launch_bounds__(
     BwdShape<D>::THREADS, BwdShape<D>::WAVES_PER_SIMD) void bwd_kernel(
     const BwdArgs a, const typename std::conditional<CAUSAL, BwdOrder, int>::type order) {
     __shared__ __attribute__((aligned(1024))) char lds[BwdLds<D>::BYTES];
-    const int heads = (int)a.kv_heads, units = a.kv_units + a.group * a.q_units;
+    const int heads = (int)a.kv_heads;
     const bool even = heads % a.num_xcds == 0;
-    const int hx = even ? heads / a.num_xcds : heads;
-    const int first = even ? (int)(blockIdx.x % a.num_xcds) * hx : 0;
-    const int i = even ? (int)(blockIdx.x / a.num_xcds) : (int)blockIdx.x;
-    // this workgroup: kind, key/value head, head of its group, block, part of how many
-    bool is_kv;
-    int head, g = 0, block, split = 0, splits = 1;
-    if (CAUSAL && a.ordered) {
-        BwdUnit u{};
-        if constexpr (CAUSAL) u = order.unit[i / hx];
-        head = i % hx;
-        is_kv = u.kv;
-        g = u.g;
-        block = u.block;
-        split = u.split;
-        splits = is_kv ? bwd_parts(bwd_kv_steps(block, a.Sq, a.Skv, a.group, true), a.kv_chunk)
-                       : bwd_parts(bwd_q_steps(block, a.Sq, a.Skv, true), a.q_chunk);
-    } else {
-        int x;  // among the head's units of the kind
-        if (CAUSAL) {  // many units, none of them split
-            const int unit = i / hx;
-            head = i - unit * hx;
-            x = bwd_kv_before(unit, a.kv_units, units);
-            is_kv = bwd_kv_before(unit + 1, a.kv_units, units) > x;
-            if (!is_kv) x = unit - x;
-        } else {
-            is_kv = i < hx * a.kv_units;
-            x = is_kv ? i : i - hx * a.kv_units;
-            const int n = is_kv ? a.kv_units : a.group * a.q_units;
-            head = x / n;
-            x -= head * n;
-        }
-        block = x;
-        if (!is_kv) {
-            block = x / a.group;
-            g = x - block * a.group;
-        }
-        if (!CAUSAL && (is_kv ? a.kv_chunk : a.q_chunk)) {  // all blocks of a kind alike
-            splits = is_kv ? bwd_parts(bwd_kv_steps(0, a.Sq, a.Skv, a.group, false), a.kv_chunk)
-                           : bwd_parts(bwd_q_steps(0, a.Sq, a.Skv, false), a.q_chunk);
-            split = block % splits;
-            block /= splits;
-        }
-        if (!is_kv) block = a.q_blocks - 1 - block;
-    }
-    head += first;
-    if (is_kv)
-        dkdv_block<D, CAUSAL>(a, lds, head, block, split, splits);
+    const int first = even ? (int)(blockIdx.x % a.num_xcds) * (heads / a.num_xcds) : 0;
+    BwdUnits units = a.units;
+    units.causal = CAUSAL;
+    const BwdUnit* named = nullptr;
+    if constexpr (CAUSAL) named = order.unit;
+    const BwdWork w = bwd_work(units, named, even ? heads / a.num_xcds : heads,
+                               even ? (int)(blockIdx.x / a.num_xcds) : (int)blockIdx.x);
+    const int head = first + w.head;
+    if (w.kv)
+        dkdv_block<D, CAUSAL>(a, lds, head, w.block, w.split, w.splits);
     else
-        dq_block<D, CAUSAL>(a, lds, head * a.group + g, block, split, splits);
+        dq_block<D, CAUSAL>(a, lds, head * a.group + w.g, w.block, w.split, w.splits);
 }
 
 // Adds up the parts of the blocks that have several, in their order, four values to a
 // thread: dK and dV (z = 0, 1), dQ (2).  HBM bound.
 template <int D>
-__global__ __launch_bounds__(256) void bwd_sum_kernel(const BwdArgs a, int causal) {
+__global__ __launch_bounds__(256) void bwd_sum_kernel(const BwdArgs a) {
     const bool q = blockIdx.z == 2;
-    const int chunk = q ? a.q_chunk : a.kv_chunk, S = q ? a.Sq : a.Skv;
+    const int chunk = q ? a.units.q_chunk : a.units.kv_chunk, S = q ? a.Sq : a.Skv;
     const long long rows = (q ? a.q_heads : a.kv_heads) * S;
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
     const long long row = i / (D / 4);
     if (!chunk || row >= rows) return;
     const int block = (int)(row % S) / kBwdBlock;
-    const int n = bwd_parts(q ? bwd_q_steps(block, a.Sq, a.Skv, causal)
-                              : bwd_kv_steps(block, a.Sq, a.Skv, a.group, causal), chunk);
+    const int n = bwd_parts(q ? bwd_q_steps(block, a.Sq, a.Skv, a.causal)
+                              : bwd_kv_steps(block, a.Sq, a.Skv, a.group, a.causal), chunk);
     if (n == 1) return;
     const float* part = (q ? a.part_q : blockIdx.z ? a.part_v : a.part_k) + i * 4;
     void* out = q ? a.dq : blockIdx.z ? a.dv : a.dk;
@@ -926,8 +887,7 @@ __global__ __launch_bounds__(256) void bwd_sum_kernel(const BwdArgs a, int causa
 }
 
 template <int D>
-hipError_t launch_d(const BwdPlan& p, const BwdArgs& a, int causal, int o_bf16,
-                    hipStream_t stream) {
+hipError_t launch_d(const BwdPlan& p, const BwdArgs& a, int o_bf16, hipStream_t stream) {
     const long long slots = a.q_heads * ((a.Sq + 31) / 32) * 32 * (D / 8);
     const dim3 row_grid((unsigned)((slots + 255) / 256));
     if (o_bf16)
@@ -937,7 +897,7 @@ hipError_t launch_d(const BwdPlan& p, const BwdArgs& a, int causal, int o_bf16,
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const dim3 grid((unsigned)p.grid);
-    if (causal)
+    if (a.causal)
         bwd_kernel<D, true><<<grid, BwdShape<D>::THREADS, 0, stream>>>(a, p.order);
     else
         bwd_kernel<D, false><<<grid, BwdShape<D>::THREADS, 0, stream>>>(a, 0);
@@ -947,29 +907,23 @@ hipError_t launch_d(const BwdPlan& p, const BwdArgs& a, int causal, int o_bf16,
     const long long q_rows = p.q_chunk ? a.q_heads * a.Sq : 0;
     const long long quads = (kv_rows > q_rows ? kv_rows : q_rows) * (D / 4);
     bwd_sum_kernel<D><<<dim3((unsigned)((quads + 255) / 256), 1, p.q_chunk ? 3 : 2), 256, 0,
-                        stream>>>(a, causal);
+                        stream>>>(a);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_bwd(const BwdPlan& p, const BwdArgs& args, int d, int causal, int o_bf16,
+hipError_t launch_bwd(const BwdPlan& p, const BwdArgs& args, int d, int o_bf16,
                       hipStream_t stream) {
     BwdArgs a = args;
-    a.kv_blocks = p.kv_blocks;
-    a.kv_units = p.kv_units;
-    a.kv_chunk = p.kv_chunk;
-    a.q_blocks = p.q_blocks;
-    a.q_units = p.q_units;
-    a.q_chunk = p.q_chunk;
-    a.ordered = p.ordered;
+    a.units = {a.Sq,       a.Skv,     a.group,    a.causal,  p.kv_blocks, p.q_blocks,
+               p.kv_units, p.q_units, p.kv_chunk, p.q_chunk, p.ordered};
     // the parts follow the row values
     const long long kv_values = a.kv_heads * a.Skv * d;
     a.part_k = a.rows + a.q_heads * ((a.Sq + 31) / 32) * 64;
     a.part_v = a.part_k + p.kv_parts * kv_values;
     a.part_q = a.part_v + p.kv_parts * kv_values;
-    return d == 64 ? launch_d<64>(p, a, causal, o_bf16, stream)
-                   : launch_d<128>(p, a, causal, o_bf16, stream);
+    return d == 64 ? launch_d<64>(p, a, o_bf16, stream) : launch_d<128>(p, a, o_bf16, stream);
 }
 
 }  // namespace attn

@@ -303,13 +303,9 @@ ATTN_HD inline int bwd_q_steps(int block, int Sq, int Skv, int causal) {
 ATTN_HD inline int bwd_parts(int steps, int chunk) {
     return chunk ? (steps + chunk - 1) / chunk : 1;
 }
-// Of a head's units (kv of all of them parts of key blocks), how many of the first n are.
-ATTN_HD inline int bwd_kv_before(int n, int kv, int all) {
-    return (int)(((long long)n * kv + all - 1) / all);
-}
 // Causal blocks differ in length: the longest parts start first.  Up to kBwdOrder units
-// are named in that order (more need no exact one: interleaved in proportion, heavy blocks
-// first): of a key/value head's, kind (1: keys), head of the group, block, part.
+// are named in that order (more need no exact one): of a key/value head's, kind (1: keys),
+// head of the group, block, part.
 constexpr int kBwdOrder = 512;
 struct BwdUnit {
     uint16_t kv : 1, g : 15, block, split;
@@ -327,6 +323,65 @@ struct BwdPlan {
     long long grid = 0;
     double modeled_us = 0.0;
 };
+// What a workgroup does: the block of keys or queries of a key/value head (of the given
+// number of heads, and of head g of its group), part `split` of `splits` of its sum.
+struct BwdWork {
+    int kv, head, g, block, split, splits;
+};
+struct BwdUnits {
+    int Sq, Skv, group, causal;
+    int kv_blocks, q_blocks, kv_units, q_units, kv_chunk, q_chunk, ordered;
+};
+// The work of workgroup i of those of `heads` key/value heads: the units of all heads in
+// the plan's order; or the parts of the blocks of keys, which take longer (four products to
+// three), and then of queries, under a causal mask the heavy blocks of all heads first, and
+// without one head by head.
+ATTN_HD inline BwdWork bwd_work(const BwdUnits& a, const BwdUnit* order, int heads, int i) {
+    BwdWork w;
+    w.g = w.split = 0;
+    if (a.ordered) {
+        const BwdUnit u = order[i / heads];
+        w.head = i % heads;
+        w.kv = u.kv;
+        w.g = u.g;
+        w.block = u.block;
+        w.split = u.split;
+        w.splits = w.kv ? bwd_parts(bwd_kv_steps(w.block, a.Sq, a.Skv, a.group, 1), a.kv_chunk)
+                        : bwd_parts(bwd_q_steps(w.block, a.Sq, a.Skv, 1), a.q_chunk);
+        return w;
+    }
+    w.kv = i < heads * a.kv_units;
+    const int x = w.kv ? i : i - heads * a.kv_units;
+    const int n = w.kv ? a.kv_units : a.group * a.q_units;  // of a head
+    int unit;
+    if (a.causal) {
+        unit = x / heads;
+        w.head = x - unit * heads;
+    } else {
+        w.head = x / n;
+        unit = x - w.head * n;
+    }
+    if (!w.kv) {
+        w.g = unit % a.group;
+        unit /= a.group;
+    }
+    const int chunk = w.kv ? a.kv_chunk : a.q_chunk, blocks = w.kv ? a.kv_blocks : a.q_blocks;
+    w.block = unit;
+    w.splits = 1;
+    if (chunk) {  // the block that holds the unit-th part
+        for (w.block = 0;; ++w.block) {
+            w.splits = w.kv ? bwd_parts(bwd_kv_steps(w.block, a.Sq, a.Skv, a.group, a.causal), chunk)
+                            : bwd_parts(bwd_q_steps(blocks - 1 - w.block, a.Sq, a.Skv, a.causal),
+                                        chunk);
+            if (unit < w.splits || w.block + 1 == blocks) break;
+            unit -= w.splits;
+        }
+        w.split = unit;
+    }
+    if (!w.kv) w.block = blocks - 1 - w.block;
+    return w;
+}
+
 struct BwdArgs {
     const uint16_t* q;    // bf16 [B][Hq][Sq][D]
     const uint16_t* k;    // bf16 [B][Hkv][Skv][D]
@@ -337,24 +392,24 @@ struct BwdArgs {
     const float* dlse;    // as lse, or null
     float* rows;          // 64 floats for every 32 query rows (-lse log2 e, -delta)
     void *dq, *dk, *dv;   // fp32 or bf16 (out_bf16)
-    int Sq, Skv, group;
+    int Sq, Skv, group, causal;
     long long q_heads, kv_heads;  // over the batch
     int num_xcds, out_bf16;
     float scale;       // of either sign, or 0
     float scale_log2;  // times log2 e; not 0 (hidden * 0 would be NaN): 0 is FLT_MIN,
     float hidden;      // with which every weight is the same; a hidden pair's score, whose
                        // product with scale_log2 is -inf
-    // from the plan
-    int kv_blocks, q_blocks, kv_units, q_units, kv_chunk, q_chunk, ordered;
+    BwdUnits units;                   // from the plan
     float *part_k, *part_v, *part_q;  // fp32 parts, each as long as the whole result
 };
+// With parts, the workspace may be as large as this (without, it holds the row values).
+constexpr long long kBwdMaxWorkspaceBytes = 1LL << 30;
 // False where a grid would have too many workgroups.
 bool plan_bwd(int num_cus, int B, int Hq, int Hkv, int Sq, int Skv, int d, int causal,
               BwdPlan* out);
 // Workspace in floats: the row values, then the parts.
 long long bwd_workspace_floats(const BwdPlan& p, int B, int Hq, int Hkv, int Sq, int Skv, int d);
-hipError_t launch_bwd(const BwdPlan& p, const BwdArgs& a, int d, int causal, int o_bf16,
-                      hipStream_t stream);
+hipError_t launch_bwd(const BwdPlan& p, const BwdArgs& a, int d, int o_bf16, hipStream_t stream);
 
 // -------------------------------------------------- per-head norm, rotation --
 constexpr int kRopeMaxTile = 16;  // tokens to a tile at most

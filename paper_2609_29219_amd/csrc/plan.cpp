@@ -1114,6 +1114,14 @@ double bwd_makespan(const BwdPlan& p, const BwdCosts& c, int num_cus, int heads,
                          (size_t)group * bwd_parts(bwd_q_steps(b, Sq, Skv, causal), p.q_chunk),
                          q_time(b));
     }
+    if ((long long)times.size() * heads > 16LL * num_cus) {  // many: near what the work allows
+        double total = 0.0, longest = 0.0;
+        for (const double t : times) {
+            total += t * heads;
+            longest = std::max(longest, t);
+        }
+        return std::max(total / num_cus, longest);
+    }
     std::vector<double> free_at(num_cus, 0.0);  // a heap, earliest first
     double last = 0.0;
     for (const double t : times)
@@ -1146,35 +1154,43 @@ bool plan_bwd(int num_cus, int B, int Hq, int Hkv, int Sq, int Skv, int d, int c
     p.grid = heads * units;
     bwd_order(&p, c, group, Sq, Skv, causal);
     *out = p;
-    if (p.grid > 8LL * num_cus) return true;  // many rounds: what a split might save is small
     const double longest =
         std::max(c.kv_step * bwd_kv_steps(0, Sq, Skv, group, causal),
                  c.q_step * bwd_q_steps(p.q_blocks - 1, Sq, Skv, causal));
-    for (int n = 1; n <= 64 && (n == 1 || longest / n >= 2 * c.kv_step);
-         n = n < 8 ? n + 1 : n + n / 4) {
+    double total = c.workgroup * p.grid;
+    for (int b = 0; b < p.kv_blocks; ++b)
+        total += c.kv_step * heads * bwd_kv_steps(b, Sq, Skv, group, causal);
+    for (int b = 0; b < p.q_blocks; ++b)
+        total += c.q_step * heads * group * bwd_q_steps(b, Sq, Skv, causal);
+    // many rounds, and no block that outlasts them: what a split might save is small
+    if (p.grid > 8LL * num_cus && longest < total / num_cus) return true;
+    const double shortest = std::max(2 * c.kv_step, 0.1 * total / num_cus);
+    for (int n = 1; n == 1 || longest / n >= shortest; n = n < 8 ? n + 1 : n + n / 4) {
         BwdPlan t = p;
         t.kv_chunk = (int)ceil(longest / n / c.kv_step);
         t.q_chunk = (int)ceil(longest / n / c.q_step);
         double values = 0.0;  // of parts, written and read
-        t.kv_units = t.q_units = 0;
+        long long kv_units = 0, q_units = 0;
         for (int b = 0; b < p.kv_blocks; ++b) {
             const int m = bwd_parts(bwd_kv_steps(b, Sq, Skv, group, causal), t.kv_chunk);
-            t.kv_units += m;
+            kv_units += m;
             t.kv_parts = std::max(t.kv_parts, m);
             if (m > 1) values += 2.0 * heads * m * kBwdBlock * d;
         }
         for (int b = 0; b < p.q_blocks; ++b) {
             const int m = bwd_parts(bwd_q_steps(b, Sq, Skv, causal), t.q_chunk);
-            t.q_units += m;
+            q_units += m;
             t.q_parts = std::max(t.q_parts, m);
             if (m > 1) values += 1.0 * heads * group * m * kBwdBlock * d;
         }
         if (t.kv_parts <= 1) t.kv_chunk = t.kv_parts = 0;
         if (t.q_parts <= 1) t.q_chunk = t.q_parts = 0;
-        t.grid = heads * (t.kv_units + (long long)group * t.q_units);
-        if (n > 1 && t.grid > 6LL * num_cus) break;
+        t.grid = heads * (kv_units + group * q_units);
+        if (n > 1 && t.grid > p.grid + 6LL * num_cus) break;
+        if (bwd_workspace_floats(t, B, Hq, Hkv, Sq, Skv, d) * 4 > kBwdMaxWorkspaceBytes) continue;
+        t.kv_units = (int)kv_units;
+        t.q_units = (int)q_units;
         bwd_order(&t, c, group, Sq, Skv, causal);
-        if (causal && n > 1 && !t.ordered) break;  // the kernel finds no parts without it
         t.modeled_us = bwd_makespan(t, c, num_cus, (int)heads, group, Sq, Skv, causal) +
                        (values > 0.0 ? 6.0 + values * 8.0 / 6.0e6 : 0.0);
         if (n == 1 || t.modeled_us < out->modeled_us) *out = t;

@@ -1,0 +1,143 @@
+// Host-only sweep of the backward pass's plan (csrc/plan.cpp) and of the work that its
+// workgroups find (bwd_work): every part of every block exactly once, each with at least
+// one step, all of a block's steps dealt out, the workspace no smaller than what the parts
+// take.  Built and run by tests/test_bwd_plan.py, under sanitizers.
+#include <stdio.h>
+#include <stdlib.h>
+#include <string.h>
+
+#include <algorithm>
+#include <random>
+#include <set>
+#include <tuple>
+
+#include "common.h"
+
+using namespace attn;
+
+static const char* check(int cus, int B, int Hq, int Hkv, int Sq, int Skv, int d, int causal,
+                         bool planted) {
+    BwdPlan p;
+    if (!plan_bwd(cus, B, Hq, Hkv, Sq, Skv, d, causal, &p)) return "no plan";
+    const int group = Hq / Hkv, heads = B * Hkv, units = p.kv_units + group * p.q_units;
+    if (p.grid != (long long)heads * units) return "grid";
+    if (p.kv_blocks != (Skv + 255) / 256 || p.q_blocks != (Sq + 255) / 256) return "blocks";
+    if (!p.kv_chunk != !p.kv_parts || !p.q_chunk != !p.q_parts) return "parts without a chunk";
+    if (p.ordered && (!causal || units > kBwdOrder)) return "an order";
+    long long kv_most = 1, q_most = 1, kv_units = 0, q_units = 0;
+    for (int b = 0; b < p.kv_blocks; ++b) {
+        const int steps = bwd_kv_steps(b, Sq, Skv, group, causal), n = bwd_parts(steps, p.kv_chunk);
+        if (steps < 1 || n > steps) return "a part of keys without a step";
+        kv_units += n;
+        if (n > kv_most) kv_most = n;
+        // the first query that any key of the block reaches lies in the first tile walked
+        if (causal) {
+            const long long first = (long long)b * 256 - (Skv - Sq);
+            const int qt0 = (Sq + 31) / 32 - steps / group;
+            if (qt0 * 32 > (first > 0 ? first : 0)) return "tiles left out";
+        }
+    }
+    for (int b = 0; b < p.q_blocks; ++b) {
+        const int steps = bwd_q_steps(b, Sq, Skv, causal), n = bwd_parts(steps, p.q_chunk);
+        if (steps < 1 || n > steps || steps > (Skv + 31) / 32) return "steps of a query block";
+        const long long last = (b + 1) * 256LL < Sq ? (b + 1) * 256LL - 1 : Sq - 1;
+        const long long reach = causal ? last + Skv - Sq : Skv - 1;
+        if (steps * 32LL <= reach) return "keys left out";
+        q_units += n;
+        if (n > q_most) q_most = n;
+    }
+    if (kv_units != p.kv_units || q_units != p.q_units) return "units";
+    if (p.kv_chunk && p.kv_parts != kv_most) return "parts of keys";
+    if (p.q_chunk && p.q_parts != q_most) return "parts of queries";
+    const long long rows = (long long)B * Hq * ((Sq + 31) / 32) * 64;
+    if (bwd_workspace_floats(p, B, Hq, Hkv, Sq, Skv, d) <
+        rows + (p.kv_chunk ? 2 * kv_most * heads * Skv * d : 0) +
+            (p.q_chunk ? q_most * B * Hq * Sq * d : 0))
+        return "workspace";
+    if ((p.kv_chunk || p.q_chunk) &&
+        bwd_workspace_floats(p, B, Hq, Hkv, Sq, Skv, d) * 4 > kBwdMaxWorkspaceBytes)
+        return "a workspace over the limit";
+    // no block outlasts the rest of the work many times over, if splitting can help it
+    double total = 0.0, longest = 0.0;
+    for (int b = 0; b < p.kv_blocks; ++b) {
+        const double steps = bwd_kv_steps(b, Sq, Skv, group, causal);
+        total += 1.25 * steps * heads;
+        longest = std::max(longest, 1.25 * steps / bwd_parts((int)steps, p.kv_chunk));
+    }
+    for (int b = 0; b < p.q_blocks; ++b) {
+        const double steps = bwd_q_steps(b, Sq, Skv, causal);
+        total += steps * heads * group;
+        longest = std::max(longest, steps / bwd_parts((int)steps, p.q_chunk));
+    }
+    if (cus == 256 && longest > 30.0 && longest > 4.0 * total / cus) return "a block that outlasts the rest";
+    const BwdUnits u = {Sq,         Skv,       group,      causal,    p.kv_blocks, p.q_blocks,
+                        p.kv_units, p.q_units, p.kv_chunk, p.q_chunk, p.ordered};
+    // all heads in one range, as on devices whose dies they do not divide evenly among, or
+    // one die's
+    for (const int hx : {heads, 1}) {
+        if (p.grid / heads * hx > 200000) continue;
+        std::set<std::tuple<int, int, int, int, int>> seen;
+        for (int i = 0; i < units * hx; ++i) {
+            BwdWork w = bwd_work(u, p.order.unit, hx, planted && i == 3 ? 2 : i);
+            const int blocks = w.kv ? p.kv_blocks : p.q_blocks;
+            if (w.head < 0 || w.head >= hx || w.g < 0 || w.g >= (w.kv ? 1 : group)) return "head";
+            if (w.block < 0 || w.block >= blocks) return "block";
+            const int steps = w.kv ? bwd_kv_steps(w.block, Sq, Skv, group, causal)
+                                   : bwd_q_steps(w.block, Sq, Skv, causal);
+            if (w.splits != bwd_parts(steps, w.kv ? p.kv_chunk : p.q_chunk)) return "splits";
+            if (w.split < 0 || w.split >= w.splits) return "split";
+            if ((long long)steps * (w.split + 1) / w.splits <= (long long)steps * w.split / w.splits)
+                return "an empty part";
+            if (!seen.insert({w.kv, w.head, w.g, w.block, w.split}).second) return "twice";
+        }
+        if ((long long)seen.size() != (long long)units * hx) return "left out";
+    }
+    return nullptr;
+}
+
+int main(int argc, char** argv) {
+    const bool planted = argc > 1 && !strcmp(argv[1], "--planted");
+    std::mt19937 rng(7);
+    auto log_int = [&](double lo, double hi) {
+        return (int)exp(std::uniform_real_distribution<double>(log(lo), log(hi))(rng));
+    };
+    const int groups[][2] = {{1, 1}, {1, 8}, {2, 4}, {8, 4}, {8, 8}, {16, 1}, {32, 1}, {3, 5},
+                             {40, 1}, {1, 64}};
+    int n = 0, split = 0, unordered = 0;
+    for (; n < 1500; ++n) {
+        const int* g = groups[rng() % 10];
+        const int B = 1 + rng() % 5, causal = rng() % 2, d = rng() % 2 ? 64 : 128;
+        int Sq = log_int(1, 70000), Skv = rng() % 2 ? Sq : log_int(1, 70000);
+        if (causal && Skv < Sq) std::swap(Sq, Skv);
+        const char* why = check(rng() % 8 ? 256 : 1 + rng() % 304, B, g[0] * g[1], g[0], Sq, Skv,
+                                d, causal, planted);
+        if (why && planted) {
+            printf("caught: %s\n", why);
+            return 0;
+        }
+        if (why) {
+            printf("B=%d Hq=%d Hkv=%d Sq=%d Skv=%d d=%d causal=%d: %s\n", B, g[0] * g[1], g[0], Sq,
+                   Skv, d, causal, why);
+            return 1;
+        }
+        BwdPlan p;
+        plan_bwd(256, B, g[0] * g[1], g[0], Sq, Skv, d, causal, &p);
+        split += p.kv_chunk || p.q_chunk;
+        unordered += causal && !p.ordered;
+    }
+    // one key/value head of many query heads; few keys under many queries and the reverse
+    const int corners[][7] = {{1, 64, 1, 8192, 8192, 128, 1}, {1, 128, 1, 30000, 30000, 64, 1},
+                              {8, 16, 16, 16384, 77, 128, 0}, {1, 64, 1, 200000, 256, 128, 0},
+                              {2, 8, 8, 5, 300000, 128, 1}, {1, 1, 1, 8000000, 1, 64, 0},
+                              {1, 1, 1, 1, 8000000, 128, 1}, {4, 32, 8, 32768, 32768, 128, 1}};
+    for (const auto& c : corners)
+        if (const char* why = check(256, c[0], c[1], c[2], c[3], c[4], c[5], c[6], false))
+            return printf("Hq=%d Hkv=%d Sq=%d Skv=%d: %s\n", c[1], c[2], c[3], c[4], why), 1;
+    // the limits: too many workgroups for a grid is no plan, not an overflow
+    BwdPlan p;
+    if (plan_bwd(256, 1 << 20, 1 << 12, 1 << 12, 4096, 4096, 64, 0, &p)) return printf("limit\n"), 1;
+    if (plan_bwd(256, 1, 1 << 30, 1, 1 << 20, 1 << 20, 64, 0, &p)) return printf("limit\n"), 1;
+    if (!split || !unordered) return printf("the sweep missed a kind\n"), 1;
+    printf("bwd_plan_check ok: %d shapes, %d split, %d without an order\n", n, split, unordered);
+    return planted;
+}

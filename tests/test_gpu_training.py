@@ -65,6 +65,18 @@ def test_attn_bwd(pa, shape, d, causal):
     attn_check(case, pa.attn_bwd(**case), f"{shape} d={d}")
 
 
+@pytest.mark.parametrize("shape", [(1, 64, 1, 700, 700, 64, True), (1, 96, 1, 400, 2000, 128, True),
+                                   (2, 8, 8, 3000, 77, 128, False), (1, 16, 2, 1500, 1, 64, False),
+                                   (1, 4, 1, 6000, 300, 128, False)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_attn_bwd_uneven(pa, shape):
+    # many query heads on one key/value head (more units than the plan names in order), and
+    # few keys under many queries: sums that are split into many parts
+    announce(f"attn_bwd {shape}")
+    case = attn_case(*shape)
+    attn_check(case, pa.attn_bwd(**case), f"{shape}")
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("scale", [-0.1, 0.0, 0.3])
 def test_attn_bwd_scales(pa, d, scale):

@@ -323,14 +323,20 @@ int attn_gemm_plan(const attn_device_desc* desc, int M, int N, int K, int flags,
  *   dlse: NULL, or fp32 [B][Hq][Sq]: the gradient of lse, where a caller uses it
  *   (merging partial attention results).
  *   dq: [B][Hq][Sq][d], dk, dv: [B][Hkv][Skv][d], fp32, or bf16 with ATTN_OUT_BF16;
- *   fully overwritten; they must not overlap each other or the inputs.
- *   workspace: NULL (the library's per-stream workspace, which grows as described
- *   under attn_decode, also under stream capture), or a 16-byte aligned device
+ *   fully overwritten; they must not overlap each other or the inputs (EINVAL).
+ *   workspace: NULL (the library's per-stream workspace, with what attn_decode says
+ *   of its growth and of calls under stream capture: a graph keeps its buffer, and
+ *   its replays have to be ordered with the other calls that use that stream's
+ *   workspace, other graphs captured on it among them), or a 16-byte aligned device
  *   buffer of at least attn_bwd_workspace_bytes(...) bytes that the caller keeps
- *   alive until the stream has passed this call; calls that share it must be ordered
- *   on one stream.  With a caller workspace the call allocates nothing.
+ *   alive until the stream has passed this call; calls that share it must be ordered.
+ *   With a caller workspace the call allocates nothing.
  * Work: seven products on bf16 MFMA with fp32 accumulation; P and dS are rounded
- * to bf16 as operands; every call gives the same bits (no atomics).
+ * to bf16 as operands; every call gives the same bits (no atomics).  Where blocks of
+ * 256 keys or queries are few or uneven, their sums are split, the parts (fp32, up
+ * to 1 GiB of the workspace) added in a fixed order.
+ * As in the forward pass, keys, values and rows that a causal mask hides from some
+ * queries still have to hold finite numbers.
  * Errors as attn_fwd_ex; EINVAL also for a misaligned workspace or one smaller
  * than needed; EUNSUPPORTED also for one head's q, k or v over 2 GiB; ENOMEM if
  * there is no memory for the library's workspace.
@@ -368,7 +374,8 @@ typedef struct attn_heads {
  *   q, k, v: bf16 projections, Hq, Hkv and Hkv heads (parts of one fused projection, or
  *   tensors of their own); v may be NULL, and then v_out too.
  *   q_out, k_out, v_out: bf16 results, of any layout: contiguous [B][H][S][d] for
- *   attn_fwd, or rows of a longer cache.  They must not overlap the inputs or each other.
+ *   attn_fwd, rows of a longer cache, or the input's own rows (in place).  Otherwise they
+ *   must not overlap the inputs or each other.
  *   q_weight, k_weight: [d], bf16, or fp32 with ATTN_WEIGHT_F32; 16-byte aligned.
  *   inv_freq: fp32 [rot / 2].
  *   positions: NULL (row s is at position s), or int32, with ATTN_POSITIONS_I64 int64,

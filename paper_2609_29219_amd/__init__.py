@@ -14,6 +14,7 @@ device.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import math
 import os
@@ -370,15 +371,15 @@ def attn_bwd(do, q, k, v, o, lse, scale: float | None = None, causal: bool = Fal
     if out_dtype not in (f32, bf16):
         raise ValueError("out_dtype must be torch.float32 or torch.bfloat16")
     if dq is None:
-        dq = torch.empty(qs, dtype=out_dtype, device=q.device)
+        dq = torch.empty_like(q, dtype=out_dtype)
     else:
         _require_on(dq, out_dtype, qs, "dq", dev)
     if dk is None:
-        dk = torch.empty(ks, dtype=out_dtype, device=q.device)
+        dk = torch.empty_like(k, dtype=out_dtype)
     else:
         _require_on(dk, out_dtype, ks, "dk", dev)
     if dv is None:
-        dv = torch.empty(ks, dtype=out_dtype, device=q.device)
+        dv = torch.empty_like(v, dtype=out_dtype)
     else:
         _require_on(dv, out_dtype, ks, "dv", dev)
     if scale is None:
@@ -417,10 +418,11 @@ def _rows(t, dtype, shape, name, dev):
 
 
 def _head_major_out(out, B, S, H, d, name, like):
-    """An output [B,H,S,d] (the given one, checked, or a new one) and its fields."""
+    """An output [B,H,S,d] (the given one, checked, or a new bf16 one as like is) and its
+    fields."""
     import torch
     if out is None:
-        out = torch.empty((B, H, S, d), dtype=torch.bfloat16, device=like.device)
+        out = like.new_empty((B, H, S, d))
         return out, (out.data_ptr(), H * S * d, d, S * d)
     return out, _head_major(out, torch.bfloat16, (B, H, S, d), name, like.get_device())
 
@@ -441,12 +443,13 @@ _NO_HEADS = (0, 0, 0, 0)
 
 
 def _heads_array(*fields):
-    """An array of attn_heads from their fields, and the address of each (None for
-    _NO_HEADS)."""
-    flat = [x for f in fields for x in f]
-    array = (ctypes.c_longlong * len(flat))(*flat)
-    base = ctypes.addressof(array)
-    return array, [base + 32 * i if f is not _NO_HEADS else None for i, f in enumerate(fields)]
+    """An array of attn_heads from their fields (four 64-bit numbers each), to be kept
+    until the call, and the address of each (None for _NO_HEADS)."""
+    heads = array.array("q")
+    for f in fields:
+        heads.extend(f)
+    base = heads.buffer_info()[0]
+    return heads, [base + 32 * i if f is not _NO_HEADS else None for i, f in enumerate(fields)]
 
 
 def _rope_common(q, k, q_weight, k_weight, inv_freq, positions, interleaved):
@@ -498,7 +501,8 @@ def qk_norm_rope(q, k, v, q_weight, k_weight, inv_freq, positions=None, eps: flo
     [d], bf16 or fp32.  inv_freq: fp32 [rot/2]; pair i is (i, i + rot/2), or interleaved
     (2i, 2i+1), and turns by position * inv_freq[i].  positions: int32 or int64 [S] or
     [B,S]; None: 0..S-1.  q_out, k_out, v_out: [B,H,S,d], any strides with contiguous rows
-    (for a step of decoding, the cache's rows: k_out=cache[:, :, pos:pos + S])."""
+    (for a step of decoding, the cache's rows: k_out=cache[:, :, pos:pos + S]; in place:
+    q_out=q.transpose(1, 2))."""
     import torch
     B, S, Hq, Hkv, d, rot, dev, flags, small = _rope_common(q, k, q_weight, k_weight, inv_freq,
                                                             positions, interleaved)
@@ -543,8 +547,7 @@ def qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, inv_freq, positions=N
     q_in = _token_major(q, bf16, q_shape, "q", dev)
     k_in = _token_major(k, bf16, k_shape, "k", dev)
     if dq_out is None or dk_out is None or (dv_out is None and dv is not None):
-        parts = torch.empty((B, S, Hq + 2 * Hkv, d), dtype=bf16,
-                            device=q.device).split_with_sizes((Hq, Hkv, Hkv), 2)
+        parts = q.new_empty((B, S, Hq + 2 * Hkv, d)).split_with_sizes((Hq, Hkv, Hkv), 2)
         dq_out = parts[0] if dq_out is None else dq_out
         dk_out = parts[1] if dk_out is None else dk_out
         if dv is not None and dv_out is None:

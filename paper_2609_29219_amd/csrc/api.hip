@@ -1052,6 +1052,19 @@ int attn_bwd(const void* q, const void* k, const void* v, const void* o, const f
         if (flags & ~(ATTN_OUT_BF16 | ATTN_O_BF16))
             return fail(ATTN_EINVAL, "unknown flags 0x%x", flags);
         if (!isfinite(scale)) return fail(ATTN_EINVAL, "scale must be finite");
+        // a result that overlaps an operand or another result would be read half written
+        const long long q_n = (long long)B * Hq * Sq * d, kv_n = (long long)B * Hkv * Skv * d;
+        const int out_size = (flags & ATTN_OUT_BF16) ? 2 : 4;
+        const std::pair<const void*, long long> spans[] = {
+            {dq, q_n * out_size}, {dk, kv_n * out_size}, {dv, kv_n * out_size},
+            {q, q_n * 2}, {k, kv_n * 2}, {v, kv_n * 2}, {d_o, q_n * 2},
+            {o, q_n * ((flags & ATTN_O_BF16) ? 2 : 4)}, {lse, q_n / d * 4}, {dlse, q_n / d * 4}};
+        for (int i = 0; i < 3; ++i)
+            for (int j = i + 1; j < 10; ++j) {
+                const uintptr_t x = (uintptr_t)spans[i].first, y = (uintptr_t)spans[j].first;
+                if (y && x < y + (uintptr_t)spans[j].second && y < x + (uintptr_t)spans[i].second)
+                    return fail(ATTN_EINVAL, "a result overlaps another result or an operand");
+            }
         DeviceState* st = nullptr;
         rc = device_state(&st);
         if (rc) return rc;

@@ -203,6 +203,12 @@ def test_attn_bwd_refusals(pa):
         pa.attn_bwd(**case, out_dtype=torch.float16)
     with pytest.raises(TypeError):
         pa.attn_bwd(**case, dq=torch.empty_like(case["q"]), dk=case["k"].float())
+    for n in ("dq", "dk"):  # a result in an operand's place, or in another result's
+        with pytest.raises(pa.AttnError):
+            pa.attn_bwd(**case, **{n: case["q" if n == "dq" else "k"]})
+    both = torch.empty_like(case["k"])
+    with pytest.raises(pa.AttnError):
+        pa.attn_bwd(**case, dk=both, dv=both)
     wide = attn_case(1, 1, 1, 50, 50, 64, True)
     with pytest.raises(pa.AttnError):  # causal with fewer keys than queries
         pa.attn_bwd(**{**wide, "k": wide["k"][:, :, :40].contiguous(),
@@ -388,6 +394,42 @@ def test_qk_norm_rope_strides_and_cache(pa):
         got = pa.qk_norm_rope(**c, k_out=caches[0][:, :, row:row + 1],
                               v_out=caches[1][:, :, row:row + 1])
         rope_check(c, got, f"cache row {row}")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_qk_norm_rope_in_place(pa, d, interleaved):
+    announce(f"qk_norm_rope in place d={d} {interleaved}")
+    for S, rot in ((1, d), (700, d), (333, d // 2)):
+        c = rope_case(2, S, 5, 2, d, rot, start=9, interleaved=interleaved)
+        want = pa.qk_norm_rope(**c)
+        outs = {n + "_out": c[n].transpose(1, 2) for n in ("q", "k", "v")}
+        got = pa.qk_norm_rope(**c, **outs)
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+        assert got[0].data_ptr() == c["q"].data_ptr()
+
+
+def test_operators_on_streams(pa):
+    # each stream's work behind its own copies, two streams at once
+    announce("norm and rotation on streams")
+    cs = [rope_case(2, 900, 8, 2, 128, 128, seed=s) for s in (1, 2)]
+    gs = [[randn(90 + 3 * s + i, 2, H, 900, 128) for i, H in enumerate((8, 2, 2))]
+          for s in range(2)]
+    back = [{n: t for n, t in c.items() if n != "v"} for c in cs]
+    want = [(*pa.qk_norm_rope(**c), *pa.qk_norm_rope_bwd(*g, **b))
+            for c, g, b in zip(cs, gs, back)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    streams = [torch.cuda.Stream() for _ in cs]
+    for _ in range(4):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append((*pa.qk_norm_rope(**cs[i]),
+                               *pa.qk_norm_rope_bwd(*gs[i], **back[i])))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for g in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(want[i], g))
 
 
 def test_qk_norm_rope_without_values(pa):

@@ -13,8 +13,11 @@ HAS_GPU = torch.cuda.is_available()
 A = 1 << 20  # a fake, 16-byte-aligned address: never dereferenced
 
 
-def bwd(q=A, k=A, v=A, o=A, lse=A, do=A, dlse=None, dq=A, dk=A, dv=A, B=1, Hq=2, Hkv=1, Sq=4,
-        Skv=4, d=64, scale=0.125, causal=0, flags=0, ws=None, ws_bytes=0):
+MB = 1 << 20
+
+
+def bwd(q=A, k=A, v=A, o=A, lse=A, do=A, dlse=None, dq=A + MB, dk=A + 2 * MB, dv=A + 3 * MB, B=1,
+        Hq=2, Hkv=1, Sq=4, Skv=4, d=64, scale=0.125, causal=0, flags=0, ws=None, ws_bytes=0):
     return pa.lib.attn_bwd(q, k, v, o, lse, do, dlse, dq, dk, dv, B, Hq, Hkv, Sq, Skv, d, scale,
                            causal, flags, ws, ws_bytes)
 
@@ -32,6 +35,10 @@ def bwd(q=A, k=A, v=A, o=A, lse=A, do=A, dlse=None, dq=A, dk=A, dv=A, B=1, Hq=2,
     (dict(d=96), pa.ATTN_EUNSUPPORTED), (dict(causal=1, Sq=5), pa.ATTN_EUNSUPPORTED),
     (dict(Skv=0x7FFFFFFF // 256 + 1, d=128), pa.ATTN_EUNSUPPORTED),
     (dict(Sq=0x7FFFFFFF // 256 + 1, d=128), pa.ATTN_EUNSUPPORTED),
+    # results over operands or each other: dq is 2 * 4 * 64 fp32 values, 2048 bytes
+    (dict(dq=A), pa.ATTN_EINVAL), (dict(dk=A + 1008), pa.ATTN_EINVAL),
+    (dict(dv=A + 2 * MB), pa.ATTN_EINVAL), (dict(dk=A + MB + 2032), pa.ATTN_EINVAL),
+    (dict(dlse=A + MB + 2044), pa.ATTN_EINVAL),
 ])
 def test_bwd_rejects_on_host(kw, code):
     assert bwd(**kw) == code
@@ -119,6 +126,9 @@ def test_workspace_queries_reject_on_host(call):
 def test_valid_calls_without_device_are_hip_errors():
     assert bwd() == pa.ATTN_EHIP
     assert bwd(flags=1 | 4, dlse=A, causal=1) == pa.ATTN_EHIP
+    # results right behind one another and behind the operands
+    assert bwd(dk=A + MB + 2048, dv=A + MB + 3072) == pa.ATTN_EHIP
+    assert bwd(dq=A + 2048, dlse=A + MB - 32) == pa.ATTN_EHIP
     assert rope() == pa.ATTN_EHIP
     assert rope(v=None, vo=None, flags=8 | 16 | 32, rot=16, pos=A) == pa.ATTN_EHIP
     # heads outside tokens, one element of any stride, a broadcast input

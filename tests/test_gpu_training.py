@@ -605,3 +605,47 @@ def test_layer_gradients(pa, interleaved):
         off = float((g.double() - w).norm() / w.norm())
         print(f"[layer] d{n}: {off:.2e}", flush=True)
         assert off <= 20 * refs.U, f"d{n}: {off}"
+
+
+# ------------------------------------------------------------- large tensors --
+def test_attn_bwd_past_32_bit_offsets(pa):
+    # 2.3e9 values of q: the last batch, against float64 (gradients from the library's own o
+    # and lse, so the bounds are those of test_attn_bwd_follows_attn_fwd)
+    announce("attn_bwd past 32-bit offsets")
+    B, Hq, S, d = 140, 128, 1024, 128
+    q = torch.empty(B, Hq, S, d, dtype=BF16, device=DEV)
+    do = torch.empty_like(q)
+    for b in range(B):
+        q[b], do[b] = randn(b, Hq, S, d), randn(1000 + b, Hq, S, d)
+    k, v = randn(1, B, 1, S, d), randn(2, B, 1, S, d)
+    o, lse = pa.attn_fwd(q, k, v, causal=True, out_dtype=BF16, return_lse=True)
+    dq, dk, dv = pa.attn_bwd(do, q, k, v, o, lse, causal=True)
+    last = slice(B - 1, B)
+    args = (q[last], k[last], v[last], do[last], 1 / math.sqrt(d), True)
+    exact, bound = refs.attn_backward(*args)
+    loose = refs.attn_backward(args[0], args[1], args[2].abs(), args[3].abs(), *args[4:],
+                               o_step=3 * refs.U)[1]
+    for n, g, e, b1, b2 in zip(("dq", "dk", "dv"), (dq, dk, dv), exact, bound, loose):
+        refs.check(g[last], e, 2 * b1 + 2 * b2, n)
+
+
+def test_qk_norm_rope_past_32_bit_offsets(pa):
+    announce("qk_norm_rope past 32-bit offsets")
+    B, S, Hq, Hkv, d = 5, 1 << 16, 48, 8, 128  # 2.7e9 values, and the gradients in float32
+    x = torch.empty(B, S, Hq + 2 * Hkv, d, dtype=BF16, device=DEV)
+    x[-1] = randn(1, S, Hq + 2 * Hkv, d)
+    x[:-1] = 1.0
+    q, k, v = x.split((Hq, Hkv, Hkv), dim=2)
+    c = rope_case(1, 1, 1, 1, d, d)
+    c.update(q=q, k=k, v=v)
+    tail = {n: t[-1:, -64:] if n in "qkv" else t for n, t in c.items()}
+    tail["positions"] = torch.arange(S - 64, S, device=DEV)
+    got = pa.qk_norm_rope(**c)
+    rope_check(tail, [t[-1:, :, -64:] for t in got], "tail")
+    del got, c["v"]
+    g = [torch.zeros(B, H, S, d, device=DEV) for H in (Hq, Hkv, Hkv)]
+    for t in g:
+        t[-1, :, -64:] = torch.randn(t.shape[1], 64, d, device=DEV)
+    back = pa.qk_norm_rope_bwd(*g, **c)
+    rope_bwd_check(tail, [t[-1:, :, -64:] for t in g],
+                   (*[t[-1:, -64:] for t in back[:3]], *back[3:]), "tail")

@@ -49,11 +49,13 @@ namespace {
 // and two blocks to a wave: every operand read from LDS serves two products (with one, LDS
 // would be as busy as the matrix cores).  With D = 64 the weights, as many for half the
 // products, take as long as those do, and two waves to a SIMD overlap the two kinds of
-// work better than one does (B4 H16 S2048 290 us against 303).
+// work better than one does (B4 H16 S2048 290 us against 303); in two workgroups of 128
+// rows, they leave out more of a causal diagonal (causal 155 us and 149).
 template <int D>
 struct BwdShape {
-    static constexpr int BLOCKS = D == 64 ? 1 : 2, WAVES = kBwdBlock / (32 * BLOCKS);
-    static constexpr int THREADS = 64 * WAVES, WAVES_PER_SIMD = WAVES / 4;
+    static constexpr int ROWS = bwd_block_rows(D), BLOCKS = D == 64 ? 1 : 2;
+    static constexpr int WAVES = ROWS / (32 * BLOCKS), THREADS = 64 * WAVES;
+    static constexpr int WAVES_PER_SIMD = WAVES * bwd_wgs_per_cu(D) / 4;
 };
 
 // Which 16-byte piece of a row holds piece c: c ^ tile_swizzle(row).
@@ -373,7 +375,7 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
     typedef BwdLds<D> L;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int k0 = block * kBwdBlock;
+    const int k0 = block * BwdShape<D>::ROWS;
     // the wave's blocks of 32 keys are KSTEP apart, so that near a causal diagonal all
     // waves have their second block hidden at the same time
     constexpr int KSTEP = 32 * BwdShape<D>::WAVES;
@@ -388,7 +390,7 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
     const int n_qt = (a.Sq + 31) / 32;
     const int qt0 = CAUSAL ? max(0, k0 - diag) / 32 : 0;
     const int per_q = n_qt - qt0;
-    const int steps = bwd_kv_steps(block, a.Sq, a.Skv, a.group, CAUSAL);
+    const int steps = a.units.size.kv_steps(block);
     const int begin = (int)((long long)steps * split / splits);
     const int end = (int)((long long)steps * (split + 1) / splits);
 
@@ -623,7 +625,7 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     // the wave's blocks of 32 queries are QSTEP apart, as the keys in dkdv_block
     constexpr int QSTEP = 32 * BwdShape<D>::WAVES;
-    const int q0 = block * kBwdBlock;
+    const int q0 = block * BwdShape<D>::ROWS;
     const int wq0 = q0 + wave * 32;  // first query of the wave's first block
 
     const int n_qt = (a.Sq + 31) / 32;
@@ -643,7 +645,7 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
     f32x16 dq[QB][CB] = {};
 
     const int diag = a.Skv - a.Sq;
-    const int steps = bwd_q_steps(block, a.Sq, a.Skv, CAUSAL);
+    const int steps = a.units.size.q_steps(block);
     const int begin = (int)((long long)steps * split / splits);
     const int end = (int)((long long)steps * (split + 1) / splits);
 
@@ -846,11 +848,9 @@ __global__ __launch_bounds__(
     const int heads = (int)a.kv_heads;
     const bool even = heads % a.num_xcds == 0;
     const int first = even ? (int)(blockIdx.x % a.num_xcds) * (heads / a.num_xcds) : 0;
-    BwdUnits units = a.units;
-    units.causal = CAUSAL;
     const BwdUnit* named = nullptr;
     if constexpr (CAUSAL) named = order.unit;
-    const BwdWork w = bwd_work(units, named, even ? heads / a.num_xcds : heads,
+    const BwdWork w = bwd_work(a.units, named, even ? heads / a.num_xcds : heads,
                                even ? (int)(blockIdx.x / a.num_xcds) : (int)blockIdx.x);
     const int head = first + w.head;
     if (w.kv)
@@ -864,14 +864,12 @@ __global__ __launch_bounds__(
 template <int D>
 __global__ __launch_bounds__(256) void bwd_sum_kernel(const BwdArgs a) {
     const bool q = blockIdx.z == 2;
-    const int chunk = q ? a.units.q_chunk : a.units.kv_chunk, S = q ? a.Sq : a.Skv;
+    const int S = q ? a.Sq : a.Skv;
     const long long rows = (q ? a.q_heads : a.kv_heads) * S;
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
     const long long row = i / (D / 4);
-    if (!chunk || row >= rows) return;
-    const int block = (int)(row % S) / kBwdBlock;
-    const int n = bwd_parts(q ? bwd_q_steps(block, a.Sq, a.Skv, a.causal)
-                              : bwd_kv_steps(block, a.Sq, a.Skv, a.group, a.causal), chunk);
+    if (row >= rows) return;
+    const int n = a.units.parts(!q, (int)(row % S) / BwdShape<D>::ROWS);
     if (n == 1) return;
     const float* part = (q ? a.part_q : blockIdx.z ? a.part_v : a.part_k) + i * 4;
     void* out = q ? a.dq : blockIdx.z ? a.dv : a.dk;
@@ -916,8 +914,8 @@ hipError_t launch_d(const BwdPlan& p, const BwdArgs& a, int o_bf16, hipStream_t 
 hipError_t launch_bwd(const BwdPlan& p, const BwdArgs& args, int d, int o_bf16,
                       hipStream_t stream) {
     BwdArgs a = args;
-    a.units = {a.Sq,       a.Skv,     a.group,    a.causal,  p.kv_blocks, p.q_blocks,
-               p.kv_units, p.q_units, p.kv_chunk, p.q_chunk, p.ordered};
+    a.units = {{bwd_block_rows(d), a.Sq, a.Skv, a.group, a.causal},
+               p.kv_blocks, p.q_blocks, p.kv_units, p.q_units, p.kv_chunk, p.q_chunk, p.ordered};
     // the parts follow the row values
     const long long kv_values = a.kv_heads * a.Skv * d;
     a.part_k = a.rows + a.q_heads * ((a.Sq + 31) / 32) * 64;

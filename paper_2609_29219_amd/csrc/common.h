@@ -283,22 +283,27 @@ hipError_t launch_decode(const DecodePlan& p, const void* q, const void* k, cons
 hipError_t launch_gemm(const GemmPlan& p, const void* a, const void* b, void* c, int M, int N,
                        int K, int out_bf16, int num_xcds, float* workspace, hipStream_t stream);
 // ------------------------------------------------------- attention backward --
-// Workgroups keep a block of kBwdBlock keys (for dK, dV) or queries (for dQ) and walk
-// the tiles of 32 queries (of every head of the group) or keys that it meets: its steps.
-constexpr int kBwdBlock = 256;
+// A workgroup keeps a block of keys (for dK, dV) or of queries (for dQ) and walks the tiles
+// of 32 queries (of every head of the group) or keys that it meets: its steps.
 #ifdef __HIP__
 #define ATTN_HD __host__ __device__
 #else
 #define ATTN_HD
 #endif
-ATTN_HD inline int bwd_kv_steps(int block, int Sq, int Skv, int group, int causal) {
-    const int n_qt = (Sq + 31) / 32, reach = block * kBwdBlock - (Skv - Sq);
-    return (n_qt - (causal && reach > 0 ? reach / 32 : 0)) * group;
-}
-ATTN_HD inline int bwd_q_steps(int block, int Sq, int Skv, int causal) {
-    const int q1 = (block + 1) * kBwdBlock < Sq ? (block + 1) * kBwdBlock : Sq;
-    return ((causal ? q1 + Skv - Sq : Skv) + 31) / 32;
-}
+// Rows of a block, and workgroups that a compute unit holds at once.
+constexpr int bwd_block_rows(int d) { return d == 64 ? 128 : 256; }
+constexpr int bwd_wgs_per_cu(int d) { return d == 64 ? 2 : 1; }
+struct BwdSize {
+    int rows, Sq, Skv, group, causal;
+    ATTN_HD int kv_steps(int block) const {
+        const int n_qt = (Sq + 31) / 32, reach = block * rows - (Skv - Sq);
+        return (n_qt - (causal && reach > 0 ? reach / 32 : 0)) * group;
+    }
+    ATTN_HD int q_steps(int block) const {
+        const int q1 = (block + 1) * rows < Sq ? (block + 1) * rows : Sq;
+        return ((causal ? q1 + Skv - Sq : Skv) + 31) / 32;
+    }
+};
 // Parts of a block's sum, of at most chunk steps each (0: one part).
 ATTN_HD inline int bwd_parts(int steps, int chunk) {
     return chunk ? (steps + chunk - 1) / chunk : 1;
@@ -329,8 +334,12 @@ struct BwdWork {
     int kv, head, g, block, split, splits;
 };
 struct BwdUnits {
-    int Sq, Skv, group, causal;
+    BwdSize size;
     int kv_blocks, q_blocks, kv_units, q_units, kv_chunk, q_chunk, ordered;
+    ATTN_HD int parts(int kv, int block) const {
+        return kv ? bwd_parts(size.kv_steps(block), kv_chunk)
+                  : bwd_parts(size.q_steps(block), q_chunk);
+    }
 };
 // The work of workgroup i of those of `heads` key/value heads: the units of all heads in
 // the plan's order; or the parts of the blocks of keys, which take longer (four products to
@@ -346,15 +355,14 @@ ATTN_HD inline BwdWork bwd_work(const BwdUnits& a, const BwdUnit* order, int hea
         w.g = u.g;
         w.block = u.block;
         w.split = u.split;
-        w.splits = w.kv ? bwd_parts(bwd_kv_steps(w.block, a.Sq, a.Skv, a.group, 1), a.kv_chunk)
-                        : bwd_parts(bwd_q_steps(w.block, a.Sq, a.Skv, 1), a.q_chunk);
+        w.splits = a.parts(w.kv, w.block);
         return w;
     }
     w.kv = i < heads * a.kv_units;
     const int x = w.kv ? i : i - heads * a.kv_units;
-    const int n = w.kv ? a.kv_units : a.group * a.q_units;  // of a head
+    const int n = w.kv ? a.kv_units : a.size.group * a.q_units;  // of a head
     int unit;
-    if (a.causal) {
+    if (a.size.causal) {
         unit = x / heads;
         w.head = x - unit * heads;
     } else {
@@ -362,17 +370,15 @@ ATTN_HD inline BwdWork bwd_work(const BwdUnits& a, const BwdUnit* order, int hea
         unit = x - w.head * n;
     }
     if (!w.kv) {
-        w.g = unit % a.group;
-        unit /= a.group;
+        w.g = unit % a.size.group;
+        unit /= a.size.group;
     }
-    const int chunk = w.kv ? a.kv_chunk : a.q_chunk, blocks = w.kv ? a.kv_blocks : a.q_blocks;
+    const int blocks = w.kv ? a.kv_blocks : a.q_blocks;
     w.block = unit;
     w.splits = 1;
-    if (chunk) {  // the block that holds the unit-th part
+    if (w.kv ? a.kv_chunk : a.q_chunk) {  // the block that holds the unit-th part
         for (w.block = 0;; ++w.block) {
-            w.splits = w.kv ? bwd_parts(bwd_kv_steps(w.block, a.Sq, a.Skv, a.group, a.causal), chunk)
-                            : bwd_parts(bwd_q_steps(blocks - 1 - w.block, a.Sq, a.Skv, a.causal),
-                                        chunk);
+            w.splits = a.parts(w.kv, w.kv ? w.block : blocks - 1 - w.block);
             if (unit < w.splits || w.block + 1 == blocks) break;
             unit -= w.splits;
         }

@@ -1067,18 +1067,19 @@ struct BwdCosts {
 };
 
 // Names the plan's units in the order of their lengths, longest first, if they are few.
-void bwd_order(BwdPlan* p, const BwdCosts& c, int group, int Sq, int Skv, int causal) {
+void bwd_order(BwdPlan* p, const BwdCosts& c, const BwdSize& size) {
+    const int group = size.group;
     const long long units = p->kv_units + (long long)group * p->q_units;
-    p->ordered = causal && units <= kBwdOrder && p->kv_blocks < 65536 && group < 32768;
+    p->ordered = size.causal && units <= kBwdOrder && p->kv_blocks < 65536 && group < 32768;
     if (!p->ordered) return;
     std::vector<std::pair<double, BwdUnit>> all;
     for (int b = 0; b < p->kv_blocks; ++b) {
-        const int steps = bwd_kv_steps(b, Sq, Skv, group, causal), n = bwd_parts(steps, p->kv_chunk);
+        const int steps = size.kv_steps(b), n = bwd_parts(steps, p->kv_chunk);
         for (int i = 0; i < n; ++i)
             all.push_back({c.kv_step * steps / n, {1, 0, (uint16_t)b, (uint16_t)i}});
     }
     for (int b = p->q_blocks - 1; b >= 0; --b) {
-        const int steps = bwd_q_steps(b, Sq, Skv, causal), n = bwd_parts(steps, p->q_chunk);
+        const int steps = size.q_steps(b), n = bwd_parts(steps, p->q_chunk);
         for (int i = 0; i < n; ++i)
             for (int g = 0; g < group; ++g)
                 all.push_back({c.q_step * steps / n, {0, (uint16_t)g, (uint16_t)b, (uint16_t)i}});
@@ -1088,41 +1089,41 @@ void bwd_order(BwdPlan* p, const BwdCosts& c, int group, int Sq, int Skv, int ca
     for (size_t i = 0; i < all.size(); ++i) p->order.unit[i] = all[i].second;
 }
 
-// Time of the workgroups of `heads` heads on num_cus compute units, in the order in which
-// the kernel starts them, each on the unit that is free first.
-double bwd_makespan(const BwdPlan& p, const BwdCosts& c, int num_cus, int heads, int group, int Sq,
-                    int Skv, int causal) {
+// Time of the workgroups of `heads` heads in the places that the compute units have for
+// them, in the order in which the kernel starts them, each in the place that is free first.
+double bwd_makespan(const BwdPlan& p, const BwdCosts& c, const BwdSize& size, int slots,
+                    int heads) {
     auto kv_time = [&](int b) {
-        const int steps = bwd_kv_steps(b, Sq, Skv, group, causal);
+        const int steps = size.kv_steps(b);
         return c.workgroup + c.kv_step * steps / bwd_parts(steps, p.kv_chunk);
     };
     auto q_time = [&](int b) {
-        const int steps = bwd_q_steps(b, Sq, Skv, causal);
+        const int steps = size.q_steps(b);
         return c.workgroup + c.q_step * steps / bwd_parts(steps, p.q_chunk);
     };
     std::vector<double> times;  // of a head's units, in order
     if (p.ordered) {
-        for (int u = 0; u < p.kv_units + group * p.q_units; ++u)
+        for (int u = 0; u < p.kv_units + size.group * p.q_units; ++u)
             times.push_back(p.order.unit[u].kv ? kv_time(p.order.unit[u].block)
                                               : q_time(p.order.unit[u].block));
     } else {
         for (int b = 0; b < p.kv_blocks; ++b)
             times.insert(times.end(),
-                         bwd_parts(bwd_kv_steps(b, Sq, Skv, group, causal), p.kv_chunk), kv_time(b));
+                         bwd_parts(size.kv_steps(b), p.kv_chunk), kv_time(b));
         for (int b = p.q_blocks - 1; b >= 0; --b)
             times.insert(times.end(),
-                         (size_t)group * bwd_parts(bwd_q_steps(b, Sq, Skv, causal), p.q_chunk),
+                         (size_t)size.group * bwd_parts(size.q_steps(b), p.q_chunk),
                          q_time(b));
     }
-    if ((long long)times.size() * heads > 16LL * num_cus) {  // many: near what the work allows
+    if ((long long)times.size() * heads > 16LL * slots) {  // many: near what the work allows
         double total = 0.0, longest = 0.0;
         for (const double t : times) {
             total += t * heads;
             longest = std::max(longest, t);
         }
-        return std::max(total / num_cus, longest);
+        return std::max(total / slots, longest);
     }
-    std::vector<double> free_at(num_cus, 0.0);  // a heap, earliest first
+    std::vector<double> free_at(slots, 0.0);  // a heap, earliest first
     double last = 0.0;
     for (const double t : times)
         for (int h = 0; h < heads; ++h) {
@@ -1140,31 +1141,32 @@ double bwd_makespan(const BwdPlan& p, const BwdCosts& c, int num_cus, int heads,
 // the fastest of the model's.
 bool plan_bwd(int num_cus, int B, int Hq, int Hkv, int Sq, int Skv, int d, int causal,
               BwdPlan* out) {
-    const int group = Hq / Hkv;
+    const int group = Hq / Hkv, rows = bwd_block_rows(d), slots = num_cus * bwd_wgs_per_cu(d);
+    const BwdSize size = {rows, Sq, Skv, group, causal};
     const long long n_qt = ((long long)Sq + 31) / 32;
     BwdPlan p;
-    p.kv_blocks = p.kv_units = (int)(((long long)Skv + kBwdBlock - 1) / kBwdBlock);
-    p.q_blocks = p.q_units = (int)(((long long)Sq + kBwdBlock - 1) / kBwdBlock);
+    p.kv_blocks = p.kv_units = (int)(((long long)Skv + rows - 1) / rows);
+    p.q_blocks = p.q_units = (int)(((long long)Sq + rows - 1) / rows);
     const long long heads = (long long)B * Hkv;
     const long long units = p.kv_units + (long long)group * p.q_units;
     if (n_qt * group > 0x3fffffffLL || heads > 0x3fffffffLL || units > 0x3fffffffLL ||
         heads * units > 0x3fffffffLL)
         return false;
-    const BwdCosts c = d == 64 ? BwdCosts{0.95, 0.75, 6.0} : BwdCosts{1.7, 1.35, 7.0};
+    const BwdCosts c = d == 64 ? BwdCosts{1.05, 0.82, 6.0} : BwdCosts{1.7, 1.35, 7.0};
     p.grid = heads * units;
-    bwd_order(&p, c, group, Sq, Skv, causal);
+    bwd_order(&p, c, size);
     *out = p;
     const double longest =
-        std::max(c.kv_step * bwd_kv_steps(0, Sq, Skv, group, causal),
-                 c.q_step * bwd_q_steps(p.q_blocks - 1, Sq, Skv, causal));
+        std::max(c.kv_step * size.kv_steps(0),
+                 c.q_step * size.q_steps(p.q_blocks - 1));
     double total = c.workgroup * p.grid;
     for (int b = 0; b < p.kv_blocks; ++b)
-        total += c.kv_step * heads * bwd_kv_steps(b, Sq, Skv, group, causal);
+        total += c.kv_step * heads * size.kv_steps(b);
     for (int b = 0; b < p.q_blocks; ++b)
-        total += c.q_step * heads * group * bwd_q_steps(b, Sq, Skv, causal);
+        total += c.q_step * heads * group * size.q_steps(b);
     // many rounds, and no block that outlasts them: what a split might save is small
-    if (p.grid > 8LL * num_cus && longest < total / num_cus) return true;
-    const double shortest = std::max(2 * c.kv_step, 0.1 * total / num_cus);
+    if (p.grid > 8LL * slots && longest < total / slots) return true;
+    const double shortest = std::max(2 * c.kv_step, 0.1 * total / slots);
     for (int n = 1; n == 1 || longest / n >= shortest; n = n < 8 ? n + 1 : n + n / 4) {
         BwdPlan t = p;
         t.kv_chunk = (int)ceil(longest / n / c.kv_step);
@@ -1172,26 +1174,26 @@ bool plan_bwd(int num_cus, int B, int Hq, int Hkv, int Sq, int Skv, int d, int c
         double values = 0.0;  // of parts, written and read
         long long kv_units = 0, q_units = 0;
         for (int b = 0; b < p.kv_blocks; ++b) {
-            const int m = bwd_parts(bwd_kv_steps(b, Sq, Skv, group, causal), t.kv_chunk);
+            const int m = bwd_parts(size.kv_steps(b), t.kv_chunk);
             kv_units += m;
             t.kv_parts = std::max(t.kv_parts, m);
-            if (m > 1) values += 2.0 * heads * m * kBwdBlock * d;
+            if (m > 1) values += 2.0 * heads * m * rows * d;
         }
         for (int b = 0; b < p.q_blocks; ++b) {
-            const int m = bwd_parts(bwd_q_steps(b, Sq, Skv, causal), t.q_chunk);
+            const int m = bwd_parts(size.q_steps(b), t.q_chunk);
             q_units += m;
             t.q_parts = std::max(t.q_parts, m);
-            if (m > 1) values += 1.0 * heads * group * m * kBwdBlock * d;
+            if (m > 1) values += 1.0 * heads * group * m * rows * d;
         }
         if (t.kv_parts <= 1) t.kv_chunk = t.kv_parts = 0;
         if (t.q_parts <= 1) t.q_chunk = t.q_parts = 0;
         t.grid = heads * (kv_units + group * q_units);
-        if (n > 1 && t.grid > p.grid + 6LL * num_cus) break;
+        if (n > 1 && t.grid > p.grid + 6LL * slots) break;
         if (bwd_workspace_floats(t, B, Hq, Hkv, Sq, Skv, d) * 4 > kBwdMaxWorkspaceBytes) continue;
         t.kv_units = (int)kv_units;
         t.q_units = (int)q_units;
-        bwd_order(&t, c, group, Sq, Skv, causal);
-        t.modeled_us = bwd_makespan(t, c, num_cus, (int)heads, group, Sq, Skv, causal) +
+        bwd_order(&t, c, size);
+        t.modeled_us = bwd_makespan(t, c, size, slots, (int)heads) +
                        (values > 0.0 ? 6.0 + values * 8.0 / 6.0e6 : 0.0);
         if (n == 1 || t.modeled_us < out->modeled_us) *out = t;
     }

@@ -21,26 +21,29 @@ static const char* check(int cus, int B, int Hq, int Hkv, int Sq, int Skv, int d
     if (!plan_bwd(cus, B, Hq, Hkv, Sq, Skv, d, causal, &p)) return "no plan";
     const int group = Hq / Hkv, heads = B * Hkv, units = p.kv_units + group * p.q_units;
     if (p.grid != (long long)heads * units) return "grid";
-    if (p.kv_blocks != (Skv + 255) / 256 || p.q_blocks != (Sq + 255) / 256) return "blocks";
+    const int rows = bwd_block_rows(d);
+    const BwdSize size = {rows, Sq, Skv, group, causal};
+    if (p.kv_blocks != (Skv + rows - 1) / rows || p.q_blocks != (Sq + rows - 1) / rows)
+        return "blocks";
     if (!p.kv_chunk != !p.kv_parts || !p.q_chunk != !p.q_parts) return "parts without a chunk";
     if (p.ordered && (!causal || units > kBwdOrder)) return "an order";
     long long kv_most = 1, q_most = 1, kv_units = 0, q_units = 0;
     for (int b = 0; b < p.kv_blocks; ++b) {
-        const int steps = bwd_kv_steps(b, Sq, Skv, group, causal), n = bwd_parts(steps, p.kv_chunk);
+        const int steps = size.kv_steps(b), n = bwd_parts(steps, p.kv_chunk);
         if (steps < 1 || n > steps) return "a part of keys without a step";
         kv_units += n;
         if (n > kv_most) kv_most = n;
         // the first query that any key of the block reaches lies in the first tile walked
         if (causal) {
-            const long long first = (long long)b * 256 - (Skv - Sq);
+            const long long first = (long long)b * rows - (Skv - Sq);
             const int qt0 = (Sq + 31) / 32 - steps / group;
             if (qt0 * 32 > (first > 0 ? first : 0)) return "tiles left out";
         }
     }
     for (int b = 0; b < p.q_blocks; ++b) {
-        const int steps = bwd_q_steps(b, Sq, Skv, causal), n = bwd_parts(steps, p.q_chunk);
+        const int steps = size.q_steps(b), n = bwd_parts(steps, p.q_chunk);
         if (steps < 1 || n > steps || steps > (Skv + 31) / 32) return "steps of a query block";
-        const long long last = (b + 1) * 256LL < Sq ? (b + 1) * 256LL - 1 : Sq - 1;
+        const long long last = (long long)(b + 1) * rows < Sq ? (long long)(b + 1) * rows - 1 : Sq - 1;
         const long long reach = causal ? last + Skv - Sq : Skv - 1;
         if (steps * 32LL <= reach) return "keys left out";
         q_units += n;
@@ -49,9 +52,9 @@ static const char* check(int cus, int B, int Hq, int Hkv, int Sq, int Skv, int d
     if (kv_units != p.kv_units || q_units != p.q_units) return "units";
     if (p.kv_chunk && p.kv_parts != kv_most) return "parts of keys";
     if (p.q_chunk && p.q_parts != q_most) return "parts of queries";
-    const long long rows = (long long)B * Hq * ((Sq + 31) / 32) * 64;
+    const long long row_values = (long long)B * Hq * ((Sq + 31) / 32) * 64;
     if (bwd_workspace_floats(p, B, Hq, Hkv, Sq, Skv, d) <
-        rows + (p.kv_chunk ? 2 * kv_most * heads * Skv * d : 0) +
+        row_values + (p.kv_chunk ? 2 * kv_most * heads * Skv * d : 0) +
             (p.q_chunk ? q_most * B * Hq * Sq * d : 0))
         return "workspace";
     if ((p.kv_chunk || p.q_chunk) &&
@@ -60,18 +63,18 @@ static const char* check(int cus, int B, int Hq, int Hkv, int Sq, int Skv, int d
     // no block outlasts the rest of the work many times over, if splitting can help it
     double total = 0.0, longest = 0.0;
     for (int b = 0; b < p.kv_blocks; ++b) {
-        const double steps = bwd_kv_steps(b, Sq, Skv, group, causal);
+        const double steps = size.kv_steps(b);
         total += 1.25 * steps * heads;
         longest = std::max(longest, 1.25 * steps / bwd_parts((int)steps, p.kv_chunk));
     }
     for (int b = 0; b < p.q_blocks; ++b) {
-        const double steps = bwd_q_steps(b, Sq, Skv, causal);
+        const double steps = size.q_steps(b);
         total += steps * heads * group;
         longest = std::max(longest, steps / bwd_parts((int)steps, p.q_chunk));
     }
     if (cus == 256 && longest > 30.0 && longest > 4.0 * total / cus) return "a block that outlasts the rest";
-    const BwdUnits u = {Sq,         Skv,       group,      causal,    p.kv_blocks, p.q_blocks,
-                        p.kv_units, p.q_units, p.kv_chunk, p.q_chunk, p.ordered};
+    const BwdUnits u = {size,      p.kv_blocks, p.q_blocks, p.kv_units, p.q_units,
+                        p.kv_chunk, p.q_chunk,   p.ordered};
     // all heads in one range, as on devices whose dies they do not divide evenly among, or
     // one die's
     for (const int hx : {heads, 1}) {
@@ -82,8 +85,8 @@ static const char* check(int cus, int B, int Hq, int Hkv, int Sq, int Skv, int d
             const int blocks = w.kv ? p.kv_blocks : p.q_blocks;
             if (w.head < 0 || w.head >= hx || w.g < 0 || w.g >= (w.kv ? 1 : group)) return "head";
             if (w.block < 0 || w.block >= blocks) return "block";
-            const int steps = w.kv ? bwd_kv_steps(w.block, Sq, Skv, group, causal)
-                                   : bwd_q_steps(w.block, Sq, Skv, causal);
+            const int steps = w.kv ? size.kv_steps(w.block)
+                                   : size.q_steps(w.block);
             if (w.splits != bwd_parts(steps, w.kv ? p.kv_chunk : p.q_chunk)) return "splits";
             if (w.split < 0 || w.split >= w.splits) return "split";
             if ((long long)steps * (w.split + 1) / w.splits <= (long long)steps * w.split / w.splits)

@@ -338,8 +338,9 @@ int attn_gemm_plan(const attn_device_desc* desc, int M, int N, int K, int flags,
  * As in the forward pass, keys, values and rows that a causal mask hides from some
  * queries still have to hold finite numbers.
  * Errors as attn_fwd_ex; EINVAL also for a misaligned workspace or one smaller
- * than needed; EUNSUPPORTED also for one head's q, k or v over 2 GiB; ENOMEM if
- * there is no memory for the library's workspace.
+ * than needed; EUNSUPPORTED also for one head's q, k or v over 2 GiB or more than
+ * 2^24 - 1 workgroups (tens of millions of heads of a few rows); ENOMEM if there is no
+ * memory for the library's workspace.
  */
 #define ATTN_O_BF16 4          /* attn_bwd flag: o is bf16 */
 int attn_bwd(const void* q, const void* k, const void* v, const void* o, const float* lse,
@@ -385,7 +386,8 @@ typedef struct attn_heads {
  * All arithmetic is fp32 (angles fp64), rounded once.  Asynchronous on the thread's
  * stream; uses no workspace.
  * Errors: EINVAL for null or misaligned pointers, bad strides or overlapping output
- * rows, dims <= 0, unknown flags or eps; EUNSUPPORTED for d or rot.
+ * rows, dims <= 0, unknown flags or eps; EUNSUPPORTED for d, rot or more than 2^28 - 16
+ * tokens.
  */
 #define ATTN_ROPE_INTERLEAVED 8
 #define ATTN_WEIGHT_F32 16

@@ -502,7 +502,8 @@ def qk_norm_rope(q, k, v, q_weight, k_weight, inv_freq, positions=None, eps: flo
     (2i, 2i+1), and turns by position * inv_freq[i].  positions: int32 or int64 [S] or
     [B,S]; None: 0..S-1.  q_out, k_out, v_out: [B,H,S,d], any strides with contiguous rows
     (for a step of decoding, the cache's rows: k_out=cache[:, :, pos:pos + S]; in place:
-    q_out=q.transpose(1, 2))."""
+    q_out=q.transpose(1, 2)), that share no memory with each other or, unless in place, with
+    the projections."""
     import torch
     B, S, Hq, Hkv, d, rot, dev, flags, small = _rope_common(q, k, q_weight, k_weight, inv_freq,
                                                             positions, interleaved)
@@ -530,8 +531,9 @@ def qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, inv_freq, positions=N
 
     dq, dk, dv: gradients of its results, bf16 or fp32 [B,H,S,d], any strides with
     contiguous rows (dv may be None); the rest as qk_norm_rope got it.  dq_out, dk_out,
-    dv_out: any strides with contiguous rows; without them, they are the heads of one fused
-    [B,S,Hq+2*Hkv,d] tensor in this order.  workspace: None (the library's), or a device
+    dv_out: any strides with contiguous rows, sharing no memory with each other or the
+    inputs; without them, they are the heads of one fused [B,S,Hq+2*Hkv,d] tensor in this
+    order.  workspace: None (the library's), or a device
     tensor of at least qk_norm_rope_bwd_workspace_bytes(...) bytes."""
     import torch
     B, S, Hq, Hkv, d, rot, dev, flags, small = _rope_common(q, k, q_weight, k_weight, inv_freq,

@@ -248,6 +248,7 @@ std::map<std::tuple<int, int, int, int, int, int, int, int>, FwdPlan> g_fwd_cach
 std::map<std::tuple<int, int, int, int, int, int, int>, DecodePlan> g_dec_cache;
 std::map<std::tuple<int, int, int, int, int>, GemmPlan> g_gemm_cache;
 std::map<std::tuple<int, int, int, int, int, int, int>, BwdPlan> g_bwd_cache;
+constexpr size_t kBwdCached = 4096;  // plans of 3 KB: training may meet any length
 
 // Structural properties from the runtime; performance properties from the
 // built-in gfx950 description.
@@ -997,6 +998,8 @@ static int validate_bwd_dims(int B, int Hq, int Hkv, int Sq, int Skv, int d, int
     if (longest * d * 2 > 0x7fffffffLL)
         return fail(ATTN_EUNSUPPORTED, "one head's q, k or v (%lld bytes) exceeds 2 GiB",
                     longest * d * 2);
+    if ((double)B * Hq * (double)longest * d > 1e17)  // (sizes in bytes are 64-bit products)
+        return fail(ATTN_EUNSUPPORTED, "tensors too large");
     return ATTN_OK;
 }
 
@@ -1012,8 +1015,9 @@ static int bwd_plan_of(DeviceState* st, int B, int Hq, int Hkv, int Sq, int Skv,
     }
     if (!known) {
         if (!plan_bwd(st->desc.num_cus, B, Hq, Hkv, Sq, Skv, d, causal ? 1 : 0, plan))
-            return fail(ATTN_EUNSUPPORTED, "no feasible backward plan for this shape");
+            return fail(ATTN_EUNSUPPORTED, "more workgroups than one launch holds");
         std::lock_guard<std::mutex> lk(g_mu);
+        if (g_bwd_cache.size() >= kBwdCached) g_bwd_cache.clear();
         g_bwd_cache[key] = *plan;
     }
     *ws_bytes = (size_t)bwd_workspace_floats(*plan, B, Hq, Hkv, Sq, Skv, d) * sizeof(float);
@@ -1111,6 +1115,8 @@ static int validate_rope_dims(int B, int S, int Hq, int Hkv, int d) {
         return fail(ATTN_EINVAL, "dimensions must be positive (B=%d S=%d Hq=%d Hkv=%d d=%d)", B,
                     S, Hq, Hkv, d);
     if (d != 64 && d != 128) return fail(ATTN_EUNSUPPORTED, "head dim %d not in {64, 128}", d);
+    if ((long long)B * S > kMaxWorkgroups * kRopeMaxTile)
+        return fail(ATTN_EUNSUPPORTED, "more than %lld tokens", kMaxWorkgroups * kRopeMaxTile);
     return ATTN_OK;
 }
 

@@ -282,6 +282,9 @@ hipError_t launch_decode(const DecodePlan& p, const void* q, const void* k, cons
 // and the reduction of the partials follows on the same stream.
 hipError_t launch_gemm(const GemmPlan& p, const void* a, const void* b, void* c, int M, int N,
                        int K, int out_bf16, int num_xcds, float* workspace, hipStream_t stream);
+// Workgroups of 256 threads that one launch holds: a grid's size counts threads, in 32 bits.
+constexpr long long kMaxWorkgroups = (1LL << 24) - 1;
+
 // ------------------------------------------------------- attention backward --
 // A workgroup keeps a block of keys (for dK, dV) or of queries (for dQ) and walks the tiles
 // of 32 queries (of every head of the group) or keys that it meets: its steps.
@@ -410,7 +413,7 @@ struct BwdArgs {
 };
 // With parts, the workspace may be as large as this (without, it holds the row values).
 constexpr long long kBwdMaxWorkspaceBytes = 1LL << 30;
-// False where a grid would have too many workgroups.
+// False where a launch would have more than kMaxWorkgroups.
 bool plan_bwd(int num_cus, int B, int Hq, int Hkv, int Sq, int Skv, int d, int causal,
               BwdPlan* out);
 // Workspace in floats: the row values, then the parts.

@@ -1149,8 +1149,10 @@ bool plan_bwd(int num_cus, int B, int Hq, int Hkv, int Sq, int Skv, int d, int c
     p.q_blocks = p.q_units = (int)(((long long)Sq + rows - 1) / rows);
     const long long heads = (long long)B * Hkv;
     const long long units = p.kv_units + (long long)group * p.q_units;
-    if (n_qt * group > 0x3fffffffLL || heads > 0x3fffffffLL || units > 0x3fffffffLL ||
-        heads * units > 0x3fffffffLL)
+    const long long row_wgs = n_qt * (d / 64);  // of a head's row values, d / 8 lanes to a row
+    if (n_qt * group > 0x3fffffffLL || heads > kMaxWorkgroups || units > kMaxWorkgroups ||
+        heads * units > kMaxWorkgroups || row_wgs * group > kMaxWorkgroups ||
+        heads * group * row_wgs > kMaxWorkgroups)
         return false;
     const BwdCosts c = d == 64 ? BwdCosts{1.05, 0.82, 6.0} : BwdCosts{1.7, 1.35, 7.0};
     p.grid = heads * units;
@@ -1188,7 +1190,7 @@ bool plan_bwd(int num_cus, int B, int Hq, int Hkv, int Sq, int Skv, int d, int c
         if (t.kv_parts <= 1) t.kv_chunk = t.kv_parts = 0;
         if (t.q_parts <= 1) t.q_chunk = t.q_parts = 0;
         t.grid = heads * (kv_units + group * q_units);
-        if (n > 1 && t.grid > p.grid + 6LL * slots) break;
+        if (n > 1 && (t.grid > p.grid + 6LL * slots || t.grid > kMaxWorkgroups)) break;
         if (bwd_workspace_floats(t, B, Hq, Hkv, Sq, Skv, d) * 4 > kBwdMaxWorkspaceBytes) continue;
         t.kv_units = (int)kv_units;
         t.q_units = (int)q_units;

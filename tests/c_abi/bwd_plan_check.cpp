@@ -140,6 +140,15 @@ int main(int argc, char** argv) {
     BwdPlan p;
     if (plan_bwd(256, 1 << 20, 1 << 12, 1 << 12, 4096, 4096, 64, 0, &p)) return printf("limit\n"), 1;
     if (plan_bwd(256, 1, 1 << 30, 1, 1 << 20, 1 << 20, 64, 0, &p)) return printf("limit\n"), 1;
+    // a launch's threads are counted in 32 bits: 2^24 workgroups of 256 are too many, of the
+    // products (two of each head here) and of the row values (d = 128: two of each tile)
+    const int many[][4] = {{1 << 23, 1, 64, 0}, {(1 << 23) - 1, 1, 64, 1}, {1 << 16, 128, 128, 0},
+                           {(1 << 18) - 1, 32, 128, 1}, {1 << 20, 32, 64, 0}};
+    for (const auto& c : many) {
+        const bool is = plan_bwd(256, c[0], c[1], 1, 1, 1, c[2], 0, &p);
+        if (is != !!c[3] || (is && p.grid >= 1LL << 24))
+            return printf("B=%d Hq=%d: %d\n", c[0], c[1], is), 1;
+    }
     if (!split || !unordered) return printf("the sweep missed a kind\n"), 1;
     printf("bwd_plan_check ok: %d shapes, %d split, %d without an order\n", n, split, unordered);
     return planted;

@@ -140,6 +140,18 @@ def test_valid_calls_without_device_are_hip_errors():
     assert pa.lib.attn_bwd_workspace_bytes(1, 2, 2, 4, 4, 64, 0) == pa.ATTN_EHIP
 
 
+def test_more_than_a_launch_holds_is_refused_on_host():
+    # 2^24 tiles of 16 tokens; products that pass 64 bits
+    big = 1 << 28
+    assert rope(B=1, S=big) == pa.ATTN_EUNSUPPORTED
+    assert rope_bwd(B=big, S=1) == pa.ATTN_EUNSUPPORTED
+    assert rope(B=0x7FFFFFFF, S=0x7FFFFFFF) == pa.ATTN_EUNSUPPORTED
+    assert pa.lib.attn_qk_norm_rope_bwd_workspace_bytes(1, big, 1, 1, 64) == pa.ATTN_EUNSUPPORTED
+    n = 0x7FFFFFFF
+    assert bwd(B=n, Hq=n, Hkv=n, Sq=1 << 23) == pa.ATTN_EUNSUPPORTED
+    assert pa.lib.attn_bwd_workspace_bytes(n, n, n, 4, 4, 64, 0) == pa.ATTN_EUNSUPPORTED
+
+
 # ------------------------------------------------------------ the references --
 @pytest.mark.parametrize("causal", [False, True])
 def test_attention_reference_is_the_gradient(causal):

@@ -14,10 +14,10 @@ device.
 """
 from __future__ import annotations
 
-import array
 import ctypes
 import math
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libattn.so")
@@ -140,6 +140,10 @@ def _load() -> ctypes.CDLL:
         [cf, ci, vp, ctypes.c_size_t]
     lib.attn_qk_norm_rope_bwd_workspace_bytes.argtypes = [ci] * 5
     lib.attn_qk_norm_rope_bwd_workspace_bytes.restype = ctypes.c_longlong
+    for fn in (lib.attn__bwd_packed, lib.attn__qk_norm_rope_packed,
+               lib.attn__qk_norm_rope_bwd_packed):
+        fn.argtypes = [ctypes.c_char_p]
+        fn.restype = ci
     for fn in (lib.attn_bwd, lib.attn_qk_norm_rope, lib.attn_qk_norm_rope_bwd,
                lib.attn_fwd, lib.attn_decode, lib.attn_fwd_ex, lib.attn_decode_ex,
                lib.attn_decode_noalloc,
@@ -307,31 +311,37 @@ def gemm(a, b, c=None, b_nk: bool = False, out_dtype=None):
     return c
 
 
+# The operands of the calls below, packed as csrc/api.hip's PackedBwd, PackedRope and
+# PackedRopeBwd: ctypes converts an argument in 0.08 us, and these calls have up to 30 numbers
+# (qk_norm_rope of one token 15.6 us with them as arguments, 12.9 packed).
+_BWD_CALL = struct.Struct("13Q8if")
+_ROPE_CALL = struct.Struct("24q4QqQ7if")
+_ROPE_BWD_CALL = struct.Struct("32q4Qq5Q7if")
+
+
 def _require_on(t, dtype, shape, name, dev) -> None:
     """_require, on device dev (one expression for a good tensor)."""
-    import torch
-    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == dev and \
-            t.shape == shape and t.is_contiguous():
+    if getattr(t, "dtype", None) is dtype and t.get_device() == dev and t.shape == shape and \
+            t.is_contiguous():
         return
     _require(t, dtype, shape, name)
     raise ValueError(f"{name} is on another device than the first operand")
 
 
-def _call_on(dev, fn, *args) -> None:
-    """A C call on device dev and its current stream."""
+def _call_on(dev, fn, packed) -> None:
+    """A C call on device dev."""
     import torch
     if torch._C._cuda_getDevice() != dev:
         with torch.cuda.device(dev):
-            return _call_on(dev, fn, *args)
-    lib.attn_set_stream(_raw_stream(dev))
-    _check(fn(*args))
+            return _call_on(dev, fn, packed)
+    _check(fn(packed))
 
 
 def _workspace(workspace, dev):
     """Address and bytes of a caller's workspace (None: the library's)."""
     import torch
     if workspace is None:
-        return None, 0
+        return 0, 0
     if not isinstance(workspace, torch.Tensor) or not workspace.is_cuda or \
             not workspace.is_contiguous():
         raise TypeError("workspace must be a contiguous tensor on a HIP device")
@@ -385,10 +395,11 @@ def attn_bwd(do, q, k, v, o, lse, scale: float | None = None, causal: bool = Fal
     if scale is None:
         scale = 1.0 / math.sqrt(d)
     flags = (ATTN_OUT_BF16 if out_dtype is bf16 else 0) | (ATTN_O_BF16 if o_bf16 else 0)
-    _call_on(dev, lib.attn_bwd, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
-             lse.data_ptr(), do.data_ptr(), None if dlse is None else dlse.data_ptr(),
-             dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), B, Hq, Hkv, Sq, Skv, d, scale,
-             1 if causal else 0, flags, *_workspace(workspace, dev))
+    _call_on(dev, lib.attn__bwd_packed, _BWD_CALL.pack(
+        q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), do.data_ptr(),
+        0 if dlse is None else dlse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+        *_workspace(workspace, dev), _raw_stream(dev), B, Hq, Hkv, Sq, Skv, d,
+        1 if causal else 0, flags, scale))
     return dq, dk, dv
 
 
@@ -404,6 +415,10 @@ def bwd_workspace_bytes(B: int, Hq: int, Hkv: int, Sq: int, Skv: int, d: int,
 def _rows(t, dtype, shape, name, dev):
     """A 4-dimensional tensor whose rows (last dimension) are contiguous, checked; its
     strides."""
+    if getattr(t, "dtype", None) is dtype and t.get_device() == dev and t.shape == shape:
+        strides = t.stride()
+        if strides[3] == 1:
+            return strides
     import torch
     if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() < 0:
         raise TypeError(f"{name} must be a {dtype} tensor on a HIP device")
@@ -411,10 +426,7 @@ def _rows(t, dtype, shape, name, dev):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if t.get_device() != dev:
         raise ValueError(f"{name} is on another device than the first operand")
-    strides = t.stride()
-    if strides[3] != 1:
-        raise ValueError(f"{name} must be contiguous in its last dimension")
-    return strides
+    raise ValueError(f"{name} must be contiguous in its last dimension")
 
 
 def _head_major_out(out, B, S, H, d, name, like):
@@ -439,17 +451,7 @@ def _head_major(t, dtype, shape, name, dev):
     return t.data_ptr(), b, s, h
 
 
-_NO_HEADS = (0, 0, 0, 0)
-
-
-def _heads_array(*fields):
-    """An array of attn_heads from their fields (four 64-bit numbers each), to be kept
-    until the call, and the address of each (None for _NO_HEADS)."""
-    heads = array.array("q")
-    for f in fields:
-        heads.extend(f)
-    base = heads.buffer_info()[0]
-    return heads, [base + 32 * i if f is not _NO_HEADS else None for i, f in enumerate(fields)]
+_NO_HEADS = (0, 0, 0, 0)  # no tensor
 
 
 def _rope_common(q, k, q_weight, k_weight, inv_freq, positions, interleaved):
@@ -470,7 +472,7 @@ def _rope_common(q, k, q_weight, k_weight, inv_freq, positions, interleaved):
     half = inv_freq.shape[0]
     _require_on(inv_freq, torch.float32, (half,), "inv_freq", dev)
     flags = (ATTN_ROPE_INTERLEAVED if interleaved else 0) | (ATTN_WEIGHT_F32 if w_f32 else 0)
-    pos_ptr, pos_stride = None, 0
+    pos_ptr = pos_stride = 0
     if positions is not None:
         if not isinstance(positions, torch.Tensor) or not positions.is_cuda or \
                 positions.dtype not in (torch.int32, torch.int64):
@@ -518,8 +520,9 @@ def qk_norm_rope(q, k, v, q_weight, k_weight, inv_freq, positions=None, eps: flo
         v_out, v_to = _head_major_out(v_out, B, S, Hkv, d, "v_out", q)
     elif v_out is not None:
         raise ValueError("v_out without v")
-    heads, at = _heads_array(q_in, k_in, v_in, q_to, k_to, v_to)
-    _call_on(dev, lib.attn_qk_norm_rope, *at, *small, B, S, Hq, Hkv, d, rot, eps, flags)
+    _call_on(dev, lib.attn__qk_norm_rope_packed, _ROPE_CALL.pack(
+        *q_in, *k_in, *v_in, *q_to, *k_to, *v_to, *small, _raw_stream(dev), B, S, Hq, Hkv, d,
+        rot, flags, eps))
     return q_out, k_out, v_out
 
 
@@ -562,13 +565,14 @@ def qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, inv_freq, positions=N
         dv_to = _token_major(dv_out, bf16, k_shape, "dv_out", dev)
     elif dv_out is not None:
         raise ValueError("dv_out without dv")
-    dqw = dkw = dqw_ptr = dkw_ptr = None
+    dqw = dkw = None
+    dqw_ptr = dkw_ptr = 0
     if weight_grads:
         dqw, dkw = torch.empty((2, d), dtype=f32, device=q.device).unbind()
         dqw_ptr, dkw_ptr = dqw.data_ptr(), dkw.data_ptr()
-    heads, at = _heads_array(dq_in, dk_in, dv_in, q_in, k_in, dq_to, dk_to, dv_to)
-    _call_on(dev, lib.attn_qk_norm_rope_bwd, *at, *small, dqw_ptr, dkw_ptr, B, S, Hq, Hkv, d, rot,
-             eps, flags, *_workspace(workspace, dev))
+    _call_on(dev, lib.attn__qk_norm_rope_bwd_packed, _ROPE_BWD_CALL.pack(
+        *dq_in, *dk_in, *dv_in, *q_in, *k_in, *dq_to, *dk_to, *dv_to, *small, dqw_ptr, dkw_ptr,
+        *_workspace(workspace, dev), _raw_stream(dev), B, S, Hq, Hkv, d, rot, flags, eps))
     return dq_out, dk_out, dv_out, dqw, dkw
 
 

@@ -1296,4 +1296,69 @@ int attn_qk_norm_rope_bwd(const attn_heads* dq, const attn_heads* dk, const attn
     });
 }
 
+// The calls as the Python binding makes them: one pointer to all operands, and the stream
+// (the thread's from then on), since a foreign-function call costs its caller time for
+// every argument.
+struct PackedBwd {
+    const void *q, *k, *v, *o;
+    const float* lse;
+    const void* d_o;
+    const float* dlse;
+    void *dq, *dk, *dv, *workspace;
+    size_t workspace_bytes;
+    hipStream_t stream;
+    int B, Hq, Hkv, Sq, Skv, d, causal, flags;
+    float scale;
+};
+static_assert(offsetof(PackedBwd, scale) == 13 * 8 + 8 * 4, "13Q8if");
+int attn__bwd_packed(const PackedBwd* c) {
+    t_stream = c->stream;
+    return attn_bwd(c->q, c->k, c->v, c->o, c->lse, c->d_o, c->dlse, c->dq, c->dk, c->dv, c->B,
+                    c->Hq, c->Hkv, c->Sq, c->Skv, c->d, c->scale, c->causal, c->flags,
+                    c->workspace, c->workspace_bytes);
+}
+
+struct PackedRope {
+    attn_heads q, k, v, q_out, k_out, v_out;  // v, v_out: none where ptr is null
+    const void *q_weight, *k_weight;
+    const float* inv_freq;
+    const void* positions;
+    long long positions_batch_stride;
+    hipStream_t stream;
+    int B, S, Hq, Hkv, d, rot, flags;
+    float eps;
+};
+static_assert(offsetof(PackedRope, eps) == 30 * 8 + 7 * 4, "24q4QqQ7if");
+static const attn_heads* given(const attn_heads& h) { return h.ptr ? &h : nullptr; }
+int attn__qk_norm_rope_packed(const PackedRope* c) {
+    t_stream = c->stream;
+    return attn_qk_norm_rope(&c->q, &c->k, given(c->v), &c->q_out, &c->k_out, given(c->v_out),
+                             c->q_weight, c->k_weight, c->inv_freq, c->positions,
+                             c->positions_batch_stride, c->B, c->S, c->Hq, c->Hkv, c->d, c->rot,
+                             c->eps, c->flags);
+}
+
+struct PackedRopeBwd {
+    attn_heads dq, dk, dv, q, k, dq_out, dk_out, dv_out;
+    const void *q_weight, *k_weight;
+    const float* inv_freq;
+    const void* positions;
+    long long positions_batch_stride;
+    float *dq_weight, *dk_weight;
+    void* workspace;
+    size_t workspace_bytes;
+    hipStream_t stream;
+    int B, S, Hq, Hkv, d, rot, flags;
+    float eps;
+};
+static_assert(offsetof(PackedRopeBwd, eps) == 42 * 8 + 7 * 4, "32q4Qq5Q7if");
+int attn__qk_norm_rope_bwd_packed(const PackedRopeBwd* c) {
+    t_stream = c->stream;
+    return attn_qk_norm_rope_bwd(&c->dq, &c->dk, given(c->dv), &c->q, &c->k, &c->dq_out,
+                                 &c->dk_out, given(c->dv_out), c->q_weight, c->k_weight,
+                                 c->inv_freq, c->positions, c->positions_batch_stride,
+                                 c->dq_weight, c->dk_weight, c->B, c->S, c->Hq, c->Hkv, c->d,
+                                 c->rot, c->eps, c->flags, c->workspace, c->workspace_bytes);
+}
+
 }  // extern "C"

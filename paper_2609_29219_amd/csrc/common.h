@@ -436,7 +436,8 @@ struct RopeArgs {
     int interleaved, weight_f32, positions_i64;
     int tile_log2;
     float eps;
-    float* ws;              // backward: weight gradients, [workgroup][2][d], or null
+    float* ws;              // backward: weight gradients, [2][d/16][workgroup][16], or
+                            // null
 };
 struct RopeLaunch {
     int tile_log2 = 0, grid_x = 0, grid_y = 1;

@@ -152,6 +152,31 @@ def test_more_than_a_launch_holds_is_refused_on_host():
     assert pa.lib.attn_bwd_workspace_bytes(n, n, n, 4, 4, 64, 0) == pa.ATTN_EUNSUPPORTED
 
 
+def test_packed_calls_reach_the_same_checks():
+    # (the last number of each call, and one before it)
+    def packed_bwd(d=64, scale=0.125):
+        ptrs = [A] * 6 + [0, A + MB, A + 2 * MB, A + 3 * MB, 0, 0, 0]
+        return pa.lib.attn__bwd_packed(pa._BWD_CALL.pack(*ptrs, 1, 2, 1, 4, 4, d, 0, 0, scale))
+
+    h = (A, 512, 128, 64)
+
+    def packed_rope(v=h, rot=64, eps=1e-6):
+        return pa.lib.attn__qk_norm_rope_packed(pa._ROPE_CALL.pack(
+            *h, *h, *v, *h, *h, *h, A, A, A, 0, 0, 0, 2, 4, 2, 2, 64, rot, 0, eps))
+
+    def packed_rope_bwd(v=h, rot=64, eps=1e-6):
+        return pa.lib.attn__qk_norm_rope_bwd_packed(pa._ROPE_BWD_CALL.pack(
+            *h, *h, *v, *h, *h, *h, *h, *h, A, A, A, 0, 0, A, A, 0, 0, 0, 2, 4, 2, 2, 64, rot, 0,
+            eps))
+
+    assert packed_bwd(d=96) == pa.ATTN_EUNSUPPORTED and "head dim 96" in pa.last_error()
+    assert packed_bwd(scale=math.inf) == pa.ATTN_EINVAL and "scale" in pa.last_error()
+    for call in (packed_rope, packed_rope_bwd):
+        assert call(rot=24) == pa.ATTN_EUNSUPPORTED and "rot (24)" in pa.last_error()
+        assert call(eps=-1.0) == pa.ATTN_EINVAL and "eps" in pa.last_error()
+        assert call(v=(0, 0, 0, 0)) == pa.ATTN_EINVAL and "go together" in pa.last_error()
+
+
 # ------------------------------------------------------------ the references --
 @pytest.mark.parametrize("causal", [False, True])
 def test_attention_reference_is_the_gradient(causal):

@@ -1033,6 +1033,7 @@ long long attn_bwd_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Skv, int 
         if (rc) return rc;
         BwdPlan plan;
         size_t bytes = 0;
+        bwd_fold(&Hq, Hkv, &Sq, d, &causal);
         rc = bwd_plan_of(st, B, Hq, Hkv, Sq, Skv, d, causal, &plan, &bytes);
         return rc ? rc : (long long)bytes;
     });
@@ -1074,6 +1075,7 @@ int attn_bwd(const void* q, const void* k, const void* v, const void* o, const f
         if (rc) return rc;
         BwdPlan plan;
         size_t need = 0;
+        bwd_fold(&Hq, Hkv, &Sq, d, &causal);
         rc = bwd_plan_of(st, B, Hq, Hkv, Sq, Skv, d, causal, &plan, &need);
         if (rc) return rc;
         void* ws = nullptr;

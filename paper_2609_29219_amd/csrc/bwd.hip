@@ -36,6 +36,7 @@
 //
 // Roundings: P and dS to bf16, as operands; everything else is fp32 until the result.
 #include <hip/hip_runtime.h>
+#include <limits.h>
 #include <stdint.h>
 
 #include <type_traits>
@@ -231,9 +232,10 @@ constexpr int stage_bytes() { return 32 * (D * 2 + 16); }
 template <int D>
 __device__ __forceinline__ void store_rows(const f32x16 (&x)[D / 32], char* stage, void* out,
                                            long long row0, long long n_rows, int bf16,
-                                           float factor, int lane) {
+                                           float factor) {
     constexpr int STRIDE = D * 2 + 16, L = D * 2 / 16, RPI = 64 / L;  // lanes to a row, rows at once
-    const int l32 = lane & 31, hh = lane >> 5;
+    // (counted anew: taken from the thread's number it would be kept over the loops)
+    const int lane = __lane_id(), l32 = lane & 31, hh = lane >> 5;
     auto flush = [&](char* base, long long row_bytes) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 32 / RPI; ++i) {
@@ -290,18 +292,17 @@ struct BwdLds {
 // A wave's own rows of a head's slab as operand registers: op[b][ks] holds row l%32 of
 // the wave's b-th block, values 16*ks + 8*(l/32) ..+7.  Loaded straight into registers, an
 // instruction touches 32 rows, 32 bytes each, and the operands of a workgroup took 5.8 us;
-// through LDS in whole rows they take 3.  own_load issues the loads, own_read reads what
-// has landed.
+// through LDS in whole rows they take 3.  own_load issues the loads of a block, own_read
+// reads the blocks that have landed.
 template <int D>
 __device__ __forceinline__ void own_load(dma_rsrc_t rsrc, uint32_t lds, int row0, int n_rows,
                                          int lane) {
     constexpr int ROWS = 512 / D;
 #pragma unroll
-    for (int p = 0; p < 32 * BwdShape<D>::BLOCKS / ROWS; ++p) {
+    for (int p = 0; p < 32 / ROWS; ++p) {
         const int r = p * ROWS + lane / (D / 8);
-        const int c = (lane % (D / 8)) ^ tile_swizzle<D>(r & 31);
-        const int row = row0 + r / 32 * (32 * BwdShape<D>::WAVES) + r % 32;
-        lds_dma16(rsrc, lds + p * 1024, min(row, n_rows - 1) * (D * 2) + c * 16, 0);
+        const int c = (lane % (D / 8)) ^ tile_swizzle<D>(r);
+        lds_dma16(rsrc, lds + p * 1024, min(row0 + r, n_rows - 1) * (D * 2) + c * 16, 0);
     }
 }
 template <int D>
@@ -560,8 +561,14 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
         const uint32_t own = rows0 + L::OWN + wave * L::OWN_WAVE;
         const uint32_t slab = (uint32_t)a.Skv * D * 2;
         const long long at = (long long)bh * a.Skv * D;
-        own_load<D>(make_dma_rsrc(a.k + at, slab), own, wk0, a.Skv, lane);
-        own_load<D>(make_dma_rsrc(a.v + at, slab), own + L::OWN_WAVE / 2, wk0, a.Skv, lane);
+        const dma_rsrc_t k_rsrc = make_dma_rsrc(a.k + at, slab);
+        const dma_rsrc_t v_rsrc = make_dma_rsrc(a.v + at, slab);
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            const int row = wk0 + kb * KSTEP;
+            own_load<D>(k_rsrc, own + kb * L::TILE, row, a.Skv, lane);
+            own_load<D>(v_rsrc, own + L::OWN_WAVE / 2 + kb * L::TILE, row, a.Skv, lane);
+        }
         asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
         own_read<D>(kf, read, own);
         own_read<D>(vf, read, own + L::OWN_WAVE / 2);
@@ -591,13 +598,15 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
         });
         ++step;
     };
+    // every wave's second block hidden (four of a diagonal's eight tiles) or past the keys
+    const int second = k0 + KSTEP < a.Skv ? k0 + KSTEP : INT_MAX;
+    auto half = [&]() __attribute__((always_inline)) {
+        return KB == 2 && (CAUSAL ? qt * 32 + 31 + diag < second : second == INT_MAX);
+    };
     while (step < end) {
-        // every wave's second block hidden: four of a diagonal's eight tiles
-        if constexpr (CAUSAL && KB == 2)
-            while (step < end && qt * 32 + 31 + diag < k0 + KSTEP)
-                tile(std::integral_constant<int, 1>{});
-        while (step < end && !(CAUSAL && KB == 2 && qt * 32 + 31 + diag < k0 + KSTEP))
-            tile(std::integral_constant<int, KB>{});
+        if constexpr (KB == 2)
+            while (step < end && half()) tile(std::integral_constant<int, 1>{});
+        while (step < end && !half()) tile(std::integral_constant<int, KB>{});
     }
 
     __syncthreads();  // the stages overlay the tiles
@@ -610,36 +619,43 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
     const int bf16 = part ? 0 : a.out_bf16;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-        store_rows<D>(dk[kb], stage, dk_out, row0 + kb * KSTEP, last, bf16, a.scale, lane);
-        store_rows<D>(dv[kb], stage, dv_out, row0 + kb * KSTEP, last, bf16, 1.f, lane);
+        store_rows<D>(dk[kb], stage, dk_out, row0 + kb * KSTEP, last, bf16, a.scale);
+        store_rows<D>(dv[kb], stage, dv_out, row0 + kb * KSTEP, last, bf16, 1.f);
     }
 }
 
 // ---------------------------------------------------------------------- dQ --
-// One block of queries (query head bh, over the batch), part `split` of `splits` of its sum.
+// One block of queries (of the group of kv head kvh, over the batch), part `split` of
+// `splits` of its sum.
 template <int D, bool CAUSAL>
-__device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, int block,
+__device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int kvh, int block,
                                          int split, int splits) {
     constexpr int QB = BwdShape<D>::BLOCKS, KD = D / 16, CB = D / 32;
     typedef BwdLds<D> L;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    // the wave's blocks of 32 queries are QSTEP apart, as the keys in dkdv_block
-    constexpr int QSTEP = 32 * BwdShape<D>::WAVES;
-    const int q0 = block * BwdShape<D>::ROWS;
-    const int wq0 = q0 + wave * 32;  // first query of the wave's first block
-
-    const int n_qt = (a.Sq + 31) / 32;
+    // The wave's tiles of 32 queries are WAVES apart in the block, as the keys in
+    // dkdv_block.  (Behind the last tile: that one again, and nothing stored.)
+    constexpr int WAVES = BwdShape<D>::WAVES;
+    const int n_qt = (a.Sq + 31) / 32, tiles = n_qt * a.group;
+    const int tile0 = block * (BwdShape<D>::ROWS / 32);
+    int wq0[QB];         // first query
+    long long head[QB];  // of which head, over the batch
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        const int t = min(tile0 + qb * WAVES + wave, tiles - 1);
+        const int qt = __builtin_amdgcn_readfirstlane(t / a.group);
+        wq0[qb] = qt * 32;
+        head[qb] = (long long)kvh * a.group + (t - qt * a.group);
+    }
     bf16x8 qf[QB][KD], gf[QB][KD];  // B operands: lane l holds query l%32
     float nl[QB];
     f32x16 nd[QB];  // -delta, from which the products of dP start
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-        const int q = wq0 + qb * QSTEP + l32;
-        // (queries past Sq: the last tile's padding, or the last row of all)
-        const long long tile = (long long)bh * n_qt + min(q, n_qt * 32 - 1) / 32;
-        nl[qb] = a.rows[tile * 64 + l32];
-        const float x = a.rows[tile * 64 + 32 + l32];
+        const float* rows = a.rows + (head[qb] * n_qt + wq0[qb] / 32) * 64;
+        nl[qb] = rows[l32];
+        const float x = rows[32 + l32];
 #pragma unroll
         for (int r = 0; r < 16; ++r) nd[qb][r] = x;
     }
@@ -656,9 +672,8 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
     read.init(lane);
     const uint32_t lds0 = lds_address(lds) + L::SLOTS;
     const uint32_t slab = (uint32_t)a.Skv * D * 2;
-    const long long head = bh / a.group;
-    const dma_rsrc_t k_rsrc = make_dma_rsrc(a.k + head * a.Skv * D, slab);
-    const dma_rsrc_t v_rsrc = make_dma_rsrc(a.v + head * a.Skv * D, slab);
+    const dma_rsrc_t k_rsrc = make_dma_rsrc(a.k + (long long)kvh * a.Skv * D, slab);
+    const dma_rsrc_t v_rsrc = make_dma_rsrc(a.v + (long long)kvh * a.Skv * D, slab);
     auto issue = [&](int step, int slot) __attribute__((always_inline)) {
         const uint32_t dst = lds0 + slot * L::SLOT;
         load.issue(k_rsrc, v_rsrc, dst, step * 32, a.Skv, wave);
@@ -712,7 +727,7 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
 #pragma unroll
         for (int qb = decltype(qf_tag)::value; qb < QB; ++qb) {
             const int last =
-                CAUSAL ? min(a.Skv - 1, wq0 + qb * QSTEP + l32 + diag) : a.Skv - 1;
+                CAUSAL ? min(a.Skv - 1, wq0[qb] + l32 + diag) : a.Skv - 1;
             const int lim = last - k0 - 4 * hh;
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[qb][r] = acc_row(r, 0) <= lim ? s[qb][r] : a.hidden;
@@ -729,7 +744,6 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
             }
         }
     };
-    constexpr int N = QB * KD;  // products, and the gaps behind them, of one kind
     constexpr int TAIL = OPS - Ring::ahead(0) + 1;  // the last slots, behind the barrier
     auto body = [&](int k0, auto qf_tag) __attribute__((always_inline)) {
         constexpr int QF = decltype(qf_tag)::value;
@@ -754,7 +768,7 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
             if constexpr (ph == 0 && j == 0) settle<0, QB>(dp);
             if constexpr (ph == 1 && j == 0) {
                 settle<QF, QB>(s);
-                if (k0 + 32 > a.Skv || (CAUSAL && k0 + 31 > wq0 + QF * QSTEP + diag))
+                if (k0 + 32 > a.Skv || (CAUSAL && k0 + 31 > wq0[QF] + diag))
                     hide(k0, qf_tag);
             }
             slot_end();
@@ -779,9 +793,13 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
     {
         const uint32_t own = lds_address(lds) + L::OWN + wave * L::OWN_WAVE;
         const uint32_t slab = (uint32_t)a.Sq * D * 2;
-        const long long at = (long long)bh * a.Sq * D;
-        own_load<D>(make_dma_rsrc(a.q + at, slab), own, wq0, a.Sq, lane);
-        own_load<D>(make_dma_rsrc(a.d_o + at, slab), own + L::OWN_WAVE / 2, wq0, a.Sq, lane);
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            const long long at = head[qb] * a.Sq * D;
+            own_load<D>(make_dma_rsrc(a.q + at, slab), own + qb * L::TILE, wq0[qb], a.Sq, lane);
+            own_load<D>(make_dma_rsrc(a.d_o + at, slab), own + L::OWN_WAVE / 2 + qb * L::TILE,
+                        wq0[qb], a.Sq, lane);
+        }
         asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
         own_read<D>(qf, read, own);
         own_read<D>(gf, read, own + L::OWN_WAVE / 2);
@@ -818,7 +836,10 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
         ++step;
     };
     // every wave's first block hidden: four of a diagonal's eight tiles, the last ones
-    const int half = CAUSAL && QB == 2 ? min(end, (q0 + QSTEP - 1 + diag) / 32 + 1) : end;
+    const int half =
+        CAUSAL && QB == 2
+            ? min(end, (min(tile0 + WAVES, tiles) - 1) / a.group + (31 + diag) / 32 + 1)
+            : end;
     while (step < half) tile(std::integral_constant<int, 0>{});
     if constexpr (CAUSAL && QB == 2)
         while (step < end) tile(std::integral_constant<int, 1>{});
@@ -827,18 +848,19 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int bh, in
 
     __syncthreads();  // the stages overlay the tiles
     const bool part = splits > 1;
-    const long long rows = a.q_heads * a.Sq, row0 = (long long)bh * a.Sq + wq0;
-    void* out = part ? a.part_q + split * rows * D : a.dq;
+    void* out = part ? a.part_q + split * a.q_heads * a.Sq * D : a.dq;
     char* stage = lds + wave * stage_bytes<D>();
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb)
-        store_rows<D>(dq[qb], stage, out, row0 + qb * QSTEP, (long long)(bh + 1) * a.Sq,
-                      part ? 0 : a.out_bf16, a.scale, lane);
+    for (int qb = 0; qb < QB; ++qb) {
+        const long long last = tile0 + qb * WAVES + wave < tiles ? (head[qb] + 1) * a.Sq : 0;
+        store_rows<D>(dq[qb], stage, out, head[qb] * a.Sq + wq0[qb], last,
+                      part ? 0 : a.out_bf16, a.scale);
+    }
 }
 
 // ------------------------------------------------------------------ kernel --
-// Workgroups: for every key/value head, the parts of its blocks of keys and of the blocks
-// of queries of its group, in one launch, so that the one kind fills the other's gaps.
+// Workgroups: for every key/value head, the parts of its blocks of keys and of its group's
+// blocks of queries, in one launch, so that the one kind fills the other's gaps.
 // The hardware deals workgroups round-robin to the XCDs; each XCD gets whole heads, whose
 // tiles stay in its L2, where they can be dealt evenly.
 //
@@ -863,7 +885,7 @@ __global__ __launch_bounds__(
     if (w.kv)
         dkdv_block<D, CAUSAL>(a, lds, head, w.block, w.split, w.splits);
     else
-        dq_block<D, CAUSAL>(a, lds, head * a.group + w.g, w.block, w.split, w.splits);
+        dq_block<D, CAUSAL>(a, lds, head, w.block, w.split, w.splits);
 }
 
 // Adds up the parts of the blocks that have several, in their order, four values to a
@@ -876,7 +898,9 @@ __global__ __launch_bounds__(256) void bwd_sum_kernel(const BwdArgs a) {
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
     const long long row = i / (D / 4);
     if (row >= rows) return;
-    const int n = a.units.parts(!q, (int)(row % S) / BwdShape<D>::ROWS);
+    const int at = (int)(row % S), g = (int)(row / S % a.group);  // (g: of a query)
+    const int n = a.units.parts(!q, q ? (at / 32 * a.group + g) / (BwdShape<D>::ROWS / 32)
+                                      : at / BwdShape<D>::ROWS);
     if (n == 1) return;
     const float* part = (q ? a.part_q : blockIdx.z ? a.part_v : a.part_k) + i * 4;
     void* out = q ? a.dq : blockIdx.z ? a.dv : a.dk;

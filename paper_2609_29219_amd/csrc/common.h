@@ -287,7 +287,10 @@ constexpr long long kMaxWorkgroups = (1LL << 24) - 1;
 
 // ------------------------------------------------------- attention backward --
 // A workgroup keeps a block of keys (for dK, dV) or of queries (for dQ) and walks the tiles
-// of 32 queries (of every head of the group) or keys that it meets: its steps.
+// of 32 queries (of every head of the group) or keys that it meets: its steps.  A block of
+// queries is a number of tiles of 32, in the order of their positions, and of the heads of
+// the group where those are the same: short sequences of several heads fill one block, and
+// long ones meet almost the same keys.
 #ifdef __HIP__
 #define ATTN_HD __host__ __device__
 #else
@@ -302,21 +305,33 @@ struct BwdSize {
         const int n_qt = (Sq + 31) / 32, reach = block * rows - (Skv - Sq);
         return (n_qt - (causal && reach > 0 ? reach / 32 : 0)) * group;
     }
+    ATTN_HD int q_tiles() const { return (Sq + 31) / 32 * group; }
+    ATTN_HD int q_blocks() const { return (q_tiles() + rows / 32 - 1) / (rows / 32); }
     ATTN_HD int q_steps(int block) const {
-        const int q1 = (block + 1) * rows < Sq ? (block + 1) * rows : Sq;
-        return ((causal ? q1 + Skv - Sq : Skv) + 31) / 32;
+        const int tiles = q_tiles(), next = (block + 1) * (rows / 32);
+        const int q1 = ((next < tiles ? next : tiles) - 1) / group * 32 + 32;
+        return ((causal ? (q1 < Sq ? q1 : Sq) + Skv - Sq : Skv) + 31) / 32;
     }
 };
+// Without a mask the heads of a group are one head of all their rows, which lie one behind
+// another: they fill tiles together.  (A single query meets every key, mask or not.)
+inline void bwd_fold(int* Hq, int Hkv, int* Sq, int d, int* causal) {
+    if (*Sq == 1) *causal = 0;
+    const long long rows = (long long)*Sq * (*Hq / Hkv);
+    if (*causal || rows * d * 2 > 0x7fffffffLL) return;
+    *Sq = (int)rows;
+    *Hq = Hkv;
+}
 // Parts of a block's sum, of at most chunk steps each (0: one part).
 ATTN_HD inline int bwd_parts(int steps, int chunk) {
     return chunk ? (steps + chunk - 1) / chunk : 1;
 }
 // Causal blocks differ in length: the longest parts start first.  Up to kBwdOrder units
 // are named in that order (more need no exact one): of a key/value head's, kind (1: keys),
-// head of the group, block, part.
+// block, part.
 constexpr int kBwdOrder = 512;
 struct BwdUnit {
-    uint16_t kv : 1, g : 15, block, split;
+    uint16_t kv, block, split;
 };
 struct BwdOrder {
     BwdUnit unit[kBwdOrder];
@@ -324,7 +339,7 @@ struct BwdOrder {
 struct BwdPlan {
     BwdOrder order;
     int ordered = 0;
-    int kv_blocks = 0, q_blocks = 0;  // of a head
+    int kv_blocks = 0, q_blocks = 0;  // of a key/value head
     int kv_units = 0, q_units = 0;    // their parts
     int kv_chunk = 0, q_chunk = 0;    // steps of a part at most; 0: no block is split
     int kv_parts = 0, q_parts = 0;    // most parts of a block (0: no block is split)
@@ -332,9 +347,9 @@ struct BwdPlan {
     double modeled_us = 0.0;
 };
 // What a workgroup does: the block of keys or queries of a key/value head (of the given
-// number of heads, and of head g of its group), part `split` of `splits` of its sum.
+// number of heads), part `split` of `splits` of its sum.
 struct BwdWork {
-    int kv, head, g, block, split, splits;
+    int kv, head, block, split, splits;
 };
 struct BwdUnits {
     BwdSize size;
@@ -350,12 +365,11 @@ struct BwdUnits {
 // without one head by head.
 ATTN_HD inline BwdWork bwd_work(const BwdUnits& a, const BwdUnit* order, int heads, int i) {
     BwdWork w;
-    w.g = w.split = 0;
+    w.split = 0;
     if (a.ordered) {
         const BwdUnit u = order[i / heads];
         w.head = i % heads;
         w.kv = u.kv;
-        w.g = u.g;
         w.block = u.block;
         w.split = u.split;
         w.splits = a.parts(w.kv, w.block);
@@ -363,7 +377,7 @@ ATTN_HD inline BwdWork bwd_work(const BwdUnits& a, const BwdUnit* order, int hea
     }
     w.kv = i < heads * a.kv_units;
     const int x = w.kv ? i : i - heads * a.kv_units;
-    const int n = w.kv ? a.kv_units : a.size.group * a.q_units;  // of a head
+    const int n = w.kv ? a.kv_units : a.q_units;  // of a head
     int unit;
     if (a.size.causal) {
         unit = x / heads;
@@ -371,10 +385,6 @@ ATTN_HD inline BwdWork bwd_work(const BwdUnits& a, const BwdUnit* order, int hea
     } else {
         w.head = x / n;
         unit = x - w.head * n;
-    }
-    if (!w.kv) {
-        w.g = unit % a.size.group;
-        unit /= a.size.group;
     }
     const int blocks = w.kv ? a.kv_blocks : a.q_blocks;
     w.block = unit;

@@ -1066,23 +1066,27 @@ struct BwdCosts {
     double kv_step, q_step, workgroup;
 };
 
+// A step of a block of keys.  (With 64 rows to a wave, one that has no more than half its
+// keys works on those alone.)
+double kv_step(const BwdCosts& c, const BwdSize& size, int block) {
+    return c.kv_step * (size.rows == 256 && size.Skv - block * size.rows <= 128 ? 0.6 : 1.0);
+}
+
 // Names the plan's units in the order of their lengths, longest first, if they are few.
 void bwd_order(BwdPlan* p, const BwdCosts& c, const BwdSize& size) {
-    const int group = size.group;
-    const long long units = p->kv_units + (long long)group * p->q_units;
-    p->ordered = size.causal && units <= kBwdOrder && p->kv_blocks < 65536 && group < 32768;
+    const long long units = (long long)p->kv_units + p->q_units;
+    p->ordered = size.causal && units <= kBwdOrder;
     if (!p->ordered) return;
     std::vector<std::pair<double, BwdUnit>> all;
     for (int b = 0; b < p->kv_blocks; ++b) {
         const int steps = size.kv_steps(b), n = bwd_parts(steps, p->kv_chunk);
         for (int i = 0; i < n; ++i)
-            all.push_back({c.kv_step * steps / n, {1, 0, (uint16_t)b, (uint16_t)i}});
+            all.push_back({kv_step(c, size, b) * steps / n, {1, (uint16_t)b, (uint16_t)i}});
     }
     for (int b = p->q_blocks - 1; b >= 0; --b) {
         const int steps = size.q_steps(b), n = bwd_parts(steps, p->q_chunk);
         for (int i = 0; i < n; ++i)
-            for (int g = 0; g < group; ++g)
-                all.push_back({c.q_step * steps / n, {0, (uint16_t)g, (uint16_t)b, (uint16_t)i}});
+            all.push_back({c.q_step * steps / n, {0, (uint16_t)b, (uint16_t)i}});
     }
     std::stable_sort(all.begin(), all.end(),
                      [](const auto& x, const auto& y) { return x.first > y.first; });
@@ -1095,7 +1099,7 @@ double bwd_makespan(const BwdPlan& p, const BwdCosts& c, const BwdSize& size, in
                     int heads) {
     auto kv_time = [&](int b) {
         const int steps = size.kv_steps(b);
-        return c.workgroup + c.kv_step * steps / bwd_parts(steps, p.kv_chunk);
+        return c.workgroup + kv_step(c, size, b) * steps / bwd_parts(steps, p.kv_chunk);
     };
     auto q_time = [&](int b) {
         const int steps = size.q_steps(b);
@@ -1103,7 +1107,7 @@ double bwd_makespan(const BwdPlan& p, const BwdCosts& c, const BwdSize& size, in
     };
     std::vector<double> times;  // of a head's units, in order
     if (p.ordered) {
-        for (int u = 0; u < p.kv_units + size.group * p.q_units; ++u)
+        for (int u = 0; u < p.kv_units + p.q_units; ++u)
             times.push_back(p.order.unit[u].kv ? kv_time(p.order.unit[u].block)
                                               : q_time(p.order.unit[u].block));
     } else {
@@ -1111,9 +1115,7 @@ double bwd_makespan(const BwdPlan& p, const BwdCosts& c, const BwdSize& size, in
             times.insert(times.end(),
                          bwd_parts(size.kv_steps(b), p.kv_chunk), kv_time(b));
         for (int b = p.q_blocks - 1; b >= 0; --b)
-            times.insert(times.end(),
-                         (size_t)size.group * bwd_parts(size.q_steps(b), p.q_chunk),
-                         q_time(b));
+            times.insert(times.end(), bwd_parts(size.q_steps(b), p.q_chunk), q_time(b));
     }
     if ((long long)times.size() * heads > 16LL * slots) {  // many: near what the work allows
         double total = 0.0, longest = 0.0;
@@ -1146,32 +1148,32 @@ bool plan_bwd(int num_cus, int B, int Hq, int Hkv, int Sq, int Skv, int d, int c
     const long long n_qt = ((long long)Sq + 31) / 32;
     BwdPlan p;
     p.kv_blocks = p.kv_units = (int)(((long long)Skv + rows - 1) / rows);
-    p.q_blocks = p.q_units = (int)(((long long)Sq + rows - 1) / rows);
     const long long heads = (long long)B * Hkv;
-    const long long units = p.kv_units + (long long)group * p.q_units;
     const long long row_wgs = n_qt * (d / 64);  // of a head's row values, d / 8 lanes to a row
-    if (n_qt * group > 0x3fffffffLL || heads > kMaxWorkgroups || units > kMaxWorkgroups ||
-        heads * units > kMaxWorkgroups || row_wgs * group > kMaxWorkgroups ||
+    if (heads > kMaxWorkgroups || row_wgs * group > kMaxWorkgroups ||
         heads * group * row_wgs > kMaxWorkgroups)
         return false;
+    p.q_blocks = p.q_units = size.q_blocks();
+    const long long units = (long long)p.kv_units + p.q_units;
+    if (units > kMaxWorkgroups || heads * units > kMaxWorkgroups) return false;
     const BwdCosts c = d == 64 ? BwdCosts{1.05, 0.82, 6.0} : BwdCosts{1.7, 1.35, 7.0};
     p.grid = heads * units;
     bwd_order(&p, c, size);
     *out = p;
     const double longest =
-        std::max(c.kv_step * size.kv_steps(0),
+        std::max(kv_step(c, size, 0) * size.kv_steps(0),
                  c.q_step * size.q_steps(p.q_blocks - 1));
     double total = c.workgroup * p.grid;
     for (int b = 0; b < p.kv_blocks; ++b)
-        total += c.kv_step * heads * size.kv_steps(b);
+        total += kv_step(c, size, b) * heads * size.kv_steps(b);
     for (int b = 0; b < p.q_blocks; ++b)
-        total += c.q_step * heads * group * size.q_steps(b);
+        total += c.q_step * heads * size.q_steps(b);
     // many rounds, and no block that outlasts them: what a split might save is small
     if (p.grid > 8LL * slots && longest < total / slots) return true;
     const double shortest = std::max(2 * c.kv_step, 0.1 * total / slots);
     for (int n = 1; n == 1 || longest / n >= shortest; n = n < 8 ? n + 1 : n + n / 4) {
         BwdPlan t = p;
-        t.kv_chunk = (int)ceil(longest / n / c.kv_step);
+        t.kv_chunk = (int)ceil(longest / n / kv_step(c, size, 0));
         t.q_chunk = (int)ceil(longest / n / c.q_step);
         double values = 0.0;  // of parts, written and read
         long long kv_units = 0, q_units = 0;
@@ -1185,11 +1187,11 @@ bool plan_bwd(int num_cus, int B, int Hq, int Hkv, int Sq, int Skv, int d, int c
             const int m = bwd_parts(size.q_steps(b), t.q_chunk);
             q_units += m;
             t.q_parts = std::max(t.q_parts, m);
-            if (m > 1) values += 1.0 * heads * group * m * rows * d;
+            if (m > 1) values += 1.0 * heads * m * rows * d;
         }
         if (t.kv_parts <= 1) t.kv_chunk = t.kv_parts = 0;
         if (t.q_parts <= 1) t.q_chunk = t.q_parts = 0;
-        t.grid = heads * (kv_units + group * q_units);
+        t.grid = heads * (kv_units + q_units);
         if (n > 1 && (t.grid > p.grid + 6LL * slots || t.grid > kMaxWorkgroups)) break;
         if (bwd_workspace_floats(t, B, Hq, Hkv, Sq, Skv, d) * 4 > kBwdMaxWorkspaceBytes) continue;
         t.kv_units = (int)kv_units;

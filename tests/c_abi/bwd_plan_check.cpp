@@ -19,11 +19,13 @@ static const char* check(int cus, int B, int Hq, int Hkv, int Sq, int Skv, int d
                          bool planted) {
     BwdPlan p;
     if (!plan_bwd(cus, B, Hq, Hkv, Sq, Skv, d, causal, &p)) return "no plan";
-    const int group = Hq / Hkv, heads = B * Hkv, units = p.kv_units + group * p.q_units;
+    const int group = Hq / Hkv, heads = B * Hkv, units = p.kv_units + p.q_units;
     if (p.grid != (long long)heads * units) return "grid";
     const int rows = bwd_block_rows(d);
     const BwdSize size = {rows, Sq, Skv, group, causal};
-    if (p.kv_blocks != (Skv + rows - 1) / rows || p.q_blocks != (Sq + rows - 1) / rows)
+    const int q_tiles = (Sq + 31) / 32 * group, per_block = rows / 32;
+    if (p.kv_blocks != (Skv + rows - 1) / rows ||
+        p.q_blocks != (q_tiles + per_block - 1) / per_block)
         return "blocks";
     if (!p.kv_chunk != !p.kv_parts || !p.q_chunk != !p.q_parts) return "parts without a chunk";
     if (p.ordered && (!causal || units > kBwdOrder)) return "an order";
@@ -43,9 +45,12 @@ static const char* check(int cus, int B, int Hq, int Hkv, int Sq, int Skv, int d
     for (int b = 0; b < p.q_blocks; ++b) {
         const int steps = size.q_steps(b), n = bwd_parts(steps, p.q_chunk);
         if (steps < 1 || n > steps || steps > (Skv + 31) / 32) return "steps of a query block";
-        const long long last = (long long)(b + 1) * rows < Sq ? (long long)(b + 1) * rows - 1 : Sq - 1;
+        long long last = 0;  // query of any of the block's tiles
+        for (int t = b * per_block; t < std::min((b + 1) * per_block, q_tiles); ++t)
+            last = std::max(last, std::min(t / group * 32LL + 31, Sq - 1LL));
         const long long reach = causal ? last + Skv - Sq : Skv - 1;
         if (steps * 32LL <= reach) return "keys left out";
+        if ((steps - 1) * 32LL > reach) return "a step past the keys";
         q_units += n;
         if (n > q_most) q_most = n;
     }
@@ -69,7 +74,7 @@ static const char* check(int cus, int B, int Hq, int Hkv, int Sq, int Skv, int d
     }
     for (int b = 0; b < p.q_blocks; ++b) {
         const double steps = size.q_steps(b);
-        total += steps * heads * group;
+        total += steps * heads;
         longest = std::max(longest, steps / bwd_parts((int)steps, p.q_chunk));
     }
     if (cus == 256 && longest > 30.0 && longest > 4.0 * total / cus) return "a block that outlasts the rest";
@@ -79,11 +84,11 @@ static const char* check(int cus, int B, int Hq, int Hkv, int Sq, int Skv, int d
     // one die's
     for (const int hx : {heads, 1}) {
         if (p.grid / heads * hx > 200000) continue;
-        std::set<std::tuple<int, int, int, int, int>> seen;
+        std::set<std::tuple<int, int, int, int>> seen;
         for (int i = 0; i < units * hx; ++i) {
             BwdWork w = bwd_work(u, p.order.unit, hx, planted && i == 3 ? 2 : i);
             const int blocks = w.kv ? p.kv_blocks : p.q_blocks;
-            if (w.head < 0 || w.head >= hx || w.g < 0 || w.g >= (w.kv ? 1 : group)) return "head";
+            if (w.head < 0 || w.head >= hx) return "head";
             if (w.block < 0 || w.block >= blocks) return "block";
             const int steps = w.kv ? size.kv_steps(w.block)
                                    : size.q_steps(w.block);
@@ -91,7 +96,7 @@ static const char* check(int cus, int B, int Hq, int Hkv, int Sq, int Skv, int d
             if (w.split < 0 || w.split >= w.splits) return "split";
             if ((long long)steps * (w.split + 1) / w.splits <= (long long)steps * w.split / w.splits)
                 return "an empty part";
-            if (!seen.insert({w.kv, w.head, w.g, w.block, w.split}).second) return "twice";
+            if (!seen.insert({w.kv, w.head, w.block, w.split}).second) return "twice";
         }
         if ((long long)seen.size() != (long long)units * hx) return "left out";
     }
@@ -136,6 +141,16 @@ int main(int argc, char** argv) {
     for (const auto& c : corners)
         if (const char* why = check(256, c[0], c[1], c[2], c[3], c[4], c[5], c[6], false))
             return printf("Hq=%d Hkv=%d Sq=%d Skv=%d: %s\n", c[1], c[2], c[3], c[4], why), 1;
+    // heads folded into one: without a mask, or of a single query, up to 2 GiB
+    const int folds[][8] = {{8, 2, 100, 128, 0, 2, 400, 0}, {8, 2, 100, 128, 1, 8, 100, 1},
+                            {8, 2, 1, 64, 1, 2, 4, 0},      {4, 4, 7, 64, 0, 4, 7, 0},
+                            {4, 1, 1 << 22, 64, 0, 4, 1 << 22, 0},
+                            {3, 1, 1 << 22, 64, 0, 1, 3 << 22, 0}};
+    for (const auto& f : folds) {
+        int Hq = f[0], Sq = f[2], causal = f[4];
+        bwd_fold(&Hq, f[1], &Sq, f[3], &causal);
+        if (Hq != f[5] || Sq != f[6] || causal != f[7]) return printf("fold\n"), 1;
+    }
     // the limits: too many workgroups for a grid is no plan, not an overflow
     BwdPlan p;
     if (plan_bwd(256, 1 << 20, 1 << 12, 1 << 12, 4096, 4096, 64, 0, &p)) return printf("limit\n"), 1;

@@ -77,6 +77,23 @@ def test_attn_bwd_uneven(pa, shape):
     attn_check(case, pa.attn_bwd(**case), f"{shape}")
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("shape", [(1, 5, 1, 100, 300), (2, 14, 2, 40, 40), (1, 24, 3, 8, 3000),
+                                   (1, 7, 1, 33, 5000), (2, 32, 2, 130, 258), (1, 2, 2, 20, 128),
+                                   (3, 3, 3, 600, 129), (1, 12, 4, 500, 385)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_attn_bwd_blocks_of_several_heads(pa, shape, d, causal):
+    # tiles of several heads of a group in a block of queries, the last block not full, groups
+    # that are no power of two; blocks of keys that are half empty
+    B, Hq, Hkv, Sq, Skv = shape
+    if causal and Sq > Skv:
+        Sq, Skv = Skv, Sq
+    announce(f"attn_bwd {shape} d={d} causal={causal}")
+    case = attn_case(B, Hq, Hkv, Sq, Skv, d, causal, dlse=True)
+    attn_check(case, pa.attn_bwd(**case), f"{shape} d={d}")
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("scale", [-0.1, 0.0, 0.3])
 def test_attn_bwd_scales(pa, d, scale):

@@ -635,15 +635,18 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int kvh, i
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     // The wave's tiles of 32 queries are WAVES apart in the block, as the keys in
-    // dkdv_block.  (Behind the last tile: that one again, and nothing stored.)
+    // dkdv_block; where the block has a tile to a wave at most, they are the second ones.
+    // (Outside of the block's tiles: the nearest one again, and nothing stored.)
     constexpr int WAVES = BwdShape<D>::WAVES;
     const int n_qt = (a.Sq + 31) / 32, tiles = n_qt * a.group;
-    const int tile0 = block * (BwdShape<D>::ROWS / 32);
+    const int block0 = block * (BwdShape<D>::ROWS / 32);
+    const bool one = QB == 2 && block0 + WAVES >= tiles;
+    const int tile0 = one ? block0 - WAVES : block0;
     int wq0[QB];         // first query
     long long head[QB];  // of which head, over the batch
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-        const int t = min(tile0 + qb * WAVES + wave, tiles - 1);
+        const int t = min(max(tile0 + qb * WAVES + wave, block0), tiles - 1);
         const int qt = __builtin_amdgcn_readfirstlane(t / a.group);
         wq0[qb] = qt * 32;
         head[qb] = (long long)kvh * a.group + (t - qt * a.group);
@@ -837,11 +840,12 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int kvh, i
     };
     // every wave's first block hidden: four of a diagonal's eight tiles, the last ones
     const int half =
-        CAUSAL && QB == 2
+        one ? begin
+        : CAUSAL && QB == 2
             ? min(end, (min(tile0 + WAVES, tiles) - 1) / a.group + (31 + diag) / 32 + 1)
             : end;
     while (step < half) tile(std::integral_constant<int, 0>{});
-    if constexpr (CAUSAL && QB == 2)
+    if constexpr (QB == 2)
         while (step < end) tile(std::integral_constant<int, 1>{});
     col_base = read.col + lds0 + (slot == 0 ? 2 : slot - 1) * L::SLOT;
     drain();
@@ -852,7 +856,8 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int kvh, i
     char* stage = lds + wave * stage_bytes<D>();
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-        const long long last = tile0 + qb * WAVES + wave < tiles ? (head[qb] + 1) * a.Sq : 0;
+        const int t = tile0 + qb * WAVES + wave;
+        const long long last = t >= block0 && t < tiles ? (head[qb] + 1) * a.Sq : 0;
         store_rows<D>(dq[qb], stage, out, head[qb] * a.Sq + wq0[qb], last,
                       part ? 0 : a.out_bf16, a.scale);
     }

@@ -312,6 +312,24 @@ struct BwdSize {
         const int q1 = ((next < tiles ? next : tiles) - 1) / group * 32 + 32;
         return ((causal ? (q1 < Sq ? q1 : Sq) + Skv - Sq : Skv) + 31) / 32;
     }
+    // Of `blocks` blocks, how many have more than x steps (x >= 0): the first blocks of keys,
+    // the last ones of queries.
+    ATTN_HD int kv_longer(int blocks, int x) const {
+        if (!causal) return kv_steps(0) > x ? blocks : 0;
+        // not more: at least n_qt - x / group whole tiles of queries before the first that
+        // reaches the block
+        const int before = (Sq + 31) / 32 - x / group;
+        if (before <= 0) return 0;
+        const long long first = ((long long)before * 32 + Skv - Sq + rows - 1) / rows;
+        return first < blocks ? (int)first : blocks;
+    }
+    ATTN_HD int q_longer(int blocks, int x) const {
+        if (!causal) return q_steps(0) > x ? blocks : 0;
+        // not more: the block's last tile ends within the queries that meet 32 x keys
+        const long long queries = 32LL * x - (Skv - Sq);
+        if (queries >= Sq) return 0;
+        return queries < 32 ? blocks : blocks - (int)(queries / 32 * group / (rows / 32));
+    }
 };
 // Without a mask the heads of a group are one head of all their rows, which lie one behind
 // another: they fill tiles together.  (A single query meets every key, mask or not.)
@@ -387,15 +405,21 @@ ATTN_HD inline BwdWork bwd_work(const BwdUnits& a, const BwdUnit* order, int hea
         unit = x - w.head * n;
     }
     const int blocks = w.kv ? a.kv_blocks : a.q_blocks;
+    const int chunk = w.kv ? a.kv_chunk : a.q_chunk;
     w.block = unit;
     w.splits = 1;
-    if (w.kv ? a.kv_chunk : a.q_chunk) {  // the block that holds the unit-th part
-        for (w.block = 0;; ++w.block) {
-            w.splits = a.parts(w.kv, w.kv ? w.block : blocks - 1 - w.block);
-            if (unit < w.splits || w.block + 1 == blocks) break;
-            unit -= w.splits;
+    if (chunk) {  // the block that holds the unit-th part: blocks of as many parts lie together
+        w.splits = a.parts(w.kv, w.kv ? 0 : blocks - 1);
+        for (w.block = 0; w.splits > 1; --w.splits) {
+            const int x = (w.splits - 1) * chunk;
+            const int same = (w.kv ? a.size.kv_longer(blocks, x) : a.size.q_longer(blocks, x)) -
+                             w.block;
+            if (unit < same * w.splits) break;
+            unit -= same * w.splits;
+            w.block += same;
         }
-        w.split = unit;
+        w.block += unit / w.splits;
+        w.split = unit % w.splits;
     }
     if (!w.kv) w.block = blocks - 1 - w.block;
     return w;

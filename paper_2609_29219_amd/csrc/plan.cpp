@@ -1066,10 +1066,13 @@ struct BwdCosts {
     double kv_step, q_step, workgroup;
 };
 
-// A step of a block of keys.  (With 64 rows to a wave, one that has no more than half its
-// keys works on those alone.)
+// A step of a block of keys or queries.  (With 64 rows to a wave, a block with no more than
+// half its rows works on those alone.)
 double kv_step(const BwdCosts& c, const BwdSize& size, int block) {
-    return c.kv_step * (size.rows == 256 && size.Skv - block * size.rows <= 128 ? 0.6 : 1.0);
+    return c.kv_step * (size.rows == 256 && size.Skv - block * 256 <= 128 ? 0.8 : 1.0);
+}
+double q_step(const BwdCosts& c, const BwdSize& size, int block) {
+    return c.q_step * (size.rows == 256 && size.q_tiles() - block * 8 <= 4 ? 0.85 : 1.0);
 }
 
 // Names the plan's units in the order of their lengths, longest first, if they are few.
@@ -1086,7 +1089,7 @@ void bwd_order(BwdPlan* p, const BwdCosts& c, const BwdSize& size) {
     for (int b = p->q_blocks - 1; b >= 0; --b) {
         const int steps = size.q_steps(b), n = bwd_parts(steps, p->q_chunk);
         for (int i = 0; i < n; ++i)
-            all.push_back({c.q_step * steps / n, {0, (uint16_t)b, (uint16_t)i}});
+            all.push_back({q_step(c, size, b) * steps / n, {0, (uint16_t)b, (uint16_t)i}});
     }
     std::stable_sort(all.begin(), all.end(),
                      [](const auto& x, const auto& y) { return x.first > y.first; });
@@ -1103,7 +1106,7 @@ double bwd_makespan(const BwdPlan& p, const BwdCosts& c, const BwdSize& size, in
     };
     auto q_time = [&](int b) {
         const int steps = size.q_steps(b);
-        return c.workgroup + c.q_step * steps / bwd_parts(steps, p.q_chunk);
+        return c.workgroup + q_step(c, size, b) * steps / bwd_parts(steps, p.q_chunk);
     };
     std::vector<double> times;  // of a head's units, in order
     if (p.ordered) {
@@ -1162,19 +1165,19 @@ bool plan_bwd(int num_cus, int B, int Hq, int Hkv, int Sq, int Skv, int d, int c
     *out = p;
     const double longest =
         std::max(kv_step(c, size, 0) * size.kv_steps(0),
-                 c.q_step * size.q_steps(p.q_blocks - 1));
+                 q_step(c, size, 0) * size.q_steps(p.q_blocks - 1));
     double total = c.workgroup * p.grid;
     for (int b = 0; b < p.kv_blocks; ++b)
         total += kv_step(c, size, b) * heads * size.kv_steps(b);
     for (int b = 0; b < p.q_blocks; ++b)
-        total += c.q_step * heads * size.q_steps(b);
+        total += q_step(c, size, b) * heads * size.q_steps(b);
     // many rounds, and no block that outlasts them: what a split might save is small
     if (p.grid > 8LL * slots && longest < total / slots) return true;
     const double shortest = std::max(2 * c.kv_step, 0.1 * total / slots);
     for (int n = 1; n == 1 || longest / n >= shortest; n = n < 8 ? n + 1 : n + n / 4) {
         BwdPlan t = p;
         t.kv_chunk = (int)ceil(longest / n / kv_step(c, size, 0));
-        t.q_chunk = (int)ceil(longest / n / c.q_step);
+        t.q_chunk = (int)ceil(longest / n / q_step(c, size, 0));
         double values = 0.0;  // of parts, written and read
         long long kv_units = 0, q_units = 0;
         for (int b = 0; b < p.kv_blocks; ++b) {

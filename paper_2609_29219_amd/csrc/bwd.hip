@@ -869,10 +869,10 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int kvh, i
 // The hardware deals workgroups round-robin to the XCDs; each XCD gets whole heads, whose
 // tiles stay in its L2, where they can be dealt evenly.
 //
-// Bound by the matrix cores, and in long calls by the power limit: B1 H32 S8192 d128 3.09 ms,
-// 1.25 PFLOP/s in the seven products at 1.99 GHz (a large GEMM of this library reaches 1.26
+// Bound by the matrix cores, and in long calls by the power limit: B1 H32 S8192 d128 3.06 ms,
+// 1.26 PFLOP/s in the seven products at 1.90 GHz (a large GEMM of this library reaches 1.23
 // on the same card).  Short causal calls also show a workgroup's start and end, some 7 us
-// each, which nothing overlaps with one wave to a SIMD: B4 H16 S2048 d128 257 us, 0.94
+// each, which nothing overlaps with one wave to a SIMD: B4 H16 S2048 d128 253 us, 0.95
 // PFLOP/s over the pairs that are not hidden.
 template <int D, bool CAUSAL>
 __global__ __launch_bounds__(

@@ -127,7 +127,7 @@ def test_valid_calls_without_device_are_hip_errors():
     assert bwd() == pa.ATTN_EHIP
     assert bwd(flags=1 | 4, dlse=A, causal=1) == pa.ATTN_EHIP
     # results right behind one another and behind the operands
-    assert bwd(dk=A + MB + 2048, dv=A + MB + 3072) == pa.ATTN_EHIP
+    assert bwd(dk=A + MB + 2048, dv=A + MB + 2048 + 1024) == pa.ATTN_EHIP
     assert bwd(dq=A + 2048, dlse=A + MB - 32) == pa.ATTN_EHIP
     assert rope() == pa.ATTN_EHIP
     assert rope(v=None, vo=None, flags=8 | 16 | 32, rot=16, pos=A) == pa.ATTN_EHIP

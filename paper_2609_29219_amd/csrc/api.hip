@@ -1003,9 +1003,11 @@ static int validate_bwd_dims(int B, int Hq, int Hkv, int Sq, int Skv, int d, int
     return ATTN_OK;
 }
 
-static int bwd_plan_of(DeviceState* st, int B, int Hq, int Hkv, int Sq, int Skv, int d,
-                       int causal, BwdPlan* plan, size_t* ws_bytes) {
-    const auto key = std::make_tuple(B, Hq, Hkv, Sq, Skv, d + (causal ? 1 : 0), st->desc.num_cus);
+static int bwd_plan_of(DeviceState* st, int B, const BwdFold& q, int Hkv, int Skv, int d,
+                       BwdPlan* plan, size_t* ws_bytes) {
+    // (the period, or 1: a mask; 0: none)
+    const int mask = q.causal ? (q.period ? q.period : 1) : 0;
+    const auto key = std::make_tuple(B, q.Hq, Hkv, q.Sq, Skv, d + mask, st->desc.num_cus);
     bool known = false;
     {
         std::lock_guard<std::mutex> lk(g_mu);
@@ -1014,13 +1016,13 @@ static int bwd_plan_of(DeviceState* st, int B, int Hq, int Hkv, int Sq, int Skv,
         if (known) *plan = it->second;
     }
     if (!known) {
-        if (!plan_bwd(st->desc.num_cus, B, Hq, Hkv, Sq, Skv, d, causal ? 1 : 0, plan))
+        if (!plan_bwd(st->desc.num_cus, B, q, Hkv, Skv, d, plan))
             return fail(ATTN_EUNSUPPORTED, "more workgroups than one launch holds");
         std::lock_guard<std::mutex> lk(g_mu);
         if (g_bwd_cache.size() >= kBwdCached) g_bwd_cache.clear();
         g_bwd_cache[key] = *plan;
     }
-    *ws_bytes = (size_t)bwd_workspace_floats(*plan, B, Hq, Hkv, Sq, Skv, d) * sizeof(float);
+    *ws_bytes = (size_t)bwd_workspace_floats(*plan, B, q, Hkv, Skv, d) * sizeof(float);
     return ATTN_OK;
 }
 
@@ -1033,8 +1035,7 @@ long long attn_bwd_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Skv, int 
         if (rc) return rc;
         BwdPlan plan;
         size_t bytes = 0;
-        bwd_fold(&Hq, Hkv, &Sq, d, &causal);
-        rc = bwd_plan_of(st, B, Hq, Hkv, Sq, Skv, d, causal, &plan, &bytes);
+        rc = bwd_plan_of(st, B, bwd_fold(Hq, Hkv, Sq, Skv, d, causal), Hkv, Skv, d, &plan, &bytes);
         return rc ? rc : (long long)bytes;
     });
 }
@@ -1075,8 +1076,8 @@ int attn_bwd(const void* q, const void* k, const void* v, const void* o, const f
         if (rc) return rc;
         BwdPlan plan;
         size_t need = 0;
-        bwd_fold(&Hq, Hkv, &Sq, d, &causal);
-        rc = bwd_plan_of(st, B, Hq, Hkv, Sq, Skv, d, causal, &plan, &need);
+        const BwdFold fold = bwd_fold(Hq, Hkv, Sq, Skv, d, causal);
+        rc = bwd_plan_of(st, B, fold, Hkv, Skv, d, &plan, &need);
         if (rc) return rc;
         void* ws = nullptr;
         std::unique_lock<std::mutex> ws_lock;  // held until the kernels are enqueued
@@ -1095,11 +1096,14 @@ int attn_bwd(const void* q, const void* k, const void* v, const void* o, const f
         a.dk = dk;
         a.dv = dv;
         a.out_bf16 = (flags & ATTN_OUT_BF16) ? 1 : 0;
-        a.Sq = Sq;
+        a.Sq = fold.Sq;
         a.Skv = Skv;
-        a.group = Hq / Hkv;
-        a.causal = causal ? 1 : 0;
-        a.q_heads = (long long)B * Hq;
+        a.group = fold.Hq / Hkv;
+        a.causal = fold.causal;
+        a.diag = fold.diag;
+        a.period = fold.period;
+        a.period_inverse = fold.period ? (uint32_t)(((1ULL << 32) + fold.period - 1) / fold.period) : 0;
+        a.q_heads = (long long)B * fold.Hq;
         a.kv_heads = (long long)B * Hkv;
         a.num_xcds = st->desc.num_xcds;
         a.scale = scale;

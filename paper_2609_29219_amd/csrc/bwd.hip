@@ -218,6 +218,15 @@ __device__ __forceinline__ void settle(f32x16 (&d)[N]) {
         asm volatile("s_nop 11" : "+v"(d[FROM]));
 }
 
+// Masks: none, causal, and causal with the heads of a group in one.  (Apart: at d = 128 the
+// causal kernel has no register to spare for finding each row's position, it would spill 27.)
+constexpr int kNoMask = 0, kCausalMask = 1, kFoldedMask = 2;
+
+// Position of a row of a folded problem.  (Exact: rows are fewer than 2^32 / period.)
+__device__ __forceinline__ int position(const BwdArgs& a, int row) {
+    return row - a.period * (int)__umulhi((uint32_t)row, a.period_inverse);
+}
+
 // Row of accumulator register r in lane half hh.
 __device__ __forceinline__ int acc_row(int r, int hh) { return 8 * (r >> 2) + 4 * hh + (r & 3); }
 
@@ -370,9 +379,10 @@ __global__ __launch_bounds__(256) void bwd_rows_kernel(const BwdArgs a) {
 
 // ------------------------------------------------------------------ dK, dV --
 // One block of keys (kv head bh, over the batch), part `split` of `splits` of its sum.
-template <int D, bool CAUSAL>
+template <int D, int MASK>
 __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, int block,
                                            int split, int splits) {
+    constexpr bool CAUSAL = MASK != kNoMask, FOLDED = MASK == kFoldedMask;
     constexpr int KB = BwdShape<D>::BLOCKS, KD = D / 16, CB = D / 32;
     typedef BwdLds<D> L;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
@@ -388,7 +398,7 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
 
     // steps: query tiles of every head of the group, from the first that reaches the
     // block's first key
-    const int diag = a.Skv - a.Sq;
+    const int diag = a.diag;
     const int n_qt = (a.Sq + 31) / 32;
     const int qt0 = CAUSAL ? max(0, k0 - diag) / 32 : 0;
     const int per_q = n_qt - qt0;
@@ -415,7 +425,7 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
     auto issue = [&](int slot) __attribute__((always_inline)) {
         const uint32_t dst = lds0 + slot * L::SLOT;
         load.issue(q_rsrc, g_rsrc, dst, load_qt * 32, a.Sq, wave);
-        if (wave == 0) lds_dma4(row_rsrc, rows0 + slot * 256, lane * 4, load_qt * 256);
+        if (wave == 0) lds_dma4(row_rsrc, rows0 + slot * 256, __lane_id() * 4, load_qt * 256);
         if (++load_qt == n_qt) {
             load_qt = qt0;
             ++load_g;
@@ -494,6 +504,13 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
     auto hide = [&](int q0, auto na, Scores& x_) __attribute__((always_inline)) {
 #pragma unroll
         for (int kb = 0; kb < decltype(na)::value; ++kb) {
+            if constexpr (FOLDED) {
+                const int lim = wk0 + kb * KSTEP + l32 - diag;
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    x_.s[kb][r] = position(a, q0 + acc_row(r, hh)) >= lim ? x_.s[kb][r] : a.hidden;
+                continue;
+            }
             const int lim = wk0 + kb * KSTEP + l32 - q0 - diag - 4 * hh;
 #pragma unroll
             for (int r = 0; r < 16; ++r) x_.s[kb][r] = acc_row(r, 0) >= lim ? x_.s[kb][r] : a.hidden;
@@ -548,7 +565,8 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
             });
             if constexpr (ph == 1 && j == 0) {
                 settle<0, NA>(x.s);
-                if (CAUSAL && q0 + diag < wk0 + (NA - 1) * KSTEP + 31) hide(q0, na, x);
+                if (CAUSAL && (FOLDED ? 0 : q0) + diag < wk0 + (NA - 1) * KSTEP + 31)
+                    hide(q0, na, x);
             }
             if constexpr (ph == 2 && j == 0) settle<0, NA>(x.dp);
             slot_end();
@@ -601,7 +619,7 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
     // every wave's second block hidden (four of a diagonal's eight tiles) or past the keys
     const int second = k0 + KSTEP < a.Skv ? k0 + KSTEP : INT_MAX;
     auto half = [&]() __attribute__((always_inline)) {
-        return KB == 2 && (CAUSAL ? qt * 32 + 31 + diag < second : second == INT_MAX);
+        return KB == 2 && (MASK == kCausalMask ? qt * 32 + 31 + diag < second : second == INT_MAX);
     };
     while (step < end) {
         if constexpr (KB == 2)
@@ -627,9 +645,10 @@ __device__ __forceinline__ void dkdv_block(const BwdArgs& a, char* lds, int bh, 
 // ---------------------------------------------------------------------- dQ --
 // One block of queries (of the group of kv head kvh, over the batch), part `split` of
 // `splits` of its sum.
-template <int D, bool CAUSAL>
+template <int D, int MASK>
 __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int kvh, int block,
                                          int split, int splits) {
+    constexpr bool CAUSAL = MASK != kNoMask, FOLDED = MASK == kFoldedMask;
     constexpr int QB = BwdShape<D>::BLOCKS, KD = D / 16, CB = D / 32;
     typedef BwdLds<D> L;
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
@@ -664,7 +683,7 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int kvh, i
     }
     f32x16 dq[QB][CB] = {};
 
-    const int diag = a.Skv - a.Sq;
+    const int diag = a.diag;
     const int steps = a.units.size.q_steps(block);
     const int begin = (int)((long long)steps * split / splits);
     const int end = (int)((long long)steps * (split + 1) / splits);
@@ -729,8 +748,9 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int kvh, i
     auto hide = [&](int k0, auto qf_tag) __attribute__((always_inline)) {
 #pragma unroll
         for (int qb = decltype(qf_tag)::value; qb < QB; ++qb) {
+            const int q = wq0[qb] + l32;
             const int last =
-                CAUSAL ? min(a.Skv - 1, wq0[qb] + l32 + diag) : a.Skv - 1;
+                CAUSAL ? min(a.Skv - 1, (FOLDED ? position(a, q) : q) + diag) : a.Skv - 1;
             const int lim = last - k0 - 4 * hh;
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[qb][r] = acc_row(r, 0) <= lim ? s[qb][r] : a.hidden;
@@ -771,7 +791,7 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int kvh, i
             if constexpr (ph == 0 && j == 0) settle<0, QB>(dp);
             if constexpr (ph == 1 && j == 0) {
                 settle<QF, QB>(s);
-                if (k0 + 32 > a.Skv || (CAUSAL && k0 + 31 > wq0[QF] + diag))
+                if (k0 + 32 > a.Skv || (CAUSAL && k0 + 31 > (FOLDED ? 0 : wq0[QF]) + diag))
                     hide(k0, qf_tag);
             }
             slot_end();
@@ -841,7 +861,7 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int kvh, i
     // every wave's first block hidden: four of a diagonal's eight tiles, the last ones
     const int half =
         one ? begin
-        : CAUSAL && QB == 2
+        : MASK == kCausalMask && QB == 2
             ? min(end, (min(tile0 + WAVES, tiles) - 1) / a.group + (31 + diag) / 32 + 1)
             : end;
     while (step < half) tile(std::integral_constant<int, 0>{});
@@ -874,23 +894,23 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int kvh, i
 // on the same card).  Short causal calls also show a workgroup's start and end, some 7 us
 // each, which nothing overlaps with one wave to a SIMD: B4 H16 S2048 d128 253 us, 0.95
 // PFLOP/s over the pairs that are not hidden.
-template <int D, bool CAUSAL>
+template <int D, int MASK>
 __global__ __launch_bounds__(
     BwdShape<D>::THREADS, BwdShape<D>::WAVES_PER_SIMD) void bwd_kernel(
-    const BwdArgs a, const typename std::conditional<CAUSAL, BwdOrder, int>::type order) {
+    const BwdArgs a, const typename std::conditional<MASK != kNoMask, BwdOrder, int>::type order) {
     __shared__ __attribute__((aligned(1024))) char lds[BwdLds<D>::BYTES];
     const int heads = (int)a.kv_heads;
     const bool even = heads % a.num_xcds == 0;
     const int first = even ? (int)(blockIdx.x % a.num_xcds) * (heads / a.num_xcds) : 0;
     const BwdUnit* named = nullptr;
-    if constexpr (CAUSAL) named = order.unit;
+    if constexpr (MASK != kNoMask) named = order.unit;
     const BwdWork w = bwd_work(a.units, named, even ? heads / a.num_xcds : heads,
                                even ? (int)(blockIdx.x / a.num_xcds) : (int)blockIdx.x);
     const int head = first + w.head;
     if (w.kv)
-        dkdv_block<D, CAUSAL>(a, lds, head, w.block, w.split, w.splits);
+        dkdv_block<D, MASK>(a, lds, head, w.block, w.split, w.splits);
     else
-        dq_block<D, CAUSAL>(a, lds, head, w.block, w.split, w.splits);
+        dq_block<D, MASK>(a, lds, head, w.block, w.split, w.splits);
 }
 
 // Adds up the parts of the blocks that have several, in their order, four values to a
@@ -931,10 +951,12 @@ hipError_t launch_d(const BwdPlan& p, const BwdArgs& a, int o_bf16, hipStream_t 
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const dim3 grid((unsigned)p.grid);
-    if (a.causal)
-        bwd_kernel<D, true><<<grid, BwdShape<D>::THREADS, 0, stream>>>(a, p.order);
+    if (a.period)
+        bwd_kernel<D, kFoldedMask><<<grid, BwdShape<D>::THREADS, 0, stream>>>(a, p.order);
+    else if (a.causal)
+        bwd_kernel<D, kCausalMask><<<grid, BwdShape<D>::THREADS, 0, stream>>>(a, p.order);
     else
-        bwd_kernel<D, false><<<grid, BwdShape<D>::THREADS, 0, stream>>>(a, 0);
+        bwd_kernel<D, kNoMask><<<grid, BwdShape<D>::THREADS, 0, stream>>>(a, 0);
     e = hipGetLastError();
     if (e != hipSuccess || (!p.kv_chunk && !p.q_chunk)) return e;
     const long long kv_rows = p.kv_chunk ? a.kv_heads * a.Skv : 0;
@@ -950,7 +972,7 @@ hipError_t launch_d(const BwdPlan& p, const BwdArgs& a, int o_bf16, hipStream_t 
 hipError_t launch_bwd(const BwdPlan& p, const BwdArgs& args, int d, int o_bf16,
                       hipStream_t stream) {
     BwdArgs a = args;
-    a.units = {{bwd_block_rows(d), a.Sq, a.Skv, a.group, a.causal},
+    a.units = {{bwd_block_rows(d), a.Sq, a.Skv, a.group, a.causal, a.diag},
                p.kv_blocks, p.q_blocks, p.kv_units, p.q_units, p.kv_chunk, p.q_chunk, p.ordered};
     // the parts follow the row values
     const long long kv_values = a.kv_heads * a.Skv * d;

@@ -299,10 +299,11 @@ constexpr long long kMaxWorkgroups = (1LL << 24) - 1;
 // Rows of a block, and workgroups that a compute unit holds at once.
 constexpr int bwd_block_rows(int d) { return d == 64 ? 128 : 256; }
 constexpr int bwd_wgs_per_cu(int d) { return d == 64 ? 2 : 1; }
+// diag: with a mask, query s meets the keys up to s + diag.
 struct BwdSize {
-    int rows, Sq, Skv, group, causal;
+    int rows, Sq, Skv, group, causal, diag;
     ATTN_HD int kv_steps(int block) const {
-        const int n_qt = (Sq + 31) / 32, reach = block * rows - (Skv - Sq);
+        const int n_qt = (Sq + 31) / 32, reach = block * rows - diag;
         return (n_qt - (causal && reach > 0 ? reach / 32 : 0)) * group;
     }
     ATTN_HD int q_tiles() const { return (Sq + 31) / 32 * group; }
@@ -310,7 +311,8 @@ struct BwdSize {
     ATTN_HD int q_steps(int block) const {
         const int tiles = q_tiles(), next = (block + 1) * (rows / 32);
         const int q1 = ((next < tiles ? next : tiles) - 1) / group * 32 + 32;
-        return ((causal ? (q1 < Sq ? q1 : Sq) + Skv - Sq : Skv) + 31) / 32;
+        const int reach = causal ? (q1 < Sq ? q1 : Sq) + diag : Skv;
+        return ((reach < Skv ? reach : Skv) + 31) / 32;
     }
     // Of `blocks` blocks, how many have more than x steps (x >= 0): the first blocks of keys,
     // the last ones of queries.
@@ -320,25 +322,33 @@ struct BwdSize {
         // reaches the block
         const int before = (Sq + 31) / 32 - x / group;
         if (before <= 0) return 0;
-        const long long first = ((long long)before * 32 + Skv - Sq + rows - 1) / rows;
+        const long long first = ((long long)before * 32 + diag + rows - 1) / rows;
         return first < blocks ? (int)first : blocks;
     }
     ATTN_HD int q_longer(int blocks, int x) const {
         if (!causal) return q_steps(0) > x ? blocks : 0;
         // not more: the block's last tile ends within the queries that meet 32 x keys
-        const long long queries = 32LL * x - (Skv - Sq);
+        const long long queries = 32LL * x - diag;
         if (queries >= Sq) return 0;
         return queries < 32 ? blocks : blocks - (int)(queries / 32 * group / (rows / 32));
     }
 };
-// Without a mask the heads of a group are one head of all their rows, which lie one behind
-// another: they fill tiles together.  (A single query meets every key, mask or not.)
-inline void bwd_fold(int* Hq, int Hkv, int* Sq, int d, int* causal) {
-    if (*Sq == 1) *causal = 0;
-    const long long rows = (long long)*Sq * (*Hq / Hkv);
-    if (*causal || rows * d * 2 > 0x7fffffffLL) return;
-    *Sq = (int)rows;
-    *Hq = Hkv;
+// The problem as the kernels see it.  The heads of a group are one head of all their rows,
+// which lie one behind another, where that fills tiles that a head alone would not: without
+// a mask, and with one where a head has less than a tile of rows.  A row's position is then
+// its number modulo `period`, the rows of a head (0: its number), and the rows of any tile
+// reach the last key.  (A single query meets every key, mask or not.)
+struct BwdFold {
+    int Hq, Sq, causal, diag, period;
+};
+inline BwdFold bwd_fold(int Hq, int Hkv, int Sq, int Skv, int d, int causal) {
+    BwdFold s = {Hq, Sq, causal && Sq > 1, Skv - Sq, 0};
+    const long long rows = (long long)Sq * (Hq / Hkv);
+    if (Hq == Hkv || (s.causal && Sq >= 32) || rows * d * 2 > 0x7fffffffLL) return s;
+    s.Hq = Hkv;
+    s.Sq = (int)rows;
+    if (s.causal) s.period = Sq;
+    return s;
 }
 // Parts of a block's sum, of at most chunk steps each (0: one part).
 ATTN_HD inline int bwd_parts(int steps, int chunk) {
@@ -436,6 +446,8 @@ struct BwdArgs {
     float* rows;          // 64 floats for every 32 query rows (-lse log2 e, -delta)
     void *dq, *dk, *dv;   // fp32 or bf16 (out_bf16)
     int Sq, Skv, group, causal;
+    int diag, period;         // as in BwdSize and bwd_fold
+    uint32_t period_inverse;  // 2^32 / period, rounded up
     long long q_heads, kv_heads;  // over the batch
     int num_xcds, out_bf16;
     float scale;       // of either sign, or 0
@@ -448,10 +460,10 @@ struct BwdArgs {
 // With parts, the workspace may be as large as this (without, it holds the row values).
 constexpr long long kBwdMaxWorkspaceBytes = 1LL << 30;
 // False where a launch would have more than kMaxWorkgroups.
-bool plan_bwd(int num_cus, int B, int Hq, int Hkv, int Sq, int Skv, int d, int causal,
-              BwdPlan* out);
+bool plan_bwd(int num_cus, int B, const BwdFold& q, int Hkv, int Skv, int d, BwdPlan* out);
 // Workspace in floats: the row values, then the parts.
-long long bwd_workspace_floats(const BwdPlan& p, int B, int Hq, int Hkv, int Sq, int Skv, int d);
+long long bwd_workspace_floats(const BwdPlan& p, int B, const BwdFold& q, int Hkv, int Skv,
+                               int d);
 hipError_t launch_bwd(const BwdPlan& p, const BwdArgs& a, int d, int o_bf16, hipStream_t stream);
 
 // -------------------------------------------------- per-head norm, rotation --

@@ -1144,10 +1144,9 @@ double bwd_makespan(const BwdPlan& p, const BwdCosts& c, const BwdSize& size, in
 // late, the sums of long blocks are split: parts of about equal time go to different
 // workgroups and a last kernel adds them up.  The number of parts of the longest block is
 // the fastest of the model's.
-bool plan_bwd(int num_cus, int B, int Hq, int Hkv, int Sq, int Skv, int d, int causal,
-              BwdPlan* out) {
-    const int group = Hq / Hkv, rows = bwd_block_rows(d), slots = num_cus * bwd_wgs_per_cu(d);
-    const BwdSize size = {rows, Sq, Skv, group, causal};
+bool plan_bwd(int num_cus, int B, const BwdFold& q, int Hkv, int Skv, int d, BwdPlan* out) {
+    const int Sq = q.Sq, group = q.Hq / Hkv, rows = bwd_block_rows(d), slots = num_cus * bwd_wgs_per_cu(d);
+    const BwdSize size = {rows, Sq, Skv, group, q.causal, q.diag};
     const long long n_qt = ((long long)Sq + 31) / 32;
     BwdPlan p;
     p.kv_blocks = p.kv_units = (int)(((long long)Skv + rows - 1) / rows);
@@ -1196,7 +1195,7 @@ bool plan_bwd(int num_cus, int B, int Hq, int Hkv, int Sq, int Skv, int d, int c
         if (t.q_parts <= 1) t.q_chunk = t.q_parts = 0;
         t.grid = heads * (kv_units + q_units);
         if (n > 1 && (t.grid > p.grid + 6LL * slots || t.grid > kMaxWorkgroups)) break;
-        if (bwd_workspace_floats(t, B, Hq, Hkv, Sq, Skv, d) * 4 > kBwdMaxWorkspaceBytes) continue;
+        if (bwd_workspace_floats(t, B, q, Hkv, Skv, d) * 4 > kBwdMaxWorkspaceBytes) continue;
         t.kv_units = (int)kv_units;
         t.q_units = (int)q_units;
         bwd_order(&t, c, size);
@@ -1207,9 +1206,10 @@ bool plan_bwd(int num_cus, int B, int Hq, int Hkv, int Sq, int Skv, int d, int c
     return true;
 }
 
-long long bwd_workspace_floats(const BwdPlan& p, int B, int Hq, int Hkv, int Sq, int Skv, int d) {
-    return (long long)B * Hq * (((long long)Sq + 31) / 32) * 64 +
-           2LL * p.kv_parts * B * Hkv * Skv * d + (long long)p.q_parts * B * Hq * Sq * d;
+long long bwd_workspace_floats(const BwdPlan& p, int B, const BwdFold& q, int Hkv, int Skv,
+                               int d) {
+    return (long long)B * q.Hq * (((long long)q.Sq + 31) / 32) * 64 +
+           2LL * p.kv_parts * B * Hkv * Skv * d + (long long)p.q_parts * B * q.Hq * q.Sq * d;
 }
 
 }  // namespace attn

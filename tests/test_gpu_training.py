@@ -81,11 +81,13 @@ def test_attn_bwd_uneven(pa, shape):
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("shape", [(1, 5, 1, 100, 300), (2, 14, 2, 40, 40), (1, 24, 3, 8, 3000),
                                    (1, 7, 1, 33, 5000), (2, 32, 2, 130, 258), (1, 2, 2, 20, 128),
-                                   (3, 3, 3, 600, 129), (1, 12, 4, 500, 385)],
+                                   (3, 3, 3, 600, 129), (1, 12, 4, 500, 385), (2, 7, 1, 31, 95),
+                                   (1, 12, 4, 2, 40), (2, 9, 3, 17, 17), (1, 64, 1, 29, 700)],
                          ids=lambda s: "x".join(map(str, s)))
 def test_attn_bwd_blocks_of_several_heads(pa, shape, d, causal):
     # tiles of several heads of a group in a block of queries, the last block not full, groups
-    # that are no power of two; blocks of keys that are half empty
+    # that are no power of two; blocks of keys that are half empty; fewer queries than a tile,
+    # whose heads share tiles, with a mask too
     B, Hq, Hkv, Sq, Skv = shape
     if causal and Sq > Skv:
         Sq, Skv = Skv, Sq

@@ -897,7 +897,7 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int kvh, i
 template <int D, int MASK>
 __global__ __launch_bounds__(
     BwdShape<D>::THREADS, BwdShape<D>::WAVES_PER_SIMD) void bwd_kernel(
-    const BwdArgs a, const typename std::conditional<MASK != kNoMask, BwdOrder, int>::type order) {
+    const BwdArgs a, const typename std::conditional<(MASK > 0), BwdOrder, int>::type order) {
     __shared__ __attribute__((aligned(1024))) char lds[BwdLds<D>::BYTES];
     const int heads = (int)a.kv_heads;
     const bool even = heads % a.num_xcds == 0;

@@ -334,13 +334,15 @@ int attn_gemm_plan(const attn_device_desc* desc, int M, int N, int K, int flags,
  * Work: seven products on bf16 MFMA with fp32 accumulation; P and dS are rounded
  * to bf16 as operands; every call gives the same bits (no atomics).  Where blocks of
  * 256 keys or queries are few or uneven, their sums are split, the parts (fp32, up
- * to 1 GiB of the workspace) added in a fixed order.
+ * to 1 GiB of the workspace) added in a fixed order.  Without memory for the parts in
+ * the library's workspace the call runs unsplit, with row values of 2 floats a query row
+ * in the workspace; its sums are then rounded in another order.
  * As in the forward pass, keys, values and rows that a causal mask hides from some
  * queries still have to hold finite numbers.
  * Errors as attn_fwd_ex; EINVAL also for a misaligned workspace or one smaller
  * than needed; EUNSUPPORTED also for one head's q, k or v over 2 GiB or more than
  * 2^24 - 1 workgroups (tens of millions of heads of a few rows); ENOMEM if there is no
- * memory for the library's workspace.
+ * memory for the row values in the library's workspace.
  */
 #define ATTN_O_BF16 4          /* attn_bwd flag: o is bf16 */
 int attn_bwd(const void* q, const void* k, const void* v, const void* o, const float* lse,

@@ -197,7 +197,11 @@ private:
     std::map<void*, std::unique_ptr<Entry>> entries_;
 };
 
+std::atomic<size_t> g_ws_limit{SIZE_MAX};  // larger buffers: no memory (attn__workspace_limit)
+
 int hip_ws_alloc(void*, void* stream, size_t bytes, bool captured, void** out) {
+    if (bytes > g_ws_limit)
+        return fail(ATTN_ENOMEM, "workspace of %zu bytes: over the limit", bytes);
     hipError_t e;
     if (captured) {  // not through the stream: that would be an allocation of the graph
         hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
@@ -465,6 +469,14 @@ int attn_get_plan_ex(const attn_device_desc* desc, int kind, int B, int Hq, int 
 int attn_get_plan_for(const attn_device_desc* desc, int kind, int B, int H, int Sq, int Skv,
                       int d, int causal, int n_splits, char* buf, int buflen) {
     return attn_get_plan_ex(desc, kind, B, H, H, Sq, Skv, d, causal, n_splits, buf, buflen);
+}
+
+// Not part of the ABI: buffers of more than `bytes` bytes are refused to the workspaces from
+// now on, as without memory (negative: none are).  For tests of the calls that then do
+// without.
+int attn__workspace_limit(long long bytes) {
+    g_ws_limit = bytes < 0 ? SIZE_MAX : (size_t)bytes;
+    return ATTN_OK;
 }
 
 // Not part of the ABI: every feasible prefill candidate with its modelled
@@ -1004,9 +1016,9 @@ static int validate_bwd_dims(int B, int Hq, int Hkv, int Sq, int Skv, int d, int
 }
 
 static int bwd_plan_of(DeviceState* st, int B, const BwdFold& q, int Hkv, int Skv, int d,
-                       BwdPlan* plan, size_t* ws_bytes) {
-    // (the period, or 1: a mask; 0: none)
-    const int mask = q.causal ? (q.period ? q.period : 1) : 0;
+                       bool may_split, BwdPlan* plan, size_t* ws_bytes) {
+    // (the period, less than 32, or 1: a mask; 0: none)
+    const int mask = (q.causal ? (q.period ? q.period : 1) : 0) + (may_split ? 0 : 32);
     const auto key = std::make_tuple(B, q.Hq, Hkv, q.Sq, Skv, d + mask, st->desc.num_cus);
     bool known = false;
     {
@@ -1016,7 +1028,7 @@ static int bwd_plan_of(DeviceState* st, int B, const BwdFold& q, int Hkv, int Sk
         if (known) *plan = it->second;
     }
     if (!known) {
-        if (!plan_bwd(st->desc.num_cus, B, q, Hkv, Skv, d, plan))
+        if (!plan_bwd(st->desc.num_cus, B, q, Hkv, Skv, d, plan, may_split))
             return fail(ATTN_EUNSUPPORTED, "more workgroups than one launch holds");
         std::lock_guard<std::mutex> lk(g_mu);
         if (g_bwd_cache.size() >= kBwdCached) g_bwd_cache.clear();
@@ -1035,7 +1047,8 @@ long long attn_bwd_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Skv, int 
         if (rc) return rc;
         BwdPlan plan;
         size_t bytes = 0;
-        rc = bwd_plan_of(st, B, bwd_fold(Hq, Hkv, Sq, Skv, d, causal), Hkv, Skv, d, &plan, &bytes);
+        rc = bwd_plan_of(st, B, bwd_fold(Hq, Hkv, Sq, Skv, d, causal), Hkv, Skv, d, true, &plan,
+                         &bytes);
         return rc ? rc : (long long)bytes;
     });
 }
@@ -1077,11 +1090,16 @@ int attn_bwd(const void* q, const void* k, const void* v, const void* o, const f
         BwdPlan plan;
         size_t need = 0;
         const BwdFold fold = bwd_fold(Hq, Hkv, Sq, Skv, d, causal);
-        rc = bwd_plan_of(st, B, fold, Hkv, Skv, d, &plan, &need);
+        rc = bwd_plan_of(st, B, fold, Hkv, Skv, d, true, &plan, &need);
         if (rc) return rc;
         void* ws = nullptr;
         std::unique_lock<std::mutex> ws_lock;  // held until the kernels are enqueued
         rc = call_workspace(st, need, workspace, workspace_bytes, &ws_lock, &ws);
+        // without memory for the parts the call runs unsplit
+        if (rc == ATTN_ENOMEM && (plan.kv_chunk || plan.q_chunk)) {
+            rc = bwd_plan_of(st, B, fold, Hkv, Skv, d, false, &plan, &need);
+            if (!rc) rc = call_workspace(st, need, nullptr, 0, &ws_lock, &ws);
+        }
         if (rc) return rc;
         BwdArgs a{};
         a.q = static_cast<const uint16_t*>(q);

@@ -459,8 +459,10 @@ struct BwdArgs {
 };
 // With parts, the workspace may be as large as this (without, it holds the row values).
 constexpr long long kBwdMaxWorkspaceBytes = 1LL << 30;
-// False where a launch would have more than kMaxWorkgroups.
-bool plan_bwd(int num_cus, int B, const BwdFold& q, int Hkv, int Skv, int d, BwdPlan* out);
+// False where a launch would have more than kMaxWorkgroups.  may_split false: every block in
+// one part, the row values alone in the workspace.
+bool plan_bwd(int num_cus, int B, const BwdFold& q, int Hkv, int Skv, int d, BwdPlan* out,
+              bool may_split = true);
 // Workspace in floats: the row values, then the parts.
 long long bwd_workspace_floats(const BwdPlan& p, int B, const BwdFold& q, int Hkv, int Skv,
                                int d);

@@ -1144,7 +1144,8 @@ double bwd_makespan(const BwdPlan& p, const BwdCosts& c, const BwdSize& size, in
 // late, the sums of long blocks are split: parts of about equal time go to different
 // workgroups and a last kernel adds them up.  The number of parts of the longest block is
 // the fastest of the model's.
-bool plan_bwd(int num_cus, int B, const BwdFold& q, int Hkv, int Skv, int d, BwdPlan* out) {
+bool plan_bwd(int num_cus, int B, const BwdFold& q, int Hkv, int Skv, int d, BwdPlan* out,
+              bool may_split) {
     const int Sq = q.Sq, group = q.Hq / Hkv, rows = bwd_block_rows(d), slots = num_cus * bwd_wgs_per_cu(d);
     const BwdSize size = {rows, Sq, Skv, group, q.causal, q.diag};
     const long long n_qt = ((long long)Sq + 31) / 32;
@@ -1162,6 +1163,7 @@ bool plan_bwd(int num_cus, int B, const BwdFold& q, int Hkv, int Skv, int d, Bwd
     p.grid = heads * units;
     bwd_order(&p, c, size);
     *out = p;
+    if (!may_split) return true;
     const double longest =
         std::max(kv_step(c, size, 0) * size.kv_steps(0),
                  q_step(c, size, 0) * size.q_steps(p.q_blocks - 1));

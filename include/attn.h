@@ -387,8 +387,10 @@ typedef struct attn_heads {
  * Supported: d in {64, 128}, rot a multiple of 16 up to d, dims >= 1, eps >= 0.
  * All arithmetic is fp32 (angles fp64), rounded once.  Asynchronous on the thread's
  * stream; uses no workspace.
- * Errors: EINVAL for null or misaligned pointers, bad strides or overlapping output
- * rows, dims <= 0, unknown flags or eps; EUNSUPPORTED for d, rot or more than 2^28 - 16
+ * Errors: EINVAL for null or misaligned pointers, bad strides, outputs that overlap
+ * (their own rows, each other or, unless in place, an input; layouts whose strides do not
+ * nest, as those of slices and permutations of one buffer do, are not all seen), dims <= 0,
+ * unknown flags or eps; EUNSUPPORTED for d, rot or more than 2^28 - 16
  * tokens.
  */
 #define ATTN_ROPE_INTERLEAVED 8

@@ -1153,7 +1153,7 @@ static int validate_heads(const attn_heads* h, const char* name, int B, int S, i
         {h->batch_stride, B}, {h->row_stride, S}, {h->head_stride, H}};
     for (const auto& x : dims)  // (a dimension of one has any stride)
         if (x.second > 1 &&
-            (x.first < 0 || x.first % 8 != 0 || (x.first > 0 && x.second > (1LL << 60) / x.first)))
+            (x.first < 0 || x.first % 8 != 0 || (x.first > 0 && x.second > (1LL << 56) / x.first)))
             return fail(ATTN_EINVAL, "%s: stride %lld is not a non-negative multiple of 8", name,
                         x.first);
     if (!written) return ATTN_OK;
@@ -1167,9 +1167,120 @@ static int validate_heads(const attn_heads* h, const char* name, int B, int S, i
     return ATTN_OK;
 }
 
+// Memory of an operand, in bytes: rows of `width`, by three dimensions (of an extent below
+// 2^60 each), from `at` to `end`.
+struct Rows {
+    const char* name;
+    uintptr_t at, end;
+    long long width, stride[3];
+    int n[3];
+};
+
+// strides: in values of `size` bytes, `row` of them to a row; any where n is one
+static Rows rows_of(const char* name, const void* p, int size, long long row, long long stride0,
+                    int n0, long long stride1 = 0, int n1 = 1, long long stride2 = 0, int n2 = 1) {
+    Rows r = {name, (uintptr_t)p, (uintptr_t)p, row * size, {stride0, stride1, stride2},
+              {n0, n1, n2}};
+    r.end += (uintptr_t)r.width;
+    for (int i = 0; i < 3; ++i) {
+        r.stride[i] = r.n[i] > 1 ? r.stride[i] * size : 0;
+        r.end += (uintptr_t)(r.stride[i] * (r.n[i] - 1));
+    }
+    return r;
+}
+
+static Rows heads_of(const char* name, const attn_heads& h, int B, int S, int H, int d, int size) {
+    return rows_of(name, h.ptr, size, d, h.batch_stride, B, h.row_stride, S, h.head_stride, H);
+}
+
+// Whether a sum of x_i * stride_i, lo_i <= x_i <= hi_i, lies between lo and hi (not on them).
+// Strides fall; rest_lo .. rest_hi and step: what the sums of the later terms lie in, and are
+// multiples of.  In tensors whose strides nest, as in all that come from one buffer by slicing
+// and permuting, one or two x_i of each term are left to try.  budget: terms tried at most;
+// what it leaves open counts as no.
+struct Term {
+    long long stride, lo, hi, rest_lo, rest_hi, step;
+};
+static bool sum_between(const Term* t, int n, long long lo, long long hi, int* budget) {
+    if (n == 0) return lo < 0 && hi > 0;
+    if (--*budget < 0) return false;
+    auto below = [](long long x, long long by) { return x / by - (x % by < 0); };  // floor(x / by)
+    if (below(hi - 1, t->step) * t->step <= lo) return false;
+    const long long from = std::max(t->lo, below(lo - t->rest_hi, t->stride) + 1);
+    const long long to = std::min(t->hi, below(hi - t->rest_lo - 1, t->stride));
+    for (long long x = from; x <= to && *budget >= 0; ++x)
+        if (sum_between(t + 1, n - 1, lo - x * t->stride, hi - x * t->stride, budget)) return true;
+    return false;
+}
+
+// Whether two operands share a byte.
+static bool rows_meet(const Rows& a, const Rows& b) {
+    if (a.end <= b.at || b.end <= a.at) return false;
+    // row i of a meets row j of b where -width_a < at_i - at_j < width_b
+    Term t[6];
+    int n = 0;
+    auto add = [&](long long stride, long long lo, long long hi) {
+        if (lo == hi || stride == 0) return;
+        int i = 0;
+        while (i < n && t[i].stride > stride) ++i;
+        if (i < n && t[i].stride == stride) {
+            t[i].lo += lo;
+            t[i].hi += hi;
+            return;
+        }
+        std::copy_backward(t + i, t + n, t + n + 1);
+        t[i] = {stride, lo, hi, 0, 0, 0};
+        ++n;
+    };
+    for (int i = 0; i < 3; ++i) add(a.stride[i], 0, a.n[i] - 1);
+    for (int i = 0; i < 3; ++i) add(b.stride[i], 1 - b.n[i], 0);
+    for (int i = n - 1; i >= 0; --i) {
+        t[i].step = t[i].stride;
+        if (i == n - 1) continue;
+        t[i].rest_lo = t[i + 1].rest_lo + t[i + 1].lo * t[i + 1].stride;
+        t[i].rest_hi = t[i + 1].rest_hi + t[i + 1].hi * t[i + 1].stride;
+        for (long long x = t[i + 1].step; x;) {  // the common divisor
+            const long long r = t[i].step % x;
+            t[i].step = x;
+            x = r;
+        }
+    }
+    const long long apart = (long long)(a.at - b.at);
+    int budget = 1 << 14;
+    return sum_between(t, n, -a.width - apart, b.width - apart, &budget);
+}
+
+// Results that share memory with each other or with an operand: another workgroup's stores
+// would change what is still to be read.  in_place: result i may be operand i, row by row.
+static int validate_apart(const Rows* results, int n_results, const Rows* operands, int n_operands,
+                          bool in_place) {
+    for (int i = 0; i < n_results; ++i) {
+        const Rows& r = results[i];
+        for (int j = i + 1; j < n_results; ++j)
+            if (rows_meet(r, results[j]))
+                return fail(ATTN_EINVAL, "%s overlaps %s", r.name, results[j].name);
+        for (int j = 0; j < n_operands; ++j) {
+            const Rows& x = operands[j];
+            bool same = in_place && i == j && r.at == x.at;
+            for (int k = 0; k < 3; ++k) same = same && r.stride[k] == x.stride[k];
+            if (!same && rows_meet(r, x))
+                return fail(ATTN_EINVAL, "%s overlaps %s", r.name, x.name);
+        }
+    }
+    return ATTN_OK;
+}
+
+// Not part of the ABI: whether the rows of a (Ha heads, values of size_a bytes) and b share a
+// byte.
+int attn__rows_meet(const attn_heads* a, const attn_heads* b, int B, int S, int Ha, int Hb, int d,
+                    int size_a, int size_b) {
+    return rows_meet(heads_of("a", *a, B, S, Ha, d, size_a),
+                     heads_of("b", *b, B, S, Hb, d, size_b));
+}
+
 static int validate_rope(const void* q_weight, const void* k_weight, const float* inv_freq,
-                         const void* positions, long long positions_batch_stride, int rot, int d,
-                         float eps, int flags, int known) {
+                         const void* positions, long long positions_batch_stride, int B, int rot,
+                         int d, float eps, int flags, int known) {
     if (!q_weight || !k_weight || !inv_freq) return fail(ATTN_EINVAL, "null weight or inv_freq");
     if (!aligned16(q_weight) || !aligned16(k_weight))
         return fail(ATTN_EINVAL, "weights must be 16-byte aligned");
@@ -1177,7 +1288,8 @@ static int validate_rope(const void* q_weight, const void* k_weight, const float
     if (((uintptr_t)inv_freq & 3u) ||
         ((uintptr_t)positions & ((flags & ATTN_POSITIONS_I64) ? 7u : 3u)))
         return fail(ATTN_EINVAL, "inv_freq or positions misaligned");
-    if (positions_batch_stride < 0) return fail(ATTN_EINVAL, "negative positions stride");
+    if (positions_batch_stride < 0 || (B > 1 && positions_batch_stride > (1LL << 56) / B))
+        return fail(ATTN_EINVAL, "positions: stride %lld", positions_batch_stride);
     if (!(eps >= 0.f) || !isfinite(eps))
         return fail(ATTN_EINVAL, "eps must be finite and not negative");
     if (rot < 16 || rot > d || rot % 16 != 0)
@@ -1206,6 +1318,17 @@ static RopeArgs rope_args(const void* q_weight, const void* k_weight, const floa
     return a;
 }
 
+// The operands of both calls that are no tensors of heads; returns how many.
+static int small_operands(const RopeArgs& a, int B, int d, Rows* out) {
+    const int w = a.weight_f32 ? 4 : 2, p = a.positions_i64 ? 8 : 4;
+    out[0] = rows_of("q_weight", a.weight[0], w, d, 0, 1);
+    out[1] = rows_of("k_weight", a.weight[1], w, d, 0, 1);
+    out[2] = rows_of("inv_freq", a.inv_freq, 4, a.rot / 2, 0, 1);
+    if (!a.positions) return 3;
+    out[3] = rows_of("positions", a.positions, p, a.S, a.positions_batch_stride, B);
+    return 4;
+}
+
 int attn_qk_norm_rope(const attn_heads* q, const attn_heads* k, const attn_heads* v,
                       const attn_heads* q_out, const attn_heads* k_out, const attn_heads* v_out,
                       const void* q_weight, const void* k_weight, const float* inv_freq,
@@ -1222,7 +1345,7 @@ int attn_qk_norm_rope(const attn_heads* q, const attn_heads* k, const attn_heads
         if (!rc && v) rc = validate_heads(v_out, "v_out", B, S, Hkv, d, true);
         if (!rc)
             rc = validate_rope(q_weight, k_weight, inv_freq, positions, positions_batch_stride,
-                               rot, d, eps, flags,
+                               B, rot, d, eps, flags,
                                ATTN_ROPE_INTERLEAVED | ATTN_WEIGHT_F32 | ATTN_POSITIONS_I64);
         if (rc) return rc;
         DeviceState* st = nullptr;
@@ -1238,6 +1361,16 @@ int attn_qk_norm_rope(const attn_heads* q, const attn_heads* k, const attn_heads
             a.in[2] = *v;
             a.out[2] = *v_out;
         }
+        static const char* const in_names[] = {"q", "k", "v"};
+        static const char* const out_names[] = {"q_out", "k_out", "v_out"};
+        Rows results[3], operands[7];
+        const int n = v ? 3 : 2;
+        for (int i = 0; i < n; ++i) {
+            results[i] = heads_of(out_names[i], a.out[i], B, S, i ? Hkv : Hq, d, 2);
+            operands[i] = heads_of(in_names[i], a.in[i], B, S, i ? Hkv : Hq, d, 2);
+        }
+        rc = validate_apart(results, n, operands, n + small_operands(a, B, d, operands + n), true);
+        if (rc) return rc;
         const RopeLaunch l = rope_launch(a.tokens, Hq, Hkv, d, st->desc.num_cus, false);
         a.tile_log2 = l.tile_log2;
         const hipError_t e = launch_rope(a, l, d, t_stream);
@@ -1282,7 +1415,7 @@ int attn_qk_norm_rope_bwd(const attn_heads* dq, const attn_heads* dk, const attn
         if (!rc && dv) rc = validate_heads(dv_out, "dv_out", B, S, Hkv, d, true);
         if (!rc)
             rc = validate_rope(q_weight, k_weight, inv_freq, positions, positions_batch_stride,
-                               rot, d, eps, flags,
+                               B, rot, d, eps, flags,
                                ATTN_ROPE_INTERLEAVED | ATTN_WEIGHT_F32 | ATTN_POSITIONS_I64 |
                                    ATTN_GRAD_F32);
         if (!rc && (!dq_weight != !dk_weight || ((uintptr_t)dq_weight & 3u) ||
@@ -1304,6 +1437,25 @@ int attn_qk_norm_rope_bwd(const attn_heads* dq, const attn_heads* dk, const attn
             a.in[2] = *dv;
             a.out[2] = *dv_out;
         }
+        static const char* const in_names[] = {"dq", "dk", "dv"};
+        static const char* const out_names[] = {"dq_out", "dk_out", "dv_out"};
+        Rows results[5], operands[9];
+        const int n = dv ? 3 : 2;
+        for (int i = 0; i < n; ++i) {
+            results[i] = heads_of(out_names[i], a.out[i], B, S, i ? Hkv : Hq, d, 2);
+            operands[i] = heads_of(in_names[i], a.in[i], B, S, i ? Hkv : Hq, d,
+                                  (flags & ATTN_GRAD_F32) ? 4 : 2);
+        }
+        operands[n] = heads_of("q", *q, B, S, Hq, d, 2);
+        operands[n + 1] = heads_of("k", *k, B, S, Hkv, d, 2);
+        const int n_operands = n + 2 + small_operands(a, B, d, operands + n + 2);
+        int n_results = n;
+        if (dq_weight) {
+            results[n_results++] = rows_of("dq_weight", dq_weight, 4, d, 0, 1);
+            results[n_results++] = rows_of("dk_weight", dk_weight, 4, d, 0, 1);
+        }
+        rc = validate_apart(results, n_results, operands, n_operands, false);
+        if (rc) return rc;
         const RopeLaunch l = rope_launch(a.tokens, Hq, Hkv, d, st->desc.num_cus, true);
         a.tile_log2 = l.tile_log2;
         void* ws = nullptr;

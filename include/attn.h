@@ -329,8 +329,9 @@ int attn_gemm_plan(const attn_device_desc* desc, int M, int N, int K, int flags,
  *   its replays have to be ordered with the other calls that use that stream's
  *   workspace, other graphs captured on it among them), or a 16-byte aligned device
  *   buffer of at least attn_bwd_workspace_bytes(...) bytes that the caller keeps
- *   alive until the stream has passed this call; calls that share it must be ordered.
- *   With a caller workspace the call allocates nothing.
+ *   alive until the stream has passed this call; calls that share it must be ordered,
+ *   and it must not overlap the tensors (EINVAL).  With a caller workspace the call
+ *   allocates nothing.
  * Work: seven products on bf16 MFMA with fp32 accumulation; P and dS are rounded
  * to bf16 as operands; every call gives the same bits (no atomics).  Where blocks of
  * 256 keys or queries are few or uneven, their sums are split, the parts (fp32, up

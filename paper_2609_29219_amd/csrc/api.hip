@@ -1092,6 +1092,12 @@ int attn_bwd(const void* q, const void* k, const void* v, const void* o, const f
         const BwdFold fold = bwd_fold(Hq, Hkv, Sq, Skv, d, causal);
         rc = bwd_plan_of(st, B, fold, Hkv, Skv, d, true, &plan, &need);
         if (rc) return rc;
+        if (workspace)
+            for (const auto& x : spans) {
+                const uintptr_t at = (uintptr_t)x.first, w = (uintptr_t)workspace;
+                if (at && at < w + need && w < at + (uintptr_t)x.second)
+                    return fail(ATTN_EINVAL, "the workspace overlaps a result or an operand");
+            }
         void* ws = nullptr;
         std::unique_lock<std::mutex> ws_lock;  // held until the kernels are enqueued
         rc = call_workspace(st, need, workspace, workspace_bytes, &ws_lock, &ws);
@@ -1439,7 +1445,7 @@ int attn_qk_norm_rope_bwd(const attn_heads* dq, const attn_heads* dk, const attn
         }
         static const char* const in_names[] = {"dq", "dk", "dv"};
         static const char* const out_names[] = {"dq_out", "dk_out", "dv_out"};
-        Rows results[5], operands[9];
+        Rows results[6], operands[9];
         const int n = dv ? 3 : 2;
         for (int i = 0; i < n; ++i) {
             results[i] = heads_of(out_names[i], a.out[i], B, S, i ? Hkv : Hq, d, 2);
@@ -1454,10 +1460,13 @@ int attn_qk_norm_rope_bwd(const attn_heads* dq, const attn_heads* dk, const attn
             results[n_results++] = rows_of("dq_weight", dq_weight, 4, d, 0, 1);
             results[n_results++] = rows_of("dk_weight", dk_weight, 4, d, 0, 1);
         }
-        rc = validate_apart(results, n_results, operands, n_operands, false);
-        if (rc) return rc;
         const RopeLaunch l = rope_launch(a.tokens, Hq, Hkv, d, st->desc.num_cus, true);
         a.tile_log2 = l.tile_log2;
+        if (dq_weight && workspace)
+            results[n_results++] =
+                rows_of("workspace", workspace, 1, (long long)rope_bwd_bytes(l, d), 0, 1);
+        rc = validate_apart(results, n_results, operands, n_operands, false);
+        if (rc) return rc;
         void* ws = nullptr;
         std::unique_lock<std::mutex> ws_lock;  // held until the kernels are enqueued
         if (dq_weight) {

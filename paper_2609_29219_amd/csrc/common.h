@@ -365,7 +365,7 @@ struct BwdOrder {
     BwdUnit unit[kBwdOrder];
 };
 struct BwdPlan {
-    BwdOrder order;
+    BwdOrder order{};  // (units that it does not name are zero)
     int ordered = 0;
     int kv_blocks = 0, q_blocks = 0;  // of a key/value head
     int kv_units = 0, q_units = 0;    // their parts

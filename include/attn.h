@@ -391,8 +391,8 @@ typedef struct attn_heads {
  * Errors: EINVAL for null or misaligned pointers, bad strides, outputs that overlap
  * (their own rows, each other or, unless in place, an input; layouts whose strides do not
  * nest, as those of slices and permutations of one buffer do, are not all seen), dims <= 0,
- * unknown flags or eps; EUNSUPPORTED for d, rot or more than 2^28 - 16
- * tokens.
+ * unknown flags or eps; EUNSUPPORTED for d, rot, more than 2^28 - 16 tokens or 2^30
+ * heads.
  */
 #define ATTN_ROPE_INTERLEAVED 8
 #define ATTN_WEIGHT_F32 16

@@ -1147,6 +1147,8 @@ static int validate_rope_dims(int B, int S, int Hq, int Hkv, int d) {
     if (d != 64 && d != 128) return fail(ATTN_EUNSUPPORTED, "head dim %d not in {64, 128}", d);
     if ((long long)B * S > kMaxWorkgroups * kRopeMaxTile)
         return fail(ATTN_EUNSUPPORTED, "more than %lld tokens", kMaxWorkgroups * kRopeMaxTile);
+    if (Hq > kRopeMaxHeads || Hkv > kRopeMaxHeads)
+        return fail(ATTN_EUNSUPPORTED, "more than %d heads", kRopeMaxHeads);
     return ATTN_OK;
 }
 

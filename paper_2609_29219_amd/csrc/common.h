@@ -470,6 +470,7 @@ hipError_t launch_bwd(const BwdPlan& p, const BwdArgs& a, int d, int o_bf16, hip
 
 // -------------------------------------------------- per-head norm, rotation --
 constexpr int kRopeMaxTile = 16;  // tokens to a tile at most
+constexpr int kRopeMaxHeads = 1 << 30;  // the kernels' head numbers, a step past the last too
 // Index 0: queries, 1: keys, 2: values (no norm, no rotation; ptr may be null).
 struct RopeArgs {
     attn_heads in[3];   // forward: projections; backward: gradients of the results

@@ -71,13 +71,16 @@ __device__ __forceinline__ int tile_swizzle(int row) {
 template <int D>
 struct TileLoad {
     static constexpr int W = BwdShape<D>::WAVES, PIECES = 32 * D * 2 / 1024;
-    static constexpr int NJ = 2 * PIECES / W, NO = PIECES > W ? PIECES / W : 1;
+    static constexpr int NJ = 2 * PIECES / W, NO = PIECES / W;
+    static_assert(PIECES % W == 0, "a wave's pieces of each tile");
     static constexpr int ROWS = 512 / D;  // of one piece
     int off[NO];  // this lane's source bytes within a tile
 
     __device__ __forceinline__ void init(int wave, int lane) {
 #pragma unroll
         for (int j = 0; j < NO; ++j) {
+            // (a wave's number is less than PIECES: it is written so because without the
+            // remainder the folded d = 128 kernel spills five registers, with it one)
             const int r = (wave % PIECES + j * W) * ROWS + lane / (D / 8);
             off[j] = r * (D * 2) + ((lane % (D / 8)) ^ tile_swizzle<D>(r)) * 16;
         }
@@ -87,8 +90,7 @@ struct TileLoad {
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
             const int piece = wave + j * W;
-            const dma_rsrc_t slab = NJ > 1 ? (j < NJ / 2 ? slab0 : slab1)
-                                           : (wave < PIECES ? slab0 : slab1);
+            const dma_rsrc_t slab = j < NJ / 2 ? slab0 : slab1;
             if (row0 + 32 <= n_rows) {
                 lds_dma16(slab, lds + piece * 1024, off[j % NO], row0 * (D * 2));
             } else {

@@ -319,6 +319,10 @@ int attn_gemm_plan(const attn_device_desc* desc, int M, int N, int K, int flags,
  * dk and dv summed over the query heads of a key/value head.
  *   q, k, v, scale, causal, dims: as the forward call got them.
  *   o, lse: its results; o fp32, or bf16 with ATTN_O_BF16.
+ *   (The forward pass's normaliser sums bf16-rounded weights: its lse is the log of a sum
+ *   up to 2^-8 off, relatively.  Recomputed from it, all weights of a row, and with them
+ *   the row's share of each gradient, carry that factor besides the roundings below; from
+ *   an exact lse they do not.)
  *   d_o: bf16 [B][Hq][Sq][d].
  *   dlse: NULL, or fp32 [B][Hq][Sq]: the gradient of lse, where a caller uses it
  *   (merging partial attention results).

@@ -338,7 +338,7 @@ int attn_gemm_plan(const attn_device_desc* desc, int M, int N, int K, int flags,
  *   allocates nothing.
  * Work: seven products on bf16 MFMA with fp32 accumulation; P and dS are rounded
  * to bf16 as operands; every call gives the same bits (no atomics).  Where blocks of
- * 256 keys or queries are few or uneven, their sums are split, the parts (fp32, up
+ * 256 (d = 64: 128) keys or queries are few or uneven, their sums are split, the parts (fp32, up
  * to 1 GiB of the workspace) added in a fixed order.  Without memory for the parts in
  * the library's workspace the call runs unsplit, with row values of 2 floats a query row
  * in the workspace; its sums are then rounded in another order.

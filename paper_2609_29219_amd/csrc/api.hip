@@ -252,7 +252,9 @@ std::map<std::tuple<int, int, int, int, int, int, int, int>, FwdPlan> g_fwd_cach
 std::map<std::tuple<int, int, int, int, int, int, int>, DecodePlan> g_dec_cache;
 std::map<std::tuple<int, int, int, int, int>, GemmPlan> g_gemm_cache;
 std::map<std::tuple<int, int, int, int, int, int, int>, BwdPlan> g_bwd_cache;
-constexpr size_t kBwdCached = 4096;  // plans of 3 KB: training may meet any length
+// Plans of 3 KB, and training may meet any length: at this many all are dropped (each is
+// planned again when its shape comes back).
+constexpr size_t kBwdCached = 4096;
 
 // Structural properties from the runtime; performance properties from the
 // built-in gfx950 description.

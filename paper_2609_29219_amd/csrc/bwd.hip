@@ -52,8 +52,8 @@ namespace {
 // and two blocks to a wave: every operand read from LDS serves two products (with one, LDS
 // would be as busy as the matrix cores).  With D = 64 the weights, as many for half the
 // products, take as long as those do, and two waves to a SIMD overlap the two kinds of
-// work better than one does (B4 H16 S2048 290 us against 303); in two workgroups of 128
-// rows, they leave out more of a causal diagonal (causal 155 us and 149).
+// work better than one does (B4 H16 S2048 4% faster, side by side); in two workgroups of 128
+// rows, they leave out more of a causal diagonal (causal 4% again).
 template <int D>
 struct BwdShape {
     static constexpr int ROWS = bwd_block_rows(D), BLOCKS = D == 64 ? 1 : 2;
@@ -333,7 +333,7 @@ __device__ __forceinline__ void own_read(bf16x8 (&op)[BwdShape<D>::BLOCKS][D / 1
 // ------------------------------------------------------------- row values --
 // For each tile of 32 query rows 64 floats: -lse * log2(e) of its rows, then -delta.
 // Rows past Sq get -inf and 0: their weights come out as exactly 0.  D/8 lanes to a row.
-// HBM bound, one read of O and dO: B4 H16 S2048 d128, 101 MB, 18.6 us (5.4 TB/s).
+// HBM bound, one read of O and dO: B4 H16 S2048 d128, 102 MB, 19 us (5.4 TB/s).
 template <int D, bool O_BF16>
 __global__ __launch_bounds__(256) void bwd_rows_kernel(const BwdArgs a) {
     constexpr int L = D / 8;
@@ -894,11 +894,13 @@ __device__ __forceinline__ void dq_block(const BwdArgs& a, char* lds, int kvh, i
 // The hardware deals workgroups round-robin to the XCDs; each XCD gets whole heads, whose
 // tiles stay in its L2, where they can be dealt evenly.
 //
-// Bound by the matrix cores, and in long calls by the power limit: B1 H32 S8192 d128 3.06 ms,
-// 1.26 PFLOP/s in the seven products at 1.90 GHz (a large GEMM of this library reaches 1.23
-// on the same card).  Short causal calls also show a workgroup's start and end, some 7 us
-// each, which nothing overlaps with one wave to a SIMD: B4 H16 S2048 d128 253 us, 0.95
-// PFLOP/s over the pairs that are not hidden.
+// Bound by the matrix cores, and in long calls by the clock that they run at: B1 H32 S8192
+// d128 2.93 ms, 1.31 PFLOP/s in the seven products, MFMA busy 62% at 2.0 of 2.4 GHz (a large
+// GEMM of this library reaches 1.24 on the same card).  Short causal calls also show a
+// workgroup's start and end, some 7 us each, which nothing overlaps with one wave to a SIMD:
+// B4 H16 S2048 d128 244 us in counter passes, 280 traced back to back: 0.99 and 0.86 PFLOP/s
+// over the pairs that are not hidden.  Few queries are bound by HBM: both kinds of blocks read
+// all of K and V (causal B2 Hq64 Hkv8 Sq6 Skv18702 d128 108 us, 453 MB for the necessary 307).
 template <int D, int MASK>
 __global__ __launch_bounds__(
     BwdShape<D>::THREADS, BwdShape<D>::WAVES_PER_SIMD) void bwd_kernel(
@@ -919,7 +921,7 @@ __global__ __launch_bounds__(
 }
 
 // Adds up the parts of the blocks that have several, in their order, four values to a
-// thread: dK and dV (z = 0, 1), dQ (2).  HBM bound: B2 Hq32 Hkv8 S1777 d128 7.8 us.
+// thread: dK and dV (z = 0, 1), dQ (2).  HBM bound: B2 Hq32 Hkv8 S1777 d128 8.2 us.
 template <int D>
 __global__ __launch_bounds__(256) void bwd_sum_kernel(const BwdArgs a) {
     const bool q = blockIdx.z == 2;

@@ -206,7 +206,9 @@ __device__ __forceinline__ long long token_offset(const attn_heads& h, int b, in
 }
 
 // Several rows are loaded before the first is worked on, to have enough bytes on their way:
-// B4 S8192 Hq32 Hkv8 d128, 805 MB, 155 us (5.2 TB/s, a large copy's rate).
+// B4 S8192 Hq32 Hkv8 d128, 805 MB, 152 us (5.3 TB/s, a large copy's rate).  With few heads to a
+// token the tile's positions, angles and two barriers ahead of the first row show: B8 S12857 Hq1
+// Hkv1 d64, 79 MB, 38 us (2.1 TB/s).
 template <int D, bool IL, bool NT>
 __global__ __launch_bounds__(kRopeThreads) void rope_fwd_kernel(const RopeArgs a) {
     constexpr int L = D / 8, U = 4;
@@ -265,8 +267,9 @@ __global__ __launch_bounds__(kRopeThreads) void rope_fwd_kernel(const RopeArgs a
 // in: the gradients of the outputs (bf16, or fp32 with G32); x: the forward pass's
 // inputs; out: their gradients.  Workgroups walk the tiles in steps of the grid; each
 // leaves the sums of its rows' weight gradients in ws[q, k][D/16][workgroup][16], which
-// rope_weight_kernel adds up in a fixed order.  B4 S8192 Hq32 Hkv8 d128, 1.14 GB, 238 us
-// (4.8 TB/s).
+// rope_weight_kernel adds up in a fixed order.  B4 S8192 Hq32 Hkv8 d128, 1.14 GB, 240 us
+// (4.8 TB/s); B2 S1777 H16 d64, 58 MB, 14.5 us (4.0 TB/s: one tile to most workgroups, whose
+// angles come before its first row).
 template <int D, bool IL, bool G32, bool NT>
 __global__ __launch_bounds__(kRopeThreads, 3) void rope_bwd_kernel(const RopeArgs a) {
     constexpr int L = D / 8, GROUPS = kRopeThreads / L, U = 2;

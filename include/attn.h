@@ -432,6 +432,102 @@ int attn_qk_norm_rope_bwd(const attn_heads* dq, const attn_heads* dk, const attn
                           size_t workspace_bytes);
 long long attn_qk_norm_rope_bwd_workspace_bytes(int B, int S, int Hq, int Hkv, int d);
 
+/*
+ * A cache in pages, for requests of different lengths.  Its rows are those of pages of
+ * page_size tokens (a power of two from 8 to 65536): an attn_heads whose batches are the
+ * pages, of any layout (a page's heads one by one, or its tokens).  Row r of the block table
+ * names the pages of request r: its token at position p is row p % page_size of page
+ * block_table[r * table_stride + p / page_size].  Tables, lengths and slots are int32 on the
+ * device, and so nothing about a step has to come back to the host; a slot is page * page_size
+ * + row.
+ *
+ * attn_paged_extend makes room for a step's new tokens.
+ *   seq_lens, new_lens [R]: each request's tokens in the cache, and its new ones (0 or more).
+ *   block_table: holds the pages of the former, ceil(seq_len / page_size) of them, and gets
+ *   those of the latter; entries behind them stay as they are.
+ *   free_pages [list_len], n_free [1]: free_pages[0 .. n_free - 1] are free.  New page i of the
+ *   call, in the order of the requests and of their positions, is free_pages[n_free - 1 - i].
+ *   n_left [1]: how many are free afterwards, for the next call's n_free.  Negative, it says
+ *   how many were missing: pages without one are -1 in the table, and the slots in them; the
+ *   lengths and the list are as they were, so that the call can be made again after pages
+ *   were released.
+ *   slots, positions [T]: of each new token, one request behind another (T: at least the sum
+ *   of new_lens; tokens behind the last have slot -1, position 0).  A token whose page would
+ *   be past max_pages has slot -1 too, and takes no page.
+ *   cu_seqlens [R + 1]: where each request's tokens begin; kv_lens [R]: seq_lens + new_lens.
+ * The results must not overlap each other or the operands.
+ */
+int attn_paged_extend(int* block_table, long long table_stride, const int* seq_lens,
+                      const int* new_lens, const int* free_pages, int list_len, const int* n_free,
+                      int* slots, int* positions, int* cu_seqlens, int* kv_lens, int* n_left,
+                      int R, int max_pages, int page_size, int T);
+
+/*
+ * Gives pages back: of each request the pages behind the first ceil(keep_len / page_size), of
+ * the ceil(seq_len / page_size) that it holds, in the order of the requests and of their
+ * positions, behind the n_free in free_pages (what does not fit into list_len is dropped).
+ * keep_lens [R]: the tokens that a request keeps (0: it ends; drafted tokens that were not
+ * accepted: the accepted length).  n_left [1]: how many are free afterwards.  The table is not
+ * changed.  The results must not overlap each other or the operands.
+ */
+int attn_paged_release(const int* block_table, long long table_stride, const int* seq_lens,
+                       const int* keep_lens, int* free_pages, int list_len, const int* n_free,
+                       int* n_left, int R, int max_pages, int page_size);
+
+/*
+ * Keys and values of new tokens into the cache.
+ *   k, v: bf16 [T][Hkv][d], as attn_heads of one batch; slots [T].  A token whose slot is
+ *   negative or outside the cache is left out.  No slot may be there twice.
+ *   k_pages, v_pages: n_pages pages; they must not overlap each other or the operands.
+ * Errors (of these calls): EINVAL for null or misaligned pointers, bad strides, dims <= 0 and
+ * overlaps; EUNSUPPORTED for d not in {64, 128}, a page size that is no such power of two, a
+ * cache or a table's row of more than 2^31 - 1 tokens, and rows of a page more than 2^26
+ * values apart.
+ */
+int attn_paged_store(const attn_heads* k, const attn_heads* v, const int* slots,
+                     const attn_heads* k_pages, const attn_heads* v_pages, int T, int Hkv, int d,
+                     int n_pages, int page_size);
+
+/*
+ * Attention of the new tokens of R requests over a paged cache that holds them already:
+ * single tokens, drafted ones, chunks of prompts and whole prompts in one call.
+ *   q: bf16 [T][Hq][d], as attn_heads of one batch: each request's new tokens, one request
+ *   behind another, request r's from cu_seqlens[r] to cu_seqlens[r + 1] - 1.  cu_seqlens
+ *   NULL: one token of each (T = R).  Hkv divides Hq, as in attn_fwd_ex.
+ *   o: [T][Hq][d], fp32, or bf16 with ATTN_OUT_BF16; lse: NULL, or fp32 [T][Hq].  Rows behind
+ *   the last request's are left as they were.
+ *   kv_lens [R]: each request's tokens, the new ones among them: the last new token is at
+ *   position kv_len - 1.
+ * Token at position p and key at position j of its request, head h:
+ *   x = scale q.k; with softcap > 0: softcap tanh(x / softcap); with slopes (fp32 [Hq]):
+ *   x - slopes[h] |p - j|;  o = sum exp(x) v / sum exp(x), lse = log sum exp(x)
+ * over the keys j < kv_len, with causal j <= p, with window > 0 (causal only) j > p - window.
+ * A token that sees no key (kv_len 0, or fewer tokens than new ones) has o = 0, lse = -inf.
+ *   max_q: no request has more new tokens than this (0: not known).  Rows of one that has are
+ *   not defined.
+ * Of the cache only the rows that some token of the request sees are read; keys and values of
+ * one request's own tokens that a mask hides from others of its tokens have to be finite.  A
+ * page number outside [0, n_pages) among the ones needed, or a kv_len of more than the table's
+ * row holds, makes the request's results NaN, and reads nothing outside the cache.
+ *   workspace: as for attn_bwd, of attn_paged_workspace_bytes(...) bytes.
+ * Work: two products on bf16 MFMA with fp32 accumulation and softmax; the weights are rounded
+ * to bf16 as operands, their sum takes them unrounded.  A capped score is off by up to
+ * softcap * 2^-22.  Every call gives the same bits (no atomics).
+ * Errors as the calls above; EINVAL also for Hkv not dividing Hq, unknown flags, a scale or
+ * softcap that is not finite, a negative softcap, window or max_q, T != R without cu_seqlens,
+ * and for the workspace as attn_bwd; EUNSUPPORTED also for a window without the causal mask
+ * and more than 2^31 - 1 query rows.
+ */
+int attn_paged(const attn_heads* q, const attn_heads* k_pages, const attn_heads* v_pages, void* o,
+               float* lse, const int* block_table, long long table_stride, const int* kv_lens,
+               const int* cu_seqlens, const float* slopes, int T, int R, int max_q, int Hq,
+               int Hkv, int d, int n_pages, int page_size, int max_pages, float scale,
+               float softcap, int window, int causal, int flags, void* workspace,
+               size_t workspace_bytes);
+
+/* Bytes of workspace attn_paged needs (needs the device), or a negative ATTN_E* code. */
+long long attn_paged_workspace_bytes(int T, int R, int Hq, int Hkv, int d, int max_q);
+
 #ifdef __cplusplus
 }
 #endif

@@ -11,6 +11,14 @@ device.
     o = attn_decode(q, k, v, n_splits=0)             # q [B,H,d], k/v [B,H,Skv,d] bf16
     dq, dk, dv = attn_bwd(do, q, k, v, o, lse)       # the gradients of attn_fwd
     q, k, v = qk_norm_rope(q, k, v, wq, wk, freq)    # [B,S,H,d] projections to [B,H,S,d]
+
+Requests of different lengths, over a cache in pages:
+
+    slots, positions, cu, kv_lens, n_left = paged_extend(table, seq_lens, new_lens, free_pages,
+                                                         n_free, page_size, n_tokens)
+    paged_store(k, v, slots, k_pages, v_pages)       # k, v [T,Hkv,d] into [P,Hkv,page,d]
+    o = attn_paged(q, k_pages, v_pages, table, kv_lens, cu)         # q [T,Hq,d]
+    n_free = paged_release(table, kv_lens, keep_lens, free_pages, n_left, page_size)
 """
 from __future__ import annotations
 
@@ -43,7 +51,9 @@ EXPORTED = ("attn_fwd", "attn_decode", "attn_fwd_ex", "attn_decode_ex",
             "attn_last_error", "attn_query_device", "attn_measure_device", "attn_get_plan",
             "attn_get_plan_for", "attn_get_plan_ex", "attn_gemm", "attn_gemm_plan", "attn_decode_noalloc",
             "attn_bwd", "attn_bwd_workspace_bytes", "attn_qk_norm_rope",
-            "attn_qk_norm_rope_bwd", "attn_qk_norm_rope_bwd_workspace_bytes")
+            "attn_qk_norm_rope_bwd", "attn_qk_norm_rope_bwd_workspace_bytes",
+            "attn_paged_extend", "attn_paged_release", "attn_paged_store", "attn_paged",
+            "attn_paged_workspace_bytes")
 NOALLOC_SCRATCH_BYTES = 16 << 20  # ATTN_NOALLOC_SCRATCH_BYTES
 
 
@@ -140,11 +150,21 @@ def _load() -> ctypes.CDLL:
         [cf, ci, vp, ctypes.c_size_t]
     lib.attn_qk_norm_rope_bwd_workspace_bytes.argtypes = [ci] * 5
     lib.attn_qk_norm_rope_bwd_workspace_bytes.restype = ctypes.c_longlong
+    lib.attn_paged_extend.argtypes = [vp, ll, vp, vp, vp, ci] + [vp] * 6 + [ci] * 4
+    lib.attn_paged_release.argtypes = [vp, ll, vp, vp, vp, ci, vp, vp] + [ci] * 3
+    lib.attn_paged_store.argtypes = [vp] * 5 + [ci] * 5
+    lib.attn_paged.argtypes = [vp] * 6 + [ll, vp, vp, vp] + [ci] * 9 + [cf, cf, ci, ci, ci, vp,
+                                                                       ctypes.c_size_t]
+    lib.attn_paged_workspace_bytes.argtypes = [ci] * 6
+    lib.attn_paged_workspace_bytes.restype = ctypes.c_longlong
     for fn in (lib.attn__bwd_packed, lib.attn__qk_norm_rope_packed,
-               lib.attn__qk_norm_rope_bwd_packed):
+               lib.attn__qk_norm_rope_bwd_packed, lib.attn__paged_extend_packed,
+               lib.attn__paged_release_packed, lib.attn__paged_store_packed,
+               lib.attn__paged_packed):
         fn.argtypes = [ctypes.c_char_p]
         fn.restype = ci
-    for fn in (lib.attn_bwd, lib.attn_qk_norm_rope, lib.attn_qk_norm_rope_bwd,
+    for fn in (lib.attn_paged_extend, lib.attn_paged_release, lib.attn_paged_store,
+               lib.attn_paged, lib.attn_bwd, lib.attn_qk_norm_rope, lib.attn_qk_norm_rope_bwd,
                lib.attn_fwd, lib.attn_decode, lib.attn_fwd_ex, lib.attn_decode_ex,
                lib.attn_decode_noalloc,
                lib.attn_set_stream, lib.attn_query_device,
@@ -579,6 +599,214 @@ def qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, inv_freq, positions=N
 def qk_norm_rope_bwd_workspace_bytes(B: int, S: int, Hq: int, Hkv: int, d: int) -> int:
     """Bytes of workspace qk_norm_rope_bwd needs with a caller-provided buffer."""
     n = lib.attn_qk_norm_rope_bwd_workspace_bytes(B, S, Hq, Hkv, d)
+    if n < 0:
+        raise AttnError(int(n), last_error())
+    return int(n)
+
+
+# csrc/paged_api.hip's PackedExtend, PackedRelease, PackedStore and PackedPaged
+_EXTEND_CALL = struct.Struct("Qq10Q5i")
+_RELEASE_CALL = struct.Struct("Qq6Q4i")
+_STORE_CALL = struct.Struct("16qQQ5i")
+_PAGED_CALL = struct.Struct("12q3Qq6Q12i2f")
+
+
+def _ints(t, shape, name, dev) -> int:
+    """Address of an int32 tensor, checked."""
+    import torch
+    _require_on(t, torch.int32, shape, name, dev)
+    return t.data_ptr()
+
+
+def _new_ints(out, n, name, like, dev):
+    """A result of n int32 (the given one, checked)."""
+    import torch
+    if out is None:
+        return torch.empty(n, dtype=torch.int32, device=like.device)
+    _require_on(out, torch.int32, (n,), name, dev)
+    return out
+
+
+def _block_table(table, R):
+    """Device, address, row stride and pages to a row of a block table of R rows."""
+    import torch
+    if not isinstance(table, torch.Tensor) or table.dtype is not torch.int32 or not table.is_cuda:
+        raise TypeError("block_table must be an int32 tensor on a HIP device")
+    if table.dim() != 2 or (R is not None and table.shape[0] != R):
+        raise ValueError(f"block_table has shape {tuple(table.shape)}, expected "
+                         f"({'R' if R is None else R}, max_pages)")
+    if table.stride(1) != 1 and table.shape[1] > 1:
+        raise ValueError("block_table must be contiguous in its last dimension")
+    return table.get_device(), table.data_ptr(), table.stride(0), table.shape[1]
+
+
+def _list(free_pages, dev):
+    """Address and length of a list of free pages."""
+    import torch
+    if not isinstance(free_pages, torch.Tensor) or free_pages.dim() != 1:
+        raise TypeError("free_pages must be a one-dimensional tensor")
+    _require_on(free_pages, torch.int32, free_pages.shape, "free_pages", dev)
+    return free_pages.data_ptr(), free_pages.shape[0]
+
+
+def paged_extend(block_table, seq_lens, new_lens, free_pages, n_free, page_size: int,
+                 n_tokens: int, slots=None, positions=None, cu_seqlens=None, kv_lens=None,
+                 n_left=None):
+    """Pages, slots and positions of a step's new tokens, on the GPU; returns (slots, positions,
+    cu_seqlens, kv_lens, n_left).  All tensors are int32.
+
+    block_table: [R,max_pages], holds the pages of each request's tokens and gets those of the
+    new ones, in place.  seq_lens, new_lens: [R], each request's tokens in the cache and its new
+    ones.  free_pages: the list of free pages, n_free: [1], how many of it are; they are taken
+    from its end.  n_tokens: at least the sum of new_lens.  slots (page * page_size + row) and
+    positions: [n_tokens], one request's tokens behind another's, -1 and 0 behind the last;
+    cu_seqlens: [R+1]; kv_lens: [R], seq_lens + new_lens; n_left: [1], the next call's n_free, or
+    negative: so many pages were missing (-1 in the table and in slots), and the call can be made
+    again when some were released.  The results may be given; they must not be the operands."""
+    if seq_lens.dim() != 1:
+        raise ValueError("seq_lens must be [R]")
+    R = seq_lens.shape[0]
+    dev, table_ptr, stride, max_pages = _block_table(block_table, R)
+    seq_ptr, new_ptr = _ints(seq_lens, (R,), "seq_lens", dev), _ints(new_lens, (R,), "new_lens", dev)
+    list_ptr, list_len = _list(free_pages, dev)
+    free_ptr = _ints(n_free, (1,), "n_free", dev)
+    slots = _new_ints(slots, n_tokens, "slots", block_table, dev)
+    positions = _new_ints(positions, n_tokens, "positions", block_table, dev)
+    cu_seqlens = _new_ints(cu_seqlens, R + 1, "cu_seqlens", block_table, dev)
+    kv_lens = _new_ints(kv_lens, R, "kv_lens", block_table, dev)
+    n_left = _new_ints(n_left, 1, "n_left", block_table, dev)
+    _call_on(dev, lib.attn__paged_extend_packed, _EXTEND_CALL.pack(
+        table_ptr, stride, seq_ptr, new_ptr, list_ptr, free_ptr, slots.data_ptr(),
+        positions.data_ptr(), cu_seqlens.data_ptr(), kv_lens.data_ptr(), n_left.data_ptr(),
+        _raw_stream(dev), list_len, R, max_pages, page_size, n_tokens))
+    return slots, positions, cu_seqlens, kv_lens, n_left
+
+
+def paged_release(block_table, seq_lens, keep_lens, free_pages, n_free, page_size: int,
+                  n_left=None):
+    """Pages given back: of each request those behind its first keep_lens tokens, into free_pages
+    behind the n_free in it, in place; returns n_left, [1], how many are free then.  Tensors as for
+    paged_extend (keep_lens: [R], 0 where a request ends); the table is not changed."""
+    if seq_lens.dim() != 1:
+        raise ValueError("seq_lens must be [R]")
+    R = seq_lens.shape[0]
+    dev, table_ptr, stride, max_pages = _block_table(block_table, R)
+    seq_ptr, keep_ptr = _ints(seq_lens, (R,), "seq_lens", dev), _ints(keep_lens, (R,), "keep_lens",
+                                                                      dev)
+    list_ptr, list_len = _list(free_pages, dev)
+    free_ptr = _ints(n_free, (1,), "n_free", dev)
+    n_left = _new_ints(n_left, 1, "n_left", block_table, dev)
+    _call_on(dev, lib.attn__paged_release_packed, _RELEASE_CALL.pack(
+        table_ptr, stride, seq_ptr, keep_ptr, list_ptr, free_ptr, n_left.data_ptr(),
+        _raw_stream(dev), list_len, R, max_pages, page_size))
+    return n_left
+
+
+def _packed_rows(t, name, dev=None):
+    """Shape, device and fields of attn_heads for [T,H,d], any strides with contiguous rows."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.bfloat16 or not t.is_cuda:
+        raise TypeError(f"{name} must be a {torch.bfloat16} tensor on a HIP device")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [T,H,d]")
+    row, head, one = t.stride()
+    if one != 1:
+        raise ValueError(f"{name} must be contiguous in its last dimension")
+    return t.shape, t.get_device(), (t.data_ptr(), 0, row, head)
+
+
+def _cache_pages(k_pages, v_pages, Hkv, d, dev):
+    """Pages, page size and fields of attn_heads of both sides of a cache."""
+    import torch
+    if not isinstance(k_pages, torch.Tensor) or k_pages.dim() != 4:
+        raise ValueError("k_pages must be [P,Hkv,page_size,d]")
+    n_pages, heads, page_size, _ = k_pages.shape
+    shape = (n_pages, heads if Hkv is None else Hkv, page_size, d)
+    k = _head_major(k_pages, torch.bfloat16, shape, "k_pages", dev)
+    return shape[1], n_pages, page_size, k, _head_major(v_pages, torch.bfloat16, shape, "v_pages",
+                                                        dev)
+
+
+def paged_store(k, v, slots, k_pages, v_pages) -> None:
+    """Keys and values of new tokens into the cache.  k, v: bf16 [T,Hkv,d]; slots: int32 [T] (as
+    from paged_extend; negative: left out; none twice); k_pages, v_pages: bf16
+    [P,Hkv,page_size,d].  Any strides with contiguous rows: heads of one projection, a cache whose
+    pages are token by token ([P,page_size,Hkv,d].transpose(1, 2)); qk_norm_rope's k as
+    k[0].transpose(0, 1)."""
+    (T, Hkv, d), dev, k_in = _packed_rows(k, "k")
+    v_shape, v_dev, v_in = _packed_rows(v, "v")
+    if v_shape != (T, Hkv, d) or v_dev != dev:
+        raise ValueError(f"v has shape {tuple(v_shape)}, expected {(T, Hkv, d)} on k's device")
+    _, n_pages, page_size, k_to, v_to = _cache_pages(k_pages, v_pages, Hkv, d, dev)
+    _call_on(dev, lib.attn__paged_store_packed, _STORE_CALL.pack(
+        *k_in, *v_in, *k_to, *v_to, _ints(slots, (T,), "slots", dev), _raw_stream(dev), T, Hkv, d,
+        n_pages, page_size))
+
+
+def attn_paged(q, k_pages, v_pages, block_table, kv_lens, cu_seqlens=None, max_q: int | None = None,
+               scale: float | None = None, causal: bool = True, window: int = 0,
+               softcap: float = 0.0, slopes=None, o=None, out_dtype=None,
+               return_lse: bool = False, workspace=None):
+    """Attention of the new tokens of R requests over a paged cache that holds them already;
+    returns o [T,Hq,d] (fp32, or out_dtype bf16), and with return_lse also the fp32 row
+    log-sum-exp [T,Hq].
+
+    q: bf16 [T,Hq,d], any strides with contiguous rows: each request's new tokens, one request
+    behind another, from cu_seqlens[r] (int32 [R+1]; None: one token of each).  k_pages, v_pages:
+    bf16 [P,Hkv,page_size,d], as for paged_store; Hkv divides Hq.  block_table: int32
+    [R,max_pages]; kv_lens: int32 [R], each request's tokens, the new ones among them.  max_q: no
+    request has more new tokens (None: not known; a small number spares kernels that only longer
+    requests need).  causal: a token sees the keys up to its own; window: and only so many of
+    them; softcap: scores become softcap * tanh(score / softcap); slopes: fp32 [Hq], scores fall
+    by slopes[h] for every position of distance.  A token that sees no key has o = 0, lse = -inf;
+    rows of q behind the last request's are left as they were.  workspace: None (the library's),
+    or a device tensor of at least paged_workspace_bytes(...) bytes."""
+    import torch
+    (T, Hq, d), dev, q_in = _packed_rows(q, "q")
+    Hkv, n_pages, page_size, k_in, v_in = _cache_pages(k_pages, v_pages, None, d, dev)
+    if kv_lens.dim() != 1:
+        raise ValueError("kv_lens must be [R]")
+    R = kv_lens.shape[0]
+    table_dev, table_ptr, stride, max_pages = _block_table(block_table, R)
+    if table_dev != dev:
+        raise ValueError("block_table is on another device than the first operand")
+    kv_ptr = _ints(kv_lens, (R,), "kv_lens", dev)
+    cu_ptr = 0
+    if cu_seqlens is not None:
+        cu_ptr = _ints(cu_seqlens, (R + 1,), "cu_seqlens", dev)
+    elif T != R:
+        raise ValueError(f"{T} tokens of {R} requests without cu_seqlens")
+    slopes_ptr = 0
+    if slopes is not None:
+        _require_on(slopes, torch.float32, (Hq,), "slopes", dev)
+        slopes_ptr = slopes.data_ptr()
+    if out_dtype is None:
+        out_dtype = o.dtype if o is not None else torch.float32
+    if out_dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("out_dtype must be torch.float32 or torch.bfloat16")
+    if o is None:
+        o = torch.empty((T, Hq, d), dtype=out_dtype, device=q.device)
+    else:
+        _require_on(o, out_dtype, (T, Hq, d), "o", dev)
+    lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device) if return_lse else None
+    if scale is None:
+        scale = 1.0 / math.sqrt(d)
+    if max_q is None:
+        max_q = 0 if cu_seqlens is not None else 1
+    elif max_q < 1:
+        raise ValueError("max_q must be positive")
+    _call_on(dev, lib.attn__paged_packed, _PAGED_CALL.pack(
+        *q_in, *k_in, *v_in, o.data_ptr(), 0 if lse is None else lse.data_ptr(), table_ptr, stride,
+        kv_ptr, cu_ptr, slopes_ptr, *_workspace(workspace, dev), _raw_stream(dev), T, R, max_q, Hq,
+        Hkv, d, n_pages, page_size, max_pages, window, 1 if causal else 0,
+        ATTN_OUT_BF16 if out_dtype is torch.bfloat16 else 0, scale, softcap))
+    return (o, lse) if return_lse else o
+
+
+def paged_workspace_bytes(T: int, R: int, Hq: int, Hkv: int, d: int,
+                          max_q: int | None = None) -> int:
+    """Bytes of workspace attn_paged needs with a caller-provided buffer."""
+    n = lib.attn_paged_workspace_bytes(T, R, Hq, Hkv, d, max_q or 0)
     if n < 0:
         raise AttnError(int(n), last_error())
     return int(n)

@@ -20,6 +20,7 @@
 #include <vector>
 
 #include "common.h"
+#include "host.h"
 
 namespace attn {
 hipError_t launch_fwd_d64(const FwdPlan&, const FwdArgs&, hipStream_t);
@@ -1177,15 +1178,6 @@ static int validate_heads(const attn_heads* h, const char* name, int B, int S, i
     return ATTN_OK;
 }
 
-// Memory of an operand, in bytes: rows of `width`, by three dimensions (of an extent below
-// 2^60 each), from `at` to `end`.
-struct Rows {
-    const char* name;
-    uintptr_t at, end;
-    long long width, stride[3];
-    int n[3];
-};
-
 // strides: in values of `size` bytes, `row` of them to a row; any where n is one
 static Rows rows_of(const char* name, const void* p, int size, long long row, long long stride0,
                     int n0, long long stride1 = 0, int n1 = 1, long long stride2 = 0, int n2 = 1) {
@@ -1551,3 +1543,55 @@ int attn__qk_norm_rope_bwd_packed(const PackedRopeBwd* c) {
 }
 
 }  // extern "C"
+
+// For the entry points of other files.
+namespace attn {
+namespace host {
+
+int fail(int code, const char* fmt, ...) {
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    t_error = buf;
+    return code;
+}
+
+int fail_hip(hipError_t e, const char* what) { return ::fail_hip(e, what); }
+
+hipStream_t stream() { return t_stream; }
+
+int device(DeviceRef* out) {
+    DeviceState* st = nullptr;
+    const int rc = device_state(&st);
+    if (rc) return rc;
+    out->state = st;
+    out->desc = &st->desc;
+    return ATTN_OK;
+}
+
+int workspace(const DeviceRef& dev, size_t need, void* given, size_t given_bytes,
+              std::unique_lock<std::mutex>* lk, void** out) {
+    return call_workspace(static_cast<DeviceState*>(dev.state), need, given, given_bytes, lk, out);
+}
+
+int check_heads(const attn_heads* h, const char* name, int B, int S, int H, int d, bool written) {
+    return validate_heads(h, name, B, S, H, d, written);
+}
+
+Rows heads_rows(const char* name, const attn_heads& h, int B, int S, int H, int d, int size) {
+    return heads_of(name, h, B, S, H, d, size);
+}
+
+Rows plain_rows(const char* name, const void* p, int size, long long row, long long stride0,
+                int n0) {
+    return rows_of(name, p, size, row, stride0, n0);
+}
+
+int check_apart(const Rows* results, int n_results, const Rows* operands, int n_operands) {
+    return validate_apart(results, n_results, operands, n_operands, false);
+}
+
+}  // namespace host
+}  // namespace attn

@@ -1,0 +1,105 @@
+// Declarations of the paged cache's operators: attention of new tokens over a cache whose rows
+// lie in pages, and the tables, slots and stores that go with it.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "common.h"
+
+namespace attn {
+
+// ------------------------------------------------------------------ tables --
+struct ExtendArgs {
+    int* table;
+    long long table_stride;
+    const int *seq_lens, *new_lens, *free_pages, *n_free;
+    int *slots, *positions, *cu, *kv_lens, *n_left;
+    int R, T, max_pages, n_list, page_log2;
+};
+struct ReleaseArgs {
+    const int* table;
+    long long table_stride;
+    const int *seq_lens, *keep_lens, *n_free;
+    int *free_pages, *n_left;
+    int R, max_pages, n_list, page_log2;
+};
+struct StoreArgs {
+    attn_heads k, v, k_pages, v_pages;  // (batch strides of k and v unused)
+    const int* slots;
+    int T, Hkv, n_pages, page_log2;
+};
+hipError_t launch_paged_extend(const ExtendArgs& a, hipStream_t stream);
+hipError_t launch_paged_release(const ReleaseArgs& a, hipStream_t stream);
+hipError_t launch_paged_store(const StoreArgs& a, int d, hipStream_t stream);
+
+// --------------------------------------------------------------- attention --
+constexpr int kPagedMinPageLog2 = 3;   // 8 rows of a tile lie in one page
+constexpr int kPagedMaxPageLog2 = 16;
+
+// A buffer of pages; head h of row s of page p starts at p * page + s * row + h * head
+struct PagedSide {
+    const uint16_t* ptr;
+    long long page, row, head;
+};
+
+struct PagedArgs {
+    const uint16_t* q;
+    long long q_row, q_head;
+    PagedSide k, v;
+    void* o;          // [T][Hq][D], fp32 or bf16 (out_bf16)
+    float* lse;       // [T][Hq] natural log, or null
+    const int* table; // [R], table_stride apart
+    long long table_stride;
+    const int *kv_lens, *cu;  // cu null: token r is request r's
+    const float* slopes;      // [Hq] or null
+    int T, R, Hq, Hkv, group;
+    int n_pages, page_log2, max_pages;
+    int causal, window;       // window 0: none
+    int out_bf16;
+    int few;                  // requests of up to this many rows (of all heads of a group) are
+                              // the row kernel's
+    float scale_log2;         // |scale| * log2(e), > 0
+    float cap_in, cap_out;    // capped scores in log2 units: cap_out tanh(s cap_in / (2 log2 e));
+                              // cap_out 0: not capped
+    uint32_t q_sign;          // sign bits xor-ed into Q (negative scale)
+    // Partial results of the row kernel, two to a workgroup: [workgroup][2][rows] of ws_m (log2
+    // units), ws_l and ws_o (D values each), and what the first one belongs to
+    float *ws_m, *ws_l, *ws_o;
+    int* meta;
+    int n_wg;
+};
+
+// A request as the kernels see it.
+struct PagedRequest {
+    int q0, qn;    // its tokens in q: first, how many
+    int pos0;      // position of the first
+    int kv, lo;    // its keys that any token sees: [lo, kv)
+    bool bad;      // more keys than its table holds
+};
+
+#ifdef __HIPCC__
+__device__ __forceinline__ PagedRequest paged_request(const PagedArgs& a, int r) {
+    const long long c0 = a.cu ? a.cu[r] : r, c1 = a.cu ? a.cu[r + 1] : r + 1;
+    PagedRequest x;
+    x.kv = max(a.kv_lens[r], 0);
+    x.bad = x.kv > ((long long)a.max_pages << a.page_log2);
+    x.q0 = (int)c0;
+    x.qn = 0;
+    if (c0 >= 0 && c1 > c0 && c0 < a.T) x.qn = (int)(min(c1, (long long)a.T) - c0);
+    x.pos0 = (int)(x.kv - max(c1 - c0, 0LL));
+    x.lo = a.window ? max(0, x.pos0 - a.window + 1) : 0;
+    if (x.bad) x.kv = x.lo = 0;
+    return x;
+}
+#endif
+
+// Keys to a step of the row kernel, and workgroups that share its work at most.
+constexpr int kPagedRowKeys = 128;
+constexpr int kPagedRowWgsPerCu = 4;
+constexpr int kPagedMeta = 8;  // ints to a workgroup
+// Rows to a block of the row kernel.
+inline int paged_row_block(int rows) { return rows <= 16 ? 16 : 32; }
+hipError_t launch_paged_rows(const PagedArgs& a, int d, int block, hipStream_t stream);
+
+}  // namespace attn

@@ -68,6 +68,12 @@ struct PagedArgs {
     float *ws_m, *ws_l, *ws_o;
     int* meta;
     int n_wg;
+    // The tile kernel's blocks of rows: their keys split `splits` ways at most, whose partial
+    // results lie at [block][head][split][row]
+    int splits;
+    long long tile_wgs;
+    float *tile_m, *tile_l, *tile_o;
+    int* tile_meta;
 };
 
 // A request as the kernels see it.
@@ -78,28 +84,22 @@ struct PagedRequest {
     bool bad;      // more keys than its table holds
 };
 
-#ifdef __HIPCC__
-__device__ __forceinline__ PagedRequest paged_request(const PagedArgs& a, int r) {
-    const long long c0 = a.cu ? a.cu[r] : r, c1 = a.cu ? a.cu[r + 1] : r + 1;
-    PagedRequest x;
-    x.kv = max(a.kv_lens[r], 0);
-    x.bad = x.kv > ((long long)a.max_pages << a.page_log2);
-    x.q0 = (int)c0;
-    x.qn = 0;
-    if (c0 >= 0 && c1 > c0 && c0 < a.T) x.qn = (int)(min(c1, (long long)a.T) - c0);
-    x.pos0 = (int)(x.kv - max(c1 - c0, 0LL));
-    x.lo = a.window ? max(0, x.pos0 - a.window + 1) : 0;
-    if (x.bad) x.kv = x.lo = 0;
-    return x;
-}
-#endif
 
 // Keys to a step of the row kernel, and workgroups that share its work at most.
 constexpr int kPagedRowKeys = 128;
 constexpr int kPagedRowWgsPerCu = 4;
 constexpr int kPagedMeta = 8;  // ints to a workgroup
-// Rows to a block of the row kernel.
-inline int paged_row_block(int rows) { return rows <= 16 ? 16 : 32; }
+// Requests of up to this many rows are the row kernel's (blocks of 16 or 32 rows).
+constexpr int kPagedFewRows = 32;
 hipError_t launch_paged_rows(const PagedArgs& a, int d, int block, hipStream_t stream);
+// Fewest tiles of keys to a split of the tile kernel.
+constexpr int kPagedMinTiles = 4;
+constexpr int kPagedMaxSplits = 16;
+// waves: 4 (128 rows to a block) or 8 (256); form: 1 capped scores, 2 slopes
+hipError_t launch_paged_tiles(const PagedArgs& a, int d, int waves, int form, hipStream_t stream);
+hipError_t launch_paged_tiles_d64_w4(const PagedArgs& a, int form, hipStream_t stream);
+hipError_t launch_paged_tiles_d64_w8(const PagedArgs& a, int form, hipStream_t stream);
+hipError_t launch_paged_tiles_d128_w4(const PagedArgs& a, int form, hipStream_t stream);
+hipError_t launch_paged_tiles_d128_w8(const PagedArgs& a, int form, hipStream_t stream);
 
 }  // namespace attn

@@ -84,20 +84,46 @@ int validate_paged_dims(int T, int R, int Hq, int Hkv, int d, int max_q) {
 
 // How a call is launched, from what the host knows of it.
 struct PagedLaunch {
-    int block = 0, n_wg = 0;
-    size_t o_floats = 0, row_floats = 0;  // of the partial results
-    size_t bytes() const {
-        return (o_floats + 2 * row_floats) * sizeof(float) + (size_t)n_wg * kPagedMeta * sizeof(int);
+    int few = 0;                      // requests of up to so many rows: the row kernel's
+    int block = 0, n_wg = 0;          // row kernel (n_wg 0: not launched)
+    int waves = 0, splits = 1;        // tile kernel (waves 0: not launched)
+    long long items = 0;              // its blocks of all heads at most
+    long long row_parts() const { return 2LL * n_wg * block; }
+    long long tile_parts() const { return splits > 1 ? items * splits * 32 * waves : 0; }
+    size_t bytes(int d) const {
+        return (size_t)(row_parts() + tile_parts()) * (d + 2) * sizeof(float) +
+               (size_t)(n_wg + items) * kPagedMeta * sizeof(int);
     }
 };
 
 PagedLaunch paged_launch(int T, int R, int Hq, int Hkv, int d, int max_q, int num_cus) {
     PagedLaunch l;
-    const long long most = (max_q ? std::min(max_q, T) : T) * (long long)(Hq / Hkv);
-    l.block = paged_row_block((int)std::min(most, 32LL));
-    l.n_wg = kPagedRowWgsPerCu * num_cus;
-    l.row_floats = (size_t)l.n_wg * 2 * l.block;
-    l.o_floats = l.row_floats * d;
+    const int group = Hq / Hkv;
+    const long long rows = (long long)T * group;
+    const long long most = (max_q ? std::min(max_q, T) : T) * (long long)group;  // of a request
+    // One request is either's; among several, each kernel takes those of its kind.
+    const bool tiles = most > kPagedFewRows;
+    l.few = !tiles ? INT_MAX : R == 1 ? 0 : kPagedFewRows;
+    if (l.few > 0) {
+        l.block = most <= 16 ? 16 : 32;
+        l.n_wg = kPagedRowWgsPerCu * num_cus;
+    }
+    if (tiles) {
+        l.waves = most <= 128 ? 4 : 8;
+        const long long requests = l.few ? std::min<long long>(R, rows / (l.few + 1)) : R;
+        l.items = (rows / (32 * l.waves) + requests) * Hkv;
+        // Rounds that the workgroups take, times the length of one, with a few tiles' time for
+        // the start, the end and the partial results of each split.
+        const long long at_once = (long long)num_cus * 8 / l.waves;
+        double best = 0;
+        for (int s = 1; s <= kPagedMaxSplits && (s == 1 || l.items * s <= 4 * at_once); ++s) {
+            const double t = (double)((l.items * s + at_once - 1) / at_once) * (1.0 / s + 0.02);
+            if (s == 1 || t < 0.95 * best) {
+                best = t;
+                l.splits = s;
+            }
+        }
+    }
     return l;
 }
 
@@ -246,7 +272,7 @@ long long attn_paged_workspace_bytes(int T, int R, int Hq, int Hkv, int d, int m
         host::DeviceRef dev;
         rc = host::device(&dev);
         if (rc) return rc;
-        return (long long)paged_launch(T, R, Hq, Hkv, d, max_q, dev.desc->num_cus).bytes();
+        return (long long)paged_launch(T, R, Hq, Hkv, d, max_q, dev.desc->num_cus).bytes(d);
     });
 }
 
@@ -296,15 +322,17 @@ int attn_paged(const attn_heads* q, const attn_heads* k_pages, const attn_heads*
         if (!rc) rc = host::device(&dev);
         if (rc) return rc;
         const PagedLaunch l = paged_launch(T, R, Hq, Hkv, d, max_q, dev.desc->num_cus);
+        const size_t need = l.bytes(d);
+        if (l.items * l.splits * 2 > kMaxWorkgroups)
+            return host::fail(ATTN_EUNSUPPORTED, "more workgroups than one launch holds");
         if (workspace) {
-            results[n_results] =
-                host::plain_rows("workspace", workspace, 1, (long long)l.bytes());
+            results[n_results] = host::plain_rows("workspace", workspace, 1, (long long)need);
             rc = host::check_apart(results, n_results + 1, operands, n_operands);
             if (rc) return rc;
         }
         void* ws = nullptr;
         std::unique_lock<std::mutex> ws_lock;  // held until the kernels are enqueued
-        rc = host::workspace(dev, l.bytes(), workspace, workspace_bytes, &ws_lock, &ws);
+        rc = host::workspace(dev, need, workspace, workspace_bytes, &ws_lock, &ws);
         if (rc) return rc;
         a.q = static_cast<const uint16_t*>(q->ptr);
         a.q_row = q->row_stride;
@@ -330,7 +358,7 @@ int attn_paged(const attn_heads* q, const attn_heads* k_pages, const attn_heads*
         a.causal = causal ? 1 : 0;
         a.window = window;
         a.out_bf16 = (flags & ATTN_OUT_BF16) ? 1 : 0;
-        a.few = INT_MAX;
+        a.few = l.few;
         // softmax in base 2; a negative scale flips Q's signs (exact), and a zero one becomes the
         // smallest normal float, with which all weights are equal
         const double log2e = 1.4426950408889634;
@@ -341,13 +369,23 @@ int attn_paged(const attn_heads* q, const attn_heads* k_pages, const attn_heads*
             a.cap_in = (float)(2.0 * s / softcap);
             a.cap_out = (float)(softcap * log2e);
         }
-        float* const f = static_cast<float*>(ws);
+        float* f = static_cast<float*>(ws);
         a.ws_o = f;
-        a.ws_m = f + l.o_floats;
-        a.ws_l = a.ws_m + l.row_floats;
-        a.meta = reinterpret_cast<int*>(a.ws_l + l.row_floats);
+        a.tile_o = f += l.row_parts() * d;
+        a.ws_m = f += l.tile_parts() * d;
+        a.ws_l = f += l.row_parts();
+        a.tile_m = f += l.row_parts();
+        a.tile_l = f += l.tile_parts();
+        a.meta = reinterpret_cast<int*>(f += l.tile_parts());
+        a.tile_meta = a.meta + l.n_wg * kPagedMeta;
         a.n_wg = l.n_wg;
-        const hipError_t e = launch_paged_rows(a, d, l.block, host::stream());
+        a.splits = l.splits;
+        a.tile_wgs = l.items * l.splits;
+        hipError_t e = hipSuccess;
+        if (l.n_wg) e = launch_paged_rows(a, d, l.block, host::stream());
+        if (e == hipSuccess && l.waves)
+            e = launch_paged_tiles(a, d, l.waves, (softcap > 0.f ? 1 : 0) | (slopes ? 2 : 0),
+                                   host::stream());
         return e == hipSuccess ? ATTN_OK : host::fail_hip(e, "paged attention launch");
     });
 }

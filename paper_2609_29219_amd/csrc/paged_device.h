@@ -1,0 +1,73 @@
+// Device code that the paged attention kernels share.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "paged.h"
+
+namespace attn {
+
+__device__ __forceinline__ PagedRequest paged_request(const PagedArgs& a, int r) {
+    const long long c0 = a.cu ? a.cu[r] : r, c1 = a.cu ? a.cu[r + 1] : r + 1;
+    PagedRequest x;
+    x.kv = max(a.kv_lens[r], 0);
+    x.bad = x.kv > ((long long)a.max_pages << a.page_log2);
+    x.q0 = (int)c0;
+    x.qn = 0;
+    if (c0 >= 0 && c1 > c0 && c0 < a.T) x.qn = (int)(min(c1, (long long)a.T) - c0);
+    x.pos0 = (int)(x.kv - max(c1 - c0, 0LL));
+    x.lo = a.window ? max(0, x.pos0 - a.window + 1) : 0;
+    if (x.bad) x.kv = x.lo = 0;
+    return x;
+}
+
+// Inclusive sum over the NT threads of the workgroup; *total: of all.  All threads call it.
+template <int NT>
+__device__ __forceinline__ long long block_scan(long long x, long long* total) {
+    constexpr int NW = NT / 64;
+    __shared__ long long waves[NW];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) {
+        const long long y = __shfl_up(x, off);
+        if (lane >= off) x += y;
+    }
+    __syncthreads();  // the last call's reads
+    if (lane == 63) waves[wave] = x;
+    __syncthreads();
+    long long before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        if (w < wave) before += waves[w];
+        all += waves[w];
+    }
+    *total = all;
+    return x + before;
+}
+
+// The request that has the nth of something of which request x has count(x), or -1; before it
+// there are found[1] (shared memory; all threads call it).
+template <int NT, typename F>
+__device__ __forceinline__ int paged_find(const PagedArgs& a, long long nth, long long* found,
+                                          F&& count) {
+    long long before = 0;
+    for (int r0 = 0; r0 < a.R; r0 += NT) {
+        const int r = r0 + threadIdx.x;
+        const long long mine = r < a.R ? count(paged_request(a, r)) : 0;
+        long long all;
+        const long long first = before + block_scan<NT>(mine, &all) - mine;
+        if (nth < before + all) {
+            if (nth >= first && nth < first + mine) {
+                found[0] = r;
+                found[1] = first;
+            }
+            __syncthreads();
+            return __builtin_amdgcn_readfirstlane((int)found[0]);
+        }
+        before += all;
+    }
+    return -1;
+}
+
+}  // namespace attn

@@ -30,6 +30,7 @@
 #include <stdint.h>
 
 #include "paged.h"
+#include "paged_device.h"
 
 namespace attn {
 namespace {
@@ -76,28 +77,6 @@ __device__ __forceinline__ Share share_of(const PagedArgs& a, const PagedRequest
     return s;
 }
 
-// Inclusive sum over the workgroup's threads; *total: of all.
-__device__ __forceinline__ long long block_scan(long long x, long long* total) {
-    __shared__ long long waves[kNW];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int off = 1; off < 64; off *= 2) {
-        const long long y = __shfl_up(x, off);
-        if (lane >= off) x += y;
-    }
-    __syncthreads();
-    if (lane == 63) waves[wave] = x;
-    __syncthreads();
-    long long before = 0, all = 0;
-#pragma unroll
-    for (int w = 0; w < kNW; ++w) {
-        if (w < wave) before += waves[w];
-        all += waves[w];
-    }
-    *total = all;
-    return x + before;
-}
-
 // o / l and the log-sum-exp of 4 of a row's values; a row without keys (l = 0) is 0, -inf.
 template <int D>
 __device__ __forceinline__ void store_row(const PagedArgs& a, long long token, int head, int col,
@@ -141,7 +120,7 @@ __global__ __launch_bounds__(kNT) void paged_rows_kernel(const PagedArgs a) {
         sum += mine;
     }
     long long total;
-    long long upto = block_scan(sum, &total);
+    long long upto = block_scan<kNT>(sum, &total);
     const int n_wg = (int)min((long long)a.n_wg, total);
     if (tid == 0) meta[0] = 0;
     if ((int)blockIdx.x >= n_wg) return;
@@ -156,7 +135,7 @@ __global__ __launch_bounds__(kNT) void paged_rows_kernel(const PagedArgs a) {
                 const Share s = share_of(a, paged_request(a, r), BLOCK);
                 mine = (long long)s.items * s.steps;
             }
-            upto = block_scan(mine, &all);
+            upto = block_scan<kNT>(mine, &all);
         }
         if (u0 < before + all) {
             const long long first = before + upto - mine;
@@ -414,41 +393,52 @@ __global__ __launch_bounds__(kNT) void paged_rows_kernel(const PagedArgs a) {
     }
 }
 
-// The items that lie in several workgroups: workgroup (g, y) adds the parts of rows y * ROWS ..
-// of the item that begins in workgroup g of the kernel above and does not end there.
-template <int D, int MT>
-__global__ __launch_bounds__(kNT) void paged_sum_kernel(const PagedArgs a) {
-    constexpr int LANES = D / 4, ROWS = kNT / LANES, BLOCK = 16 * MT;
-    const int* const meta = a.meta + (long long)blockIdx.x * kPagedMeta;
+// Adds parts of rows: workgroup (g, y) those of rows y * ROWS .. of the item g.  After the row
+// kernel (TILES false) item g is the one that begins in its workgroup g and does not end there:
+// its first part is that workgroup's second one, the others are the following workgroups' first.
+// After the tile kernel item g is a block of a head, its splits one behind another.
+template <int D, bool TILES>
+__global__ __launch_bounds__(kNT) void paged_sum_kernel(const PagedArgs a, int block) {
+    constexpr int LANES = D / 4, ROWS = kNT / LANES;
+    const int* const meta = (TILES ? a.tile_meta : a.meta) + (long long)blockIdx.x * kPagedMeta;
+    const float* const ws_m = TILES ? a.tile_m : a.ws_m;
+    const float* const ws_l = TILES ? a.tile_l : a.ws_l;
+    const float* const ws_o = TILES ? a.tile_o : a.ws_o;
     const int n = meta[0];
     const int row = blockIdx.y * ROWS + threadIdx.x / LANES, col = threadIdx.x % LANES * 4;
     if (n == 0 || row >= meta[4]) return;
     auto at = [&](int i) {  // part i
-        return (((long long)blockIdx.x + i) * 2 + (i == 0)) * BLOCK + row;
+        const long long part = TILES ? (long long)blockIdx.x * a.splits + i
+                                     : ((long long)blockIdx.x + i) * 2 + (i == 0);
+        return part * block + row;
     };
     float M = -INFINITY;
-    for (int i = 0; i < n; ++i) M = fmaxf(M, a.ws_m[at(i)]);
+    for (int i = 0; i < n; ++i) M = fmaxf(M, ws_m[at(i)]);
     const float ref = M == -INFINITY ? 0.f : M;
     float L = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     for (int i = 0; i < n; ++i) {
-        const float w = __builtin_amdgcn_exp2f(a.ws_m[at(i)] - ref);
-        L = fmaf(w, a.ws_l[at(i)], L);
-        acc += w * *reinterpret_cast<const f32x4*>(a.ws_o + at(i) * D + col);
+        const float w = __builtin_amdgcn_exp2f(ws_m[at(i)] - ref);
+        L = fmaf(w, ws_l[at(i)], L);
+        acc += w * *reinterpret_cast<const f32x4*>(ws_o + at(i) * D + col);
     }
     const int rr = meta[3] + row, tok = rr / a.group;
     store_row<D>(a, meta[1] + tok, meta[2] + rr - tok * a.group, col, acc, M, L);
+}
+
+template <int D, bool TILES>
+hipError_t launch_sum(const PagedArgs& a, int items, int block, hipStream_t stream) {
+    constexpr int rows = kNT / (D / 4);
+    hipLaunchKernelGGL((paged_sum_kernel<D, TILES>), dim3(items, (block + rows - 1) / rows),
+                       dim3(kNT), 0, stream, a, block);
+    return hipGetLastError();
 }
 
 template <int D, int MT>
 hipError_t launch_rows(const PagedArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((paged_rows_kernel<D, MT>), dim3(a.n_wg), dim3(kNT), 0, stream, a);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    constexpr int rows = kNT / (D / 4);
-    hipLaunchKernelGGL((paged_sum_kernel<D, MT>), dim3(a.n_wg, (16 * MT + rows - 1) / rows),
-                       dim3(kNT), 0, stream, a);
-    return hipGetLastError();
+    return e != hipSuccess ? e : launch_sum<D, false>(a, a.n_wg, 16 * MT, stream);
 }
 
 }  // namespace
@@ -459,6 +449,18 @@ hipError_t launch_paged_rows(const PagedArgs& a, int d, int block, hipStream_t s
     if (d == 128 && block == 16) return launch_rows<128, 1>(a, stream);
     if (d == 128 && block == 32) return launch_rows<128, 2>(a, stream);
     return hipErrorInvalidValue;
+}
+
+hipError_t launch_paged_tiles(const PagedArgs& a, int d, int waves, int form, hipStream_t stream) {
+    hipError_t e = hipErrorInvalidValue;
+    if (d == 64 && waves == 4) e = launch_paged_tiles_d64_w4(a, form, stream);
+    if (d == 64 && waves == 8) e = launch_paged_tiles_d64_w8(a, form, stream);
+    if (d == 128 && waves == 4) e = launch_paged_tiles_d128_w4(a, form, stream);
+    if (d == 128 && waves == 8) e = launch_paged_tiles_d128_w8(a, form, stream);
+    if (e != hipSuccess || a.splits == 1) return e;
+    const int items = (int)(a.tile_wgs / a.splits);
+    return d == 64 ? launch_sum<64, true>(a, items, 32 * waves, stream)
+                   : launch_sum<128, true>(a, items, 32 * waves, stream);
 }
 
 }  // namespace attn

@@ -1,0 +1,14 @@
+// The paged tile kernels for d = 64, blocks of 256 rows.
+#include "paged_tiles.h"
+
+namespace attn {
+
+hipError_t launch_paged_tiles_d64_w8(const PagedArgs& a, int form, hipStream_t stream) {
+    if (form == 0) return launch_paged_tiles_form<64, 8, 0>(a, stream);
+    if (form == 1) return launch_paged_tiles_form<64, 8, 1>(a, stream);
+    if (form == 2) return launch_paged_tiles_form<64, 8, 2>(a, stream);
+    if (form == 3) return launch_paged_tiles_form<64, 8, 3>(a, stream);
+    return hipErrorInvalidValue;
+}
+
+}  // namespace attn

@@ -37,10 +37,12 @@ hipError_t launch_paged_store(const StoreArgs& a, int d, hipStream_t stream);
 constexpr int kPagedMinPageLog2 = 3;   // 8 rows of a tile lie in one page
 constexpr int kPagedMaxPageLog2 = 16;
 
-// A buffer of pages; head h of row s of page p starts at p * page + s * row + h * head
+// A buffer of pages; head h of row s of page p starts at (p * page16 + s * row16) * 8 + h * head
+// values
 struct PagedSide {
     const uint16_t* ptr;
-    long long page, row, head;
+    uint32_t page16, row16;  // 16 bytes each
+    long long head;
 };
 
 struct PagedArgs {
@@ -68,6 +70,7 @@ struct PagedArgs {
     float *ws_m, *ws_l, *ws_o;
     int* meta;
     int n_wg;
+    int unit_log2;  // its work is shared out in units of 2^unit_log2 steps
     // The tile kernel's blocks of rows: their keys split `splits` ways at most, whose partial
     // results lie at [block][head][split][row]
     int splits;
@@ -81,13 +84,13 @@ struct PagedRequest {
     int q0, qn;    // its tokens in q: first, how many
     int pos0;      // position of the first
     int kv, lo;    // its keys that any token sees: [lo, kv)
-    bool bad;      // more keys than its table holds
+    int bad;       // more keys than its table holds
 };
 
 
-// Keys to a step of the row kernel, and workgroups that share its work at most.
+// Keys to a step of the row kernel, and its workgroups that a compute unit holds at once.
 constexpr int kPagedRowKeys = 128;
-constexpr int kPagedRowWgsPerCu = 4;
+constexpr int paged_row_wgs_per_cu(int d) { return d == 64 ? 4 : 2; }
 constexpr int kPagedMeta = 8;  // ints to a workgroup
 // Requests of up to this many rows are the row kernel's (blocks of 16 or 32 rows).
 constexpr int kPagedFewRows = 32;

@@ -50,9 +50,10 @@ int validate_pages(const attn_heads* p, const char* name, int n_pages, int page_
                    int d, bool written) {
     int rc = host::check_heads(p, name, n_pages, page_size, Hkv, d, written);
     if (rc) return rc;
-    // (offsets inside eight rows are 32-bit)
-    if (p->row_stride > (1LL << 26))
-        return host::fail(ATTN_EUNSUPPORTED, "%s: rows %lld values apart", name, p->row_stride);
+    // (offsets inside eight rows, and strides in steps of 16 bytes, are 32-bit)
+    if (p->row_stride > (1LL << 26) || (n_pages > 1 && p->batch_stride / 8 > UINT32_MAX))
+        return host::fail(ATTN_EUNSUPPORTED, "%s: rows %lld or pages %lld values apart", name,
+                          p->row_stride, p->batch_stride);
     return ATTN_OK;
 }
 
@@ -106,7 +107,7 @@ PagedLaunch paged_launch(int T, int R, int Hq, int Hkv, int d, int max_q, int nu
     l.few = !tiles ? INT_MAX : R == 1 ? 0 : kPagedFewRows;
     if (l.few > 0) {
         l.block = most <= 16 ? 16 : 32;
-        l.n_wg = kPagedRowWgsPerCu * num_cus;
+        l.n_wg = paged_row_wgs_per_cu(d) * num_cus;
     }
     if (tiles) {
         l.waves = most <= 128 ? 4 : 8;
@@ -337,10 +338,14 @@ int attn_paged(const attn_heads* q, const attn_heads* k_pages, const attn_heads*
         a.q = static_cast<const uint16_t*>(q->ptr);
         a.q_row = q->row_stride;
         a.q_head = q->head_stride;
-        a.k = {static_cast<const uint16_t*>(k_pages->ptr), k_pages->batch_stride,
-               k_pages->row_stride, k_pages->head_stride};
-        a.v = {static_cast<const uint16_t*>(v_pages->ptr), v_pages->batch_stride,
-               v_pages->row_stride, v_pages->head_stride};
+        auto side = [](const attn_heads& p, int n_pages) {
+            // (a single page's stride is any number)
+            return PagedSide{static_cast<const uint16_t*>(p.ptr),
+                             n_pages > 1 ? (uint32_t)(p.batch_stride / 8) : 0,
+                             (uint32_t)(p.row_stride / 8), p.head_stride};
+        };
+        a.k = side(*k_pages, n_pages);
+        a.v = side(*v_pages, n_pages);
         a.o = o;
         a.lse = lse;
         a.table = block_table;
@@ -379,6 +384,14 @@ int attn_paged(const attn_heads* q, const attn_heads* k_pages, const attn_heads*
         a.meta = reinterpret_cast<int*>(f += l.tile_parts());
         a.tile_meta = a.meta + l.n_wg * kPagedMeta;
         a.n_wg = l.n_wg;
+        // so few units that their number is 32-bit, whatever the lengths are
+        double units = 0;
+        do {
+            const double steps = (double)max_pages * page_size / kPagedRowKeys + 2;
+            units = ((double)T * a.group / 16 + R) * Hkv * (steps / (1 << a.unit_log2) + 1);
+        } while (units >= 2147483647.0 && ++a.unit_log2 < 24);
+        if (units >= 2147483647.0)
+            return host::fail(ATTN_EUNSUPPORTED, "more than 2^31 - 1 rows of heads");
         a.splits = l.splits;
         a.tile_wgs = l.items * l.splits;
         hipError_t e = hipSuccess;

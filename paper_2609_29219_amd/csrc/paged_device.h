@@ -22,21 +22,28 @@ __device__ __forceinline__ PagedRequest paged_request(const PagedArgs& a, int r)
     return x;
 }
 
+// Inclusive sum over a wave, by moves between lanes inside rows of 16, then of the rows' sums.
+__device__ __forceinline__ int wave_scan(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast 15, into 1, 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast 31, into 2, 3
+    return x;
+}
+
 // Inclusive sum over the NT threads of the workgroup; *total: of all.  All threads call it.
 template <int NT>
-__device__ __forceinline__ long long block_scan(long long x, long long* total) {
+__device__ __forceinline__ int block_scan(int x, int* total) {
     constexpr int NW = NT / 64;
-    __shared__ long long waves[NW];
+    __shared__ int waves[NW];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int off = 1; off < 64; off *= 2) {
-        const long long y = __shfl_up(x, off);
-        if (lane >= off) x += y;
-    }
+    x = wave_scan(x);
     __syncthreads();  // the last call's reads
     if (lane == 63) waves[wave] = x;
     __syncthreads();
-    long long before = 0, all = 0;
+    int before = 0, all = 0;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
         if (w < wave) before += waves[w];
@@ -49,21 +56,20 @@ __device__ __forceinline__ long long block_scan(long long x, long long* total) {
 // The request that has the nth of something of which request x has count(x), or -1; before it
 // there are found[1] (shared memory; all threads call it).
 template <int NT, typename F>
-__device__ __forceinline__ int paged_find(const PagedArgs& a, long long nth, long long* found,
-                                          F&& count) {
-    long long before = 0;
+__device__ __forceinline__ int paged_find(const PagedArgs& a, int nth, int* found, F&& count) {
+    int before = 0;
     for (int r0 = 0; r0 < a.R; r0 += NT) {
         const int r = r0 + threadIdx.x;
-        const long long mine = r < a.R ? count(paged_request(a, r)) : 0;
-        long long all;
-        const long long first = before + block_scan<NT>(mine, &all) - mine;
+        const int mine = r < a.R ? count(paged_request(a, r)) : 0;
+        int all;
+        const int first = before + block_scan<NT>(mine, &all) - mine;
         if (nth < before + all) {
             if (nth >= first && nth < first + mine) {
                 found[0] = r;
                 found[1] = first;
             }
             __syncthreads();
-            return __builtin_amdgcn_readfirstlane((int)found[0]);
+            return __builtin_amdgcn_readfirstlane(found[0]);
         }
         before += all;
     }

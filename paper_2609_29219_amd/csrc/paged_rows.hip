@@ -29,6 +29,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "lds_dma.h"
 #include "paged.h"
 #include "paged_device.h"
 
@@ -63,17 +64,20 @@ __device__ __forceinline__ float rows4_sum(float x) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// Items of a request and steps of each, for blocks of `block` rows.
+// Items of a request, and units (of 2^unit_log2 steps) of each, for blocks of `block` rows.
 struct Share {
-    int items, blocks, steps;
+    int items, blocks, steps, units;
 };
 __device__ __forceinline__ Share share_of(const PagedArgs& a, const PagedRequest& x, int block) {
-    Share s = {0, 0, 0};
+    Share s = {0, 0, 0, 0};
     const long long rows = (long long)x.qn * a.group;
     if (rows == 0 || rows > a.few) return s;
-    s.blocks = (int)((rows + block - 1) / block);
+    s.blocks = (int)((uint32_t)(rows + block - 1) / (uint32_t)block);
     s.items = s.blocks * a.Hkv;
-    s.steps = x.kv > x.lo ? (x.kv + kPagedRowKeys - 1) / kPagedRowKeys - x.lo / kPagedRowKeys : 1;
+    s.steps = x.kv > x.lo ? (int)((uint32_t)(x.kv + kPagedRowKeys - 1) / kPagedRowKeys) -
+                                x.lo / kPagedRowKeys
+                          : 1;
+    s.units = (s.steps + (1 << a.unit_log2) - 1) >> a.unit_log2;
     return s;
 }
 
@@ -94,70 +98,134 @@ __device__ __forceinline__ void store_row(const PagedArgs& a, long long token, i
         a.lse[token * a.Hq + head] = L == 0.f ? -INFINITY : (M + __builtin_log2f(L)) * kLn2;
 }
 
+// A step's 32 keys of a wave in LDS: whole rows, 1 KiB (4 or 8 rows) to a load, K's pieces 16
+// bytes apart.  A row's 16-byte pieces are exchanged inside it (by the source address of each
+// lane), so that K's reads (16 rows of one piece) and V's (8 rows of 32 bytes) are free of bank
+// conflicts.
+template <int D>
+struct RowLds {
+    static constexpr int PIECE_ROWS = 512 / D, PIECES = 32 / PIECE_ROWS;
+    static constexpr int K_PIECE = 1024 + 16, V_PIECE = 1024;
+    static constexpr int K_BYTES = PIECES * K_PIECE, V_BYTES = PIECES * V_PIECE;
+    static constexpr int WAVE = K_BYTES + V_BYTES;
+    __device__ static constexpr int k_swap(int row) {
+        return D == 128 ? 4 * (row & 3) : 2 * ((row >> 1) & 3);
+    }
+    __device__ static constexpr int v_swap(int row) {
+        return D == 128 ? 4 * (row & 3) ^ 2 * ((row >> 2) & 1) : 2 * ((row >> 1) & 3);
+    }
+};
+
+// Past the caches: each row is read once.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void load_past(dma_rsrc_t rsrc, uint32_t dst, int voffset, int soffset) {
+    asm volatile(
+        "s_mov_b32 m0, %0\n\t"
+        "s_nop 0\n\t"
+        "buffer_load_dwordx4 %1, %2, %3 offen nt lds"
+        :
+        : "s"(dst), "v"(voffset), "s"(rsrc), "s"(soffset)
+        : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
+
 template <int D, int MT>
-__global__ __launch_bounds__(kNT) void paged_rows_kernel(const PagedArgs a) {
+__global__ __launch_bounds__(kNT, 2) void paged_rows_kernel(const PagedArgs a) {
+    using L = RowLds<D>;
     constexpr int KS = D / 32;       // MFMA steps over a row
     constexpr int DB = D / 16;       // 16-column blocks of O^T
-    constexpr int VST = D + 32;      // bf16 to a row of V in LDS
     constexpr int OST = D + 4;       // floats to a row where the waves meet
     constexpr int BLOCK = 16 * MT;
-    __shared__ __attribute__((aligned(16))) uint16_t vtile[kNW][32 * VST];
+    constexpr int LOADS = L::PIECES; // of an operand and step
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kNW * L::WAVE];
     __shared__ float sm[kNW][BLOCK], sl[kNW][BLOCK];
-    __shared__ long long found[2];  // request, steps before it
-    static_assert(kNW * 16 * OST * 4 <= (int)sizeof(vtile), "");
+    __shared__ int found[8];
+    static_assert(kNW * 16 * OST * 4 <= (int)sizeof(lds), "");
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, g4 = lane >> 4;
     int* const meta = a.meta + (long long)blockIdx.x * kPagedMeta;
+    auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
 
-    // ---- this workgroup's part of the line of all steps ------------------------
-    long long mine = 0;  // up to kNT requests: this thread's
-    long long sum = 0;
+    // ---- this workgroup's part of the line of all units ------------------------
+    // (less than 2^31 of them: the host chose their size)
+    PagedRequest x = {0, 0, 0, 0, 0, 0};
+    int mine = 0, sum = 0;  // (up to kNT requests: this thread's alone)
     for (int r = tid; r < a.R; r += kNT) {
-        const Share s = share_of(a, paged_request(a, r), BLOCK);
-        mine = (long long)s.items * s.steps;
+        x = paged_request(a, r);
+        const Share s = share_of(a, x, BLOCK);
+        mine = s.items * s.units;
         sum += mine;
     }
-    long long total;
-    long long upto = block_scan<kNT>(sum, &total);
-    const int n_wg = (int)min((long long)a.n_wg, total);
+    int total;
+    int upto = block_scan<kNT>(sum, &total);
+    const int n_wg = min(a.n_wg, total), wg = blockIdx.x;
     if (tid == 0) meta[0] = 0;
-    if ((int)blockIdx.x >= n_wg) return;
-    const long long u0 = total * blockIdx.x / n_wg, u1 = total * (blockIdx.x + 1) / n_wg;
-    long long before = 0;
+    if (wg >= n_wg) return;
+    // the first `more` workgroups have a unit more than the others
+    const int per = (uint32_t)total / (uint32_t)n_wg, more = total - per * n_wg;
+    const int u0 = per * wg + min(wg, more), u1 = u0 + per + (wg < more);
+    int before = 0;
     for (int r0 = 0; r0 < a.R; r0 += kNT) {
-        long long all = total;
+        int all = total;
         if (a.R > kNT) {
             const int r = r0 + tid;
             mine = 0;
             if (r < a.R) {
-                const Share s = share_of(a, paged_request(a, r), BLOCK);
-                mine = (long long)s.items * s.steps;
+                x = paged_request(a, r);
+                const Share s = share_of(a, x, BLOCK);
+                mine = s.items * s.units;
             }
             upto = block_scan<kNT>(mine, &all);
         }
         if (u0 < before + all) {
-            const long long first = before + upto - mine;
+            const int first = before + upto - mine;
             if (u0 >= first && u0 < first + mine) {
                 found[0] = r0 + tid;
                 found[1] = first;
+                found[2] = x.q0;
+                found[3] = x.qn;
+                found[4] = x.pos0;
+                found[5] = x.kv;
+                found[6] = x.lo;
+                found[7] = x.bad;
             }
             break;
         }
         before += all;
     }
     __syncthreads();
-    int r = __builtin_amdgcn_readfirstlane((int)found[0]);
-    long long r_first = found[1];  // of the line, where request r begins
+    int r = uniform(found[0]), r_first = uniform(found[1]);  // request, its first unit
+    x = {uniform(found[2]), uniform(found[3]), uniform(found[4]),
+         uniform(found[5]), uniform(found[6]), uniform(found[7])};
 
-    const int rk = 8 * (l16 >> 2) + (l16 & 3);  // this lane's keys of a step: rk, rk + 4
     const int page_mask = (1 << a.page_log2) - 1;
-    uint16_t* const vt = vtile[wave];
-    for (long long u = u0; u < u1;) {
-        const PagedRequest x = paged_request(a, r);
+    const uint32_t k_lds = lds_address(lds) + wave * L::WAVE, v_lds = k_lds + L::K_BYTES;
+    uint8_t* const k_tile = lds + wave * L::WAVE;
+    uint8_t* const v_tile = k_tile + L::K_BYTES;
+    // this lane's place in a 1 KiB piece, and its source (V: in even and in odd pieces)
+    const int p_row = lane / (D / 8), p_chunk = lane % (D / 8);
+    const int k_off = p_row * (int)a.k.row16 * 16 + (p_chunk ^ L::k_swap(p_row)) * 16;
+    const int v_off0 = p_row * (int)a.v.row16 * 16 + (p_chunk ^ L::v_swap(p_row)) * 16;
+    const int v_off1 =
+        p_row * (int)a.v.row16 * 16 + (p_chunk ^ L::v_swap(p_row + L::PIECE_ROWS)) * 16;
+    // operands: K row l16 (and + 16), piece 4 s + g4; V rows 4 g4 + l16 / 4 (and + 16), column
+    // 16 db + 4 (l16 % 4)
+    const int k_row = (l16 / L::PIECE_ROWS) * L::K_PIECE + (l16 % L::PIECE_ROWS) * (D * 2);
+    constexpr int K_16 = 16 / L::PIECE_ROWS * L::K_PIECE;
+    const int tr_row = 4 * g4 + (l16 >> 2);
+    const int v_row = tr_row * (D * 2) + 8 * (l16 & 1);
+    for (int u = u0; u < u1;) {
         const Share share = share_of(a, x, BLOCK);
-        const long long mine_here = (long long)share.items * share.steps;
+        const int mine_here = share.items * share.units;
         if (u >= r_first + mine_here) {  // the next request that has any
             r_first += mine_here;
             for (++r;; r += 64) {
@@ -170,16 +238,69 @@ __global__ __launch_bounds__(kNT) void paged_rows_kernel(const PagedArgs a) {
                 }
                 if (r + 64 >= a.R) return;  // (never: u1 <= total)
             }
-            r = __builtin_amdgcn_readfirstlane(r);
+            r = uniform(r);
+            x = paged_request(a, r);
             continue;
         }
-        const int item = (int)((u - r_first) / share.steps);
-        const int t0 = (int)(u - r_first - (long long)item * share.steps);
-        const int t1 = (int)min((long long)share.steps, t0 + (u1 - u));
-        const long long item_first = u - t0;  // of the line
-        u += t1 - t0;
-        const int head = item / share.blocks, blk = item - head * share.blocks;
+        const int item = (uint32_t)(u - r_first) / (uint32_t)share.units;
+        const int unit0 = u - r_first - item * share.units;
+        const int unit1 = min(share.units, unit0 + (u1 - u));
+        const int t0 = unit0 << a.unit_log2, t1 = min(share.steps, unit1 << a.unit_log2);
+        const int item_first = u - unit0;  // of the line
+        u += unit1 - unit0;
+        int head = item, blk = 0;
+        if (share.blocks > 1) {
+            head = (uint32_t)item / (uint32_t)share.blocks;
+            blk = item - head * share.blocks;
+        }
         const int n_rows = min(x.qn * a.group - blk * BLOCK, BLOCK);
+
+        // ---- loads of a step: a wave's 32 keys, in aligned runs of eight ------------------
+        const uint16_t* const k_head = a.k.ptr + head * a.k.head;
+        const uint16_t* const v_head = a.v.ptr + head * a.v.head;
+        const int* const table = a.table + (long long)r * a.table_stride;
+        int bad = x.bad;
+        const bool any_keys = x.kv > x.lo;
+        const int key0 = x.lo / kPagedRowKeys * kPagedRowKeys + 32 * wave;
+        // first key of a run, clamped to the runs that hold a key that some row sees
+        auto run_of = [&](int t, int i) __attribute__((always_inline)) {
+            return max(min(key0 + t * kPagedRowKeys + 8 * i, (x.kv - 1) & ~7), x.lo & ~7);
+        };
+        // page numbers of a step's runs, in lanes 0 to 3
+        auto entries = [&](int t) __attribute__((always_inline)) {
+            int e = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                int p = table[run_of(t, i) >> a.page_log2];
+                if ((uint32_t)p >= (uint32_t)a.n_pages) {
+                    p = 0;
+                    bad = 1;
+                }
+                e = lane == i ? p : e;
+            }
+            return e;
+        };
+        auto load = [&](const PagedSide& side, const uint16_t* base, uint32_t dst, int piece,
+                        int off0, int off1, int t, int e) __attribute__((always_inline)) {
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) {
+                const uint64_t at =
+                    (uint64_t)(uint32_t)__builtin_amdgcn_readlane(e, i) * side.page16 +
+                    (uint64_t)(uint32_t)(run_of(t, i) & page_mask) * side.row16;
+                const dma_rsrc_t rsrc = make_dma_rsrc(base + at * 8, 0x7fffffffu);
+                load_past(rsrc, uniform(dst), off0, 0);
+                if constexpr (L::PIECE_ROWS == 4)
+                    load_past(rsrc, uniform(dst + piece), off1, uniform(4 * side.row16 * 16));
+                dst += piece * (8 / L::PIECE_ROWS);
+            }
+        };
+        auto load_k = [&](int t, int e) __attribute__((always_inline)) {
+            load(a.k, k_head, k_lds, L::K_PIECE, k_off, k_off, t, e);
+        };
+        auto load_v = [&](int t, int e) __attribute__((always_inline)) {
+            load(a.v, v_head, v_lds, L::V_PIECE, v_off0, v_off1, t, e);
+        };
+        int entry = 0;
 
         // ---- this lane's queries: Q^T, dims 32 s + 8 g4 .. + 7 of row l16 -----------
         bf16x8 qf[MT][KS];
@@ -188,7 +309,8 @@ __global__ __launch_bounds__(kNT) void paged_rows_kernel(const PagedArgs a) {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             const int row = blk * BLOCK + min(mt * 16 + l16, n_rows - 1);
-            const int tok = row / a.group, h = head * a.group + row - tok * a.group;
+            const int tok = (uint32_t)row / (uint32_t)a.group;
+            const int h = head * a.group + row - tok * a.group;
             const uint16_t* qp = a.q + (x.q0 + tok) * a.q_row + h * a.q_head + 8 * g4;
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
@@ -202,12 +324,10 @@ __global__ __launch_bounds__(kNT) void paged_rows_kernel(const PagedArgs a) {
             slope[mt] = a.slopes ? a.slopes[h] * 1.4426950408889634f : 0.f;
         }
         // keys from here to there are seen by every row
-        const int tok_last = (blk * BLOCK + n_rows - 1) / a.group;
-        const int all_hi = a.causal ? x.pos0 + blk * BLOCK / a.group : x.kv - 1;
+        const int tok_first = (uint32_t)(blk * BLOCK) / (uint32_t)a.group;
+        const int tok_last = (uint32_t)(blk * BLOCK + n_rows - 1) / (uint32_t)a.group;
+        const int all_hi = a.causal ? min(x.pos0 + tok_first, x.kv - 1) : x.kv - 1;
         const int all_lo = a.window ? x.pos0 + tok_last - a.window + 1 : 0;
-        const uint16_t* const kp = a.k.ptr + head * a.k.head + 8 * g4;
-        const uint16_t* const vp = a.v.ptr + head * a.v.head + 8 * g4;
-        const int* const table = a.table + (long long)r * a.table_stride;
 
         float m[MT], l[MT];
         f32x4 oacc[MT][DB];
@@ -218,173 +338,196 @@ __global__ __launch_bounds__(kNT) void paged_rows_kernel(const PagedArgs a) {
 #pragma unroll
             for (int db = 0; db < DB; ++db) oacc[mt][db] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        bool bad = x.bad;
-        const int key0 = x.lo / kPagedRowKeys * kPagedRowKeys + 32 * wave;
-        auto key_of = [&](int kb, int i) { return max(min(kb + i, x.kv - 1), x.lo); };
-        int entry = 0;
-        if (x.kv > x.lo) entry = table[key_of(key0 + t0 * kPagedRowKeys, rk) >> a.page_log2];
-        for (int t = t0; t < t1; ++t) {
+        // One slot to an operand: K's next rows are asked for as soon as its operands are in
+        // registers, V's likewise, so that a wave's 16 KiB are on their way nearly always.  (The
+        // first step's loads are those of a step -1 without work: one copy of the code.)
+        if (any_keys) entry = entries(t0);
+        for (int t = any_keys ? t0 - 1 : t1; t < t1; ++t) {
             const int kb = key0 + t * kPagedRowKeys;
-            int next = 0;
-            if (t + 1 < t1) next = table[key_of(kb + kPagedRowKeys, rk) >> a.page_log2];
-            if (kb < x.kv && kb + 32 > x.lo) {
-                const bool out = (uint32_t)entry >= (uint32_t)a.n_pages;
-                bad |= out;
-                const long long page = out ? 0 : entry;
-                u32x4 kr[2][KS], vr[2][KS];
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const int s0 = key_of(kb, rk + 4 * b) & page_mask;
-                    const uint16_t* const kk = kp + page * a.k.page + s0 * a.k.row;
-                    const uint16_t* const vv = vp + page * a.v.page + s0 * a.v.row;
-#pragma unroll
-                    for (int s = 0; s < KS; ++s) {
-                        kr[b][s] = __builtin_nontemporal_load(
-                            reinterpret_cast<const u32x4*>(kk + 32 * s));
-                        vr[b][s] = __builtin_nontemporal_load(
-                            reinterpret_cast<const u32x4*>(vv + 32 * s));
-                    }
-                }
+            const bool work = t >= t0, more_steps = t + 1 < t1;
+            bf16x8 kf[2][KS];
+            if (work) {
+                wait_loads<LOADS>();  // K's have landed (V's are newer)
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
                     for (int s = 0; s < KS; ++s)
-                        *reinterpret_cast<u32x4*>(vt + (rk + 4 * b) * VST + 32 * s + 8 * g4) =
-                            vr[b][s];
-                bf16x8 pf[MT];
+                        kf[b][s] = *reinterpret_cast<const bf16x8*>(
+                            k_tile + b * K_16 + k_row + (((4 * s + g4) ^ L::k_swap(l16)) * 16));
+                wait_lds();
+            }
+            if (more_steps) load_k(t + 1, entry);
+            f32x4 sa[MT], sb[MT];
+            if (work) {
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    // lane (row l16, g4) gets keys kb + 8 g4 + e, e = 0..7
-                    f32x4 sa = {0.f, 0.f, 0.f, 0.f}, sb = {0.f, 0.f, 0.f, 0.f};
+            for (int mt = 0; mt < MT; ++mt) {
+                sa[mt] = sb[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int s = 0; s < KS; ++s) {
-                        sa = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                            __builtin_bit_cast(bf16x8, kr[0][s]), qf[mt][s], sa, 0, 0, 0);
-                        sb = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                            __builtin_bit_cast(bf16x8, kr[1][s]), qf[mt][s], sb, 0, 0, 0);
-                    }
-                    float sc[8];
+                for (int s = 0; s < KS; ++s) {
+                    sa[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[0][s], qf[mt][s], sa[mt],
+                                                                    0, 0, 0);
+                    sb[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[1][s], qf[mt][s], sb[mt],
+                                                                    0, 0, 0);
+                }
+            }
+            bf16x8 pf[MT];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        sc[i] = sa[i];
-                        sc[4 + i] = sb[i];
-                    }
-                    // log2 units; tanh y = 1 - 2 / (1 + e^2y)
-                    if (a.cap_out != 0.f) {
+            for (int mt = 0; mt < MT; ++mt) {
+                // lane (row l16, g4) has keys kb + 4 g4 + e and, from e = 4 on, 12 further
+                float sc[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const float w = __builtin_amdgcn_exp2f(sc[e] * a.cap_in);
-                            sc[e] = fmaf(-2.f * a.cap_out, __builtin_amdgcn_rcpf(1.f + w),
-                                         a.cap_out);
-                        }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) sc[e] *= a.scale_log2;
-                    }
-                    const int kl = kb + 8 * g4;
-                    if (a.slopes) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            sc[e] = fmaf(-slope[mt], (float)abs(pos[mt] - (kl + e)), sc[e]);
-                    }
-                    if (kb + 31 > all_hi || kb < all_lo) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (kl + e > hi[mt] || kl + e < lo[mt]) sc[e] = -INFINITY;
-                    }
-                    float mx = sc[0];
-#pragma unroll
-                    for (int e = 1; e < 8; ++e) mx = fmaxf(mx, sc[e]);
-                    mx = rows4_max(mx);
-                    const float m_new = fmaxf(m[mt], mx);
-                    const float ref = m_new == -INFINITY ? 0.f : m_new;  // no key seen yet
-                    const float alpha = __builtin_amdgcn_exp2f(m[mt] - ref);
-                    l[mt] *= alpha;
-#pragma unroll
-                    for (int db = 0; db < DB; ++db) oacc[mt][db] *= alpha;
-                    m[mt] = m_new;
-                    // P is rounded to bf16 (2^-9 of each weight) as the operand it has to be; its
-                    // sum takes the weights as they are, so that the log-sum-exp is fp32's
+                for (int i = 0; i < 4; ++i) {
+                    sc[i] = sa[mt][i];
+                    sc[4 + i] = sb[mt][i];
+                }
+                // log2 units; tanh y = 1 - 2 / (1 + e^2y)
+                if (a.cap_out != 0.f) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const float p = __builtin_amdgcn_exp2f(sc[e] - ref);
-                        l[mt] += p;
-                        pf[mt][e] = (__bf16)p;
+                        const float w = __builtin_amdgcn_exp2f(sc[e] * a.cap_in);
+                        sc[e] = fmaf(-2.f * a.cap_out, __builtin_amdgcn_rcpf(1.f + w), a.cap_out);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sc[e] *= a.scale_log2;
+                }
+                const int kl = kb + 4 * g4;
+                if (a.slopes) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        sc[e] = fmaf(-slope[mt], (float)abs(pos[mt] - (kl + 12 * (e / 4) + e)),
+                                     sc[e]);
+                }
+                if (kb + 31 > all_hi || kb < all_lo) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int key = kl + 12 * (e / 4) + e;
+                        if (key > hi[mt] || key < lo[mt]) sc[e] = -INFINITY;
                     }
                 }
-                // O^T += V^T P^T: lane (i, g) of a 16-lane group reads row 8 g + i / 4 (and
-                // + 4) at column 16 db + 4 (i % 4) and receives column 16 db + i of keys
-                // 8 g .. 8 g + 3 (and 8 g + 4 .. 8 g + 7)
-                const uint16_t* const vs = vt + (8 * g4 + (l16 >> 2)) * VST + 4 * (l16 & 3);
+                float mx = sc[0];
+#pragma unroll
+                for (int e = 1; e < 8; ++e) mx = fmaxf(mx, sc[e]);
+                mx = rows4_max(mx);
+                const float m_new = fmaxf(m[mt], mx);
+                const float ref = m_new == -INFINITY ? 0.f : m_new;  // no key seen yet
+                const float alpha = __builtin_amdgcn_exp2f(m[mt] - ref);
+                l[mt] *= alpha;
+#pragma unroll
+                for (int db = 0; db < DB; ++db) oacc[mt][db] *= alpha;
+                m[mt] = m_new;
+                // P is rounded to bf16 (at most 2^-8 of each weight) as the operand it has to
+                // be; its sum takes the weights as they are, so that the log-sum-exp is fp32's
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float p = __builtin_amdgcn_exp2f(sc[e] - ref);
+                    l[mt] += p;
+                    pf[mt][e] = (__bf16)p;
+                }
+            }
+                // O^T += V^T P^T, 16 columns at a time: lane i of 16 reads 4 values of row i / 4 of
+                // four, and receives column i of these four keys
+                if (more_steps)
+                    wait_loads<LOADS>();  // V's have landed (K's next are newer)
+                else
+                    wait_loads<0>();
+                if (kb < x.lo || kb + 32 > x.kv) {
+                    // rows that no query sees hold what the page does: weights of 0 need numbers
+#pragma unroll 1
+                    for (int p = 0; p < L::PIECES; ++p) {
+                        const int key = kb + p * L::PIECE_ROWS + p_row;
+                        if (key < x.lo || key >= x.kv)
+                            *reinterpret_cast<u32x4*>(v_tile + p * L::V_PIECE + lane * 16) =
+                                u32x4{0u, 0u, 0u, 0u};
+                    }
+                    wait_lds();
+                }
+                bf16x8 vf[DB];
 #pragma unroll
                 for (int db = 0; db < DB; ++db) {
+                    const int chunk = 2 * db + ((l16 >> 1) & 1);
+                    const uint8_t* const at = v_tile + v_row + (chunk ^ L::v_swap(tr_row)) * 16;
                     const s16x4 w0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (__attribute__((address_space(3))) s16x4*)(vs + 16 * db));
+                        (__attribute__((address_space(3))) s16x4*)(at));
                     const s16x4 w1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (__attribute__((address_space(3))) s16x4*)(vs + 4 * VST + 16 * db));
+                        (__attribute__((address_space(3))) s16x4*)(at + 16 * D * 2));
                     const s16x8 w = {w0[0], w0[1], w0[2], w0[3], w1[0], w1[1], w1[2], w1[3]};
+                    vf[db] = __builtin_bit_cast(bf16x8, w);
+                }
+                wait_lds();
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt)
                         oacc[mt][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                            __builtin_bit_cast(bf16x8, w), pf[mt], oacc[mt][db], 0, 0, 0);
-                }
+                            vf[db], pf[mt], oacc[mt][db], 0, 0, 0);
             }
-            entry = next;
+            if (more_steps) {
+                load_v(t + 1, entry);
+                entry = entries(min(t + 2, t1 - 1));
+            }
         }
 
         // ---- the waves meet, 16 rows at a time -----------------------------------
         bad = __syncthreads_or(bad);
-        const bool whole = t0 == 0 && t1 == share.steps;
-        const int part = t0 == 0 ? 1 : 0;
-        if (!whole && tid == 0 && t0 == 0) {  // the first part of an item: its others follow
-            const int last =
-                (int)(((item_first + share.steps) * n_wg - 1) / total);  // who has its last step
+        const bool whole = unit0 == 0 && unit1 == share.units;
+        const int part = unit0 == 0 ? 1 : 0;
+        if (!whole && tid == 0 && unit0 == 0) {  // the first part of an item: its others follow
+            const int end = item_first + share.units - 1;  // its last unit, and whose it is
+            const int big = more * (per + 1);
+            const int last = end < big ? (uint32_t)end / (uint32_t)(per + 1)
+                                       : more + (uint32_t)(end - big) / (uint32_t)per;
             meta[1] = x.q0;
             meta[2] = head * a.group;
             meta[3] = blk * BLOCK;
             meta[4] = n_rows;
-            meta[0] = last - (int)blockIdx.x + 1;
+            meta[0] = last - wg + 1;
         }
-        float* const so = reinterpret_cast<float*>(&vtile[0][0]);  // [wave][16][OST]
+        // (addresses from an opaque copy of the thread's number: else they are computed before
+        // the loop and kept in registers through it)
+        int etid = tid;
+        asm volatile("" : "+v"(etid));
+        const int e16 = etid & 15, eg4 = (etid >> 4) & 3;
+        float* const so = reinterpret_cast<float*>(lds);  // [wave][16][OST]
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             if (mt > 0) __syncthreads();
             const float lsum = rows4_sum(l[mt]);  // the lane groups have different keys
-            if (g4 == 0) {
-                sm[wave][mt * 16 + l16] = m[mt];
-                sl[wave][mt * 16 + l16] = bad ? NAN : lsum;
+            if (eg4 == 0) {
+                sm[wave][mt * 16 + e16] = m[mt];
+                sl[wave][mt * 16 + e16] = bad ? NAN : lsum;
             }
 #pragma unroll
             for (int db = 0; db < DB; ++db)
-                *reinterpret_cast<f32x4*>(so + (wave * 16 + l16) * OST + 16 * db + 4 * g4) =
+                *reinterpret_cast<f32x4*>(so + (wave * 16 + e16) * OST + 16 * db + 4 * eg4) =
                     oacc[mt][db];
             __syncthreads();
-            for (int i = tid; i < 16 * D / 4; i += kNT) {
+            for (int i = etid; i < 16 * D / 4; i += kNT) {
                 const int row = mt * 16 + i / (D / 4), col = i % (D / 4) * 4;
                 if (row >= n_rows) break;
                 float M = sm[0][row];
 #pragma unroll
                 for (int w = 1; w < kNW; ++w) M = fmaxf(M, sm[w][row]);
                 const float ref = M == -INFINITY ? 0.f : M;
-                float L = 0.f;
+                float L0 = 0.f;
                 f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int w = 0; w < kNW; ++w) {
                     const float wt = __builtin_amdgcn_exp2f(sm[w][row] - ref);
-                    L = fmaf(wt, sl[w][row], L);
-                    acc += wt * *reinterpret_cast<const f32x4*>(so + (w * 16 + row - mt * 16) * OST +
-                                                                col);
+                    L0 = fmaf(wt, sl[w][row], L0);
+                    acc += wt * *reinterpret_cast<const f32x4*>(
+                                    so + (w * 16 + row - mt * 16) * OST + col);
                 }
                 if (whole) {
-                    const int rr = blk * BLOCK + row, tok = rr / a.group;
+                    const int rr = blk * BLOCK + row, tok = (uint32_t)rr / (uint32_t)a.group;
                     store_row<D>(a, x.q0 + tok, head * a.group + rr - tok * a.group, col, acc, M,
-                                 L);
+                                 L0);
                 } else {
-                    const long long at = ((long long)blockIdx.x * 2 + part) * BLOCK + row;
+                    const long long at = ((long long)wg * 2 + part) * BLOCK + row;
                     *reinterpret_cast<f32x4*>(a.ws_o + at * D + col) = acc;
                     if (col == 0) {
                         a.ws_m[at] = M;
-                        a.ws_l[at] = L;
+                        a.ws_l[at] = L0;
                     }
                 }
             }
@@ -393,44 +536,88 @@ __global__ __launch_bounds__(kNT) void paged_rows_kernel(const PagedArgs a) {
     }
 }
 
-// Adds parts of rows: workgroup (g, y) those of rows y * ROWS .. of the item g.  After the row
+// Adds parts of rows: workgroup (g, y) those of rows 2 y and 2 y + 1 of item g.  After the row
 // kernel (TILES false) item g is the one that begins in its workgroup g and does not end there:
 // its first part is that workgroup's second one, the others are the following workgroups' first.
 // After the tile kernel item g is a block of a head, its splits one behind another.
+//
+// Bound by latency: the parts were just written by other CUs.  The lane groups of a row take
+// every GP-th part, four on their way, and meet in LDS.
+constexpr int kSumRows = 2;
 template <int D, bool TILES>
 __global__ __launch_bounds__(kNT) void paged_sum_kernel(const PagedArgs a, int block) {
-    constexpr int LANES = D / 4, ROWS = kNT / LANES;
-    const int* const meta = (TILES ? a.tile_meta : a.meta) + (long long)blockIdx.x * kPagedMeta;
+    constexpr int LANES = D / 4, GROUPS = kNT / LANES, GP = GROUPS / kSumRows, U = 4;
+    const int4* const meta = reinterpret_cast<const int4*>(TILES ? a.tile_meta : a.meta) +
+                             (long long)blockIdx.x * (kPagedMeta / 4);
     const float* const ws_m = TILES ? a.tile_m : a.ws_m;
     const float* const ws_l = TILES ? a.tile_l : a.ws_l;
     const float* const ws_o = TILES ? a.tile_o : a.ws_o;
-    const int n = meta[0];
-    const int row = blockIdx.y * ROWS + threadIdx.x / LANES, col = threadIdx.x % LANES * 4;
-    if (n == 0 || row >= meta[4]) return;
+    const int4 item = meta[0];
+    const int n_rows = meta[1].x, n = item.x;
+    if (n == 0 || (int)blockIdx.y * kSumRows >= n_rows) return;
+    const int grp = threadIdx.x / LANES, lane = threadIdx.x % LANES, col = lane * 4;
+    const int row = min((int)blockIdx.y * kSumRows + grp / GP, n_rows - 1);
     auto at = [&](int i) {  // part i
         const long long part = TILES ? (long long)blockIdx.x * a.splits + i
                                      : ((long long)blockIdx.x + i) * 2 + (i == 0);
         return part * block + row;
     };
-    float M = -INFINITY;
-    for (int i = 0; i < n; ++i) M = fmaxf(M, ws_m[at(i)]);
-    const float ref = M == -INFINITY ? 0.f : M;
-    float L = 0.f;
+    float M = -INFINITY, L = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < n; ++i) {
-        const float w = __builtin_amdgcn_exp2f(ws_m[at(i)] - ref);
-        L = fmaf(w, ws_l[at(i)], L);
-        acc += w * *reinterpret_cast<const f32x4*>(ws_o + at(i) * D + col);
+    for (int i0 = grp % GP; i0 < n; i0 += U * GP) {
+        float m[U], l[U];
+        f32x4 o[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {  // (past the end the last part's, unused)
+            const long long p = at(min(i0 + u * GP, n - 1));
+            m[u] = ws_m[p];
+            l[u] = ws_l[p];
+            o[u] = *reinterpret_cast<const f32x4*>(ws_o + p * D + col);
+        }
+        float top = M;
+#pragma unroll
+        for (int u = 0; u < U; ++u) top = i0 + u * GP < n ? fmaxf(top, m[u]) : top;
+        const float ref = top == -INFINITY ? 0.f : top;
+        const float w0 = __builtin_amdgcn_exp2f(M - ref);
+        L *= w0;
+        acc *= w0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i0 + u * GP >= n) break;
+            const float w = __builtin_amdgcn_exp2f(m[u] - ref);
+            L = fmaf(w, l[u], L);
+            acc += w * o[u];
+        }
+        M = top;
     }
-    const int rr = meta[3] + row, tok = rr / a.group;
-    store_row<D>(a, meta[1] + tok, meta[2] + rr - tok * a.group, col, acc, M, L);
+    __shared__ f32x4 so[GROUPS][LANES];
+    __shared__ float sm[GROUPS], sl[GROUPS];
+    so[grp][lane] = acc;
+    if (lane == 0) {
+        sm[grp] = M;
+        sl[grp] = L;
+    }
+    __syncthreads();
+    if (grp % GP != 0 || (int)blockIdx.y * kSumRows + grp / GP >= n_rows) return;
+#pragma unroll
+    for (int q = 1; q < GP; ++q) M = fmaxf(M, sm[grp + q]);
+    const float ref = M == -INFINITY ? 0.f : M;
+    L = 0.f;
+    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int q = 0; q < GP; ++q) {
+        const float w = __builtin_amdgcn_exp2f(sm[grp + q] - ref);
+        L = fmaf(w, sl[grp + q], L);
+        acc += w * so[grp + q][lane];
+    }
+    const int rr = item.w + row, tok = rr / a.group;
+    store_row<D>(a, item.y + tok, item.z + rr - tok * a.group, col, acc, M, L);
 }
 
 template <int D, bool TILES>
 hipError_t launch_sum(const PagedArgs& a, int items, int block, hipStream_t stream) {
-    constexpr int rows = kNT / (D / 4);
-    hipLaunchKernelGGL((paged_sum_kernel<D, TILES>), dim3(items, (block + rows - 1) / rows),
-                       dim3(kNT), 0, stream, a, block);
+    hipLaunchKernelGGL((paged_sum_kernel<D, TILES>), dim3(items, block / kSumRows), dim3(kNT), 0,
+                       stream, a, block);
     return hipGetLastError();
 }
 

@@ -64,7 +64,7 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
     constexpr int RUN_PIECES = 8 / L::PIECE_ROWS;       // instructions to a run
     constexpr int STAGE = NW * kFwdStageWaveBytes;
     __shared__ __attribute__((aligned(16))) uint8_t lds[L::BYTES > STAGE ? L::BYTES : STAGE];
-    __shared__ long long found[2];
+    __shared__ int found[2];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -75,9 +75,9 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
     const int nth = unit / a.splits, split = unit - nth * a.splits;
     int* const meta = a.tile_meta + ((long long)nth * a.Hkv + head) * kPagedMeta;
     const int r = paged_find<NT>(
-        a, nth, found, [&](const PagedRequest& x) __attribute__((always_inline)) -> long long {
+        a, nth, found, [&](const PagedRequest& x) __attribute__((always_inline)) -> int {
             const long long rows = (long long)x.qn * a.group;
-            return rows > a.few ? (rows + BM - 1) / BM : 0;
+            return rows > a.few ? (int)((uint32_t)(rows + BM - 1) / BM) : 0;
         });
     if (r < 0) {  // there are fewer blocks
         if (a.splits > 1 && split == 0 && tid == 0) meta[0] = 0;
@@ -85,7 +85,7 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
     }
     const PagedRequest x = paged_request(a, r);
     const int n_blocks = (x.qn * a.group + BM - 1) / BM;
-    const int blk = n_blocks - 1 - (int)(nth - found[1]);
+    const int blk = n_blocks - 1 - (nth - found[1]);
     const int n_rows = min(x.qn * a.group - blk * BM, BM);
 
     // ---- its rows and keys -------------------------------------------------------
@@ -138,11 +138,11 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
     constexpr int KS0 = 0, KS1 = L::K_TILE, VS0 = 2 * L::K_TILE, VS1 = VS0 + L::V_TILE;
     const uint16_t* const k_head = a.k.ptr + head * a.k.head;
     const uint16_t* const v_head = a.v.ptr + head * a.v.head;
-    bool bad = x.bad;
+    bool bad = x.bad != 0;
     // this lane's place in a 1 KiB piece, and its source inside the run's first piece
     const int p_row = lane / (D / 8), p_chunk = lane % (D / 8);
-    const int k_off = (int)(p_row * a.k.row * 2) + (p_chunk ^ L::k_swap(p_row)) * 16;
-    const int v_off = (int)(p_row * a.v.row * 2) + (p_chunk ^ L::v_swap(p_row)) * 16;
+    const int k_off = p_row * (int)a.k.row16 * 16 + (p_chunk ^ L::k_swap(p_row)) * 16;
+    const int v_off = p_row * (int)a.v.row16 * 16 + (p_chunk ^ L::v_swap(p_row)) * 16;
     const int last_key = x.kv - 1;
     // the run of eight keys that the wave brings as its i-th of tile t: first key, clamped to
     // runs that hold a key that some row sees
@@ -162,10 +162,10 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
             const int key0 = run_of(t, i);
             const bool out = (uint32_t)entry[i] >= (uint32_t)a.n_pages;
             bad |= out;
-            const long long page = out ? 0 : entry[i];
-            const uint16_t* const at = (IS_K ? k_head : v_head) + page * side.page +
-                                       (key0 & page_mask) * side.row;
-            const dma_rsrc_t rsrc = make_dma_rsrc(at, 0x7fffffffu);
+            const uint32_t page = out ? 0 : entry[i];
+            const uint64_t at = (uint64_t)page * side.page16 +
+                                (uint64_t)(uint32_t)(key0 & page_mask) * side.row16;
+            const dma_rsrc_t rsrc = make_dma_rsrc((IS_K ? k_head : v_head) + at * 8, 0x7fffffffu);
             const int piece0 = (wave * RUNS + i) * RUN_PIECES;
             auto pieces = [&](auto edge_tag) __attribute__((always_inline)) {
 #pragma unroll
@@ -173,12 +173,12 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
                     const uint32_t dst = lds_base + slot +
                                          (piece0 + p) * (IS_K ? L::K_PIECE : L::V_PIECE);
                     int off = IS_K ? k_off : v_off;
-                    int soff = p * L::PIECE_ROWS * (int)side.row * 2;
+                    int soff = p * L::PIECE_ROWS * (int)side.row16 * 16;
                     if constexpr (decltype(edge_tag)::value) {
                         // keys that no row sees are copies of the nearest that one does
                         const int rr = p * L::PIECE_ROWS + p_row;
                         const int key = max(min(key0 + rr, last_key), x.lo) - key0;
-                        off = key * (int)side.row * 2 +
+                        off = key * (int)side.row16 * 16 +
                               (p_chunk ^ (IS_K ? L::k_swap(p_row) : L::v_swap(p_row))) * 16;
                         soff = 0;
                     }

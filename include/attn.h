@@ -526,7 +526,8 @@ int attn_paged(const attn_heads* q, const attn_heads* k_pages, const attn_heads*
                size_t workspace_bytes);
 
 /* Bytes of workspace attn_paged needs (needs the device), or a negative ATTN_E* code. */
-long long attn_paged_workspace_bytes(int T, int R, int Hq, int Hkv, int d, int max_q);
+long long attn_paged_workspace_bytes(int T, int R, int max_q, int Hq, int Hkv, int d,
+                                     int page_size, int max_pages, int window);
 
 #ifdef __cplusplus
 }

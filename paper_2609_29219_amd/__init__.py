@@ -155,7 +155,7 @@ def _load() -> ctypes.CDLL:
     lib.attn_paged_store.argtypes = [vp] * 5 + [ci] * 5
     lib.attn_paged.argtypes = [vp] * 6 + [ll, vp, vp, vp] + [ci] * 9 + [cf, cf, ci, ci, ci, vp,
                                                                        ctypes.c_size_t]
-    lib.attn_paged_workspace_bytes.argtypes = [ci] * 6
+    lib.attn_paged_workspace_bytes.argtypes = [ci] * 9
     lib.attn_paged_workspace_bytes.restype = ctypes.c_longlong
     for fn in (lib.attn__bwd_packed, lib.attn__qk_norm_rope_packed,
                lib.attn__qk_norm_rope_bwd_packed, lib.attn__paged_extend_packed,
@@ -803,10 +803,10 @@ def attn_paged(q, k_pages, v_pages, block_table, kv_lens, cu_seqlens=None, max_q
     return (o, lse) if return_lse else o
 
 
-def paged_workspace_bytes(T: int, R: int, Hq: int, Hkv: int, d: int,
-                          max_q: int | None = None) -> int:
+def paged_workspace_bytes(T: int, R: int, Hq: int, Hkv: int, d: int, page_size: int,
+                          max_pages: int, max_q: int | None = None, window: int = 0) -> int:
     """Bytes of workspace attn_paged needs with a caller-provided buffer."""
-    n = lib.attn_paged_workspace_bytes(T, R, Hq, Hkv, d, max_q or 0)
+    n = lib.attn_paged_workspace_bytes(T, R, max_q or 0, Hq, Hkv, d, page_size, max_pages, window)
     if n < 0:
         raise AttnError(int(n), last_error())
     return int(n)

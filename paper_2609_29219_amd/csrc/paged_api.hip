@@ -97,7 +97,8 @@ struct PagedLaunch {
     }
 };
 
-PagedLaunch paged_launch(int T, int R, int Hq, int Hkv, int d, int max_q, int num_cus) {
+PagedLaunch paged_launch(int T, int R, int Hq, int Hkv, int d, int max_q, long long max_keys,
+                         int window, int num_cus) {
     PagedLaunch l;
     const int group = Hq / Hkv;
     const long long rows = (long long)T * group;
@@ -112,14 +113,22 @@ PagedLaunch paged_launch(int T, int R, int Hq, int Hkv, int d, int max_q, int nu
     if (tiles) {
         l.waves = most <= 128 ? 4 : 8;
         const long long requests = l.few ? std::min<long long>(R, rows / (l.few + 1)) : R;
-        l.items = (rows / (32 * l.waves) + requests) * Hkv;
-        // Rounds that the workgroups take, times the length of one, with a few tiles' time for
-        // the start, the end and the partial results of each split.
-        const long long at_once = (long long)num_cus * 8 / l.waves;
+        // (all but one row of a block each may be missing from the requests' last blocks)
+        l.items = (rows + requests * (32 * l.waves - 1)) / (32 * l.waves) * Hkv;
+        // The keys are split where that is faster by this estimate, in us on this card: rounds
+        // of workgroups, each with 6 us of start and end and 2 to a tile, then 4 us and the
+        // partial results' traffic.  (Requests as long as their table or their window allows, up
+        // to 16384, every other one with rows for a block of its own; what the device finds may
+        // need fewer splits, and the others end at once.)
+        const double at_once = num_cus * 8 / l.waves;
+        const double items = ((double)rows / (32 * l.waves) + (requests > 1 ? requests / 2 : 0)) * Hkv;
+        double keys = std::min(16384.0, (double)max_keys);
+        if (window) keys = std::min(keys, window + 32.0 * l.waves / group);
         double best = 0;
-        for (int s = 1; s <= kPagedMaxSplits && (s == 1 || l.items * s <= 4 * at_once); ++s) {
-            const double t = (double)((l.items * s + at_once - 1) / at_once) * (1.0 / s + 0.02);
-            if (s == 1 || t < 0.95 * best) {
+        for (int s = 1; s <= kPagedMaxSplits && (s == 1 || items * s <= 4 * at_once); ++s) {
+            double t = ceil(items * s / at_once) * (6 + 2 * keys / 64 / s);
+            if (s > 1) t += 4 + items * s * 32 * l.waves * d * 4 / 5e6;
+            if (s == 1 || t < best) {
                 best = t;
                 l.splits = s;
             }
@@ -266,14 +275,22 @@ int attn_paged_store(const attn_heads* k, const attn_heads* v, const int* slots,
     });
 }
 
-long long attn_paged_workspace_bytes(int T, int R, int Hq, int Hkv, int d, int max_q) {
+long long attn_paged_workspace_bytes(int T, int R, int max_q, int Hq, int Hkv, int d,
+                                     int page_size, int max_pages, int window) {
     return host::guarded([&]() -> long long {
-        int rc = validate_paged_dims(T, R, Hq, Hkv, d, max_q);
+        int log2 = 0;
+        int rc = page_log2(page_size, &log2);
+        if (!rc) rc = validate_paged_dims(T, R, Hq, Hkv, d, max_q);
+        if (!rc && (max_pages <= 0 || window < 0))
+            rc = host::fail(ATTN_EINVAL, "max_pages (%d) must be positive, window (%d) not negative",
+                            max_pages, window);
         if (rc) return rc;
         host::DeviceRef dev;
         rc = host::device(&dev);
         if (rc) return rc;
-        return (long long)paged_launch(T, R, Hq, Hkv, d, max_q, dev.desc->num_cus).bytes(d);
+        return (long long)paged_launch(T, R, Hq, Hkv, d, max_q, (long long)max_pages << log2, window,
+                                       dev.desc->num_cus)
+            .bytes(d);
     });
 }
 
@@ -322,7 +339,8 @@ int attn_paged(const attn_heads* q, const attn_heads* k_pages, const attn_heads*
         rc = host::check_apart(results, n_results, operands, n_operands);
         if (!rc) rc = host::device(&dev);
         if (rc) return rc;
-        const PagedLaunch l = paged_launch(T, R, Hq, Hkv, d, max_q, dev.desc->num_cus);
+        const PagedLaunch l = paged_launch(T, R, Hq, Hkv, d, max_q, (long long)max_pages * page_size,
+                                           window, dev.desc->num_cus);
         const size_t need = l.bytes(d);
         if (l.items * l.splits * 2 > kMaxWorkgroups)
             return host::fail(ATTN_EUNSUPPORTED, "more workgroups than one launch holds");

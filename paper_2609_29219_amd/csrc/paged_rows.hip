@@ -536,17 +536,20 @@ __global__ __launch_bounds__(kNT, 2) void paged_rows_kernel(const PagedArgs a) {
     }
 }
 
-// Adds parts of rows: workgroup (g, y) those of rows 2 y and 2 y + 1 of item g.  After the row
+// Adds parts of rows: workgroup (g, y) those of ROWS rows of item g.  After the row
 // kernel (TILES false) item g is the one that begins in its workgroup g and does not end there:
 // its first part is that workgroup's second one, the others are the following workgroups' first.
 // After the tile kernel item g is a block of a head, its splits one behind another.
 //
-// Bound by latency: the parts were just written by other CUs.  The lane groups of a row take
-// every GP-th part, four on their way, and meet in LDS.
-constexpr int kSumRows = 2;
+// Bound by latency after the row kernel: few rows of many parts, just written by other CUs.  The
+// lane groups of a row take every GP-th part, four on their way, and meet in LDS.  After the tile
+// kernel there are many rows of few parts (bound: HBM), and each lane group has its own.
+template <int D, bool TILES>
+constexpr int kSumRows = TILES ? kNT / (D / 4) : 2;
 template <int D, bool TILES>
 __global__ __launch_bounds__(kNT) void paged_sum_kernel(const PagedArgs a, int block) {
-    constexpr int LANES = D / 4, GROUPS = kNT / LANES, GP = GROUPS / kSumRows, U = 4;
+    constexpr int ROWS = kSumRows<D, TILES>;
+    constexpr int LANES = D / 4, GROUPS = kNT / LANES, GP = GROUPS / ROWS, U = 4;
     const int4* const meta = reinterpret_cast<const int4*>(TILES ? a.tile_meta : a.meta) +
                              (long long)blockIdx.x * (kPagedMeta / 4);
     const float* const ws_m = TILES ? a.tile_m : a.ws_m;
@@ -554,9 +557,9 @@ __global__ __launch_bounds__(kNT) void paged_sum_kernel(const PagedArgs a, int b
     const float* const ws_o = TILES ? a.tile_o : a.ws_o;
     const int4 item = meta[0];
     const int n_rows = meta[1].x, n = item.x;
-    if (n == 0 || (int)blockIdx.y * kSumRows >= n_rows) return;
+    if (n == 0 || (int)blockIdx.y * ROWS >= n_rows) return;
     const int grp = threadIdx.x / LANES, lane = threadIdx.x % LANES, col = lane * 4;
-    const int row = min((int)blockIdx.y * kSumRows + grp / GP, n_rows - 1);
+    const int row = min((int)blockIdx.y * ROWS + grp / GP, n_rows - 1);
     auto at = [&](int i) {  // part i
         const long long part = TILES ? (long long)blockIdx.x * a.splits + i
                                      : ((long long)blockIdx.x + i) * 2 + (i == 0);
@@ -590,33 +593,36 @@ __global__ __launch_bounds__(kNT) void paged_sum_kernel(const PagedArgs a, int b
         }
         M = top;
     }
-    __shared__ f32x4 so[GROUPS][LANES];
-    __shared__ float sm[GROUPS], sl[GROUPS];
-    so[grp][lane] = acc;
-    if (lane == 0) {
-        sm[grp] = M;
-        sl[grp] = L;
-    }
-    __syncthreads();
-    if (grp % GP != 0 || (int)blockIdx.y * kSumRows + grp / GP >= n_rows) return;
+    if constexpr (GP > 1) {
+        __shared__ f32x4 so[GROUPS][LANES];
+        __shared__ float sm[GROUPS], sl[GROUPS];
+        so[grp][lane] = acc;
+        if (lane == 0) {
+            sm[grp] = M;
+            sl[grp] = L;
+        }
+        __syncthreads();
+        if (grp % GP != 0) return;
 #pragma unroll
-    for (int q = 1; q < GP; ++q) M = fmaxf(M, sm[grp + q]);
-    const float ref = M == -INFINITY ? 0.f : M;
-    L = 0.f;
-    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int q = 1; q < GP; ++q) M = fmaxf(M, sm[grp + q]);
+        const float ref = M == -INFINITY ? 0.f : M;
+        L = 0.f;
+        acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int q = 0; q < GP; ++q) {
-        const float w = __builtin_amdgcn_exp2f(sm[grp + q] - ref);
-        L = fmaf(w, sl[grp + q], L);
-        acc += w * so[grp + q][lane];
+        for (int q = 0; q < GP; ++q) {
+            const float w = __builtin_amdgcn_exp2f(sm[grp + q] - ref);
+            L = fmaf(w, sl[grp + q], L);
+            acc += w * so[grp + q][lane];
+        }
     }
+    if ((int)blockIdx.y * ROWS + grp / GP >= n_rows) return;
     const int rr = item.w + row, tok = rr / a.group;
     store_row<D>(a, item.y + tok, item.z + rr - tok * a.group, col, acc, M, L);
 }
 
 template <int D, bool TILES>
 hipError_t launch_sum(const PagedArgs& a, int items, int block, hipStream_t stream) {
-    hipLaunchKernelGGL((paged_sum_kernel<D, TILES>), dim3(items, block / kSumRows), dim3(kNT), 0,
+    hipLaunchKernelGGL((paged_sum_kernel<D, TILES>), dim3(items, block / kSumRows<D, TILES>), dim3(kNT), 0,
                        stream, a, block);
     return hipGetLastError();
 }

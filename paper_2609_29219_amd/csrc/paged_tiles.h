@@ -14,8 +14,9 @@
 // between them; while it does, the next tiles come from memory straight into LDS (two slots to
 // an operand, one barrier to a tile).
 //
-// Pages.  A wave brings aligned runs of eight keys, which lie in one page: the page number is a
-// scalar, and so is all arithmetic on it; a lane's offset inside the run never changes.  Tiles
+// Pages.  A wave brings aligned runs of 16 keys, which lie in one page (or two of eight rows): the
+// page number is a scalar, and so is all arithmetic on it; a lane's offset inside the run never
+// changes.  Tiles
 // lie in LDS as whole rows, 1 KiB to an instruction, their 16-byte pieces exchanged inside a row
 // (by the source address of each lane) so that both kinds of reads are free of bank conflicts:
 // K is read 16 rows at a time, V four rows of 64 bytes.
@@ -54,14 +55,17 @@ struct PagedLds {
     }
 };
 
-// FORM: 1 capped scores, 2 slopes
-template <int D, int NW, int FORM>
+// FORM: 1 capped scores, 2 slopes.  MSUM: the rows' sums are the matrix cores', of the weights as
+// rounded to bf16 (a product with a 0/1 operand that leaves each lane its own row's, as in
+// fwd_kernel.h): 32 additions a tile less beside the products.  For calls without a log-sum-exp,
+// whose sums have to be of the weights as they are.
+template <int D, int NW, int FORM, bool MSUM>
 __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs a) {
     using L = PagedLds<D>;
     constexpr int NT = NW * 64, BM = NW * 32, BN = kTileKeys;
     constexpr int KD = D / 16, KB = BN / 32, CB = D / 32;
-    constexpr int RUNS = 8 / NW;                        // runs of eight keys to a wave and tile
-    constexpr int RUN_PIECES = 8 / L::PIECE_ROWS;       // instructions to a run
+    constexpr int JOBS = 8 / NW;                        // of 16 rows, to a wave and tile
+    constexpr int JOB_PIECES = 16 / L::PIECE_ROWS;      // instructions to a job
     constexpr int STAGE = NW * kFwdStageWaveBytes;
     __shared__ __attribute__((aligned(16))) uint8_t lds[L::BYTES > STAGE ? L::BYTES : STAGE];
     __shared__ int found[2];
@@ -132,70 +136,108 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
     const float slope = (FORM & 2) ? a.slopes[qh] * 1.4426950408889634f : 0.f;
 
     // ---- tile loads ------------------------------------------------------------
+    // A tile's 64 rows of K and of V are eight jobs of 16 rows.  Of eight waves the first four
+    // bring K's, the others V's, so that each has one page to find for a tile (with pages of
+    // eight rows two); of four waves each has a job of either.
     const int* const table = a.table + (long long)r * a.table_stride;
     const int page_mask = (1 << a.page_log2) - 1;
+    const bool small_pages = a.page_log2 == 3;
     const uint32_t lds_base = lds_address(lds);
     constexpr int KS0 = 0, KS1 = L::K_TILE, VS0 = 2 * L::K_TILE, VS1 = VS0 + L::V_TILE;
-    const uint16_t* const k_head = a.k.ptr + head * a.k.head;
-    const uint16_t* const v_head = a.v.ptr + head * a.v.head;
     bool bad = x.bad != 0;
-    // this lane's place in a 1 KiB piece, and its source inside the run's first piece
-    const int p_row = lane / (D / 8), p_chunk = lane % (D / 8);
-    const int k_off = p_row * (int)a.k.row16 * 16 + (p_chunk ^ L::k_swap(p_row)) * 16;
-    const int v_off = p_row * (int)a.v.row16 * 16 + (p_chunk ^ L::v_swap(p_row)) * 16;
+    const int p_row = lane / (D / 8), p_chunk = lane % (D / 8);  // this lane's place in 1 KiB
     const int last_key = x.kv - 1;
-    // the run of eight keys that the wave brings as its i-th of tile t: first key, clamped to
-    // runs that hold a key that some row sees
-    auto run_of = [&](int t, int i) __attribute__((always_inline)) {
-        return max(min(t * BN + 8 * (wave * RUNS + i), last_key & ~7), x.lo & ~7);
+    struct Job {
+        const uint16_t* base;       // head's first row
+        uint32_t page16, row16;
+        int ahead;                  // tiles from the one at work to the one that is loaded
+        int first, slot0, slot1, piece;
+        int swap, off;              // this lane's source in the job's first piece
+        int entry0, entry1;         // page numbers of the next tile that is loaded
+    } job[JOBS];
+#pragma unroll
+    for (int i = 0; i < JOBS; ++i) {
+        const bool is_k = JOBS == 2 ? i == 0 : wave < 4;
+        const PagedSide& side = is_k ? a.k : a.v;
+        Job& b = job[i];
+        b.base = side.ptr + head * side.head;
+        b.page16 = side.page16;
+        b.row16 = side.row16;
+        b.ahead = is_k ? 2 : 1;
+        b.first = 16 * (wave & 3);
+        b.piece = is_k ? L::K_PIECE : L::V_PIECE;
+        b.slot0 = (is_k ? KS0 : VS0) + b.first / L::PIECE_ROWS * b.piece;
+        b.slot1 = b.slot0 + (is_k ? L::K_TILE : L::V_TILE);
+        b.swap = p_chunk ^ (is_k ? L::k_swap(p_row) : L::v_swap(p_row));
+        b.off = p_row * (int)side.row16 * 16 + b.swap * 16;
+        b.entry0 = b.entry1 = 0;
+    }
+    // first key of `n` (8 or 16) aligned ones, clamped to those that hold a key that some row sees
+    auto run_of = [&](const Job& b, int t, int at, int n) __attribute__((always_inline)) {
+        return max(min(t * BN + b.first + at, last_key & ~(n - 1)), x.lo & ~(n - 1));
     };
-    auto entry_of = [&](int t, int i) __attribute__((always_inline)) {
-        return table[run_of(t, i) >> a.page_log2];
+    // (as vector loads, which land with the tiles' before the barrier: scalar ones would hold up
+    // the tile's first reads from LDS, which are waited for by the same count)
+    int zero;
+    asm volatile("v_mov_b32 %0, 0" : "=v"(zero));
+    auto read_entries = [&](Job& b, int t) __attribute__((always_inline)) {
+        if (small_pages) {
+            b.entry0 = table[(run_of(b, t, 0, 8) >> 3) + zero];
+            b.entry1 = table[(run_of(b, t, 8, 8) >> 3) + zero];
+        } else {
+            b.entry0 = table[(run_of(b, t, 0, 16) >> a.page_log2) + zero];
+        }
     };
-    auto dma = [&](auto is_k_tag, int t, const int (&entry)[RUNS], int slot)
+    // Rows of tile t from piece p0 to p1 of the job, which lie in page `entry` from key0 on.
+    auto bring_run = [&](const Job& b, int t, int key0, int entry, auto p0c, auto p1c, int slot)
         __attribute__((always_inline)) {
-        constexpr bool IS_K = decltype(is_k_tag)::value;
-        const PagedSide& side = IS_K ? a.k : a.v;
-        const bool edge = t * BN < x.lo || t * BN + BN > x.kv;
+        constexpr int p0 = decltype(p0c)::value, p1 = decltype(p1c)::value;
+        const bool out = (uint32_t)entry >= (uint32_t)a.n_pages;
+        bad |= out;
+        const uint64_t at = (uint64_t)(uint32_t)(out ? 0 : entry) * b.page16 +
+                            (uint64_t)(uint32_t)(key0 & page_mask) * b.row16;
+        const dma_rsrc_t rsrc = make_dma_rsrc(b.base + at * 8, 0x7fffffffu);
+        if (t * BN < x.lo || t * BN + BN > x.kv) {
+            // keys that no row sees are copies of the nearest that one does
+#pragma unroll 1
+            for (int p = 0; p < p1 - p0; ++p) {
+                const int rr = p * L::PIECE_ROWS + p_row;
+                const int from = max(min(key0 + rr, last_key), x.lo) - key0;
+                lds_dma16(rsrc, lds_base + slot + (p0 + p) * b.piece,
+                          from * (int)b.row16 * 16 + b.swap * 16, 0);
+            }
+        } else {
 #pragma unroll
-        for (int i = 0; i < RUNS; ++i) {
-            const int key0 = run_of(t, i);
-            const bool out = (uint32_t)entry[i] >= (uint32_t)a.n_pages;
-            bad |= out;
-            const uint32_t page = out ? 0 : entry[i];
-            const uint64_t at = (uint64_t)page * side.page16 +
-                                (uint64_t)(uint32_t)(key0 & page_mask) * side.row16;
-            const dma_rsrc_t rsrc = make_dma_rsrc((IS_K ? k_head : v_head) + at * 8, 0x7fffffffu);
-            const int piece0 = (wave * RUNS + i) * RUN_PIECES;
-            auto pieces = [&](auto edge_tag) __attribute__((always_inline)) {
-#pragma unroll
-                for (int p = 0; p < RUN_PIECES; ++p) {
-                    const uint32_t dst = lds_base + slot +
-                                         (piece0 + p) * (IS_K ? L::K_PIECE : L::V_PIECE);
-                    int off = IS_K ? k_off : v_off;
-                    int soff = p * L::PIECE_ROWS * (int)side.row16 * 16;
-                    if constexpr (decltype(edge_tag)::value) {
-                        // keys that no row sees are copies of the nearest that one does
-                        const int rr = p * L::PIECE_ROWS + p_row;
-                        const int key = max(min(key0 + rr, last_key), x.lo) - key0;
-                        off = key * (int)side.row16 * 16 +
-                              (p_chunk ^ (IS_K ? L::k_swap(p_row) : L::v_swap(p_row))) * 16;
-                        soff = 0;
-                    }
-                    lds_dma16(rsrc, dst, off, soff);
-                }
-            };
-            if (edge)
-                pieces(std::true_type{});
-            else
-                pieces(std::false_type{});
+            for (int p = p0; p < p1; ++p)
+                lds_dma16(rsrc, lds_base + slot + p * b.piece, b.off,
+                          (p - p0) * L::PIECE_ROWS * (int)b.row16 * 16);
+        }
+    };
+    auto bring_job = [&](const Job& b, int t, int slot) __attribute__((always_inline)) {
+        using std::integral_constant;
+        auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+        integral_constant<int, 0> none;
+        integral_constant<int, JOB_PIECES / 2> half;
+        integral_constant<int, JOB_PIECES> all;
+        if (small_pages) {
+            bring_run(b, t, run_of(b, t, 0, 8), uniform(b.entry0), none, half, slot);
+            bring_run(b, t, run_of(b, t, 8, 8), uniform(b.entry1), half, all, slot);
+        } else {
+            bring_run(b, t, run_of(b, t, 0, 16), uniform(b.entry0), none, all, slot);
         }
     };
 
     // ---- online softmax, one row to a lane ------------------------------------
     float m_i = -INFINITY;  // reference of the row's weights, log2 units
     float l_i = 0.f;        // their sum (this lane's half of the keys), unrounded: the
-                            // log-sum-exp is fp32's
+                            // log-sum-exp is fp32's; or
+    f32x4 lsum = {0.f, 0.f, 0.f, 0.f};  // with MSUM, in all four registers
+    bf16x8 sel;
+    if constexpr (MSUM) {
+        const __bf16 v = ((lane >> 4) & 1) == ((lane >> 2) & 1) ? (__bf16)1.0f : (__bf16)0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sel[e] = v;
+    }
     f32x16 oacc[CB];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
@@ -204,27 +246,26 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
     const float scale_log2 = a.scale_log2;
 
     // K operands: lane reads row l32 of a 32-row block, 16-byte piece 2 ks + hh
-    const int k_row = (l32 / L::PIECE_ROWS) * L::K_PIECE + (l32 % L::PIECE_ROWS) * (D * 2);
-    const int k_swap = L::k_swap(l32) * 16;
-    auto k_addr = [&](int ks) __attribute__((always_inline)) {
-        return k_row + (((2 * ks + hh) * 16) ^ k_swap);
-    };
+    const uint8_t* k_at[KD];
+#pragma unroll
+    for (int ks = 0; ks < KD; ++ks)
+        k_at[ks] = lds + (l32 / L::PIECE_ROWS) * L::K_PIECE + (l32 % L::PIECE_ROWS) * (D * 2) +
+                   (((2 * ks + hh) ^ L::k_swap(l32)) * 16);
     constexpr int K_BLOCK = 32 / L::PIECE_ROWS * L::K_PIECE;  // bytes of 32 rows
     // V operands: lane i of 16 reads row i / 4 of four, at column 16 ((lane / 16) % 2) + 4 (i % 4)
-    // of 32
+    // of 32 (the rows' numbers are i / 4 more than multiples of 4)
     const int tr_row = (lane & 15) >> 2;
-    const int v_row = tr_row * (D * 2) + ((lane >> 4) & 1) * 32 + 8 * (lane & 3);
-    auto v_addr = [&](int cb) __attribute__((always_inline)) {
-        // (the rows' numbers are tr_row more than multiples of 4)
-        return v_row + ((cb * 64) ^ (L::v_swap(tr_row) * 16));
-    };
-
+    const uint8_t* v_at[CB];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+        v_at[cb] = lds + (4 * hh + tr_row) * (D * 2) + ((cb * 64) ^ (L::v_swap(tr_row) * 16)) +
+                   ((lane >> 4) & 1) * 32 + 8 * (lane & 3);
     auto fetch_k = [&](int kslot, int kb, int ks) __attribute__((always_inline)) -> bf16x8 {
-        return *reinterpret_cast<const bf16x8*>(lds + kslot + kb * K_BLOCK + k_addr(ks));
+        return *reinterpret_cast<const bf16x8*>(k_at[ks] + kslot + kb * K_BLOCK);
     };
     auto fetch_v = [&](int vslot, int kb, int h2, int cb) __attribute__((always_inline)) -> bf16x8 {
         const uint16_t* const p = reinterpret_cast<const uint16_t*>(
-            lds + vslot + (kb * 32 + 16 * h2 + 4 * hh) * (D * 2) + v_addr(cb));
+            v_at[cb] + vslot + (kb * 32 + 16 * h2) * (D * 2));
         const s16x4 w0 = lds_read_tr(p), w1 = lds_read_tr(p + 8 * D);
         const s16x8 w = {w0[0], w0[1], w0[2], w0[3], w1[0], w1[1], w1[2], w1[3]};
         return __builtin_bit_cast(bf16x8, w);
@@ -253,7 +294,10 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
         if (__any(move)) {
             const float m_new = move ? tmax : m_i;
             const float alpha = move ? __builtin_amdgcn_exp2f(m_i - m_new) : 1.f;
-            l_i *= alpha;
+            if constexpr (MSUM)
+                lsum *= alpha;
+            else
+                l_i *= alpha;
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
@@ -269,12 +313,14 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
     // One tile t: the products of S(t + 1) into s_nxt (HAS_S) and of PV(t), one by one; between
     // them the weights of tile t (scores s_cur) and, once S(t + 1) is there, its finished scores
     // and their maximum, which is returned.
-    auto fused_tile = [&](int kslot, int vslot, const f32x16 (&s_cur)[KB], f32x16 (&s_nxt)[KB],
+    auto fused_tile = [&](auto odd_tag, const f32x16 (&s_cur)[KB], f32x16 (&s_nxt)[KB],
                           int t, float m_ref, auto has_s_tag, auto mask_tag)
         __attribute__((always_inline)) -> float {
-        constexpr bool HAS_S = decltype(has_s_tag)::value;
+        constexpr bool HAS_S = decltype(has_s_tag)::value, ODD = decltype(odd_tag)::value;
+        constexpr int kslot = ODD ? KS0 : KS1, vslot = ODD ? VS1 : VS0;  // of tiles t + 1 and t
         constexpr int NS = HAS_S ? KB * KD : 0, NPV = KB * 2 * CB, NM = NS + NPV;
-        constexpr int PF = 2;                               // operands on their way
+        constexpr int PF = NW == 8 ? 3 : 2;  // operands on their way, and in use (with four waves, each
+                                             // with two jobs of loads, a third one spills)
         constexpr int NPAIR = KB * 8;
         constexpr int EXP_SLOTS = HAS_S ? NS + NPV / 2 : 0;  // slots with exponentials
         constexpr int MAX0 = EXP_SLOTS + 1;                  // first slot with the next maximum
@@ -295,8 +341,10 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
             const bf16x2 pk = {(__bf16)xe[pp][0], (__bf16)xe[pp][1]};
             pb[kb][h2][e] = pk[0];
             pb[kb][h2][e + 1] = pk[1];
-            rs0 += xe[pp][0];
-            rs1 += xe[pp][1];
+            if constexpr (!MSUM) {
+                rs0 += xe[pp][0];
+                rs1 += xe[pp][1];
+            }
         };
         if (!HAS_S) {
 #pragma unroll
@@ -308,12 +356,6 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
         const int key1 = (t + 1) * BN + 4 * hh;
         const int room = hi - key1, below = lo - key1;
         const float away = (float)(pos - key1);
-        if (HAS_S) {
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s_nxt[kb][e] = 0.f;
-        }
         auto fetch = [&](auto ic) __attribute__((always_inline)) -> bf16x8 {
             constexpr int i = decltype(ic)::value;
             if constexpr (i < NS) {
@@ -325,7 +367,9 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
         };
         __builtin_amdgcn_sched_barrier(0);
         bf16x8 fr[PF];
-        fr[0] = fetch(std::integral_constant<int, 0>{});
+        static_for<0, PF - 1>([&](auto ic) __attribute__((always_inline)) {
+            fr[decltype(ic)::value] = fetch(ic);
+        });
         static_for<0, NM>([&](auto ic) __attribute__((always_inline)) {
             constexpr int i = decltype(ic)::value;
             const bf16x8 op = fr[i % PF];
@@ -333,11 +377,15 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
                 fr[(i + PF - 1) % PF] = fetch(std::integral_constant<int, i + PF - 1>{});
             if constexpr (i < NS) {
                 constexpr int ks = i / KB, kb = i % KB;
-                s_nxt[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, qf[ks], s_nxt[kb], 0, 0, 0);
+                f32x16 c = {};
+                if constexpr (ks > 0) c = s_nxt[kb];
+                s_nxt[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, qf[ks], c, 0, 0, 0);
             } else {
                 constexpr int j = i - NS, kb = j / (2 * CB), h2 = (j / CB) % 2, cb = j % CB;
                 oacc[cb] =
                     __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, pb[kb][h2], oacc[cb], 0, 0, 0);
+                if constexpr (MSUM && cb == 0)
+                    lsum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sel, pb[kb][h2], lsum, 0, 0, 0);
             }
             if constexpr (HAS_S) {
                 static_for<0, NPAIR>([&](auto pc) __attribute__((always_inline)) {
@@ -355,35 +403,32 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
                         mx = __builtin_elementwise_maximum(mx, s_nxt[kb][e]);
                     }
                 });
-                asm volatile("" : "+v"(rs0), "+v"(rs1), "+v"(mx));
+                if constexpr (MSUM) asm volatile("" : "+v"(mx));
+                if constexpr (!MSUM) asm volatile("" : "+v"(rs0), "+v"(rs1), "+v"(mx));
             }
             __builtin_amdgcn_sched_barrier(0);
         });
-        l_i += rs0 + rs1;
+        if constexpr (!MSUM) l_i += rs0 + rs1;
         return HAS_S ? half_swap_max(mx) : -INFINITY;
     };
 
     // ---- the loop ------------------------------------------------------------------
     // While iteration t runs, LDS holds K(t + 1) and V(t), and K(t + 2) and V(t + 1) come in:
     // tile j in slot (j - t_begin) % 2.  Page numbers are read an iteration ahead.
-    constexpr std::true_type is_k{};
-    constexpr std::false_type is_v{};
-    int e_v[RUNS], e_k[RUNS], e_next[RUNS];  // of tiles t + 1, t + 2, t + 3
-    auto entries = [&](int t, int (&e)[RUNS]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < RUNS; ++i) e[i] = entry_of(min(t, t_end - 1), i);
-    };
     f32x16 sA[KB], sB[KB];
     float mx_next = -INFINITY;
     const bool has_keys = t_end > t_begin;
     if (has_keys) {
-        int e0[RUNS];
-        entries(t_begin, e0);
-        entries(t_begin + 1, e_v);
-        entries(t_begin + 2, e_k);
-        dma(is_k, t_begin, e0, KS0);
-        dma(is_v, t_begin, e0, VS0);
-        if (t_begin + 1 < t_end) dma(is_k, t_begin + 1, e_v, KS1);
+#pragma unroll
+        for (int i = 0; i < JOBS; ++i) {
+            read_entries(job[i], t_begin);
+            bring_job(job[i], t_begin, job[i].slot0);
+            read_entries(job[i], min(t_begin + 1, t_end - 1));
+            if (job[i].ahead == 2) {
+                if (t_begin + 1 < t_end) bring_job(job[i], t_begin + 1, job[i].slot1);
+                read_entries(job[i], min(t_begin + 2, t_end - 1));
+            }
+        }
         publish_barrier<0>();
         if (t_last >= t_begin) {
 #pragma unroll
@@ -410,53 +455,56 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
     }
     // loads of iteration t
     auto bring = [&](int t, bool odd) __attribute__((always_inline)) {
-        entries(t + 3, e_next);
-        if (t + 2 < t_end) dma(is_k, t + 2, e_k, odd ? KS1 : KS0);
-        if (t + 1 < t_end) dma(is_v, t + 1, e_v, odd ? VS0 : VS1);
 #pragma unroll
-        for (int i = 0; i < RUNS; ++i) {
-            e_v[i] = e_k[i];
-            e_k[i] = e_next[i];
+        for (int i = 0; i < JOBS; ++i) {
+            Job& b = job[i];
+            const int to = t + b.ahead;
+            if (to < t_end) bring_job(b, to, (b.ahead == 2) == odd ? b.slot1 : b.slot0);
+            read_entries(b, min(to + 1, t_end - 1));
         }
     };
-    auto iter = [&](int t, const f32x16 (&s_cur)[KB], f32x16 (&s_nxt)[KB], auto mask_tag)
-        __attribute__((always_inline)) {
-        const bool odd = (t - t_begin) & 1;
-        bring(t, odd);
+    // Iteration t of a wave: scores of an even tile (from t_begin) are in set A, of an odd one in
+    // set B, so that slots and sets are known at compile time.
+    auto iter = [&](auto odd_tag, int t, const f32x16 (&s_cur)[KB], f32x16 (&s_nxt)[KB],
+                    auto mask_tag) __attribute__((always_inline)) {
+        bring(t, decltype(odd_tag)::value);
         const float m_ref = update_ref(mx_next);
-        mx_next = fused_tile(odd ? KS0 : KS1, odd ? VS1 : VS0, s_cur, s_nxt, t, m_ref,
-                             std::true_type{}, mask_tag);
+        mx_next = fused_tile(odd_tag, s_cur, s_nxt, t, m_ref, std::true_type{}, mask_tag);
         publish_barrier<0>();
     };
-    // Iterations [t0, t1); the scores begin, and end, in set A.
+    // Iterations [t0, t1), t0 being even (from t_begin).
     auto run = [&](int t0, int t1, auto mask_tag) __attribute__((always_inline)) {
+#pragma unroll 1
         for (int t = t0; t < t1; t += 2) {
-            iter(t, sA, sB, mask_tag);
-            if (t + 1 < t1) iter(t + 1, sB, sA, mask_tag);
-        }
-        if (t1 > t0 && ((t1 - t0) & 1)) {
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb) sA[kb] = sB[kb];
+            iter(std::false_type{}, t, sA, sB, mask_tag);
+            if (t + 1 < t1) iter(std::true_type{}, t + 1, sB, sA, mask_tag);
         }
     };
+    auto last_iter = [&](auto odd_tag, const f32x16 (&s_cur)[KB], f32x16 (&s_nxt)[KB])
+        __attribute__((always_inline)) {
+        bring(t_last, decltype(odd_tag)::value);
+        const float m_ref = update_ref(mx_next);
+        fused_tile(odd_tag, s_cur, s_nxt, t_last, m_ref, std::false_type{}, std::true_type{});
+        publish_barrier<0>();
+    };
     if (t_last >= t_begin) {
-        // iteration t finishes tile t + 1: masked where the window begins, not in between,
-        // masked at the diagonal and at the end
+        // iteration t finishes tile t + 1: masked where the window begins, not in between (an
+        // even number of tiles from an even one), masked at the diagonal and at the end
         const int first_free = max(w_lo_max + BN - 1, 0) / BN;
         const int first_masked = max(w_hi_min + 1, 0) / BN;
-        const int s1 = min(max(first_free - 1, t_begin), t_last);
-        const int s2 = min(max(first_masked - 1, s1), t_last);
+        int s1 = max(first_free - 1, t_begin);
+        s1 = min(s1 + ((s1 - t_begin) & 1), t_last);
+        int s2 = min(max(first_masked - 1, s1), t_last);
+        s2 = max(s2 - ((s2 - t_begin) & 1), s1);
 #pragma unroll 1
         for (int pass = 0; pass < 2; ++pass) {
             run(pass ? s2 : t_begin, pass ? t_last : s1, std::true_type{});
             if (pass == 0) run(s1, s2, std::false_type{});
         }
-        const bool odd = (t_last - t_begin) & 1;
-        bring(t_last, odd);
-        const float m_ref = update_ref(mx_next);
-        fused_tile(odd ? KS0 : KS1, odd ? VS1 : VS0, sA, sB, t_last, m_ref, std::false_type{},
-                   std::true_type{});
-        publish_barrier<0>();
+        if ((t_last - t_begin) & 1)
+            last_iter(std::true_type{}, sB, sA);
+        else
+            last_iter(std::false_type{}, sA, sB);
     }
     for (int t = max(t_last + 1, t_begin); t < t_end; ++t) {
         bring(t, (t - t_begin) & 1);
@@ -465,7 +513,7 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
 
     // ---- epilogue: O = O^T / l, through LDS so that stores are whole lines ---------------
     bad = __syncthreads_or(bad);
-    const float l_row = bad ? NAN : half_swap_sum(l_i);
+    const float l_row = bad ? NAN : MSUM ? lsum[0] : half_swap_sum(l_i);
     const bool partial = n_splits > 1;
     const float inv = partial ? 1.f : l_row == 0.f ? 0.f : 1.f / l_row;
     const bool out16 = a.out_bf16 && !partial;
@@ -539,11 +587,23 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
     }
 }
 
-template <int D, int NW, int FORM>
+template <int D, int NW, int FORM, bool MSUM>
 hipError_t launch_paged_tiles_form(const PagedArgs& a, hipStream_t stream) {
-    hipLaunchKernelGGL((paged_tiles_kernel<D, NW, FORM>), dim3((unsigned)a.tile_wgs), dim3(NW * 64),
-                       0, stream, a);
+    hipLaunchKernelGGL((paged_tiles_kernel<D, NW, FORM, MSUM>), dim3((unsigned)a.tile_wgs),
+                       dim3(NW * 64), 0, stream, a);
     return hipGetLastError();
+}
+
+// (the sums are a small part of the other forms' work beside the products)
+template <int D, int NW>
+hipError_t launch_paged_tiles_d(const PagedArgs& a, int form, hipStream_t stream) {
+    if (form == 0)
+        return a.lse ? launch_paged_tiles_form<D, NW, 0, false>(a, stream)
+                     : launch_paged_tiles_form<D, NW, 0, true>(a, stream);
+    if (form == 1) return launch_paged_tiles_form<D, NW, 1, false>(a, stream);
+    if (form == 2) return launch_paged_tiles_form<D, NW, 2, false>(a, stream);
+    if (form == 3) return launch_paged_tiles_form<D, NW, 3, false>(a, stream);
+    return hipErrorInvalidValue;
 }
 
 }  // namespace attn

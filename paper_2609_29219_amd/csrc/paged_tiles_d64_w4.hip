@@ -4,11 +4,7 @@
 namespace attn {
 
 hipError_t launch_paged_tiles_d64_w4(const PagedArgs& a, int form, hipStream_t stream) {
-    if (form == 0) return launch_paged_tiles_form<64, 4, 0>(a, stream);
-    if (form == 1) return launch_paged_tiles_form<64, 4, 1>(a, stream);
-    if (form == 2) return launch_paged_tiles_form<64, 4, 2>(a, stream);
-    if (form == 3) return launch_paged_tiles_form<64, 4, 3>(a, stream);
-    return hipErrorInvalidValue;
+    return launch_paged_tiles_d<64, 4>(a, form, stream);
 }
 
 }  // namespace attn

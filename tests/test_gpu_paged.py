@@ -246,7 +246,7 @@ def test_large_scores(pa):
 def test_caller_workspace(pa):
     announce("attn_paged workspace")
     s = scene([(1, 3000), (200, 1500), (5, 77)], 16, 4, 128, 16)
-    n = pa.paged_workspace_bytes(206, 3, 16, 4, 128)
+    n = pa.paged_workspace_bytes(206, 3, 16, 4, 128, 16, s["table"].shape[1])
     ws = torch.empty(n, dtype=torch.uint8, device=DEV)
     want = call(pa, s)
     got = call(pa, s, workspace=ws)

@@ -137,9 +137,11 @@ def test_attn_paged_rejects_on_host(kw, code):
     assert pa.last_error() != ""
 
 
-@pytest.mark.parametrize("args", [(0, 1, 2, 1, 64, 0), (1, 0, 2, 1, 64, 0), (1, 1, 3, 2, 64, 0),
-                                  (1, 1, 2, 1, 96, 0), (1, 1, 2, 1, 64, -1),
-                                  (1 << 30, 1, 2, 1, 64, 0)])
+@pytest.mark.parametrize("args", [(0, 1, 0, 2, 1, 64, 16, 4, 0), (1, 0, 0, 2, 1, 64, 16, 4, 0),
+                                  (1, 1, 0, 3, 2, 64, 16, 4, 0), (1, 1, 0, 2, 1, 96, 16, 4, 0),
+                                  (1, 1, -1, 2, 1, 64, 16, 4, 0), (1, 1, 0, 2, 1, 64, 12, 4, 0),
+                                  (1, 1, 0, 2, 1, 64, 16, 0, 0), (1, 1, 0, 2, 1, 64, 16, 4, -1),
+                                  (1 << 30, 1, 0, 2, 1, 64, 16, 4, 0)])
 def test_workspace_query_rejects_on_host(args):
     assert pa.lib.attn_paged_workspace_bytes(*args) < 0
     assert pa.last_error() != ""

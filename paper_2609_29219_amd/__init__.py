@@ -611,42 +611,54 @@ _STORE_CALL = struct.Struct("16qQQ5i")
 _PAGED_CALL = struct.Struct("12q3Qq6Q12i2f")
 
 
+try:
+    from torch import bfloat16 as _BF16, float32 as _F32, int32 as _I32
+except ImportError:
+    _BF16 = _F32 = _I32 = None
+
+
 def _ints(t, shape, name, dev) -> int:
     """Address of an int32 tensor, checked."""
-    import torch
-    _require_on(t, torch.int32, shape, name, dev)
+    if getattr(t, "dtype", None) is _I32 and t.get_device() == dev and t.shape == shape and \
+            t.is_contiguous():
+        return t.data_ptr()
+    _require_on(t, _I32, shape, name, dev)
     return t.data_ptr()
 
 
-def _new_ints(out, n, name, like, dev):
-    """A result of n int32 (the given one, checked)."""
-    import torch
-    if out is None:
-        return torch.empty(n, dtype=torch.int32, device=like.device)
-    _require_on(out, torch.int32, (n,), name, dev)
+def _new_ints(given, sizes, names, like, dev):
+    """Int32 results of the given sizes: those given, checked, and the others from one new
+    tensor."""
+    if all(t is None for t in given):
+        return like.new_empty(sum(sizes)).split_with_sizes(sizes)
+    out = []
+    for t, n, name in zip(given, sizes, names):
+        if t is None:
+            t = like.new_empty(n)
+        else:
+            _require_on(t, _I32, (n,), name, dev)
+        out.append(t)
     return out
 
 
 def _block_table(table, R):
     """Device, address, row stride and pages to a row of a block table of R rows."""
-    import torch
-    if not isinstance(table, torch.Tensor) or table.dtype is not torch.int32 or not table.is_cuda:
+    if getattr(table, "dtype", None) is not _I32 or not table.is_cuda:
         raise TypeError("block_table must be an int32 tensor on a HIP device")
     if table.dim() != 2 or (R is not None and table.shape[0] != R):
         raise ValueError(f"block_table has shape {tuple(table.shape)}, expected "
                          f"({'R' if R is None else R}, max_pages)")
-    if table.stride(1) != 1 and table.shape[1] > 1:
+    stride, one = table.stride()
+    if one != 1 and table.shape[1] > 1:
         raise ValueError("block_table must be contiguous in its last dimension")
-    return table.get_device(), table.data_ptr(), table.stride(0), table.shape[1]
+    return table.get_device(), table.data_ptr(), stride, table.shape[1]
 
 
 def _list(free_pages, dev):
     """Address and length of a list of free pages."""
-    import torch
-    if not isinstance(free_pages, torch.Tensor) or free_pages.dim() != 1:
-        raise TypeError("free_pages must be a one-dimensional tensor")
-    _require_on(free_pages, torch.int32, free_pages.shape, "free_pages", dev)
-    return free_pages.data_ptr(), free_pages.shape[0]
+    if getattr(free_pages, "dtype", None) is not _I32 or free_pages.dim() != 1:
+        raise TypeError("free_pages must be a one-dimensional int32 tensor")
+    return _ints(free_pages, free_pages.shape, "free_pages", dev), free_pages.shape[0]
 
 
 def paged_extend(block_table, seq_lens, new_lens, free_pages, n_free, page_size: int,
@@ -670,11 +682,9 @@ def paged_extend(block_table, seq_lens, new_lens, free_pages, n_free, page_size:
     seq_ptr, new_ptr = _ints(seq_lens, (R,), "seq_lens", dev), _ints(new_lens, (R,), "new_lens", dev)
     list_ptr, list_len = _list(free_pages, dev)
     free_ptr = _ints(n_free, (1,), "n_free", dev)
-    slots = _new_ints(slots, n_tokens, "slots", block_table, dev)
-    positions = _new_ints(positions, n_tokens, "positions", block_table, dev)
-    cu_seqlens = _new_ints(cu_seqlens, R + 1, "cu_seqlens", block_table, dev)
-    kv_lens = _new_ints(kv_lens, R, "kv_lens", block_table, dev)
-    n_left = _new_ints(n_left, 1, "n_left", block_table, dev)
+    slots, positions, cu_seqlens, kv_lens, n_left = _new_ints(
+        (slots, positions, cu_seqlens, kv_lens, n_left), (n_tokens, n_tokens, R + 1, R, 1),
+        ("slots", "positions", "cu_seqlens", "kv_lens", "n_left"), block_table, dev)
     _call_on(dev, lib.attn__paged_extend_packed, _EXTEND_CALL.pack(
         table_ptr, stride, seq_ptr, new_ptr, list_ptr, free_ptr, slots.data_ptr(),
         positions.data_ptr(), cu_seqlens.data_ptr(), kv_lens.data_ptr(), n_left.data_ptr(),
@@ -695,7 +705,7 @@ def paged_release(block_table, seq_lens, keep_lens, free_pages, n_free, page_siz
                                                                       dev)
     list_ptr, list_len = _list(free_pages, dev)
     free_ptr = _ints(n_free, (1,), "n_free", dev)
-    n_left = _new_ints(n_left, 1, "n_left", block_table, dev)
+    n_left, = _new_ints((n_left,), (1,), ("n_left",), block_table, dev)
     _call_on(dev, lib.attn__paged_release_packed, _RELEASE_CALL.pack(
         table_ptr, stride, seq_ptr, keep_ptr, list_ptr, free_ptr, n_left.data_ptr(),
         _raw_stream(dev), list_len, R, max_pages, page_size))
@@ -704,9 +714,8 @@ def paged_release(block_table, seq_lens, keep_lens, free_pages, n_free, page_siz
 
 def _packed_rows(t, name, dev=None):
     """Shape, device and fields of attn_heads for [T,H,d], any strides with contiguous rows."""
-    import torch
-    if not isinstance(t, torch.Tensor) or t.dtype is not torch.bfloat16 or not t.is_cuda:
-        raise TypeError(f"{name} must be a {torch.bfloat16} tensor on a HIP device")
+    if getattr(t, "dtype", None) is not _BF16 or not t.is_cuda:
+        raise TypeError(f"{name} must be a torch.bfloat16 tensor on a HIP device")
     if t.dim() != 3:
         raise ValueError(f"{name} must be [T,H,d]")
     row, head, one = t.stride()
@@ -717,14 +726,14 @@ def _packed_rows(t, name, dev=None):
 
 def _cache_pages(k_pages, v_pages, Hkv, d, dev):
     """Pages, page size and fields of attn_heads of both sides of a cache."""
-    import torch
-    if not isinstance(k_pages, torch.Tensor) or k_pages.dim() != 4:
+    if len(getattr(k_pages, "shape", ())) != 4:
         raise ValueError("k_pages must be [P,Hkv,page_size,d]")
     n_pages, heads, page_size, _ = k_pages.shape
-    shape = (n_pages, heads if Hkv is None else Hkv, page_size, d)
-    k = _head_major(k_pages, torch.bfloat16, shape, "k_pages", dev)
-    return shape[1], n_pages, page_size, k, _head_major(v_pages, torch.bfloat16, shape, "v_pages",
-                                                        dev)
+    if Hkv is None:
+        Hkv = heads
+    shape = (n_pages, Hkv, page_size, d)
+    k = _head_major(k_pages, _BF16, shape, "k_pages", dev)
+    return Hkv, n_pages, page_size, k, _head_major(v_pages, _BF16, shape, "v_pages", dev)
 
 
 def paged_store(k, v, slots, k_pages, v_pages) -> None:
@@ -761,7 +770,6 @@ def attn_paged(q, k_pages, v_pages, block_table, kv_lens, cu_seqlens=None, max_q
     by slopes[h] for every position of distance.  A token that sees no key has o = 0, lse = -inf;
     rows of q behind the last request's are left as they were.  workspace: None (the library's),
     or a device tensor of at least paged_workspace_bytes(...) bytes."""
-    import torch
     (T, Hq, d), dev, q_in = _packed_rows(q, "q")
     Hkv, n_pages, page_size, k_in, v_in = _cache_pages(k_pages, v_pages, None, d, dev)
     if kv_lens.dim() != 1:
@@ -778,17 +786,17 @@ def attn_paged(q, k_pages, v_pages, block_table, kv_lens, cu_seqlens=None, max_q
         raise ValueError(f"{T} tokens of {R} requests without cu_seqlens")
     slopes_ptr = 0
     if slopes is not None:
-        _require_on(slopes, torch.float32, (Hq,), "slopes", dev)
+        _require_on(slopes, _F32, (Hq,), "slopes", dev)
         slopes_ptr = slopes.data_ptr()
     if out_dtype is None:
-        out_dtype = o.dtype if o is not None else torch.float32
-    if out_dtype not in (torch.float32, torch.bfloat16):
+        out_dtype = o.dtype if o is not None else _F32
+    if out_dtype not in (_F32, _BF16):
         raise ValueError("out_dtype must be torch.float32 or torch.bfloat16")
     if o is None:
-        o = torch.empty((T, Hq, d), dtype=out_dtype, device=q.device)
+        o = q.new_empty((T, Hq, d), dtype=out_dtype)
     else:
         _require_on(o, out_dtype, (T, Hq, d), "o", dev)
-    lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device) if return_lse else None
+    lse = q.new_empty((T, Hq), dtype=_F32) if return_lse else None
     if scale is None:
         scale = 1.0 / math.sqrt(d)
     if max_q is None:
@@ -799,7 +807,7 @@ def attn_paged(q, k_pages, v_pages, block_table, kv_lens, cu_seqlens=None, max_q
         *q_in, *k_in, *v_in, o.data_ptr(), 0 if lse is None else lse.data_ptr(), table_ptr, stride,
         kv_ptr, cu_ptr, slopes_ptr, *_workspace(workspace, dev), _raw_stream(dev), T, R, max_q, Hq,
         Hkv, d, n_pages, page_size, max_pages, window, 1 if causal else 0,
-        ATTN_OUT_BF16 if out_dtype is torch.bfloat16 else 0, scale, softcap))
+        ATTN_OUT_BF16 if out_dtype is _BF16 else 0, scale, softcap))
     return (o, lse) if return_lse else o
 
 

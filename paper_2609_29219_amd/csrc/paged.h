@@ -56,6 +56,7 @@ struct PagedArgs {
     const int *kv_lens, *cu;  // cu null: token r is request r's
     const float* slopes;      // [Hq] or null
     int T, R, Hq, Hkv, group;
+    uint32_t group_inverse;   // 2^32 / group, rounded up (group at most kPagedMaxGroup)
     int n_pages, page_log2, max_pages;
     int causal, window;       // window 0: none
     int out_bf16;
@@ -66,7 +67,8 @@ struct PagedArgs {
                               // cap_out 0: not capped
     uint32_t q_sign;          // sign bits xor-ed into Q (negative scale)
     // Partial results of the row kernel, two to a workgroup: [workgroup][2][rows] of ws_m (log2
-    // units), ws_l and ws_o (D values each), and what the first one belongs to
+    // units), ws_l and ws_o (D values each), and what the second one belongs to; meta null: no
+    // item is shared by workgroups
     float *ws_m, *ws_l, *ws_o;
     int* meta;
     int n_wg;
@@ -92,9 +94,13 @@ struct PagedRequest {
 constexpr int kPagedRowKeys = 128;
 constexpr int paged_row_wgs_per_cu(int d) { return d == 64 ? 4 : 2; }
 constexpr int kPagedMeta = 8;  // ints to a workgroup
+constexpr int kPagedMaxGroup = 1 << 15;
 // Requests of up to this many rows are the row kernel's (blocks of 16 or 32 rows).
 constexpr int kPagedFewRows = 32;
 hipError_t launch_paged_rows(const PagedArgs& a, int d, int block, hipStream_t stream);
+// Adds both kernels' partial results.
+hipError_t launch_paged_sums(const PagedArgs& a, int d, int row_block, int tile_block,
+                             hipStream_t stream);
 // Fewest tiles of keys to a split of the tile kernel.
 constexpr int kPagedMinTiles = 4;
 constexpr int kPagedMaxSplits = 16;

@@ -80,6 +80,9 @@ int validate_paged_dims(int T, int R, int Hq, int Hkv, int d, int max_q) {
     if (max_q < 0) return host::fail(ATTN_EINVAL, "max_q (%d) must not be negative", max_q);
     if ((long long)T * Hq > INT_MAX)
         return host::fail(ATTN_EUNSUPPORTED, "more than 2^31 - 1 query rows");
+    if (Hq / Hkv > kPagedMaxGroup)
+        return host::fail(ATTN_EUNSUPPORTED, "more than %d query heads to a key/value head",
+                          kPagedMaxGroup);
     return ATTN_OK;
 }
 
@@ -87,9 +90,11 @@ int validate_paged_dims(int T, int R, int Hq, int Hkv, int d, int max_q) {
 struct PagedLaunch {
     int few = 0;                      // requests of up to so many rows: the row kernel's
     int block = 0, n_wg = 0;          // row kernel (n_wg 0: not launched)
+    bool shared = false;              // its workgroups may share an item
+    int unit_log2 = 0;
     int waves = 0, splits = 1;        // tile kernel (waves 0: not launched)
     long long items = 0;              // its blocks of all heads at most
-    long long row_parts() const { return 2LL * n_wg * block; }
+    long long row_parts() const { return shared ? 2LL * n_wg * block : 0; }
     long long tile_parts() const { return splits > 1 ? items * splits * 32 * waves : 0; }
     size_t bytes(int d) const {
         return (size_t)(row_parts() + tile_parts()) * (d + 2) * sizeof(float) +
@@ -105,10 +110,22 @@ PagedLaunch paged_launch(int T, int R, int Hq, int Hkv, int d, int max_q, long l
     const long long most = (max_q ? std::min(max_q, T) : T) * (long long)group;  // of a request
     // One request is either's; among several, each kernel takes those of its kind.
     const bool tiles = most > kPagedFewRows;
-    l.few = !tiles ? INT_MAX : R == 1 ? 0 : kPagedFewRows;
+    // (Without the tile kernel, what has more rows than the caller said is nobody's.)
+    l.few = !tiles ? (int)most : R == 1 ? 0 : kPagedFewRows;
     if (l.few > 0) {
         l.block = most <= 16 ? 16 : 32;
         l.n_wg = paged_row_wgs_per_cu(d) * num_cus;
+        // steps of a request at most (its tokens are no more than its rows)
+        double steps = (double)max_keys / kPagedRowKeys + 1;
+        if (window) steps = std::min(steps, ((double)window + l.few) / kPagedRowKeys + 2);
+        // Few steps to every item: each is one workgroup's.  An item's steps one behind another
+        // cost about 1 us each, adding up its parts a launch of 5 us.
+        l.shared = steps > 6;
+        while ((1 << l.unit_log2) < steps && !l.shared) ++l.unit_log2;
+        // so few units that their number is 32-bit, whatever the lengths are
+        const double items = ((double)rows / 16 + R) * Hkv;
+        while (items * (steps / (1 << l.unit_log2) + 1) >= 2147483647.0 && l.unit_log2 < 24)
+            ++l.unit_log2;
     }
     if (tiles) {
         l.waves = most <= 128 ? 4 : 8;
@@ -376,6 +393,7 @@ int attn_paged(const attn_heads* q, const attn_heads* k_pages, const attn_heads*
         a.Hq = Hq;
         a.Hkv = Hkv;
         a.group = Hq / Hkv;
+        a.group_inverse = (uint32_t)(((1ULL << 32) + a.group - 1) / a.group);
         a.n_pages = n_pages;
         a.max_pages = max_pages;
         a.causal = causal ? 1 : 0;
@@ -399,17 +417,11 @@ int attn_paged(const attn_heads* q, const attn_heads* k_pages, const attn_heads*
         a.ws_l = f += l.row_parts();
         a.tile_m = f += l.row_parts();
         a.tile_l = f += l.tile_parts();
-        a.meta = reinterpret_cast<int*>(f += l.tile_parts());
-        a.tile_meta = a.meta + l.n_wg * kPagedMeta;
+        int* const meta = reinterpret_cast<int*>(f += l.tile_parts());
+        a.meta = l.shared ? meta : nullptr;
+        a.tile_meta = meta + l.n_wg * kPagedMeta;
         a.n_wg = l.n_wg;
-        // so few units that their number is 32-bit, whatever the lengths are
-        double units = 0;
-        do {
-            const double steps = (double)max_pages * page_size / kPagedRowKeys + 2;
-            units = ((double)T * a.group / 16 + R) * Hkv * (steps / (1 << a.unit_log2) + 1);
-        } while (units >= 2147483647.0 && ++a.unit_log2 < 24);
-        if (units >= 2147483647.0)
-            return host::fail(ATTN_EUNSUPPORTED, "more than 2^31 - 1 rows of heads");
+        a.unit_log2 = l.unit_log2;
         a.splits = l.splits;
         a.tile_wgs = l.items * l.splits;
         hipError_t e = hipSuccess;
@@ -417,6 +429,8 @@ int attn_paged(const attn_heads* q, const attn_heads* k_pages, const attn_heads*
         if (e == hipSuccess && l.waves)
             e = launch_paged_tiles(a, d, l.waves, (softcap > 0.f ? 1 : 0) | (slopes ? 2 : 0),
                                    host::stream());
+        if (e == hipSuccess)
+            e = launch_paged_sums(a, d, l.block, 32 * l.waves, host::stream());
         return e == hipSuccess ? ATTN_OK : host::fail_hip(e, "paged attention launch");
     });
 }

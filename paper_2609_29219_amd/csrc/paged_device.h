@@ -22,6 +22,26 @@ __device__ __forceinline__ PagedRequest paged_request(const PagedArgs& a, int r)
     return x;
 }
 
+// Rows of a block, `first` being the first one's number in the request: which token, and which
+// head of the group (row = token * group + head).  Inside a block by a product with the inverse,
+// 2^32 / group rounded up, which is exact as long as the dividend times the group is under 2^32.
+struct GroupDiv {
+    int token0, rest, group;
+    uint32_t inverse;
+    __device__ __forceinline__ GroupDiv(const PagedArgs& a, int first) {
+        group = a.group;
+        inverse = a.group_inverse;
+        token0 = (uint32_t)first / (uint32_t)group;
+        rest = first - token0 * group;
+    }
+    __device__ __forceinline__ int token(int i, int* head) const {
+        const int x = rest + i;
+        const int t = group == 1 ? x : (int)__umulhi((uint32_t)x, inverse);
+        *head = x - t * group;
+        return token0 + t;
+    }
+};
+
 // Inclusive sum over a wave, by moves between lanes inside rows of 16, then of the rows' sums.
 __device__ __forceinline__ int wave_scan(int x) {
     x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8

@@ -146,7 +146,7 @@ __global__ __launch_bounds__(kNT, 2) void paged_rows_kernel(const PagedArgs a) {
     constexpr int LOADS = L::PIECES; // of an operand and step
     __shared__ __attribute__((aligned(16))) uint8_t lds[kNW * L::WAVE];
     __shared__ float sm[kNW][BLOCK], sl[kNW][BLOCK];
-    __shared__ int found[8];
+    __shared__ int found[2];
     static_assert(kNW * 16 * OST * 4 <= (int)sizeof(lds), "");
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -156,56 +156,67 @@ __global__ __launch_bounds__(kNT, 2) void paged_rows_kernel(const PagedArgs a) {
     auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
 
     // ---- this workgroup's part of the line of all units ------------------------
-    // (less than 2^31 of them: the host chose their size)
+    // (less than 2^31 of them: the host chose their size)  Up to 64 requests: each wave by itself.
+    auto units_of = [&](const PagedRequest& x) {
+        const Share s = share_of(a, x, BLOCK);
+        return s.items * s.units;
+    };
+    const bool alone = a.R <= 64;
+    const int first_r = alone ? lane : tid;
     PagedRequest x = {0, 0, 0, 0, 0, 0};
     int mine = 0, sum = 0;  // (up to kNT requests: this thread's alone)
-    for (int r = tid; r < a.R; r += kNT) {
+    for (int r = first_r; r < a.R; r += kNT) {
         x = paged_request(a, r);
-        const Share s = share_of(a, x, BLOCK);
-        mine = s.items * s.units;
+        mine = units_of(x);
         sum += mine;
     }
-    int total;
-    int upto = block_scan<kNT>(sum, &total);
+    int total, upto;
+    if (alone) {
+        upto = wave_scan(sum);
+        total = __builtin_amdgcn_readlane(upto, 63);
+    } else {
+        upto = block_scan<kNT>(sum, &total);
+    }
     const int n_wg = min(a.n_wg, total), wg = blockIdx.x;
-    if (tid == 0) meta[0] = 0;
+    if (a.meta && tid == 0) meta[0] = 0;
     if (wg >= n_wg) return;
     // the first `more` workgroups have a unit more than the others
     const int per = (uint32_t)total / (uint32_t)n_wg, more = total - per * n_wg;
     const int u0 = per * wg + min(wg, more), u1 = u0 + per + (wg < more);
-    int before = 0;
-    for (int r0 = 0; r0 < a.R; r0 += kNT) {
-        int all = total;
-        if (a.R > kNT) {
-            const int r = r0 + tid;
-            mine = 0;
-            if (r < a.R) {
-                x = paged_request(a, r);
-                const Share s = share_of(a, x, BLOCK);
-                mine = s.items * s.units;
+    int r, r_first;  // request, its first unit
+    if (alone) {
+        const unsigned long long here = __ballot(u0 >= upto - mine && u0 < upto);
+        r = __ffsll((long long)here) - 1;
+        auto from = [&](int v) { return __builtin_amdgcn_readlane(v, r); };
+        r_first = from(upto - mine);
+        x = {from(x.q0), from(x.qn), from(x.pos0), from(x.kv), from(x.lo), from(x.bad)};
+    } else {
+        int before = 0;
+        for (int r0 = 0; r0 < a.R; r0 += kNT) {
+            int all = total;
+            if (a.R > kNT) {
+                mine = 0;
+                if (r0 + tid < a.R) {
+                    x = paged_request(a, r0 + tid);
+                    mine = units_of(x);
+                }
+                upto = block_scan<kNT>(mine, &all);
             }
-            upto = block_scan<kNT>(mine, &all);
-        }
-        if (u0 < before + all) {
-            const int first = before + upto - mine;
-            if (u0 >= first && u0 < first + mine) {
-                found[0] = r0 + tid;
-                found[1] = first;
-                found[2] = x.q0;
-                found[3] = x.qn;
-                found[4] = x.pos0;
-                found[5] = x.kv;
-                found[6] = x.lo;
-                found[7] = x.bad;
+            if (u0 < before + all) {
+                const int first = before + upto - mine;
+                if (u0 >= first && u0 < first + mine) {
+                    found[0] = r0 + tid;
+                    found[1] = first;
+                }
+                break;
             }
-            break;
+            before += all;
         }
-        before += all;
+        __syncthreads();
+        r = uniform(found[0]);
+        r_first = uniform(found[1]);
+        x = paged_request(a, r);
     }
-    __syncthreads();
-    int r = uniform(found[0]), r_first = uniform(found[1]);  // request, its first unit
-    x = {uniform(found[2]), uniform(found[3]), uniform(found[4]),
-         uniform(found[5]), uniform(found[6]), uniform(found[7])};
 
     const int page_mask = (1 << a.page_log2) - 1;
     const uint32_t k_lds = lds_address(lds) + wave * L::WAVE, v_lds = k_lds + L::K_BYTES;
@@ -254,6 +265,7 @@ __global__ __launch_bounds__(kNT, 2) void paged_rows_kernel(const PagedArgs a) {
             blk = item - head * share.blocks;
         }
         const int n_rows = min(x.qn * a.group - blk * BLOCK, BLOCK);
+        const GroupDiv rows(a, blk * BLOCK);
 
         // ---- loads of a step: a wave's 32 keys, in aligned runs of eight ------------------
         const uint16_t* const k_head = a.k.ptr + head * a.k.head;
@@ -308,9 +320,9 @@ __global__ __launch_bounds__(kNT, 2) void paged_rows_kernel(const PagedArgs a) {
         float slope[MT];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            const int row = blk * BLOCK + min(mt * 16 + l16, n_rows - 1);
-            const int tok = (uint32_t)row / (uint32_t)a.group;
-            const int h = head * a.group + row - tok * a.group;
+            int h;
+            const int tok = rows.token(min(mt * 16 + l16, n_rows - 1), &h);
+            h += head * a.group;
             const uint16_t* qp = a.q + (x.q0 + tok) * a.q_row + h * a.q_head + 8 * g4;
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
@@ -324,10 +336,10 @@ __global__ __launch_bounds__(kNT, 2) void paged_rows_kernel(const PagedArgs a) {
             slope[mt] = a.slopes ? a.slopes[h] * 1.4426950408889634f : 0.f;
         }
         // keys from here to there are seen by every row
-        const int tok_first = (uint32_t)(blk * BLOCK) / (uint32_t)a.group;
-        const int tok_last = (uint32_t)(blk * BLOCK + n_rows - 1) / (uint32_t)a.group;
-        const int all_hi = a.causal ? min(x.pos0 + tok_first, x.kv - 1) : x.kv - 1;
-        const int all_lo = a.window ? x.pos0 + tok_last - a.window + 1 : 0;
+        int unused;
+        const int all_hi = a.causal ? min(x.pos0 + rows.token(0, &unused), x.kv - 1) : x.kv - 1;
+        const int all_lo =
+            a.window ? x.pos0 + rows.token(n_rows - 1, &unused) - a.window + 1 : 0;
 
         float m[MT], l[MT];
         f32x4 oacc[MT][DB];
@@ -519,9 +531,9 @@ __global__ __launch_bounds__(kNT, 2) void paged_rows_kernel(const PagedArgs a) {
                                     so + (w * 16 + row - mt * 16) * OST + col);
                 }
                 if (whole) {
-                    const int rr = blk * BLOCK + row, tok = (uint32_t)rr / (uint32_t)a.group;
-                    store_row<D>(a, x.q0 + tok, head * a.group + rr - tok * a.group, col, acc, M,
-                                 L0);
+                    int h;
+                    const int tok = rows.token(row, &h);
+                    store_row<D>(a, x.q0 + tok, head * a.group + h, col, acc, M, L0);
                 } else {
                     const long long at = ((long long)wg * 2 + part) * BLOCK + row;
                     *reinterpret_cast<f32x4*>(a.ws_o + at * D + col) = acc;
@@ -536,10 +548,10 @@ __global__ __launch_bounds__(kNT, 2) void paged_rows_kernel(const PagedArgs a) {
     }
 }
 
-// Adds parts of rows: workgroup (g, y) those of ROWS rows of item g.  After the row
-// kernel (TILES false) item g is the one that begins in its workgroup g and does not end there:
-// its first part is that workgroup's second one, the others are the following workgroups' first.
-// After the tile kernel item g is a block of a head, its splits one behind another.
+// Adds parts of rows, ROWS rows of an item to a workgroup.  After the row kernel (TILES false)
+// item g is the one that begins in its workgroup g and does not end there: its first part is that
+// workgroup's second one, the others are the following workgroups' first.  After the tile kernel
+// item g is a block of a head, its splits one behind another.
 //
 // Bound by latency after the row kernel: few rows of many parts, just written by other CUs.  The
 // lane groups of a row take every GP-th part, four on their way, and meet in LDS.  After the tile
@@ -547,22 +559,22 @@ __global__ __launch_bounds__(kNT, 2) void paged_rows_kernel(const PagedArgs a) {
 template <int D, bool TILES>
 constexpr int kSumRows = TILES ? kNT / (D / 4) : 2;
 template <int D, bool TILES>
-__global__ __launch_bounds__(kNT) void paged_sum_kernel(const PagedArgs a, int block) {
+__device__ __forceinline__ void sum_rows(const PagedArgs& a, int index, int block) {
     constexpr int ROWS = kSumRows<D, TILES>;
     constexpr int LANES = D / 4, GROUPS = kNT / LANES, GP = GROUPS / ROWS, U = 4;
+    const int g = index / (block / ROWS), row0 = (index - g * (block / ROWS)) * ROWS;
     const int4* const meta = reinterpret_cast<const int4*>(TILES ? a.tile_meta : a.meta) +
-                             (long long)blockIdx.x * (kPagedMeta / 4);
+                             (long long)g * (kPagedMeta / 4);
     const float* const ws_m = TILES ? a.tile_m : a.ws_m;
     const float* const ws_l = TILES ? a.tile_l : a.ws_l;
     const float* const ws_o = TILES ? a.tile_o : a.ws_o;
     const int4 item = meta[0];
     const int n_rows = meta[1].x, n = item.x;
-    if (n == 0 || (int)blockIdx.y * ROWS >= n_rows) return;
+    if (n == 0 || row0 >= n_rows) return;
     const int grp = threadIdx.x / LANES, lane = threadIdx.x % LANES, col = lane * 4;
-    const int row = min((int)blockIdx.y * ROWS + grp / GP, n_rows - 1);
+    const int row = min(row0 + grp / GP, n_rows - 1);
     auto at = [&](int i) {  // part i
-        const long long part = TILES ? (long long)blockIdx.x * a.splits + i
-                                     : ((long long)blockIdx.x + i) * 2 + (i == 0);
+        const long long part = TILES ? (long long)g * a.splits + i : ((long long)g + i) * 2 + (i == 0);
         return part * block + row;
     };
     float M = -INFINITY, L = 0.f;
@@ -615,26 +627,45 @@ __global__ __launch_bounds__(kNT) void paged_sum_kernel(const PagedArgs a, int b
             acc += w * so[grp + q][lane];
         }
     }
-    if ((int)blockIdx.y * ROWS + grp / GP >= n_rows) return;
-    const int rr = item.w + row, tok = rr / a.group;
+    if (row0 + grp / GP >= n_rows) return;
+    const int rr = item.w + row, tok = (uint32_t)rr / (uint32_t)a.group;
     store_row<D>(a, item.y + tok, item.z + rr - tok * a.group, col, acc, M, L);
 }
 
-template <int D, bool TILES>
-hipError_t launch_sum(const PagedArgs& a, int items, int block, hipStream_t stream) {
-    hipLaunchKernelGGL((paged_sum_kernel<D, TILES>), dim3(items, block / kSumRows<D, TILES>), dim3(kNT), 0,
-                       stream, a, block);
+// The first row_wgs workgroups add the row kernel's parts, the others the tile kernel's.
+template <int D>
+__global__ __launch_bounds__(kNT) void paged_sum_kernel(const PagedArgs a, int row_wgs,
+                                                        int row_block, int tile_block) {
+    if ((int)blockIdx.x < row_wgs)
+        sum_rows<D, false>(a, blockIdx.x, row_block);
+    else
+        sum_rows<D, true>(a, blockIdx.x - row_wgs, tile_block);
+}
+
+template <int D>
+hipError_t launch_sums(const PagedArgs& a, int row_block, int tile_block, hipStream_t stream) {
+    const long long rows = a.meta ? (long long)a.n_wg * (row_block / kSumRows<D, false>) : 0;
+    const long long tiles =
+        a.splits > 1 ? a.tile_wgs / a.splits * (tile_block / kSumRows<D, true>) : 0;
+    if (rows + tiles == 0) return hipSuccess;
+    hipLaunchKernelGGL(paged_sum_kernel<D>, dim3((unsigned)(rows + tiles)), dim3(kNT), 0, stream,
+                       a, (int)rows, row_block, tile_block);
     return hipGetLastError();
 }
 
 template <int D, int MT>
 hipError_t launch_rows(const PagedArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((paged_rows_kernel<D, MT>), dim3(a.n_wg), dim3(kNT), 0, stream, a);
-    const hipError_t e = hipGetLastError();
-    return e != hipSuccess ? e : launch_sum<D, false>(a, a.n_wg, 16 * MT, stream);
+    return hipGetLastError();
 }
 
 }  // namespace
+
+hipError_t launch_paged_sums(const PagedArgs& a, int d, int row_block, int tile_block,
+                             hipStream_t stream) {
+    return d == 64 ? launch_sums<64>(a, row_block, tile_block, stream)
+                   : launch_sums<128>(a, row_block, tile_block, stream);
+}
 
 hipError_t launch_paged_rows(const PagedArgs& a, int d, int block, hipStream_t stream) {
     if (d == 64 && block == 16) return launch_rows<64, 1>(a, stream);
@@ -650,10 +681,7 @@ hipError_t launch_paged_tiles(const PagedArgs& a, int d, int waves, int form, hi
     if (d == 64 && waves == 8) e = launch_paged_tiles_d64_w8(a, form, stream);
     if (d == 128 && waves == 4) e = launch_paged_tiles_d128_w4(a, form, stream);
     if (d == 128 && waves == 8) e = launch_paged_tiles_d128_w8(a, form, stream);
-    if (e != hipSuccess || a.splits == 1) return e;
-    const int items = (int)(a.tile_wgs / a.splits);
-    return d == 64 ? launch_sum<64, true>(a, items, 32 * waves, stream)
-                   : launch_sum<128, true>(a, items, 32 * waves, stream);
+    return e;
 }
 
 }  // namespace attn

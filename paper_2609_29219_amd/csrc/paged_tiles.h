@@ -95,9 +95,14 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
     // ---- its rows and keys -------------------------------------------------------
     const int w_row0 = blk * BM + wave * 32;                // first row of this wave
     const int last_row = blk * BM + n_rows - 1;
-    const int row = min(w_row0 + l32, last_row);            // rows past the end repeat the last
-    const int tok = row / a.group, qh = head * a.group + row - tok * a.group;
-    auto pos_of = [&](int rr) { return x.pos0 + min(rr, last_row) / a.group; };
+    const GroupDiv rows(a, blk * BM);
+    int qh;
+    const int tok = rows.token(min(wave * 32 + l32, n_rows - 1), &qh);  // rows past the end repeat
+    qh += head * a.group;                                               // the last
+    auto pos_of = [&](int rr) {
+        int unused;
+        return x.pos0 + rows.token(min(rr, last_row) - blk * BM, &unused);
+    };
     const int pos = x.pos0 + tok;
     const int hi = a.causal ? min(pos, x.kv - 1) : x.kv - 1;
     const int lo = a.window ? pos - a.window + 1 : 0;
@@ -526,10 +531,11 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
     bool there[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const int i = (lane >> 3) + 8 * j, rr = w_row0 + i, tk = rr / a.group;
-        there[j] = rr <= last_row;
-        orow[j] = partial ? part0 + wave * 32 + i
-                          : (long long)(x.q0 + tk) * a.Hq + head * a.group + rr - tk * a.group;
+        const int i = wave * 32 + (lane >> 3) + 8 * j;
+        there[j] = i < n_rows;
+        int h;
+        const int tk = rows.token(i, &h);
+        orow[j] = partial ? part0 + i : (long long)(x.q0 + tk) * a.Hq + head * a.group + h;
     }
     auto emit = [&](int piece) __attribute__((always_inline)) {
         u32x4 w[4];

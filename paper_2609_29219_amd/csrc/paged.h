@@ -99,16 +99,14 @@ constexpr int kPagedMaxGroup = 1 << 15;
 constexpr int kPagedFewRows = 32;
 hipError_t launch_paged_rows(const PagedArgs& a, int d, int block, hipStream_t stream);
 // Adds both kernels' partial results.
-hipError_t launch_paged_sums(const PagedArgs& a, int d, int row_block, int tile_block,
-                             hipStream_t stream);
+hipError_t launch_paged_sums(const PagedArgs& a, int d, int row_block, hipStream_t stream);
 // Fewest tiles of keys to a split of the tile kernel.
 constexpr int kPagedMinTiles = 4;
-constexpr int kPagedMaxSplits = 16;
-// waves: 4 (128 rows to a block) or 8 (256); form: 1 capped scores, 2 slopes
-hipError_t launch_paged_tiles(const PagedArgs& a, int d, int waves, int form, hipStream_t stream);
-hipError_t launch_paged_tiles_d64_w4(const PagedArgs& a, int form, hipStream_t stream);
-hipError_t launch_paged_tiles_d64_w8(const PagedArgs& a, int form, hipStream_t stream);
-hipError_t launch_paged_tiles_d128_w4(const PagedArgs& a, int form, hipStream_t stream);
-hipError_t launch_paged_tiles_d128_w8(const PagedArgs& a, int form, hipStream_t stream);
+constexpr int kPagedMaxSplits = 64;
+constexpr int kPagedTileRows = 256;  // to a block of the tile kernel
+// form: 1 capped scores, 2 slopes
+hipError_t launch_paged_tiles(const PagedArgs& a, int d, int form, hipStream_t stream);
+hipError_t launch_paged_tiles_d64(const PagedArgs& a, int form, hipStream_t stream);
+hipError_t launch_paged_tiles_d128(const PagedArgs& a, int form, hipStream_t stream);
 
 }  // namespace attn

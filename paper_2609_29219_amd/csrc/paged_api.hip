@@ -92,10 +92,10 @@ struct PagedLaunch {
     int block = 0, n_wg = 0;          // row kernel (n_wg 0: not launched)
     bool shared = false;              // its workgroups may share an item
     int unit_log2 = 0;
-    int waves = 0, splits = 1;        // tile kernel (waves 0: not launched)
-    long long items = 0;              // its blocks of all heads at most
+    long long items = 0;              // tile kernel: blocks of all heads at most (0: not launched)
+    int splits = 1;
     long long row_parts() const { return shared ? 2LL * n_wg * block : 0; }
-    long long tile_parts() const { return splits > 1 ? items * splits * 32 * waves : 0; }
+    long long tile_parts() const { return splits > 1 ? items * splits * kPagedTileRows : 0; }
     size_t bytes(int d) const {
         return (size_t)(row_parts() + tile_parts()) * (d + 2) * sizeof(float) +
                (size_t)(n_wg + items) * kPagedMeta * sizeof(int);
@@ -128,23 +128,30 @@ PagedLaunch paged_launch(int T, int R, int Hq, int Hkv, int d, int max_q, long l
             ++l.unit_log2;
     }
     if (tiles) {
-        l.waves = most <= 128 ? 4 : 8;
+        const int block = kPagedTileRows;
         const long long requests = l.few ? std::min<long long>(R, rows / (l.few + 1)) : R;
         // (all but one row of a block each may be missing from the requests' last blocks)
-        l.items = (rows + requests * (32 * l.waves - 1)) / (32 * l.waves) * Hkv;
+        l.items = (rows + requests * (block - 1)) / block * Hkv;
         // The keys are split where that is faster by this estimate, in us on this card: rounds
         // of workgroups, each with 6 us of start and end and 2 to a tile, then 4 us and the
-        // partial results' traffic.  (Requests as long as their table or their window allows, up
-        // to 16384, every other one with rows for a block of its own; what the device finds may
-        // need fewer splits, and the others end at once.)
-        const double at_once = num_cus * 8 / l.waves;
-        const double items = ((double)rows / (32 * l.waves) + (requests > 1 ? requests / 2 : 0)) * Hkv;
+        // partial results' traffic.  (All rows in requests of the most rows, so that a full batch
+        // is estimated as it is, or every fourth request with a block that is not full.  Keys as
+        // many as the table or the window allows, up to 16384.  What the device finds may need
+        // fewer splits, and the others end at once.)  Measured: 64 requests of 40 rows over 8192
+        // keys in two splits 88 us, in four, as chosen, 67; 32 of 64 rows over 4096 keys of 8
+        // heads in two 130 us, unsplit, as chosen, 110.
+        const double at_once = num_cus;
+        const bool exact = rows == R * most;
+        double items = (double)rows / most * ((most + block - 1) / block);
+        if (!exact) items = std::max(items, (double)rows / block + requests / 4.0);
+        items *= Hkv;
         double keys = std::min(16384.0, (double)max_keys);
-        if (window) keys = std::min(keys, window + 32.0 * l.waves / group);
+        if (window) keys = std::min(keys, window + (double)block / group);
         double best = 0;
         for (int s = 1; s <= kPagedMaxSplits && (s == 1 || items * s <= 4 * at_once); ++s) {
-            double t = ceil(items * s / at_once) * (6 + 2 * keys / 64 / s);
-            if (s > 1) t += 4 + items * s * 32 * l.waves * d * 4 / 5e6;
+            const double rounds = items * s / at_once;
+            double t = (exact ? ceil(rounds) : std::max(1.0, rounds)) * (6 + 2 * keys / 64 / s);
+            if (s > 1) t += 4 + items * s * block * d * 4 / 5e6;
             if (s == 1 || t < best) {
                 best = t;
                 l.splits = s;
@@ -426,11 +433,11 @@ int attn_paged(const attn_heads* q, const attn_heads* k_pages, const attn_heads*
         a.tile_wgs = l.items * l.splits;
         hipError_t e = hipSuccess;
         if (l.n_wg) e = launch_paged_rows(a, d, l.block, host::stream());
-        if (e == hipSuccess && l.waves)
-            e = launch_paged_tiles(a, d, l.waves, (softcap > 0.f ? 1 : 0) | (slopes ? 2 : 0),
+        if (e == hipSuccess && l.items)
+            e = launch_paged_tiles(a, d, (softcap > 0.f ? 1 : 0) | (slopes ? 2 : 0),
                                    host::stream());
         if (e == hipSuccess)
-            e = launch_paged_sums(a, d, l.block, 32 * l.waves, host::stream());
+            e = launch_paged_sums(a, d, l.block, host::stream());
         return e == hipSuccess ? ATTN_OK : host::fail_hip(e, "paged attention launch");
     });
 }

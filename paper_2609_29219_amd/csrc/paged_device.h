@@ -73,27 +73,51 @@ __device__ __forceinline__ int block_scan(int x, int* total) {
     return x + before;
 }
 
-// The request that has the nth of something of which request x has count(x), or -1; before it
-// there are found[1] (shared memory; all threads call it).
+// The request (r, or -1) that has the nth of something of which request y has count(y), and how
+// many there are before it.  found: shared memory.  All threads call it; up to 64 requests each
+// wave finds it by itself.
+struct PagedFound {
+    int r, first;
+    PagedRequest x;
+};
 template <int NT, typename F>
-__device__ __forceinline__ int paged_find(const PagedArgs& a, int nth, int* found, F&& count) {
+__device__ __forceinline__ PagedFound paged_find(const PagedArgs& a, int nth, int* found,
+                                                 F&& count) {
+    auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    if (a.R <= 64) {
+        const int lane = threadIdx.x & 63;
+        PagedRequest y = {0, 0, 0, 0, 0, 0};
+        int mine = 0;
+        if (lane < a.R) {
+            y = paged_request(a, lane);
+            mine = count(y);
+        }
+        const int upto = wave_scan(mine);
+        const unsigned long long here = __ballot(nth >= upto - mine && nth < upto);
+        const int r = here ? __ffsll((long long)here) - 1 : 0;
+        auto from = [&](int v) { return __builtin_amdgcn_readlane(v, r); };
+        return {here ? r : -1,
+                from(upto - mine),
+                {from(y.q0), from(y.qn), from(y.pos0), from(y.kv), from(y.lo), from(y.bad)}};
+    }
     int before = 0;
     for (int r0 = 0; r0 < a.R; r0 += NT) {
         const int r = r0 + threadIdx.x;
         const int mine = r < a.R ? count(paged_request(a, r)) : 0;
         int all;
-        const int first = before + block_scan<NT>(mine, &all) - mine;
+        const int at = before + block_scan<NT>(mine, &all) - mine;
         if (nth < before + all) {
-            if (nth >= first && nth < first + mine) {
+            if (nth >= at && nth < at + mine) {
                 found[0] = r;
-                found[1] = first;
+                found[1] = at;
             }
             __syncthreads();
-            return __builtin_amdgcn_readfirstlane(found[0]);
+            const int here = uniform(found[0]);
+            return {here, uniform(found[1]), paged_request(a, here)};
         }
         before += all;
     }
-    return -1;
+    return {-1, 0, {0, 0, 0, 0, 0, 0}};
 }
 
 }  // namespace attn

@@ -635,21 +635,21 @@ __device__ __forceinline__ void sum_rows(const PagedArgs& a, int index, int bloc
 // The first row_wgs workgroups add the row kernel's parts, the others the tile kernel's.
 template <int D>
 __global__ __launch_bounds__(kNT) void paged_sum_kernel(const PagedArgs a, int row_wgs,
-                                                        int row_block, int tile_block) {
+                                                        int row_block) {
     if ((int)blockIdx.x < row_wgs)
         sum_rows<D, false>(a, blockIdx.x, row_block);
     else
-        sum_rows<D, true>(a, blockIdx.x - row_wgs, tile_block);
+        sum_rows<D, true>(a, blockIdx.x - row_wgs, kPagedTileRows);
 }
 
 template <int D>
-hipError_t launch_sums(const PagedArgs& a, int row_block, int tile_block, hipStream_t stream) {
+hipError_t launch_sums(const PagedArgs& a, int row_block, hipStream_t stream) {
     const long long rows = a.meta ? (long long)a.n_wg * (row_block / kSumRows<D, false>) : 0;
     const long long tiles =
-        a.splits > 1 ? a.tile_wgs / a.splits * (tile_block / kSumRows<D, true>) : 0;
+        a.splits > 1 ? a.tile_wgs / a.splits * (kPagedTileRows / kSumRows<D, true>) : 0;
     if (rows + tiles == 0) return hipSuccess;
     hipLaunchKernelGGL(paged_sum_kernel<D>, dim3((unsigned)(rows + tiles)), dim3(kNT), 0, stream,
-                       a, (int)rows, row_block, tile_block);
+                       a, (int)rows, row_block);
     return hipGetLastError();
 }
 
@@ -661,10 +661,9 @@ hipError_t launch_rows(const PagedArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_paged_sums(const PagedArgs& a, int d, int row_block, int tile_block,
-                             hipStream_t stream) {
-    return d == 64 ? launch_sums<64>(a, row_block, tile_block, stream)
-                   : launch_sums<128>(a, row_block, tile_block, stream);
+hipError_t launch_paged_sums(const PagedArgs& a, int d, int row_block, hipStream_t stream) {
+    return d == 64 ? launch_sums<64>(a, row_block, stream)
+                   : launch_sums<128>(a, row_block, stream);
 }
 
 hipError_t launch_paged_rows(const PagedArgs& a, int d, int block, hipStream_t stream) {
@@ -675,13 +674,10 @@ hipError_t launch_paged_rows(const PagedArgs& a, int d, int block, hipStream_t s
     return hipErrorInvalidValue;
 }
 
-hipError_t launch_paged_tiles(const PagedArgs& a, int d, int waves, int form, hipStream_t stream) {
-    hipError_t e = hipErrorInvalidValue;
-    if (d == 64 && waves == 4) e = launch_paged_tiles_d64_w4(a, form, stream);
-    if (d == 64 && waves == 8) e = launch_paged_tiles_d64_w8(a, form, stream);
-    if (d == 128 && waves == 4) e = launch_paged_tiles_d128_w4(a, form, stream);
-    if (d == 128 && waves == 8) e = launch_paged_tiles_d128_w8(a, form, stream);
-    return e;
+hipError_t launch_paged_tiles(const PagedArgs& a, int d, int form, hipStream_t stream) {
+    if (d == 64) return launch_paged_tiles_d64(a, form, stream);
+    if (d == 128) return launch_paged_tiles_d128(a, form, stream);
+    return hipErrorInvalidValue;
 }
 
 }  // namespace attn

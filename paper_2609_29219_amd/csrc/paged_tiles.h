@@ -1,7 +1,7 @@
 // Attention of requests with many new tokens over a paged cache (see paged_rows.hip for the
 // definition, and for the requests with few).
 //
-// A workgroup computes a block of 32 NW rows (token by token, row = token * group + head of the
+// A workgroup computes a block of 256 rows (token by token, row = token * group + head of the
 // group) of one request and key/value head: S^T = K Q^T and O^T += V^T P^T on
 // v_mfma_f32_32x32x16_bf16, K and V in tiles of 64 keys through LDS, an online softmax.  Each
 // wave has 32 rows, one to a lane and its mate 32 lanes on, so the softmax is in a lane but for
@@ -59,13 +59,13 @@ struct PagedLds {
 // rounded to bf16 (a product with a 0/1 operand that leaves each lane its own row's, as in
 // fwd_kernel.h): 32 additions a tile less beside the products.  For calls without a log-sum-exp,
 // whose sums have to be of the weights as they are.
-template <int D, int NW, int FORM, bool MSUM>
-__global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs a) {
+template <int D, int FORM, bool MSUM>
+__global__ __launch_bounds__(512, 2) void paged_tiles_kernel(const PagedArgs a) {
     using L = PagedLds<D>;
-    constexpr int NT = NW * 64, BM = NW * 32, BN = kTileKeys;
+    constexpr int NW = 8, NT = NW * 64, BM = kPagedTileRows, BN = kTileKeys;
+    static_assert(BM == 32 * NW, "");
     constexpr int KD = D / 16, KB = BN / 32, CB = D / 32;
-    constexpr int JOBS = 8 / NW;                        // of 16 rows, to a wave and tile
-    constexpr int JOB_PIECES = 16 / L::PIECE_ROWS;      // instructions to a job
+    constexpr int JOB_PIECES = 16 / L::PIECE_ROWS;  // instructions to a wave's part of a tile
     constexpr int STAGE = NW * kFwdStageWaveBytes;
     __shared__ __attribute__((aligned(16))) uint8_t lds[L::BYTES > STAGE ? L::BYTES : STAGE];
     __shared__ int found[2];
@@ -78,18 +78,19 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
     const int unit = blockIdx.x / a.Hkv, head = blockIdx.x - unit * a.Hkv;
     const int nth = unit / a.splits, split = unit - nth * a.splits;
     int* const meta = a.tile_meta + ((long long)nth * a.Hkv + head) * kPagedMeta;
-    const int r = paged_find<NT>(
-        a, nth, found, [&](const PagedRequest& x) __attribute__((always_inline)) -> int {
-            const long long rows = (long long)x.qn * a.group;
-            return rows > a.few ? (int)((uint32_t)(rows + BM - 1) / BM) : 0;
-        });
+    auto blocks_of = [&](const PagedRequest& x) __attribute__((always_inline)) -> int {
+        const long long rows = (long long)x.qn * a.group;
+        return rows > a.few ? (int)((uint32_t)(rows + BM - 1) / BM) : 0;
+    };
+    const PagedFound here = paged_find<NT>(a, nth, found, blocks_of);
+    const int r = here.r;
     if (r < 0) {  // there are fewer blocks
         if (a.splits > 1 && split == 0 && tid == 0) meta[0] = 0;
         return;
     }
-    const PagedRequest x = paged_request(a, r);
+    const PagedRequest x = here.x;
     const int n_blocks = (x.qn * a.group + BM - 1) / BM;
-    const int blk = n_blocks - 1 - (nth - found[1]);
+    const int blk = n_blocks - 1 - (nth - here.first);
     const int n_rows = min(x.qn * a.group - blk * BM, BM);
 
     // ---- its rows and keys -------------------------------------------------------
@@ -141,9 +142,8 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
     const float slope = (FORM & 2) ? a.slopes[qh] * 1.4426950408889634f : 0.f;
 
     // ---- tile loads ------------------------------------------------------------
-    // A tile's 64 rows of K and of V are eight jobs of 16 rows.  Of eight waves the first four
-    // bring K's, the others V's, so that each has one page to find for a tile (with pages of
-    // eight rows two); of four waves each has a job of either.
+    // A tile's 64 rows of K are four waves' job, 16 rows to each, and V's the others', so that a
+    // wave has one page to find for a tile (two of eight rows).
     const int* const table = a.table + (long long)r * a.table_stride;
     const int page_mask = (1 << a.page_log2) - 1;
     const bool small_pages = a.page_log2 == 3;
@@ -152,83 +152,70 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
     bool bad = x.bad != 0;
     const int p_row = lane / (D / 8), p_chunk = lane % (D / 8);  // this lane's place in 1 KiB
     const int last_key = x.kv - 1;
-    struct Job {
-        const uint16_t* base;       // head's first row
-        uint32_t page16, row16;
-        int ahead;                  // tiles from the one at work to the one that is loaded
-        int first, slot0, slot1, piece;
-        int swap, off;              // this lane's source in the job's first piece
-        int entry0, entry1;         // page numbers of the next tile that is loaded
-    } job[JOBS];
-#pragma unroll
-    for (int i = 0; i < JOBS; ++i) {
-        const bool is_k = JOBS == 2 ? i == 0 : wave < 4;
-        const PagedSide& side = is_k ? a.k : a.v;
-        Job& b = job[i];
-        b.base = side.ptr + head * side.head;
-        b.page16 = side.page16;
-        b.row16 = side.row16;
-        b.ahead = is_k ? 2 : 1;
-        b.first = 16 * (wave & 3);
-        b.piece = is_k ? L::K_PIECE : L::V_PIECE;
-        b.slot0 = (is_k ? KS0 : VS0) + b.first / L::PIECE_ROWS * b.piece;
-        b.slot1 = b.slot0 + (is_k ? L::K_TILE : L::V_TILE);
-        b.swap = p_chunk ^ (is_k ? L::k_swap(p_row) : L::v_swap(p_row));
-        b.off = p_row * (int)side.row16 * 16 + b.swap * 16;
-        b.entry0 = b.entry1 = 0;
-    }
+    const bool is_k = wave < 4;
+    const PagedSide& side = is_k ? a.k : a.v;
+    const uint16_t* const base = side.ptr + head * side.head;
+    const uint32_t page16 = side.page16, row16 = side.row16;
+    const int ahead = is_k ? 2 : 1;  // tiles from the one at work to the one that is loaded
+    const int job_row = 16 * (wave & 3);
+    const int piece = is_k ? L::K_PIECE : L::V_PIECE;
+    const int slot0 = (is_k ? KS0 : VS0) + job_row / L::PIECE_ROWS * piece;
+    const int slot1 = slot0 + (is_k ? L::K_TILE : L::V_TILE);
+    // this lane's source in the job's first piece
+    const int swap = p_chunk ^ (is_k ? L::k_swap(p_row) : L::v_swap(p_row));
+    const int off = p_row * (int)row16 * 16 + swap * 16;
+    int next0 = 0, next1 = 0;  // page numbers of the next tile that is loaded
     // first key of `n` (8 or 16) aligned ones, clamped to those that hold a key that some row sees
-    auto run_of = [&](const Job& b, int t, int at, int n) __attribute__((always_inline)) {
-        return max(min(t * BN + b.first + at, last_key & ~(n - 1)), x.lo & ~(n - 1));
+    auto run_of = [&](int t, int at, int n) __attribute__((always_inline)) {
+        return max(min(t * BN + job_row + at, last_key & ~(n - 1)), x.lo & ~(n - 1));
     };
     // (as vector loads, which land with the tiles' before the barrier: scalar ones would hold up
     // the tile's first reads from LDS, which are waited for by the same count)
     int zero;
     asm volatile("v_mov_b32 %0, 0" : "=v"(zero));
-    auto read_entries = [&](Job& b, int t) __attribute__((always_inline)) {
-        if (small_pages) {
-            b.entry0 = table[(run_of(b, t, 0, 8) >> 3) + zero];
-            b.entry1 = table[(run_of(b, t, 8, 8) >> 3) + zero];
-        } else {
-            b.entry0 = table[(run_of(b, t, 0, 16) >> a.page_log2) + zero];
-        }
+    auto entry0_of = [&](int t) __attribute__((always_inline)) -> int {
+        const int at = small_pages ? run_of(t, 0, 8) >> 3 : run_of(t, 0, 16) >> a.page_log2;
+        return table[at + zero];
+    };
+    auto entry1_of = [&](int t) __attribute__((always_inline)) -> int {  // with small_pages
+        return table[(run_of(t, 8, 8) >> 3) + zero];
     };
     // Rows of tile t from piece p0 to p1 of the job, which lie in page `entry` from key0 on.
-    auto bring_run = [&](const Job& b, int t, int key0, int entry, auto p0c, auto p1c, int slot)
+    auto bring_run = [&](int t, int key0, int entry, auto p0c, auto p1c, int slot)
         __attribute__((always_inline)) {
         constexpr int p0 = decltype(p0c)::value, p1 = decltype(p1c)::value;
         const bool out = (uint32_t)entry >= (uint32_t)a.n_pages;
         bad |= out;
-        const uint64_t at = (uint64_t)(uint32_t)(out ? 0 : entry) * b.page16 +
-                            (uint64_t)(uint32_t)(key0 & page_mask) * b.row16;
-        const dma_rsrc_t rsrc = make_dma_rsrc(b.base + at * 8, 0x7fffffffu);
+        const uint64_t at = (uint64_t)(uint32_t)(out ? 0 : entry) * page16 +
+                            (uint64_t)(uint32_t)(key0 & page_mask) * row16;
+        const dma_rsrc_t rsrc = make_dma_rsrc(base + at * 8, 0x7fffffffu);
         if (t * BN < x.lo || t * BN + BN > x.kv) {
             // keys that no row sees are copies of the nearest that one does
 #pragma unroll 1
             for (int p = 0; p < p1 - p0; ++p) {
                 const int rr = p * L::PIECE_ROWS + p_row;
                 const int from = max(min(key0 + rr, last_key), x.lo) - key0;
-                lds_dma16(rsrc, lds_base + slot + (p0 + p) * b.piece,
-                          from * (int)b.row16 * 16 + b.swap * 16, 0);
+                lds_dma16(rsrc, lds_base + slot + (p0 + p) * piece,
+                          from * (int)row16 * 16 + swap * 16, 0);
             }
         } else {
 #pragma unroll
             for (int p = p0; p < p1; ++p)
-                lds_dma16(rsrc, lds_base + slot + p * b.piece, b.off,
-                          (p - p0) * L::PIECE_ROWS * (int)b.row16 * 16);
+                lds_dma16(rsrc, lds_base + slot + p * piece, off,
+                          (p - p0) * L::PIECE_ROWS * (int)row16 * 16);
         }
     };
-    auto bring_job = [&](const Job& b, int t, int slot) __attribute__((always_inline)) {
+    auto bring_job = [&](int t, int slot, int entry0, int entry1) __attribute__((always_inline)) {
         using std::integral_constant;
         auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
         integral_constant<int, 0> none;
         integral_constant<int, JOB_PIECES / 2> half;
         integral_constant<int, JOB_PIECES> all;
         if (small_pages) {
-            bring_run(b, t, run_of(b, t, 0, 8), uniform(b.entry0), none, half, slot);
-            bring_run(b, t, run_of(b, t, 8, 8), uniform(b.entry1), half, all, slot);
+            bring_run(t, run_of(t, 0, 8), uniform(entry0), none, half, slot);
+            bring_run(t, run_of(t, 8, 8), uniform(entry1), half, all, slot);
         } else {
-            bring_run(b, t, run_of(b, t, 0, 16), uniform(b.entry0), none, all, slot);
+            bring_run(t, run_of(t, 0, 16), uniform(entry0), none, all, slot);
         }
     };
 
@@ -324,8 +311,7 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
         constexpr bool HAS_S = decltype(has_s_tag)::value, ODD = decltype(odd_tag)::value;
         constexpr int kslot = ODD ? KS0 : KS1, vslot = ODD ? VS1 : VS0;  // of tiles t + 1 and t
         constexpr int NS = HAS_S ? KB * KD : 0, NPV = KB * 2 * CB, NM = NS + NPV;
-        constexpr int PF = NW == 8 ? 3 : 2;  // operands on their way, and in use (with four waves, each
-                                             // with two jobs of loads, a third one spills)
+        constexpr int PF = 3;                                // operands on their way, and in use
         constexpr int NPAIR = KB * 8;
         constexpr int EXP_SLOTS = HAS_S ? NS + NPV / 2 : 0;  // slots with exponentials
         constexpr int MAX0 = EXP_SLOTS + 1;                  // first slot with the next maximum
@@ -424,16 +410,18 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
     float mx_next = -INFINITY;
     const bool has_keys = t_end > t_begin;
     if (has_keys) {
-#pragma unroll
-        for (int i = 0; i < JOBS; ++i) {
-            read_entries(job[i], t_begin);
-            bring_job(job[i], t_begin, job[i].slot0);
-            read_entries(job[i], min(t_begin + 1, t_end - 1));
-            if (job[i].ahead == 2) {
-                if (t_begin + 1 < t_end) bring_job(job[i], t_begin + 1, job[i].slot1);
-                read_entries(job[i], min(t_begin + 2, t_end - 1));
-            }
+        // (all page numbers first: a wait for one is a wait for every load before it)
+        const int second = min(t_begin + 1, t_end - 1), third = min(t_begin + ahead, t_end - 1);
+        const int a0 = entry0_of(t_begin), b0 = entry0_of(second);
+        next0 = entry0_of(third);
+        int a1 = 0, b1 = 0;
+        if (small_pages) {
+            a1 = entry1_of(t_begin);
+            b1 = entry1_of(second);
+            next1 = entry1_of(third);
         }
+        bring_job(t_begin, slot0, a0, a1);
+        if (is_k && t_begin + 1 < t_end) bring_job(t_begin + 1, slot1, b0, b1);
         publish_barrier<0>();
         if (t_last >= t_begin) {
 #pragma unroll
@@ -460,13 +448,11 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
     }
     // loads of iteration t
     auto bring = [&](int t, bool odd) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < JOBS; ++i) {
-            Job& b = job[i];
-            const int to = t + b.ahead;
-            if (to < t_end) bring_job(b, to, (b.ahead == 2) == odd ? b.slot1 : b.slot0);
-            read_entries(b, min(to + 1, t_end - 1));
-        }
+        const int to = t + ahead;
+        if (to < t_end) bring_job(to, is_k == odd ? slot1 : slot0, next0, next1);
+        const int then = min(to + 1, t_end - 1);
+        next0 = entry0_of(then);
+        if (small_pages) next1 = entry1_of(then);
     };
     // Iteration t of a wave: scores of an even tile (from t_begin) are in set A, of an odd one in
     // set B, so that slots and sets are known at compile time.
@@ -593,22 +579,22 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_tiles_kernel(const PagedArgs
     }
 }
 
-template <int D, int NW, int FORM, bool MSUM>
+template <int D, int FORM, bool MSUM>
 hipError_t launch_paged_tiles_form(const PagedArgs& a, hipStream_t stream) {
-    hipLaunchKernelGGL((paged_tiles_kernel<D, NW, FORM, MSUM>), dim3((unsigned)a.tile_wgs),
-                       dim3(NW * 64), 0, stream, a);
+    hipLaunchKernelGGL((paged_tiles_kernel<D, FORM, MSUM>), dim3((unsigned)a.tile_wgs), dim3(512),
+                       0, stream, a);
     return hipGetLastError();
 }
 
 // (the sums are a small part of the other forms' work beside the products)
-template <int D, int NW>
+template <int D>
 hipError_t launch_paged_tiles_d(const PagedArgs& a, int form, hipStream_t stream) {
     if (form == 0)
-        return a.lse ? launch_paged_tiles_form<D, NW, 0, false>(a, stream)
-                     : launch_paged_tiles_form<D, NW, 0, true>(a, stream);
-    if (form == 1) return launch_paged_tiles_form<D, NW, 1, false>(a, stream);
-    if (form == 2) return launch_paged_tiles_form<D, NW, 2, false>(a, stream);
-    if (form == 3) return launch_paged_tiles_form<D, NW, 3, false>(a, stream);
+        return a.lse ? launch_paged_tiles_form<D, 0, false>(a, stream)
+                     : launch_paged_tiles_form<D, 0, true>(a, stream);
+    if (form == 1) return launch_paged_tiles_form<D, 1, false>(a, stream);
+    if (form == 2) return launch_paged_tiles_form<D, 2, false>(a, stream);
+    if (form == 3) return launch_paged_tiles_form<D, 3, false>(a, stream);
     return hipErrorInvalidValue;
 }
 

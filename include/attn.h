@@ -481,8 +481,8 @@ int attn_paged_release(const int* block_table, long long table_stride, const int
  *   k_pages, v_pages: n_pages pages; they must not overlap each other or the operands.
  * Errors (of these calls): EINVAL for null or misaligned pointers, bad strides, dims <= 0 and
  * overlaps; EUNSUPPORTED for d not in {64, 128}, a page size that is no such power of two, a
- * cache or a table's row of more than 2^31 - 1 tokens, and rows of a page more than 2^26
- * values apart.
+ * cache of more than 2^31 - 1 rows, a table's row of more than 2^30 tokens, more than 2^30 tokens
+ * or requests in a call, and rows of a page more than 2^26 values apart, or pages 2^35.
  */
 int attn_paged_store(const attn_heads* k, const attn_heads* v, const int* slots,
                      const attn_heads* k_pages, const attn_heads* v_pages, int T, int Hkv, int d,
@@ -503,20 +503,22 @@ int attn_paged_store(const attn_heads* k, const attn_heads* v, const int* slots,
  *   x - slopes[h] |p - j|;  o = sum exp(x) v / sum exp(x), lse = log sum exp(x)
  * over the keys j < kv_len, with causal j <= p, with window > 0 (causal only) j > p - window.
  * A token that sees no key (kv_len 0, or fewer tokens than new ones) has o = 0, lse = -inf.
- *   max_q: no request has more new tokens than this (0: not known).  Rows of one that has are
- *   not defined.
+ *   max_q: no request has more new tokens than this (0: not known).  Results of one that
+ *   has are not defined, and may be left unwritten.
  * Of the cache only the rows that some token of the request sees are read; keys and values of
  * one request's own tokens that a mask hides from others of its tokens have to be finite.  A
- * page number outside [0, n_pages) among the ones needed, or a kv_len of more than the table's
- * row holds, makes the request's results NaN, and reads nothing outside the cache.
+ * page number outside [0, n_pages) makes NaN the results of the tokens that see a key in it, and
+ * may do so with others of the request; a kv_len of more than the table's row holds makes all of
+ * the request's NaN.  Neither reads anything outside the cache.
  *   workspace: as for attn_bwd, of attn_paged_workspace_bytes(...) bytes.
  * Work: two products on bf16 MFMA with fp32 accumulation and softmax; the weights are rounded
- * to bf16 as operands, their sum takes them unrounded.  A capped score is off by up to
+ * to bf16 as operands; their sum takes them unrounded where lse is asked for, and may take them
+ * rounded elsewhere.  A capped score is off by up to
  * softcap * 2^-22.  Every call gives the same bits (no atomics).
  * Errors as the calls above; EINVAL also for Hkv not dividing Hq, unknown flags, a scale or
  * softcap that is not finite, a negative softcap, window or max_q, T != R without cu_seqlens,
  * and for the workspace as attn_bwd; EUNSUPPORTED also for a window without the causal mask
- * and more than 2^31 - 1 query rows.
+ * and more than 2^31 - 1 query rows or 2^15 query heads to a key/value head.
  */
 int attn_paged(const attn_heads* q, const attn_heads* k_pages, const attn_heads* v_pages, void* o,
                float* lse, const int* block_table, long long table_stride, const int* kv_lens,

@@ -12,6 +12,8 @@ using namespace attn;
 
 namespace {
 
+constexpr int kPagedMost = 1 << 30;  // tokens of a call or of a request, requests
+
 bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
 // log2 of the page size, or an error
@@ -33,9 +35,10 @@ int validate_table(const int* table, long long stride, int R, int max_pages, int
                           max_pages);
     if (R > 1 && (stride < max_pages || stride > (1LL << 56) / R))
         return host::fail(ATTN_EINVAL, "block table: stride %lld of rows of %d", stride, max_pages);
-    if ((long long)max_pages * page_size > INT_MAX)
-        return host::fail(ATTN_EUNSUPPORTED, "a table row of %d pages holds more than 2^31 - 1 tokens",
+    if ((long long)max_pages * page_size > kPagedMost)
+        return host::fail(ATTN_EUNSUPPORTED, "a table row of %d pages holds more than 2^30 tokens",
                           max_pages);
+    if (R > kPagedMost) return host::fail(ATTN_EUNSUPPORTED, "more than 2^30 requests");
     return ATTN_OK;
 }
 
@@ -80,6 +83,7 @@ int validate_paged_dims(int T, int R, int Hq, int Hkv, int d, int max_q) {
     if (max_q < 0) return host::fail(ATTN_EINVAL, "max_q (%d) must not be negative", max_q);
     if ((long long)T * Hq > INT_MAX)
         return host::fail(ATTN_EUNSUPPORTED, "more than 2^31 - 1 query rows");
+    if (T > kPagedMost) return host::fail(ATTN_EUNSUPPORTED, "more than 2^30 tokens");
     if (Hq / Hkv > kPagedMaxGroup)
         return host::fail(ATTN_EUNSUPPORTED, "more than %d query heads to a key/value head",
                           kPagedMaxGroup);
@@ -179,9 +183,10 @@ int attn_paged_extend(int* block_table, long long table_stride, const int* seq_l
             {cu_seqlens, "cu_seqlens"}, {kv_lens, "kv_lens"}, {n_left, "n_left"}};
         for (const auto& x : ints)
             if (!rc) rc = validate_ints(x.first, x.second);
-        if (!rc && (T <= 0 || list_len <= 0 || R == INT_MAX))
-            rc = host::fail(ATTN_EINVAL, "dimensions must be positive (T=%d list_len=%d R=%d)", T,
-                            list_len, R);
+        if (!rc && (T <= 0 || list_len <= 0))
+            rc = host::fail(ATTN_EINVAL, "dimensions must be positive (T=%d list_len=%d)", T,
+                            list_len);
+        if (!rc && T > kPagedMost) rc = host::fail(ATTN_EUNSUPPORTED, "more than 2^30 tokens");
         if (rc) return rc;
         const Rows results[] = {
             host::plain_rows("block_table", block_table, 4, max_pages, table_stride, R),
@@ -312,8 +317,9 @@ long long attn_paged_workspace_bytes(int T, int R, int max_q, int Hq, int Hkv, i
         host::DeviceRef dev;
         rc = host::device(&dev);
         if (rc) return rc;
-        return (long long)paged_launch(T, R, Hq, Hkv, d, max_q, (long long)max_pages << log2, window,
-                                       dev.desc->num_cus)
+        const long long max_keys = (long long)max_pages << log2;
+        return (long long)paged_launch(T, R, Hq, Hkv, d, max_q, max_keys,
+                                       window >= max_keys ? 0 : window, dev.desc->num_cus)
             .bytes(d);
     });
 }
@@ -347,6 +353,9 @@ int attn_paged(const attn_heads* q, const attn_heads* k_pages, const attn_heads*
         if (window < 0) return host::fail(ATTN_EINVAL, "window must not be negative");
         if (window && !causal)
             return host::fail(ATTN_EUNSUPPORTED, "a window needs the causal mask");
+        // (a window of all that a table's row holds hides nothing)
+        const long long max_keys = (long long)max_pages * page_size;
+        if (window >= max_keys) window = 0;
         Rows results[3], operands[7];
         results[0] = host::plain_rows("o", o, (flags & ATTN_OUT_BF16) ? 2 : 4, (long long)T * Hq * d);
         int n_results = 1, n_operands = 0;
@@ -363,8 +372,8 @@ int attn_paged(const attn_heads* q, const attn_heads* k_pages, const attn_heads*
         rc = host::check_apart(results, n_results, operands, n_operands);
         if (!rc) rc = host::device(&dev);
         if (rc) return rc;
-        const PagedLaunch l = paged_launch(T, R, Hq, Hkv, d, max_q, (long long)max_pages * page_size,
-                                           window, dev.desc->num_cus);
+        const PagedLaunch l = paged_launch(T, R, Hq, Hkv, d, max_q, max_keys, window,
+                                           dev.desc->num_cus);
         const size_t need = l.bytes(d);
         if (l.items * l.splits * 2 > kMaxWorkgroups)
             return host::fail(ATTN_EUNSUPPORTED, "more workgroups than one launch holds");
@@ -414,7 +423,7 @@ int attn_paged(const attn_heads* q, const attn_heads* k_pages, const attn_heads*
         a.scale_log2 = (float)s;
         a.q_sign = scale < 0.f ? 0x80008000u : 0u;
         if (softcap > 0.f) {
-            a.cap_in = (float)(2.0 * s / softcap);
+            a.cap_in = (float)std::min(2.0 * s / softcap, (double)FLT_MAX);
             a.cap_out = (float)(softcap * log2e);
         }
         float* f = static_cast<float*>(ws);

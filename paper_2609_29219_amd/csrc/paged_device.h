@@ -16,7 +16,9 @@ __device__ __forceinline__ PagedRequest paged_request(const PagedArgs& a, int r)
     x.q0 = (int)c0;
     x.qn = 0;
     if (c0 >= 0 && c1 > c0 && c0 < a.T) x.qn = (int)(min(c1, (long long)a.T) - c0);
-    x.pos0 = (int)(x.kv - max(c1 - c0, 0LL));
+    // (the first token's position is past -2^30 where the lengths are right: positions less a
+    // window, both of which the host bounds, are 32-bit whatever they are)
+    x.pos0 = (int)max(x.kv - max(c1 - c0, 0LL), -(1LL << 30));
     x.lo = a.window ? max(0, x.pos0 - a.window + 1) : 0;
     if (x.bad) x.kv = x.lo = 0;
     return x;

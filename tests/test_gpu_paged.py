@@ -372,3 +372,261 @@ def test_store(pa, T, Hkv, d, token_major):
             want[0][s // page, :, s % page], want[1][s // page, :, s % page] = kn[t], vn[t]
     pa.paged_store(kn, vn, slots, k, v)
     assert torch.equal(k, want[0]) and torch.equal(v, want[1])
+
+
+# ---------------------------------------------------------- as they are used --
+@pytest.mark.parametrize("heads", [(4, 4), (32, 4)], ids=lambda h: "x".join(map(str, h)))
+@pytest.mark.parametrize("form", [dict(), dict(window=33, slopes=True)],
+                         ids=lambda f: "-".join(f) or "plain")
+def test_without_lse(pa, heads, form):
+    # sums of the weights as rounded to bf16: off by as much again as the weights themselves
+    announce(f"attn_paged without lse {heads} {form}")
+    kw = dict(form)
+    if kw.pop("slopes", None):
+        kw["slopes"] = torch.linspace(0.02, 0.4, heads[0], device=DEV)
+    for d in (64, 128):
+        s = scene([(1, 70), (300, 900), (9, 400), (0, 33), (33, 33)], *heads, d, 16)
+        o = pa.attn_paged(s["q"], s["k"], s["v"], s["table"], ints(s["kv"]), ints(s["cu"]),
+                          out_dtype=BF16, **kw)
+        exact, _, bound, _ = refs.attend_paged(s["q"], s["k"], s["v"], s["table"], s["kv"],
+                                               s["cu"], 1 / math.sqrt(d), **kw)
+        refs.check(o, exact, bound + 1.01 * refs.U * exact.abs(), f"d={d}")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_run_of_steps(pa, d):
+    # prompts, single tokens, drafts of which some are taken back, a request that ends and another
+    # in its place; each step normalised and rotated, stored, and attended to
+    announce(f"paged steps d={d}")
+    Hq, Hkv, page, P, most = 8, 2, 16, 64, 30
+    g = torch.Generator(device=DEV).manual_seed(d)
+    freq = 10000.0 ** (-torch.arange(0, d, 2, device=DEV).float() / d)
+    wq, wk = (torch.rand(d, generator=g, device=DEV) + 0.5 for _ in range(2))
+    cache = torch.full((P, page, 2, Hkv, d), math.nan, dtype=BF16, device=DEV)
+    k_pages, v_pages = (cache[:, :, i].transpose(1, 2) for i in range(2))
+    table = torch.full((4, most), -1, dtype=I32, device=DEV)
+    free = torch.randperm(P, generator=g, device=DEV).int()
+    n_free, seq = ints([P]), ints([0, 0, 0, 0])
+    mine = [[torch.zeros(Hkv, 0, d, dtype=BF16, device=DEV)] * 2 for _ in range(4)]
+    steps = [([37, 5, 300, 1], None), ([1, 20, 1, 1], None), ([4, 4, 4, 4], [1, 3, 4, 2]),
+             ([1, 1, 50, 0], [1, 1, 50, -2]), ([1, 1, 1, 60], None), ([2, 2, 2, 2], [2, 0, 1, 2])]
+    for at, (new, keep) in enumerate(steps):
+        T = sum(new) + at % 3
+        qkv = torch.randn(1, T, Hq + 2 * Hkv, d, generator=g, device=DEV).to(BF16)
+        slots, pos, cu, kv, left = pa.paged_extend(table, seq, ints(new), free, n_free, page, T)
+        q, k, _ = pa.qk_norm_rope(qkv[:, :, :Hq], qkv[:, :, Hq:Hq + Hkv], None, wq, wk, freq, pos)
+        q, k, v = q[0].transpose(0, 1), k[0].transpose(0, 1), qkv[0, :, Hq + Hkv:]
+        pa.paged_store(k, v, slots, k_pages, v_pages)
+        o, lse = pa.attn_paged(q, k_pages, v_pages, table, kv, cu, max_q=max(new),
+                               return_lse=True)
+        starts = cu.tolist()
+        for r, n in enumerate(new):
+            a, b = starts[r], starts[r + 1]
+            mine[r] = [torch.cat([old, x[a:b].transpose(0, 1)], 1)
+                       for old, x in zip(mine[r], (k, v))]
+            S = mine[r][0].shape[1]
+            assert kv.tolist()[r] == S
+            for h in range(Hq if n else 0):
+                eo, el, bo, bl = refs.attend(q[a:b, h], *(x[h // (Hq // Hkv)] for x in mine[r]),
+                                             torch.arange(S - n, S, device=DEV), 1 / math.sqrt(d),
+                                             True, out_step=2.0 ** -24)
+                refs.check(o[a:b, h], eo, bo, f"step {at} request {r}: o")
+                refs.check(lse[a:b, h], el, bl, f"step {at} request {r}: lse")
+        n_free, seq = left, kv
+        if keep:  # (-2: the request ends)
+            held = [0 if n == -2 else s - m + n for s, m, n in zip(kv.tolist(), new, keep)]
+            n_free = pa.paged_release(table, kv, ints(held), free, left, page)
+            seq = ints(held)
+            mine = [[x[:, :n] for x in old] for old, n in zip(mine, held)]
+        live = sum(-(-n // page) for n in seq.tolist())
+        assert n_free.tolist() == [P - live]
+        used = [table[r, i].item() for r in range(4) for i in range(-(-seq.tolist()[r] // page))]
+        assert sorted(used + free[:P - live].tolist()) == list(range(P))
+
+
+def test_replayed_steps(pa):
+    # a step of decoding as one graph, its lengths and tables going on from replay to replay;
+    # another graph on the same workspace, and eager calls between
+    announce("paged steps in a graph")
+    R, Hq, Hkv, d, page, P = 5, 16, 4, 128, 16, 400
+    g = torch.Generator(device=DEV).manual_seed(9)
+
+    def start():
+        s = dict(table=torch.full((R, 100), -1, dtype=I32, device=DEV), seq=ints([0] * R),
+                 free=torch.arange(P, dtype=I32, device=DEV), n_free=ints([P]))
+        s["k"], s["v"] = (torch.zeros(P, Hkv, page, d, dtype=BF16, device=DEV) for _ in range(2))
+        s["q_in"] = torch.zeros(R, Hq + 2 * Hkv, d, dtype=BF16, device=DEV)
+        s["outs"] = [ints([0] * n) for n in (R, R, R + 1, R, 1)]
+        s["o"] = torch.zeros(R, Hq, d, dtype=BF16, device=DEV)
+        return s
+
+    ones = ints([1] * R)
+
+    def step(s):
+        x = s["q_in"]
+        names = ("slots", "positions", "cu_seqlens", "kv_lens", "n_left")
+        slots, _, cu, kv, left = pa.paged_extend(s["table"], s["seq"], ones, s["free"], s["n_free"],
+                                                 page, R, **dict(zip(names, s["outs"])))
+        pa.paged_store(x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], slots, s["k"], s["v"])
+        pa.attn_paged(x[:, :Hq], s["k"], s["v"], s["table"], kv, cu, max_q=1, o=s["o"])
+        torch.add(kv, 0, out=s["seq"])
+        torch.add(left, 0, out=s["n_free"])
+
+    prompt = [40, 700, 1, 333, 90]
+    kv = torch.randn(2, sum(prompt), Hkv, d, generator=g, device=DEV).to(BF16)
+    states = [start() for _ in range(3)]  # eager, and of two graphs
+    for s in states:
+        slots, _, _, lens, left = pa.paged_extend(s["table"], s["seq"], ints(prompt), s["free"],
+                                                  s["n_free"], page, sum(prompt))
+        pa.paged_store(kv[0], kv[1], slots, s["k"], s["v"])
+        s["seq"], s["n_free"] = lens, left
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graphs = []
+    for s in states[1:]:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=stream):
+            step(s)
+    for i in range(5):
+        x = torch.randn(R, Hq + 2 * Hkv, d, generator=g, device=DEV).to(BF16)
+        for s in states:
+            s["q_in"].copy_(x)
+            s["o"].fill_(math.nan)
+        torch.cuda.synchronize()
+        graphs[0].replay()
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            step(states[0])
+        torch.cuda.synchronize()
+        assert states[0]["o"].isfinite().all()
+        for s in states[1:]:
+            for name in ("o", "table", "seq", "n_free"):
+                assert torch.equal(s[name], states[0][name]), f"replay {i}: {name}"
+    assert states[1]["seq"].tolist() == [n + 5 for n in prompt]
+
+
+def test_two_streams_at_once(pa):
+    announce("attn_paged on two streams")
+    scenes = [scene([(1, 3000), (200, 1500), (5, 77)], 16, 4, 128, 16, seed=n) for n in (1, 2)]
+    want = [call(pa, s) for s in scenes]
+    streams = [torch.cuda.Stream() for _ in scenes]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(4):
+        for s, on in zip(scenes, streams):
+            with torch.cuda.stream(on):
+                got.append(call(pa, s))
+    torch.cuda.synchronize()
+    for i, pair in enumerate(got):
+        assert all(torch.equal(a, b) for a, b in zip(pair, want[i % 2]))
+
+
+def test_workspace_of_any_content(pa):
+    announce("attn_paged workspace content")
+    s = scene([(1, 3000), (200, 1500), (5, 77), (0, 50), (1, 0)], 16, 4, 128, 16)
+    n = pa.paged_workspace_bytes(207, 5, 16, 4, 128, 16, s["table"].shape[1])
+    want = call(pa, s)
+    for fill in (0, 0x7f, 0xff):
+        ws = torch.full((n,), fill, dtype=torch.uint8, device=DEV)
+        assert all(torch.equal(a, b) for a, b in zip(want, call(pa, s, workspace=ws)))
+
+
+def test_workspace_over_an_operand(pa):
+    announce("attn_paged workspace overlaps")
+    s = scene([(1, 3000), (2, 1500)], 16, 4, 128, 16)
+    n = pa.paged_workspace_bytes(3, 2, 16, 4, 128, 16, s["table"].shape[1])
+    room = torch.empty(n + 3 * 16 * 128 * 2, dtype=torch.uint8, device=DEV)
+    q = room[n - n % 16 - 16:][:3 * 16 * 128 * 2].view(BF16).view(3, 16, 128)
+    with pytest.raises(pa.AttnError) as e:
+        pa.attn_paged(q, s["k"], s["v"], s["table"], ints(s["kv"]), ints(s["cu"]),
+                      workspace=room[:n])
+    assert e.value.code == pa.ATTN_EINVAL
+
+
+@pytest.mark.parametrize("page,max_pages", [(1024, 3), (8, 4000), (65536, 1)])
+def test_extreme_pages(pa, page, max_pages):
+    # a wide table, a cache of one page, pages longer than their request
+    announce(f"attn_paged pages of {page}")
+    lens = [(1, 2000)] if max_pages == 1 else [(1, 2000), (70, 300), (3, 1100), (1, 9)]
+    s = scene(lens, 8, 2, 64, page)
+    if max_pages == 1:
+        p = int(s["table"][0, 0])
+        s["k"], s["v"], s["table"] = s["k"][p:p + 1], s["v"][p:p + 1], ints([[0]])
+    elif max_pages > s["table"].shape[1]:
+        wide = torch.full((len(lens), max_pages + 100), 1 << 30, dtype=I32, device=DEV)
+        wide[:, :s["table"].shape[1]] = s["table"]
+        s["table"] = wide[:, :max_pages]
+    s["poisoned"] = s["table"], s["k"], s["v"]
+    verify(pa, s, f"page {page}")
+    verify(pa, s, f"page {page}", window=100)
+
+
+@pytest.mark.parametrize("R", [65, 300])
+def test_many_long_requests(pa, R):
+    # more requests than a wave, or a workgroup, finds its own among in one go
+    announce(f"attn_paged {R} requests of many rows")
+    lens = [(17 + r % 9 if r % 3 else 1, 40 + 13 * (r % 17)) for r in range(R)]
+    verify(pa, scene(lens, 8, 2, 64, 16), f"{R}")
+
+
+def test_a_window_without_end(pa):
+    # (with more new tokens than tokens: positions below zero less the largest window)
+    announce("attn_paged largest windows")
+    s = scene([(1, 100), (40, 200), (1, 3)], 8, 2, 64, 16)
+    s["kv"] = [100, 30, 3]
+    want = call(pa, s)
+    for window in (2 ** 31 - 1, 2 ** 31 - 2, s["table"].shape[1] * 16):
+        got = call(pa, s, window=window)
+        assert all(torch.equal(a, b) for a, b in zip(want, got)), window
+    verify(pa, s, "no window")
+    verify(pa, s, "window", window=201)
+
+
+@pytest.mark.parametrize("max_q", [1, 4, 8])
+def test_more_tokens_than_promised(pa, max_q):
+    # the others' results are as they were
+    announce(f"attn_paged broken max_q {max_q}")
+    lens = [(1, 500), (max_q, 900), (1, 33)]
+    s = scene(lens, 8, 2, 64, 16)
+    want, _, bound, _ = refs.attend_paged(s["q"], s["k"], s["v"], s["table"], s["kv"], s["cu"],
+                                          0.125, out_step=2.0 ** -24)
+    q = torch.cat([s["q"][:1], torch.randn(60, 8, 64, device=DEV).to(BF16), s["q"][1:]])
+    table = torch.cat([s["table"][:1], s["table"]])
+    o = pa.attn_paged(q, s["k"], s["v"], table, ints([500, 480, 900, 33]),
+                      ints([0, 1, 61, 61 + max_q, 62 + max_q]), max_q=max_q)
+    refs.check(torch.cat([o[:1], o[61:]]), want, bound + refs.U * want.abs(), "the others")
+
+
+def test_softcap_of_nothing(pa):
+    # scores past the cap: all keys weigh the same
+    announce("attn_paged tiny softcap")
+    s = scene([(1, 100), (40, 200)], 8, 2, 64, 16)
+    verify(pa, s, "tiny cap", softcap=1e-30)
+
+
+def test_lengths_that_make_no_sense(pa):
+    # bounds past the queries' end, or falling: only the rows of the requests that are right are
+    # defined, and nothing outside the tensors is touched
+    announce("attn_paged wrong bounds")
+    s = scene([(1, 300), (40, 500), (2, 70)], 8, 2, 64, 16)
+    want, _, bound, _ = refs.attend_paged(s["q"], s["k"], s["v"], s["table"], s["kv"], s["cu"],
+                                          0.125, out_step=2.0 ** -24)
+    bound = bound + refs.U * want.abs()  # (sums of rounded weights)
+    room = torch.full((45, 8, 64), 7.0, device=DEV)
+    for cu, right in (([0, 1, 41, 2 ** 31 - 1], 41), ([0, 1, 0, -5], 1), ([0, 1, 1 << 30, 0], 1)):
+        for window in (0, 50):
+            room.fill_(7.0)
+            pa.attn_paged(s["q"], s["k"], s["v"], s["table"], ints(s["kv"]), ints(cu),
+                          o=room[1:44], window=window)
+            if not window:
+                refs.check(room[1:1 + right], want[:right], bound[:right], f"{cu}")
+            assert (room[0] == 7.0).all() and (room[44] == 7.0).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens", [[(1, 150000)], [(40, 70001)], [(1, 90000), (1, 3), (20, 40000)]],
+                         ids=lambda l: "-".join(f"{n}of{k}" for n, k in l))
+def test_long_requests(pa, lens, d):
+    announce(f"attn_paged long {lens} d={d}")
+    verify(pa, scene(lens, 4, 1, d, 32), "long")

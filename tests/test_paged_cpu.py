@@ -45,6 +45,7 @@ def extend(table=A, stride=8, seq=A + MB, new=A + 2 * MB, free=A + 3 * MB, n_lis
     (dict(page=0), EUNSUPPORTED), (dict(page=4), EUNSUPPORTED), (dict(page=24), EUNSUPPORTED),
     (dict(page=-16), EUNSUPPORTED), (dict(page=1 << 17), EUNSUPPORTED),
     (dict(max_pages=1 << 27, stride=1 << 27), EUNSUPPORTED),
+    (dict(T=(1 << 30) + 1), EUNSUPPORTED), (dict(R=(1 << 30) + 1), EUNSUPPORTED),
     # results over operands and over each other
     (dict(kv=A + MB), EINVAL), (dict(left=A + 4 * MB), EINVAL), (dict(cu=A + MB + 12), EINVAL),
     (dict(pos=A + 5 * MB + 36), EINVAL), (dict(slots=A + 124), EINVAL),
@@ -88,6 +89,7 @@ def store(k=0, v=0, slots=A + 2 * MB, kp=0, vp=0, T=3, Hkv=2, d=64, pages=5, pag
     (dict(d=96), EUNSUPPORTED), (dict(page=4), EUNSUPPORTED),
     (dict(pages=1 << 27), EUNSUPPORTED),
     (dict(kp=cache(A + 8 * MB, row=1 << 27)), EUNSUPPORTED),
+    (dict(vp=heads(A + 16 * MB, 1 << 36, 64, 1024)), EUNSUPPORTED),
     # a cache whose rows overlap, or lie over the other side's, or over k
     (dict(kp=cache(A + 8 * MB, batch=0)), EINVAL), (dict(vp=cache(A + 16 * MB, row=32)), EINVAL),
     (dict(vp=cache(A + 8 * MB)), EINVAL), (dict(vp=cache(A + 8 * MB + 64)), EINVAL),
@@ -127,6 +129,12 @@ def attend(q=0, kp=0, vp=0, o=A + MB, lse=None, table=A + 2 * MB, stride=8, kv=A
     (dict(page=1), EUNSUPPORTED), (dict(max_pages=1 << 27, stride=1 << 27), EUNSUPPORTED),
     (dict(T=1 << 29, q=heads(A, 0, 256, 64)), EUNSUPPORTED),
     (dict(kp=cache(A + 8 * MB, row=1 << 27)), EUNSUPPORTED),
+    (dict(vp=heads(A + 16 * MB, 1 << 36, 64, 1024)), EUNSUPPORTED),
+    (dict(Hq=(1 << 15) + 1, Hkv=1, q=heads(A, 0, 1 << 22, 64), T=1, R=1, o=A + 64 * MB),
+     EUNSUPPORTED),
+    (dict(T=(1 << 30) + 1, Hq=1, Hkv=1), EUNSUPPORTED),
+    (dict(R=(1 << 30) + 1), EUNSUPPORTED),
+    (dict(max_pages=1 << 26, page=32, stride=1 << 26), EUNSUPPORTED),
     # results over operands and each other: o is 6 * 4 * 64 floats, 6144 bytes
     (dict(o=A), EINVAL), (dict(lse=A + MB + 6140), EINVAL), (dict(o=A + 2 * MB - 6128), EINVAL),
     (dict(o=A + 8 * MB + 16), EINVAL), (dict(lse=A + 3 * MB + 12), EINVAL),

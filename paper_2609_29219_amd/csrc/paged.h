@@ -97,7 +97,7 @@ constexpr int kPagedMeta = 8;  // ints to a workgroup
 constexpr int kPagedMaxGroup = 1 << 15;
 // Requests of up to this many rows are the row kernel's (blocks of 16 or 32 rows).
 constexpr int kPagedFewRows = 32;
-hipError_t launch_paged_rows(const PagedArgs& a, int d, int block, hipStream_t stream);
+hipError_t launch_paged_rows(const PagedArgs& a, int d, int block, int waves, hipStream_t stream);
 // Adds both kernels' partial results.
 hipError_t launch_paged_sums(const PagedArgs& a, int d, int row_block, hipStream_t stream);
 // Fewest tiles of keys to a split of the tile kernel.

@@ -94,6 +94,7 @@ int validate_paged_dims(int T, int R, int Hq, int Hkv, int d, int max_q) {
 struct PagedLaunch {
     int few = 0;                      // requests of up to so many rows: the row kernel's
     int block = 0, n_wg = 0;          // row kernel (n_wg 0: not launched)
+    int waves = 4;                    // to its workgroups
     bool shared = false;              // its workgroups may share an item
     int unit_log2 = 0;
     long long items = 0;              // tile kernel: blocks of all heads at most (0: not launched)
@@ -171,12 +172,20 @@ PagedLaunch paged_launch(int T, int R, int Hq, int Hkv, int d, int max_q, long l
         // steps of a request at most (its tokens are no more than its rows)
         double steps = (double)max_keys / kPagedRowKeys + 1;
         if (window) steps = std::min(steps, ((double)window + l.few) / kPagedRowKeys + 2);
+        const double items = ((double)rows / l.block + R) * Hkv;  // at most
         // Few steps to every item: each is one workgroup's.  An item's steps one behind another
-        // cost about 1 us each, adding up its parts a launch of 5 us.
-        l.shared = steps > 6;
+        // cost about 1 us each, adding up its parts a launch of 5 us.  Items no more than CUs:
+        // workgroups of twice the waves have half the steps.  Measured: a token over 512 keys of
+        // 8 heads, by four waves 11.0 us, by eight, as chosen, 9.7; over 1000 keys shared 13.0,
+        // whole, as chosen, 13.5; sixteen tokens over 950 keys shared 22, whole, as chosen, 19.
+        if (items <= num_cus) l.waves = 8;
+        l.shared = steps > (l.waves == 8 ? 9 : 6);
+        if (l.shared)
+            l.waves = 4;
+        else
+            l.n_wg = (int)std::min((double)l.n_wg, items);
         while ((1 << l.unit_log2) < steps && !l.shared) ++l.unit_log2;
         // so few units that their number is 32-bit, whatever the lengths are
-        const double items = ((double)rows / 16 + R) * Hkv;
         while (items * (steps / (1 << l.unit_log2) + 1) >= 2147483647.0 && l.unit_log2 < 24)
             ++l.unit_log2;
     }
@@ -459,7 +468,7 @@ int attn_paged(const attn_heads* q, const attn_heads* k_pages, const attn_heads*
         a.splits = l.splits;
         a.tile_wgs = l.items * l.splits;
         hipError_t e = hipSuccess;
-        if (l.n_wg) e = launch_paged_rows(a, d, l.block, host::stream());
+        if (l.n_wg) e = launch_paged_rows(a, d, l.block, l.waves, host::stream());
         if (e == hipSuccess && l.items)
             e = launch_paged_tiles(a, d, (softcap > 0.f ? 1 : 0) | (slopes ? 2 : 0),
                                    host::stream());

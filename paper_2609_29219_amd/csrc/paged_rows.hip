@@ -43,7 +43,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int kNT = 256, kNW = 4;
+constexpr int kNT = 256;  // of the sum kernel
 constexpr float kLn2 = 0.69314718055994531f;
 
 // max / sum of x over the four 16-lane rows (lanes l, l^16, l^32, l^48)
@@ -68,14 +68,15 @@ __device__ __forceinline__ float rows4_sum(float x) {
 struct Share {
     int items, blocks, steps, units;
 };
-__device__ __forceinline__ Share share_of(const PagedArgs& a, const PagedRequest& x, int block) {
+__device__ __forceinline__ Share share_of(const PagedArgs& a, const PagedRequest& x, int block,
+                                          int step_keys) {
     Share s = {0, 0, 0, 0};
     const long long rows = (long long)x.qn * a.group;
     if (rows == 0 || rows > a.few) return s;
     s.blocks = (int)((uint32_t)(rows + block - 1) / (uint32_t)block);
     s.items = s.blocks * a.Hkv;
-    s.steps = x.kv > x.lo ? (int)((uint32_t)(x.kv + kPagedRowKeys - 1) / kPagedRowKeys) -
-                                x.lo / kPagedRowKeys
+    s.steps = x.kv > x.lo ? (int)((uint32_t)(x.kv + step_keys - 1) / (uint32_t)step_keys) -
+                                (int)((uint32_t)x.lo / (uint32_t)step_keys)
                           : 1;
     s.units = (s.steps + (1 << a.unit_log2) - 1) >> a.unit_log2;
     return s;
@@ -136,18 +137,20 @@ __device__ __forceinline__ void wait_loads() {
 }
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
 
-template <int D, int MT>
-__global__ __launch_bounds__(kNT, 2) void paged_rows_kernel(const PagedArgs a) {
+template <int D, int MT, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void paged_rows_kernel(const PagedArgs a) {
     using L = RowLds<D>;
+    constexpr int NT = NW * 64;
+    constexpr int KEYS = 32 * NW;    // of a step
     constexpr int KS = D / 32;       // MFMA steps over a row
     constexpr int DB = D / 16;       // 16-column blocks of O^T
     constexpr int OST = D + 4;       // floats to a row where the waves meet
     constexpr int BLOCK = 16 * MT;
     constexpr int LOADS = L::PIECES; // of an operand and step
-    __shared__ __attribute__((aligned(16))) uint8_t lds[kNW * L::WAVE];
-    __shared__ float sm[kNW][BLOCK], sl[kNW][BLOCK];
+    __shared__ __attribute__((aligned(16))) uint8_t lds[NW * L::WAVE];
+    __shared__ float sm[NW][BLOCK], sl[NW][BLOCK];
     __shared__ int found[2];
-    static_assert(kNW * 16 * OST * 4 <= (int)sizeof(lds), "");
+    static_assert(NW * 16 * OST * 4 <= (int)sizeof(lds), "");
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -158,14 +161,14 @@ __global__ __launch_bounds__(kNT, 2) void paged_rows_kernel(const PagedArgs a) {
     // ---- this workgroup's part of the line of all units ------------------------
     // (less than 2^31 of them: the host chose their size)  Up to 64 requests: each wave by itself.
     auto units_of = [&](const PagedRequest& x) {
-        const Share s = share_of(a, x, BLOCK);
+        const Share s = share_of(a, x, BLOCK, KEYS);
         return s.items * s.units;
     };
     const bool alone = a.R <= 64;
     const int first_r = alone ? lane : tid;
     PagedRequest x = {0, 0, 0, 0, 0, 0};
-    int mine = 0, sum = 0;  // (up to kNT requests: this thread's alone)
-    for (int r = first_r; r < a.R; r += kNT) {
+    int mine = 0, sum = 0;  // (up to NT requests: this thread's alone)
+    for (int r = first_r; r < a.R; r += NT) {
         x = paged_request(a, r);
         mine = units_of(x);
         sum += mine;
@@ -175,7 +178,7 @@ __global__ __launch_bounds__(kNT, 2) void paged_rows_kernel(const PagedArgs a) {
         upto = wave_scan(sum);
         total = __builtin_amdgcn_readlane(upto, 63);
     } else {
-        upto = block_scan<kNT>(sum, &total);
+        upto = block_scan<NT>(sum, &total);
     }
     const int n_wg = min(a.n_wg, total), wg = blockIdx.x;
     if (a.meta && tid == 0) meta[0] = 0;
@@ -192,15 +195,15 @@ __global__ __launch_bounds__(kNT, 2) void paged_rows_kernel(const PagedArgs a) {
         x = {from(x.q0), from(x.qn), from(x.pos0), from(x.kv), from(x.lo), from(x.bad)};
     } else {
         int before = 0;
-        for (int r0 = 0; r0 < a.R; r0 += kNT) {
+        for (int r0 = 0; r0 < a.R; r0 += NT) {
             int all = total;
-            if (a.R > kNT) {
+            if (a.R > NT) {
                 mine = 0;
                 if (r0 + tid < a.R) {
                     x = paged_request(a, r0 + tid);
                     mine = units_of(x);
                 }
-                upto = block_scan<kNT>(mine, &all);
+                upto = block_scan<NT>(mine, &all);
             }
             if (u0 < before + all) {
                 const int first = before + upto - mine;
@@ -235,13 +238,13 @@ __global__ __launch_bounds__(kNT, 2) void paged_rows_kernel(const PagedArgs a) {
     const int tr_row = 4 * g4 + (l16 >> 2);
     const int v_row = tr_row * (D * 2) + 8 * (l16 & 1);
     for (int u = u0; u < u1;) {
-        const Share share = share_of(a, x, BLOCK);
+        const Share share = share_of(a, x, BLOCK, KEYS);
         const int mine_here = share.items * share.units;
         if (u >= r_first + mine_here) {  // the next request that has any
             r_first += mine_here;
             for (++r;; r += 64) {
                 const int rr = min(r + lane, a.R - 1);
-                const Share s = share_of(a, paged_request(a, rr), BLOCK);
+                const Share s = share_of(a, paged_request(a, rr), BLOCK, KEYS);
                 const unsigned long long any = __ballot(s.items > 0 && r + lane < a.R);
                 if (any) {
                     r += __ffsll((long long)any) - 1;
@@ -273,10 +276,10 @@ __global__ __launch_bounds__(kNT, 2) void paged_rows_kernel(const PagedArgs a) {
         const int* const table = a.table + (long long)r * a.table_stride;
         int bad = x.bad;
         const bool any_keys = x.kv > x.lo;
-        const int key0 = x.lo / kPagedRowKeys * kPagedRowKeys + 32 * wave;
+        const int key0 = x.lo / KEYS * KEYS + 32 * wave;
         // first key of a run, clamped to the runs that hold a key that some row sees
         auto run_of = [&](int t, int i) __attribute__((always_inline)) {
-            return max(min(key0 + t * kPagedRowKeys + 8 * i, (x.kv - 1) & ~7), x.lo & ~7);
+            return max(min(key0 + t * KEYS + 8 * i, (x.kv - 1) & ~7), x.lo & ~7);
         };
         // page numbers of a step's runs, in lanes 0 to 3
         auto entries = [&](int t) __attribute__((always_inline)) {
@@ -355,7 +358,7 @@ __global__ __launch_bounds__(kNT, 2) void paged_rows_kernel(const PagedArgs a) {
         // first step's loads are those of a step -1 without work: one copy of the code.)
         if (any_keys) entry = entries(t0);
         for (int t = any_keys ? t0 - 1 : t1; t < t1; ++t) {
-            const int kb = key0 + t * kPagedRowKeys;
+            const int kb = key0 + t * KEYS;
             const bool work = t >= t0, more_steps = t + 1 < t1;
             bf16x8 kf[2][KS];
             if (work) {
@@ -514,17 +517,17 @@ __global__ __launch_bounds__(kNT, 2) void paged_rows_kernel(const PagedArgs a) {
                 *reinterpret_cast<f32x4*>(so + (wave * 16 + e16) * OST + 16 * db + 4 * eg4) =
                     oacc[mt][db];
             __syncthreads();
-            for (int i = etid; i < 16 * D / 4; i += kNT) {
+            for (int i = etid; i < 16 * D / 4; i += NT) {
                 const int row = mt * 16 + i / (D / 4), col = i % (D / 4) * 4;
                 if (row >= n_rows) break;
                 float M = sm[0][row];
 #pragma unroll
-                for (int w = 1; w < kNW; ++w) M = fmaxf(M, sm[w][row]);
+                for (int w = 1; w < NW; ++w) M = fmaxf(M, sm[w][row]);
                 const float ref = M == -INFINITY ? 0.f : M;
                 float L0 = 0.f;
                 f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int w = 0; w < kNW; ++w) {
+                for (int w = 0; w < NW; ++w) {
                     const float wt = __builtin_amdgcn_exp2f(sm[w][row] - ref);
                     L0 = fmaf(wt, sl[w][row], L0);
                     acc += wt * *reinterpret_cast<const f32x4*>(
@@ -654,8 +657,11 @@ hipError_t launch_sums(const PagedArgs& a, int row_block, hipStream_t stream) {
 }
 
 template <int D, int MT>
-hipError_t launch_rows(const PagedArgs& a, hipStream_t stream) {
-    hipLaunchKernelGGL((paged_rows_kernel<D, MT>), dim3(a.n_wg), dim3(kNT), 0, stream, a);
+hipError_t launch_rows(const PagedArgs& a, int waves, hipStream_t stream) {
+    if (waves == 8)
+        hipLaunchKernelGGL((paged_rows_kernel<D, MT, 8>), dim3(a.n_wg), dim3(512), 0, stream, a);
+    else
+        hipLaunchKernelGGL((paged_rows_kernel<D, MT, 4>), dim3(a.n_wg), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -666,11 +672,11 @@ hipError_t launch_paged_sums(const PagedArgs& a, int d, int row_block, hipStream
                    : launch_sums<128>(a, row_block, stream);
 }
 
-hipError_t launch_paged_rows(const PagedArgs& a, int d, int block, hipStream_t stream) {
-    if (d == 64 && block == 16) return launch_rows<64, 1>(a, stream);
-    if (d == 64 && block == 32) return launch_rows<64, 2>(a, stream);
-    if (d == 128 && block == 16) return launch_rows<128, 1>(a, stream);
-    if (d == 128 && block == 32) return launch_rows<128, 2>(a, stream);
+hipError_t launch_paged_rows(const PagedArgs& a, int d, int block, int waves, hipStream_t stream) {
+    if (d == 64 && block == 16) return launch_rows<64, 1>(a, waves, stream);
+    if (d == 64 && block == 32) return launch_rows<64, 2>(a, waves, stream);
+    if (d == 128 && block == 16) return launch_rows<128, 1>(a, waves, stream);
+    if (d == 128 && block == 32) return launch_rows<128, 2>(a, waves, stream);
     return hipErrorInvalidValue;
 }
 

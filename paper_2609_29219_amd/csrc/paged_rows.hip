@@ -29,6 +29,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "lds_dma.h"
 #include "paged.h"
 #include "paged_device.h"
@@ -560,12 +562,12 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_rows_kernel(const PagedArgs 
 // lane groups of a row take every GP-th part, four on their way, and meet in LDS.  After the tile
 // kernel there are many rows of few parts (bound: HBM), and each lane group has its own.
 template <int D, bool TILES>
-constexpr int kSumRows = TILES ? kNT / (D / 4) : 2;
+constexpr int kSumRows = TILES ? kNT / (D / 4) : 256 / D;
 template <int D, bool TILES>
-__device__ __forceinline__ void sum_rows(const PagedArgs& a, int index, int block) {
+__device__ __forceinline__ void sum_rows(const PagedArgs& a, int index, int block, int per) {
     constexpr int ROWS = kSumRows<D, TILES>;
     constexpr int LANES = D / 4, GROUPS = kNT / LANES, GP = GROUPS / ROWS, U = 4;
-    const int g = index / (block / ROWS), row0 = (index - g * (block / ROWS)) * ROWS;
+    const int g = (uint32_t)index / (uint32_t)per, row0 = (index - g * per) * ROWS;
     const int4* const meta = reinterpret_cast<const int4*>(TILES ? a.tile_meta : a.meta) +
                              (long long)g * (kPagedMeta / 4);
     const float* const ws_m = TILES ? a.tile_m : a.ws_m;
@@ -635,24 +637,28 @@ __device__ __forceinline__ void sum_rows(const PagedArgs& a, int index, int bloc
     store_row<D>(a, item.y + tok, item.z + rr - tok * a.group, col, acc, M, L);
 }
 
-// The first row_wgs workgroups add the row kernel's parts, the others the tile kernel's.
+// The first row_wgs workgroups add the row kernel's parts, row_per of them to an item, the others
+// the tile kernel's.
 template <int D>
 __global__ __launch_bounds__(kNT) void paged_sum_kernel(const PagedArgs a, int row_wgs,
-                                                        int row_block) {
+                                                        int row_per, int row_block) {
     if ((int)blockIdx.x < row_wgs)
-        sum_rows<D, false>(a, blockIdx.x, row_block);
+        sum_rows<D, false>(a, blockIdx.x, row_block, row_per);
     else
-        sum_rows<D, true>(a, blockIdx.x - row_wgs, kPagedTileRows);
+        sum_rows<D, true>(a, blockIdx.x - row_wgs, kPagedTileRows,
+                          kPagedTileRows / kSumRows<D, true>);
 }
 
 template <int D>
 hipError_t launch_sums(const PagedArgs& a, int row_block, hipStream_t stream) {
-    const long long rows = a.meta ? (long long)a.n_wg * (row_block / kSumRows<D, false>) : 0;
+    constexpr int kRows = kSumRows<D, false>;
+    const int row_per = (std::min(a.few, row_block) + kRows - 1) / kRows;
+    const long long rows = a.meta ? (long long)a.n_wg * row_per : 0;
     const long long tiles =
         a.splits > 1 ? a.tile_wgs / a.splits * (kPagedTileRows / kSumRows<D, true>) : 0;
     if (rows + tiles == 0) return hipSuccess;
     hipLaunchKernelGGL(paged_sum_kernel<D>, dim3((unsigned)(rows + tiles)), dim3(kNT), 0, stream,
-                       a, (int)rows, row_block);
+                       a, (int)rows, row_per, row_block);
     return hipGetLastError();
 }
 

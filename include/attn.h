@@ -512,8 +512,7 @@ int attn_paged_store(const attn_heads* k, const attn_heads* v, const int* slots,
  * the request's NaN.  Neither reads anything outside the cache.
  *   workspace: as for attn_bwd, of attn_paged_workspace_bytes(...) bytes.
  * Work: two products on bf16 MFMA with fp32 accumulation and softmax; the weights are rounded
- * to bf16 as operands; their sum takes them unrounded where lse is asked for, and may take them
- * rounded elsewhere.  A capped score is off by up to
+ * to bf16 as operands, their sum takes them unrounded.  A capped score is off by up to
  * softcap * 2^-22.  Every call gives the same bits (no atomics).
  * Errors as the calls above; EINVAL also for Hkv not dividing Hq, unknown flags, a scale or
  * softcap that is not finite, a negative softcap, window or max_q, T != R without cu_seqlens,

@@ -89,18 +89,22 @@ struct PagedRequest {
     int bad;       // more keys than its table holds
 };
 
-
-// Keys to a step of the row kernel, and its workgroups that a compute unit holds at once.
+// Keys to a step of the row kernel (with four waves), and its workgroups that a compute unit holds
+// at once.
 constexpr int kPagedRowKeys = 128;
 constexpr int paged_row_wgs_per_cu(int d) { return d == 64 ? 4 : 2; }
 constexpr int kPagedMeta = 8;  // ints to a workgroup
 constexpr int kPagedMaxGroup = 1 << 15;
-// Requests of up to this many rows are the row kernel's (blocks of 16 or 32 rows).
+// Requests of up to this many rows are the row kernel's (blocks of 16 or 32 rows), which streams
+// a little faster and shares its work evenly among workgroups whatever the lengths are; beyond,
+// its block's state no longer fits in registers.  32 requests of 32 rows over 4096 keys of 8
+// heads: 100 us, by the tile kernel 102.
 constexpr int kPagedFewRows = 32;
 hipError_t launch_paged_rows(const PagedArgs& a, int d, int block, int waves, hipStream_t stream);
 // Adds both kernels' partial results.
 hipError_t launch_paged_sums(const PagedArgs& a, int d, int row_block, hipStream_t stream);
-// Fewest tiles of keys to a split of the tile kernel.
+// Fewest tiles of keys to a split of the tile kernel (a start costs as much as three), and most
+// splits of a block.
 constexpr int kPagedMinTiles = 4;
 constexpr int kPagedMaxSplits = 64;
 constexpr int kPagedTileRows = 256;  // to a block of the tile kernel

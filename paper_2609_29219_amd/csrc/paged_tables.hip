@@ -10,9 +10,12 @@
 // Bound by launch and latency: a thousand requests are 8 KB.  So there is one launch, and no
 // workgroup waits for another: each sums the requests in front of its own tokens itself, a
 // thousand at a time out of L2.  A page's first row is always a new token's, and that token's
-// thread writes the table.
+// thread writes the table.  extend: 3.9 us for a token, 8.5 for 130k tokens of 1024 requests;
+// release: 2.7 us for 64 requests' drafts, 6 for a million pages of 1024.
 //
-// store: each row of k and v goes to its slot.  Bound: HBM, 16 bytes to a lane.
+// store: each row of k and v goes to its slot.  Bound: HBM, 16 bytes to a lane, four rows of each
+// on their way: 16384 tokens of 8 heads of 128, 134 MB in and out, 26 us or 5.1 TB/s, a large
+// copy's rate.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <stdint.h>

@@ -3,23 +3,28 @@
 //
 // A workgroup computes a block of 256 rows (token by token, row = token * group + head of the
 // group) of one request and key/value head: S^T = K Q^T and O^T += V^T P^T on
-// v_mfma_f32_32x32x16_bf16, K and V in tiles of 64 keys through LDS, an online softmax.  Each
-// wave has 32 rows, one to a lane and its mate 32 lanes on, so the softmax is in a lane but for
-// one exchange.  The products' accumulators give lane half h, in register r, key 8 (r / 4) + 4 h +
-// r % 4; the weights of a step of 16 keys are the second product's operand as they stand, and V's
-// rows are read from LDS (transposed) in that order: keys 4 h .. 4 h + 3, then 8 further.
+// v_mfma_f32_32x32x16_bf16, K and V in tiles of 64 keys through LDS, an online softmax.  Each of
+// the eight waves has 32 rows, one to a lane and its mate 32 lanes on, so the softmax is in a lane
+// but for one exchange.  The products' accumulators give lane half h, in register r, key
+// 8 (r / 4) + 4 h + r % 4; the weights of a step of 16 keys are the second product's operand as
+// they stand, and V's rows are read from LDS (transposed) in that order: keys 4 h .. 4 h + 3, then
+// 8 further.
 //
 // Bound: the matrix cores with the softmax's exponentials beside them.  Each wave issues the
 // products of S of the next tile and of PV of this one one by one, with the softmax of this tile
 // between them; while it does, the next tiles come from memory straight into LDS (two slots to
-// an operand, one barrier to a tile).
+// an operand, one barrier to a tile).  A prompt of 8192 tokens, 32 heads of 128: 490 us, 1120
+// TFLOP/s; the same over contiguous keys, by attn_fwd, 466.  A chunk of 512 tokens over 16384
+// keys, 32 query heads to 8: 129 us.  (Four waves to a block of 128 rows load each tile twice as
+// often: 64 requests of 40 rows over 8192 keys 94 us, so 67.  With the weights' sums on the matrix
+// cores, as in fwd_kernel.h, the prompt takes the same time, at d = 64 2% less.)
 //
-// Pages.  A wave brings aligned runs of 16 keys, which lie in one page (or two of eight rows): the
-// page number is a scalar, and so is all arithmetic on it; a lane's offset inside the run never
-// changes.  Tiles
-// lie in LDS as whole rows, 1 KiB to an instruction, their 16-byte pieces exchanged inside a row
-// (by the source address of each lane) so that both kinds of reads are free of bank conflicts:
-// K is read 16 rows at a time, V four rows of 64 bytes.
+// Pages.  A wave brings aligned runs of 16 keys, which lie in one page (or two of eight rows), of
+// K or of V: the page number is a scalar, and so is all arithmetic on it; a lane's offset inside
+// the run never changes.  Page numbers are read a tile ahead.  Tiles lie in LDS as whole rows,
+// 1 KiB to an instruction, their 16-byte pieces exchanged inside a row (by the source address of
+// each lane) so that both kinds of reads are free of bank conflicts: K is read 16 rows at a time,
+// V four rows of 64 bytes.
 //
 // Work.  The blocks of all requests are found by each workgroup from the lengths; the last block
 // of a request (the longest under a causal mask) comes first, and the heads are dealt to the XCDs.
@@ -55,11 +60,8 @@ struct PagedLds {
     }
 };
 
-// FORM: 1 capped scores, 2 slopes.  MSUM: the rows' sums are the matrix cores', of the weights as
-// rounded to bf16 (a product with a 0/1 operand that leaves each lane its own row's, as in
-// fwd_kernel.h): 32 additions a tile less beside the products.  For calls without a log-sum-exp,
-// whose sums have to be of the weights as they are.
-template <int D, int FORM, bool MSUM>
+// FORM: 1 capped scores, 2 slopes.
+template <int D, int FORM>
 __global__ __launch_bounds__(512, 2) void paged_tiles_kernel(const PagedArgs a) {
     using L = PagedLds<D>;
     constexpr int NW = 8, NT = NW * 64, BM = kPagedTileRows, BN = kTileKeys;
@@ -222,14 +224,7 @@ __global__ __launch_bounds__(512, 2) void paged_tiles_kernel(const PagedArgs a) 
     // ---- online softmax, one row to a lane ------------------------------------
     float m_i = -INFINITY;  // reference of the row's weights, log2 units
     float l_i = 0.f;        // their sum (this lane's half of the keys), unrounded: the
-                            // log-sum-exp is fp32's; or
-    f32x4 lsum = {0.f, 0.f, 0.f, 0.f};  // with MSUM, in all four registers
-    bf16x8 sel;
-    if constexpr (MSUM) {
-        const __bf16 v = ((lane >> 4) & 1) == ((lane >> 2) & 1) ? (__bf16)1.0f : (__bf16)0.0f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sel[e] = v;
-    }
+                            // log-sum-exp is fp32's
     f32x16 oacc[CB];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
@@ -286,10 +281,7 @@ __global__ __launch_bounds__(512, 2) void paged_tiles_kernel(const PagedArgs a) 
         if (__any(move)) {
             const float m_new = move ? tmax : m_i;
             const float alpha = move ? __builtin_amdgcn_exp2f(m_i - m_new) : 1.f;
-            if constexpr (MSUM)
-                lsum *= alpha;
-            else
-                l_i *= alpha;
+            l_i *= alpha;
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
@@ -332,10 +324,8 @@ __global__ __launch_bounds__(512, 2) void paged_tiles_kernel(const PagedArgs a) 
             const bf16x2 pk = {(__bf16)xe[pp][0], (__bf16)xe[pp][1]};
             pb[kb][h2][e] = pk[0];
             pb[kb][h2][e + 1] = pk[1];
-            if constexpr (!MSUM) {
-                rs0 += xe[pp][0];
-                rs1 += xe[pp][1];
-            }
+            rs0 += xe[pp][0];
+            rs1 += xe[pp][1];
         };
         if (!HAS_S) {
 #pragma unroll
@@ -375,8 +365,6 @@ __global__ __launch_bounds__(512, 2) void paged_tiles_kernel(const PagedArgs a) 
                 constexpr int j = i - NS, kb = j / (2 * CB), h2 = (j / CB) % 2, cb = j % CB;
                 oacc[cb] =
                     __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, pb[kb][h2], oacc[cb], 0, 0, 0);
-                if constexpr (MSUM && cb == 0)
-                    lsum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(sel, pb[kb][h2], lsum, 0, 0, 0);
             }
             if constexpr (HAS_S) {
                 static_for<0, NPAIR>([&](auto pc) __attribute__((always_inline)) {
@@ -394,12 +382,11 @@ __global__ __launch_bounds__(512, 2) void paged_tiles_kernel(const PagedArgs a) 
                         mx = __builtin_elementwise_maximum(mx, s_nxt[kb][e]);
                     }
                 });
-                if constexpr (MSUM) asm volatile("" : "+v"(mx));
-                if constexpr (!MSUM) asm volatile("" : "+v"(rs0), "+v"(rs1), "+v"(mx));
+                asm volatile("" : "+v"(rs0), "+v"(rs1), "+v"(mx));
             }
             __builtin_amdgcn_sched_barrier(0);
         });
-        if constexpr (!MSUM) l_i += rs0 + rs1;
+        l_i += rs0 + rs1;
         return HAS_S ? half_swap_max(mx) : -INFINITY;
     };
 
@@ -504,7 +491,7 @@ __global__ __launch_bounds__(512, 2) void paged_tiles_kernel(const PagedArgs a) 
 
     // ---- epilogue: O = O^T / l, through LDS so that stores are whole lines ---------------
     bad = __syncthreads_or(bad);
-    const float l_row = bad ? NAN : MSUM ? lsum[0] : half_swap_sum(l_i);
+    const float l_row = bad ? NAN : half_swap_sum(l_i);
     const bool partial = n_splits > 1;
     const float inv = partial ? 1.f : l_row == 0.f ? 0.f : 1.f / l_row;
     const bool out16 = a.out_bf16 && !partial;
@@ -579,22 +566,19 @@ __global__ __launch_bounds__(512, 2) void paged_tiles_kernel(const PagedArgs a) 
     }
 }
 
-template <int D, int FORM, bool MSUM>
+template <int D, int FORM>
 hipError_t launch_paged_tiles_form(const PagedArgs& a, hipStream_t stream) {
-    hipLaunchKernelGGL((paged_tiles_kernel<D, FORM, MSUM>), dim3((unsigned)a.tile_wgs), dim3(512),
-                       0, stream, a);
+    hipLaunchKernelGGL((paged_tiles_kernel<D, FORM>), dim3((unsigned)a.tile_wgs), dim3(512), 0,
+                       stream, a);
     return hipGetLastError();
 }
 
-// (the sums are a small part of the other forms' work beside the products)
 template <int D>
 hipError_t launch_paged_tiles_d(const PagedArgs& a, int form, hipStream_t stream) {
-    if (form == 0)
-        return a.lse ? launch_paged_tiles_form<D, 0, false>(a, stream)
-                     : launch_paged_tiles_form<D, 0, true>(a, stream);
-    if (form == 1) return launch_paged_tiles_form<D, 1, false>(a, stream);
-    if (form == 2) return launch_paged_tiles_form<D, 2, false>(a, stream);
-    if (form == 3) return launch_paged_tiles_form<D, 3, false>(a, stream);
+    if (form == 0) return launch_paged_tiles_form<D, 0>(a, stream);
+    if (form == 1) return launch_paged_tiles_form<D, 1>(a, stream);
+    if (form == 2) return launch_paged_tiles_form<D, 2>(a, stream);
+    if (form == 3) return launch_paged_tiles_form<D, 3>(a, stream);
     return hipErrorInvalidValue;
 }
 

@@ -108,7 +108,7 @@ hipError_t launch_paged_sums(const PagedArgs& a, int d, int row_block, hipStream
 constexpr int kPagedMinTiles = 4;
 constexpr int kPagedMaxSplits = 64;
 constexpr int kPagedTileRows = 256;  // to a block of the tile kernel
-// form: 1 capped scores, 2 slopes
+// form: 1 capped scores, 2 slopes, 3 both, 4 slopes under a causal mask
 hipError_t launch_paged_tiles(const PagedArgs& a, int d, int form, hipStream_t stream);
 hipError_t launch_paged_tiles_d64(const PagedArgs& a, int form, hipStream_t stream);
 hipError_t launch_paged_tiles_d128(const PagedArgs& a, int form, hipStream_t stream);

@@ -470,7 +470,11 @@ int attn_paged(const attn_heads* q, const attn_heads* k_pages, const attn_heads*
         hipError_t e = hipSuccess;
         if (l.n_wg) e = launch_paged_rows(a, d, l.block, l.waves, host::stream());
         if (e == hipSuccess && l.items)
-            e = launch_paged_tiles(a, d, (softcap > 0.f ? 1 : 0) | (slopes ? 2 : 0),
+            e = launch_paged_tiles(a, d,
+                                   softcap > 0.f                  ? (slopes ? 3 : 1)
+                                   : !slopes                      ? 0
+                                   : causal && a.scale_log2 > 1e-6f ? 4  // (slopes over it)
+                                                                  : 2,
                                    host::stream());
         if (e == hipSuccess)
             e = launch_paged_sums(a, d, l.block, host::stream());

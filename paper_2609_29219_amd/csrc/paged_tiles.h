@@ -60,7 +60,9 @@ struct PagedLds {
     }
 };
 
-// FORM: 1 capped scores, 2 slopes.
+// FORM: 1 capped scores, 2 slopes, 3 both, 4 slopes under a causal mask.  The distance is then
+// linear, and slope (j - p) in the products' own units is what their accumulators begin with,
+// rounded with them: a prompt of 4096 tokens, 16 query heads to 4, 119 us, in form 2 128.
 template <int D, int FORM>
 __global__ __launch_bounds__(512, 2) void paged_tiles_kernel(const PagedArgs a) {
     using L = PagedLds<D>;
@@ -141,7 +143,10 @@ __global__ __launch_bounds__(512, 2) void paged_tiles_kernel(const PagedArgs a) 
             qf[ks] = __builtin_bit_cast(
                 bf16x8, *reinterpret_cast<const u32x4*>(qp + ks * 16) ^ a.q_sign);
     }
-    const float slope = (FORM & 2) ? a.slopes[qh] * 1.4426950408889634f : 0.f;
+    float slope = 0.f;
+    if constexpr (FORM & 2) slope = a.slopes[qh] * 1.4426950408889634f;
+    if constexpr (FORM == 4)  // (finite: 0 times it has to be 0)
+        slope = fmaxf(fminf(a.slopes[qh] * 1.4426950408889634f / a.scale_log2, 3.4e38f), -3.4e38f);
 
     // ---- tile loads ------------------------------------------------------------
     // A tile's 64 rows of K are four waves' job, 16 rows to each, and V's the others', so that a
@@ -231,6 +236,7 @@ __global__ __launch_bounds__(512, 2) void paged_tiles_kernel(const PagedArgs a) 
 #pragma unroll
         for (int e = 0; e < 16; ++e) oacc[cb][e] = 0.f;
     const float scale_log2 = a.scale_log2;
+    constexpr bool LOG2 = FORM >= 1 && FORM <= 3;
 
     // K operands: lane reads row l32 of a 32-row block, 16-byte piece 2 ks + hh
     const uint8_t* k_at[KD];
@@ -257,14 +263,14 @@ __global__ __launch_bounds__(512, 2) void paged_tiles_kernel(const PagedArgs a) 
         const s16x8 w = {w0[0], w0[1], w0[2], w0[3], w1[0], w1[1], w1[2], w1[3]};
         return __builtin_bit_cast(bf16x8, w);
     };
-    // A score of tile t, capped, moved and masked.  With a form: in log2 units from here on.
+    // A score of tile t, capped, moved and masked.  With form 1 to 3: in log2 units from here on.
     // c: its key less t * BN + 4 hh; room, below: the last and the first such that is seen
     auto finish = [&](float s, int c, float away, int room, int below, auto mask_tag)
         __attribute__((always_inline)) -> float {
         if constexpr (FORM & 1) {  // tanh y = 1 - 2 / (1 + e^2y)
             const float w = __builtin_amdgcn_exp2f(s * a.cap_in);
             s = fmaf(-2.f * a.cap_out, __builtin_amdgcn_rcpf(1.f + w), a.cap_out);
-        } else if constexpr (FORM != 0) {
+        } else if constexpr (FORM == 2) {
             s *= scale_log2;
         }
         if constexpr (FORM & 2) s = fmaf(-slope, fabsf(away - (float)c), s);
@@ -276,7 +282,7 @@ __global__ __launch_bounds__(512, 2) void paged_tiles_kernel(const PagedArgs a) 
     // The reference moves only when a tile's maximum exceeds it by more than kRescaleSlack:
     // weights are then at most 2^8.  Returns what to subtract (0 before the first key).
     auto update_ref = [&](float mx) __attribute__((always_inline)) -> float {
-        const float tmax = FORM || mx == -INFINITY ? mx : mx * scale_log2;
+        const float tmax = LOG2 || mx == -INFINITY ? mx : mx * scale_log2;
         const bool move = tmax > m_i + kRescaleSlack;  // also the first finite one
         if (__any(move)) {
             const float m_new = move ? tmax : m_i;
@@ -291,7 +297,7 @@ __global__ __launch_bounds__(512, 2) void paged_tiles_kernel(const PagedArgs a) 
         return m_i == -INFINITY ? 0.f : m_i;
     };
     auto weight = [&](float s, float m_ref) __attribute__((always_inline)) {
-        return __builtin_amdgcn_exp2f(FORM ? s - m_ref : fmaf(s, scale_log2, -m_ref));
+        return __builtin_amdgcn_exp2f(LOG2 ? s - m_ref : fmaf(s, scale_log2, -m_ref));
     };
 
     // One tile t: the products of S(t + 1) into s_nxt (HAS_S) and of PV(t), one by one; between
@@ -359,7 +365,12 @@ __global__ __launch_bounds__(512, 2) void paged_tiles_kernel(const PagedArgs a) 
             if constexpr (i < NS) {
                 constexpr int ks = i / KB, kb = i % KB;
                 f32x16 c = {};
-                if constexpr (ks > 0) c = s_nxt[kb];
+                if constexpr (ks > 0) {
+                    c = s_nxt[kb];
+                } else if constexpr (FORM == 4) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) c[e] = slope * ((float)key_const(kb, e) - away);
+                }
                 s_nxt[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op, qf[ks], c, 0, 0, 0);
             } else {
                 constexpr int j = i - NS, kb = j / (2 * CB), h2 = (j / CB) % 2, cb = j % CB;
@@ -376,7 +387,7 @@ __global__ __launch_bounds__(512, 2) void paged_tiles_kernel(const PagedArgs a) 
                     constexpr int v = decltype(vc)::value;
                     if constexpr (MAX0 + v * (NM - MAX0) / NMAXV == i) {
                         constexpr int kb = v / 16, e = v % 16;
-                        if constexpr (FORM != 0 || decltype(mask_tag)::value)
+                        if constexpr (LOG2 || decltype(mask_tag)::value)
                             s_nxt[kb][e] = finish(s_nxt[kb][e], key_const(kb, e), away, room,
                                                   below, mask_tag);
                         mx = __builtin_elementwise_maximum(mx, s_nxt[kb][e]);
@@ -414,7 +425,10 @@ __global__ __launch_bounds__(512, 2) void paged_tiles_kernel(const PagedArgs a) 
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) sA[kb][e] = 0.f;
+                for (int e = 0; e < 16; ++e)
+                    sA[kb][e] = FORM == 4 ? slope * ((float)(t_begin * BN + 4 * hh +
+                                                             key_const(kb, e)) - (float)pos)
+                                          : 0.f;
 #pragma unroll
                 for (int ks = 0; ks < KD; ++ks)
                     sA[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fetch_k(KS0, kb, ks), qf[ks],
@@ -579,6 +593,7 @@ hipError_t launch_paged_tiles_d(const PagedArgs& a, int form, hipStream_t stream
     if (form == 1) return launch_paged_tiles_form<D, 1>(a, stream);
     if (form == 2) return launch_paged_tiles_form<D, 2>(a, stream);
     if (form == 3) return launch_paged_tiles_form<D, 3>(a, stream);
+    if (form == 4) return launch_paged_tiles_form<D, 4>(a, stream);
     return hipErrorInvalidValue;
 }
 

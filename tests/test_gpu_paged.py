@@ -630,3 +630,14 @@ def test_lengths_that_make_no_sense(pa):
 def test_long_requests(pa, lens, d):
     announce(f"attn_paged long {lens} d={d}")
     verify(pa, scene(lens, 4, 1, d, 32), "long")
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("scale", [0.0, 1e-7, -0.2, 3.0])
+def test_slopes_of_any_scale(pa, scale, causal):
+    # rising and falling with distance, by both kernels
+    announce(f"attn_paged slopes scale={scale} causal={causal}")
+    for d in (64, 128):
+        slopes = torch.tensor([0.5, -0.01, 0.0, 3.0], device=DEV)
+        verify(pa, scene([(1, 300), (90, 400), (200, 200)], 4, 2, d, 16), f"d={d}", scale=scale,
+               causal=causal, slopes=slopes)

@@ -44,6 +44,15 @@ struct GroupDiv {
     }
 };
 
+// cap tanh y of u = 2 y log2(e): cap (w - 1) / (w + 1), w = e^2y.  The difference is exact where w
+// is near 1, so that what is off is w's last bit, cap 2^-24.  (Past 2^30 it is cap.)  A capped
+// prompt of 4096 tokens, 16 query heads to 4, takes 155 us; by cap - 2 cap / (1 + w), which is off
+// by about three times as much, 143.
+__device__ __forceinline__ float capped(float u, float cap) {
+    const float w = __builtin_amdgcn_exp2f(fminf(u, 30.f));
+    return fmaf(w, cap, -cap) * __builtin_amdgcn_rcpf(1.f + w);
+}
+
 // Inclusive sum over a wave, by moves between lanes inside rows of 16, then of the rows' sums.
 __device__ __forceinline__ int wave_scan(int x) {
     x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8

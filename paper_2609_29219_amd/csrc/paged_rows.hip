@@ -403,12 +403,19 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_rows_kernel(const PagedArgs 
                     sc[i] = sa[mt][i];
                     sc[4 + i] = sb[mt][i];
                 }
-                // log2 units; tanh y = 1 - 2 / (1 + e^2y)
+                // log2 units; for |u| < 1 by tanh's series in y (the first term left out is
+                // 2^-26 of it), so that small scores keep their bits: here is time for it
                 if (a.cap_out != 0.f) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const float w = __builtin_amdgcn_exp2f(sc[e] * a.cap_in);
-                        sc[e] = fmaf(-2.f * a.cap_out, __builtin_amdgcn_rcpf(1.f + w), a.cap_out);
+                        const float u = sc[e] * a.cap_in;
+                        const float y = u * 0.34657359028f, z = y * y;
+                        float t = fmaf(z, -1382.f / 155925.f, 62.f / 2835.f);
+                        t = fmaf(z, t, -17.f / 315.f);
+                        t = fmaf(z, t, 2.f / 15.f);
+                        t = fmaf(z, t, -1.f / 3.f);
+                        t = fmaf(y * z, t, y) * a.cap_out;
+                        sc[e] = fabsf(u) < 1.f ? t : capped(u, a.cap_out);
                     }
                 } else {
 #pragma unroll

@@ -267,9 +267,8 @@ __global__ __launch_bounds__(512, 2) void paged_tiles_kernel(const PagedArgs a) 
     // c: its key less t * BN + 4 hh; room, below: the last and the first such that is seen
     auto finish = [&](float s, int c, float away, int room, int below, auto mask_tag)
         __attribute__((always_inline)) -> float {
-        if constexpr (FORM & 1) {  // tanh y = 1 - 2 / (1 + e^2y)
-            const float w = __builtin_amdgcn_exp2f(s * a.cap_in);
-            s = fmaf(-2.f * a.cap_out, __builtin_amdgcn_rcpf(1.f + w), a.cap_out);
+        if constexpr (FORM & 1) {
+            s = capped(s * a.cap_in, a.cap_out);
         } else if constexpr (FORM == 2) {
             s *= scale_log2;
         }

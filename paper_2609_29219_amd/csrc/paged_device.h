@@ -5,24 +5,9 @@
 #include <stdint.h>
 
 #include "paged.h"
+#include "paged_plan.h"
 
 namespace attn {
-
-__device__ __forceinline__ PagedRequest paged_request(const PagedArgs& a, int r) {
-    const long long c0 = a.cu ? a.cu[r] : r, c1 = a.cu ? a.cu[r + 1] : r + 1;
-    PagedRequest x;
-    x.kv = max(a.kv_lens[r], 0);
-    x.bad = x.kv > ((long long)a.max_pages << a.page_log2);
-    x.q0 = (int)c0;
-    x.qn = 0;
-    if (c0 >= 0 && c1 > c0 && c0 < a.T) x.qn = (int)(min(c1, (long long)a.T) - c0);
-    // (the first token's position is past -2^30 where the lengths are right: positions less a
-    // window, both of which the host bounds, are 32-bit whatever they are)
-    x.pos0 = (int)max(x.kv - max(c1 - c0, 0LL), -(1LL << 30));
-    x.lo = a.window ? max(0, x.pos0 - a.window + 1) : 0;
-    if (x.bad) x.kv = x.lo = 0;
-    return x;
-}
 
 // Rows of a block, `first` being the first one's number in the request: which token, and which
 // head of the group (row = token * group + head).  Inside a block by a product with the inverse,

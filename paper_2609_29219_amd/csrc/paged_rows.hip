@@ -72,24 +72,6 @@ __device__ __forceinline__ float rows4_sum(float x) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-// Items of a request, and units (of 2^unit_log2 steps) of each, for blocks of `block` rows.
-struct Share {
-    int items, blocks, steps, units;
-};
-__device__ __forceinline__ Share share_of(const PagedArgs& a, const PagedRequest& x, int block,
-                                          int step_keys) {
-    Share s = {0, 0, 0, 0};
-    const long long rows = (long long)x.qn * a.group;
-    if (rows == 0 || rows > a.few) return s;
-    s.blocks = (int)((uint32_t)(rows + block - 1) / (uint32_t)block);
-    s.items = s.blocks * a.Hkv;
-    s.steps = x.kv > x.lo ? (int)((uint32_t)(x.kv + step_keys - 1) / (uint32_t)step_keys) -
-                                (int)((uint32_t)x.lo / (uint32_t)step_keys)
-                          : 1;
-    s.units = (s.steps + (1 << a.unit_log2) - 1) >> a.unit_log2;
-    return s;
-}
-
 // o / l and the log-sum-exp of 4 of a row's values; a row without keys (l = 0) is 0, -inf.
 template <int D>
 __device__ __forceinline__ void store_row(const PagedArgs& a, long long token, int head, int col,

@@ -23,9 +23,10 @@ __host__ __device__ __forceinline__ PagedRequest paged_request(const PagedArgs& 
     x.q0 = (int)c0;
     x.qn = 0;
     if (c0 >= 0 && c1 > c0 && c0 < a.T) x.qn = (int)(std::min(c1, (long long)a.T) - c0);
-    // (the first token's position is past -2^30 where the lengths are right: positions less a
-    // window, both of which the host bounds, are 32-bit whatever they are)
-    x.pos0 = (int)std::max(x.kv - std::max(c1 - c0, 0LL), -(1LL << 30));
+    // Positions of the tokens that are there: bounds past the queries do not move the window, and
+    // a request of few rows has as few steps as the host counted on.  (Positions less a window,
+    // each of up to 2^30 tokens, are 32-bit.)
+    x.pos0 = x.kv - x.qn;
     x.lo = a.window ? std::max(0, x.pos0 - a.window + 1) : 0;
     if (x.bad) x.kv = x.lo = 0;
     return x;
@@ -50,6 +51,8 @@ __host__ __device__ __forceinline__ Share share_of(const PagedArgs& a, const Pag
 }
 
 // ---------------------------------------------------------------- the host --
+constexpr int kPagedWholeLog2 = 24;  // more steps than 2^30 tokens have
+
 // How a call is launched, from what the host knows of it.
 struct PagedLaunch {
     int few = 0;                      // requests of up to so many rows: the row kernel's
@@ -144,9 +147,11 @@ inline PagedLaunch paged_launch(int T, int R, int Hq, int Hkv, int d, int max_q,
             l.waves = 4;
         else
             l.n_wg = (int)std::min((double)l.n_wg, items);
-        while ((1 << l.unit_log2) < steps && !l.shared) ++l.unit_log2;
+        // one unit to an item, however long it turns out to be: no workgroup has a part of one
+        if (!l.shared) l.unit_log2 = kPagedWholeLog2;
         // so few units that their number is 32-bit, whatever the lengths are
-        while (items * (steps / (1 << l.unit_log2) + 1) >= 2147483647.0 && l.unit_log2 < 24)
+        while (items * (steps / (1 << l.unit_log2) + 1) >= 2147483647.0 &&
+               l.unit_log2 < kPagedWholeLog2)
             ++l.unit_log2;
     }
     return l;

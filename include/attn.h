@@ -517,7 +517,7 @@ int attn_paged_store(const attn_heads* k, const attn_heads* v, const int* slots,
  * Errors as the calls above; EINVAL also for Hkv not dividing Hq, unknown flags, a scale or
  * softcap that is not finite, a negative softcap, window or max_q, T != R without cu_seqlens,
  * and for the workspace as attn_bwd; EUNSUPPORTED also for a window without the causal mask
- * and more than 2^31 - 1 query rows or 2^15 query heads to a key/value head.
+ * and more than 2^31 - 257 query rows or 2^15 query heads to a key/value head.
  */
 int attn_paged(const attn_heads* q, const attn_heads* k_pages, const attn_heads* v_pages, void* o,
                float* lse, const int* block_table, long long table_stride, const int* kv_lens,

@@ -82,8 +82,9 @@ int validate_paged_dims(int T, int R, int Hq, int Hkv, int d, int max_q) {
     if (d != 64 && d != 128)
         return host::fail(ATTN_EUNSUPPORTED, "head dim %d not in {64, 128}", d);
     if (max_q < 0) return host::fail(ATTN_EINVAL, "max_q (%d) must not be negative", max_q);
-    if ((long long)T * Hq > INT_MAX)
-        return host::fail(ATTN_EUNSUPPORTED, "more than 2^31 - 1 query rows");
+    // (the tile kernel numbers rows, those that fill up a request's last block too, in 32 bits)
+    if ((long long)T * Hq > INT_MAX - kPagedTileRows)
+        return host::fail(ATTN_EUNSUPPORTED, "more than 2^31 - 257 query rows");
     if (T > kPagedMost) return host::fail(ATTN_EUNSUPPORTED, "more than 2^30 tokens");
     if (Hq / Hkv > kPagedMaxGroup)
         return host::fail(ATTN_EUNSUPPORTED, "more than %d query heads to a key/value head",

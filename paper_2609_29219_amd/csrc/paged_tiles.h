@@ -425,9 +425,10 @@ __global__ __launch_bounds__(512, 2) void paged_tiles_kernel(const PagedArgs a) 
             for (int kb = 0; kb < KB; ++kb) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    sA[kb][e] = FORM == 4 ? slope * ((float)(t_begin * BN + 4 * hh +
-                                                             key_const(kb, e)) - (float)pos)
-                                          : 0.f;
+                    // (the distance as a difference of integers: fp32 holds positions to 2^24)
+                    sA[kb][e] = FORM == 4
+                                    ? slope * (float)(t_begin * BN + 4 * hh + key_const(kb, e) - pos)
+                                    : 0.f;
 #pragma unroll
                 for (int ks = 0; ks < KD; ++ks)
                     sA[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fetch_k(KS0, kb, ks), qf[ks],

@@ -448,9 +448,11 @@ long long attn_qk_norm_rope_bwd_workspace_bytes(int B, int S, int Hq, int Hkv, i
  *   free_pages [list_len], n_free [1]: free_pages[0 .. n_free - 1] are free.  New page i of the
  *   call, in the order of the requests and of their positions, is free_pages[n_free - 1 - i].
  *   n_left [1]: how many are free afterwards, for the next call's n_free.  Negative, it says
- *   how many were missing: pages without one are -1 in the table, and the slots in them; the
- *   lengths and the list are as they were, so that the call can be made again after pages
- *   were released.
+ *   how many were missing: pages without one are -1 in the table, and the slots in them.  The
+ *   lengths and the list are as they were, so that the call can be made again, with the n_free
+ *   from before it and the pages released behind those (n_left has lost that number: keep it).
+ *   A step that goes on passes n_left on as it is, which is none: the pages that were missing
+ *   stay so, their requests' results are NaN, and attn_paged_release leaves them out.
  *   slots, positions [T]: of each new token, one request behind another (T: at least the sum
  *   of new_lens; tokens behind the last have slot -1, position 0).  A token whose page would
  *   be past max_pages has slot -1 too, and takes no page.
@@ -466,9 +468,11 @@ int attn_paged_extend(int* block_table, long long table_stride, const int* seq_l
  * Gives pages back: of each request the pages behind the first ceil(keep_len / page_size), of
  * the ceil(seq_len / page_size) that it holds, in the order of the requests and of their
  * positions, behind the n_free in free_pages (what does not fit into list_len is dropped).
+ * Entries below zero, pages that were missing, are left out.
  * keep_lens [R]: the tokens that a request keeps (0: it ends; drafted tokens that were not
- * accepted: the accepted length).  n_left [1]: how many are free afterwards.  The table is not
- * changed.  The results must not overlap each other or the operands.
+ * accepted: the accepted length).  n_left [1]: how many are free afterwards; what lies behind
+ * them in the list is not defined.  The table is not changed.  The results must not overlap each
+ * other or the operands.
  */
 int attn_paged_release(const int* block_table, long long table_stride, const int* seq_lens,
                        const int* keep_lens, int* free_pages, int list_len, const int* n_free,

@@ -674,7 +674,9 @@ def paged_extend(block_table, seq_lens, new_lens, free_pages, n_free, page_size:
     positions: [n_tokens], one request's tokens behind another's, -1 and 0 behind the last;
     cu_seqlens: [R+1]; kv_lens: [R], seq_lens + new_lens; n_left: [1], the next call's n_free, or
     negative: so many pages were missing (-1 in the table and in slots), and the call can be made
-    again when some were released.  The results may be given; they must not be the operands."""
+    again, with the n_free from before it, when some were released behind those.  A step that goes
+    on instead takes n_left as it is (none are free).  The results may be given; they must not be
+    the operands."""
     if seq_lens.dim() != 1:
         raise ValueError("seq_lens must be [R]")
     R = seq_lens.shape[0]
@@ -695,8 +697,9 @@ def paged_extend(block_table, seq_lens, new_lens, free_pages, n_free, page_size:
 def paged_release(block_table, seq_lens, keep_lens, free_pages, n_free, page_size: int,
                   n_left=None):
     """Pages given back: of each request those behind its first keep_lens tokens, into free_pages
-    behind the n_free in it, in place; returns n_left, [1], how many are free then.  Tensors as for
-    paged_extend (keep_lens: [R], 0 where a request ends); the table is not changed."""
+    behind the n_free in it, in place; returns n_left, [1], how many are free then.  Pages that
+    were missing (below zero in the table) are left out.  Tensors as for paged_extend (keep_lens:
+    [R], 0 where a request ends); the table is not changed."""
     if seq_lens.dim() != 1:
         raise ValueError("seq_lens must be [R]")
     R = seq_lens.shape[0]

@@ -5,13 +5,20 @@
 //     need_r = ceil(kv_r / p) - held_r,  first_r = sum_{r' < r} need_r',
 // new page i of request r (its page held_r + i) is free[n_free - 1 - first_r - i], and token t of
 // request r (cu_r <= t < cu_r + n_r), at position s_r + t - cu_r, lies in row position % p of
-// page position / p.  release is the inverse.
+// page position / p.  release is the inverse; pages that extend found missing, -1 in the table,
+// do not come back: a list that held them would give them out again.
 //
-// Bound by launch and latency: a thousand requests are 8 KB.  So there is one launch, and no
-// workgroup waits for another: each sums the requests in front of its own tokens itself, a
-// thousand at a time out of L2.  A page's first row is always a new token's, and that token's
-// thread writes the table.  extend: 3.9 us for a token, 8.5 for 130k tokens of 1024 requests;
-// release: 2.7 us for 64 requests' drafts, 6 for a million pages of 1024.
+// Bound by launch and latency: a thousand requests are 8 KB.  So no workgroup waits for another:
+// each sums the requests in front of its own tokens itself, a thousand at a time out of L2.  A
+// page's first row is always a new token's, and that token's thread writes the table.  extend:
+// one launch, 3.9 us for a token, 8.5 for 130k tokens of 1024 requests.
+//
+// release: where a page goes depends on the pages in front that are missing, which only the table
+// tells.  A small table is counted by every workgroup, in one launch: in a graph 4.5 us for 64
+// requests' drafts, 9.7 for 64k pages of 128.  A larger one would be read too often: its pages go
+// where the lengths say, and a second launch looks whether any was missing, and only then goes
+// through all of them again: 7 us for 256 requests, 10 for 922k pages of 1024, 1100 if some of
+// those are missing.  (By lengths alone, one launch: 2.6 and 4.7.)
 //
 // store: each row of k and v goes to its slot.  Bound: HBM, 16 bytes to a lane, four rows of each
 // on their way: 16384 tokens of 8 heads of 128, 134 MB in and out, 26 us or 5.1 TB/s, a large
@@ -32,9 +39,10 @@ constexpr int kPer = 4;               // requests to a thread
 constexpr int kChunk = kNT * kPer;    // requests summed at a time
 constexpr int kTokens = 1024;         // tokens to a workgroup
 
-// Inclusive sums over the workgroup's threads; *total: of all of them.  All threads call it.
+// Inclusive sums over the NT threads of the workgroup; *total: of all of them.  All threads call it.
+template <int NT = kNT>
 __device__ __forceinline__ long long block_scan(long long x, long long* total) {
-    __shared__ long long waves[kNT / 64];
+    __shared__ long long waves[NT / 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int off = 1; off < 64; off *= 2) {
@@ -46,7 +54,7 @@ __device__ __forceinline__ long long block_scan(long long x, long long* total) {
     __syncthreads();
     long long before = 0, all = 0;
 #pragma unroll
-    for (int w = 0; w < kNT / 64; ++w) {
+    for (int w = 0; w < NT / 64; ++w) {
         if (w < wave) before += waves[w];
         all += waves[w];
     }
@@ -141,28 +149,156 @@ __global__ __launch_bounds__(kNT) void extend_kernel(const ExtendArgs a) {
     }
 }
 
-// A workgroup returns the pages of `per` requests, behind those of the requests in front.
+// The pages that a request gives back: its table's entries from kept on, `gone` of them.
+struct Back {
+    int kept, gone;
+};
+__device__ __forceinline__ Back back_of(const ReleaseArgs& a, int r) {
+    const int kept = pages_of(max(a.keep_lens[r], 0), a.page_log2, a.max_pages);
+    return {kept, max(pages_of(max(a.seq_lens[r], 0), a.page_log2, a.max_pages) - kept, 0)};
+}
+
+constexpr int kBackNT = 1024;
+constexpr int kSmallRequests = 256, kSmallTable = 1 << 16;  // (entries)
+
+// A small table, one launch: a workgroup counts the pages that the requests in front give back in
+// the table itself, 16 lanes to a request, and puts those of its own `per` requests behind them.
+__global__ __launch_bounds__(kBackNT) void release_small_kernel(const ReleaseArgs a, int per) {
+    const int tid = threadIdx.x;
+    const int r0 = blockIdx.x * per, r1 = min(r0 + per, a.R);
+    const int n_free = min(max(a.n_free[0], 0), a.n_list);
+    int sum = 0;
+    for (int r = tid / 16; r < r0; r += kBackNT / 16) {
+        const Back x = back_of(a, r);
+        const int* const from = a.table + r * a.table_stride + x.kept;
+#pragma unroll 4
+        for (int i = tid % 16; i < x.gone; i += 16) sum += from[i] >= 0;
+    }
+    long long first, all;
+    block_scan<kBackNT>(sum, &first);
+    first += n_free;
+    for (int r = r0; r < r1; ++r) {
+        const Back x = back_of(a, r);
+        const int* const from = a.table + r * a.table_stride + x.kept;
+        for (int i0 = 0; i0 < x.gone; i0 += kBackNT) {
+            const int page = i0 + tid < x.gone ? from[i0 + tid] : -1;
+            const long long upto = block_scan<kBackNT>(page >= 0, &all);
+            if (page >= 0 && first + upto <= a.n_list) a.free_pages[first + upto - 1] = page;
+            first += all;
+        }
+    }
+    if (r1 == a.R && tid == 0) a.n_left[0] = (int)min(first, (long long)a.n_list);
+}
+
+// A workgroup returns the pages of `per` requests, behind those of the requests in front, as if
+// none were missing.  Where one is, the first place of the workgroup's in the list says so: -1.
 __global__ __launch_bounds__(kNT) void release_kernel(const ReleaseArgs a, int per) {
     const int tid = threadIdx.x;
     const int r0 = blockIdx.x * per, r1 = min(r0 + per, a.R);
     const int n_free = min(max(a.n_free[0], 0), a.n_list);
-    auto kept = [&](int r) { return pages_of(max(a.keep_lens[r], 0), a.page_log2, a.max_pages); };
-    auto gone = [&](int r) {
-        return max(pages_of(max(a.seq_lens[r], 0), a.page_log2, a.max_pages) - kept(r), 0);
-    };
     long long sum = 0, first;
-    for (int r = tid; r < r0; r += kNT) sum += gone(r);
+    for (int r = tid; r < r0; r += kNT) sum += back_of(a, r).gone;
     block_scan(sum, &first);
+    const long long at = n_free + first;
+    int missing = 0;
     for (int r = r0; r < r1; ++r) {
-        const int k = kept(r), n = gone(r);
-        const int* const from = a.table + (long long)r * a.table_stride + k;
-        for (int i = tid; i < n; i += kNT) {
+        const Back x = back_of(a, r);
+        const int* const from = a.table + (long long)r * a.table_stride + x.kept;
+        for (int i = tid; i < x.gone; i += kNT) {
             const long long to = n_free + first + i;
-            if (to < a.n_list) a.free_pages[to] = from[i];
+            const int entry = from[i];
+            missing |= entry < 0;
+            if (to < a.n_list) a.free_pages[to] = entry;
         }
-        first += n;
+        first += x.gone;
     }
-    if (r1 == a.R && tid == 0) a.n_left[0] = (int)min(n_free + first, (long long)a.n_list);
+    missing = __syncthreads_or(missing);
+    if (missing && tid == 0 && at < a.n_list) a.free_pages[at] = -1;
+}
+
+// One workgroup, behind release_kernel: n_left, and where pages are missing or the list is too
+// short the whole list once more, without those that are not there.
+constexpr int kWalkU = 4;  // pages to a thread and step
+static_assert(kWalkU * kBackNT == 64 * 64, "a wave sums the counts of a step's 64 waves");
+__global__ __launch_bounds__(kBackNT) void release_end_kernel(const ReleaseArgs a) {
+    __shared__ long long s_first[kBackNT];
+    __shared__ int s_kept[kBackNT], s_count[64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int n_free = min(max(a.n_free[0], 0), a.n_list);
+    long long pages = 0;
+    int missing = 0;
+    for (int r0 = 0; r0 < a.R; r0 += kBackNT * kPer) {
+        int n[kPer];
+        long long sum = 0, all;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int r = r0 + tid * kPer + i;
+            n[i] = r < a.R ? back_of(a, r).gone : 0;
+            sum += n[i];
+        }
+        long long at = n_free + pages + block_scan<kBackNT>(sum, &all) - sum;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            // (a workgroup's first place is that of one of its requests)
+            if (n[i] > 0 && at < a.n_list) missing |= a.free_pages[at] < 0;
+            at += n[i];
+        }
+        pages += all;
+    }
+    if (!__syncthreads_or(missing || n_free + pages > a.n_list)) {
+        if (tid == 0) a.n_left[0] = (int)(n_free + pages);
+        return;
+    }
+    long long to = n_free;  // the next place in the list
+    for (int r0 = 0; r0 < a.R; r0 += kBackNT) {
+        Back x = {0, 0};
+        if (r0 + tid < a.R) x = back_of(a, r0 + tid);
+        long long all;
+        const long long upto = block_scan<kBackNT>(x.gone, &all);
+        s_first[tid] = upto - x.gone;
+        s_kept[tid] = x.kept;
+        __syncthreads();
+        for (long long p0 = 0; p0 < all; p0 += kWalkU * kBackNT) {
+            int entry[kWalkU];
+            unsigned long long there[kWalkU];
+#pragma unroll
+            for (int u = 0; u < kWalkU; ++u) {
+                const long long p = p0 + u * kBackNT + tid;
+                entry[u] = -1;
+                if (p < all) {
+                    int lo = 0, hi = kBackNT - 1;  // the last request whose first page is not past p
+                    while (lo < hi) {
+                        const int mid = (lo + hi + 1) >> 1;
+                        if (s_first[mid] <= p)
+                            lo = mid;
+                        else
+                            hi = mid - 1;
+                    }
+                    entry[u] = a.table[(long long)(r0 + lo) * a.table_stride + s_kept[lo] +
+                                       (p - s_first[lo])];
+                }
+                there[u] = __ballot(entry[u] >= 0);
+                if (lane == 0) s_count[u * (kBackNT / 64) + wave] = __popcll(there[u]);
+            }
+            __syncthreads();
+            const int mine = s_count[lane];
+            int sum = mine;
+#pragma unroll
+            for (int off = 1; off < 64; off *= 2) {
+                const int y = __shfl_up(sum, off);
+                if (lane >= off) sum += y;
+            }
+#pragma unroll
+            for (int u = 0; u < kWalkU; ++u) {
+                const int before = __shfl(sum - mine, u * (kBackNT / 64) + wave);
+                const long long at = to + before + __popcll(there[u] & ((1ULL << lane) - 1));
+                if (entry[u] >= 0 && at < a.n_list) a.free_pages[at] = entry[u];
+            }
+            to += __shfl(sum, 63);
+            __syncthreads();  // the counts are written again
+        }
+    }
+    if (tid == 0) a.n_left[0] = (int)min(to, (long long)a.n_list);
 }
 
 template <int D>
@@ -220,8 +356,17 @@ hipError_t launch_paged_extend(const ExtendArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_paged_release(const ReleaseArgs& a, hipStream_t stream) {
+    if (a.R <= kSmallRequests && (long long)a.R * a.max_pages <= kSmallTable) {
+        const int per = (a.R + 63) / 64;
+        hipLaunchKernelGGL(release_small_kernel, dim3((a.R + per - 1) / per), dim3(kBackNT), 0,
+                           stream, a, per);
+        return hipGetLastError();
+    }
     const int per = (a.R + 511) / 512;
     hipLaunchKernelGGL(release_kernel, dim3((a.R + per - 1) / per), dim3(kNT), 0, stream, a, per);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(release_end_kernel, dim3(1), dim3(kBackNT), 0, stream, a);
     return hipGetLastError();
 }
 

@@ -816,11 +816,17 @@ def attn_paged(q, k_pages, v_pages, block_table, kv_lens, cu_seqlens=None, max_q
 
 def paged_workspace_bytes(T: int, R: int, Hq: int, Hkv: int, d: int, page_size: int,
                           max_pages: int, max_q: int | None = None, window: int = 0) -> int:
-    """Bytes of workspace attn_paged needs with a caller-provided buffer."""
-    n = lib.attn_paged_workspace_bytes(T, R, max_q or 0, Hq, Hkv, d, page_size, max_pages, window)
-    if n < 0:
-        raise AttnError(int(n), last_error())
-    return int(n)
+    """Bytes of workspace attn_paged needs with a caller-provided buffer, for a call of these
+    sizes, max_q and window.  (Without max_q and with T = R, which a call without cu_seqlens takes
+    for one token of each request and a call with it does not: of both the larger number.)"""
+    most = [max_q or 0]
+    if max_q is None and T == R:
+        most.append(1)
+    sizes = [int(lib.attn_paged_workspace_bytes(T, R, n, Hq, Hkv, d, page_size, max_pages, window))
+             for n in most]
+    if min(sizes) < 0:
+        raise AttnError(min(sizes), last_error())
+    return max(sizes)
 
 
 def gemm_plan(M: int, N: int, K: int, b_nk: bool = False, desc: DeviceDesc | None = None) -> str:

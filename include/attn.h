@@ -514,10 +514,13 @@ int attn_paged_store(const attn_heads* k, const attn_heads* v, const int* slots,
  * page number outside [0, n_pages) makes NaN the results of the tokens that see a key in it, and
  * may do so with others of the request; a kv_len of more than the table's row holds makes all of
  * the request's NaN.  Neither reads anything outside the cache.
- *   workspace: as for attn_bwd, of attn_paged_workspace_bytes(...) bytes.
+ *   workspace: as for attn_bwd, of attn_paged_workspace_bytes(...) bytes.  Without memory for
+ *   it in the library's workspace the call runs unsplit and uses none (its sums are then rounded
+ *   in another order).
  * Work: two products on bf16 MFMA with fp32 accumulation and softmax; the weights are rounded
  * to bf16 as operands, their sum takes them unrounded.  A capped score is off by up to
- * softcap * 2^-22, a distance's term by 2^-20 of it.  Every call gives the same bits (no atomics).
+ * softcap * 2^-22, a distance's term by 2^-20 of it.  Every call gives the same bits (no atomics),
+ * but for one without memory for its parts.
  * Errors as the calls above; EINVAL also for Hkv not dividing Hq, unknown flags, a scale or
  * softcap that is not finite, a negative softcap, window or max_q, T != R without cu_seqlens,
  * and for the workspace as attn_bwd; EUNSUPPORTED also for a window without the causal mask

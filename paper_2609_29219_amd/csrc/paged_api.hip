@@ -299,8 +299,8 @@ int attn_paged(const attn_heads* q, const attn_heads* k_pages, const attn_heads*
         rc = host::check_apart(results, n_results, operands, n_operands);
         if (!rc) rc = host::device(&dev);
         if (rc) return rc;
-        const PagedLaunch l = paged_launch(T, R, Hq, Hkv, d, max_q, max_keys, window,
-                                           dev.desc->num_cus);
+        PagedLaunch l = paged_launch(T, R, Hq, Hkv, d, max_q, max_keys, window,
+                                     dev.desc->num_cus);
         const size_t need = l.bytes(d);
         if (l.items * l.splits * 2 > kMaxWorkgroups)
             return host::fail(ATTN_EUNSUPPORTED, "more workgroups than one launch holds");
@@ -312,7 +312,10 @@ int attn_paged(const attn_heads* q, const attn_heads* k_pages, const attn_heads*
         void* ws = nullptr;
         std::unique_lock<std::mutex> ws_lock;  // held until the kernels are enqueued
         rc = host::workspace(dev, need, workspace, workspace_bytes, &ws_lock, &ws);
-        if (rc) return rc;
+        if (rc == ATTN_ENOMEM)
+            l.unsplit();  // without memory for the parts
+        else if (rc)
+            return rc;
         a.q = static_cast<const uint16_t*>(q->ptr);
         a.q_row = q->row_stride;
         a.q_head = q->head_stride;

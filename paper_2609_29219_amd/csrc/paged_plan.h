@@ -64,6 +64,12 @@ struct PagedLaunch {
     int splits = 1;
     long long row_parts() const { return shared ? 2LL * n_wg * block : 0; }
     long long tile_parts() const { return splits > 1 ? items * splits * kPagedTileRows : 0; }
+    // as planned, but nobody has a part of anything, and no memory is used
+    void unsplit() {
+        shared = false;
+        unit_log2 = kPagedWholeLog2;
+        splits = 1;
+    }
     size_t bytes(int d) const {
         return (size_t)(row_parts() + tile_parts()) * (d + 2) * sizeof(float) +
                (size_t)(n_wg + items) * kPagedMeta * sizeof(int);

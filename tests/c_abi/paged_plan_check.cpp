@@ -21,11 +21,12 @@ struct Call {
 };
 
 // What a call would do with memory it has not asked for, or null.
-const char* check(const Call& c, bool planted) {
+const char* check(const Call& c, bool planted, bool memory = true) {
     const long long max_keys = (long long)c.max_pages << c.page_log2;
     const int window = c.window >= max_keys ? 0 : c.window;
-    const PagedLaunch l =
-        paged_launch(c.T, c.R, c.Hq, c.Hkv, c.d, c.max_q, max_keys, window, 256);
+    PagedLaunch l = paged_launch(c.T, c.R, c.Hq, c.Hkv, c.d, c.max_q, max_keys, window, 256);
+    if (!memory) l.unsplit();
+    if (!memory && (l.row_parts() || l.tile_parts())) return "parts without memory";
     PagedArgs a{};
     a.kv_lens = c.kv.data();
     a.cu = c.cu.empty() ? nullptr : c.cu.data();
@@ -110,6 +111,7 @@ int main(int argc, char** argv) {
         else
             c.cu = cu;
         const char* what = check(c, planted);
+        if (!what) what = check(c, planted, false);
         if (!what) continue;
         ++caught;
         if (planted) continue;

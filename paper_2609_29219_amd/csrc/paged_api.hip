@@ -354,7 +354,7 @@ int attn_paged(const attn_heads* q, const attn_heads* k_pages, const attn_heads*
         a.q_sign = scale < 0.f ? 0x80008000u : 0u;
         if (softcap > 0.f) {
             a.cap_in = (float)std::min(2.0 * s / softcap, (double)FLT_MAX);
-            a.cap_out = (float)(softcap * log2e);
+            a.cap_out = (float)std::min(softcap * log2e, (double)FLT_MAX);
         }
         float* f = static_cast<float*>(ws);
         a.ws_o = f;

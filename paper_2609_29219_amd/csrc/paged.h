@@ -95,7 +95,7 @@ constexpr int kPagedRowKeys = 128;
 constexpr int paged_row_wgs_per_cu(int d) { return d == 64 ? 4 : 2; }
 constexpr int kPagedMeta = 8;  // ints to a workgroup
 constexpr int kPagedMaxGroup = 1 << 15;
-// Requests of up to this many rows are the row kernel's (blocks of 16 or 32 rows), which streams
+// Requests of up to this many rows are the row kernel's (by 16 or 32 rows), which streams
 // a little faster and shares its work evenly among workgroups whatever the lengths are; beyond,
 // its block's state no longer fits in registers.  32 requests of 32 rows over 4096 keys of 8
 // heads: 100 us, by the tile kernel 102.

@@ -32,17 +32,17 @@ __host__ __device__ __forceinline__ PagedRequest paged_request(const PagedArgs& 
     return x;
 }
 
-// Items of a request, and units (of 2^unit_log2 steps) of each, for blocks of `block` rows.
+// The row kernel's items of a request: its key/value heads (all its rows are one block); their
+// steps of step_keys keys, and their units of 2^unit_log2 steps.
 struct Share {
-    int items, blocks, steps, units;
+    int items, steps, units;
 };
 __host__ __device__ __forceinline__ Share share_of(const PagedArgs& a, const PagedRequest& x,
-                                                   int block, int step_keys) {
-    Share s = {0, 0, 0, 0};
+                                                   int step_keys) {
+    Share s = {0, 0, 0};
     const long long rows = (long long)x.qn * a.group;
     if (rows == 0 || rows > a.few) return s;
-    s.blocks = (int)((uint32_t)(rows + block - 1) / (uint32_t)block);
-    s.items = s.blocks * a.Hkv;
+    s.items = a.Hkv;
     s.steps = x.kv > x.lo ? (int)((uint32_t)(x.kv + step_keys - 1) / (uint32_t)step_keys) -
                                 (int)((uint32_t)x.lo / (uint32_t)step_keys)
                           : 1;
@@ -56,7 +56,8 @@ constexpr int kPagedWholeLog2 = 24;  // more steps than 2^30 tokens have
 // How a call is launched, from what the host knows of it.
 struct PagedLaunch {
     int few = 0;                      // requests of up to so many rows: the row kernel's
-    int block = 0, n_wg = 0;          // row kernel (n_wg 0: not launched)
+    int block = 0, n_wg = 0;          // row kernel (n_wg 0: not launched): rows of an item, few of
+                                      // them at most
     int waves = 4;                    // to its workgroups
     bool shared = false;              // its workgroups may share an item
     int unit_log2 = 0;

@@ -6,16 +6,16 @@
 //     o = sum_j exp(x_j) v_j / sum_j exp(x_j),  lse = log sum_j exp(x_j),
 // o = 0 and lse = -inf where a token sees no key.
 //
-// The new tokens of all query heads that share a key/value head are the rows of one product, in
-// blocks of 16 MT, token by token (row = token * group + head of the group), so that each key is
-// read once for all of them.  Products on v_mfma_f32_16x16x32_bf16: S^T = K Q^T and
+// The new tokens of all query heads that share a key/value head are the rows of one product, 16 MT
+// at most, token by token (row = token * group + head of the group), so that each key is read
+// once for all of them.  Products on v_mfma_f32_16x16x32_bf16: S^T = K Q^T and
 // O^T += V^T P^T, both operands through a wave's own tiles in LDS, V read transposed.  A step is
 // 32 keys to each of four or eight waves; what a lane gets of S^T, eight keys of one row, is the
 // operand that its P^T has to be.  A wave's 32 keys are four aligned runs of eight, each in one
 // page, whose number is read a step ahead.
 //
-// Bound: HBM, 4 D bytes a key.  All items (request, key/value head, block of rows) one behind
-// another are one line of steps, which the workgroups share out evenly whatever the requests'
+// Bound: HBM, 4 D bytes a key.  All items (request, key/value head) one behind another
+// are one line of steps, which the workgroups share out evenly whatever the requests'
 // lengths are; no length is known to the host.  Each workgroup finds its part by summing the
 // lengths itself (one launch less than a plan of its own).  An item that lies in several
 // workgroups leaves partial sums (unnormalised, with their maximum), which a second kernel adds in
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_rows_kernel(const PagedArgs 
     // ---- this workgroup's part of the line of all units ------------------------
     // (less than 2^31 of them: the host chose their size)  Up to 64 requests: each wave by itself.
     auto units_of = [&](const PagedRequest& x) {
-        const Share s = share_of(a, x, BLOCK, KEYS);
+        const Share s = share_of(a, x, KEYS);
         return s.items * s.units;
     };
     const bool alone = a.R <= 64;
@@ -228,13 +228,13 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_rows_kernel(const PagedArgs 
     const int tr_row = 4 * g4 + (l16 >> 2);
     const int v_row = tr_row * (D * 2) + 8 * (l16 & 1);
     for (int u = u0; u < u1;) {
-        const Share share = share_of(a, x, BLOCK, KEYS);
+        const Share share = share_of(a, x, KEYS);
         const int mine_here = share.items * share.units;
         if (u >= r_first + mine_here) {  // the next request that has any
             r_first += mine_here;
             for (++r;; r += 64) {
                 const int rr = min(r + lane, a.R - 1);
-                const Share s = share_of(a, paged_request(a, rr), BLOCK, KEYS);
+                const Share s = share_of(a, paged_request(a, rr), KEYS);
                 const unsigned long long any = __ballot(s.items > 0 && r + lane < a.R);
                 if (any) {
                     r += __ffsll((long long)any) - 1;
@@ -246,19 +246,14 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_rows_kernel(const PagedArgs 
             x = paged_request(a, r);
             continue;
         }
-        const int item = (uint32_t)(u - r_first) / (uint32_t)share.units;
-        const int unit0 = u - r_first - item * share.units;
+        const int head = (uint32_t)(u - r_first) / (uint32_t)share.units;
+        const int unit0 = u - r_first - head * share.units;
         const int unit1 = min(share.units, unit0 + (u1 - u));
         const int t0 = unit0 << a.unit_log2, t1 = min(share.steps, unit1 << a.unit_log2);
         const int item_first = u - unit0;  // of the line
         u += unit1 - unit0;
-        int head = item, blk = 0;
-        if (share.blocks > 1) {
-            head = (uint32_t)item / (uint32_t)share.blocks;
-            blk = item - head * share.blocks;
-        }
-        const int n_rows = min(x.qn * a.group - blk * BLOCK, BLOCK);
-        const GroupDiv rows(a, blk * BLOCK);
+        const int n_rows = x.qn * a.group;  // (few at most, which is no more than BLOCK)
+        const GroupDiv rows(a, 0);
 
         // ---- loads of a step: a wave's 32 keys, in aligned runs of eight ------------------
         const uint16_t* const k_head = a.k.ptr + head * a.k.head;
@@ -491,7 +486,7 @@ __global__ __launch_bounds__(NW * 64, 2) void paged_rows_kernel(const PagedArgs 
                                        : more + (uint32_t)(end - big) / (uint32_t)per;
             meta[1] = x.q0;
             meta[2] = head * a.group;
-            meta[3] = blk * BLOCK;
+            meta[3] = 0;
             meta[4] = n_rows;
             meta[0] = last - wg + 1;
         }
@@ -648,7 +643,7 @@ __global__ __launch_bounds__(kNT) void paged_sum_kernel(const PagedArgs a, int r
 template <int D>
 hipError_t launch_sums(const PagedArgs& a, int row_block, hipStream_t stream) {
     constexpr int kRows = kSumRows<D, false>;
-    const int row_per = (std::min(a.few, row_block) + kRows - 1) / kRows;
+    const int row_per = (a.few + kRows - 1) / kRows;
     const long long rows = a.meta ? (long long)a.n_wg * row_per : 0;
     const long long tiles =
         a.splits > 1 ? a.tile_wgs / a.splits * (kPagedTileRows / kSumRows<D, true>) : 0;

@@ -47,7 +47,7 @@ const char* check(const Call& c, bool planted, bool memory = true) {
         if (x.lo < 0 || x.kv < 0 || x.kv > max_keys) return "keys outside the table";
         const long long rows = (long long)x.qn * a.group;
         if (l.n_wg) {
-            const Share s = share_of(a, x, l.block, 32 * l.waves);
+            const Share s = share_of(a, x, 32 * l.waves);
             if (rows > l.few ? s.items != 0 : s.items < (rows > 0)) return "a request of nobody's";
             if (s.items && !l.shared && s.units != 1)
                 return "an item of several units, and no memory for parts";

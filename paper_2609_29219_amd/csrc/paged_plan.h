@@ -142,12 +142,13 @@ inline PagedLaunch paged_launch(int T, int R, int Hq, int Hkv, int d, int max_q,
         // steps of a request at most (its tokens are no more than its rows)
         double steps = (double)max_keys / kPagedRowKeys + 1;
         if (window) steps = std::min(steps, ((double)window + l.few) / kPagedRowKeys + 2);
-        const double items = ((double)rows / l.block + R) * Hkv;  // at most
+        const double items = (double)R * Hkv;
         // Few steps to every item: each is one workgroup's.  An item's steps one behind another
         // cost about 1 us each, adding up its parts a launch of 5 us.  Items no more than CUs:
         // workgroups of twice the waves have half the steps.  Measured: a token over 512 keys of
         // 8 heads, by four waves 11.0 us, by eight, as chosen, 9.7; over 1000 keys shared 13.0,
-        // whole, as chosen, 13.5; sixteen tokens over 950 keys shared 22, whole, as chosen, 19.
+        // whole, as chosen, 13.5; sixteen tokens over 950 keys shared 22, whole, as chosen, 19;
+        // 28 over 900 keys by four waves, shared, 26.5, by eight, as chosen, 22.5.
         if (items <= num_cus) l.waves = 8;
         l.shared = steps > (l.waves == 8 ? 9 : 6);
         if (l.shared)

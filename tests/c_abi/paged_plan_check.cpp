@@ -57,6 +57,9 @@ const char* check(const Call& c, bool planted, bool memory = true) {
     }
     if (units > 2147483647) return "more units than a 32-bit number holds";
     if (c.right && l.items && blocks * c.Hkv > l.items) return "blocks without a workgroup";
+    // items are requests' heads: no more than CUs, and short enough, they get eight waves
+    if (l.n_wg && (long long)c.R * c.Hkv <= 256 && max_keys <= 8 * 128 && l.waves != 8)
+        return "four waves to few items";
     if (l.n_wg && (l.few > l.block || l.n_wg < 1)) return "requests of more rows than a block";
     return nullptr;
 }

@@ -90,9 +90,11 @@ struct PagedRequest {
 };
 
 // Keys to a step of the row kernel (with four waves), and its workgroups that a compute unit holds
-// at once.
+// at once: as many as share the work of a call, since one more would have its part alone at the
+// end.  (By LDS at d = 64 with 16 rows and at d = 128, by registers at d = 64 with 32 rows, of
+// which 32 times 8 over 4096 keys take 61 us by three, by four 70.)
 constexpr int kPagedRowKeys = 128;
-constexpr int paged_row_wgs_per_cu(int d) { return d == 64 ? 4 : 2; }
+constexpr int paged_row_wgs_per_cu(int d, int block) { return d == 128 ? 2 : block == 16 ? 4 : 3; }
 constexpr int kPagedMeta = 8;  // ints to a workgroup
 constexpr int kPagedMaxGroup = 1 << 15;
 // Requests of up to this many rows are the row kernel's (by 16 or 32 rows), which streams

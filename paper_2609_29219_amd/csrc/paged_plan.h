@@ -138,7 +138,7 @@ inline PagedLaunch paged_launch(int T, int R, int Hq, int Hkv, int d, int max_q,
     if (tiles) plan_tiles(&l, R, rows, most, max_q > 0, Hkv, d, group, max_keys, window, num_cus);
     if (l.few > 0) {
         l.block = most <= 16 ? 16 : 32;
-        l.n_wg = paged_row_wgs_per_cu(d) * num_cus;
+        l.n_wg = paged_row_wgs_per_cu(d, l.block) * num_cus;
         // steps of a request at most (its tokens are no more than its rows)
         double steps = (double)max_keys / kPagedRowKeys + 1;
         if (window) steps = std::min(steps, ((double)window + l.few) / kPagedRowKeys + 2);

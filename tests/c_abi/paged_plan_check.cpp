@@ -1,7 +1,8 @@
 // Host-only check of how paged attention shares out its work (csrc/paged_plan.h): what the host
 // plans from the sizes against what the kernels find from the lengths, also where the lengths are
 // wrong.  Built and run by tests/test_paged_plan.py, under sanitizers; with --planted items that
-// stay whole are counted in units of four steps, and it has to catch that.
+// stay whole are counted in units of four steps, and it has to catch that; with --resident it says
+// how many workgroups of the row kernel the plan takes to be on a compute unit.
 #include <stdio.h>
 #include <string.h>
 
@@ -68,6 +69,12 @@ const char* check(const Call& c, bool planted, bool memory = true) {
 
 int main(int argc, char** argv) {
     const bool planted = argc > 1 && !strcmp(argv[1], "--planted");
+    if (argc > 1 && !strcmp(argv[1], "--resident")) {
+        for (int d : {64, 128})
+            for (int block : {16, 32})
+                printf("%d %d %d\n", d, block, paged_row_wgs_per_cu(d, block));
+        return 0;
+    }
     // single tokens in a window, the last bound far past the queries
     Call far = {16, 16, 32, 8, 128, 1, 4, 1250, 512, {}, {}, false};
     for (int r = 0; r <= 16; ++r) far.cu.push_back(r == 16 ? 20016 : r);

@@ -102,7 +102,8 @@ __device__ __forceinline__ PagedFound paged_find(const PagedArgs& a, int nth, in
         const int mine = r < a.R ? count(paged_request(a, r)) : 0;
         int all;
         const int at = before + block_scan<NT>(mine, &all) - mine;
-        if (nth < before + all) {
+        // (bounds that overlap: up to 2^31 blocks of these requests, behind fewer than 2^31)
+        if ((uint32_t)nth < (uint32_t)before + (uint32_t)all) {
             if (nth >= at && nth < at + mine) {
                 found[0] = r;
                 found[1] = at;

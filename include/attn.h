@@ -509,8 +509,9 @@ int attn_paged_store(const attn_heads* k, const attn_heads* v, const int* slots,
  * A token that sees no key (kv_len 0, or fewer tokens than new ones) has o = 0, lse = -inf.
  *   max_q: no request has more new tokens than this (0: not known).  Results of one that
  *   has are not defined, and may be left unwritten.
- * Of the cache only the rows that some token of the request sees are read; keys and values of
- * one request's own tokens that a mask hides from others of its tokens have to be finite.  A
+ * Of the cache only the aligned runs of eight rows that hold one that some token of the request
+ * sees are read, and what no token sees may be anything; keys and values of one request's own
+ * tokens that a mask hides from others of its tokens have to be finite.  A
  * page number outside [0, n_pages) makes NaN the results of the tokens that see a key in it, and
  * may do so with others of the request; a kv_len of more than the table's row holds makes all of
  * the request's NaN.  Neither reads anything outside the cache.

@@ -29,9 +29,14 @@
 // workgroups have a few steps each, their start (3 us) and the adding up (4 us) count: 16 tokens
 // over 73k keys of 8 heads 55 us, 5.4 TB/s; one over 512 keys 9 us.
 //
-// Only keys in [lo, kv) are read, lo being the first that any of the request's tokens sees; rows
-// of a tile outside it are copies of its first or last key with weight 0.  A page number outside
-// the cache is replaced by 0 and makes the request's results NaN.
+// Only the aligned runs of eight rows that hold a key in [lo, kv) are read, lo being the first that
+// any of the request's tokens sees: a run past these is the nearest of them again.  The scores of
+// keys outside [lo, kv) are masked, and their rows of V become zeros in LDS, whatever the page
+// holds there.  A page number outside the cache is replaced by 0 and makes the request's results
+// NaN.
+//
+// The scalars of a workgroup's share, of its item and of both descriptors are more than there are
+// scalar registers: 76 to 86 of them lie in lanes of a vector register, most through the loop.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

@@ -323,7 +323,7 @@ __global__ __launch_bounds__(512, 2) void paged_tiles_kernel(const PagedArgs a) 
             xe[pp][0] = weight(s_cur[kb][e], m_ref);
             xe[pp][1] = weight(s_cur[kb][e + 1], m_ref);
         };
-        // P is rounded to bf16 (2^-9 of each weight) as the operand it has to be
+        // P is rounded to bf16 (at most 2^-8 of each weight) as the operand it has to be
         auto round_sum = [&](int pp) __attribute__((always_inline)) {
             const int kb = pp / 8, h2 = (pp / 4) % 2, e = 2 * (pp % 4);
             const bf16x2 pk = {(__bf16)xe[pp][0], (__bf16)xe[pp][1]};

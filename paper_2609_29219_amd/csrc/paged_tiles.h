@@ -14,7 +14,7 @@
 // products of S of the next tile and of PV of this one one by one, with the softmax of this tile
 // between them; while it does, the next tiles come from memory straight into LDS (two slots to
 // an operand, one barrier to a tile).  A prompt of 8192 tokens, 32 heads of 128: 490 us, 1120
-// TFLOP/s; the same over contiguous keys, by attn_fwd, 466.  A chunk of 512 tokens over 16384
+// TFLOP/s (535 on a slower card); the same over contiguous keys, by attn_fwd, 466.  A chunk of 512 tokens over 16384
 // keys, 32 query heads to 8: 129 us.  (Four waves to a block of 128 rows load each tile twice as
 // often: 64 requests of 40 rows over 8192 keys 94 us, so 67.  With the weights' sums on the matrix
 // cores, as in fwd_kernel.h, the prompt takes the same time, at d = 64 2% less.)

@@ -101,10 +101,11 @@ def test_many_steps_short_of_pages(pa):
     assert short > 5
 
 
-def test_replayed_release(pa):
-    # one captured call, holes in some replays and none in others
-    announce("paged_release in a graph")
-    R, page, most = 70, 16, 400
+@pytest.mark.parametrize("R", [70, 300])
+def test_replayed_release(pa, R):
+    # one captured call, of one launch or two, holes in some replays and none in others
+    announce(f"paged_release in a graph R={R}")
+    page, most = 16, 400
     rng = random.Random(6)
     seq, keep = ints([most * page] * R), ints([16 * (i % 3) for i in range(R)])
     free, n_free = torch.zeros(R * most + 4, dtype=I32, device=DEV), ints([2])
